@@ -395,6 +395,100 @@ int ampq_select_in_order(int L, const int *order, const double *d_low, const dou
 int ampq_score_segment_noalloc(int device, void *cuda_stream, int dtype, int fmt, const void *values,
                                const void *grads, long long numel, float amax, double *dev_out);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit activation checkpoints.  The memory a calibration pass needs beyond the
+ * model is mostly the activations kept for the backward pass (Sec. 1): the
+ * inputs of the linear layers and of the norms.  These calls keep them in 8
+ * bits and use them from there.
+ *
+ * Format.  A matrix of `rows` x `cols` elements is stored row by row in groups
+ * of AMPQ_CKPT_GROUP consecutive columns (the last one may be shorter):
+ *   a    = max |x| over the group,
+ *   e    = the smallest integer with fmax * 2^e >= a, kept in [-110, 119] (E4M3)
+ *          or [-110, 112] (E5M2); 0 when a = 0,
+ *   code = RNE saturating FP8 cast of x * 2^-e,   scale byte = e + 127.
+ * Decoded: code * 2^e, exactly a bf16 number.  A group that holds an Inf or a
+ * NaN has scale byte 255 and codes 0, and decodes to NaN as a whole.
+ *   codes   one byte per element, rows ld_codes bytes apart; 16-byte aligned,
+ *           ld_codes a multiple of 16 and at least cols rounded up to whole
+ *           groups.  The columns behind the last of a row's last group are
+ *           written as 0; bytes further right are left alone.
+ *   scales  one byte per group, rows ld_scales bytes apart, ld_scales at least
+ *           the number of groups; no alignment.
+ * A reader takes codes and scales as ampq_ckpt_pack or ampq_norm_forward wrote
+ * them; other bytes give unspecified values, never a fault.
+ *
+ * All calls below take the device and a cudaStream_t on it (0 = the default
+ * stream), are asynchronous on that stream, allocate nothing, keep nothing
+ * between calls, and may be captured into a graph.  Pointers are device
+ * pointers.  A matrix has rows `ld` elements apart (ld >= its columns); base and
+ * row pitch aligned to 16 bytes give the vectorised path, anything aligned to
+ * the element is right through a slower one.  rows = 0 and cols = 0 are
+ * allowed.  Outputs must not overlap inputs or each other.  Sums and statistics
+ * are held in fp32 and added in an order fixed by the sizes and the device:
+ * results are reproducible run to run.  A workspace is the caller's, 256-byte
+ * aligned, at least as large as the query says for the same arguments, and free
+ * again when the work on the stream has finished: calls that may overlap on the
+ * GPU need one each.  Sizes: rows (all samples together) up to 2^31 - 1, columns
+ * up to 2^30 - 1, AMPQ_ERR_TOO_LARGE beyond. */
+#define AMPQ_CKPT_GROUP 32
+
+/* Writes the checkpoint of `values` in format `fmt` (AMPQ_FMT_E4M3 or
+ * AMPQ_FMT_E5M2). */
+int ampq_ckpt_pack(int device, void *cuda_stream, int dtype, int fmt, const void *values, long long rows, long long cols, long long ld,
+                   unsigned char *codes, long long ld_codes, unsigned char *scales, long long ld_scales);
+
+/* Writes the decoded values of a checkpoint as `dtype` (both types hold them
+ * exactly). */
+int ampq_ckpt_unpack(int device, void *cuda_stream, int dtype, int fmt, const unsigned char *codes, long long ld_codes,
+                     const unsigned char *scales, long long ld_scales, long long rows, long long cols, void *dev_out, long long ld);
+
+/* Weight gradient of a linear layer Y = X W^T + b from the checkpoint of its
+ * input, sample by sample (the per-sample gradient of Sec. 2.2):
+ *   gw[r][k][c] = sum_n gy[r][n][k] * x[r][n][c],   gb[r][k] = sum_n gy[r][n][k],
+ * r < samples, n < rows, k < outs, c < cols.  samples = 1 with all rows is the
+ * gradient of the whole batch.
+ *   gy      [samples * rows, outs] of `dtype`, rows ld_gy elements apart
+ *   codes, scales   checkpoint of [samples * rows, cols]
+ *   gw      [samples, outs, cols] of `dtype`, contiguous
+ *   gb      [samples, outs] of `dtype`, contiguous, or NULL
+ * rows = 0 gives zeros.  Products are exact, sums are fp32, one rounding to
+ * `dtype` at the end.  The workspace query takes the same gy (only its alignment
+ * matters), and bias = 1 if gb will be asked for. */
+int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void *gy, long long ld_gy, long long samples, long long rows,
+                                    long long cols, long long outs, int bias, long long *bytes);
+int ampq_ckpt_weight_grad(int device, void *cuda_stream, int dtype, int fmt, const void *gy, long long ld_gy, const unsigned char *codes,
+                          long long ld_codes, const unsigned char *scales, long long ld_scales, long long samples, long long rows,
+                          long long cols, long long outs, void *gw, void *gb, void *workspace, long long workspace_bytes);
+
+/* The norms of a transformer block over the columns of each row, up to
+ * AMPQ_NORM_MAX_COLS of them (AMPQ_ERR_TOO_LARGE beyond):
+ *   LAYER  y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(var + eps), var the mean of (x - mean)^2
+ *   RMS    y = x * rstd * weight, rstd = 1 / sqrt(mean of x^2 + eps)
+ * weight, bias: `param_dtype`, cols elements, each may be NULL (1 and 0; bias is
+ * LAYER only).  mean (LAYER only) and rstd: fp32, one per row, kept for the
+ * backward pass.  fmt = AMPQ_FMT_E4M3 or AMPQ_FMT_E5M2 also writes the
+ * checkpoint of x in the same read; AMPQ_FMT_BASE does not (codes and scales are
+ * ignored). */
+enum { AMPQ_NORM_LAYER = 0, AMPQ_NORM_RMS = 1 };
+#define AMPQ_NORM_MAX_COLS 16384
+int ampq_norm_forward(int device, void *cuda_stream, int kind, int dtype, int param_dtype, int fmt, const void *x, long long ld_x,
+                      long long rows, long long cols, const void *weight, const void *bias, float eps, void *y, long long ld_y,
+                      float *mean, float *rstd, unsigned char *codes, long long ld_codes, unsigned char *scales, long long ld_scales);
+
+/* Backward pass of the norms.  With h = (x - mean) * rstd and t = gy * weight:
+ *   LAYER  gx = rstd * (t - mean_c(t) - h * mean_c(t * h)),  gweight = sum_n gy * h,  gbias = sum_n gy
+ *   RMS    gx = rstd * (t - h * mean_c(t * h)),              gweight = sum_n gy * h
+ * x: the input itself (fmt = AMPQ_FMT_BASE) or its checkpoint in `fmt` (x is
+ * ignored then); mean and rstd as the forward pass left them.  gweight, gbias:
+ * `param_dtype`, cols elements, NULL where not wanted (gbias needs gweight).  The
+ * workspace is needed when gweight is. */
+int ampq_norm_backward_workspace(int device, long long rows, long long cols, long long *bytes);
+int ampq_norm_backward(int device, void *cuda_stream, int kind, int dtype, int param_dtype, int fmt, const void *gy, long long ld_gy,
+                       const void *x, long long ld_x, const unsigned char *codes, long long ld_codes, const unsigned char *scales,
+                       long long ld_scales, long long rows, long long cols, const float *mean, const float *rstd, const void *weight,
+                       void *gx, long long ld_gx, void *gweight, void *gbias, void *workspace, long long workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

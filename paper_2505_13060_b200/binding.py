@@ -23,6 +23,8 @@ LINEAR, BGEMM = 0, 1
 D_MODEL, D_MEASURED = 0, 1
 MEM_DEVICE, MEM_HOST = 0, 1
 SCALE_AMAX, SCALE_POW2 = 0, 1
+NORM_LAYER, NORM_RMS = 0, 1
+CKPT_GROUP, NORM_MAX_COLS = 32, 16384
 
 OK = 0
 ERR_INVALID, ERR_ALIGN, ERR_STATE, ERR_CUDA = -1, -2, -3, -4
@@ -39,6 +41,8 @@ EXPORTS = [
     "ampq_partition", "ampq_gain_table", "ampq_select_in_order",
     "ampq_set_scale_mode", "ampq_measure_amax", "ampq_get_amax", "ampq_set_causal", "ampq_set_measured",
     "ampq_set_sharing", "ampq_get_pass_bytes", "ampq_merge_sample_tables", "ampq_get_layer_table", "ampq_last_tile_shift",
+    "ampq_ckpt_pack", "ampq_ckpt_unpack", "ampq_ckpt_weight_grad_workspace", "ampq_ckpt_weight_grad",
+    "ampq_norm_forward", "ampq_norm_backward_workspace", "ampq_norm_backward",
 ]
 NOALLOC_MAX_NUMEL = 2147483648
 
@@ -106,6 +110,13 @@ def lib():
     L.ampq_select.argtypes = [vp, i, C.c_double, vp, dp, dp]
     L.ampq_select_tables.argtypes = [i, vp, vp, vp, vp, C.c_double, vp, dp, dp]
     L.ampq_score_segment_noalloc.argtypes = [i, vp, i, i, vp, vp, ll, C.c_float, vp]
+    L.ampq_ckpt_pack.argtypes = [i, vp, i, i, vp, ll, ll, ll, vp, ll, vp, ll]
+    L.ampq_ckpt_unpack.argtypes = [i, vp, i, i, vp, ll, vp, ll, ll, ll, vp, ll]
+    L.ampq_ckpt_weight_grad_workspace.argtypes = [i, i, vp, ll, ll, ll, ll, ll, i, C.POINTER(ll)]
+    L.ampq_ckpt_weight_grad.argtypes = [i, vp, i, i, vp, ll, vp, ll, vp, ll, ll, ll, ll, ll, vp, vp, vp, ll]
+    L.ampq_norm_forward.argtypes = [i, vp, i, i, i, i, vp, ll, ll, ll, vp, vp, C.c_float, vp, ll, vp, vp, vp, ll, vp, ll]
+    L.ampq_norm_backward_workspace.argtypes = [i, ll, ll, C.POINTER(ll)]
+    L.ampq_norm_backward.argtypes = [i, vp, i, i, i, i, vp, ll, vp, ll, vp, ll, vp, ll, ll, ll, vp, vp, vp, vp, ll, vp, vp, vp, ll]
     for name in EXPORTS:
         if name not in ("ampq_strerror", "ampq_last_error"):
             getattr(L, name).restype = i

@@ -12,8 +12,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libampq.so")
-SOURCES = ["ampq_kernels.cu", "ampq_lib.cu", "ampq_noalloc.cu", "ampq_select.cpp", "ampq_graph.cpp"]
-HEADERS = ["ampq_device.h", "ampq_kernels.h", "ampq_select.h", os.path.join("..", "..", "include", "ampq.h")]
+SOURCES = ["ampq_kernels.cu", "ampq_lib.cu", "ampq_noalloc.cu", "ampq_select.cpp", "ampq_graph.cpp",
+           "ampq_ckpt.cu", "ampq_norm.cu", "ampq_wgrad.cu"]
+HEADERS = ["ampq_device.h", "ampq_kernels.h", "ampq_select.h", "ampq_ckpt.h", os.path.join("..", "..", "include", "ampq.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -44,9 +45,20 @@ def build(force: bool = False, verbose: bool = False, out: str | None = None, de
         return LIB
     tmp = lib + ".tmp.%d" % os.getpid()
     cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-D" + d for d in defines]
-    cmd += ["-shared", "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.check_call(cmd)
-    os.replace(tmp, lib)
+    objs = ["%s.%s.o" % (tmp, s) for s in SOURCES]
+    try:
+        # one compiler per source, side by side; all are waited for before the first failure is raised
+        jobs = [subprocess.Popen(cmd + ["-c", "-o", o, os.path.join(CSRC, s)]) for s, o in zip(SOURCES, objs)]
+        codes = [j.wait() for j in jobs]
+        for s, rc in zip(SOURCES, codes):
+            if rc:
+                raise subprocess.CalledProcessError(rc, "nvcc " + s)
+        subprocess.check_call(cmd + ["-shared", "-o", tmp] + objs)
+        os.replace(tmp, lib)
+    finally:
+        for path in objs + [tmp]:
+            if os.path.exists(path):
+                os.unlink(path)
     return lib
 
 

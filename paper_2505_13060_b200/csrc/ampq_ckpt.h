@@ -1,0 +1,271 @@
+// 8-bit checkpoints: the group format, and what the kernels that write or read
+// it share (ampq_ckpt.cu, ampq_norm.cu, ampq_wgrad.cu).
+//
+// A row of `cols` elements is stored in groups of 32 consecutive columns.  A
+// group has a power of two p = 2^e and one FP8 code per element:
+//   e    = the smallest integer with fmax * 2^e >= max|x|, kept in
+//          [kMinScaleExp, kMaxScaleExp]; 0 for a group of zeros,
+//   code = RNE_sat(x * 2^-e); scale byte = e + 127.
+// A power of two makes x * 2^-e exact (up to values far below the smallest
+// code) and code * 2^e exactly representable in bf16: 4 or 3 significant bits,
+// and the bounds on e keep the smallest code a normal bf16 (2^-9 * 2^-110 and
+// 2^-16 * 2^-110) and the largest one finite.  The products of the weight
+// gradient therefore see the stored values without a further rounding.
+// A group that holds an Inf or a NaN cannot be stored: its scale byte is 255,
+// its codes are 0, and it decodes to NaN as a whole.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/ampq.h"
+
+namespace ampq {
+
+constexpr int kGroup = 32;
+constexpr int kMinScaleExp = -110;
+constexpr unsigned kNanScale = 255;
+
+template <int FMT>
+struct Fp8;
+template <>
+struct Fp8<AMPQ_FMT_E4M3> {
+    static constexpr int kTopExp = 8;         // fmax = 1.75 * 2^8
+    static constexpr int kMaxScaleExp = 119;  // 1.75 * 2^127 is finite
+};
+template <>
+struct Fp8<AMPQ_FMT_E5M2> {
+    static constexpr int kTopExp = 15;  // fmax = 1.75 * 2^15
+    static constexpr int kMaxScaleExp = 112;
+};
+
+// Scale byte of a group from the bits of max|x| (an integer maximum of the
+// absolute values' bits, so an Inf or a NaN comes out on top).
+template <int FMT>
+__device__ __forceinline__ unsigned scale_byte(unsigned amax_bits) {
+    if (amax_bits >= 0x7F800000u) return kNanScale;
+    if (amax_bits == 0) return 127;
+    int e = (int)(amax_bits >> 23) - 127 - Fp8<FMT>::kTopExp + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    e = max(kMinScaleExp, min(Fp8<FMT>::kMaxScaleExp, e));
+    return (unsigned)(e + 127);
+}
+
+// 2^-e of a scale byte.  For the NaN byte any finite value: the caller stores codes 0.
+__device__ __forceinline__ float inv_scale_of(unsigned byte) { return __uint_as_float((byte == kNanScale ? 127u : 254u - byte) << 23); }
+
+// 2^e of a scale byte, NaN for the NaN byte.
+__device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte == kNanScale ? 0x7FC00000u : byte << 23); }
+
+// Eight scaled elements -> eight codes (element 0 in the lowest byte).
+template <int FMT>
+__device__ __forceinline__ uint2 encode8(const float (&y)[8]) {
+    unsigned short h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (FMT == AMPQ_FMT_E4M3)
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
+        else
+            asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
+    }
+    return make_uint2(h[0] | ((unsigned)h[1] << 16), h[2] | ((unsigned)h[3] << 16));
+}
+
+// Eight codes -> their exact values, not yet multiplied by the group's scale.
+template <int FMT>
+__device__ __forceinline__ void decode8(uint2 c, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned short h = (unsigned short)((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
+        unsigned r;
+        if (FMT == AMPQ_FMT_E4M3)
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(h));
+        else
+            asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(r) : "h"(h));
+        const float2 f = __half22float2(*reinterpret_cast<__half2*>(&r));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// eight consecutive elements of a row
+
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+    unsigned r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ float load_elem(const float* p) { return __ldg(p); }
+__device__ __forceinline__ float load_elem(const __nv_bfloat16* p) {
+    return __uint_as_float((unsigned)__ldg(reinterpret_cast<const unsigned short*>(p)) << 16);
+}
+__device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_elem(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// The raw bits of eight elements: what stays in registers between two uses.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    uint4 a, b;
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+        v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        a = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        b = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    }
+    __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldg(reinterpret_cast<const uint4*>(p));
+        b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+    }
+    __device__ __forceinline__ void store(float* p) const {
+        reinterpret_cast<uint4*>(p)[0] = a;
+        reinterpret_cast<uint4*>(p)[1] = b;
+    }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
+        v[4] = __uint_as_float(a.z << 16); v[5] = __uint_as_float(a.z & 0xFFFF0000u);
+        v[6] = __uint_as_float(a.w << 16); v[7] = __uint_as_float(a.w & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = a; }
+};
+
+// Loads `n` (<= 8) elements at p, zeros behind them; VEC: p is 16-byte aligned.
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(Raw8<T>& r, const T* p, int n) {
+    if (VEC && n == 8) {
+        r.load(p);
+        return;
+    }
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? load_elem(p + i) : 0.0f;
+    r.set(v);  // exact: the values come from this type
+}
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(const Raw8<T>& r, T* p, int n) {
+    if (VEC && n == 8) {
+        r.store(p);
+        return;
+    }
+    float v[8];
+    r.values(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) store_elem(p + i, v[i]);
+}
+
+// Largest absolute value's bits of eight elements.
+__device__ __forceinline__ unsigned amax_bits8(const float (&v)[8]) {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+
+// Encodes eight elements whose group's scale byte is known.
+template <int FMT>
+__device__ __forceinline__ uint2 encode_group8(const float (&v)[8], unsigned byte) {
+    const float inv = inv_scale_of(byte);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = v[i] * inv;
+    const uint2 c = encode8<FMT>(y);
+    return byte == kNanScale ? make_uint2(0, 0) : c;
+}
+
+// ---------------------------------------------------------------------------
+// host side
+
+struct CkptDevice {  // makes `device` current for the life of the object
+    int prev = -1;
+    int status = AMPQ_OK;
+    explicit CkptDevice(int dev) {
+        int n = 0;
+        if (cudaGetDeviceCount(&n) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            status = AMPQ_ERR_CUDA;
+            return;
+        }
+        if (dev < 0 || dev >= n) {
+            status = AMPQ_ERR_INVALID;
+            return;
+        }
+        if (cudaGetDevice(&prev) != cudaSuccess) {
+            cudaGetLastError();
+            prev = -1;
+            status = AMPQ_ERR_CUDA;
+            return;
+        }
+        if (prev == dev)
+            prev = -1;
+        else if (cudaSetDevice(dev) != cudaSuccess) {
+            cudaGetLastError();
+            status = AMPQ_ERR_CUDA;
+        }
+    }
+    ~CkptDevice() {
+        if (prev >= 0) cudaSetDevice(prev);
+    }
+};
+
+inline int launched() {
+    if (cudaGetLastError() != cudaSuccess) return AMPQ_ERR_CUDA;
+    return AMPQ_OK;
+}
+
+inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline size_t elem_bytes(int dtype) { return dtype == AMPQ_F32 ? 4 : 2; }
+inline bool known_dtype(int dtype) { return dtype == AMPQ_F32 || dtype == AMPQ_BF16; }
+inline bool known_fp8(int fmt) { return fmt == AMPQ_FMT_E4M3 || fmt == AMPQ_FMT_E5M2; }
+// rows of ld elements can be read 16 bytes at a time
+inline bool rows_aligned(const void* p, long long ld, int dtype) { return aligned_to(p, 16) && (ld * (long long)elem_bytes(dtype)) % 16 == 0; }
+
+constexpr long long kMaxRows = 0x7FFFFFFFLL;
+constexpr long long kMaxCols = 0x3FFFFFFFLL;
+
+// Arguments of a matrix whose rows lie ld elements apart.
+inline int check_matrix(const void* p, long long rows, long long cols, long long ld, int dtype) {
+    if (rows < 0 || cols < 0 || ld < cols) return AMPQ_ERR_INVALID;
+    if (rows > 0 && cols > 0 && !p) return AMPQ_ERR_INVALID;
+    if (rows > kMaxRows || cols > kMaxCols || ld > (1LL << 40)) return AMPQ_ERR_TOO_LARGE;
+    if (!aligned_to(p, elem_bytes(dtype))) return AMPQ_ERR_ALIGN;
+    return AMPQ_OK;
+}
+
+// Arguments of a checkpoint of rows x cols elements.
+inline int check_ckpt(const unsigned char* codes, long long ld_codes, const unsigned char* scales, long long ld_scales, long long rows,
+                      long long cols) {
+    const long long groups = (cols + kGroup - 1) / kGroup;
+    if (ld_codes < groups * kGroup || ld_scales < groups) return AMPQ_ERR_INVALID;
+    if (rows > 0 && cols > 0 && (!codes || !scales)) return AMPQ_ERR_INVALID;
+    if (ld_codes > (1LL << 40) || ld_scales > (1LL << 40)) return AMPQ_ERR_TOO_LARGE;
+    if (ld_codes % 16 || !aligned_to(codes, 16)) return AMPQ_ERR_ALIGN;
+    return AMPQ_OK;
+}
+
+int sm_count(int device);  // multiprocessors of a device, 0 on error
+
+// Sums `parts` fp32 partial rows of `cols` columns in a fixed order and stores
+// them in `dtype`: out[b][c] = sum_p part[b][p][c], `batches` of them.  With
+// `second` (two batches) batch 1 goes there.
+int launch_join_columns(const float* part, long long batches, int parts, long long cols, void* out, void* second, int dtype, cudaStream_t st);
+
+}  // namespace ampq
