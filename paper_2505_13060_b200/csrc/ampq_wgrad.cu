@@ -28,7 +28,7 @@ constexpr int kCtaCols = 128;                 // checkpoint columns (c) of one C
 constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
 constexpr int kStages = 6;
-constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kEpilogueWarp = 4, kDecodeWarp = 8;
+constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kRelayWarp = 3, kEpilogueWarp = 4, kDecodeWarp = 8;
 constexpr int kEpilogueWarps = 4, kDecodeWarps = 8;
 constexpr int kThreads = 32 * (kDecodeWarp + kDecodeWarps);
 constexpr int kSmemBytes = kStages * 2 * kTileBytes + 1024 + 512;
@@ -50,25 +50,39 @@ __device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)_
 __device__ __forceinline__ void mbar_init(unsigned bar, unsigned count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
+// One poll of a phase.  CLUSTER: the arrivals came from another CTA.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_poll(unsigned bar, unsigned parity, unsigned hint_ns) {
     unsigned ok;
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-        "selp.u32 %0, 1, 0, p;\n"
-        "}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(hint_ns)
-        : "memory");
+    if (CLUSTER)
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
+            "selp.u32 %0, 1, 0, p;\n"
+            "}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(hint_ns)
+            : "memory");
+    else
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+            "selp.u32 %0, 1, 0, p;\n"
+            "}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(hint_ns)
+            : "memory");
     return ok != 0;
 }
 // Waits for a phase; false when the limit runs out or the CTA has given up.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatile int* gave_up) {
-    if (mbar_poll(bar, parity, kWaitHintNs)) return true;
+    if (mbar_poll<CLUSTER>(bar, parity, kWaitHintNs)) return true;
     for (unsigned i = 0; i < kWaitPolls; ++i) {
         if (*gave_up) return false;
-        if (mbar_poll(bar, parity, kWaitHintNs)) return true;
+        if (mbar_poll<CLUSTER>(bar, parity, kWaitHintNs)) return true;
     }
     *gave_up = 1;
     return false;
@@ -82,6 +96,9 @@ __device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {
     unsigned r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+__device__ __forceinline__ void mbar_arrive(unsigned bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
@@ -272,9 +289,14 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
 // accumulators.  CG = 1: one 128 x 128 tile per CTA.  Two accumulators, so that a
 // tile is stored while the next one is computed.
 //
-// Barriers, per stage: `loaded` (gY has landed, own CTA), `ready` (both operands
-// are in place in all CTAs; held by the first CTA), `empty` (the products that
-// read the stage are done).  Per accumulator: `filled`, `drained`.
+// Barriers, per stage: `loaded` (gY has landed), `decoded` (X^ is written), both
+// for the own CTA; `peer` (both are in place in the pair's second CTA; held by the
+// first); `empty` (the products that read the stage are done).  Per accumulator:
+// `filled`, `drained`.  One warp of the second CTA passes its `loaded` and
+// `decoded` on to `peer`: an arrival in another CTA has to release at cluster
+// scope, which waits for the arriving thread's memory operations, and the decoding
+// warps always have loads in flight (arriving there themselves they ran at a
+// third of the speed).
 //
 // A wait that runs out raises the CTA's flag; its threads then leave their loops,
 // the copies and products in flight are waited for, and what was not stored yet
@@ -282,7 +304,7 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
 template <int CG, int FMT, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map, const WgradArgs a) {
     extern __shared__ unsigned char raw_smem[];
-    __shared__ alignas(8) unsigned long long s_bars[3 * kStages + 5];
+    __shared__ alignas(8) unsigned long long s_bars[4 * kStages + 5];
     __shared__ unsigned s_tmem;
     __shared__ int s_gave_up;
     constexpr int kTileOuts = CG * kCtaOuts, kTileCols = CG * kCtaCols;
@@ -294,17 +316,19 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
     const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes;
     const unsigned bars = smem_u32(s_bars);
     auto loaded = [&](unsigned s) { return bars + 8 * s; };
-    auto ready = [&](unsigned s) { return bars + 8 * (kStages + s); };
-    auto empty = [&](unsigned s) { return bars + 8 * (2 * kStages + s); };
-    auto filled = [&](unsigned k) { return bars + 8 * (3 * kStages + k); };
-    auto drained = [&](unsigned k) { return bars + 8 * (3 * kStages + 2 + k); };
-    const unsigned finished = bars + 8 * (3 * kStages + 4);
+    auto decoded = [&](unsigned s) { return bars + 8 * (kStages + s); };
+    auto peer = [&](unsigned s) { return bars + 8 * (2 * kStages + s); };
+    auto empty = [&](unsigned s) { return bars + 8 * (3 * kStages + s); };
+    auto filled = [&](unsigned k) { return bars + 8 * (4 * kStages + k); };
+    auto drained = [&](unsigned k) { return bars + 8 * (4 * kStages + 2 + k); };
+    const unsigned finished = bars + 8 * (4 * kStages + 4);
     volatile int* gave_up = &s_gave_up;
 
     if (threadIdx.x == 0) {
         for (unsigned s = 0; s < kStages; ++s) {
             mbar_init(loaded(s), 1);
-            mbar_init(ready(s), CG * kDecodeWarps);
+            mbar_init(decoded(s), kDecodeWarps);
+            mbar_init(peer(s), 1);
             mbar_init(empty(s), 1);
         }
         for (unsigned k = 0; k < 2; ++k) {
@@ -372,11 +396,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             bool ok = true;
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
-                ok = mbar_wait(drained(acc), acc_parity ^ 1, gave_up);
+                ok = mbar_wait<CG == 2>(drained(acc), acc_parity ^ 1, gave_up);
                 if (!ok) break;
                 fence_tcgen05_after();
                 for (int step = p.first_step; step < p.last_step; ++step) {
-                    ok = mbar_wait(ready(stage), parity, gave_up);
+                    ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(decoded(stage), parity, gave_up);
+                    if (CG == 2) ok = ok && mbar_wait<true>(peer(stage), parity, gave_up);
                     if (!ok) break;
                     fence_tcgen05_after();
                     const unsigned long long da = operand_desc(tiles_a + stage * kTileBytes), db = operand_desc(tiles_b + stage * kTileBytes);
@@ -397,6 +422,22 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             // every product has finished before the memory it reads and writes is given up
             asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(finished), "n"(CG) : "memory");
             mbar_drain(finished, 0);
+        }
+    } else if (warp == kRelayWarp) {
+        if (CG == 2 && rank == 1 && lane == 0) {
+            unsigned stage = 0, parity = 0;
+            bool ok = true;
+            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
+                const TilePos p(a, t);
+                for (int step = p.first_step; step < p.last_step && ok; ++step) {
+                    ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(decoded(stage), parity, gave_up);
+                    if (ok) mbar_arrive_cluster(in_cta(peer(stage), 0));
+                    if (++stage == kStages) {
+                        stage = 0;
+                        parity ^= 1;
+                    }
+                }
+            }
         }
     } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
         const unsigned quarter = warp - kEpilogueWarp;  // TMEM lanes 32 * quarter .. + 31 are this warp's
@@ -442,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
         walk.stride = tile_stride;
         walk.rank = rank;
         walk.open(a, c16);
-        constexpr int kAhead = 2;
+        constexpr int kAhead = 3;
         CodeRow buf[kAhead][2];
         bool have[kAhead];
 #pragma unroll
@@ -474,20 +515,18 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + first), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + second), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(decoded(stage));
+                if (++stage == kStages) {
+                    stage = 0;
+                    parity ^= 1;
+                }
+                // behind the fence, which would wait for loads in flight
                 have[b] = walk.more(a);
                 if (have[b]) {
                     walk.load(a, row, buf[b]);
                     walk.next(a, c16);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                // the first decoding warp also vouches for the stage's gradient tile
-                if (warp == kDecodeWarp) ok = mbar_wait(loaded(stage), parity, gave_up);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (ok && lane == 0) mbar_arrive_cluster(CG == 2 ? in_cta(ready(stage), 0) : ready(stage));
-                if (++stage == kStages) {
-                    stage = 0;
-                    parity ^= 1;
                 }
             }
         }
