@@ -5,10 +5,10 @@
 // The product runs on the tensor cores (tcgen05, kind::f16, fp32 accumulators in
 // TMEM).  Its reduction axis is the token n, along which neither operand is
 // contiguous, so both are given to the tensor core "MN-major", 128-byte
-// swizzled.  gY comes in by TMA.  X^ is read as codes and scale bytes into
-// registers by eight warps, which write the bf16 values (exact, see ampq_ckpt.h)
-// into the same swizzled layout: 33/32 byte per element from HBM and L2 instead
-// of two, and no bf16 copy of X anywhere.
+// swizzled.  gY and the codes of X^ come in by TMA; eight warps widen the codes to
+// bf16 (exact, see ampq_ckpt.h) from shared memory into the same swizzled layout:
+// 33/32 byte per element of X from HBM and L2 instead of two, and no bf16 copy of
+// X in memory.
 //
 // fp32 gradients are first cut into three bf16 planes, g = g0 + g1 + g2 exactly
 // (24 significant bits), and the token axis walks all three: the products stay
@@ -27,11 +27,12 @@ constexpr int kCtaOuts = 128;                 // gradient columns (k) of one CTA
 constexpr int kCtaCols = 128;                 // checkpoint columns (c) of one CTA's stage
 constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
-constexpr int kStages = 6;
-constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kRelayWarp = 3, kEpilogueWarp = 4, kDecodeWarp = 8;
+constexpr int kCodeBytes = kStepRows * kCtaCols;  // the codes of one stage
+constexpr int kStages = 5;
+constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kEpilogueWarp = 4, kDecodeWarp = 8;
 constexpr int kEpilogueWarps = 4, kDecodeWarps = 8;
 constexpr int kThreads = 32 * (kDecodeWarp + kDecodeWarps);
-constexpr int kSmemBytes = kStages * 2 * kTileBytes + 1024 + 512;
+constexpr int kSmemBytes = kStages * (2 * kTileBytes + kCodeBytes) + 1024;
 
 // Polls of an mbarrier before a wait gives up.  A test build lets the waits
 // between the stages give up at once; the waits that drain copies and products
@@ -50,39 +51,25 @@ __device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)_
 __device__ __forceinline__ void mbar_init(unsigned bar, unsigned count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
-// One poll of a phase.  CLUSTER: the arrivals came from another CTA.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_poll(unsigned bar, unsigned parity, unsigned hint_ns) {
     unsigned ok;
-    if (CLUSTER)
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(hint_ns)
-            : "memory");
-    else
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(hint_ns)
-            : "memory");
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(hint_ns)
+        : "memory");
     return ok != 0;
 }
 // Waits for a phase; false when the limit runs out or the CTA has given up.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatile int* gave_up) {
-    if (mbar_poll<CLUSTER>(bar, parity, kWaitHintNs)) return true;
+    if (mbar_poll(bar, parity, kWaitHintNs)) return true;
     for (unsigned i = 0; i < kWaitPolls; ++i) {
         if (*gave_up) return false;
-        if (mbar_poll<CLUSTER>(bar, parity, kWaitHintNs)) return true;
+        if (mbar_poll(bar, parity, kWaitHintNs)) return true;
     }
     *gave_up = 1;
     return false;
@@ -101,7 +88,7 @@ __device__ __forceinline__ void mbar_arrive(unsigned bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void mbar_expect(unsigned bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -111,6 +98,11 @@ __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, u
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
         "l"(map), "r"(bar), "r"(k), "r"(n), "r"(r), "r"(plane)
         : "memory");
+}
+__device__ __forceinline__ void tma_load_codes(unsigned dst, const CUtensorMap* map, unsigned bar, int c, int n, int r) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(c), "r"(n), "r"(r)
+                 : "memory");
 }
 __device__ __forceinline__ void fence_tcgen05_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_tcgen05_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -171,12 +163,11 @@ __device__ __forceinline__ unsigned long long operand_desc(unsigned addr) {
 }
 
 struct WgradArgs {
-    const unsigned char *codes, *scales;
+    const unsigned char* scales;
     void* out;                                // gw, or fp32 partial sums [samples][splits][outs][cols]
-    long long ld_codes, ld_scales, cols, outs, rows;
+    long long ld_scales, cols, outs, rows;
     long long tiles;                          // (sample, split, k tile, c tile)
     int k_tiles, c_tiles, splits, steps_per_plane, steps, steps_per_split;
-    unsigned stored_cols;                     // columns that have codes: cols rounded up to whole groups
     bool vec;                                 // rows of the output start on 16-byte boundaries
 };
 
@@ -199,68 +190,79 @@ struct TilePos {
     }
 };
 
-// Sixteen codes on their way from memory to a stage.
-struct CodeRow {
-    uint4 q;
-    unsigned scale;  // byte, or 0 where there is nothing: decodes to 0
-};
-
-// Two codes (in the upper bytes of the halves of x) -> two bf16 values times
-// 2^-120 (E4M3) or 2^-112 (E5M2): exponent and mantissa fields moved into the
-// low end of bf16's, subnormal codes into bf16's subnormals.
-template <int FMT>
-__device__ __forceinline__ unsigned widen(unsigned x) {
-    return FMT == AMPQ_FMT_E4M3 ? ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u) : ((x >> 3) & 0x0FE00FE0u) | (x & 0x80008000u);
-}
 __device__ __forceinline__ unsigned mul_bf16x2(unsigned a, unsigned b) {
     unsigned r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 
-// Four codes -> four bf16 values: widen, times 2^120 (2^112): the code's own
-// value; times the group's scale.  Both products are exact.
+// Four codes -> four bf16 values, in the order 0, 2, 1, 3.  A code moved into the
+// upper byte of a 16-bit half and shifted right by four (three) has its exponent
+// and mantissa fields at the low end of bf16's, subnormal codes among bf16's
+// subnormals: the value times 2^-120 (E4M3) or 2^-112 (E5M2).  One exact product
+// with `unit` puts that and the group's scale right.
 template <int FMT>
-__device__ __forceinline__ uint2 decode4(unsigned w, unsigned scale2) {
-    constexpr unsigned kUnit = FMT == AMPQ_FMT_E4M3 ? (247u << 7) * 0x10001u : (239u << 7) * 0x10001u;
-    const unsigned lo = widen<FMT>(__byte_perm(w, 0, 0x1404)), hi = widen<FMT>(__byte_perm(w, 0, 0x3424));
-    return make_uint2(mul_bf16x2(mul_bf16x2(lo, kUnit), scale2), mul_bf16x2(mul_bf16x2(hi, kUnit), scale2));
+__device__ __forceinline__ uint2 widen4(unsigned w, unsigned unit) {
+    constexpr unsigned kField = FMT == AMPQ_FMT_E4M3 ? 0x07F007F0u : 0x0FE00FE0u;
+    constexpr int kShift = FMT == AMPQ_FMT_E4M3 ? 4 : 3;
+    const unsigned even = ((w << (8 - kShift)) & kField) | ((w << 8) & 0x80008000u);
+    const unsigned odd = ((w >> kShift) & kField) | (w & 0x80008000u);
+    return make_uint2(mul_bf16x2(even, unit), mul_bf16x2(odd, unit));
 }
 
-// The walk of one decoding thread over its cluster's stages, one row pair ahead.
+// Sixteen codes of one group -> two 16-byte pieces of a row.  byte: the scale, or
+// 0 where there is no row, which decodes to 0.
+template <int FMT>
+__device__ __forceinline__ void widen16(uint4 q, unsigned byte, uint4& lo, uint4& hi) {
+    const unsigned field = byte ? byte + (FMT == AMPQ_FMT_E4M3 ? 120u : 112u) : 0u;  // bf16 exponent field of the factor
+    const unsigned unit = (min(field, 254u) << 7) * 0x10001u;
+    const uint2 a = widen4<FMT>(q.x, unit), b = widen4<FMT>(q.y, unit), c = widen4<FMT>(q.z, unit), d = widen4<FMT>(q.w, unit);
+    lo = make_uint4(a.x, a.y, b.x, b.y);
+    hi = make_uint4(c.x, c.y, d.x, d.y);
+    if (field > 254u) {  // a scale above 2^7 (2^15): the factor is no bf16 number, its second part follows; NaN for the NaN byte
+        const unsigned rest = (byte == kNanScale ? 0x7FC0u : (field - 127u) << 7) * 0x10001u;
+        lo = make_uint4(mul_bf16x2(lo.x, rest), mul_bf16x2(lo.y, rest), mul_bf16x2(lo.z, rest), mul_bf16x2(lo.w, rest));
+        hi = make_uint4(mul_bf16x2(hi.x, rest), mul_bf16x2(hi.y, rest), mul_bf16x2(hi.z, rest), mul_bf16x2(hi.w, rest));
+    }
+}
+
+// The scale bytes of one decoding thread (rows n and n + 32 of a stage, one
+// group), stage by stage through all of its tiles.
 template <int CG>
-struct CodeWalk {
-    long long t, stride;
-    int step, last_step, sample;
-    long long col;
-    unsigned rank;
-    __device__ __forceinline__ void open(const WgradArgs& a, unsigned c16) {
+struct ScaleWalk {
+    long long t;
+    const unsigned char* p;
+    int step, last_step, plane_step;
+    long long n;
+    bool in;
+    __device__ __forceinline__ void open(const WgradArgs& a, long long tile, unsigned rank, unsigned row, unsigned c16) {
+        t = tile;
         if (t >= a.tiles) return;
-        const TilePos p(a, t);
-        step = p.first_step;
-        last_step = p.last_step;
-        sample = p.sample;
-        col = (long long)p.ct * (CG * kCtaCols) + rank * kCtaCols + c16 * 16;
+        const TilePos pos(a, t);
+        step = pos.first_step;
+        last_step = pos.last_step;
+        plane_step = step % a.steps_per_plane;
+        n = (long long)plane_step * kStepRows + row;
+        const long long col = (long long)pos.ct * (CG * kCtaCols) + rank * kCtaCols + c16 * 16;
+        in = col < a.cols;
+        p = a.scales + (pos.sample * a.rows + n) * a.ld_scales + col / kGroup;
     }
-    __device__ __forceinline__ bool more(const WgradArgs& a) const { return t < a.tiles; }
-    __device__ __forceinline__ void load(const WgradArgs& a, unsigned row, CodeRow (&out)[2]) {
-        const int n0 = step % a.steps_per_plane * kStepRows;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int n = n0 + (int)row + 32 * h;
-            out[h].q = make_uint4(0, 0, 0, 0);
-            out[h].scale = 0;
-            if (n < a.rows && col < (long long)a.stored_cols) {
-                const long long at = (long long)sample * a.rows + n;
-                out[h].q = __ldg(reinterpret_cast<const uint4*>(a.codes + at * a.ld_codes + col));
-                out[h].scale = __ldg(a.scales + at * a.ld_scales + col / kGroup);
-            }
+    __device__ __forceinline__ void fetch(const WgradArgs& a, unsigned (&byte)[2]) const {
+        byte[0] = in && n < a.rows ? __ldg(p) : 0u;
+        byte[1] = in && n + 32 < a.rows ? __ldg(p + 32 * a.ld_scales) : 0u;
+    }
+    __device__ __forceinline__ void next(const WgradArgs& a, long long tile_stride, unsigned rank, unsigned row, unsigned c16) {
+        if (++step == last_step) {
+            open(a, t + tile_stride, rank, row, c16);
+            return;
         }
-    }
-    __device__ __forceinline__ void next(const WgradArgs& a, unsigned c16) {
-        if (++step < last_step) return;
-        t += stride;
-        open(a, c16);
+        n += kStepRows;
+        p += kStepRows * a.ld_scales;
+        if (++plane_step == a.steps_per_plane) {  // the next plane of the gradient meets the same rows
+            plane_step = 0;
+            n = row;
+            p -= (long long)a.steps_per_plane * kStepRows * a.ld_scales;
+        }
     }
 };
 
@@ -292,17 +294,16 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
 // Barriers, per stage: `loaded` (gY has landed), `decoded` (X^ is written), both
 // for the own CTA; `peer` (both are in place in the pair's second CTA; held by the
 // first); `empty` (the products that read the stage are done).  Per accumulator:
-// `filled`, `drained`.  One warp of the second CTA passes its `loaded` and
-// `decoded` on to `peer`: an arrival in another CTA has to release at cluster
-// scope, which waits for the arriving thread's memory operations, and the decoding
-// warps always have loads in flight (arriving there themselves they ran at a
-// third of the speed).
+// `filled`, `drained`.  What the second CTA's warps wrote is read by the tensor
+// core alone, for which the proxy fence before their arrival makes it visible; the
+// arrival itself does not release at cluster scope, which would wait for every
+// load in flight (1.5 us a stage).
 //
 // A wait that runs out raises the CTA's flag; its threads then leave their loops,
 // the copies and products in flight are waited for, and what was not stored yet
 // becomes NaN.
 template <int CG, int FMT, typename OUT>
-__global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map, const WgradArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const WgradArgs a) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ alignas(8) unsigned long long s_bars[4 * kStages + 5];
     __shared__ unsigned s_tmem;
@@ -313,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
     unsigned rank = 0;
     if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const unsigned base = (smem_u32(raw_smem) + 1023u) & ~1023u;
-    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes;
+    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = base + 2 * kStages * kTileBytes;
     const unsigned bars = smem_u32(s_bars);
     auto loaded = [&](unsigned s) { return bars + 8 * s; };
     auto decoded = [&](unsigned s) { return bars + 8 * (kStages + s); };
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
         for (unsigned s = 0; s < kStages; ++s) {
             mbar_init(loaded(s), 1);
             mbar_init(decoded(s), kDecodeWarps);
-            mbar_init(peer(s), 1);
+            mbar_init(peer(s), kDecodeWarps);
             mbar_init(empty(s), 1);
         }
         for (unsigned k = 0; k < 2; ++k) {
@@ -362,12 +363,13 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             bool ok = true;
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
-                const int k0 = p.kt * kTileOuts + (int)rank * kCtaOuts;
+                const int k0 = p.kt * kTileOuts + (int)rank * kCtaOuts, c0 = p.ct * kTileCols + (int)rank * kCtaCols;
                 for (int step = p.first_step; step < p.last_step; ++step) {
                     ok = mbar_wait(empty(stage), parity ^ 1, gave_up);
                     if (!ok) break;
                     const int plane = step / a.steps_per_plane, n0 = (step - plane * a.steps_per_plane) * kStepRows;
-                    mbar_expect(loaded(stage), kTileBytes);
+                    mbar_expect(loaded(stage), kTileBytes + kCodeBytes);
+                    tma_load_codes(tiles_q + stage * kCodeBytes, &code_map, loaded(stage), c0, n0, p.sample);
                     tma_load(tiles_a + stage * kTileBytes, &map, loaded(stage), k0, n0, p.sample, plane);
                     tma_load(tiles_a + stage * kTileBytes + kBoxBytes, &map, loaded(stage), k0 + 64, n0, p.sample, plane);
                     ++pending;
@@ -396,12 +398,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             bool ok = true;
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
-                ok = mbar_wait<CG == 2>(drained(acc), acc_parity ^ 1, gave_up);
+                ok = mbar_wait(drained(acc), acc_parity ^ 1, gave_up);
                 if (!ok) break;
                 fence_tcgen05_after();
                 for (int step = p.first_step; step < p.last_step; ++step) {
                     ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(decoded(stage), parity, gave_up);
-                    if (CG == 2) ok = ok && mbar_wait<true>(peer(stage), parity, gave_up);
+                    if (CG == 2) ok = ok && mbar_wait(peer(stage), parity, gave_up);
                     if (!ok) break;
                     fence_tcgen05_after();
                     const unsigned long long da = operand_desc(tiles_a + stage * kTileBytes), db = operand_desc(tiles_b + stage * kTileBytes);
@@ -422,22 +424,6 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             // every product has finished before the memory it reads and writes is given up
             asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(finished), "n"(CG) : "memory");
             mbar_drain(finished, 0);
-        }
-    } else if (warp == kRelayWarp) {
-        if (CG == 2 && rank == 1 && lane == 0) {
-            unsigned stage = 0, parity = 0;
-            bool ok = true;
-            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
-                const TilePos p(a, t);
-                for (int step = p.first_step; step < p.last_step && ok; ++step) {
-                    ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(decoded(stage), parity, gave_up);
-                    if (ok) mbar_arrive_cluster(in_cta(peer(stage), 0));
-                    if (++stage == kStages) {
-                        stage = 0;
-                        parity ^= 1;
-                    }
-                }
-            }
         }
     } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
         const unsigned quarter = warp - kEpilogueWarp;  // TMEM lanes 32 * quarter .. + 31 are this warp's
@@ -460,6 +446,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
                 }
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {  // the decoding warps' order of columns
+                    const float x = v[i + 1];
+                    v[i + 1] = v[i + 2];
+                    v[i + 2] = x;
+                }
                 if (k < a.outs) store_row(row + c, v, a.cols - c0 - c, a.vec);
             }
             fence_tcgen05_before();
@@ -469,29 +461,28 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             if (acc == 0) acc_parity ^= 1;
         }
     } else if (warp >= kDecodeWarp) {
-        // eight threads to a row of 128 codes, 32 rows at a time, two rows per
-        // thread and stage; the codes of the next two stages are on their way
+        // eight threads to a row of 128 codes, two rows per thread and stage; the
+        // scale bytes of the next two stages are on their way.
+        // Chunk (8 bf16, 16 bytes) j of row n lies at (j ^ (n & 7)) * 16 of the row's
+        // 128 bytes; the upper four of eight lanes store their second chunk first, so
+        // that the eight meet all 32 banks.
         const unsigned d = threadIdx.x - 32 * kDecodeWarp;
         const unsigned c16 = d % 8, row = d / 8;
-        // chunk (8 bf16, 16 bytes) j of row n lies at (j ^ (n & 7)) * 16 of the row's 128 bytes; the upper half of the
-        // lanes stores its second chunk first, so that eight lanes meet all 32 banks
-        const unsigned box = c16 / 4, swap = box, j0 = c16 % 4 * 2;
-        const unsigned at = tiles_b + box * kBoxBytes + row * 128;
-        const unsigned first = ((j0 + swap) ^ (row & 7)) * 16, second = ((j0 + 1 - swap) ^ (row & 7)) * 16;
-        CodeWalk<CG> walk;
-        walk.t = first_tile;
-        walk.stride = tile_stride;
-        walk.rank = rank;
-        walk.open(a, c16);
-        constexpr int kAhead = 3;
-        CodeRow buf[kAhead][2];
+        const unsigned swap = c16 / 4, j0 = c16 % 4 * 2;
+        const unsigned at = tiles_b + swap * kBoxBytes + row * 128;
+        const unsigned first = at + ((j0 + swap) ^ (row & 7)) * 16, second = at + ((j0 + 1 - swap) ^ (row & 7)) * 16;
+        const unsigned from = tiles_q + row * kCtaCols + c16 * 16;
+        constexpr int kAhead = 2;
+        unsigned bytes[kAhead][2];
         bool have[kAhead];
+        ScaleWalk<CG> walk;
+        walk.open(a, first_tile, rank, row, c16);
 #pragma unroll
         for (int b = 0; b < kAhead; ++b) {
-            have[b] = walk.more(a);
+            have[b] = walk.t < a.tiles;
             if (have[b]) {
-                walk.load(a, row, buf[b]);
-                walk.next(a, c16);
+                walk.fetch(a, bytes[b]);
+                walk.next(a, tile_stride, rank, row, c16);
             }
         }
         unsigned stage = 0, parity = 0;
@@ -499,34 +490,37 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
         while (have[0] && ok) {
 #pragma unroll
             for (int b = 0; b < kAhead; ++b) {
-                if (!have[b] || !ok) break;
-                ok = mbar_wait(empty(stage), parity ^ 1, gave_up);
-                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!have[b]) break;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(loaded(stage), parity, gave_up));  // and so the stage is free
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const unsigned byte = buf[b][h].scale;
-                    const unsigned s2 = (byte == kNanScale ? 0x7FC0u : byte << 7) * 0x10001u;
-                    const uint4 q = buf[b][h].q;
-                    const uint2 v0 = decode4<FMT>(q.x, s2), v1 = decode4<FMT>(q.y, s2), v2 = decode4<FMT>(q.z, s2), v3 = decode4<FMT>(q.w, s2);
-                    const uint4 lo = make_uint4(v0.x, v0.y, v1.x, v1.y), hi = make_uint4(v2.x, v2.y, v3.x, v3.y);
+                    uint4 q, lo, hi;
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+                                 : "r"(from + stage * kCodeBytes + h * 32 * kCtaCols));
+                    widen16<FMT>(q, bytes[b][h], lo, hi);
                     const uint4 s0 = swap ? hi : lo, s1 = swap ? lo : hi;
-                    const unsigned dst = at + stage * kTileBytes + h * 32 * 128;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + first), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + second), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
+                    const unsigned off = stage * kTileBytes + h * 32 * 128;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(first + off), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(second + off), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(decoded(stage));
+                if (lane == 0) {
+                    if (rank == 0)
+                        mbar_arrive(decoded(stage));
+                    else
+                        mbar_arrive_cluster(in_cta(peer(stage), 0));
+                }
                 if (++stage == kStages) {
                     stage = 0;
                     parity ^= 1;
                 }
-                // behind the fence, which would wait for loads in flight
-                have[b] = walk.more(a);
-                if (have[b]) {
-                    walk.load(a, row, buf[b]);
-                    walk.next(a, c16);
+                have[b] = walk.t < a.tiles;
+                if (have[b]) {  // behind the fence, which would wait for them
+                    walk.fetch(a, bytes[b]);
+                    walk.next(a, tile_stride, rank, row, c16);
                 }
             }
         }
@@ -735,8 +729,25 @@ int gradient_map(CUtensorMap* map, const void* base, const Problem& q, const Pla
     return rc == CUDA_SUCCESS ? AMPQ_OK : AMPQ_ERR_CUDA;
 }
 
+// The codes as [samples][rows][columns with codes]: 64 tokens x 128 columns per copy, zeros outside each sample.
+int code_map_of(CUtensorMap* map, const unsigned char* codes, long long ld_codes, const Problem& q) {
+    const EncodeFn encode = encode_fn();
+    if (!encode) return AMPQ_ERR_CUDA;
+    unsigned long long row = (unsigned long long)ld_codes, sample = row * (unsigned long long)q.rows;
+    if (q.samples == 1) sample = row;  // never stepped over
+    const unsigned long long limit = 1ull << 40;
+    if (row >= limit || sample >= limit) return AMPQ_ERR_TOO_LARGE;
+    const cuuint64_t dims[3] = {(cuuint64_t)round_up(q.cols, kGroup), (cuuint64_t)q.rows, (cuuint64_t)q.samples};
+    const cuuint64_t strides[2] = {row, sample};
+    const cuuint32_t box[3] = {kCtaCols, kStepRows, 1}, one[3] = {1, 1, 1};
+    const CUresult rc = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<unsigned char*>(codes), dims, strides, box, one,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? AMPQ_OK : AMPQ_ERR_CUDA;
+}
+
 template <int CG, int FMT, typename OUT>
-int launch_product(const CUtensorMap& map, const WgradArgs& a, int device, int sms, cudaStream_t st) {
+int launch_product(const CUtensorMap& map, const CUtensorMap& code_map, const WgradArgs& a, int device, int sms, cudaStream_t st) {
     constexpr int kMaxDevices = 64;
     static std::atomic<bool> prepared[kMaxDevices];  // the attribute is set once per device and kernel
     if (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire)) {
@@ -758,7 +769,7 @@ int launch_product(const CUtensorMap& map, const WgradArgs& a, int device, int s
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, wgrad_kernel<CG, FMT, OUT>, map, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, wgrad_kernel<CG, FMT, OUT>, map, code_map, a) != cudaSuccess) {
         cudaGetLastError();
         return AMPQ_ERR_CUDA;
     }
@@ -766,8 +777,8 @@ int launch_product(const CUtensorMap& map, const WgradArgs& a, int device, int s
 }
 
 template <int FMT, typename OUT>
-int run_product(const CUtensorMap& map, const WgradArgs& a, bool pair, int device, int sms, cudaStream_t st) {
-    return pair ? launch_product<2, FMT, OUT>(map, a, device, sms, st) : launch_product<1, FMT, OUT>(map, a, device, sms, st);
+int run_product(const CUtensorMap& map, const CUtensorMap& code_map, const WgradArgs& a, bool pair, int device, int sms, cudaStream_t st) {
+    return pair ? launch_product<2, FMT, OUT>(map, code_map, a, device, sms, st) : launch_product<1, FMT, OUT>(map, code_map, a, device, sms, st);
 }
 
 template <typename T>
@@ -847,15 +858,14 @@ int ampq_ckpt_weight_grad(int device, void* cuda_stream, int dtype, int fmt, con
             rc = dtype == AMPQ_F32 ? lay_out<float>(q, p, ws, st) : lay_out<__nv_bfloat16>(q, p, ws, st);
             if (rc) return rc;
         }
-        CUtensorMap map;
+        CUtensorMap map, code_map;
         rc = gradient_map(&map, p.copy ? ws : gy, q, p);
+        if (!rc) rc = code_map_of(&code_map, codes, ld_codes, q);
         if (rc) return rc;
         const bool partial = p.splits > 1, f32 = partial || dtype == AMPQ_F32;
         WgradArgs a;
-        a.codes = codes;
         a.scales = scales;
         a.out = partial ? ws + p.at_part : gw;
-        a.ld_codes = ld_codes;
         a.ld_scales = ld_scales;
         a.cols = cols;
         a.outs = outs;
@@ -867,12 +877,11 @@ int ampq_ckpt_weight_grad(int device, void* cuda_stream, int dtype, int fmt, con
         a.steps_per_plane = p.steps_per_plane;
         a.steps = p.steps;
         a.steps_per_split = p.steps_per_split;
-        a.stored_cols = (unsigned)round_up(cols, kGroup);
         a.vec = rows_aligned(a.out, cols, f32 ? AMPQ_F32 : AMPQ_BF16);
         if (fmt == AMPQ_FMT_E4M3)
-            rc = f32 ? run_product<AMPQ_FMT_E4M3, float>(map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E4M3, __nv_bfloat16>(map, a, p.pair, device, sms, st);
+            rc = f32 ? run_product<AMPQ_FMT_E4M3, float>(map, code_map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E4M3, __nv_bfloat16>(map, code_map, a, p.pair, device, sms, st);
         else
-            rc = f32 ? run_product<AMPQ_FMT_E5M2, float>(map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E5M2, __nv_bfloat16>(map, a, p.pair, device, sms, st);
+            rc = f32 ? run_product<AMPQ_FMT_E5M2, float>(map, code_map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E5M2, __nv_bfloat16>(map, code_map, a, p.pair, device, sms, st);
         if (rc) return rc;
         if (partial) {
             const long long n = outs * cols, blocks = (samples * n + 255) / 256;
