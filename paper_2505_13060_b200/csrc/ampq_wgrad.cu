@@ -29,10 +29,13 @@ constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
 constexpr int kCodeBytes = kStepRows * kCtaCols;  // the codes of one stage
 constexpr int kStages = 5;
-constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kEpilogueWarp = 4, kDecodeWarp = 8;
-constexpr int kEpilogueWarps = 4, kDecodeWarps = 8;
+constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kScaleWarp = 3, kEpilogueWarp = 4, kDecodeWarp = 8;
+constexpr int kEpilogueWarps = 4;
+constexpr int kDecodeTeams = 2, kTeamWarps = 4;  // team i widens stages i, i + kDecodeTeams, ...
+constexpr int kDecodeWarps = kDecodeTeams * kTeamWarps;
 constexpr int kThreads = 32 * (kDecodeWarp + kDecodeWarps);
-constexpr int kSmemBytes = kStages * (2 * kTileBytes + kCodeBytes) + 1024;
+constexpr int kScaleBytes = 4 * kStepRows;       // their scale bytes, four a row
+constexpr int kSmemBytes = kStages * (2 * kTileBytes + kCodeBytes + kScaleBytes) + 1024;
 
 // Polls of an mbarrier before a wait gives up.  A test build lets the waits
 // between the stages give up at once; the waits that drain copies and products
@@ -168,6 +171,7 @@ struct WgradArgs {
     long long ld_scales, cols, outs, rows;
     long long tiles;                          // (sample, split, k tile, c tile)
     int k_tiles, c_tiles, splits, steps_per_plane, steps, steps_per_split;
+    bool scale_words;                         // rows of scale bytes start on 4-byte boundaries
     bool vec;                                 // rows of the output start on 16-byte boundaries
 };
 
@@ -226,41 +230,49 @@ __device__ __forceinline__ void widen16(uint4 q, unsigned byte, uint4& lo, uint4
     }
 }
 
-// The scale bytes of one decoding thread (rows n and n + 32 of a stage, one
-// group), stage by stage through all of its tiles.
+// The scale bytes of a CTA's stages, one after the other through all of its
+// tiles: one lane's rows n and n + 32, the four groups of the CTA's 128 columns in
+// one word.  0 (decodes to 0) where there is no row or no column.
 template <int CG>
 struct ScaleWalk {
     long long t;
     const unsigned char* p;
-    int step, last_step, plane_step;
+    int step, last_step, plane_step, groups;
     long long n;
-    bool in;
-    __device__ __forceinline__ void open(const WgradArgs& a, long long tile, unsigned rank, unsigned row, unsigned c16) {
+    __device__ __forceinline__ void open(const WgradArgs& a, long long tile, unsigned rank, unsigned lane) {
         t = tile;
         if (t >= a.tiles) return;
         const TilePos pos(a, t);
         step = pos.first_step;
         last_step = pos.last_step;
         plane_step = step % a.steps_per_plane;
-        n = (long long)plane_step * kStepRows + row;
-        const long long col = (long long)pos.ct * (CG * kCtaCols) + rank * kCtaCols + c16 * 16;
-        in = col < a.cols;
-        p = a.scales + (pos.sample * a.rows + n) * a.ld_scales + col / kGroup;
+        n = (long long)plane_step * kStepRows + lane;
+        const long long group = (long long)pos.ct * (CG * kCtaCols / kGroup) + rank * (kCtaCols / kGroup);
+        groups = (int)max(0LL, min(4LL, (a.cols + kGroup - 1) / kGroup - group));
+        p = a.scales + (pos.sample * a.rows + n) * a.ld_scales + group;
     }
-    __device__ __forceinline__ void fetch(const WgradArgs& a, unsigned (&byte)[2]) const {
-        byte[0] = in && n < a.rows ? __ldg(p) : 0u;
-        byte[1] = in && n + 32 < a.rows ? __ldg(p + 32 * a.ld_scales) : 0u;
+    __device__ __forceinline__ unsigned word(const unsigned char* q, bool words) const {
+        if (words && groups == 4) return __ldg(reinterpret_cast<const unsigned*>(q));
+        unsigned w = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            if (g < groups) w |= (unsigned)__ldg(q + g) << (8 * g);
+        return w;
     }
-    __device__ __forceinline__ void next(const WgradArgs& a, long long tile_stride, unsigned rank, unsigned row, unsigned c16) {
+    __device__ __forceinline__ void fetch(const WgradArgs& a, unsigned (&w)[2]) const {
+        w[0] = n < a.rows ? word(p, a.scale_words) : 0u;
+        w[1] = n + 32 < a.rows ? word(p + 32 * a.ld_scales, a.scale_words) : 0u;
+    }
+    __device__ __forceinline__ void next(const WgradArgs& a, long long tile_stride, unsigned rank, unsigned lane) {
         if (++step == last_step) {
-            open(a, t + tile_stride, rank, row, c16);
+            open(a, t + tile_stride, rank, lane);
             return;
         }
         n += kStepRows;
         p += kStepRows * a.ld_scales;
         if (++plane_step == a.steps_per_plane) {  // the next plane of the gradient meets the same rows
             plane_step = 0;
-            n = row;
+            n = lane;
             p -= (long long)a.steps_per_plane * kStepRows * a.ld_scales;
         }
     }
@@ -291,8 +303,8 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
 // accumulators.  CG = 1: one 128 x 128 tile per CTA.  Two accumulators, so that a
 // tile is stored while the next one is computed.
 //
-// Barriers, per stage: `loaded` (gY has landed), `decoded` (X^ is written), both
-// for the own CTA; `peer` (both are in place in the pair's second CTA; held by the
+// Barriers, per stage: `loaded` (gY and the codes have landed), `scaled` (the
+// scale bytes), `decoded` (X^ is written), for the own CTA; `peer` (both are in place in the pair's second CTA; held by the
 // first); `empty` (the products that read the stage are done).  Per accumulator:
 // `filled`, `drained`.  What the second CTA's warps wrote is read by the tensor
 // core alone, for which the proxy fence before their arrival makes it visible; the
@@ -305,7 +317,7 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
 template <int CG, int FMT, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const WgradArgs a) {
     extern __shared__ unsigned char raw_smem[];
-    __shared__ alignas(8) unsigned long long s_bars[4 * kStages + 5];
+    __shared__ alignas(8) unsigned long long s_bars[5 * kStages + 5];
     __shared__ unsigned s_tmem;
     __shared__ int s_gave_up;
     constexpr int kTileOuts = CG * kCtaOuts, kTileCols = CG * kCtaCols;
@@ -314,22 +326,25 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
     unsigned rank = 0;
     if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const unsigned base = (smem_u32(raw_smem) + 1023u) & ~1023u;
-    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = base + 2 * kStages * kTileBytes;
+    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = base + 2 * kStages * kTileBytes,
+                   tiles_s = tiles_q + kStages * kCodeBytes;
     const unsigned bars = smem_u32(s_bars);
     auto loaded = [&](unsigned s) { return bars + 8 * s; };
     auto decoded = [&](unsigned s) { return bars + 8 * (kStages + s); };
     auto peer = [&](unsigned s) { return bars + 8 * (2 * kStages + s); };
     auto empty = [&](unsigned s) { return bars + 8 * (3 * kStages + s); };
-    auto filled = [&](unsigned k) { return bars + 8 * (4 * kStages + k); };
-    auto drained = [&](unsigned k) { return bars + 8 * (4 * kStages + 2 + k); };
-    const unsigned finished = bars + 8 * (4 * kStages + 4);
+    auto scaled = [&](unsigned s) { return bars + 8 * (4 * kStages + s); };
+    auto filled = [&](unsigned k) { return bars + 8 * (5 * kStages + k); };
+    auto drained = [&](unsigned k) { return bars + 8 * (5 * kStages + 2 + k); };
+    const unsigned finished = bars + 8 * (5 * kStages + 4);
     volatile int* gave_up = &s_gave_up;
 
     if (threadIdx.x == 0) {
         for (unsigned s = 0; s < kStages; ++s) {
             mbar_init(loaded(s), 1);
-            mbar_init(decoded(s), kDecodeWarps);
-            mbar_init(peer(s), kDecodeWarps);
+            mbar_init(scaled(s), 1);
+            mbar_init(decoded(s), kTeamWarps);
+            mbar_init(peer(s), kTeamWarps);
             mbar_init(empty(s), 1);
         }
         for (unsigned k = 0; k < 2; ++k) {
@@ -425,6 +440,45 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(finished), "n"(CG) : "memory");
             mbar_drain(finished, 0);
         }
+    } else if (warp == kScaleWarp) {
+        // the scale bytes of the stages, some stages ahead of where they go
+        constexpr int kAhead = 4;
+        unsigned w[kAhead][2];
+        bool have[kAhead];
+        ScaleWalk<CG> walk;
+        walk.open(a, first_tile, rank, lane);
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            have[b] = walk.t < a.tiles;
+            if (have[b]) {
+                walk.fetch(a, w[b]);
+                walk.next(a, tile_stride, rank, lane);
+            }
+        }
+        unsigned stage = 0, parity = 0;
+        bool ok = true;
+        while (have[0] && ok) {
+#pragma unroll
+            for (int b = 0; b < kAhead; ++b) {
+                if (!have[b]) break;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(stage), parity ^ 1, gave_up));
+                if (!ok) break;
+                const unsigned to = tiles_s + stage * kScaleBytes + lane * 4;
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(w[b][0]) : "memory");
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 128), "r"(w[b][1]) : "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(scaled(stage));
+                if (++stage == kStages) {
+                    stage = 0;
+                    parity ^= 1;
+                }
+                have[b] = walk.t < a.tiles;
+                if (have[b]) {
+                    walk.fetch(a, w[b]);
+                    walk.next(a, tile_stride, rank, lane);
+                }
+            }
+        }
     } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
         const unsigned quarter = warp - kEpilogueWarp;  // TMEM lanes 32 * quarter .. + 31 are this warp's
         unsigned acc = 0, acc_parity = 0;
@@ -461,67 +515,51 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             if (acc == 0) acc_parity ^= 1;
         }
     } else if (warp >= kDecodeWarp) {
-        // eight threads to a row of 128 codes, two rows per thread and stage; the
-        // scale bytes of the next two stages are on their way.
-        // Chunk (8 bf16, 16 bytes) j of row n lies at (j ^ (n & 7)) * 16 of the row's
-        // 128 bytes; the upper four of eight lanes store their second chunk first, so
-        // that the eight meet all 32 banks.
-        const unsigned d = threadIdx.x - 32 * kDecodeWarp;
+        // Eight threads to a row of 128 codes.  Chunk (8 bf16, 16 bytes) j of row n lies
+        // at (j ^ (n & 7)) * 16 of the row's 128 bytes; the upper four of eight lanes
+        // store their second chunk first, so that the eight meet all 32 banks.
+        const unsigned team = (warp - kDecodeWarp) / kTeamWarps, d = threadIdx.x - 32 * (kDecodeWarp + team * kTeamWarps);
         const unsigned c16 = d % 8, row = d / 8;
         const unsigned swap = c16 / 4, j0 = c16 % 4 * 2;
         const unsigned at = tiles_b + swap * kBoxBytes + row * 128;
         const unsigned first = at + ((j0 + swap) ^ (row & 7)) * 16, second = at + ((j0 + 1 - swap) ^ (row & 7)) * 16;
-        const unsigned from = tiles_q + row * kCtaCols + c16 * 16;
-        constexpr int kAhead = 2;
-        unsigned bytes[kAhead][2];
-        bool have[kAhead];
-        ScaleWalk<CG> walk;
-        walk.open(a, first_tile, rank, row, c16);
-#pragma unroll
-        for (int b = 0; b < kAhead; ++b) {
-            have[b] = walk.t < a.tiles;
-            if (have[b]) {
-                walk.fetch(a, bytes[b]);
-                walk.next(a, tile_stride, rank, row, c16);
-            }
+        const unsigned from = tiles_q + row * kCtaCols + c16 * 16, scale_from = tiles_s + row * 4 + c16 / 2;
+        constexpr unsigned kTeamRows = 4 * kTeamWarps;
+        long long todo = 0;  // stages of this CTA
+        for (long long t = first_tile; t < a.tiles; t += tile_stride) {
+            const TilePos p(a, t);
+            todo += p.last_step - p.first_step;
         }
-        unsigned stage = 0, parity = 0;
-        bool ok = true;
-        while (have[0] && ok) {
+        unsigned stage = team, parity = 0;
+        static_assert(kDecodeTeams <= kStages, "a team's stages wrap once at a time");
+        for (long long i = team; i < todo; i += kDecodeTeams) {
+            const bool ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(scaled(stage), parity, gave_up);  // and so the stage is free
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            const unsigned qs = from + stage * kCodeBytes, ss = scale_from + stage * kScaleBytes;
+            const unsigned f = first + stage * kTileBytes, g = second + stage * kTileBytes;
 #pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                if (!have[b]) break;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(loaded(stage), parity, gave_up));  // and so the stage is free
-                if (!ok) break;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint4 q, lo, hi;
-                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
-                                 : "r"(from + stage * kCodeBytes + h * 32 * kCtaCols));
-                    widen16<FMT>(q, bytes[b][h], lo, hi);
-                    const uint4 s0 = swap ? hi : lo, s1 = swap ? lo : hi;
-                    const unsigned off = stage * kTileBytes + h * 32 * 128;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(first + off), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(second + off), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    if (rank == 0)
-                        mbar_arrive(decoded(stage));
-                    else
-                        mbar_arrive_cluster(in_cta(peer(stage), 0));
-                }
-                if (++stage == kStages) {
-                    stage = 0;
-                    parity ^= 1;
-                }
-                have[b] = walk.t < a.tiles;
-                if (have[b]) {  // behind the fence, which would wait for them
-                    walk.fetch(a, bytes[b]);
-                    walk.next(a, tile_stride, rank, row, c16);
-                }
+            for (unsigned h = 0; h < kStepRows; h += kTeamRows) {
+                uint4 q, lo, hi;
+                unsigned byte;
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(qs + h * kCtaCols));
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(ss + h * 4));
+                widen16<FMT>(q, byte, lo, hi);
+                const uint4 s0 = swap ? hi : lo, s1 = swap ? lo : hi;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(f + h * 128), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(g + h * 128), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (rank == 0)
+                    mbar_arrive(decoded(stage));
+                else
+                    mbar_arrive_cluster(in_cta(peer(stage), 0));
+            }
+            stage += kDecodeTeams;
+            if (stage >= kStages) {
+                stage -= kStages;
+                parity ^= 1;
             }
         }
     }
@@ -877,6 +915,7 @@ int ampq_ckpt_weight_grad(int device, void* cuda_stream, int dtype, int fmt, con
         a.steps_per_plane = p.steps_per_plane;
         a.steps = p.steps;
         a.steps_per_split = p.steps_per_split;
+        a.scale_words = aligned_to(scales, 4) && ld_scales % 4 == 0;
         a.vec = rows_aligned(a.out, cols, f32 ? AMPQ_F32 : AMPQ_BF16);
         if (fmt == AMPQ_FMT_E4M3)
             rc = f32 ? run_product<AMPQ_FMT_E4M3, float>(map, code_map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E4M3, __nv_bfloat16>(map, code_map, a, p.pair, device, sms, st);
