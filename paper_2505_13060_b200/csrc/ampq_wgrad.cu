@@ -28,14 +28,15 @@ constexpr int kCtaCols = 128;                 // checkpoint columns (c) of one C
 constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
 constexpr int kCodeBytes = kStepRows * kCtaCols;  // the codes of one stage
-constexpr int kStages = 5;
+constexpr int kStages = 6;                    // stages of what is loaded: gY, codes, scale bytes
+constexpr int kWideStages = 4;                // stages of the widened codes
 constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kScaleWarp = 3, kEpilogueWarp = 4, kDecodeWarp = 8;
 constexpr int kEpilogueWarps = 4;
 constexpr int kDecodeTeams = 2, kTeamWarps = 4;  // team i widens stages i, i + kDecodeTeams, ...
 constexpr int kDecodeWarps = kDecodeTeams * kTeamWarps;
 constexpr int kThreads = 32 * (kDecodeWarp + kDecodeWarps);
 constexpr int kScaleBytes = 4 * kStepRows;       // their scale bytes, four a row
-constexpr int kSmemBytes = kStages * (2 * kTileBytes + kCodeBytes + kScaleBytes) + 1024;
+constexpr int kSmemBytes = kStages * (kTileBytes + kCodeBytes + kScaleBytes) + kWideStages * kTileBytes + 1024;
 
 // Polls of an mbarrier before a wait gives up.  A test build lets the waits
 // between the stages give up at once; the waits that drain copies and products
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
     unsigned rank = 0;
     if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const unsigned base = (smem_u32(raw_smem) + 1023u) & ~1023u;
-    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = base + 2 * kStages * kTileBytes,
+    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = tiles_b + kWideStages * kTileBytes,
                    tiles_s = tiles_q + kStages * kCodeBytes;
     const unsigned bars = smem_u32(s_bars);
     auto loaded = [&](unsigned s) { return bars + 8 * s; };
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             // fp32 accumulators, bf16 operands, both MN-major
             constexpr unsigned kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((unsigned)(kTileCols / 8) << 17) |
                                         ((unsigned)(kTileOuts / 16) << 24);
-            unsigned stage = 0, parity = 0, acc = 0, acc_parity = 0;
+            unsigned stage = 0, parity = 0, wide = 0, acc = 0, acc_parity = 0;
             bool ok = true;
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
@@ -421,11 +422,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
                     if (CG == 2) ok = ok && mbar_wait(peer(stage), parity, gave_up);
                     if (!ok) break;
                     fence_tcgen05_after();
-                    const unsigned long long da = operand_desc(tiles_a + stage * kTileBytes), db = operand_desc(tiles_b + stage * kTileBytes);
+                    const unsigned long long da = operand_desc(tiles_a + stage * kTileBytes), db = operand_desc(tiles_b + wide * kTileBytes);
 #pragma unroll
                     for (int i = 0; i < kStepRows / 16; ++i)  // 16 tokens: two groups of eight, 2048 bytes
                         tcgen05_mma<CG>(tmem + acc * kTileCols, da + i * (2048 >> 4), db + i * (2048 >> 4), kIdesc, step > p.first_step || i > 0);
                     tcgen05_commit<CG>(empty(stage));
+                    if (++wide == kWideStages) wide = 0;
                     if (++stage == kStages) {
                         stage = 0;
                         parity ^= 1;
@@ -530,13 +532,16 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
             const TilePos p(a, t);
             todo += p.last_step - p.first_step;
         }
-        unsigned stage = team, parity = 0;
-        static_assert(kDecodeTeams <= kStages, "a team's stages wrap once at a time");
+        unsigned stage = team, parity = 0, wide = team;
+        // the stage whose products used the same place for widened codes before: kWideStages back
+        unsigned before = (kStages - kWideStages + team) % kStages, before_parity = team < kWideStages ? 1 : 0;
+        static_assert(kDecodeTeams <= kWideStages && kWideStages < kStages, "a team's stages wrap once at a time");
         for (long long i = team; i < todo; i += kDecodeTeams) {
-            const bool ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(scaled(stage), parity, gave_up);  // and so the stage is free
+            const bool ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(scaled(stage), parity, gave_up) &&
+                            (i < kWideStages || mbar_wait(empty(before), before_parity, gave_up));
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const unsigned qs = from + stage * kCodeBytes, ss = scale_from + stage * kScaleBytes;
-            const unsigned f = first + stage * kTileBytes, g = second + stage * kTileBytes;
+            const unsigned f = first + wide * kTileBytes, g = second + wide * kTileBytes;
 #pragma unroll
             for (unsigned h = 0; h < kStepRows; h += kTeamRows) {
                 uint4 q, lo, hi;
@@ -561,6 +566,13 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constan
                 stage -= kStages;
                 parity ^= 1;
             }
+            before += kDecodeTeams;
+            if (before >= kStages) {
+                before -= kStages;
+                before_parity ^= 1;
+            }
+            wide += kDecodeTeams;
+            if (wide >= kWideStages) wide -= kWideStages;
         }
     }
 
