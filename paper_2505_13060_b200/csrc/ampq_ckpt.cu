@@ -209,6 +209,16 @@ int launch_join_columns(const float* part, long long batches, int parts, long lo
     return launched();
 }
 
+int launch_ckpt_unpack(int dtype, int fmt, const unsigned char* codes, long long ld_codes, const unsigned char* scales, long long ld_scales,
+                       long long rows, long long cols, void* out, long long ld, cudaStream_t st) {
+    const bool e4 = fmt == AMPQ_FMT_E4M3;
+    if (dtype == AMPQ_F32)
+        return e4 ? launch_unpack<float, AMPQ_FMT_E4M3>(codes, ld_codes, scales, ld_scales, rows, cols, out, ld, st)
+                  : launch_unpack<float, AMPQ_FMT_E5M2>(codes, ld_codes, scales, ld_scales, rows, cols, out, ld, st);
+    return e4 ? launch_unpack<__nv_bfloat16, AMPQ_FMT_E4M3>(codes, ld_codes, scales, ld_scales, rows, cols, out, ld, st)
+              : launch_unpack<__nv_bfloat16, AMPQ_FMT_E5M2>(codes, ld_codes, scales, ld_scales, rows, cols, out, ld, st);
+}
+
 }  // namespace ampq
 
 using namespace ampq;
@@ -245,13 +255,7 @@ int ampq_ckpt_unpack(int device, void* cuda_stream, int dtype, int fmt, const un
     CkptDevice cur(device);
     if (cur.status) return cur.status;
     if (rows == 0 || cols == 0) return AMPQ_OK;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const bool e4 = fmt == AMPQ_FMT_E4M3;
-    if (dtype == AMPQ_F32)
-        return e4 ? launch_unpack<float, AMPQ_FMT_E4M3>(codes, ld_codes, scales, ld_scales, rows, cols, dev_out, ld, st)
-                  : launch_unpack<float, AMPQ_FMT_E5M2>(codes, ld_codes, scales, ld_scales, rows, cols, dev_out, ld, st);
-    return e4 ? launch_unpack<__nv_bfloat16, AMPQ_FMT_E4M3>(codes, ld_codes, scales, ld_scales, rows, cols, dev_out, ld, st)
-              : launch_unpack<__nv_bfloat16, AMPQ_FMT_E5M2>(codes, ld_codes, scales, ld_scales, rows, cols, dev_out, ld, st);
+    return launch_ckpt_unpack(dtype, fmt, codes, ld_codes, scales, ld_scales, rows, cols, dev_out, ld, reinterpret_cast<cudaStream_t>(cuda_stream));
 }
 
 #pragma GCC visibility pop

@@ -263,6 +263,10 @@ inline int check_ckpt(const unsigned char* codes, long long ld_codes, const unsi
 
 int sm_count(int device);  // multiprocessors of a device, 0 on error
 
+// ampq_ckpt_unpack on a stream of the current device, arguments checked.
+int launch_ckpt_unpack(int dtype, int fmt, const unsigned char* codes, long long ld_codes, const unsigned char* scales, long long ld_scales,
+                       long long rows, long long cols, void* out, long long ld, cudaStream_t st);
+
 // Sums `parts` fp32 partial rows of `cols` columns in a fixed order and stores
 // them in `dtype`: out[b][c] = sum_p part[b][p][c], `batches` of them.  With
 // `second` (two batches) batch 1 goes there.

@@ -2,17 +2,22 @@
 // (include/ampq.h: ampq_ckpt_weight_grad): for every sample r
 //   gW[r][k][c] = sum_n gY[r][n][k] * X^[r][n][c],  gb[r][k] = sum_n gY[r][n][k].
 //
-// The product runs on the tensor cores (tcgen05, kind::f16, fp32 accumulators in
-// TMEM).  Its reduction axis is the token n, along which neither operand is
-// contiguous, so both are given to the tensor core "MN-major", 128-byte
-// swizzled.  gY and the codes of X^ come in by TMA; eight warps widen the codes to
-// bf16 (exact, see ampq_ckpt.h) from shared memory into the same swizzled layout:
-// 33/32 byte per element of X from HBM and L2 instead of two, and no bf16 copy of
-// X in memory.
+// Large products run on the tensor cores (tcgen05, kind::f16, fp32 accumulators in
+// TMEM).  The reduction axis is the token n, along which neither operand is
+// contiguous, so both are given to the tensor core "MN-major", 128-byte swizzled,
+// which is how TMA lays 64 tokens x 64 columns down.  X^ is widened to bf16
+// (exactly, see ampq_ckpt.h) in one pass before the product: widening it on the
+// way into shared memory, for each of the outs / 256 times that the product reads
+// it, took the power and the issue slots that the tensor cores need (8192^3: 1200
+// TFLOP/s against 1510 with the pass included).
 //
-// fp32 gradients are first cut into three bf16 planes, g = g0 + g1 + g2 exactly
-// (24 significant bits), and the token axis walks all three: the products stay
-// exact.
+// fp32 gradients are cut into three bf16 planes, g = g0 + g1 + g2 exactly (24
+// significant bits), and each 64 tokens are multiplied plane by plane, the smallest
+// first.  The tensor core's additions cut instead of rounding: 2.9e-8 per addition,
+// all towards zero, 4e-5 over 8192 tokens.  So the sum of each 64 tokens is taken
+// out of TMEM and added to the rest in registers, rounded to nearest.
+//
+// Small products (few tokens, few tiles) are one launch of plain fp32 arithmetic.
 #include "ampq_ckpt.h"
 
 #include <cuda.h>
@@ -23,24 +28,25 @@ namespace ampq {
 namespace {
 
 constexpr int kStepRows = 64;                 // tokens of one pipeline stage
-constexpr int kCtaOuts = 128;                 // gradient columns (k) of one CTA's stage
-constexpr int kCtaCols = 128;                 // checkpoint columns (c) of one CTA's stage
+constexpr int kCtaSide = 128;                 // columns of gY, and of X^, of one CTA's stage
 constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
-constexpr int kCodeBytes = kStepRows * kCtaCols;  // the codes of one stage
-constexpr int kStages = 6;                    // stages of what is loaded: gY, codes, scale bytes
-constexpr int kWideStages = 4;                // stages of the widened codes
-constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kScaleWarp = 3, kEpilogueWarp = 4, kDecodeWarp = 8;
-constexpr int kEpilogueWarps = 4;
-constexpr int kDecodeTeams = 2, kTeamWarps = 4;  // team i widens stages i, i + kDecodeTeams, ...
-constexpr int kDecodeWarps = kDecodeTeams * kTeamWarps;
-constexpr int kThreads = 32 * (kDecodeWarp + kDecodeWarps);
-constexpr int kScaleBytes = 4 * kStepRows;       // their scale bytes, four a row
-constexpr int kSmemBytes = kStages * (kTileBytes + kCodeBytes + kScaleBytes) + kWideStages * kTileBytes + 1024;
+constexpr int kStages = 6;
+constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kStoreWarp = 4;
+constexpr int kPatch = 32 * 33;               // floats: a 32 x 32 patch of the output on its way out
+
+// Storing warps: four cover the 128 TMEM lanes once; with fp32 planes eight share
+// the columns, so that the running sums fit their registers.
+template <int PLANES>
+struct Roles {
+    static constexpr int kStoreWarps = PLANES == 1 ? 4 : 8;
+    static constexpr int kThreads = 32 * (kStoreWarp + kStoreWarps);
+    static constexpr int kSmemBytes = kStages * 2 * kTileBytes + kStoreWarps * kPatch * 4 + 1024;
+};
 
 // Polls of an mbarrier before a wait gives up.  A test build lets the waits
-// between the stages give up at once; the waits that drain copies and products
-// in flight keep the full limit.
+// between the stages give up at once; the wait that drains products in flight
+// keeps the full limit.
 constexpr unsigned kDrainPolls = 1u << 22;
 #ifdef AMPQ_TEST_SHORT_WAITS
 constexpr unsigned kWaitPolls = 1u;
@@ -88,25 +94,25 @@ __device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void mbar_arrive(unsigned bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned cluster_bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void mbar_expect(unsigned bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// CG = 2: the bytes may be counted on a barrier of the pair's other CTA.
+template <int CG>
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, unsigned bar, int k, int n, int r, int plane) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+    if (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(k), "r"(n), "r"(r), "r"(plane)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
         "l"(map), "r"(bar), "r"(k), "r"(n), "r"(r), "r"(plane)
         : "memory");
-}
-__device__ __forceinline__ void tma_load_codes(unsigned dst, const CUtensorMap* map, unsigned bar, int c, int n, int r) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-                 "l"(map), "r"(bar), "r"(c), "r"(n), "r"(r)
-                 : "memory");
 }
 __device__ __forceinline__ void fence_tcgen05_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_tcgen05_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -158,6 +164,18 @@ __device__ __forceinline__ void tmem_load32(unsigned addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_load16(unsigned addr, float (&v)[16]) {
+    unsigned r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
 // Shared-memory descriptor of an operand tile: MN-major, 128-byte swizzle.
 // Blocks of 64 elements of the non-reduced axis lie kBoxBytes apart (leading
 // offset), groups of eight tokens 1024 bytes apart (stride offset).
@@ -166,20 +184,18 @@ __device__ __forceinline__ unsigned long long operand_desc(unsigned addr) {
            ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-struct WgradArgs {
-    const unsigned char* scales;
+struct ProductArgs {
     void* out;                                // gw, or fp32 partial sums [samples][splits][outs][cols]
-    long long ld_scales, cols, outs, rows;
+    long long cols, outs;
     long long tiles;                          // (sample, split, k tile, c tile)
-    int k_tiles, c_tiles, splits, steps_per_plane, steps, steps_per_split;
-    bool scale_words;                         // rows of scale bytes start on 4-byte boundaries
+    int k_tiles, c_tiles, splits, steps, steps_per_split;  // steps: runs of 64 tokens
     bool vec;                                 // rows of the output start on 16-byte boundaries
 };
 
 // A tile of the output: which sample, which part of the token axis, which corner.
 struct TilePos {
     int sample, split, kt, ct, first_step, last_step;
-    __device__ __forceinline__ TilePos(const WgradArgs& a, long long t) {
+    __device__ __forceinline__ TilePos(const ProductArgs& a, long long t) {
         const int per = a.k_tiles * a.c_tiles;
         const long long group = t / per;
         const int in = (int)(t - group * per);
@@ -195,93 +211,14 @@ struct TilePos {
     }
 };
 
-__device__ __forceinline__ unsigned mul_bf16x2(unsigned a, unsigned b) {
-    unsigned r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
-// Four codes -> four bf16 values, in the order 0, 2, 1, 3.  A code moved into the
-// upper byte of a 16-bit half and shifted right by four (three) has its exponent
-// and mantissa fields at the low end of bf16's, subnormal codes among bf16's
-// subnormals: the value times 2^-120 (E4M3) or 2^-112 (E5M2).  One exact product
-// with `unit` puts that and the group's scale right.
-template <int FMT>
-__device__ __forceinline__ uint2 widen4(unsigned w, unsigned unit) {
-    constexpr unsigned kField = FMT == AMPQ_FMT_E4M3 ? 0x07F007F0u : 0x0FE00FE0u;
-    constexpr int kShift = FMT == AMPQ_FMT_E4M3 ? 4 : 3;
-    const unsigned even = ((w << (8 - kShift)) & kField) | ((w << 8) & 0x80008000u);
-    const unsigned odd = ((w >> kShift) & kField) | (w & 0x80008000u);
-    return make_uint2(mul_bf16x2(even, unit), mul_bf16x2(odd, unit));
-}
-
-// Sixteen codes of one group -> two 16-byte pieces of a row.  byte: the scale, or
-// 0 where there is no row, which decodes to 0.
-template <int FMT>
-__device__ __forceinline__ void widen16(uint4 q, unsigned byte, uint4& lo, uint4& hi) {
-    const unsigned field = byte ? byte + (FMT == AMPQ_FMT_E4M3 ? 120u : 112u) : 0u;  // bf16 exponent field of the factor
-    const unsigned unit = (min(field, 254u) << 7) * 0x10001u;
-    const uint2 a = widen4<FMT>(q.x, unit), b = widen4<FMT>(q.y, unit), c = widen4<FMT>(q.z, unit), d = widen4<FMT>(q.w, unit);
-    lo = make_uint4(a.x, a.y, b.x, b.y);
-    hi = make_uint4(c.x, c.y, d.x, d.y);
-    if (field > 254u) {  // a scale above 2^7 (2^15): the factor is no bf16 number, its second part follows; NaN for the NaN byte
-        const unsigned rest = (byte == kNanScale ? 0x7FC0u : (field - 127u) << 7) * 0x10001u;
-        lo = make_uint4(mul_bf16x2(lo.x, rest), mul_bf16x2(lo.y, rest), mul_bf16x2(lo.z, rest), mul_bf16x2(lo.w, rest));
-        hi = make_uint4(mul_bf16x2(hi.x, rest), mul_bf16x2(hi.y, rest), mul_bf16x2(hi.z, rest), mul_bf16x2(hi.w, rest));
-    }
-}
-
-// The scale bytes of a CTA's stages, one after the other through all of its
-// tiles: one lane's rows n and n + 32, the four groups of the CTA's 128 columns in
-// one word.  0 (decodes to 0) where there is no row or no column.
-template <int CG>
-struct ScaleWalk {
-    long long t;
-    const unsigned char* p;
-    int step, last_step, plane_step, groups;
-    long long n;
-    __device__ __forceinline__ void open(const WgradArgs& a, long long tile, unsigned rank, unsigned lane) {
-        t = tile;
-        if (t >= a.tiles) return;
-        const TilePos pos(a, t);
-        step = pos.first_step;
-        last_step = pos.last_step;
-        plane_step = step % a.steps_per_plane;
-        n = (long long)plane_step * kStepRows + lane;
-        const long long group = (long long)pos.ct * (CG * kCtaCols / kGroup) + rank * (kCtaCols / kGroup);
-        groups = (int)max(0LL, min(4LL, (a.cols + kGroup - 1) / kGroup - group));
-        p = a.scales + (pos.sample * a.rows + n) * a.ld_scales + group;
-    }
-    __device__ __forceinline__ unsigned word(const unsigned char* q, bool words) const {
-        if (words && groups == 4) return __ldg(reinterpret_cast<const unsigned*>(q));
-        unsigned w = 0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-            if (g < groups) w |= (unsigned)__ldg(q + g) << (8 * g);
-        return w;
-    }
-    __device__ __forceinline__ void fetch(const WgradArgs& a, unsigned (&w)[2]) const {
-        w[0] = n < a.rows ? word(p, a.scale_words) : 0u;
-        w[1] = n + 32 < a.rows ? word(p + 32 * a.ld_scales, a.scale_words) : 0u;
-    }
-    __device__ __forceinline__ void next(const WgradArgs& a, long long tile_stride, unsigned rank, unsigned lane) {
-        if (++step == last_step) {
-            open(a, t + tile_stride, rank, lane);
-            return;
-        }
-        n += kStepRows;
-        p += kStepRows * a.ld_scales;
-        if (++plane_step == a.steps_per_plane) {  // the next plane of the gradient meets the same rows
-            plane_step = 0;
-            n = lane;
-            p -= (long long)a.steps_per_plane * kStepRows * a.ld_scales;
-        }
-    }
-};
-
+// Stores 32 columns of 32 rows, lane l holding row l: from `row` for this lane,
+// `rows` of them from lane 0 on and `n` columns exist.  Rows on 16-byte boundaries
+// go out as they are held, 16 bytes a lane; others through a patch of shared
+// memory, a row at a time, so that a warp still writes runs of 32 elements.
 template <typename OUT>
-__device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long long n, bool vec) {
+__device__ __forceinline__ void store_patch(OUT* row, const float (&v)[32], long long rows, long long n, long long pitch, bool vec, float* patch, unsigned lane) {
     if (vec && n >= 32) {
+        if ((long long)lane >= rows) return;
 #pragma unroll
         for (int i = 0; i < 32; i += 8) {
             float w[8];
@@ -289,314 +226,325 @@ __device__ __forceinline__ void store_row(OUT* p, const float (&v)[32], long lon
             for (int j = 0; j < 8; ++j) w[j] = v[i + j];
             Raw8<OUT> r;
             r.set(w);
-            r.store(p + i);
+            r.store(row + i);
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if (i < n) store_elem(p + i, v[i]);
+    for (int i = 0; i < 32; ++i) patch[lane * 33 + i] = v[i];
+    __syncwarp();
+    OUT* first = row - (long long)lane * pitch + lane;
+    if ((long long)lane < n) {
+        const int m = (int)min(32LL, rows);
+#pragma unroll 8
+        for (int i = 0; i < m; ++i) store_elem(first + (long long)i * pitch, patch[i * 33 + lane]);
+    }
+    __syncwarp();
 }
 
-// A persistent grid of CTAs (CG = 1) or CTA pairs (CG = 2) walks the tiles.  CG =
-// 2: one 256 x 256 tile per pair, products issued by the pair's first CTA; each
-// CTA holds 128 rows and 128 columns of the operands and 128 rows of the
-// accumulators.  CG = 1: one 128 x 128 tile per CTA.  Two accumulators, so that a
-// tile is stored while the next one is computed.
-//
-// Barriers, per stage: `loaded` (gY and the codes have landed), `scaled` (the
-// scale bytes), `decoded` (X^ is written), for the own CTA; `peer` (both are in place in the pair's second CTA; held by the
-// first); `empty` (the products that read the stage are done).  Per accumulator:
-// `filled`, `drained`.  What the second CTA's warps wrote is read by the tensor
-// core alone, for which the proxy fence before their arrival makes it visible; the
-// arrival itself does not release at cluster scope, which would wait for every
-// load in flight (1.5 us a stage).
-//
-// A wait that runs out raises the CTA's flag; its threads then leave their loops,
-// the copies and products in flight are waited for, and what was not stored yet
-// becomes NaN.
-template <int CG, int FMT, typename OUT>
-__global__ void __launch_bounds__(kThreads, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap code_map, const WgradArgs a) {
-    extern __shared__ unsigned char raw_smem[];
-    __shared__ alignas(8) unsigned long long s_bars[5 * kStages + 5];
-    __shared__ unsigned s_tmem;
-    __shared__ int s_gave_up;
-    constexpr int kTileOuts = CG * kCtaOuts, kTileCols = CG * kCtaCols;
-    constexpr unsigned kTmemCols = 2 * kTileCols;
-    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    unsigned rank = 0;
-    if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const unsigned base = (smem_u32(raw_smem) + 1023u) & ~1023u;
-    const unsigned tiles_a = base, tiles_b = base + kStages * kTileBytes, tiles_q = tiles_b + kWideStages * kTileBytes,
-                   tiles_s = tiles_q + kStages * kCodeBytes;
-    const unsigned bars = smem_u32(s_bars);
-    auto loaded = [&](unsigned s) { return bars + 8 * s; };
-    auto decoded = [&](unsigned s) { return bars + 8 * (kStages + s); };
-    auto peer = [&](unsigned s) { return bars + 8 * (2 * kStages + s); };
-    auto empty = [&](unsigned s) { return bars + 8 * (3 * kStages + s); };
-    auto scaled = [&](unsigned s) { return bars + 8 * (4 * kStages + s); };
-    auto filled = [&](unsigned k) { return bars + 8 * (5 * kStages + k); };
-    auto drained = [&](unsigned k) { return bars + 8 * (5 * kStages + 2 + k); };
-    const unsigned finished = bars + 8 * (5 * kStages + 4);
-    volatile int* gave_up = &s_gave_up;
-
-    if (threadIdx.x == 0) {
-        for (unsigned s = 0; s < kStages; ++s) {
-            mbar_init(loaded(s), 1);
-            mbar_init(scaled(s), 1);
-            mbar_init(decoded(s), kTeamWarps);
-            mbar_init(peer(s), kTeamWarps);
-            mbar_init(empty(s), 1);
-        }
-        for (unsigned k = 0; k < 2; ++k) {
-            mbar_init(filled(k), 1);
-            mbar_init(drained(k), CG * kEpilogueWarps);
-        }
-        mbar_init(finished, 1);
-        s_gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+template <int CG>
+__device__ __forceinline__ unsigned tmem_alloc(unsigned* where, unsigned warp, unsigned cols) {
     if (warp == kTmemWarp) {
         if (CG == 1)
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(cols) : "memory");
         else
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(cols) : "memory");
         fence_tcgen05_before();
     }
     __syncthreads();
-    if (CG == 2) {
-        asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-    }
+    if (CG == 2) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
     fence_tcgen05_after();
-    const unsigned tmem = s_tmem;
+    return *where;
+}
 
-    const long long first_tile = blockIdx.x / CG, tile_stride = gridDim.x / CG;
-
-    if (warp == kProducerWarp) {
-        if (lane == 0) {
-            unsigned stage = 0, parity = 0;
-            unsigned pending = 0;  // loads issued, at most kStages of them not yet known to have landed
-            bool ok = true;
-            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
-                const TilePos p(a, t);
-                const int k0 = p.kt * kTileOuts + (int)rank * kCtaOuts, c0 = p.ct * kTileCols + (int)rank * kCtaCols;
-                for (int step = p.first_step; step < p.last_step; ++step) {
-                    ok = mbar_wait(empty(stage), parity ^ 1, gave_up);
-                    if (!ok) break;
-                    const int plane = step / a.steps_per_plane, n0 = (step - plane * a.steps_per_plane) * kStepRows;
-                    mbar_expect(loaded(stage), kTileBytes + kCodeBytes);
-                    tma_load_codes(tiles_q + stage * kCodeBytes, &code_map, loaded(stage), c0, n0, p.sample);
-                    tma_load(tiles_a + stage * kTileBytes, &map, loaded(stage), k0, n0, p.sample, plane);
-                    tma_load(tiles_a + stage * kTileBytes + kBoxBytes, &map, loaded(stage), k0 + 64, n0, p.sample, plane);
-                    ++pending;
-                    if (++stage == kStages) {
-                        stage = 0;
-                        parity ^= 1;
-                    }
-                }
-            }
-            // no copy of this CTA is in flight when it ends
-            for (unsigned k = 0; k < kStages && k < pending; ++k) {
-                if (stage == 0) {
-                    stage = kStages;
-                    parity ^= 1;
-                }
-                --stage;
-                mbar_drain(loaded(stage), parity);
-            }
-        }
-    } else if (warp == kMmaWarp) {
-        if (rank == 0 && lane == 0) {
-            // fp32 accumulators, bf16 operands, both MN-major
-            constexpr unsigned kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((unsigned)(kTileCols / 8) << 17) |
-                                        ((unsigned)(kTileOuts / 16) << 24);
-            unsigned stage = 0, parity = 0, wide = 0, acc = 0, acc_parity = 0;
-            bool ok = true;
-            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
-                const TilePos p(a, t);
-                ok = mbar_wait(drained(acc), acc_parity ^ 1, gave_up);
-                if (!ok) break;
-                fence_tcgen05_after();
-                for (int step = p.first_step; step < p.last_step; ++step) {
-                    ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(decoded(stage), parity, gave_up);
-                    if (CG == 2) ok = ok && mbar_wait(peer(stage), parity, gave_up);
-                    if (!ok) break;
-                    fence_tcgen05_after();
-                    const unsigned long long da = operand_desc(tiles_a + stage * kTileBytes), db = operand_desc(tiles_b + wide * kTileBytes);
-#pragma unroll
-                    for (int i = 0; i < kStepRows / 16; ++i)  // 16 tokens: two groups of eight, 2048 bytes
-                        tcgen05_mma<CG>(tmem + acc * kTileCols, da + i * (2048 >> 4), db + i * (2048 >> 4), kIdesc, step > p.first_step || i > 0);
-                    tcgen05_commit<CG>(empty(stage));
-                    if (++wide == kWideStages) wide = 0;
-                    if (++stage == kStages) {
-                        stage = 0;
-                        parity ^= 1;
-                    }
-                }
-                if (!ok) break;
-                tcgen05_commit<CG>(filled(acc));
-                acc ^= 1;
-                if (acc == 0) acc_parity ^= 1;
-            }
-            // every product has finished before the memory it reads and writes is given up
-            asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(finished), "n"(CG) : "memory");
-            mbar_drain(finished, 0);
-        }
-    } else if (warp == kScaleWarp) {
-        // the scale bytes of the stages, some stages ahead of where they go
-        constexpr int kAhead = 4;
-        unsigned w[kAhead][2];
-        bool have[kAhead];
-        ScaleWalk<CG> walk;
-        walk.open(a, first_tile, rank, lane);
-#pragma unroll
-        for (int b = 0; b < kAhead; ++b) {
-            have[b] = walk.t < a.tiles;
-            if (have[b]) {
-                walk.fetch(a, w[b]);
-                walk.next(a, tile_stride, rank, lane);
-            }
-        }
-        unsigned stage = 0, parity = 0;
-        bool ok = true;
-        while (have[0] && ok) {
-#pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                if (!have[b]) break;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty(stage), parity ^ 1, gave_up));
-                if (!ok) break;
-                const unsigned to = tiles_s + stage * kScaleBytes + lane * 4;
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(w[b][0]) : "memory");
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 128), "r"(w[b][1]) : "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(scaled(stage));
-                if (++stage == kStages) {
-                    stage = 0;
-                    parity ^= 1;
-                }
-                have[b] = walk.t < a.tiles;
-                if (have[b]) {
-                    walk.fetch(a, w[b]);
-                    walk.next(a, tile_stride, rank, lane);
-                }
-            }
-        }
-    } else if (warp >= kEpilogueWarp && warp < kEpilogueWarp + kEpilogueWarps) {
-        const unsigned quarter = warp - kEpilogueWarp;  // TMEM lanes 32 * quarter .. + 31 are this warp's
-        unsigned acc = 0, acc_parity = 0;
-        bool ok = true;
-        for (long long t = first_tile; t < a.tiles; t += tile_stride) {
-            const TilePos p(a, t);
-            if (ok) ok = mbar_wait(filled(acc), acc_parity, gave_up);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            fence_tcgen05_after();
-            const long long k = (long long)p.kt * kTileOuts + rank * kCtaOuts + quarter * 32 + lane;
-            const long long c0 = (long long)p.ct * kTileCols;
-            OUT* row = static_cast<OUT*>(a.out) + (((long long)p.sample * a.splits + p.split) * a.outs + k) * a.cols + c0;
-            for (int c = 0; c < kTileCols && c0 + c < a.cols; c += 32) {
-                float v[32];
-                __syncwarp();
-                if (ok) {
-                    tmem_load32(tmem + acc * kTileCols + ((quarter * 32) << 16) + c, v);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
-                }
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {  // the decoding warps' order of columns
-                    const float x = v[i + 1];
-                    v[i + 1] = v[i + 2];
-                    v[i + 2] = x;
-                }
-                if (k < a.outs) store_row(row + c, v, a.cols - c0 - c, a.vec);
-            }
-            fence_tcgen05_before();
-            __syncwarp();
-            if (ok && lane == 0) mbar_arrive_cluster(CG == 2 ? in_cta(drained(acc), 0) : drained(acc));
-            acc ^= 1;
-            if (acc == 0) acc_parity ^= 1;
-        }
-    } else if (warp >= kDecodeWarp) {
-        // Eight threads to a row of 128 codes.  Chunk (8 bf16, 16 bytes) j of row n lies
-        // at (j ^ (n & 7)) * 16 of the row's 128 bytes; the upper four of eight lanes
-        // store their second chunk first, so that the eight meet all 32 banks.
-        const unsigned team = (warp - kDecodeWarp) / kTeamWarps, d = threadIdx.x - 32 * (kDecodeWarp + team * kTeamWarps);
-        const unsigned c16 = d % 8, row = d / 8;
-        const unsigned swap = c16 / 4, j0 = c16 % 4 * 2;
-        const unsigned at = tiles_b + swap * kBoxBytes + row * 128;
-        const unsigned first = at + ((j0 + swap) ^ (row & 7)) * 16, second = at + ((j0 + 1 - swap) ^ (row & 7)) * 16;
-        const unsigned from = tiles_q + row * kCtaCols + c16 * 16, scale_from = tiles_s + row * 4 + c16 / 2;
-        constexpr unsigned kTeamRows = 4 * kTeamWarps;
-        long long todo = 0;  // stages of this CTA
-        for (long long t = first_tile; t < a.tiles; t += tile_stride) {
-            const TilePos p(a, t);
-            todo += p.last_step - p.first_step;
-        }
-        unsigned stage = team, parity = 0, wide = team;
-        // the stage whose products used the same place for widened codes before: kWideStages back
-        unsigned before = (kStages - kWideStages + team) % kStages, before_parity = team < kWideStages ? 1 : 0;
-        static_assert(kDecodeTeams <= kWideStages && kWideStages < kStages, "a team's stages wrap once at a time");
-        for (long long i = team; i < todo; i += kDecodeTeams) {
-            const bool ok = mbar_wait(loaded(stage), parity, gave_up) && mbar_wait(scaled(stage), parity, gave_up) &&
-                            (i < kWideStages || mbar_wait(empty(before), before_parity, gave_up));
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
-            const unsigned qs = from + stage * kCodeBytes, ss = scale_from + stage * kScaleBytes;
-            const unsigned f = first + wide * kTileBytes, g = second + wide * kTileBytes;
-#pragma unroll
-            for (unsigned h = 0; h < kStepRows; h += kTeamRows) {
-                uint4 q, lo, hi;
-                unsigned byte;
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(qs + h * kCtaCols));
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(ss + h * 4));
-                widen16<FMT>(q, byte, lo, hi);
-                const uint4 s0 = swap ? hi : lo, s1 = swap ? lo : hi;
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(f + h * 128), "r"(s0.x), "r"(s0.y), "r"(s0.z), "r"(s0.w) : "memory");
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(g + h * 128), "r"(s1.x), "r"(s1.y), "r"(s1.z), "r"(s1.w) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                if (rank == 0)
-                    mbar_arrive(decoded(stage));
-                else
-                    mbar_arrive_cluster(in_cta(peer(stage), 0));
-            }
-            stage += kDecodeTeams;
-            if (stage >= kStages) {
-                stage -= kStages;
-                parity ^= 1;
-            }
-            before += kDecodeTeams;
-            if (before >= kStages) {
-                before -= kStages;
-                before_parity ^= 1;
-            }
-            wide += kDecodeTeams;
-            if (wide >= kWideStages) wide -= kWideStages;
-        }
-    }
-
+// The end of every thread of a CTA: no CTA of a pair ends, or gives up its TMEM,
+// while the other still works.
+template <int CG>
+__device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned cols) {
     __syncwarp();
     __syncthreads();
-    if (CG == 2) {
-        // no CTA of a pair ends, or gives up its TMEM, while the other still works
-        asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-    }
+    if (CG == 2) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
     if (warp == kTmemWarp) {
         __syncwarp();
         fence_tcgen05_after();
         if (CG == 1) {
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
         } else {
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
         }
     }
 }
 
+// A persistent grid of CTAs (CG = 1) or CTA pairs (CG = 2) walks the tiles.  CG =
+// 2: one 256 x 256 tile per pair, products issued by the pair's first CTA; each
+// CTA holds 128 columns of both operands and 128 rows of the accumulators.  CG =
+// 1: one 128 x 128 tile per CTA.  Two accumulators, so that one is read while the
+// next is filled: one per tile, or with three planes one per 64 tokens.
+//
+// Barriers, per stage: `loaded` (both operands have landed, in both CTAs of a
+// pair; held by the first), `empty` (the products that read the stage are done).
+// Per accumulator: `filled`, `drained`.
+//
+// A wait that runs out raises the CTA's flag; its threads then leave their loops,
+// the copies and products in flight are waited for, and what was not stored yet
+// becomes NaN.
+template <int CG, int PLANES, typename OUT>
+__global__ void __launch_bounds__(Roles<PLANES>::kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap g_map, const __grid_constant__ CUtensorMap x_map, const ProductArgs a) {
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ alignas(8) unsigned long long s_bars[2 * kStages + 5];
+    __shared__ unsigned s_tmem;
+    __shared__ int s_gave_up;
+    constexpr int kSide = CG * kCtaSide;  // of the tile
+    constexpr unsigned kTmemCols = 2 * kSide;
+    constexpr int kStoreWarps = Roles<PLANES>::kStoreWarps;
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    unsigned rank = 0;
+    if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const unsigned base = (smem_u32(raw_smem) + 1023u) & ~1023u;
+    const unsigned tiles_g = base, tiles_x = base + kStages * kTileBytes;
+    const unsigned bars = smem_u32(s_bars);
+    auto loaded = [&](unsigned s) { return bars + 8 * s; };
+    auto empty = [&](unsigned s) { return bars + 8 * (kStages + s); };
+    auto filled = [&](unsigned k) { return bars + 8 * (2 * kStages + k); };
+    auto drained = [&](unsigned k) { return bars + 8 * (2 * kStages + 2 + k); };
+    const unsigned finished = bars + 8 * (2 * kStages + 4);
+    volatile int* gave_up = &s_gave_up;
+
+    if (threadIdx.x == 0) {
+        for (unsigned s = 0; s < kStages; ++s) {
+            mbar_init(loaded(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (unsigned k = 0; k < 2; ++k) {
+            mbar_init(filled(k), 1);
+            mbar_init(drained(k), CG * kStoreWarps);
+        }
+        mbar_init(finished, 1);
+        s_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    const unsigned tmem = tmem_alloc<CG>(&s_tmem, warp, kTmemCols);
+    const long long first_tile = blockIdx.x / CG, tile_stride = gridDim.x / CG;
+
+    if (warp == kProducerWarp) {
+        if (lane == 0) {
+            unsigned stage = 0, parity = 0;
+            bool ok = true;
+            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
+                const TilePos p(a, t);
+                const int k0 = p.kt * kSide + (int)rank * kCtaSide, c0 = p.ct * kSide + (int)rank * kCtaSide;
+                for (int step = p.first_step; step < p.last_step && ok; ++step) {
+#pragma unroll 1
+                    for (int plane = PLANES - 1; plane >= 0; --plane) {
+                        ok = mbar_wait(empty(stage), parity ^ 1, gave_up);
+                        if (!ok) break;
+                        const unsigned to = stage * kTileBytes, bar = CG == 2 ? in_cta(loaded(stage), 0) : loaded(stage);
+                        const int n0 = step * kStepRows;
+                        if (rank == 0) mbar_expect(loaded(stage), CG * 2 * kTileBytes);
+                        tma_load<CG>(tiles_g + to, &g_map, bar, k0, n0, p.sample, plane);
+                        tma_load<CG>(tiles_g + to + kBoxBytes, &g_map, bar, k0 + 64, n0, p.sample, plane);
+                        tma_load<CG>(tiles_x + to, &x_map, bar, c0, n0, p.sample, 0);
+                        tma_load<CG>(tiles_x + to + kBoxBytes, &x_map, bar, c0 + 64, n0, p.sample, 0);
+                        if (++stage == kStages) {
+                            stage = 0;
+                            parity ^= 1;
+                        }
+                    }
+                }
+            }
+            // Every stage loaded has been multiplied before the last accumulator is
+            // filled, which the storing warps wait for.  A CTA that gave up does not
+            // know which copies are in flight: it lets a millisecond pass.
+            if (!ok)
+                for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        }
+    } else if (warp == kMmaWarp) {
+        if (rank == 0 && lane == 0) {
+            // fp32 accumulators, bf16 operands, both MN-major
+            constexpr unsigned kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((unsigned)(kSide / 8) << 17) | ((unsigned)(kSide / 16) << 24);
+            unsigned stage = 0, parity = 0, acc = 0, acc_parity = 0;
+            bool ok = true;
+            for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
+                const TilePos p(a, t);
+                for (int step = p.first_step; step < p.last_step && ok; ++step) {
+                    if (PLANES > 1 || step == p.first_step) {
+                        ok = mbar_wait(drained(acc), acc_parity ^ 1, gave_up);
+                        if (!ok) break;
+                        fence_tcgen05_after();
+                    }
+#pragma unroll 1
+                    for (int plane = PLANES - 1; plane >= 0; --plane) {
+                        ok = mbar_wait(loaded(stage), parity, gave_up);
+                        if (!ok) break;
+                        fence_tcgen05_after();
+                        const unsigned long long dg = operand_desc(tiles_g + stage * kTileBytes), dx = operand_desc(tiles_x + stage * kTileBytes);
+                        const bool more = PLANES > 1 ? plane < PLANES - 1 : step > p.first_step;
+#pragma unroll
+                        for (int i = 0; i < kStepRows / 16; ++i)  // 16 tokens: two groups of eight, 2048 bytes
+                            tcgen05_mma<CG>(tmem + acc * kSide, dg + i * (2048 >> 4), dx + i * (2048 >> 4), kIdesc, more || i > 0);
+                        tcgen05_commit<CG>(empty(stage));
+                        if (++stage == kStages) {
+                            stage = 0;
+                            parity ^= 1;
+                        }
+                    }
+                    if (ok && (PLANES > 1 || step + 1 == p.last_step)) {
+                        tcgen05_commit<CG>(filled(acc));
+                        acc ^= 1;
+                        if (acc == 0) acc_parity ^= 1;
+                    }
+                }
+            }
+            // every product has finished before the memory it reads and writes is given up
+            asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(finished), "n"(CG) : "memory");
+            mbar_drain(finished, 0);
+        }
+    } else if (warp >= kStoreWarp) {
+        constexpr int kCols = kSide / (kStoreWarps / 4);  // columns of this warp
+        const unsigned quarter = warp % 4;                // TMEM lanes 32 * quarter .. + 31 are this warp's
+        const unsigned from = warp < kStoreWarp + 4 ? 0 : kCols;
+        float* patch = reinterpret_cast<float*>(raw_smem + (base - smem_u32(raw_smem)) + 2 * kStages * kTileBytes) + (warp - kStoreWarp) * kPatch;
+        unsigned acc = 0, acc_parity = 0;
+        bool ok = true;
+        for (long long t = first_tile; t < a.tiles; t += tile_stride) {
+            const TilePos p(a, t);
+            const long long k0 = (long long)p.kt * kSide + rank * kCtaSide + quarter * 32, c0 = (long long)p.ct * kSide + from;
+            OUT* row = static_cast<OUT*>(a.out) + (((long long)p.sample * a.splits + p.split) * a.outs + k0 + lane) * a.cols + c0;
+            const unsigned lanes = tmem + ((quarter * 32) << 16) + from;
+            if constexpr (PLANES == 1) {
+                if (ok) ok = mbar_wait(filled(acc), acc_parity, gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                fence_tcgen05_after();
+                for (int c = 0; c < kCols && c0 + c < a.cols; c += 32) {
+                    float v[32];
+                    __syncwarp();
+                    if (ok) {
+                        tmem_load32(lanes + acc * kSide + c, v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
+                    }
+                    store_patch(row + c, v, a.outs - k0, a.cols - c0 - c, a.cols, a.vec, patch, lane);
+                }
+                fence_tcgen05_before();
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive_cluster(CG == 2 ? in_cta(drained(acc), 0) : drained(acc));
+                acc ^= 1;
+                if (acc == 0) acc_parity ^= 1;
+            } else {
+                float sum[kCols / 32][32];
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum[c][i] = 0.0f;
+                for (int step = p.first_step; step < p.last_step && ok; ++step) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(filled(acc), acc_parity, gave_up));
+                    if (!ok) break;
+                    fence_tcgen05_after();
+#pragma unroll
+                    for (int c = 0; c < kCols / 16; ++c) {
+                        float v[16];
+                        __syncwarp();
+                        tmem_load16(lanes + acc * kSide + c * 16, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[c / 2][c % 2 * 16 + i] += v[i];
+                    }
+                    fence_tcgen05_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(CG == 2 ? in_cta(drained(acc), 0) : drained(acc));
+                    acc ^= 1;
+                    if (acc == 0) acc_parity ^= 1;
+                }
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    if (!ok) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[c][i] = __uint_as_float(0x7FC00000u);
+                    }
+                    if (c0 + c * 32 < a.cols) store_patch(row + c * 32, sum[c], a.outs - k0, a.cols - c0 - c * 32, a.cols, a.vec, patch, lane);
+                }
+            }
+        }
+    }
+    tmem_free<CG>(tmem, warp, kTmemCols);
+}
+
 // ---------------------------------------------------------------------------
-// gradients that TMA cannot read as they lie
+// small products
+
+constexpr int kSmallSide = 64, kSmallStep = 16;
+
+// A 64 x 64 tile of one sample's gradient per block, sixteen tokens at a time
+// through shared memory, fp32 products and sums.  The blocks of the first column
+// of tiles also sum the columns of gY.
+template <typename T, int FMT>
+__global__ void __launch_bounds__(256) small_product_kernel(const T* __restrict__ gy, long long ld_gy, const unsigned char* __restrict__ codes, long long ld_codes,
+                                                            const unsigned char* __restrict__ scales, long long ld_scales, long long rows, long long cols,
+                                                            long long outs, T* __restrict__ gw, T* __restrict__ gb) {
+    __shared__ float sg[kSmallStep][kSmallSide + 4], sx[kSmallStep][kSmallSide + 4];
+    const long long k0 = (long long)blockIdx.x * kSmallSide, c0 = (long long)blockIdx.y * kSmallSide, r = blockIdx.z;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    // this thread's part of a step: four gradient elements, and (half of the threads) eight codes
+    const int gn = threadIdx.x / 16, gk = threadIdx.x % 16;
+    const int xn = threadIdx.x / 8, xc = threadIdx.x % 8 * 8;
+    float g[4], x[8];
+    auto fetch = [&](long long n0) {
+        const T* p = gy + (r * rows + n0 + gn) * ld_gy + k0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = n0 + gn < rows && k0 + gk + 16 * i < outs ? load_elem(p + gk + 16 * i) : 0.0f;
+        if (threadIdx.x < kSmallStep * 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+            if (n0 + xn < rows && c0 + xc < cols) {
+                const long long row = r * rows + n0 + xn;
+                decode8<FMT>(__ldg(reinterpret_cast<const uint2*>(codes + row * ld_codes + c0 + xc)), x);
+                const float s = scale_of(__ldg(scales + row * ld_scales + (c0 + xc) / kGroup));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] *= s;
+            }
+        }
+    };
+    float acc[4][4] = {}, sum[4] = {};
+    const bool bias = gb && blockIdx.y == 0 && tx == 0;
+    fetch(0);
+    for (long long n0 = 0; n0 < rows; n0 += kSmallStep) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sg[gn][gk + 16 * i] = g[i];
+        if (threadIdx.x < kSmallStep * 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sx[xn][xc + i] = x[i];
+        }
+        __syncthreads();
+        if (n0 + kSmallStep < rows) fetch(n0 + kSmallStep);
+#pragma unroll
+        for (int n = 0; n < kSmallStep; ++n) {
+            const float4 u = *reinterpret_cast<const float4*>(&sg[n][ty * 4]), v = *reinterpret_cast<const float4*>(&sx[n][tx * 4]);
+            const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(uu[i], vv[j], acc[i][j]);
+            if (bias)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += uu[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long k = k0 + ty * 4 + i;
+        if (k >= outs) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c0 + tx * 4 + j < cols) store_elem(gw + (r * outs + k) * cols + c0 + tx * 4 + j, acc[i][j]);
+        if (bias) store_elem(gb + r * outs + k, sum[i]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// what a large product needs beforehand
 
 // fp32 -> three bf16 planes that add up to it exactly: the upper 8 significant
 // bits, the next 8, the last 8.  A value that is not finite keeps its kind in the
@@ -617,7 +565,8 @@ __device__ __forceinline__ void cut3(float g, unsigned short (&h)[3]) {
 }
 
 // Copies gY into rows of `pitch` (a multiple of 8) bf16, one plane for bf16, three
-// for fp32.  One pair of columns per thread.
+// for fp32: for gradients that TMA cannot read as they lie.  One pair of columns
+// per thread.
 template <typename T>
 __global__ void __launch_bounds__(256) lay_out_kernel(const T* __restrict__ g, long long ld, long long rows, long long cols, unsigned* __restrict__ out,
                                                       long long pitch) {
@@ -640,9 +589,6 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const T* __restrict__ g, l
     }
 }
 
-// ---------------------------------------------------------------------------
-// partial sums
-
 // out[r][i] = sum over the splits of part[r][s][i], in order.
 template <typename T>
 __global__ void __launch_bounds__(256) join_splits_kernel(const float* __restrict__ part, long long samples, int splits, long long n, T* __restrict__ out) {
@@ -655,36 +601,51 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* __restric
     }
 }
 
-// Partial column sums: block (x, y, r) sums rows y * 8 + lane, + 8 * gridDim.y, ... of
-// sample r for 32 columns.
-constexpr int kSumCols = 32, kSumWays = 8;
+// Column sums of gY, in parts: block (x, y, r) sums every gridDim.y-th run of
+// kSumRows rows of sample r for 256 columns.  Eight columns a thread; `part` has
+// one row per part, or `out` takes the sums if there is one part.
+constexpr int kSumCols = 256, kSumWays = 8, kSumRows = 64;
 
 template <typename T>
-__global__ void __launch_bounds__(kSumCols * kSumWays) column_sums_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols,
-                                                                          float* __restrict__ part) {
+__global__ void __launch_bounds__(256) column_sums_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols,
+                                                          float* __restrict__ part, T* __restrict__ out, bool vec) {
     __shared__ float sums[kSumWays][kSumCols];
-    const long long c = (long long)blockIdx.x * kSumCols + threadIdx.x;
+    const int cx = threadIdx.x % 32 * 8, way = threadIdx.x / 32;
+    const long long c = (long long)blockIdx.x * kSumCols + cx;
+    const int n_cols = (int)max(0LL, min(8LL, cols - c));
     for (long long r = blockIdx.z; r < samples; r += gridDim.z) {
-        float s = 0.0f;
-        if (c < cols)
-            for (long long n = (long long)blockIdx.y * kSumWays + threadIdx.y; n < rows; n += (long long)gridDim.y * kSumWays)
-                s += load_elem(g + (r * rows + n) * ld + c);
+        float s[8] = {};
+        if (n_cols > 0)
+            for (long long run = (long long)blockIdx.y * kSumRows; run < rows; run += (long long)gridDim.y * kSumRows) {
+                const long long last = min(rows, run + kSumRows);
+#pragma unroll 4
+                for (long long n = run + way; n < last; n += kSumWays) {
+                    Raw8<T> raw;
+                    if (vec)
+                        load8<true>(raw, g + (r * rows + n) * ld + c, n_cols);
+                    else
+                        load8<false>(raw, g + (r * rows + n) * ld + c, n_cols);
+                    float v[8];
+                    raw.values(v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i] += v[i];
+                }
+            }
         __syncthreads();
-        sums[threadIdx.y][threadIdx.x] = s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[way][cx + i] = s[i];
         __syncthreads();
-        if (threadIdx.y == 0 && c < cols) {
+        const long long col = (long long)blockIdx.x * kSumCols + threadIdx.x;
+        if (col < cols) {
             float t = 0.0f;
 #pragma unroll
             for (int k = 0; k < kSumWays; ++k) t += sums[k][threadIdx.x];
-            part[(r * gridDim.y + blockIdx.y) * cols + c] = t;
+            if (gridDim.y > 1)
+                part[(r * gridDim.y + blockIdx.y) * cols + col] = t;
+            else
+                store_elem(out + r * cols + col, t);
         }
     }
-}
-
-// Row parts of the column sums: about 64 rows to a thread.
-int sum_parts(long long rows) {
-    const long long p = (rows + 64 * kSumWays - 1) / (64 * kSumWays);
-    return (int)(p < 1 ? 1 : p > 256 ? 256 : p);
 }
 
 // ---------------------------------------------------------------------------
@@ -697,26 +658,34 @@ struct Problem {
     bool bias;
 };
 
-// How a product is run, and what its workspace holds: the copied gradient, the
-// partial products, the partial column sums, each at a multiple of 256 bytes.
+// How a product is run, and what its workspace holds: the copied gradient, X^ in
+// bf16, the partial products, the partial column sums, each at a multiple of 256
+// bytes.
 struct Plan {
-    bool copy, pair;
-    int planes, splits;
-    long long pitch;
-    int k_tiles, c_tiles, steps_per_plane, steps, steps_per_split;
+    bool small, copy, pair;
+    int planes, splits, sum_parts;
+    long long pitch, x_pitch;
+    int k_tiles, c_tiles, steps, steps_per_split;
     long long tiles;
-    long long at_part, at_sums, bytes;
+    long long at_x, at_part, at_sums, bytes;
 };
+
+// Products of at most this many tokens, and of no more 64 x 64 tiles than four per
+// SM, are small.
+constexpr long long kSmallRows = 256;
 
 long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 
 Plan make_plan(const Problem& q, int sms) {
-    Plan p;
+    Plan p = {};
+    const long long small_tiles = ((q.outs + kSmallSide - 1) / kSmallSide) * ((q.cols + kSmallSide - 1) / kSmallSide);
+    p.small = q.rows <= kSmallRows && small_tiles <= 65535 && q.samples <= 65535 && small_tiles * q.samples <= 4LL * sms;
+    if (p.small) return p;
     p.copy = q.dtype == AMPQ_F32 || !rows_aligned(q.gy, q.ld_gy, q.dtype);
     p.planes = q.dtype == AMPQ_F32 ? 3 : 1;
     p.pitch = p.copy ? round_up(q.outs, 8) : q.ld_gy;
-    p.steps_per_plane = (int)((q.rows + kStepRows - 1) / kStepRows);
-    p.steps = p.planes * p.steps_per_plane;
+    p.x_pitch = round_up(q.cols, 8);
+    p.steps = (int)((q.rows + kStepRows - 1) / kStepRows);
     const long long pairs = ((q.outs + 255) / 256) * ((q.cols + 255) / 256) * q.samples;
     p.pair = pairs * 2 >= sms;
     const int side = p.pair ? 256 : 128;
@@ -724,19 +693,26 @@ Plan make_plan(const Problem& q, int sms) {
     p.c_tiles = (int)((q.cols + side - 1) / side);
     const long long tiles = (long long)p.k_tiles * p.c_tiles * q.samples;
     const int units = p.pair ? sms / 2 : sms;
-    // few tiles and many tokens: several parts of the token axis per tile, at least eight stages each
+    // few tiles and many tokens: several parts of the token axis per tile, at least 512 tokens each
     long long splits = tiles > 0 && tiles < units ? units / tiles : 1;
     if (splits > p.steps / 8) splits = p.steps / 8;
     if (splits < 1) splits = 1;
     p.steps_per_split = p.steps > 0 ? (int)((p.steps + splits - 1) / splits) : 1;
     p.splits = p.steps > 0 ? (p.steps + p.steps_per_split - 1) / p.steps_per_split : 1;
     p.tiles = tiles * p.splits;
+    // about four blocks of column sums per SM
+    const long long sum_blocks = (q.outs + kSumCols - 1) / kSumCols * (q.samples > 0 ? q.samples : 1), runs = (q.rows + kSumRows - 1) / kSumRows;
+    long long parts = sum_blocks > 0 ? 4LL * sms / sum_blocks : 1;
+    if (parts > runs) parts = runs;
+    p.sum_parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
     long long at = 0;
     if (p.copy) at = round_up(2LL * p.planes * q.samples * q.rows * p.pitch, 256);
+    p.at_x = at;
+    at += round_up(2LL * q.samples * q.rows * p.x_pitch, 256);
     p.at_part = at;
     if (p.splits > 1) at += round_up(4LL * q.samples * p.splits * q.outs * q.cols, 256);
     p.at_sums = at;
-    if (q.bias) at += round_up(4LL * q.samples * sum_parts(q.rows) * q.outs, 256);
+    if (q.bias && p.sum_parts > 1) at += round_up(4LL * q.samples * p.sum_parts * q.outs, 256);
     p.bytes = at;
     return p;
 }
@@ -760,17 +736,18 @@ EncodeFn encode_fn() {
     return f;
 }
 
-// gY as [planes][samples][rows][outs]: 64 tokens x 64 columns per copy, zeros outside each sample.
-int gradient_map(CUtensorMap* map, const void* base, const Problem& q, const Plan& p) {
+// A bf16 matrix as [planes][samples][rows][cols], rows `pitch` elements apart: 64
+// tokens x 64 columns per copy, zeros outside each sample.
+int operand_map(CUtensorMap* map, const void* base, long long pitch, long long cols, const Problem& q, int planes) {
     const EncodeFn encode = encode_fn();
     if (!encode) return AMPQ_ERR_CUDA;
-    const unsigned long long row = 2ull * (unsigned long long)p.pitch;
+    const unsigned long long row = 2ull * (unsigned long long)pitch;
     unsigned long long sample = row * (unsigned long long)q.rows, plane = sample * (unsigned long long)q.samples;
     if (q.samples == 1) sample = row;  // never stepped over
-    if (p.planes == 1) plane = row;
+    if (planes == 1) plane = row;
     const unsigned long long limit = 1ull << 40;
     if (row >= limit || sample >= limit || plane >= limit) return AMPQ_ERR_TOO_LARGE;
-    const cuuint64_t dims[4] = {(cuuint64_t)q.outs, (cuuint64_t)q.rows, (cuuint64_t)q.samples, (cuuint64_t)p.planes};
+    const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)q.rows, (cuuint64_t)q.samples, (cuuint64_t)planes};
     const cuuint64_t strides[3] = {row, sample, plane};
     const cuuint32_t box[4] = {64, kStepRows, 1, 1}, one[4] = {1, 1, 1, 1};
     const CUresult rc = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, one,
@@ -779,74 +756,132 @@ int gradient_map(CUtensorMap* map, const void* base, const Problem& q, const Pla
     return rc == CUDA_SUCCESS ? AMPQ_OK : AMPQ_ERR_CUDA;
 }
 
-// The codes as [samples][rows][columns with codes]: 64 tokens x 128 columns per copy, zeros outside each sample.
-int code_map_of(CUtensorMap* map, const unsigned char* codes, long long ld_codes, const Problem& q) {
-    const EncodeFn encode = encode_fn();
-    if (!encode) return AMPQ_ERR_CUDA;
-    unsigned long long row = (unsigned long long)ld_codes, sample = row * (unsigned long long)q.rows;
-    if (q.samples == 1) sample = row;  // never stepped over
-    const unsigned long long limit = 1ull << 40;
-    if (row >= limit || sample >= limit) return AMPQ_ERR_TOO_LARGE;
-    const cuuint64_t dims[3] = {(cuuint64_t)round_up(q.cols, kGroup), (cuuint64_t)q.rows, (cuuint64_t)q.samples};
-    const cuuint64_t strides[2] = {row, sample};
-    const cuuint32_t box[3] = {kCtaCols, kStepRows, 1}, one[3] = {1, 1, 1};
-    const CUresult rc = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<unsigned char*>(codes), dims, strides, box, one,
-                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return rc == CUDA_SUCCESS ? AMPQ_OK : AMPQ_ERR_CUDA;
-}
+constexpr int kMaxDevices = 64;
 
-template <int CG, int FMT, typename OUT>
-int launch_product(const CUtensorMap& map, const CUtensorMap& code_map, const WgradArgs& a, int device, int sms, cudaStream_t st) {
-    constexpr int kMaxDevices = 64;
-    static std::atomic<bool> prepared[kMaxDevices];  // the attribute is set once per device and kernel
+using ProductKernel = void (*)(const CUtensorMap, const CUtensorMap, const ProductArgs);
+
+// One CTA (pair) per SM (two), no more than there are tiles.  `prepared`: on which
+// devices the kernel may use its shared memory already.
+int launch_persistent(ProductKernel kernel, std::atomic<bool>* prepared, int cg, int threads, int smem, const CUtensorMap& map, const CUtensorMap& second,
+                      const ProductArgs& a, int device, int sms, cudaStream_t st) {
     if (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire)) {
-        if (cudaFuncSetAttribute(wgrad_kernel<CG, FMT, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
             cudaGetLastError();
             return AMPQ_ERR_CUDA;
         }
         if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
     }
-    const long long units = sms / CG;
+    const long long units = sms / cg;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(CG * (a.tiles < units ? a.tiles : units)));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.gridDim = dim3((unsigned)(cg * (a.tiles < units ? a.tiles : units)));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.x = cg;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, wgrad_kernel<CG, FMT, OUT>, map, code_map, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kernel, map, second, a) != cudaSuccess) {
         cudaGetLastError();
         return AMPQ_ERR_CUDA;
     }
     return AMPQ_OK;
 }
 
-template <int FMT, typename OUT>
-int run_product(const CUtensorMap& map, const CUtensorMap& code_map, const WgradArgs& a, bool pair, int device, int sms, cudaStream_t st) {
-    return pair ? launch_product<2, FMT, OUT>(map, code_map, a, device, sms, st) : launch_product<1, FMT, OUT>(map, code_map, a, device, sms, st);
+template <int CG, int PLANES, typename OUT>
+int launch_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, int device, int sms, cudaStream_t st) {
+    static std::atomic<bool> prepared[kMaxDevices];
+    return launch_persistent(product_kernel<CG, PLANES, OUT>, prepared, CG, Roles<PLANES>::kThreads, Roles<PLANES>::kSmemBytes, g_map, x_map, a, device, sms, st);
 }
 
-template <typename T>
-int lay_out(const Problem& q, const Plan& p, void* out, cudaStream_t st) {
-    const long long rows = q.samples * q.rows, bx = (q.outs + 511) / 512;
-    const unsigned by = (unsigned)(rows < 65535 ? rows : 65535);
-    lay_out_kernel<T><<<dim3((unsigned)bx, by), 256, 0, st>>>(static_cast<const T*>(q.gy), q.ld_gy, rows, q.outs, static_cast<unsigned*>(out), p.pitch);
+template <int PLANES, typename OUT>
+int run_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, bool pair, int device, int sms, cudaStream_t st) {
+    return pair ? launch_product<2, PLANES, OUT>(g_map, x_map, a, device, sms, st) : launch_product<1, PLANES, OUT>(g_map, x_map, a, device, sms, st);
+}
+
+struct Operands {
+    const unsigned char *codes, *scales;
+    long long ld_codes, ld_scales;
+    int fmt;
+    void *gw, *gb;
+    unsigned char* ws;
+};
+
+template <typename T, int FMT>
+int run_small(const Problem& q, const Operands& o, cudaStream_t st) {
+    const dim3 grid((unsigned)((q.outs + kSmallSide - 1) / kSmallSide), (unsigned)((q.cols + kSmallSide - 1) / kSmallSide), (unsigned)q.samples);
+    small_product_kernel<T, FMT><<<grid, 256, 0, st>>>(static_cast<const T*>(q.gy), q.ld_gy, o.codes, o.ld_codes, o.scales, o.ld_scales, q.rows, q.cols, q.outs,
+                                                       static_cast<T*>(o.gw), static_cast<T*>(o.gb));
     return launched();
 }
 
 template <typename T>
-int bias_grad(const Problem& q, void* gb, float* part, cudaStream_t st) {
-    const int parts = sum_parts(q.rows);
+int run_large(const Problem& q, const Plan& p, const Operands& o, int device, int sms, cudaStream_t st) {
+    const long long rows = q.samples * q.rows;
+    int rc;
+    if (p.copy) {
+        const unsigned by = (unsigned)(rows < 65535 ? rows : 65535);
+        lay_out_kernel<T><<<dim3((unsigned)((q.outs + 511) / 512), by), 256, 0, st>>>(static_cast<const T*>(q.gy), q.ld_gy, rows, q.outs, reinterpret_cast<unsigned*>(o.ws), p.pitch);
+        if ((rc = launched())) return rc;
+    }
+    if ((rc = launch_ckpt_unpack(AMPQ_BF16, o.fmt, o.codes, o.ld_codes, o.scales, o.ld_scales, rows, q.cols, o.ws + p.at_x, p.x_pitch, st))) return rc;
+    CUtensorMap g_map, x_map;
+    if ((rc = operand_map(&g_map, p.copy ? o.ws : q.gy, p.pitch, q.outs, q, p.planes))) return rc;
+    if ((rc = operand_map(&x_map, o.ws + p.at_x, p.x_pitch, q.cols, q, 1))) return rc;
+    const bool partial = p.splits > 1;
+    ProductArgs a;
+    a.out = partial ? o.ws + p.at_part : o.gw;
+    a.cols = q.cols;
+    a.outs = q.outs;
+    a.tiles = p.tiles;
+    a.k_tiles = p.k_tiles;
+    a.c_tiles = p.c_tiles;
+    a.splits = p.splits;
+    a.steps = p.steps;
+    a.steps_per_split = p.steps_per_split;
+    a.vec = rows_aligned(a.out, q.cols, partial ? AMPQ_F32 : q.dtype);
+    constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+    rc = partial ? run_product<kPlanes, float>(g_map, x_map, a, p.pair, device, sms, st) : run_product<kPlanes, T>(g_map, x_map, a, p.pair, device, sms, st);
+    if (rc || !partial) return rc;
+    const long long n = q.outs * q.cols, blocks = (q.samples * n + 255) / 256;
+    join_splits_kernel<T><<<(unsigned)(blocks < 8LL * sms ? blocks : 8LL * sms), 256, 0, st>>>(reinterpret_cast<const float*>(o.ws + p.at_part), q.samples, p.splits, n,
+                                                                                               static_cast<T*>(o.gw));
+    return launched();
+}
+
+template <typename T>
+int bias_grad(const Problem& q, const Plan& p, const Operands& o, cudaStream_t st) {
+    float* part = reinterpret_cast<float*>(o.ws + p.at_sums);
     const unsigned bz = (unsigned)(q.samples < 65535 ? q.samples : 65535);
-    column_sums_kernel<T><<<dim3((unsigned)((q.outs + kSumCols - 1) / kSumCols), parts, bz), dim3(kSumCols, kSumWays), 0, st>>>(
-        static_cast<const T*>(q.gy), q.ld_gy, q.samples, q.rows, q.outs, part);
+    column_sums_kernel<T><<<dim3((unsigned)((q.outs + kSumCols - 1) / kSumCols), p.sum_parts, bz), 256, 0, st>>>(
+        static_cast<const T*>(q.gy), q.ld_gy, q.samples, q.rows, q.outs, part, static_cast<T*>(o.gb), rows_aligned(q.gy, q.ld_gy, q.dtype));
     const int rc = launched();
-    return rc ? rc : launch_join_columns(part, q.samples, parts, q.outs, gb, nullptr, q.dtype, st);
+    return rc || p.sum_parts == 1 ? rc : launch_join_columns(part, q.samples, p.sum_parts, q.outs, o.gb, nullptr, q.dtype, st);
+}
+
+template <typename T>
+int run(const Problem& q, const Plan& p, const Operands& o, int device, int sms, cudaStream_t st) {
+    if (q.rows > 0 && q.cols > 0) {
+        if (p.small) return o.fmt == AMPQ_FMT_E4M3 ? run_small<T, AMPQ_FMT_E4M3>(q, o, st) : run_small<T, AMPQ_FMT_E5M2>(q, o, st);
+        const int rc = run_large<T>(q, p, o, device, sms, st);
+        return rc || !o.gb ? rc : bias_grad<T>(q, p, o, st);
+    }
+    // no product: zeros, or no columns at all
+    bool ok = true;
+    if (q.rows == 0) {
+        if (q.cols > 0) ok = cudaMemsetAsync(o.gw, 0, (size_t)(q.samples * q.outs * q.cols) * sizeof(T), st) == cudaSuccess;
+        if (o.gb) ok = ok && cudaMemsetAsync(o.gb, 0, (size_t)(q.samples * q.outs) * sizeof(T), st) == cudaSuccess;
+    }
+    if (!ok) {
+        cudaGetLastError();
+        return AMPQ_ERR_CUDA;
+    }
+    if (q.rows == 0 || !o.gb) return AMPQ_OK;
+    Plan one = p;
+    one.sum_parts = 1;
+    return bias_grad<T>(q, one, o, st);
 }
 
 int check_sizes(int dtype, long long samples, long long rows, long long cols, long long outs) {
@@ -874,7 +909,7 @@ int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void* gy, long 
     if (cur.status) return cur.status;
     const int sms = sm_count(device);
     if (sms < 2) return AMPQ_ERR_CUDA;
-    *bytes = make_plan(Problem{dtype, gy, ld_gy, samples, rows, cols, outs, bias != 0}, sms).bytes;
+    *bytes = rows > 0 && cols > 0 ? make_plan(Problem{dtype, gy, ld_gy, samples, rows, cols, outs, bias != 0}, sms).bytes : 0;
     return AMPQ_OK;
 }
 
@@ -894,61 +929,11 @@ int ampq_ckpt_weight_grad(int device, void* cuda_stream, int dtype, int fmt, con
     const int sms = sm_count(device);
     if (sms < 2) return AMPQ_ERR_CUDA;
     const Problem q{dtype, gy, ld_gy, samples, rows, cols, outs, gb != nullptr};
-    const Plan p = make_plan(q, sms);
-    if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return AMPQ_ERR_INVALID;
+    Plan p = make_plan(q, sms);
+    if (rows > 0 && cols > 0 && p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return AMPQ_ERR_INVALID;
+    const Operands o{codes, scales, ld_codes, ld_scales, fmt, gw, gb, static_cast<unsigned char*>(workspace)};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    unsigned char* ws = static_cast<unsigned char*>(workspace);
-    if (rows == 0) {
-        if (cols > 0 && cudaMemsetAsync(gw, 0, (size_t)(samples * outs * cols) * elem_bytes(dtype), st) != cudaSuccess) {
-            cudaGetLastError();
-            return AMPQ_ERR_CUDA;
-        }
-    } else if (cols > 0) {
-        if (p.copy) {
-            rc = dtype == AMPQ_F32 ? lay_out<float>(q, p, ws, st) : lay_out<__nv_bfloat16>(q, p, ws, st);
-            if (rc) return rc;
-        }
-        CUtensorMap map, code_map;
-        rc = gradient_map(&map, p.copy ? ws : gy, q, p);
-        if (!rc) rc = code_map_of(&code_map, codes, ld_codes, q);
-        if (rc) return rc;
-        const bool partial = p.splits > 1, f32 = partial || dtype == AMPQ_F32;
-        WgradArgs a;
-        a.scales = scales;
-        a.out = partial ? ws + p.at_part : gw;
-        a.ld_scales = ld_scales;
-        a.cols = cols;
-        a.outs = outs;
-        a.rows = rows;
-        a.tiles = p.tiles;
-        a.k_tiles = p.k_tiles;
-        a.c_tiles = p.c_tiles;
-        a.splits = p.splits;
-        a.steps_per_plane = p.steps_per_plane;
-        a.steps = p.steps;
-        a.steps_per_split = p.steps_per_split;
-        a.scale_words = aligned_to(scales, 4) && ld_scales % 4 == 0;
-        a.vec = rows_aligned(a.out, cols, f32 ? AMPQ_F32 : AMPQ_BF16);
-        if (fmt == AMPQ_FMT_E4M3)
-            rc = f32 ? run_product<AMPQ_FMT_E4M3, float>(map, code_map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E4M3, __nv_bfloat16>(map, code_map, a, p.pair, device, sms, st);
-        else
-            rc = f32 ? run_product<AMPQ_FMT_E5M2, float>(map, code_map, a, p.pair, device, sms, st) : run_product<AMPQ_FMT_E5M2, __nv_bfloat16>(map, code_map, a, p.pair, device, sms, st);
-        if (rc) return rc;
-        if (partial) {
-            const long long n = outs * cols, blocks = (samples * n + 255) / 256;
-            const unsigned grid = (unsigned)(blocks < 8LL * sms ? blocks : 8LL * sms);
-            const float* part = reinterpret_cast<const float*>(ws + p.at_part);
-            if (dtype == AMPQ_F32)
-                join_splits_kernel<float><<<grid, 256, 0, st>>>(part, samples, p.splits, n, static_cast<float*>(gw));
-            else
-                join_splits_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(part, samples, p.splits, n, static_cast<__nv_bfloat16*>(gw));
-            rc = launched();
-            if (rc) return rc;
-        }
-    }
-    if (!gb) return AMPQ_OK;
-    float* part = reinterpret_cast<float*>(ws + p.at_sums);
-    return dtype == AMPQ_F32 ? bias_grad<float>(q, gb, part, st) : bias_grad<__nv_bfloat16>(q, gb, part, st);
+    return dtype == AMPQ_F32 ? run<float>(q, p, o, device, sms, st) : run<__nv_bfloat16>(q, p, o, device, sms, st);
 }
 
 #pragma GCC visibility pop
