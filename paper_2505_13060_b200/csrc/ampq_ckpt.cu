@@ -8,8 +8,11 @@ namespace ampq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;                                     // vectors of eight a thread has in flight
-constexpr int kGroupsPerBlock = kThreads / 4 * kUnroll;        // four threads per group
+constexpr int kUnroll = 4;  // chunks a thread has in flight
+
+// Groups of one block: 32 bytes of x to a thread.
+template <typename T>
+constexpr int kGroupsPerBlock = kThreads / Chunk<T>::kLanes * kUnroll;
 
 // n / d for n < 2^31 by a multiplication: magic = floor(2^(31+s)/d) + 1 with 2^s >= d.
 struct FastDiv {
@@ -24,9 +27,9 @@ struct FastDiv {
     __device__ __forceinline__ unsigned operator()(unsigned n) const { return d <= 1 ? n : __umulhi(n, magic) >> shift; }
 };
 
-// The group that a thread's vector belongs to: groups are numbered row by row,
-// a block takes kGroupsPerBlock of them, four threads share one.  The 64-bit
-// division is done once per block.
+// The group that a thread's chunk belongs to: groups are numbered row by row and
+// a block takes kGroupsPerBlock of them.  The 64-bit division is done once per
+// block.
 struct Place {
     long long row;
     unsigned group;
@@ -35,8 +38,8 @@ struct Place {
 struct BlockStart {
     long long row0;
     unsigned group0;
-    __device__ __forceinline__ BlockStart(unsigned groups) {
-        const long long first = (long long)blockIdx.x * kGroupsPerBlock;
+    __device__ __forceinline__ BlockStart(unsigned groups, int per_block) {
+        const long long first = (long long)blockIdx.x * per_block;
         row0 = first / groups;
         group0 = (unsigned)(first - row0 * groups);
     }
@@ -47,75 +50,69 @@ struct BlockStart {
     }
 };
 
-// One read of x, one write of codes and scale bytes: bound by HBM.  A thread
-// holds eight consecutive columns (one 16-byte load of bf16, two of fp32), four
-// lanes a group, so the group's maximum is two shuffles.
-template <typename T, int FMT, bool VEC>
+// One read of x, one write of codes and scale bytes: bound by HBM.  A thread holds
+// 32 bytes of a row; two (bf16) or four (fp32) lanes make a group, so the group's
+// maximum is one or two shuffles.
+template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) pack_kernel(const T* __restrict__ x, long long rows, unsigned cols, long long ld,
                                                         unsigned groups, FastDiv div, unsigned char* __restrict__ codes, long long ld_codes,
                                                         unsigned char* __restrict__ scales, long long ld_scales) {
-    const BlockStart start(groups);
-    Raw8<T> raw[kUnroll];
+    using K = Chunk<T>;
+    const BlockStart start(groups, kGroupsPerBlock<T>);
+    unsigned w[kUnroll][8];
     Place pl[kUnroll];
-    const unsigned lane4 = threadIdx.x & 3;
+    const unsigned part = threadIdx.x % K::kLanes;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        pl[u] = start.at(u * (kThreads / 4) + threadIdx.x / 4, groups, div);
-        const unsigned c0 = pl[u].group * kGroup + lane4 * 8;
-        const int n = pl[u].row < rows ? max(0, min(8, (int)cols - (int)c0)) : 0;
-        if (n > 0)
-            load8<VEC>(raw[u], x + pl[u].row * ld + c0, n);
-        else
-            raw[u].zero();
+        pl[u] = start.at((u * kThreads + threadIdx.x) / K::kLanes, groups, div);
+        const int c0 = (int)(pl[u].group * kGroup + part * K::kElems);
+        const int n = pl[u].row < rows ? min(K::kElems, (int)cols - c0) : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[u][i] = 0;
+        if (n > 0) K::load_words(x + pl[u].row * ld + c0, n, w[u]);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        float v[8];
-        raw[u].values(v);
-        unsigned m = amax_bits8(v);
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-        const unsigned byte = scale_byte<FMT>(m);
-        const uint2 c = encode_group8<FMT>(v, byte);
+        K k;
+        k.from_words(w[u]);
+        const unsigned byte = scale_byte<FMT>(k.group_amax());
+        unsigned c[K::kElems / 4];
+        k.template encode<FMT>(byte, c);
         if (pl[u].row < rows) {
-            *reinterpret_cast<uint2*>(codes + pl[u].row * ld_codes + pl[u].group * kGroup + lane4 * 8) = c;
-            if (lane4 == 0) scales[pl[u].row * ld_scales + pl[u].group] = (unsigned char)byte;
+            store_codes(codes + pl[u].row * ld_codes + pl[u].group * kGroup + part * K::kElems, c);
+            if (part == 0) scales[pl[u].row * ld_scales + pl[u].group] = (unsigned char)byte;
         }
     }
 }
 
-template <typename T, int FMT, bool VEC>
+template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads) unpack_kernel(const unsigned char* __restrict__ codes, long long ld_codes,
                                                           const unsigned char* __restrict__ scales, long long ld_scales, long long rows,
                                                           unsigned cols, unsigned groups, FastDiv div, T* __restrict__ out, long long ld) {
-    const BlockStart start(groups);
-    uint2 c[kUnroll];
+    using K = Chunk<T>;
+    const BlockStart start(groups, kGroupsPerBlock<T>);
+    unsigned c[kUnroll][K::kElems / 4];
     unsigned byte[kUnroll];
     Place pl[kUnroll];
-    const unsigned lane4 = threadIdx.x & 3;
+    const unsigned part = threadIdx.x % K::kLanes;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        pl[u] = start.at(u * (kThreads / 4) + threadIdx.x / 4, groups, div);
-        c[u] = make_uint2(0, 0);
+        pl[u] = start.at((u * kThreads + threadIdx.x) / K::kLanes, groups, div);
         byte[u] = 127;
         if (pl[u].row < rows) {
-            c[u] = __ldg(reinterpret_cast<const uint2*>(codes + pl[u].row * ld_codes + pl[u].group * kGroup + lane4 * 8));
+            load_codes(codes + pl[u].row * ld_codes + pl[u].group * kGroup + part * K::kElems, c[u]);
             byte[u] = __ldg(scales + pl[u].row * ld_scales + pl[u].group);
         }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        const unsigned c0 = pl[u].group * kGroup + lane4 * 8;
-        const int n = pl[u].row < rows ? max(0, min(8, (int)cols - (int)c0)) : 0;
+        const int c0 = (int)(pl[u].group * kGroup + part * K::kElems);
+        const int n = pl[u].row < rows ? min(K::kElems, (int)cols - c0) : 0;
         if (n <= 0) continue;
-        float v[8];
-        decode8<FMT>(c[u], v);
-        const float p = scale_of(byte[u]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= p;
-        Raw8<T> r;
-        r.set(v);
-        store8<VEC>(r, out + pl[u].row * ld + c0, n);
+        K k;
+        k.template decode<FMT>(c[u]);
+        k.scale(scale_of(byte[u]));
+        k.store(out + pl[u].row * ld + c0, n);
     }
 }
 
@@ -147,14 +144,10 @@ template <typename T, int FMT>
 int launch_pack(const void* x, long long rows, long long cols, long long ld, unsigned char* codes, long long ld_codes,
                 unsigned char* scales, long long ld_scales, cudaStream_t st) {
     const unsigned groups = (unsigned)((cols + kGroup - 1) / kGroup);
-    const long long blocks = (rows * groups + kGroupsPerBlock - 1) / kGroupsPerBlock;
+    const long long blocks = (rows * groups + kGroupsPerBlock<T> - 1) / kGroupsPerBlock<T>;
     if (blocks > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    const int dtype = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
-    const T* p = static_cast<const T*>(x);
-    if (rows_aligned(x, ld, dtype))
-        pack_kernel<T, FMT, true><<<(unsigned)blocks, kThreads, 0, st>>>(p, rows, (unsigned)cols, ld, groups, FastDiv(groups), codes, ld_codes, scales, ld_scales);
-    else
-        pack_kernel<T, FMT, false><<<(unsigned)blocks, kThreads, 0, st>>>(p, rows, (unsigned)cols, ld, groups, FastDiv(groups), codes, ld_codes, scales, ld_scales);
+    pack_kernel<T, FMT><<<(unsigned)blocks, kThreads, 0, st>>>(static_cast<const T*>(x), rows, (unsigned)cols, ld, groups, FastDiv(groups), codes, ld_codes,
+                                                               scales, ld_scales);
     return launched();
 }
 
@@ -162,14 +155,10 @@ template <typename T, int FMT>
 int launch_unpack(const unsigned char* codes, long long ld_codes, const unsigned char* scales, long long ld_scales, long long rows,
                   long long cols, void* out, long long ld, cudaStream_t st) {
     const unsigned groups = (unsigned)((cols + kGroup - 1) / kGroup);
-    const long long blocks = (rows * groups + kGroupsPerBlock - 1) / kGroupsPerBlock;
+    const long long blocks = (rows * groups + kGroupsPerBlock<T> - 1) / kGroupsPerBlock<T>;
     if (blocks > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    const int dtype = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
-    T* p = static_cast<T*>(out);
-    if (rows_aligned(out, ld, dtype))
-        unpack_kernel<T, FMT, true><<<(unsigned)blocks, kThreads, 0, st>>>(codes, ld_codes, scales, ld_scales, rows, (unsigned)cols, groups, FastDiv(groups), p, ld);
-    else
-        unpack_kernel<T, FMT, false><<<(unsigned)blocks, kThreads, 0, st>>>(codes, ld_codes, scales, ld_scales, rows, (unsigned)cols, groups, FastDiv(groups), p, ld);
+    unpack_kernel<T, FMT><<<(unsigned)blocks, kThreads, 0, st>>>(codes, ld_codes, scales, ld_scales, rows, (unsigned)cols, groups, FastDiv(groups),
+                                                                 static_cast<T*>(out), ld);
     return launched();
 }
 

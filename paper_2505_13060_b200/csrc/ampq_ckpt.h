@@ -58,20 +58,6 @@ __device__ __forceinline__ float inv_scale_of(unsigned byte) { return __uint_as_
 // 2^e of a scale byte, NaN for the NaN byte.
 __device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte == kNanScale ? 0x7FC00000u : byte << 23); }
 
-// Eight scaled elements -> eight codes (element 0 in the lowest byte).
-template <int FMT>
-__device__ __forceinline__ uint2 encode8(const float (&y)[8]) {
-    unsigned short h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (FMT == AMPQ_FMT_E4M3)
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
-        else
-            asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
-    }
-    return make_uint2(h[0] | ((unsigned)h[1] << 16), h[2] | ((unsigned)h[3] << 16));
-}
-
 // Eight codes -> their exact values, not yet multiplied by the group's scale.
 template <int FMT>
 __device__ __forceinline__ void decode8(uint2 c, float (&v)[8]) {
@@ -172,23 +158,171 @@ __device__ __forceinline__ void store8(const Raw8<T>& r, T* p, int n) {
         if (i < n) store_elem(p + i, v[i]);
 }
 
-// Largest absolute value's bits of eight elements.
-__device__ __forceinline__ unsigned amax_bits8(const float (&v)[8]) {
-    unsigned m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return m;
-}
+// ---------------------------------------------------------------------------
+// chunks: 32 consecutive bytes of a row, 16 bf16 or 8 fp32, one thread's share
 
-// Encodes eight elements whose group's scale byte is known.
-template <int FMT>
-__device__ __forceinline__ uint2 encode_group8(const float (&v)[8], unsigned byte) {
-    const float inv = inv_scale_of(byte);
-    float y[8];
+template <typename T>
+struct Chunk {
+    static constexpr int kElems = 32 / (int)sizeof(T);
+    static constexpr int kLanes = kGroup / kElems;  // neighbouring lanes that make a group
+    float2 v[kElems / 2];
+
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = v[i] * inv;
-    const uint2 c = encode8<FMT>(y);
-    return byte == kNanScale ? make_uint2(0, 0) : c;
+        for (int i = 0; i < kElems / 2; ++i) v[i] = make_float2(0.0f, 0.0f);
+    }
+    // From the eight words of the chunk.
+    __device__ __forceinline__ void from_words(const unsigned (&w)[8]) {
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < kElems / 2; ++i) v[i] = make_float2(__uint_as_float(w[(2 * i) & 7]), __uint_as_float(w[(2 * i + 1) & 7]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kElems / 2; ++i) v[i] = make_float2(__uint_as_float(w[i & 7] << 16), __uint_as_float(w[i & 7] & 0xFFFF0000u));
+        }
+    }
+    __device__ __forceinline__ void to_words(unsigned (&w)[8]) const {
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(i & 1 ? v[(i / 2) % (kElems / 2)].y : v[(i / 2) % (kElems / 2)].x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[i % (kElems / 2)].x, v[i % (kElems / 2)].y);
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? v[i / 2].y : v[i / 2].x; }
+    // The words of the first n (<= kElems) elements at p, zeros behind them.  Whole
+    // chunks on 16-byte boundaries are two loads, others on 4-byte boundaries eight;
+    // bf16 rows that start between two words take their pairs from neighbouring
+    // words, of which the outermost two halves are read on their own.
+    __device__ static __forceinline__ void load_words(const T* p, int n, unsigned (&w)[8]) {
+        const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15);
+        if (n < kElems) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (sizeof(T) == 4) {
+                    w[i] = i < n ? __ldg(reinterpret_cast<const unsigned*>(p) + i) : 0u;
+                } else {
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+                    w[i] = 2 * i < n ? __ldg(h + 2 * i) : 0u;
+                    if (2 * i + 1 < n) w[i] |= (unsigned)__ldg(h + 2 * i + 1) << 16;
+                }
+            }
+        } else if (off == 0) {
+            const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+            w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        } else if ((off & 3) == 0) {
+            const unsigned* q = reinterpret_cast<const unsigned*>(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __ldg(q + i);
+        } else {  // bf16 only
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+            const unsigned* q = reinterpret_cast<const unsigned*>(h + 1);
+            unsigned u = (unsigned)__ldg(h) << 16;
+#pragma unroll
+            for (int i = 0; i < 7; ++i) {
+                const unsigned next = __ldg(q + i);
+                w[i] = __funnelshift_r(u, next, 16);
+                u = next;
+            }
+            w[7] = __funnelshift_r(u, (unsigned)__ldg(h + 15), 16);
+        }
+    }
+    __device__ __forceinline__ void load(const T* p, int n) {
+        unsigned w[8];
+        load_words(p, n, w);
+        from_words(w);
+    }
+    __device__ __forceinline__ void store(T* p, int n) const {
+        const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15);
+        if (n < kElems) {
+#pragma unroll
+            for (int i = 0; i < kElems; ++i)
+                if (i < n) store_elem(p + i, at(i));
+            return;
+        }
+        unsigned w[8];
+        to_words(w);
+        if (off == 0) {
+            reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        } else if ((off & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) reinterpret_cast<unsigned*>(p)[i] = w[i];
+        } else {
+            unsigned short* h = reinterpret_cast<unsigned short*>(p);
+            unsigned* q = reinterpret_cast<unsigned*>(h + 1);
+            h[0] = (unsigned short)w[0];
+#pragma unroll
+            for (int i = 0; i < 7; ++i) q[i] = __funnelshift_r(w[i], w[i + 1], 16);
+            h[15] = (unsigned short)(w[7] >> 16);
+        }
+    }
+    // Bits of the largest absolute value of the group this chunk is part of; a NaN
+    // comes out on top.  All lanes of the warp call it.
+    __device__ __forceinline__ unsigned group_amax() const {
+        float m = fabsf(v[0].x);
+#pragma unroll
+        for (int i = 0; i < kElems / 2; ++i) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[i].x), "f"(v[i].y));
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__shfl_xor_sync(0xFFFFFFFFu, m, o)));
+        return __float_as_uint(m) & 0x7FFFFFFFu;
+    }
+    // Codes of the chunk under a scale byte, element 0 in the lowest byte.
+    template <int FMT>
+    __device__ __forceinline__ void encode(unsigned byte, unsigned (&c)[kElems / 4]) const {
+        const float inv = inv_scale_of(byte);
+#pragma unroll
+        for (int i = 0; i < kElems / 4; ++i) {
+            const float2 a = __fmul2_rn(v[2 * i], make_float2(inv, inv)), b = __fmul2_rn(v[2 * i + 1], make_float2(inv, inv));
+            unsigned short lo, hi;
+            if (FMT == AMPQ_FMT_E4M3) {
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(a.y), "f"(a.x));
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(b.y), "f"(b.x));
+            } else {
+                asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(a.y), "f"(a.x));
+                asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(b.y), "f"(b.x));
+            }
+            c[i] = byte == kNanScale ? 0u : (unsigned)lo | (unsigned)hi << 16;
+        }
+    }
+    // The chunk's codes, not yet multiplied by the scale.
+    template <int FMT>
+    __device__ __forceinline__ void decode(const unsigned (&c)[kElems / 4]) {
+#pragma unroll
+        for (int i = 0; i < kElems / 2; ++i) {
+            const unsigned short h = (unsigned short)(c[i / 2] >> (16 * (i & 1)));
+            unsigned r;
+            if (FMT == AMPQ_FMT_E4M3)
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(h));
+            else
+                asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(r) : "h"(h));
+            v[i] = __half22float2(*reinterpret_cast<__half2*>(&r));
+        }
+    }
+    __device__ __forceinline__ void scale(float p) {
+#pragma unroll
+        for (int i = 0; i < kElems / 2; ++i) v[i] = __fmul2_rn(v[i], make_float2(p, p));
+    }
+};
+
+template <int N>
+__device__ __forceinline__ void load_codes(const unsigned char* p, unsigned (&c)[N]) {
+    if (N == 4) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+        c[0] = q.x; c[1] = q.y; c[2 % N] = q.z; c[3 % N] = q.w;
+    } else {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+        c[0] = q.x; c[1] = q.y;
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_codes(unsigned char* p, const unsigned (&c)[N]) {
+    if (N == 4)
+        *reinterpret_cast<uint4*>(p) = make_uint4(c[0], c[1], c[2 % N], c[3 % N]);
+    else
+        *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
 }
 
 // ---------------------------------------------------------------------------

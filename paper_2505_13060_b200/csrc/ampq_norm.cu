@@ -3,6 +3,7 @@
 // input written by the forward pass and read by the backward pass.
 #include "ampq_ckpt.h"
 
+#include <atomic>
 #include <cmath>
 
 namespace ampq {
@@ -10,28 +11,12 @@ namespace {
 
 constexpr int kMaxNormCols = AMPQ_NORM_MAX_COLS;
 
-// Eight elements of a parameter vector, in fp32.  p: float or bf16 by `bf16`;
-// vec: 16-byte aligned.
-__device__ __forceinline__ void load_param8(const void* p, bool bf16, bool vec, int c0, int n, float (&v)[8]) {
-    if (bf16) {
-        Raw8<__nv_bfloat16> r;
-        if (vec)
-            load8<true>(r, static_cast<const __nv_bfloat16*>(p) + c0, n);
-        else
-            load8<false>(r, static_cast<const __nv_bfloat16*>(p) + c0, n);
-        r.values(v);
-    } else {
-        Raw8<float> r;
-        if (vec)
-            load8<true>(r, static_cast<const float*>(p) + c0, n);
-        else
-            load8<false>(r, static_cast<const float*>(p) + c0, n);
-        r.values(v);
-    }
-}
+// One thread holds 16 elements of a row: one chunk of bf16 or two of fp32.
+template <typename T>
+constexpr int kChunks = 16 / Chunk<T>::kElems;
 
-// Sum of one value (two) over the WPR warps of a row group; every thread of the
-// CTA calls it.  The order is fixed.
+// Sums N values over the WPR warps of a row group; every thread of the CTA calls
+// it.  The order is fixed.
 template <int WPR, int N>
 __device__ __forceinline__ void row_sum(float (&s)[N], float* red, int warp) {
 #pragma unroll
@@ -39,18 +24,18 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* red, int warp) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], o);
     if (WPR == 1) return;
-    __syncthreads();  // red is free again
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
         for (int k = 0; k < N; ++k) red[warp * N + k] = s[k];
     __syncthreads();
-    const int first = warp / WPR * WPR;
+    // 32 lanes take one warp's sum each and add them up as before
+    const int first = warp / WPR * WPR, lane = threadIdx.x & 31;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        float t = 0.0f;
+        float t = lane < WPR ? red[(first + lane) * N + k] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < WPR; ++i) t += red[(first + i) * N + k];
-        s[k] = t;
+        for (int o = WPR / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+        s[k] = __shfl_sync(0xFFFFFFFFu, t, 0);
     }
 }
 
@@ -59,7 +44,32 @@ struct Shape {
     static constexpr int kWarps = WPR < 8 ? 8 : WPR;   // warps of a CTA
     static constexpr int kGroups = kWarps / WPR;       // rows a CTA works on at a time
     static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kSpan = 512 * WPR;            // most columns of a row
 };
+
+// 16 elements of a parameter vector in fp32, as pairs.
+template <typename T>
+__device__ __forceinline__ void load_params(const void* p, bool bf16, int c0, int n, Chunk<T>& k) {
+    constexpr int E = Chunk<T>::kElems;
+    if (bf16 == (sizeof(T) == 2)) {
+        k.load(static_cast<const T*>(p) + c0, n);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+        float2 f = make_float2(0.0f, 0.0f);
+        if (bf16) {
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p) + c0;
+            if (2 * i < n) f.x = load_elem(q + 2 * i);
+            if (2 * i + 1 < n) f.y = load_elem(q + 2 * i + 1);
+        } else {
+            const float* q = static_cast<const float*>(p) + c0;
+            if (2 * i < n) f.x = load_elem(q + 2 * i);
+            if (2 * i + 1 < n) f.y = load_elem(q + 2 * i + 1);
+        }
+        k.v[i] = f;
+    }
+}
 
 struct ForwardArgs {
     const void *x, *w, *b;
@@ -69,102 +79,91 @@ struct ForwardArgs {
     long long rows, ld_x, ld_y, ld_codes, ld_scales;
     int cols;
     float eps;
-    bool layer, param_bf16, vec_x, vec_y, vec_p;
+    bool layer, param_bf16;
 };
 
-// One row per group of WPR warps, held in registers between the statistics (two
-// passes over the registers: mean, then the sum of squared differences) and the
-// output, so x is read once.  Lane l of the group holds columns
-// (j * threads + l) * 8 .. + 7: loads are contiguous and four neighbouring lanes
-// make one group of the checkpoint.
-template <typename T, int FMT, int WPR, int V>
-__global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_forward_kernel(const ForwardArgs a) {
+// One row per group of WPR warps, held in registers between the statistics (mean,
+// then the sum of squared differences from it) and the output, so x is read once.
+// Thread t of a group holds the chunks (j * threads + t): loads are contiguous
+// and neighbouring lanes make the groups of the checkpoint.
+template <typename T, int FMT, int WPR>
+__global__ void __launch_bounds__(Shape<WPR>::kThreads, 2048 / Shape<WPR>::kThreads > 4 ? 4 : 1) norm_forward_kernel(const ForwardArgs a) {
     using S = Shape<WPR>;
-    __shared__ float red[S::kWarps];
+    using K = Chunk<T>;
+    constexpr int V = kChunks<T>, E = K::kElems;
+    __shared__ float red[2][S::kWarps];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
     const long long row = (long long)blockIdx.x * S::kGroups + warp / WPR;
     const bool live = row < a.rows;
     const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    Raw8<T> raw[V];
+    K k[V];
     int n[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int c0 = (j * 32 * WPR + t) * 8;
-        n[j] = live ? max(0, min(8, a.cols - c0)) : 0;
-        if (n[j] <= 0)
-            raw[j].zero();
-        else if (a.vec_x)
-            load8<true>(raw[j], x + c0, n[j]);
-        else
-            load8<false>(raw[j], x + c0, n[j]);
+        const int c0 = (j * 32 * WPR + t) * E;
+        n[j] = live ? min(E, a.cols - c0) : 0;
+        k[j].zero();
+        if (n[j] > 0) k[j].load(x + c0, n[j]);
     }
-    const float cols = (float)a.cols;
+    const float inv_cols = 1.0f / (float)a.cols;
     float mean = 0.0f;
     if (a.layer) {
-        float s[1] = {0.0f};
+        float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float v[8];
-            raw[j].values(v);
+        for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += v[i];
-        }
-        row_sum<WPR, 1>(s, red, warp);
-        mean = s[0] / cols;
+            for (int i = 0; i < E / 2; ++i) s2 = __fadd2_rn(s2, k[j].v[i]);
+        float s[1] = {s2.x + s2.y};
+        row_sum<WPR, 1>(s, red[0], warp);
+        mean = s[0] * inv_cols;
     }
-    float q[1] = {0.0f};
+    const float2 minus = make_float2(-mean, -mean);
+    float2 q2 = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        float v[8];
-        raw[j].values(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = i < n[j] ? v[i] - mean : 0.0f;
-            q[0] = fmaf(d, d, q[0]);
+        for (int i = 0; i < E / 2; ++i) {
+            float2 d = __fadd2_rn(k[j].v[i], minus);
+            if (n[j] < E) d = make_float2(2 * i < n[j] ? d.x : 0.0f, 2 * i + 1 < n[j] ? d.y : 0.0f);
+            q2 = __ffma2_rn(d, d, q2);
         }
     }
-    row_sum<WPR, 1>(q, red, warp);
-    const float rstd = 1.0f / sqrtf(q[0] / cols + a.eps);
+    float q[1] = {q2.x + q2.y};
+    row_sum<WPR, 1>(q, red[1], warp);
+    const float rstd = 1.0f / sqrtf(q[0] * inv_cols + a.eps);
     if (live && t == 0) {
         if (a.layer) a.mean[row] = mean;
         a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int c0 = (j * 32 * WPR + t) * 8;
-        float v[8];
-        raw[j].values(v);
+        const int c0 = (j * 32 * WPR + t) * E;
         if (FMT != AMPQ_FMT_BASE) {
             constexpr int F = FMT == AMPQ_FMT_BASE ? AMPQ_FMT_E4M3 : FMT;
-            unsigned m = amax_bits8(v);
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-            const unsigned byte = scale_byte<F>(m);
-            const uint2 c = encode_group8<F>(v, byte);
+            const unsigned byte = scale_byte<F>(k[j].group_amax());
             if (live && (c0 & ~(kGroup - 1)) < a.cols) {  // whole groups: the columns behind the last are stored as 0
-                *reinterpret_cast<uint2*>(a.codes + row * a.ld_codes + c0) = c;
-                if ((t & 3) == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
+                unsigned c[E / 4];
+                k[j].template encode<F>(byte, c);
+                store_codes(a.codes + row * a.ld_codes + c0, c);
+                if (t % K::kLanes == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
             }
         }
         if (n[j] <= 0) continue;
-        float w[8], b[8];
-        if (a.w) load_param8(a.w, a.param_bf16, a.vec_p, c0, n[j], w);
-        if (a.b) load_param8(a.b, a.param_bf16, a.vec_p, c0, n[j], b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float h = (v[i] - mean) * rstd;
-            if (a.w) h *= w[i];
-            if (a.b) h += b[i];
-            v[i] = h;
+        for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(__fadd2_rn(k[j].v[i], minus), make_float2(rstd, rstd));
+        K p;
+        if (a.w) {
+            load_params(a.w, a.param_bf16, c0, n[j], p);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(k[j].v[i], p.v[i]);
         }
-        Raw8<T> out;
-        out.set(v);
-        T* y = static_cast<T*>(a.y) + row * a.ld_y + c0;
-        if (a.vec_y)
-            store8<true>(out, y, n[j]);
-        else
-            store8<false>(out, y, n[j]);
+        if (a.b) {
+            load_params(a.b, a.param_bf16, c0, n[j], p);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fadd2_rn(k[j].v[i], p.v[i]);
+        }
+        k[j].store(static_cast<T*>(a.y) + row * a.ld_y + c0, n[j]);
     }
 }
 
@@ -176,164 +175,297 @@ struct BackwardArgs {
     float* part;  // [2][CTAs][cols]: sums of gy*h, then of gy
     long long rows, ld_gy, ld_x, ld_codes, ld_scales, ld_gx;
     int cols;
-    bool param_bf16, vec_gy, vec_x, vec_gx, vec_p, sum_b;
+    bool param_bf16, sum_b;
+    bool async_gy, async_x;  // rows start on 16-byte boundaries: copied to shared memory ahead of time
 };
 
-// Rows are dealt to the row groups of a persistent grid; a thread keeps the
-// fp32 sums of gy*h and gy of its columns in registers over all its rows.  The
-// groups of a CTA are joined in shared memory, the CTAs by join_columns_kernel,
-// both in a fixed order.
-template <typename T, int FMT, bool LAYER, int WPR, int V>
+__device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 take16(unsigned src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
+
+// Shared memory of a CTA per row on its way: 32 bytes of gy and of x (or its
+// codes, 16) for each chunk of each thread.
+template <typename T, int FMT, int WPR>
+constexpr int kRowBytes = Shape<WPR>::kThreads * (kChunks<T> * 32 + (FMT == AMPQ_FMT_BASE ? kChunks<T> * 32 : 16));
+
+// Rows on their way, the current one among them: four, or as many as leave room
+// for the CTAs meant to be resident; 0 where not even two fit (fp32 rows of more
+// than 8192 columns, kept in full) and rows are read as they come.
+template <typename T, int FMT, int WPR>
+struct Ring {
+    static constexpr int kFit = (WPR <= 8 ? 104 : 208) * 1024 / kRowBytes<T, FMT, WPR>;
+    static constexpr int kRows = kFit >= 4 ? 4 : kFit >= 2 ? kFit : 0;
+    static constexpr int kBytes = kRows * kRowBytes<T, FMT, WPR>;
+};
+
+// Rows are dealt to the row groups of a persistent grid; a thread keeps the fp32
+// sums of gy*h and gy of its 16 columns in registers over all its rows.  Each
+// thread copies its own parts of the next rows to shared memory while it works on
+// one (no barrier: nobody else reads them), which keeps enough bytes on the way
+// with the few threads that the sums' registers allow.  The groups of a CTA are
+// joined in shared memory, the CTAs by join_columns_kernel, in a fixed order.
+template <typename T, int FMT, bool LAYER, int WPR>
 __global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(const BackwardArgs a) {
     using S = Shape<WPR>;
-    __shared__ float red[S::kWarps * 2];
-    __shared__ float join[S::kGroups > 1 ? S::kGroups * WPR * 256 * V : 1];
+    using K = Chunk<T>;
+    constexpr int V = kChunks<T>, E = K::kElems, kThreads = S::kThreads;
+    constexpr bool kKept = FMT != AMPQ_FMT_BASE;
+    static_assert(!kKept || Ring<T, FMT, WPR>::kRows > 0, "codes are read from the ring");
+    constexpr int kAhead = Ring<T, FMT, WPR>::kRows;
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ float red[2][S::kWarps * 2];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
     const int group = warp / WPR;
-    float sum_w[V][8], sum_b[V][8];
+    const unsigned ring_gy = (unsigned)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    const unsigned ring_x = ring_gy + kAhead * kThreads * 32 * V;
+    float2 sum_w[V][E / 2], sum_b[V][E / 2];
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum_w[j][i] = sum_b[j][i] = 0.0f;
+        for (int i = 0; i < E / 2; ++i) sum_w[j][i] = sum_b[j][i] = make_float2(0.0f, 0.0f);
     const float inv_cols = 1.0f / (float)a.cols;
-    for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += (long long)gridDim.x * S::kGroups) {
+    const long long stride = (long long)gridDim.x * S::kGroups;
+    const bool async_gy = kAhead > 0 && a.async_gy, async_x = kAhead > 0 && a.async_x;
+    auto begin_copy = [&](long long row, int slot) {
+        if (row < a.rows) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c0 = (j * 32 * WPR + t) * E, n = min(E, a.cols - c0);
+                if (n <= 0) continue;
+                const int bytes = n * (int)sizeof(T);
+                const unsigned to = (unsigned)((slot * V + j) * 2 * kThreads * 16);
+                if (async_gy) {
+                    const unsigned char* p = reinterpret_cast<const unsigned char*>(static_cast<const T*>(a.gy) + row * a.ld_gy + c0);
+                    copy16(ring_gy + to, p, min(16, bytes));
+                    if (bytes > 16) copy16(ring_gy + to + kThreads * 16, p + 16, bytes - 16);
+                }
+                if (!kKept && async_x) {
+                    const unsigned char* p = reinterpret_cast<const unsigned char*>(static_cast<const T*>(a.x) + row * a.ld_x + c0);
+                    copy16(ring_x + to, p, min(16, bytes));
+                    if (bytes > 16) copy16(ring_x + to + kThreads * 16, p + 16, bytes - 16);
+                }
+                if (kKept && kAhead > 0) {
+                    const unsigned char* p = a.codes + row * a.ld_codes + c0;
+                    if (E == 16)
+                        copy16(ring_x + (unsigned)(slot * kThreads * 16), p, 16);
+                    else
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_x + (unsigned)(slot * kThreads * 16) + 8 * j), "l"(p) : "memory");
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto words_of = [&](unsigned from, int slot, int j, unsigned(&w)[8], int n) {
+        const unsigned at = from + (unsigned)((slot * V + j) * 2 * kThreads * 16);
+        const uint4 p = take16(at), q = n * (int)sizeof(T) > 16 ? take16(at + kThreads * 16) : make_uint4(0, 0, 0, 0);
+        w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
+        w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
+    };
+    const long long first = (long long)blockIdx.x * S::kGroups + group;
+#pragma unroll
+    for (int s = 0; s < kAhead - 1; ++s) begin_copy(first + s * stride, s);
+    int slot = 0;
+    int phase = 0;
+    // the statistics and scale bytes of the next row are loaded one row ahead
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    unsigned next_byte[V];
+    auto fetch_small = [&](long long row) {
+        if (row >= a.rows) return;
+        next_rstd = __ldg(a.rstd + row);
+        if (LAYER) next_mean = __ldg(a.mean + row);
+        if (kKept) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c0 = (j * 32 * WPR + t) * E;
+                next_byte[j] = c0 < a.cols ? __ldg(a.scales + row * a.ld_scales + c0 / kGroup) : 127u;
+            }
+        }
+    };
+    fetch_small(first);
+    for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += stride) {
         const long long row = row0 + group;
         const bool live = row < a.rows;
-        const float mean = LAYER && live ? __ldg(a.mean + row) : 0.0f;
-        const float rstd = live ? __ldg(a.rstd + row) : 0.0f;
-        float h[V][8], g[V][8];
-        float c[2] = {0.0f, 0.0f};
+        if (kAhead > 0) begin_copy(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
+        const float mean = next_mean, rstd = live ? next_rstd : 0.0f;
+        float p[V];
+        if (kKept) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = (j * 32 * WPR + t) * 8;
-            const int n = live ? max(0, min(8, a.cols - c0)) : 0;
-            if (n <= 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[j][i] = g[j][i] = 0.0f;
-                continue;
-            }
-            Raw8<T> r;
-            const T* gy = static_cast<const T*>(a.gy) + row * a.ld_gy + c0;
-            if (a.vec_gy)
-                load8<true>(r, gy, n);
-            else
-                load8<false>(r, gy, n);
-            r.values(g[j]);
-            if (FMT != AMPQ_FMT_BASE) {
-                constexpr int F = FMT == AMPQ_FMT_BASE ? AMPQ_FMT_E4M3 : FMT;
-                decode8<F>(__ldg(reinterpret_cast<const uint2*>(a.codes + row * a.ld_codes + c0)), h[j]);
-                const float p = scale_of(__ldg(a.scales + row * a.ld_scales + c0 / kGroup));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[j][i] *= p;
-            } else {
-                const T* x = static_cast<const T*>(a.x) + row * a.ld_x + c0;
-                if (a.vec_x)
-                    load8<true>(r, x, n);
-                else
-                    load8<false>(r, x, n);
-                r.values(h[j]);
-            }
-            float w[8];
-            if (a.w) load_param8(a.w, a.param_bf16, a.vec_p, c0, n, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                h[j][i] = i < n ? (h[j][i] - mean) * rstd : 0.0f;
-                sum_w[j][i] = fmaf(g[j][i], h[j][i], sum_w[j][i]);
-                sum_b[j][i] += g[j][i];
-                if (a.w) g[j][i] *= w[i];
-                c[0] = fmaf(g[j][i], h[j][i], c[0]);
-                c[1] += g[j][i];
-            }
+            for (int j = 0; j < V; ++j) p[j] = scale_of(next_byte[j]);
         }
-        row_sum<WPR, 2>(c, red, warp);
-        const float c2 = c[0] * inv_cols, c1 = LAYER ? c[1] * inv_cols : 0.0f;
+        fetch_small(row + stride);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead > 0 ? kAhead - 1 : 0) : "memory");
+        K h[V], g[V];
+        float2 c2 = make_float2(0.0f, 0.0f), c1 = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int c0 = (j * 32 * WPR + t) * 8;
-            const int n = live ? max(0, min(8, a.cols - c0)) : 0;
+            const int c0 = (j * 32 * WPR + t) * E;
+            const int n = live ? min(E, a.cols - c0) : 0;
+            h[j].zero();
+            g[j].zero();
             if (n <= 0) continue;
-            float o[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = rstd * (fmaf(-h[j][i], c2, g[j][i]) - c1);
-            Raw8<T> r;
-            r.set(o);
-            T* gx = static_cast<T*>(a.gx) + row * a.ld_gx + c0;
-            if (a.vec_gx)
-                store8<true>(r, gx, n);
+            unsigned w8[8];
+            if (async_gy)
+                words_of(ring_gy, slot, j, w8, n);
             else
-                store8<false>(r, gx, n);
+                K::load_words(static_cast<const T*>(a.gy) + row * a.ld_gy + c0, n, w8);
+            g[j].from_words(w8);
+            if (kKept) {
+                constexpr int F = kKept ? FMT : AMPQ_FMT_E4M3;
+                const uint4 q = take16(ring_x + (unsigned)(slot * kThreads * 16));
+                unsigned c[E / 4];
+                if (E == 16) {
+                    c[0] = q.x; c[1] = q.y; c[2 % (E / 4)] = q.z; c[3 % (E / 4)] = q.w;
+                } else {
+                    c[0] = j ? q.z : q.x;
+                    c[1] = j ? q.w : q.y;
+                }
+                h[j].template decode<F>(c);
+            } else {
+                if (async_x)
+                    words_of(ring_x, slot, j, w8, n);
+                else
+                    K::load_words(static_cast<const T*>(a.x) + row * a.ld_x + c0, n, w8);
+                h[j].from_words(w8);
+            }
+            K w;
+            if (a.w) load_params(a.w, a.param_bf16, c0, n, w);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                // (x - mean) * rstd; the scale of a kept x joins the subtraction
+                const float2 d = kKept ? __ffma2_rn(h[j].v[i], make_float2(p[j], p[j]), make_float2(-mean, -mean)) : __fadd2_rn(h[j].v[i], make_float2(-mean, -mean));
+                float2 hh = __fmul2_rn(d, make_float2(rstd, rstd));
+                if (n < E) hh = make_float2(2 * i < n ? hh.x : 0.0f, 2 * i + 1 < n ? hh.y : 0.0f);
+                h[j].v[i] = hh;
+                sum_w[j][i] = __ffma2_rn(g[j].v[i], hh, sum_w[j][i]);
+                if (LAYER) sum_b[j][i] = __fadd2_rn(sum_b[j][i], g[j].v[i]);
+                if (a.w) g[j].v[i] = __fmul2_rn(g[j].v[i], w.v[i]);
+                c2 = __ffma2_rn(g[j].v[i], hh, c2);
+                if (LAYER) c1 = __fadd2_rn(c1, g[j].v[i]);
+            }
         }
+        float both[2] = {c2.x + c2.y, c1.x + c1.y};
+        if (LAYER) {
+            row_sum<WPR, 2>(both, red[phase], warp);
+        } else {
+            float one[1] = {both[0]};
+            row_sum<WPR, 1>(one, red[phase], warp);
+            both[0] = one[0];
+        }
+        phase ^= 1;
+        const float m2 = -both[0] * inv_cols, m1 = LAYER ? -both[1] * inv_cols : 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c0 = (j * 32 * WPR + t) * E;
+            const int n = live ? min(E, a.cols - c0) : 0;
+            if (n <= 0) continue;
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float2 o = __ffma2_rn(h[j].v[i], make_float2(m2, m2), g[j].v[i]);
+                if (LAYER) o = __fadd2_rn(o, make_float2(m1, m1));
+                g[j].v[i] = __fmul2_rn(o, make_float2(rstd, rstd));
+            }
+            g[j].store(static_cast<T*>(a.gx) + row * a.ld_gx + c0, n);
+        }
+        if (++slot == kAhead) slot = 0;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.part) return;
-    for (int k = 0; k < (a.sum_b ? 2 : 1); ++k) {
+    float* join = reinterpret_cast<float*>(ring);
+    for (int k = 0; k < (LAYER && a.sum_b ? 2 : 1); ++k) {
         float* out = a.part + ((long long)k * gridDim.x + blockIdx.x) * a.cols;
         if (S::kGroups == 1) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int c0 = (j * 32 * WPR + t) * 8;
+                const int c0 = (j * 32 * WPR + t) * E;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c0 + i < a.cols) out[c0 + i] = k ? sum_b[j][i] : sum_w[j][i];
+                for (int i = 0; i < E; ++i) {
+                    const float2 f = k ? sum_b[j][i / 2] : sum_w[j][i / 2];
+                    if (c0 + i < a.cols) out[c0 + i] = i & 1 ? f.y : f.x;
+                }
             }
         } else {
-            constexpr int kSpan = WPR * 256 * V;
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < V; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) join[group * kSpan + (j * 32 * WPR + t) * 8 + i] = k ? sum_b[j][i] : sum_w[j][i];
+                for (int i = 0; i < E / 2; ++i)
+                    *reinterpret_cast<float2*>(join + group * S::kSpan + (j * 32 * WPR + t) * E + 2 * i) = k ? sum_b[j][i] : sum_w[j][i];
             __syncthreads();
-            for (int i = threadIdx.x; i < a.cols; i += S::kThreads) {
+            for (int i = threadIdx.x; i < a.cols; i += kThreads) {
                 float s = 0.0f;
 #pragma unroll
-                for (int g = 0; g < S::kGroups; ++g) s += join[g * kSpan + i];
+                for (int g = 0; g < S::kGroups; ++g) s += join[g * S::kSpan + i];
                 out[i] = s;
             }
         }
     }
 }
 
-// CTAs of the backward pass: every row group gets a row before one gets two,
-// and no more CTAs than are resident, so that the sums stay in registers.
+// Warps of a row: 512 columns each, a power of two.
+int warps_per_row(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 8192 ? 16 : 32; }
+
+// CTAs of the backward pass: every row group gets a row before one gets two, and
+// no more CTAs than are resident, so that the sums stay in registers.
 int backward_ctas(long long rows, int cols, int sms) {
-    const int wpr = cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 8192 ? 16 : 32;
-    const int groups = wpr < 8 ? 8 / wpr : 1;
+    const int wpr = warps_per_row(cols), groups = wpr < 8 ? 8 / wpr : 1;
     const long long need = (rows + groups - 1) / groups;
     const long long most = (long long)sms * (wpr <= 8 ? 2 : 1);
     return (int)(need < most ? need : most);
 }
 
+template <typename T, int FMT, int WPR>
+void start_forward(const ForwardArgs& a, cudaStream_t st) {
+    const long long blocks = (a.rows + Shape<WPR>::kGroups - 1) / Shape<WPR>::kGroups;
+    norm_forward_kernel<T, FMT, WPR><<<(unsigned)blocks, Shape<WPR>::kThreads, 0, st>>>(a);
+}
+
 template <typename T, int FMT>
 int launch_forward(const ForwardArgs& a, cudaStream_t st) {
-#define AMPQ_FWD(WPR, V)                                                                                      \
-    do {                                                                                                      \
-        const long long blocks = (a.rows + Shape<WPR>::kGroups - 1) / Shape<WPR>::kGroups;                    \
-        norm_forward_kernel<T, FMT, WPR, V><<<(unsigned)blocks, Shape<WPR>::kThreads, 0, st>>>(a);            \
-    } while (0)
-    if (a.cols <= 256) AMPQ_FWD(1, 1);
-    else if (a.cols <= 512) AMPQ_FWD(1, 2);
-    else if (a.cols <= 1024) AMPQ_FWD(1, 4);
-    else if (a.cols <= 2048) AMPQ_FWD(2, 4);
-    else if (a.cols <= 4096) AMPQ_FWD(4, 4);
-    else if (a.cols <= 8192) AMPQ_FWD(8, 4);
-    else AMPQ_FWD(16, 4);
-#undef AMPQ_FWD
+    switch (warps_per_row(a.cols)) {
+        case 1: start_forward<T, FMT, 1>(a, st); break;
+        case 2: start_forward<T, FMT, 2>(a, st); break;
+        case 4: start_forward<T, FMT, 4>(a, st); break;
+        case 8: start_forward<T, FMT, 8>(a, st); break;
+        case 16: start_forward<T, FMT, 16>(a, st); break;
+        default: start_forward<T, FMT, 32>(a, st);
+    }
+    return launched();
+}
+
+constexpr int kMaxDevices = 64;
+
+template <typename T, int FMT, bool LAYER, int WPR>
+int start_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
+    static std::atomic<bool> prepared[kMaxDevices];  // the kernel may use its shared memory on that device
+    constexpr int kJoin = Shape<WPR>::kGroups > 1 ? Shape<WPR>::kGroups * Shape<WPR>::kSpan * 4 : 0;
+    constexpr int kBytes = Ring<T, FMT, WPR>::kBytes > kJoin ? Ring<T, FMT, WPR>::kBytes : kJoin;
+    if (kBytes > 32 * 1024 && (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire))) {
+        if (cudaFuncSetAttribute(norm_backward_kernel<T, FMT, LAYER, WPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+            cudaGetLastError();
+            return AMPQ_ERR_CUDA;
+        }
+        if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
+    }
+    norm_backward_kernel<T, FMT, LAYER, WPR><<<(unsigned)ctas, Shape<WPR>::kThreads, kBytes, st>>>(a);
     return launched();
 }
 
 template <typename T, int FMT, bool LAYER>
-int launch_backward(const BackwardArgs& a, int ctas, cudaStream_t st) {
-#define AMPQ_BWD(WPR, V) norm_backward_kernel<T, FMT, LAYER, WPR, V><<<(unsigned)ctas, Shape<WPR>::kThreads, 0, st>>>(a)
-    if (a.cols <= 256) AMPQ_BWD(1, 1);
-    else if (a.cols <= 512) AMPQ_BWD(1, 2);
-    else if (a.cols <= 1024) AMPQ_BWD(2, 2);
-    else if (a.cols <= 2048) AMPQ_BWD(4, 2);
-    else if (a.cols <= 4096) AMPQ_BWD(8, 2);
-    else if (a.cols <= 8192) AMPQ_BWD(16, 2);
-    else AMPQ_BWD(32, 2);
-#undef AMPQ_BWD
-    return launched();
+int launch_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
+    switch (warps_per_row(a.cols)) {
+        case 1: return start_backward<T, FMT, LAYER, 1>(a, device, ctas, st);
+        case 2: return start_backward<T, FMT, LAYER, 2>(a, device, ctas, st);
+        case 4: return start_backward<T, FMT, LAYER, 4>(a, device, ctas, st);
+        case 8: return start_backward<T, FMT, LAYER, 8>(a, device, ctas, st);
+        case 16: return start_backward<T, FMT, LAYER, 16>(a, device, ctas, st);
+        default: return start_backward<T, FMT, LAYER, 32>(a, device, ctas, st);
+    }
 }
 
 template <typename T>
@@ -344,10 +476,10 @@ int dispatch_forward(int fmt, const ForwardArgs& a, cudaStream_t st) {
 }
 
 template <typename T, bool LAYER>
-int dispatch_backward(int fmt, const BackwardArgs& a, int ctas, cudaStream_t st) {
-    if (fmt == AMPQ_FMT_E4M3) return launch_backward<T, AMPQ_FMT_E4M3, LAYER>(a, ctas, st);
-    if (fmt == AMPQ_FMT_E5M2) return launch_backward<T, AMPQ_FMT_E5M2, LAYER>(a, ctas, st);
-    return launch_backward<T, AMPQ_FMT_BASE, LAYER>(a, ctas, st);
+int dispatch_backward(int fmt, const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
+    if (fmt == AMPQ_FMT_E4M3) return launch_backward<T, AMPQ_FMT_E4M3, LAYER>(a, device, ctas, st);
+    if (fmt == AMPQ_FMT_E5M2) return launch_backward<T, AMPQ_FMT_E5M2, LAYER>(a, device, ctas, st);
+    return launch_backward<T, AMPQ_FMT_BASE, LAYER>(a, device, ctas, st);
 }
 
 int check_norm(int kind, int dtype, int param_dtype, int fmt, long long cols) {
@@ -392,9 +524,6 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     a.eps = eps;
     a.layer = layer;
     a.param_bf16 = param_dtype == AMPQ_BF16;
-    a.vec_x = rows_aligned(x, ld_x, dtype);
-    a.vec_y = rows_aligned(y, ld_y, dtype);
-    a.vec_p = aligned_to(weight, 16) && aligned_to(bias, 16);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     return dtype == AMPQ_F32 ? dispatch_forward<float>(fmt, a, st) : dispatch_forward<__nv_bfloat16>(fmt, a, st);
 }
@@ -444,15 +573,13 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.rows = rows; a.ld_gy = ld_gy; a.ld_x = ld_x; a.ld_codes = ld_codes; a.ld_scales = ld_scales; a.ld_gx = ld_gx;
         a.cols = (int)cols;
         a.param_bf16 = param_dtype == AMPQ_BF16;
-        a.vec_gy = rows_aligned(gy, ld_gy, dtype);
-        a.vec_x = rows_aligned(x, ld_x, dtype);
-        a.vec_gx = rows_aligned(gx, ld_gx, dtype);
-        a.vec_p = aligned_to(weight, 16);
         a.sum_b = gbias != nullptr;
+        a.async_gy = rows_aligned(gy, ld_gy, dtype);
+        a.async_x = rows_aligned(x, ld_x, dtype);
         if (dtype == AMPQ_F32)
-            rc = layer ? dispatch_backward<float, true>(fmt, a, ctas, st) : dispatch_backward<float, false>(fmt, a, ctas, st);
+            rc = layer ? dispatch_backward<float, true>(fmt, a, device, ctas, st) : dispatch_backward<float, false>(fmt, a, device, ctas, st);
         else
-            rc = layer ? dispatch_backward<__nv_bfloat16, true>(fmt, a, ctas, st) : dispatch_backward<__nv_bfloat16, false>(fmt, a, ctas, st);
+            rc = layer ? dispatch_backward<__nv_bfloat16, true>(fmt, a, device, ctas, st) : dispatch_backward<__nv_bfloat16, false>(fmt, a, device, ctas, st);
         if (rc) return rc;
     }
     if (!sums) return AMPQ_OK;
