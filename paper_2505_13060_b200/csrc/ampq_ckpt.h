@@ -209,9 +209,15 @@ struct Chunk {
                 }
             }
         } else if (off == 0) {
-            const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
-            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-            w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+            if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
+                asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                             : "l"(p));
+            } else {
+                const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+            }
         } else if ((off & 3) == 0) {
             const unsigned* q = reinterpret_cast<const unsigned*>(p);
 #pragma unroll
@@ -245,8 +251,14 @@ struct Chunk {
         unsigned w[8];
         to_words(w);
         if (off == 0) {
-            reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                             "r"(w[5]), "r"(w[6]), "r"(w[7])
+                             : "memory");
+            } else {
+                reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
         } else if ((off & 3) == 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) reinterpret_cast<unsigned*>(p)[i] = w[i];

@@ -11,9 +11,9 @@ namespace {
 
 constexpr int kMaxNormCols = AMPQ_NORM_MAX_COLS;
 
-// One thread holds 16 elements of a row: one chunk of bf16 or two of fp32.
-template <typename T>
-constexpr int kChunks = 16 / Chunk<T>::kElems;
+// One thread holds 16 * WIDE elements of a row: so many chunks.
+template <typename T, int WIDE>
+constexpr int kChunks = 16 * WIDE / Chunk<T>::kElems;
 
 // Sums N values over the WPR warps of a row group; every thread of the CTA calls
 // it.  The order is fixed.
@@ -28,23 +28,21 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* red, int warp) {
 #pragma unroll
         for (int k = 0; k < N; ++k) red[warp * N + k] = s[k];
     __syncthreads();
-    // 32 lanes take one warp's sum each and add them up as before
-    const int first = warp / WPR * WPR, lane = threadIdx.x & 31;
+    // every lane takes one of the group's sums and they are added up as before
+    const int from = warp / WPR * WPR + (threadIdx.x & (WPR - 1));
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        float t = lane < WPR ? red[(first + lane) * N + k] : 0.0f;
+        s[k] = red[from * N + k];
 #pragma unroll
-        for (int o = WPR / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-        s[k] = __shfl_sync(0xFFFFFFFFu, t, 0);
+        for (int o = WPR / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], o);
     }
 }
 
-template <int WPR>
+template <int WPR, int WIDE>
 struct Shape {
     static constexpr int kWarps = WPR < 8 ? 8 : WPR;   // warps of a CTA
     static constexpr int kGroups = kWarps / WPR;       // rows a CTA works on at a time
     static constexpr int kThreads = 32 * kWarps;
-    static constexpr int kSpan = 512 * WPR;            // most columns of a row
 };
 
 // 16 elements of a parameter vector in fp32, as pairs.
@@ -79,18 +77,19 @@ struct ForwardArgs {
     long long rows, ld_x, ld_y, ld_codes, ld_scales;
     int cols;
     float eps;
-    bool layer, param_bf16;
+    bool param_bf16;
+    bool whole;  // the last chunk of a row is a whole one
 };
 
 // One row per group of WPR warps, held in registers between the statistics (mean,
 // then the sum of squared differences from it) and the output, so x is read once.
 // Thread t of a group holds the chunks (j * threads + t): loads are contiguous
 // and neighbouring lanes make the groups of the checkpoint.
-template <typename T, int FMT, int WPR>
-__global__ void __launch_bounds__(Shape<WPR>::kThreads, 2048 / Shape<WPR>::kThreads > 4 ? 4 : 1) norm_forward_kernel(const ForwardArgs a) {
-    using S = Shape<WPR>;
+template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads) norm_forward_kernel(const ForwardArgs a) {
+    using S = Shape<WPR, WIDE>;
     using K = Chunk<T>;
-    constexpr int V = kChunks<T>, E = K::kElems;
+    constexpr int V = kChunks<T, WIDE>, E = K::kElems;
     __shared__ float red[2][S::kWarps];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
@@ -108,7 +107,7 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads, 2048 / Shape<WPR>::kThre
     }
     const float inv_cols = 1.0f / (float)a.cols;
     float mean = 0.0f;
-    if (a.layer) {
+    if (LAYER) {
         float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -120,20 +119,31 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads, 2048 / Shape<WPR>::kThre
     }
     const float2 minus = make_float2(-mean, -mean);
     float2 q2 = make_float2(0.0f, 0.0f);
+    if (!LAYER || a.whole) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
+        for (int j = 0; j < V; ++j) {
+            if (LAYER && n[j] <= 0) continue;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            float2 d = __fadd2_rn(k[j].v[i], minus);
-            if (n[j] < E) d = make_float2(2 * i < n[j] ? d.x : 0.0f, 2 * i + 1 < n[j] ? d.y : 0.0f);
-            q2 = __ffma2_rn(d, d, q2);
+            for (int i = 0; i < E / 2; ++i) {
+                const float2 d = LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i];
+                q2 = __ffma2_rn(d, d, q2);
+            }
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float2 d = __fadd2_rn(k[j].v[i], minus);
+                d = make_float2(2 * i < n[j] ? d.x : 0.0f, 2 * i + 1 < n[j] ? d.y : 0.0f);
+                q2 = __ffma2_rn(d, d, q2);
+            }
     }
     float q[1] = {q2.x + q2.y};
     row_sum<WPR, 1>(q, red[1], warp);
     const float rstd = 1.0f / sqrtf(q[0] * inv_cols + a.eps);
     if (live && t == 0) {
-        if (a.layer) a.mean[row] = mean;
+        if (LAYER) a.mean[row] = mean;
         a.rstd[row] = rstd;
     }
 #pragma unroll
@@ -151,14 +161,14 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads, 2048 / Shape<WPR>::kThre
         }
         if (n[j] <= 0) continue;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(__fadd2_rn(k[j].v[i], minus), make_float2(rstd, rstd));
+        for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i], make_float2(rstd, rstd));
         K p;
         if (a.w) {
             load_params(a.w, a.param_bf16, c0, n[j], p);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(k[j].v[i], p.v[i]);
         }
-        if (a.b) {
+        if (LAYER && a.b) {
             load_params(a.b, a.param_bf16, c0, n[j], p);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fadd2_rn(k[j].v[i], p.v[i]);
@@ -176,7 +186,7 @@ struct BackwardArgs {
     long long rows, ld_gy, ld_x, ld_codes, ld_scales, ld_gx;
     int cols;
     bool param_bf16, sum_b;
-    bool async_gy, async_x;  // rows start on 16-byte boundaries: copied to shared memory ahead of time
+    bool aligned_gy, aligned_x;  // rows start on 16-byte boundaries
 };
 
 __device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
@@ -188,42 +198,120 @@ __device__ __forceinline__ uint4 take16(unsigned src) {
     return v;
 }
 
-// Shared memory of a CTA per row on its way: 32 bytes of gy and of x (or its
-// codes, 16) for each chunk of each thread.
-template <typename T, int FMT, int WPR>
-constexpr int kRowBytes = Shape<WPR>::kThreads * (kChunks<T> * 32 + (FMT == AMPQ_FMT_BASE ? kChunks<T> * 32 : 16));
+__device__ __forceinline__ void copy4(unsigned dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A warp's chunks of one row on their way: 1024 bytes, and a word for rows that
+// start between two words, kept 16-byte aligned.
+constexpr int kPiece = 1024 + 16;
+
+// The columns of one warp (32 chunks from element `at` on, of `cols`) of row `row`,
+// copied to shared memory.  16 bytes a lane where rows start on 16-byte boundaries,
+// zeros behind the row's end.  Otherwise words from the one the piece starts in;
+// what lies behind the row's end in the matrix is copied too, a word that the
+// matrix holds only half of is put together by hand.
+template <typename T>
+__device__ __forceinline__ void copy_piece(unsigned to, const T* m, long long ld, long long rows, int cols, long long row, int at, bool aligned, unsigned lane) {
+    const T* p = m + row * ld + at;
+    if (aligned) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            constexpr int kPer = 16 / (int)sizeof(T);
+            const int first = (32 * k + (int)lane) * kPer, bytes = min(16, (cols - at - first) * (int)sizeof(T));
+            if (bytes > 0) copy16(to + 16 * (32 * k + lane), p + first, bytes);
+        }
+        return;
+    }
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(p), down = a0 & ~(uintptr_t)3;
+    const int bytes = min(1024, (cols - at) * (int)sizeof(T));
+    const int words = bytes > 0 ? ((int)(a0 - down) + bytes + 3) / 4 : 0;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(m), end = reinterpret_cast<uintptr_t>(m + (rows - 1) * ld + cols);
+#pragma unroll
+    for (int k = 0; k < 9; ++k) {
+        const int w = 32 * k + (int)lane;
+        if (w >= words) break;
+        const uintptr_t q = down + 4 * w;
+        if (q >= begin && q + 4 <= end) {
+            copy4(to + 4 * w, reinterpret_cast<const void*>(q));
+        } else {
+            const bool lower = q >= begin;  // the half that exists
+            const unsigned half = __ldg(reinterpret_cast<const unsigned short*>(lower ? q : q + 2));
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * w), "r"(lower ? half : half << 16) : "memory");
+        }
+    }
+}
+
+// This lane's chunk of a piece, zeros from element n on.  All lanes call it.
+template <typename T>
+__device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long ld, long long row, int at, bool aligned, unsigned lane, int n, unsigned (&w)[8]) {
+    // the upper four of eight lanes read their second half first: the eight meet all 32 banks
+    const unsigned swap = (lane >> 2) & 1, a = from + 32 * lane;
+    const uint4 p = take16(a + 16 * swap), q = take16(a + 16 * (1 - swap));
+    const uint4 lo = swap ? q : p, hi = swap ? p : q;
+    w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w;
+    w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+    if (aligned) {
+        if (n * (int)sizeof(T) <= 16) w[4] = w[5] = w[6] = w[7] = 0;
+        return;
+    }
+    if (reinterpret_cast<uintptr_t>(m + row * ld + at) & 2) {
+        unsigned next = __shfl_down_sync(0xFFFFFFFFu, w[0], 1);
+        if (lane == 31) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(next) : "r"(from + 1024) : "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __funnelshift_r(w[i], i < 7 ? w[i + 1] : next, 16);
+    }
+    if (n < Chunk<T>::kElems) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (sizeof(T) == 4) {
+                if (i >= n) w[i] = 0;
+            } else {
+                if (2 * i >= n) w[i] = 0;
+                if (2 * i + 1 == n) w[i] &= 0xFFFFu;
+            }
+        }
+    }
+}
+
+// Shared memory of a CTA per row on its way: gy, and x or its codes.
+template <typename T, int FMT, int WPR, int WIDE>
+constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (FMT == AMPQ_FMT_BASE ? kChunks<T, WIDE> * kPiece : 512 * WIDE));
 
 // Rows on their way, the current one among them: four, or as many as leave room
 // for the CTAs meant to be resident; 0 where not even two fit (fp32 rows of more
 // than 8192 columns, kept in full) and rows are read as they come.
-template <typename T, int FMT, int WPR>
+template <typename T, int FMT, int WPR, int WIDE>
 struct Ring {
-    static constexpr int kFit = (WPR <= 8 ? 104 : 208) * 1024 / kRowBytes<T, FMT, WPR>;
+    static constexpr int kFit = (WPR <= 8 ? 104 : 208) * 1024 / kRowBytes<T, FMT, WPR, WIDE>;
     static constexpr int kRows = kFit >= 4 ? 4 : kFit >= 2 ? kFit : 0;
-    static constexpr int kBytes = kRows * kRowBytes<T, FMT, WPR>;
+    static constexpr int kBytes = kRows * kRowBytes<T, FMT, WPR, WIDE>;
 };
 
 // Rows are dealt to the row groups of a persistent grid; a thread keeps the fp32
-// sums of gy*h and gy of its 16 columns in registers over all its rows.  Each
-// thread copies its own parts of the next rows to shared memory while it works on
-// one (no barrier: nobody else reads them), which keeps enough bytes on the way
-// with the few threads that the sums' registers allow.  The groups of a CTA are
-// joined in shared memory, the CTAs by join_columns_kernel, in a fixed order.
-template <typename T, int FMT, bool LAYER, int WPR>
-__global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(const BackwardArgs a) {
-    using S = Shape<WPR>;
+// sums of gy*h and gy of its columns in registers over all its rows.  Each warp
+// copies its own parts of the next rows to shared memory while it works on one (no
+// barrier: no other warp reads them), which keeps enough bytes on the way with the
+// few threads that the sums' registers allow.  The groups of a CTA are joined in
+// shared memory, the CTAs by join_columns_kernel, in a fixed order.
+template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::kThreads == 256 ? 2 : 1) norm_backward_kernel(const BackwardArgs a) {
+    using S = Shape<WPR, WIDE>;
     using K = Chunk<T>;
-    constexpr int V = kChunks<T>, E = K::kElems, kThreads = S::kThreads;
+    constexpr int V = kChunks<T, WIDE>, E = K::kElems, kThreads = S::kThreads, kSpan = 512 * WPR * WIDE;
     constexpr bool kKept = FMT != AMPQ_FMT_BASE;
-    static_assert(!kKept || Ring<T, FMT, WPR>::kRows > 0, "codes are read from the ring");
-    constexpr int kAhead = Ring<T, FMT, WPR>::kRows;
+    static_assert(!kKept || Ring<T, FMT, WPR, WIDE>::kRows > 0, "codes are read from the ring");
+    constexpr int kAhead = Ring<T, FMT, WPR, WIDE>::kRows;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float red[2][S::kWarps * 2];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
     const int group = warp / WPR;
-    const unsigned ring_gy = (unsigned)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
-    const unsigned ring_x = ring_gy + kAhead * kThreads * 32 * V;
+    const unsigned lane = threadIdx.x % 32;
+    constexpr int kGyRow = S::kWarps * V * kPiece;  // bytes of a row's gy, in pieces by warp and chunk
+    const unsigned ring_gy = (unsigned)__cvta_generic_to_shared(ring) + warp * V * kPiece;
+    const unsigned ring_x = ring_gy + kAhead * kGyRow;
+    const unsigned ring_codes = (unsigned)__cvta_generic_to_shared(ring) + kAhead * kGyRow + threadIdx.x * 16;
     float2 sum_w[V][E / 2], sum_b[V][E / 2];
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -231,41 +319,24 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(con
         for (int i = 0; i < E / 2; ++i) sum_w[j][i] = sum_b[j][i] = make_float2(0.0f, 0.0f);
     const float inv_cols = 1.0f / (float)a.cols;
     const long long stride = (long long)gridDim.x * S::kGroups;
-    const bool async_gy = kAhead > 0 && a.async_gy, async_x = kAhead > 0 && a.async_x;
     auto begin_copy = [&](long long row, int slot) {
         if (row < a.rows) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int c0 = (j * 32 * WPR + t) * E, n = min(E, a.cols - c0);
-                if (n <= 0) continue;
-                const int bytes = n * (int)sizeof(T);
-                const unsigned to = (unsigned)((slot * V + j) * 2 * kThreads * 16);
-                if (async_gy) {
-                    const unsigned char* p = reinterpret_cast<const unsigned char*>(static_cast<const T*>(a.gy) + row * a.ld_gy + c0);
-                    copy16(ring_gy + to, p, min(16, bytes));
-                    if (bytes > 16) copy16(ring_gy + to + kThreads * 16, p + 16, bytes - 16);
-                }
-                if (!kKept && async_x) {
-                    const unsigned char* p = reinterpret_cast<const unsigned char*>(static_cast<const T*>(a.x) + row * a.ld_x + c0);
-                    copy16(ring_x + to, p, min(16, bytes));
-                    if (bytes > 16) copy16(ring_x + to + kThreads * 16, p + 16, bytes - 16);
-                }
-                if (kKept && kAhead > 0) {
+                const int at = (j * 32 * WPR + t - (int)lane) * E, c0 = at + (int)lane * E;
+                const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
+                copy_piece(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, a.rows, a.cols, row, at, a.aligned_gy, lane);
+                if (!kKept) copy_piece(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, a.rows, a.cols, row, at, a.aligned_x, lane);
+                if (kKept && c0 < a.cols) {
                     const unsigned char* p = a.codes + row * a.ld_codes + c0;
                     if (E == 16)
-                        copy16(ring_x + (unsigned)(slot * kThreads * 16), p, 16);
+                        copy16(ring_codes + (unsigned)((slot * WIDE + j) * kThreads * 16), p, 16);
                     else
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_x + (unsigned)(slot * kThreads * 16) + 8 * j), "l"(p) : "memory");
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_codes + (unsigned)((slot * WIDE + j / 2) * kThreads * 16) + 8 * (j & 1)), "l"(p) : "memory");
                 }
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    auto words_of = [&](unsigned from, int slot, int j, unsigned(&w)[8], int n) {
-        const unsigned at = from + (unsigned)((slot * V + j) * 2 * kThreads * 16);
-        const uint4 p = take16(at), q = n * (int)sizeof(T) > 16 ? take16(at + kThreads * 16) : make_uint4(0, 0, 0, 0);
-        w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
-        w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
     };
     const long long first = (long long)blockIdx.x * S::kGroups + group;
 #pragma unroll
@@ -288,9 +359,20 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(con
         }
     };
     fetch_small(first);
+    // the weight stays in registers where it is of the operands' type
+    const bool own_type = a.param_bf16 == (sizeof(T) == 2);
+    unsigned weight[V][8];
+    if (a.w && own_type) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c0 = (j * 32 * WPR + t) * E;
+            if (c0 < a.cols) K::load_words(static_cast<const T*>(a.w) + c0, min(E, a.cols - c0), weight[j]);
+        }
+    }
     for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += stride) {
         const long long row = row0 + group;
         const bool live = row < a.rows;
+        __syncwarp();  // the piece that is copied over has been read by all lanes
         if (kAhead > 0) begin_copy(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
         const float mean = next_mean, rstd = live ? next_rstd : 0.0f;
         float p[V];
@@ -300,52 +382,67 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(con
         }
         fetch_small(row + stride);
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead > 0 ? kAhead - 1 : 0) : "memory");
+        __syncwarp();
         K h[V], g[V];
         float2 c2 = make_float2(0.0f, 0.0f), c1 = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int c0 = (j * 32 * WPR + t) * E;
             const int n = live ? min(E, a.cols - c0) : 0;
+            unsigned w8[8], x8[8];
+            if (kAhead > 0) {
+                const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
+                take_chunk(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, row, c0, a.aligned_gy, lane, n, w8);
+                if (!kKept) take_chunk(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, row, c0, a.aligned_x, lane, n, x8);
+            } else if (n > 0) {
+                K::load_words(static_cast<const T*>(a.gy) + row * a.ld_gy + c0, n, w8);
+                if (!kKept) K::load_words(static_cast<const T*>(a.x) + row * a.ld_x + c0, n, x8);
+            }
             h[j].zero();
             g[j].zero();
             if (n <= 0) continue;
-            unsigned w8[8];
-            if (async_gy)
-                words_of(ring_gy, slot, j, w8, n);
-            else
-                K::load_words(static_cast<const T*>(a.gy) + row * a.ld_gy + c0, n, w8);
             g[j].from_words(w8);
             if (kKept) {
                 constexpr int F = kKept ? FMT : AMPQ_FMT_E4M3;
-                const uint4 q = take16(ring_x + (unsigned)(slot * kThreads * 16));
+                const uint4 q = take16(ring_codes + (unsigned)((slot * WIDE + j * E / 16) * kThreads * 16));
                 unsigned c[E / 4];
                 if (E == 16) {
                     c[0] = q.x; c[1] = q.y; c[2 % (E / 4)] = q.z; c[3 % (E / 4)] = q.w;
                 } else {
-                    c[0] = j ? q.z : q.x;
-                    c[1] = j ? q.w : q.y;
+                    c[0] = j & 1 ? q.z : q.x;
+                    c[1] = j & 1 ? q.w : q.y;
                 }
                 h[j].template decode<F>(c);
             } else {
-                if (async_x)
-                    words_of(ring_x, slot, j, w8, n);
-                else
-                    K::load_words(static_cast<const T*>(a.x) + row * a.ld_x + c0, n, w8);
-                h[j].from_words(w8);
+                h[j].from_words(x8);
             }
-            K w;
-            if (a.w) load_params(a.w, a.param_bf16, c0, n, w);
+            // (x - mean) * rstd; the scale of a kept x joins the subtraction
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                // (x - mean) * rstd; the scale of a kept x joins the subtraction
-                const float2 d = kKept ? __ffma2_rn(h[j].v[i], make_float2(p[j], p[j]), make_float2(-mean, -mean)) : __fadd2_rn(h[j].v[i], make_float2(-mean, -mean));
-                float2 hh = __fmul2_rn(d, make_float2(rstd, rstd));
-                if (n < E) hh = make_float2(2 * i < n ? hh.x : 0.0f, 2 * i + 1 < n ? hh.y : 0.0f);
-                h[j].v[i] = hh;
-                sum_w[j][i] = __ffma2_rn(g[j].v[i], hh, sum_w[j][i]);
+                float2 d = h[j].v[i];
+                if (kKept && LAYER) d = __ffma2_rn(d, make_float2(p[j], p[j]), make_float2(-mean, -mean));
+                if (kKept && !LAYER) d = __fmul2_rn(d, make_float2(p[j], p[j]));
+                if (!kKept && LAYER) d = __fadd2_rn(d, make_float2(-mean, -mean));
+                h[j].v[i] = __fmul2_rn(d, make_float2(rstd, rstd));
+            }
+            // behind the last column gy is 0, and h finite unless the row's sums are not
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                sum_w[j][i] = __ffma2_rn(g[j].v[i], h[j].v[i], sum_w[j][i]);
                 if (LAYER) sum_b[j][i] = __fadd2_rn(sum_b[j][i], g[j].v[i]);
-                if (a.w) g[j].v[i] = __fmul2_rn(g[j].v[i], w.v[i]);
-                c2 = __ffma2_rn(g[j].v[i], hh, c2);
+            }
+            if (a.w) {
+                K w;
+                if (own_type)
+                    w.from_words(weight[j]);
+                else
+                    load_params(a.w, a.param_bf16, c0, n, w);
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) g[j].v[i] = __fmul2_rn(g[j].v[i], w.v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                c2 = __ffma2_rn(g[j].v[i], h[j].v[i], c2);
                 if (LAYER) c1 = __fadd2_rn(c1, g[j].v[i]);
             }
         }
@@ -395,84 +492,87 @@ __global__ void __launch_bounds__(Shape<WPR>::kThreads) norm_backward_kernel(con
             for (int j = 0; j < V; ++j)
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i)
-                    *reinterpret_cast<float2*>(join + group * S::kSpan + (j * 32 * WPR + t) * E + 2 * i) = k ? sum_b[j][i] : sum_w[j][i];
+                    *reinterpret_cast<float2*>(join + group * kSpan + (j * 32 * WPR + t) * E + 2 * i) = k ? sum_b[j][i] : sum_w[j][i];
             __syncthreads();
             for (int i = threadIdx.x; i < a.cols; i += kThreads) {
                 float s = 0.0f;
 #pragma unroll
-                for (int g = 0; g < S::kGroups; ++g) s += join[g * S::kSpan + i];
+                for (int g = 0; g < S::kGroups; ++g) s += join[g * kSpan + i];
                 out[i] = s;
             }
         }
     }
 }
 
-// Warps of a row: 512 columns each, a power of two.
-int warps_per_row(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 8192 ? 16 : 32; }
+// Warps of a row, a power of two: 512 columns each, 1024 above 4096 columns.
+int warps_per_row(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 8192 ? 8 : 16; }
+// of the backward pass
+int backward_warps(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 8192 ? 16 : 32; }
 
 // CTAs of the backward pass: every row group gets a row before one gets two, and
 // no more CTAs than are resident, so that the sums stay in registers.
 int backward_ctas(long long rows, int cols, int sms) {
-    const int wpr = warps_per_row(cols), groups = wpr < 8 ? 8 / wpr : 1;
+    const int wpr = backward_warps(cols), groups = wpr < 8 ? 8 / wpr : 1;
     const long long need = (rows + groups - 1) / groups;
     const long long most = (long long)sms * (wpr <= 8 ? 2 : 1);
     return (int)(need < most ? need : most);
 }
 
-template <typename T, int FMT, int WPR>
-void start_forward(const ForwardArgs& a, cudaStream_t st) {
-    const long long blocks = (a.rows + Shape<WPR>::kGroups - 1) / Shape<WPR>::kGroups;
-    norm_forward_kernel<T, FMT, WPR><<<(unsigned)blocks, Shape<WPR>::kThreads, 0, st>>>(a);
+template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+int start_forward(const ForwardArgs& a, cudaStream_t st) {
+    using S = Shape<WPR, WIDE>;
+    const long long blocks = (a.rows + S::kGroups - 1) / S::kGroups;
+    norm_forward_kernel<T, FMT, LAYER, WPR, WIDE><<<(unsigned)blocks, S::kThreads, 0, st>>>(a);
+    return launched();
 }
 
-template <typename T, int FMT>
+template <typename T, int FMT, bool LAYER>
 int launch_forward(const ForwardArgs& a, cudaStream_t st) {
+    if (a.cols > 4096) return a.cols <= 8192 ? start_forward<T, FMT, LAYER, 8, 2>(a, st) : start_forward<T, FMT, LAYER, 16, 2>(a, st);
     switch (warps_per_row(a.cols)) {
-        case 1: start_forward<T, FMT, 1>(a, st); break;
-        case 2: start_forward<T, FMT, 2>(a, st); break;
-        case 4: start_forward<T, FMT, 4>(a, st); break;
-        case 8: start_forward<T, FMT, 8>(a, st); break;
-        case 16: start_forward<T, FMT, 16>(a, st); break;
-        default: start_forward<T, FMT, 32>(a, st);
+        case 1: return start_forward<T, FMT, LAYER, 1, 1>(a, st);
+        case 2: return start_forward<T, FMT, LAYER, 2, 1>(a, st);
+        case 4: return start_forward<T, FMT, LAYER, 4, 1>(a, st);
+        default: return start_forward<T, FMT, LAYER, 8, 1>(a, st);
     }
-    return launched();
 }
 
 constexpr int kMaxDevices = 64;
 
-template <typename T, int FMT, bool LAYER, int WPR>
+template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
 int start_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
     static std::atomic<bool> prepared[kMaxDevices];  // the kernel may use its shared memory on that device
-    constexpr int kJoin = Shape<WPR>::kGroups > 1 ? Shape<WPR>::kGroups * Shape<WPR>::kSpan * 4 : 0;
-    constexpr int kBytes = Ring<T, FMT, WPR>::kBytes > kJoin ? Ring<T, FMT, WPR>::kBytes : kJoin;
+    using S = Shape<WPR, WIDE>;
+    constexpr int kJoin = S::kGroups > 1 ? S::kGroups * 512 * WPR * WIDE * 4 : 0;
+    constexpr int kBytes = Ring<T, FMT, WPR, WIDE>::kBytes > kJoin ? Ring<T, FMT, WPR, WIDE>::kBytes : kJoin;
     if (kBytes > 32 * 1024 && (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire))) {
-        if (cudaFuncSetAttribute(norm_backward_kernel<T, FMT, LAYER, WPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+        if (cudaFuncSetAttribute(norm_backward_kernel<T, FMT, LAYER, WPR, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
             cudaGetLastError();
             return AMPQ_ERR_CUDA;
         }
         if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
     }
-    norm_backward_kernel<T, FMT, LAYER, WPR><<<(unsigned)ctas, Shape<WPR>::kThreads, kBytes, st>>>(a);
+    norm_backward_kernel<T, FMT, LAYER, WPR, WIDE><<<(unsigned)ctas, S::kThreads, kBytes, st>>>(a);
     return launched();
 }
 
 template <typename T, int FMT, bool LAYER>
 int launch_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
-    switch (warps_per_row(a.cols)) {
-        case 1: return start_backward<T, FMT, LAYER, 1>(a, device, ctas, st);
-        case 2: return start_backward<T, FMT, LAYER, 2>(a, device, ctas, st);
-        case 4: return start_backward<T, FMT, LAYER, 4>(a, device, ctas, st);
-        case 8: return start_backward<T, FMT, LAYER, 8>(a, device, ctas, st);
-        case 16: return start_backward<T, FMT, LAYER, 16>(a, device, ctas, st);
-        default: return start_backward<T, FMT, LAYER, 32>(a, device, ctas, st);
+    switch (backward_warps(a.cols)) {
+        case 1: return start_backward<T, FMT, LAYER, 1, 1>(a, device, ctas, st);
+        case 2: return start_backward<T, FMT, LAYER, 2, 1>(a, device, ctas, st);
+        case 4: return start_backward<T, FMT, LAYER, 4, 1>(a, device, ctas, st);
+        case 8: return start_backward<T, FMT, LAYER, 8, 1>(a, device, ctas, st);
+        case 16: return start_backward<T, FMT, LAYER, 16, 1>(a, device, ctas, st);
+        default: return start_backward<T, FMT, LAYER, 32, 1>(a, device, ctas, st);
     }
 }
 
-template <typename T>
+template <typename T, bool LAYER>
 int dispatch_forward(int fmt, const ForwardArgs& a, cudaStream_t st) {
-    if (fmt == AMPQ_FMT_E4M3) return launch_forward<T, AMPQ_FMT_E4M3>(a, st);
-    if (fmt == AMPQ_FMT_E5M2) return launch_forward<T, AMPQ_FMT_E5M2>(a, st);
-    return launch_forward<T, AMPQ_FMT_BASE>(a, st);
+    if (fmt == AMPQ_FMT_E4M3) return launch_forward<T, AMPQ_FMT_E4M3, LAYER>(a, st);
+    if (fmt == AMPQ_FMT_E5M2) return launch_forward<T, AMPQ_FMT_E5M2, LAYER>(a, st);
+    return launch_forward<T, AMPQ_FMT_BASE, LAYER>(a, st);
 }
 
 template <typename T, bool LAYER>
@@ -522,10 +622,11 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     a.rows = rows; a.ld_x = ld_x; a.ld_y = ld_y; a.ld_codes = ld_codes; a.ld_scales = ld_scales;
     a.cols = (int)cols;
     a.eps = eps;
-    a.layer = layer;
+    a.whole = cols % (dtype == AMPQ_F32 ? 8 : 16) == 0;
     a.param_bf16 = param_dtype == AMPQ_BF16;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    return dtype == AMPQ_F32 ? dispatch_forward<float>(fmt, a, st) : dispatch_forward<__nv_bfloat16>(fmt, a, st);
+    if (dtype == AMPQ_F32) return layer ? dispatch_forward<float, true>(fmt, a, st) : dispatch_forward<float, false>(fmt, a, st);
+    return layer ? dispatch_forward<__nv_bfloat16, true>(fmt, a, st) : dispatch_forward<__nv_bfloat16, false>(fmt, a, st);
 }
 
 int ampq_norm_backward_workspace(int device, long long rows, long long cols, long long* bytes) {
@@ -574,8 +675,8 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.cols = (int)cols;
         a.param_bf16 = param_dtype == AMPQ_BF16;
         a.sum_b = gbias != nullptr;
-        a.async_gy = rows_aligned(gy, ld_gy, dtype);
-        a.async_x = rows_aligned(x, ld_x, dtype);
+        a.aligned_gy = rows_aligned(gy, ld_gy, dtype);
+        a.aligned_x = rows_aligned(x, ld_x, dtype);
         if (dtype == AMPQ_F32)
             rc = layer ? dispatch_backward<float, true>(fmt, a, device, ctas, st) : dispatch_backward<float, false>(fmt, a, device, ctas, st);
         else
