@@ -242,6 +242,28 @@ __device__ __forceinline__ void copy_piece(unsigned to, const T* m, long long ld
     }
 }
 
+// The scale bytes of a warp's chunk of one row (groups g0 to g0 + count - 1 of
+// `groups`), copied to shared memory by words from the one the first byte is in;
+// words that the matrix holds only parts of are put together by hand.
+__device__ __forceinline__ void copy_scales(unsigned to, const unsigned char* scales, long long ld, long long rows, int groups, long long row, int g0, int count,
+                                            unsigned lane) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(scales + row * ld + g0), down = p & ~(uintptr_t)3;
+    const int n = min(count, groups - g0);
+    const int words = n > 0 ? ((int)(p - down) + n + 3) / 4 : 0;
+    if ((int)lane >= words) return;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(scales), end = reinterpret_cast<uintptr_t>(scales + (rows - 1) * ld + groups);
+    const uintptr_t q = down + 4 * lane;
+    if (q >= begin && q + 4 <= end) {
+        copy4(to + 4 * lane, reinterpret_cast<const void*>(q));
+    } else {
+        unsigned w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (q + i >= begin && q + i < end) w |= (unsigned)__ldg(reinterpret_cast<const unsigned char*>(q + i)) << (8 * i);
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 4 * lane), "r"(w) : "memory");
+    }
+}
+
 // This lane's chunk of a piece, zeros from element n on.  All lanes call it.
 template <typename T>
 __device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long ld, long long row, int at, bool aligned, unsigned lane, int n, unsigned (&w)[8]) {
@@ -274,9 +296,13 @@ __device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long 
     }
 }
 
-// Shared memory of a CTA per row on its way: gy, and x or its codes.
+// Per warp: a row's mean and rstd, and the scale bytes of each chunk (at most five words).
+template <typename T, int WIDE>
+constexpr int kSmallPiece = 16 + 32 * kChunks<T, WIDE>;
+
+// Shared memory of a CTA per row on its way: gy, x or its codes, the row's small values.
 template <typename T, int FMT, int WPR, int WIDE>
-constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (FMT == AMPQ_FMT_BASE ? kChunks<T, WIDE> * kPiece : 512 * WIDE));
+constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (FMT == AMPQ_FMT_BASE ? kChunks<T, WIDE> * kPiece : 512 * WIDE) + kSmallPiece<T, WIDE>);
 
 // Rows on their way, the current one among them: four, or as many as leave room
 // for the CTAs meant to be resident; 0 where not even two fit (fp32 rows of more
@@ -312,6 +338,9 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     const unsigned ring_gy = (unsigned)__cvta_generic_to_shared(ring) + warp * V * kPiece;
     const unsigned ring_x = ring_gy + kAhead * kGyRow;
     const unsigned ring_codes = (unsigned)__cvta_generic_to_shared(ring) + kAhead * kGyRow + threadIdx.x * 16;
+    constexpr int kSmall = kSmallPiece<T, WIDE>;
+    const unsigned ring_small = (unsigned)__cvta_generic_to_shared(ring) + kAhead * (kRowBytes<T, FMT, WPR, WIDE> - S::kWarps * kSmall) + warp * kSmall;
+    const int groups = (a.cols + kGroup - 1) / kGroup;
     float2 sum_w[V][E / 2], sum_b[V][E / 2];
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -327,6 +356,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
                 copy_piece(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, a.rows, a.cols, row, at, a.aligned_gy, lane);
                 if (!kKept) copy_piece(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, a.rows, a.cols, row, at, a.aligned_x, lane);
+                if (kKept) copy_scales(ring_small + (unsigned)(slot * S::kWarps * kSmall + 16 + 32 * j), a.scales, a.ld_scales, a.rows, groups, row, at / kGroup, E, lane);
                 if (kKept && c0 < a.cols) {
                     const unsigned char* p = a.codes + row * a.ld_codes + c0;
                     if (E == 16)
@@ -336,6 +366,10 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 }
             }
         }
+        if (row < a.rows && lane < 2) {
+            const float* p = lane ? a.rstd : a.mean;
+            if (lane || LAYER) copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall) + 4 * lane, p + row);
+        }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     const long long first = (long long)blockIdx.x * S::kGroups + group;
@@ -343,22 +377,6 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     for (int s = 0; s < kAhead - 1; ++s) begin_copy(first + s * stride, s);
     int slot = 0;
     int phase = 0;
-    // the statistics and scale bytes of the next row are loaded one row ahead
-    float next_mean = 0.0f, next_rstd = 0.0f;
-    unsigned next_byte[V];
-    auto fetch_small = [&](long long row) {
-        if (row >= a.rows) return;
-        next_rstd = __ldg(a.rstd + row);
-        if (LAYER) next_mean = __ldg(a.mean + row);
-        if (kKept) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c0 = (j * 32 * WPR + t) * E;
-                next_byte[j] = c0 < a.cols ? __ldg(a.scales + row * a.ld_scales + c0 / kGroup) : 127u;
-            }
-        }
-    };
-    fetch_small(first);
     // the weight stays in registers where it is of the operands' type
     const bool own_type = a.param_bf16 == (sizeof(T) == 2);
     unsigned weight[V][8];
@@ -374,15 +392,28 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         const bool live = row < a.rows;
         __syncwarp();  // the piece that is copied over has been read by all lanes
         if (kAhead > 0) begin_copy(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
-        const float mean = next_mean, rstd = live ? next_rstd : 0.0f;
-        float p[V];
-        if (kKept) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = scale_of(next_byte[j]);
-        }
-        fetch_small(row + stride);
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead > 0 ? kAhead - 1 : 0) : "memory");
         __syncwarp();
+        float mean = 0.0f, rstd = 0.0f, p[V];
+        if (live) {
+            if (kAhead > 0) {
+                const unsigned small = ring_small + (unsigned)(slot * S::kWarps * kSmall);
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rstd) : "r"(small + 4) : "memory");
+                if (LAYER) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(mean) : "r"(small) : "memory");
+                if (kKept) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const unsigned from = (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3);
+                        unsigned byte;
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(small + 16 + 32 * j + from + lane / K::kLanes) : "memory");
+                        p[j] = scale_of(byte);
+                    }
+                }
+            } else {
+                rstd = __ldg(a.rstd + row);
+                if (LAYER) mean = __ldg(a.mean + row);
+            }
+        }
         K h[V], g[V];
         float2 c2 = make_float2(0.0f, 0.0f), c1 = make_float2(0.0f, 0.0f);
 #pragma unroll
