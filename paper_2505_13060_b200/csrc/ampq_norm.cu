@@ -187,6 +187,7 @@ struct BackwardArgs {
     int cols;
     bool param_bf16, sum_b;
     bool aligned_gy, aligned_x;  // rows start on 16-byte boundaries
+    bool aligned_scales;         // rows of scale bytes are whole words
 };
 
 __device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
@@ -348,7 +349,54 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         for (int i = 0; i < E / 2; ++i) sum_w[j][i] = sum_b[j][i] = make_float2(0.0f, 0.0f);
     const float inv_cols = 1.0f / (float)a.cols;
     const long long stride = (long long)gridDim.x * S::kGroups;
-    auto begin_copy = [&](long long row, int slot) {
+    // Rows on 16-byte boundaries: where this lane copies from next, and how much.
+    const bool straight = a.aligned_gy && (kKept ? a.aligned_scales : a.aligned_x);
+    constexpr int kPer = 16 / (int)sizeof(T);
+    const long long copy_first = (long long)blockIdx.x * S::kGroups + group;
+    const T* from_gy = static_cast<const T*>(a.gy) + copy_first * a.ld_gy + (t - (int)lane) * E + (int)lane * kPer;
+    const T* from_x = kKept ? nullptr : static_cast<const T*>(a.x) + copy_first * a.ld_x + (t - (int)lane) * E + (int)lane * kPer;
+    const unsigned char* from_codes = kKept ? a.codes + copy_first * a.ld_codes + t * E : nullptr;
+    const unsigned char* from_scales = kKept ? a.scales + copy_first * a.ld_scales + (t - (int)lane) * E / kGroup + 4 * lane : nullptr;
+    const float* from_stats = (lane ? a.rstd : a.mean) + copy_first;
+    auto copy_straight = [&](long long row, int slot) {
+        if (row < a.rows) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                constexpr int kStep = 32 * WPR * E;
+                const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = j * kStep + (t - (int)lane) * E + (32 * k + (int)lane) * kPer;
+                    const int bytes = min(16, (a.cols - at) * (int)sizeof(T));
+                    if (bytes > 0) {
+                        copy16(ring_gy + piece + 16 * (32 * k + lane), from_gy + j * kStep + 32 * k * kPer, bytes);
+                        if (!kKept) copy16(ring_x + piece + 16 * (32 * k + lane), from_x + j * kStep + 32 * k * kPer, bytes);
+                    }
+                }
+                if (kKept) {
+                    const int c0 = (j * 32 * WPR + t) * E;
+                    if (c0 < a.cols) {
+                        if (E == 16)
+                            copy16(ring_codes + (unsigned)((slot * WIDE + j) * kThreads * 16), from_codes + j * kStep, 16);
+                        else
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_codes + (unsigned)((slot * WIDE + j / 2) * kThreads * 16) + 8 * (j & 1)), "l"(from_codes + j * kStep) : "memory");
+                    }
+                    if ((int)lane < E / 4 && (j * kStep + (t - (int)lane) * E) / kGroup + 4 * (int)lane < groups)
+                        copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall + 16 + 32 * j) + 4 * lane, from_scales + j * kStep / kGroup);
+                }
+            }
+            if (lane < 2 && (lane || LAYER)) copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall) + 4 * lane, from_stats);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        from_gy += stride * a.ld_gy;
+        if (!kKept) from_x += stride * a.ld_x;
+        if (kKept) {
+            from_codes += stride * a.ld_codes;
+            from_scales += stride * a.ld_scales;
+        }
+        from_stats += stride;
+    };
+    auto copy_any = [&](long long row, int slot) {
         if (row < a.rows) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -372,20 +420,26 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    auto begin_copy = [&](long long row, int slot) {
+        if (straight)
+            copy_straight(row, slot);
+        else
+            copy_any(row, slot);
+    };
     const long long first = (long long)blockIdx.x * S::kGroups + group;
 #pragma unroll
     for (int s = 0; s < kAhead - 1; ++s) begin_copy(first + s * stride, s);
     int slot = 0;
     int phase = 0;
-    // the weight stays in registers where it is of the operands' type
-    const bool own_type = a.param_bf16 == (sizeof(T) == 2);
-    unsigned weight[V][8];
-    if (a.w && own_type) {
+    K weight[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = (j * 32 * WPR + t) * E;
-            if (c0 < a.cols) K::load_words(static_cast<const T*>(a.w) + c0, min(E, a.cols - c0), weight[j]);
-        }
+    for (int j = 0; j < V; ++j) {
+        const int c0 = (j * 32 * WPR + t) * E;
+        if (a.w && c0 < a.cols)
+            load_params(a.w, a.param_bf16, c0, min(E, a.cols - c0), weight[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) weight[j].v[i] = make_float2(1.0f, 1.0f);
     }
     for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += stride) {
         const long long row = row0 + group;
@@ -403,7 +457,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 if (kKept) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const unsigned from = (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3);
+                        const unsigned from = straight ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3);
                         unsigned byte;
                         asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(small + 16 + 32 * j + from + lane / K::kLanes) : "memory");
                         p[j] = scale_of(byte);
@@ -462,15 +516,8 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 sum_w[j][i] = __ffma2_rn(g[j].v[i], h[j].v[i], sum_w[j][i]);
                 if (LAYER) sum_b[j][i] = __fadd2_rn(sum_b[j][i], g[j].v[i]);
             }
-            if (a.w) {
-                K w;
-                if (own_type)
-                    w.from_words(weight[j]);
-                else
-                    load_params(a.w, a.param_bf16, c0, n, w);
 #pragma unroll
-                for (int i = 0; i < E / 2; ++i) g[j].v[i] = __fmul2_rn(g[j].v[i], w.v[i]);
-            }
+            for (int i = 0; i < E / 2; ++i) g[j].v[i] = __fmul2_rn(g[j].v[i], weight[j].v[i]);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
                 c2 = __ffma2_rn(g[j].v[i], h[j].v[i], c2);
@@ -708,6 +755,7 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.sum_b = gbias != nullptr;
         a.aligned_gy = rows_aligned(gy, ld_gy, dtype);
         a.aligned_x = rows_aligned(x, ld_x, dtype);
+        a.aligned_scales = aligned_to(scales, 4) && ld_scales % 4 == 0 && ((cols + kGroup - 1) / kGroup) % 4 == 0;
         if (dtype == AMPQ_F32)
             rc = layer ? dispatch_backward<float, true>(fmt, a, device, ctas, st) : dispatch_backward<float, false>(fmt, a, device, ctas, st);
         else
