@@ -14,6 +14,7 @@ slice of a wider tensor is read in place), anything else is made contiguous.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -59,11 +60,13 @@ def _check(rc: int, what: str):
         raise AmpqError(rc, what)
 
 
-def _where(t: torch.Tensor):
-    """(device index, current stream's handle) of a tensor."""
+def _device_of(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("tensors are on a CUDA device, got %s" % t.device)
-    return t.device.index, torch._C._cuda_getCurrentRawStream(t.device.index)
+    return t.device.index
+
+
+_stream_of = torch._C._cuda_getCurrentRawStream  # the handle of torch's current stream on a device
 
 
 def _code(t: torch.Tensor) -> int:
@@ -75,35 +78,39 @@ def _code(t: torch.Tensor) -> int:
 
 def _pitch(t: torch.Tensor) -> int:
     """Elements between two rows of a matrix with contiguous rows."""
-    return t.stride(0) if t.shape[0] > 1 and t.shape[1] > 0 else t.shape[1]
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 and cols > 0 else cols
 
 
 def _matrix(t: torch.Tensor) -> torch.Tensor:
     """t as rows of its last dimension, without a copy where the layout allows it."""
-    if t.dim() == 0:
-        raise ValueError("operands have at least one dimension")
-    m = t
     if t.dim() != 2:
+        if t.dim() == 0:
+            raise ValueError("operands have at least one dimension")
         rows = 1
         for d in t.shape[:-1]:
             rows *= d
-        m = t.reshape(rows, t.shape[-1])  # a view where it can be one
-    if (m.shape[1] > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < m.shape[1]):
-        m = m.contiguous()
-    return m
+        t = t.reshape(rows, t.shape[-1])  # a view where it can be one
+    if not t.is_contiguous():
+        rows, cols = t.shape
+        if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+            t = t.contiguous()
+    return t
 
 
-def _same_device(first: torch.Tensor, *others):
+def _same_device(device: int, *others):
     for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("operands are on one device, got %s and %s" % (first.device, t.device))
+        if t is not None and (not t.is_cuda or t.device.index != device):
+            raise ValueError("operands are on one device, got cuda:%d and %s" % (device, t.device))
 
 
 def _new_packed(rows: int, cols: int, fmt: int, device) -> Packed:
     groups = -(-cols // ampq.CKPT_GROUP)
-    codes = torch.empty(rows, groups * ampq.CKPT_GROUP, dtype=torch.uint8, device=device)
-    scales = torch.empty(rows, groups, dtype=torch.uint8, device=device)
-    return Packed(codes, scales, cols, fmt)
+    p = object.__new__(Packed)
+    p.codes = torch.empty(rows, groups * ampq.CKPT_GROUP, dtype=torch.uint8, device=device)
+    p.scales = torch.empty(rows, groups, dtype=torch.uint8, device=device)
+    p.cols, p.fmt = cols, fmt
+    return p
 
 
 def _packed_args(p: Packed):
@@ -118,28 +125,46 @@ def _param(t, cols: int, like=None):
         raise ValueError("a norm over %d columns has parameters of that many elements, got %s" % (cols, tuple(t.shape)))
     if like is not None and like.dtype != t.dtype:
         raise TypeError("weight and bias are of one type, got %s and %s" % (like.dtype, t.dtype))
-    return t.reshape(-1).contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
 
+# The workspaces depend on sizes, types and alignment alone.
+@functools.lru_cache(maxsize=4096)
+def _weight_grad_bytes(device: int, code: int, misalignment: int, pitch: int, samples: int, rows: int, cols: int, outs: int, bias: int) -> int:
+    need = C.c_longlong()
+    _check(ampq.lib().ampq_ckpt_weight_grad_workspace(device, code, misalignment, pitch, samples, rows, cols, outs, bias, C.byref(need)),
+           "ampq_ckpt_weight_grad_workspace")
+    return need.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_backward_bytes(device: int, rows: int, cols: int) -> int:
+    need = C.c_longlong()
+    _check(ampq.lib().ampq_norm_backward_workspace(device, rows, cols, C.byref(need)), "ampq_norm_backward_workspace")
+    return need.value
+
+
 def pack(x: torch.Tensor, fmt: int = ampq.FMT_E4M3) -> Packed:
     """The 8-bit checkpoint of x."""
     m = _matrix(x)
-    device, stream = _where(m)
-    p = _new_packed(m.shape[0], m.shape[1], fmt, m.device)
-    _check(ampq.lib().ampq_ckpt_pack(device, stream, _code(m), fmt, m.data_ptr(), m.shape[0], m.shape[1], _pitch(m), *_packed_args(p)),
+    device = _device_of(m)
+    rows, cols = m.shape
+    p = _new_packed(rows, cols, fmt, m.device)
+    _check(ampq.lib().ampq_ckpt_pack(device, _stream_of(device), _code(m), fmt, m.data_ptr(), rows, cols, _pitch(m), *_packed_args(p)),
            "ampq_ckpt_pack")
     return p
 
 
 def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values a checkpoint stands for, [rows, cols]; exact in either type."""
-    out = torch.empty(p.rows, p.cols, dtype=dtype, device=p.device)
-    device, stream = _where(out)
-    _check(ampq.lib().ampq_ckpt_unpack(device, stream, _code(out), p.fmt, *_packed_args(p), p.rows, p.cols, out.data_ptr(), _pitch(out)),
+    rows, cols = p.codes.shape[0], p.cols
+    device = _device_of(p.codes)
+    out = torch.empty(rows, cols, dtype=dtype, device=p.codes.device)
+    _check(ampq.lib().ampq_ckpt_unpack(device, _stream_of(device), _code(out), p.fmt, *_packed_args(p), rows, cols, out.data_ptr(), cols),
            "ampq_ckpt_unpack")
     return out
 
@@ -149,20 +174,18 @@ def weight_grad(p: Packed, gy: torch.Tensor, samples: int = 1, bias: bool = Fals
     gradient of its output, one per sample: the rows are ``samples`` equal runs.
     Returns (gw [samples, outs, cols], gb [samples, outs] or None) in gy's type."""
     g = _matrix(gy)
-    _same_device(p.codes, g)
-    if samples < 1 or g.shape[0] != p.rows or p.rows % samples:
-        raise ValueError("%d gradient rows, %d checkpoint rows, %d samples" % (g.shape[0], p.rows, samples))
-    device, stream = _where(g)
-    rows, outs, code = p.rows // samples, g.shape[1], _code(g)
-    L = ampq.lib()
-    gw = torch.empty(samples, outs, p.cols, dtype=g.dtype, device=g.device)
-    gb = torch.empty(samples, outs, dtype=g.dtype, device=g.device) if bias else None
-    need = C.c_longlong()
-    _check(L.ampq_ckpt_weight_grad_workspace(device, code, g.data_ptr(), _pitch(g), samples, rows, p.cols, outs, 1 if bias else 0,
-                                             C.byref(need)), "ampq_ckpt_weight_grad_workspace")
-    ws = torch.empty(need.value, dtype=torch.uint8, device=g.device) if need.value else None
-    _check(L.ampq_ckpt_weight_grad(device, stream, code, p.fmt, g.data_ptr(), _pitch(g), *_packed_args(p), samples, rows, p.cols, outs,
-                                   gw.data_ptr(), _ptr(gb), _ptr(ws), need.value), "ampq_ckpt_weight_grad")
+    device = _device_of(g)
+    _same_device(device, p.codes)
+    total, outs = g.shape
+    if samples < 1 or total != p.codes.shape[0] or total % samples:
+        raise ValueError("%d gradient rows, %d checkpoint rows, %d samples" % (total, p.rows, samples))
+    rows, cols, code, pitch, where, ptr = total // samples, p.cols, _code(g), _pitch(g), g.device, g.data_ptr()
+    gw = torch.empty(samples, outs, cols, dtype=g.dtype, device=where)
+    gb = torch.empty(samples, outs, dtype=g.dtype, device=where) if bias else None
+    need = _weight_grad_bytes(device, code, ptr % 16, pitch, samples, rows, cols, outs, 1 if bias else 0)
+    ws = torch.empty(need, dtype=torch.uint8, device=where) if need else None
+    _check(ampq.lib().ampq_ckpt_weight_grad(device, _stream_of(device), code, p.fmt, ptr, pitch, *_packed_args(p), samples, rows, cols, outs,
+                                            gw.data_ptr(), _ptr(gb), _ptr(ws), need), "ampq_ckpt_weight_grad")
     return gw, gb
 
 
@@ -170,19 +193,20 @@ def norm_forward(x: torch.Tensor, weight, bias, eps: float, kind: int = ampq.NOR
     """Layer norm or RMS norm over the last dimension.  Returns (y, mean, rstd, p):
     mean is None for an RMS norm, p the checkpoint of x or None for ``FMT_BASE``."""
     m = _matrix(x)
-    _same_device(m, weight, bias)
-    device, stream = _where(m)
+    device = _device_of(m)
+    _same_device(device, weight, bias)
+    where, code = m.device, _code(m)
     rows, cols = m.shape
     weight = _param(weight, cols)
     bias = _param(bias, cols, weight)
-    first = weight if weight is not None else bias
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    mean = torch.empty(rows, dtype=torch.float32, device=x.device) if kind == ampq.NORM_LAYER else None
-    p = _new_packed(rows, cols, fmt, x.device) if fmt != ampq.FMT_BASE else None
-    _check(ampq.lib().ampq_norm_forward(device, stream, kind, _code(m), _code(first) if first is not None else _code(m), fmt, m.data_ptr(),
-                                        _pitch(m), rows, cols, _ptr(weight), _ptr(bias), eps, y.data_ptr(), cols, _ptr(mean),
-                                        rstd.data_ptr(), *(_packed_args(p) if p is not None else (0, 0, 0, 0))), "ampq_norm_forward")
+    y = torch.empty(x.shape, dtype=x.dtype, device=where)
+    rstd = torch.empty(rows, dtype=torch.float32, device=where)
+    mean = torch.empty(rows, dtype=torch.float32, device=where) if kind == ampq.NORM_LAYER else None
+    p = _new_packed(rows, cols, fmt, where) if fmt != ampq.FMT_BASE else None
+    pcode = _code(weight) if weight is not None else _code(bias) if bias is not None else code
+    _check(ampq.lib().ampq_norm_forward(device, _stream_of(device), kind, code, pcode, fmt, m.data_ptr(), _pitch(m), rows, cols, _ptr(weight),
+                                        _ptr(bias), eps, y.data_ptr(), cols, _ptr(mean), rstd.data_ptr(),
+                                        *(_packed_args(p) if p is not None else (0, 0, 0, 0))), "ampq_norm_forward")
     return y, mean, rstd, p
 
 
@@ -190,33 +214,98 @@ def norm_backward(gy: torch.Tensor, x, mean, rstd: torch.Tensor, weight, kind: i
     """Backward pass of ``norm_forward``; x is the input or its checkpoint.  Returns
     (gx, gw, gb): gw is None without a weight, gb unless a layer norm with a bias."""
     g = _matrix(gy)
+    device = _device_of(g)
     rows, cols = g.shape
     kept = isinstance(x, Packed)
     if not kept:
         x = _matrix(x)
-    _same_device(g, x.codes if kept else x, mean, rstd, weight)
+    _same_device(device, x.codes if kept else x, mean, rstd, weight)
     if (x.rows, x.cols) != (rows, cols) if kept else tuple(x.shape) != (rows, cols):
         raise ValueError("the input does not have the gradient's %d rows of %d columns" % (rows, cols))
     if not kept and x.dtype != g.dtype:
         raise TypeError("input and gradient are of one type, got %s and %s" % (x.dtype, g.dtype))
-    for t in (rstd, mean) if kind == ampq.NORM_LAYER else (rstd,):
+    layer = kind == ampq.NORM_LAYER
+    for t in (rstd, mean) if layer else (rstd,):
         if t is None or t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous():
             raise ValueError("mean and rstd are as norm_forward returned them")
-    device, stream = _where(g)
+    where, code = g.device, _code(g)
     weight = _param(weight, cols)
-    gx = torch.empty(gy.shape, dtype=g.dtype, device=g.device)
-    pdtype = weight.dtype if weight is not None else g.dtype
-    bias = bias and kind == ampq.NORM_LAYER
-    sums = weight is not None or bias
-    gw = torch.empty(cols, dtype=pdtype, device=g.device) if sums else None
-    gb = torch.empty(cols, dtype=pdtype, device=g.device) if bias else None
-    L = ampq.lib()
-    need, ws = C.c_longlong(), None
-    if sums:
-        _check(L.ampq_norm_backward_workspace(device, rows, cols, C.byref(need)), "ampq_norm_backward_workspace")
-        ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=g.device)
-    _check(L.ampq_norm_backward(device, stream, kind, _code(g), _code(weight) if weight is not None else _code(g), x.fmt if kept else ampq.FMT_BASE, g.data_ptr(), _pitch(g),
-                                0 if kept else x.data_ptr(), 0 if kept else _pitch(x), *(_packed_args(x) if kept else (0, 0, 0, 0)), rows, cols,
-                                _ptr(mean) if kind == ampq.NORM_LAYER else 0, rstd.data_ptr(), _ptr(weight), gx.data_ptr(), cols, _ptr(gw), _ptr(gb),
-                                _ptr(ws), need.value), "ampq_norm_backward")
+    pdtype, pcode = (weight.dtype, _code(weight)) if weight is not None else (g.dtype, code)
+    gx = torch.empty(gy.shape, dtype=g.dtype, device=where)
+    bias = bias and layer
+    gw = torch.empty(cols, dtype=pdtype, device=where) if weight is not None or bias else None
+    gb = torch.empty(cols, dtype=pdtype, device=where) if bias else None
+    need, ws = 0, None
+    if gw is not None:
+        need = _norm_backward_bytes(device, rows, cols)
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=where)
+    _check(ampq.lib().ampq_norm_backward(device, _stream_of(device), kind, code, pcode, x.fmt if kept else ampq.FMT_BASE, g.data_ptr(), _pitch(g),
+                                         0 if kept else x.data_ptr(), 0 if kept else _pitch(x), *(_packed_args(x) if kept else (0, 0, 0, 0)),
+                                         rows, cols, _ptr(mean) if layer else 0, rstd.data_ptr(), _ptr(weight), gx.data_ptr(), cols, _ptr(gw),
+                                         _ptr(gb), _ptr(ws), need), "ampq_norm_backward")
     return gx, gw if weight is not None else None, gb
+
+
+# -- differentiable forms ---------------------------------------------------------------------------------------------
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, fmt):
+        y = torch.nn.functional.linear(x, weight, bias)
+        p = pack(x.detach(), fmt) if weight.requires_grad else None
+        ctx.save_for_backward(weight, *((p.codes, p.scales) if p is not None else ()))
+        ctx.x_shape, ctx.fmt, ctx.bias = x.shape, fmt, bias is not None
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        weight, *kept = ctx.saved_tensors
+        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+        gx = gw = gb = None
+        if need_x:
+            gx = torch.matmul(gy, weight)
+        if need_w:
+            gw, gb = weight_grad(Packed(*kept, ctx.x_shape[-1], ctx.fmt), gy, bias=ctx.bias and need_b)
+            gw = gw[0]
+            gb = gb[0] if gb is not None else None
+        elif need_b:
+            gb = gy.reshape(-1, gy.shape[-1]).sum(0)
+        return gx, gw, gb, None
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, kind, fmt):
+        y, mean, rstd, p = norm_forward(x.detach(), weight, bias, eps, kind, fmt)
+        ctx.kept = p is not None
+        ctx.save_for_backward(weight, mean, rstd, *((p.codes, p.scales) if p is not None else (x,)))
+        ctx.cols, ctx.kind, ctx.fmt = x.shape[-1], kind, fmt
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        weight, mean, rstd, *kept = ctx.saved_tensors
+        need_b = ctx.needs_input_grad[2]
+        x = Packed(*kept, ctx.cols, ctx.fmt) if ctx.kept else kept[0]
+        gx, gw, gb = norm_backward(gy, x, mean, rstd, weight, ctx.kind, bias=need_b)
+        return gx, gw, gb, None, None, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias=None, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
+    """``torch.nn.functional.linear`` that keeps x for the backward pass in 8 bits:
+    the weight's gradient is that of the decoded x, everything else is exact."""
+    return _Linear.apply(x, weight, bias, fmt)
+
+
+def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
+    """Layer norm over the last dimension; x is kept for the backward pass in 8 bits,
+    or in full with ``FMT_BASE``."""
+    return _Norm.apply(x, weight, bias, eps, ampq.NORM_LAYER, fmt)
+
+
+def rms_norm(x: torch.Tensor, weight=None, eps: float = 1e-5, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
+    """RMS norm over the last dimension; x is kept as in ``layer_norm``."""
+    return _Norm.apply(x, weight, None, eps, ampq.NORM_RMS, fmt)

@@ -17,6 +17,17 @@ context's stream after the sample has completed, with at most two samples
 pending.  Everything the method computes happens in the CUDA library; this
 module only moves pointers.
 
+With ``checkpoint=FMT_E4M3`` (or ``FMT_E5M2``) the calibration keeps the inputs of
+the linear layers and of ``torch.nn.LayerNorm`` and ``torch.nn.RMSNorm`` modules in
+8 bits between the forward and the backward pass -- the memory that calibration
+needs beyond the model (Sec. 1) -- and forms the sample's weight gradients and the
+norms' gradients from there (``checkpoint``).  What is scored is what the backward
+pass has: the decoded inputs, each off by at most half a step of the format
+(2^-4 relative in E4M3), so the model's term S of an operand is off by at most
+13 %, on average by about the format's noise constant.  The measured term of a
+tensor that was already rounded says nothing, so the context is switched to the
+model's term alone (``set_measured(False)``).
+
 ``quantised(...)`` runs the model with chosen layers' inputs and weights replaced
 by their FP8-rounded values (``ampq_fake_quant``), which is how the predicted
 loss MSE is checked against a measured one (Sec. 3.2).
@@ -28,6 +39,7 @@ import contextlib
 import torch
 
 from . import binding as ampq
+from . import checkpoint as ckpt
 
 
 class BatchedMatmul(torch.nn.Module):
@@ -38,9 +50,37 @@ class BatchedMatmul(torch.nn.Module):
         return torch.matmul(a, b)
 
 
+class _ScoredLinear(torch.autograd.Function):
+    """A linear layer of a calibration with 8-bit checkpoints: its input is kept
+    packed, its backward pass streams the layer's two operands."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, calibrator, idx):
+        y = torch.nn.functional.linear(x, weight, bias)
+        p = ckpt.pack(x.detach(), calibrator.checkpoint)
+        ctx.save_for_backward(weight, p.codes, p.scales)
+        ctx.x_shape, ctx.calibrator, ctx.idx, ctx.r = x.shape, calibrator, idx, calibrator._r
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        weight, codes, scales = ctx.saved_tensors
+        cal, (need_x, need_w, need_b) = ctx.calibrator, ctx.needs_input_grad[:3]
+        p = ckpt.Packed(codes, scales, ctx.x_shape[-1], cal.checkpoint)
+        gx = torch.matmul(gy, weight)
+        gw, gb = ckpt.weight_grad(p, gy, bias=need_b)
+        if cal._r is not None:
+            cal._stream_linear(ctx.idx, ctx.r, ckpt.unpack(p, weight.dtype), gx, weight.detach(), gw[0])
+        return gx if need_x else None, gw[0] if need_w else None, gb[0] if need_b else None, None, None
+
+
 class Calibrator:
-    def __init__(self, ctx: "ampq.Context", model: torch.nn.Module, R: int):
-        self.ctx, self.model, self.R = ctx, model, R
+    def __init__(self, ctx: "ampq.Context", model: torch.nn.Module, R: int, checkpoint: int = ampq.FMT_BASE):
+        if checkpoint not in (ampq.FMT_BASE, ampq.FMT_E4M3, ampq.FMT_E5M2):
+            raise ValueError("checkpoint is FMT_BASE (inputs kept in full), FMT_E4M3 or FMT_E5M2")
+        self.ctx, self.model, self.R, self.checkpoint = ctx, model, R, checkpoint
+        self._replaced = []   # (module, its own forward attribute if it had one)
         self.modules, self.layer_ids = [], []
         for name, m in model.named_modules():
             if isinstance(m, torch.nn.Linear):
@@ -95,24 +135,67 @@ class Calibrator:
                     self.ctx.stream_sample(lid, k, self._r, ampq.torch_dtype_code(x), x.data_ptr(), gx.data_ptr(), x.numel())
                     self._keep += [x, gx]
                 return
-            x = self._x.pop(idx).contiguous()
+            x = self._x.pop(idx)
             gy = grad_output[0].detach()
             gx = grad_input[0]
-            w = module.weight.detach().contiguous()
+            w = module.weight.detach()
             if gx is None:   # the model input needs no gradient: form dL/dX here
                 gx = gy.reshape(-1, gy.shape[-1]) @ w
-            gx = gx.detach().reshape(x.shape).contiguous()
-            gw = (gy.reshape(-1, gy.shape[-1]).t() @ x.reshape(-1, x.shape[-1])).contiguous()
-            code = ampq.torch_dtype_code(x)
-            lid = self.layer_ids[idx]
-            self.ctx.stream_sample(lid, 0, self._r, code, x.data_ptr(), gx.data_ptr(), x.numel())
-            self.ctx.stream_sample(lid, 1, self._r, code, w.data_ptr(), gw.data_ptr(), w.numel())
-            self._keep += [x, gx, w, gw]
+            gw = gy.reshape(-1, gy.shape[-1]).t() @ x.reshape(-1, x.shape[-1])
+            self._stream_linear(idx, self._r, x, gx.detach(), w, gw)
         return hook
+
+    def _stream_linear(self, idx, r, x, gx, w, gw):
+        """Streams both operands of a linear layer for sample r."""
+        if not self._same_stream():
+            torch.cuda.ExternalStream(self.ctx.stream).wait_stream(torch.cuda.current_stream())
+        x, w, gw = x.contiguous(), w.contiguous(), gw.contiguous()
+        gx = gx.reshape(x.shape).contiguous()
+        code = ampq.torch_dtype_code(x)
+        lid = self.layer_ids[idx]
+        self.ctx.stream_sample(lid, 0, r, code, x.data_ptr(), gx.data_ptr(), x.numel())
+        self.ctx.stream_sample(lid, 1, r, code, w.data_ptr(), gw.data_ptr(), w.numel())
+        self._keep += [x, gx, w, gw]
+
+    # -- 8-bit checkpoints ------------------------------------------------------
+    def _replace(self, module, forward):
+        self._replaced.append((module, module.__dict__.get("forward")))
+        module.forward = forward
+
+    def _use_checkpoints(self):
+        """Sends the linear layers and norms through the calls that keep their input in 8 bits."""
+        fmt = self.checkpoint
+
+        def active(x):
+            return self._r is not None and torch.is_grad_enabled() and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16)
+
+        for idx, (_, m) in enumerate(self.modules):
+            if isinstance(m, torch.nn.Linear):
+
+                def linear(x, m=m, idx=idx, plain=m.forward):
+                    return _ScoredLinear.apply(x, m.weight, m.bias, self, idx) if active(x) else plain(x)
+
+                self._replace(m, linear)
+        for m in self.model.modules():
+            if isinstance(m, (torch.nn.LayerNorm, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
+
+                def norm(x, m=m, plain=m.forward):
+                    if not active(x):
+                        return plain(x)
+                    if isinstance(m, torch.nn.LayerNorm):
+                        return ckpt.layer_norm(x, m.weight, m.bias, m.eps, fmt)
+                    return ckpt.rms_norm(x, m.weight, torch.finfo(x.dtype).eps if m.eps is None else m.eps, fmt)
+
+                self._replace(m, norm)
 
     def begin(self):
         self._handles = []
+        if self.checkpoint != ampq.FMT_BASE:
+            self.ctx.set_measured(False)
+            self._use_checkpoints()
         for idx, (_, m) in enumerate(self.modules):
+            if self._replaced and isinstance(m, torch.nn.Linear):
+                continue
             self._handles.append(m.register_forward_hook(self._fwd(idx)))
             self._handles.append(m.register_full_backward_hook(self._bwd(idx)))
         self.ctx.stream_begin()
@@ -136,6 +219,12 @@ class Calibrator:
         for h in self._handles:
             h.remove()
         self._handles = []
+        for m, own in self._replaced:
+            if own is None:
+                del m.forward   # the class's again
+            else:
+                m.forward = own
+        self._replaced = []
         return res
 
     # -- running the model in a low-precision configuration --------------------

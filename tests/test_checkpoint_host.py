@@ -116,3 +116,10 @@ def test_reference_properties(fmt):
     assert np.array_equal(ref.unpack(codes2, scales2, 70, fmt), v)
     a = np.abs(np.pad(x, ((0, 0), (0, 26)))).reshape(200, 3, 32).max(2)
     assert (fmax * 2.0 ** (scales.astype(float) - 127) >= a).all() and (fmax * 2.0 ** (scales.astype(float) - 128) < a).all()
+
+
+def test_calibrator_refuses_unknown_checkpoints():
+    from paper_2505_13060_b200 import hooks
+
+    with pytest.raises(ValueError, match="checkpoint"):
+        hooks.Calibrator(None, torch.nn.Linear(2, 2), 1, checkpoint=3)
