@@ -454,9 +454,9 @@ int ampq_ckpt_unpack(int device, void *cuda_stream, int dtype, int fmt, const un
  *   gb      [samples, outs] of `dtype`, contiguous, or NULL
  * rows = 0 gives zeros.  Products are exact, sums are fp32, one rounding to
  * `dtype` at the end.  The workspace query takes the same gy (only its alignment
- * matters), and bias = 1 if gb will be asked for. */
+ * matters). */
 int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void *gy, long long ld_gy, long long samples, long long rows,
-                                    long long cols, long long outs, int bias, long long *bytes);
+                                    long long cols, long long outs, long long *bytes);
 int ampq_ckpt_weight_grad(int device, void *cuda_stream, int dtype, int fmt, const void *gy, long long ld_gy, const unsigned char *codes,
                           long long ld_codes, const unsigned char *scales, long long ld_scales, long long samples, long long rows,
                           long long cols, long long outs, void *gw, void *gb, void *workspace, long long workspace_bytes);

@@ -112,7 +112,7 @@ def lib():
     L.ampq_score_segment_noalloc.argtypes = [i, vp, i, i, vp, vp, ll, C.c_float, vp]
     L.ampq_ckpt_pack.argtypes = [i, vp, i, i, vp, ll, ll, ll, vp, ll, vp, ll]
     L.ampq_ckpt_unpack.argtypes = [i, vp, i, i, vp, ll, vp, ll, ll, ll, vp, ll]
-    L.ampq_ckpt_weight_grad_workspace.argtypes = [i, i, vp, ll, ll, ll, ll, ll, i, C.POINTER(ll)]
+    L.ampq_ckpt_weight_grad_workspace.argtypes = [i, i, vp, ll, ll, ll, ll, ll, C.POINTER(ll)]
     L.ampq_ckpt_weight_grad.argtypes = [i, vp, i, i, vp, ll, vp, ll, vp, ll, ll, ll, ll, ll, vp, vp, vp, ll]
     L.ampq_norm_forward.argtypes = [i, vp, i, i, i, i, vp, ll, ll, ll, vp, vp, C.c_float, vp, ll, vp, vp, vp, ll, vp, ll]
     L.ampq_norm_backward_workspace.argtypes = [i, ll, ll, C.POINTER(ll)]

@@ -134,9 +134,9 @@ def _ptr(t):
 
 # The workspaces depend on sizes, types and alignment alone.
 @functools.lru_cache(maxsize=4096)
-def _weight_grad_bytes(device: int, code: int, misalignment: int, pitch: int, samples: int, rows: int, cols: int, outs: int, bias: int) -> int:
+def _weight_grad_bytes(device: int, code: int, misalignment: int, pitch: int, samples: int, rows: int, cols: int, outs: int) -> int:
     need = C.c_longlong()
-    _check(ampq.lib().ampq_ckpt_weight_grad_workspace(device, code, misalignment, pitch, samples, rows, cols, outs, bias, C.byref(need)),
+    _check(ampq.lib().ampq_ckpt_weight_grad_workspace(device, code, misalignment, pitch, samples, rows, cols, outs, C.byref(need)),
            "ampq_ckpt_weight_grad_workspace")
     return need.value
 
@@ -182,7 +182,7 @@ def weight_grad(p: Packed, gy: torch.Tensor, samples: int = 1, bias: bool = Fals
     rows, cols, code, pitch, where, ptr = total // samples, p.cols, _code(g), _pitch(g), g.device, g.data_ptr()
     gw = torch.empty(samples, outs, cols, dtype=g.dtype, device=where)
     gb = torch.empty(samples, outs, dtype=g.dtype, device=where) if bias else None
-    need = _weight_grad_bytes(device, code, ptr % 16, pitch, samples, rows, cols, outs, 1 if bias else 0)
+    need = _weight_grad_bytes(device, code, ptr % 16, pitch, samples, rows, cols, outs)
     ws = torch.empty(need, dtype=torch.uint8, device=where) if need else None
     _check(ampq.lib().ampq_ckpt_weight_grad(device, _stream_of(device), code, p.fmt, ptr, pitch, *_packed_args(p), samples, rows, cols, outs,
                                             gw.data_ptr(), _ptr(gb), _ptr(ws), need), "ampq_ckpt_weight_grad")

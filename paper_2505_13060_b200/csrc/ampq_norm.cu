@@ -29,12 +29,13 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* red, int warp) {
         for (int k = 0; k < N; ++k) red[warp * N + k] = s[k];
     __syncthreads();
     // every lane takes one of the group's sums and they are added up as before
-    const int from = warp / WPR * WPR + (threadIdx.x & (WPR - 1));
+    constexpr int kLanes = WPR <= 2 ? 2 : WPR <= 4 ? 4 : WPR <= 8 ? 8 : WPR <= 16 ? 16 : 32;
+    const int from = threadIdx.x & (kLanes - 1);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        s[k] = red[from * N + k];
+        s[k] = from < WPR ? red[(warp / WPR * WPR + from) * N + k] : 0.0f;
 #pragma unroll
-        for (int o = WPR / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], o);
+        for (int o = kLanes / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], o);
     }
 }
 
@@ -79,13 +80,14 @@ struct ForwardArgs {
     float eps;
     bool param_bf16;
     bool whole;  // the last chunk of a row is a whole one
+    bool e4m3;   // the checkpoint's format
 };
 
 // One row per group of WPR warps, held in registers between the statistics (mean,
 // then the sum of squared differences from it) and the output, so x is read once.
 // Thread t of a group holds the chunks (j * threads + t): loads are contiguous
 // and neighbouring lanes make the groups of the checkpoint.
-template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads) norm_forward_kernel(const ForwardArgs a) {
     using S = Shape<WPR, WIDE>;
     using K = Chunk<T>;
@@ -149,12 +151,15 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads) norm_forward_kerne
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c0 = (j * 32 * WPR + t) * E;
-        if (FMT != AMPQ_FMT_BASE) {
-            constexpr int F = FMT == AMPQ_FMT_BASE ? AMPQ_FMT_E4M3 : FMT;
-            const unsigned byte = scale_byte<F>(k[j].group_amax());
+        if (KEPT) {
+            const unsigned amax = k[j].group_amax();
+            const unsigned byte = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(amax) : scale_byte<AMPQ_FMT_E5M2>(amax);
             if (live && (c0 & ~(kGroup - 1)) < a.cols) {  // whole groups: the columns behind the last are stored as 0
                 unsigned c[E / 4];
-                k[j].template encode<F>(byte, c);
+                if (a.e4m3)
+                    k[j].template encode<AMPQ_FMT_E4M3>(byte, c);
+                else
+                    k[j].template encode<AMPQ_FMT_E5M2>(byte, c);
                 store_codes(a.codes + row * a.ld_codes + c0, c);
                 if (t % K::kLanes == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
             }
@@ -186,6 +191,7 @@ struct BackwardArgs {
     long long rows, ld_gy, ld_x, ld_codes, ld_scales, ld_gx;
     int cols;
     bool param_bf16, sum_b;
+    bool e4m3;               // the checkpoint's format
     bool aligned_gy, aligned_x;  // rows start on 16-byte boundaries
     bool aligned_scales;         // rows of scale bytes are whole words
 };
@@ -228,7 +234,14 @@ __device__ __forceinline__ void copy_piece(unsigned to, const T* m, long long ld
     const int bytes = min(1024, (cols - at) * (int)sizeof(T));
     const int words = bytes > 0 ? ((int)(a0 - down) + bytes + 3) / 4 : 0;
     const uintptr_t begin = reinterpret_cast<uintptr_t>(m), end = reinterpret_cast<uintptr_t>(m + (rows - 1) * ld + cols);
+    if (down >= begin && down + 4 * words <= end) {  // nearly all pieces
+        const unsigned char* q = reinterpret_cast<const unsigned char*>(down) + 4 * lane;
 #pragma unroll
+        for (int k = 0; k < 9; ++k)
+            if (32 * k + (int)lane < words) copy4(to + 4 * (32 * k + lane), q + 128 * k);
+        return;
+    }
+#pragma unroll 1
     for (int k = 0; k < 9; ++k) {
         const int w = 32 * k + (int)lane;
         if (w >= words) break;
@@ -302,17 +315,17 @@ template <typename T, int WIDE>
 constexpr int kSmallPiece = 16 + 32 * kChunks<T, WIDE>;
 
 // Shared memory of a CTA per row on its way: gy, x or its codes, the row's small values.
-template <typename T, int FMT, int WPR, int WIDE>
-constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (FMT == AMPQ_FMT_BASE ? kChunks<T, WIDE> * kPiece : 512 * WIDE) + kSmallPiece<T, WIDE>);
+template <typename T, bool KEPT, int WPR, int WIDE>
+constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (KEPT ? 512 * WIDE : kChunks<T, WIDE> * kPiece) + kSmallPiece<T, WIDE>);
 
 // Rows on their way, the current one among them: four, or as many as leave room
 // for the CTAs meant to be resident; 0 where not even two fit (fp32 rows of more
 // than 8192 columns, kept in full) and rows are read as they come.
-template <typename T, int FMT, int WPR, int WIDE>
+template <typename T, bool KEPT, int WPR, int WIDE>
 struct Ring {
-    static constexpr int kFit = (WPR <= 8 ? 104 : 208) * 1024 / kRowBytes<T, FMT, WPR, WIDE>;
+    static constexpr int kFit = (WPR <= 10 ? 104 : 208) * 1024 / kRowBytes<T, KEPT, WPR, WIDE>;
     static constexpr int kRows = kFit >= 4 ? 4 : kFit >= 2 ? kFit : 0;
-    static constexpr int kBytes = kRows * kRowBytes<T, FMT, WPR, WIDE>;
+    static constexpr int kBytes = kRows * kRowBytes<T, KEPT, WPR, WIDE>;
 };
 
 // Rows are dealt to the row groups of a persistent grid; a thread keeps the fp32
@@ -321,14 +334,14 @@ struct Ring {
 // barrier: no other warp reads them), which keeps enough bytes on the way with the
 // few threads that the sums' registers allow.  The groups of a CTA are joined in
 // shared memory, the CTAs by join_columns_kernel, in a fixed order.
-template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
-__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::kThreads == 256 ? 2 : 1) norm_backward_kernel(const BackwardArgs a) {
+template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
+__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::kThreads <= 320 ? 2 : 1) norm_backward_kernel(const BackwardArgs a) {
     using S = Shape<WPR, WIDE>;
     using K = Chunk<T>;
     constexpr int V = kChunks<T, WIDE>, E = K::kElems, kThreads = S::kThreads, kSpan = 512 * WPR * WIDE;
-    constexpr bool kKept = FMT != AMPQ_FMT_BASE;
-    static_assert(!kKept || Ring<T, FMT, WPR, WIDE>::kRows > 0, "codes are read from the ring");
-    constexpr int kAhead = Ring<T, FMT, WPR, WIDE>::kRows;
+    constexpr bool kTwice = kThreads > 256 && kThreads != 512;  // too few registers to hold (x - mean) * rstd for a row's output
+    static_assert(!KEPT || Ring<T, KEPT, WPR, WIDE>::kRows > 0, "codes are read from the ring");
+    constexpr int kAhead = Ring<T, KEPT, WPR, WIDE>::kRows;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float red[2][S::kWarps * 2];
     const int warp = threadIdx.x / 32;
@@ -340,7 +353,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     const unsigned ring_x = ring_gy + kAhead * kGyRow;
     const unsigned ring_codes = (unsigned)__cvta_generic_to_shared(ring) + kAhead * kGyRow + threadIdx.x * 16;
     constexpr int kSmall = kSmallPiece<T, WIDE>;
-    const unsigned ring_small = (unsigned)__cvta_generic_to_shared(ring) + kAhead * (kRowBytes<T, FMT, WPR, WIDE> - S::kWarps * kSmall) + warp * kSmall;
+    const unsigned ring_small = (unsigned)__cvta_generic_to_shared(ring) + kAhead * (kRowBytes<T, KEPT, WPR, WIDE> - S::kWarps * kSmall) + warp * kSmall;
     const int groups = (a.cols + kGroup - 1) / kGroup;
     float2 sum_w[V][E / 2], sum_b[V][E / 2];
 #pragma unroll
@@ -350,13 +363,13 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     const float inv_cols = 1.0f / (float)a.cols;
     const long long stride = (long long)gridDim.x * S::kGroups;
     // Rows on 16-byte boundaries: where this lane copies from next, and how much.
-    const bool straight = a.aligned_gy && (kKept ? a.aligned_scales : a.aligned_x);
+    const bool straight = a.aligned_gy && (KEPT ? a.aligned_scales : a.aligned_x);
     constexpr int kPer = 16 / (int)sizeof(T);
     const long long copy_first = (long long)blockIdx.x * S::kGroups + group;
     const T* from_gy = static_cast<const T*>(a.gy) + copy_first * a.ld_gy + (t - (int)lane) * E + (int)lane * kPer;
-    const T* from_x = kKept ? nullptr : static_cast<const T*>(a.x) + copy_first * a.ld_x + (t - (int)lane) * E + (int)lane * kPer;
-    const unsigned char* from_codes = kKept ? a.codes + copy_first * a.ld_codes + t * E : nullptr;
-    const unsigned char* from_scales = kKept ? a.scales + copy_first * a.ld_scales + (t - (int)lane) * E / kGroup + 4 * lane : nullptr;
+    const T* from_x = KEPT ? nullptr : static_cast<const T*>(a.x) + copy_first * a.ld_x + (t - (int)lane) * E + (int)lane * kPer;
+    const unsigned char* from_codes = KEPT ? a.codes + copy_first * a.ld_codes + t * E : nullptr;
+    const unsigned char* from_scales = KEPT ? a.scales + copy_first * a.ld_scales + (t - (int)lane) * E / kGroup + 4 * lane : nullptr;
     const float* from_stats = (lane ? a.rstd : a.mean) + copy_first;
     auto copy_straight = [&](long long row, int slot) {
         if (row < a.rows) {
@@ -370,10 +383,10 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                     const int bytes = min(16, (a.cols - at) * (int)sizeof(T));
                     if (bytes > 0) {
                         copy16(ring_gy + piece + 16 * (32 * k + lane), from_gy + j * kStep + 32 * k * kPer, bytes);
-                        if (!kKept) copy16(ring_x + piece + 16 * (32 * k + lane), from_x + j * kStep + 32 * k * kPer, bytes);
+                        if (!KEPT) copy16(ring_x + piece + 16 * (32 * k + lane), from_x + j * kStep + 32 * k * kPer, bytes);
                     }
                 }
-                if (kKept) {
+                if (KEPT) {
                     const int c0 = (j * 32 * WPR + t) * E;
                     if (c0 < a.cols) {
                         if (E == 16)
@@ -389,8 +402,8 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         from_gy += stride * a.ld_gy;
-        if (!kKept) from_x += stride * a.ld_x;
-        if (kKept) {
+        if (!KEPT) from_x += stride * a.ld_x;
+        if (KEPT) {
             from_codes += stride * a.ld_codes;
             from_scales += stride * a.ld_scales;
         }
@@ -403,9 +416,9 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 const int at = (j * 32 * WPR + t - (int)lane) * E, c0 = at + (int)lane * E;
                 const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
                 copy_piece(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, a.rows, a.cols, row, at, a.aligned_gy, lane);
-                if (!kKept) copy_piece(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, a.rows, a.cols, row, at, a.aligned_x, lane);
-                if (kKept) copy_scales(ring_small + (unsigned)(slot * S::kWarps * kSmall + 16 + 32 * j), a.scales, a.ld_scales, a.rows, groups, row, at / kGroup, E, lane);
-                if (kKept && c0 < a.cols) {
+                if (!KEPT) copy_piece(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, a.rows, a.cols, row, at, a.aligned_x, lane);
+                if (KEPT) copy_scales(ring_small + (unsigned)(slot * S::kWarps * kSmall + 16 + 32 * j), a.scales, a.ld_scales, a.rows, groups, row, at / kGroup, E, lane);
+                if (KEPT && c0 < a.cols) {
                     const unsigned char* p = a.codes + row * a.ld_codes + c0;
                     if (E == 16)
                         copy16(ring_codes + (unsigned)((slot * WIDE + j) * kThreads * 16), p, 16);
@@ -454,7 +467,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 const unsigned small = ring_small + (unsigned)(slot * S::kWarps * kSmall);
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rstd) : "r"(small + 4) : "memory");
                 if (LAYER) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(mean) : "r"(small) : "memory");
-                if (kKept) {
+                if (KEPT) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const unsigned from = straight ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3);
@@ -468,59 +481,66 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 if (LAYER) mean = __ldg(a.mean + row);
             }
         }
-        K h[V], g[V];
+        K g[V], h[kTwice ? 1 : V];                 // gy * weight; (x - mean) * rstd, or
+        unsigned xr[V][KEPT ? E / 4 : 8];          // the codes or words of x to form it again
+        // the scale of a kept x joins the subtraction
+        auto normalized = [&](int j) {
+            K k;
+            if constexpr (KEPT) {
+                if (a.e4m3)
+                    k.template decode<AMPQ_FMT_E4M3>(xr[j]);
+                else
+                    k.template decode<AMPQ_FMT_E5M2>(xr[j]);
+            } else {
+                k.from_words(xr[j]);
+            }
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                float2 d = k.v[i];
+                if (KEPT && LAYER) d = __ffma2_rn(d, make_float2(p[j], p[j]), make_float2(-mean, -mean));
+                if (KEPT && !LAYER) d = __fmul2_rn(d, make_float2(p[j], p[j]));
+                if (!KEPT && LAYER) d = __fadd2_rn(d, make_float2(-mean, -mean));
+                k.v[i] = __fmul2_rn(d, make_float2(rstd, rstd));
+            }
+            return k;
+        };
         float2 c2 = make_float2(0.0f, 0.0f), c1 = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int c0 = (j * 32 * WPR + t) * E;
             const int n = live ? min(E, a.cols - c0) : 0;
-            unsigned w8[8], x8[8];
-            if (kAhead > 0) {
+            unsigned w8[8];
+            if constexpr (kAhead > 0) {
                 const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
                 take_chunk(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, row, c0, a.aligned_gy, lane, n, w8);
-                if (!kKept) take_chunk(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, row, c0, a.aligned_x, lane, n, x8);
+                if constexpr (!KEPT) take_chunk(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, row, c0, a.aligned_x, lane, n, xr[j]);
             } else if (n > 0) {
                 K::load_words(static_cast<const T*>(a.gy) + row * a.ld_gy + c0, n, w8);
-                if (!kKept) K::load_words(static_cast<const T*>(a.x) + row * a.ld_x + c0, n, x8);
+                if constexpr (!KEPT) K::load_words(static_cast<const T*>(a.x) + row * a.ld_x + c0, n, xr[j]);
             }
-            h[j].zero();
-            g[j].zero();
             if (n <= 0) continue;
-            g[j].from_words(w8);
-            if (kKept) {
-                constexpr int F = kKept ? FMT : AMPQ_FMT_E4M3;
+            if constexpr (KEPT) {
                 const uint4 q = take16(ring_codes + (unsigned)((slot * WIDE + j * E / 16) * kThreads * 16));
-                unsigned c[E / 4];
                 if (E == 16) {
-                    c[0] = q.x; c[1] = q.y; c[2 % (E / 4)] = q.z; c[3 % (E / 4)] = q.w;
+                    xr[j][0] = q.x; xr[j][1] = q.y; xr[j][2 % (E / 4)] = q.z; xr[j][3 % (E / 4)] = q.w;
                 } else {
-                    c[0] = j & 1 ? q.z : q.x;
-                    c[1] = j & 1 ? q.w : q.y;
+                    xr[j][0] = j & 1 ? q.z : q.x;
+                    xr[j][1] = j & 1 ? q.w : q.y;
                 }
-                h[j].template decode<F>(c);
-            } else {
-                h[j].from_words(x8);
             }
-            // (x - mean) * rstd; the scale of a kept x joins the subtraction
+            g[j].from_words(w8);
+            const K k = normalized(j);  // behind the last column gy is 0, and this finite unless the row's sums are not
+            if constexpr (!kTwice) h[j] = k;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                float2 d = h[j].v[i];
-                if (kKept && LAYER) d = __ffma2_rn(d, make_float2(p[j], p[j]), make_float2(-mean, -mean));
-                if (kKept && !LAYER) d = __fmul2_rn(d, make_float2(p[j], p[j]));
-                if (!kKept && LAYER) d = __fadd2_rn(d, make_float2(-mean, -mean));
-                h[j].v[i] = __fmul2_rn(d, make_float2(rstd, rstd));
-            }
-            // behind the last column gy is 0, and h finite unless the row's sums are not
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                sum_w[j][i] = __ffma2_rn(g[j].v[i], h[j].v[i], sum_w[j][i]);
+                sum_w[j][i] = __ffma2_rn(g[j].v[i], k.v[i], sum_w[j][i]);
                 if (LAYER) sum_b[j][i] = __fadd2_rn(sum_b[j][i], g[j].v[i]);
             }
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) g[j].v[i] = __fmul2_rn(g[j].v[i], weight[j].v[i]);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                c2 = __ffma2_rn(g[j].v[i], h[j].v[i], c2);
+                c2 = __ffma2_rn(g[j].v[i], k.v[i], c2);
                 if (LAYER) c1 = __fadd2_rn(c1, g[j].v[i]);
             }
         }
@@ -539,9 +559,14 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
             const int c0 = (j * 32 * WPR + t) * E;
             const int n = live ? min(E, a.cols - c0) : 0;
             if (n <= 0) continue;
+            K k;
+            if constexpr (kTwice)
+                k = normalized(j);
+            else
+                k = h[j];
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                float2 o = __ffma2_rn(h[j].v[i], make_float2(m2, m2), g[j].v[i]);
+                float2 o = __ffma2_rn(k.v[i], make_float2(m2, m2), g[j].v[i]);
                 if (LAYER) o = __fadd2_rn(o, make_float2(m1, m1));
                 g[j].v[i] = __fmul2_rn(o, make_float2(rstd, rstd));
             }
@@ -584,80 +609,79 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
 
 // Warps of a row, a power of two: 512 columns each, 1024 above 4096 columns.
 int warps_per_row(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 8192 ? 8 : 16; }
-// of the backward pass
-int backward_warps(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 8192 ? 16 : 32; }
+// of the backward pass: 512 columns each, and ten warps up to 5120
+int backward_warps(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 5120 ? 10 : cols <= 8192 ? 16 : 32; }
 
 // CTAs of the backward pass: every row group gets a row before one gets two, and
 // no more CTAs than are resident, so that the sums stay in registers.
 int backward_ctas(long long rows, int cols, int sms) {
     const int wpr = backward_warps(cols), groups = wpr < 8 ? 8 / wpr : 1;
     const long long need = (rows + groups - 1) / groups;
-    const long long most = (long long)sms * (wpr <= 8 ? 2 : 1);
+    const long long most = (long long)sms * (wpr <= 10 ? 2 : 1);
     return (int)(need < most ? need : most);
 }
 
-template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 int start_forward(const ForwardArgs& a, cudaStream_t st) {
     using S = Shape<WPR, WIDE>;
     const long long blocks = (a.rows + S::kGroups - 1) / S::kGroups;
-    norm_forward_kernel<T, FMT, LAYER, WPR, WIDE><<<(unsigned)blocks, S::kThreads, 0, st>>>(a);
+    norm_forward_kernel<T, KEPT, LAYER, WPR, WIDE><<<(unsigned)blocks, S::kThreads, 0, st>>>(a);
     return launched();
 }
 
-template <typename T, int FMT, bool LAYER>
+template <typename T, bool KEPT, bool LAYER>
 int launch_forward(const ForwardArgs& a, cudaStream_t st) {
-    if (a.cols > 4096) return a.cols <= 8192 ? start_forward<T, FMT, LAYER, 8, 2>(a, st) : start_forward<T, FMT, LAYER, 16, 2>(a, st);
+    if (a.cols > 4096) return a.cols <= 8192 ? start_forward<T, KEPT, LAYER, 8, 2>(a, st) : start_forward<T, KEPT, LAYER, 16, 2>(a, st);
     switch (warps_per_row(a.cols)) {
-        case 1: return start_forward<T, FMT, LAYER, 1, 1>(a, st);
-        case 2: return start_forward<T, FMT, LAYER, 2, 1>(a, st);
-        case 4: return start_forward<T, FMT, LAYER, 4, 1>(a, st);
-        default: return start_forward<T, FMT, LAYER, 8, 1>(a, st);
+        case 1: return start_forward<T, KEPT, LAYER, 1, 1>(a, st);
+        case 2: return start_forward<T, KEPT, LAYER, 2, 1>(a, st);
+        case 4: return start_forward<T, KEPT, LAYER, 4, 1>(a, st);
+        default: return start_forward<T, KEPT, LAYER, 8, 1>(a, st);
     }
 }
 
 constexpr int kMaxDevices = 64;
 
-template <typename T, int FMT, bool LAYER, int WPR, int WIDE>
+template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 int start_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
     static std::atomic<bool> prepared[kMaxDevices];  // the kernel may use its shared memory on that device
     using S = Shape<WPR, WIDE>;
     constexpr int kJoin = S::kGroups > 1 ? S::kGroups * 512 * WPR * WIDE * 4 : 0;
-    constexpr int kBytes = Ring<T, FMT, WPR, WIDE>::kBytes > kJoin ? Ring<T, FMT, WPR, WIDE>::kBytes : kJoin;
+    constexpr int kBytes = Ring<T, KEPT, WPR, WIDE>::kBytes > kJoin ? Ring<T, KEPT, WPR, WIDE>::kBytes : kJoin;
     if (kBytes > 32 * 1024 && (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire))) {
-        if (cudaFuncSetAttribute(norm_backward_kernel<T, FMT, LAYER, WPR, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+        if (cudaFuncSetAttribute(norm_backward_kernel<T, KEPT, LAYER, WPR, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
             cudaGetLastError();
             return AMPQ_ERR_CUDA;
         }
         if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
     }
-    norm_backward_kernel<T, FMT, LAYER, WPR, WIDE><<<(unsigned)ctas, S::kThreads, kBytes, st>>>(a);
+    norm_backward_kernel<T, KEPT, LAYER, WPR, WIDE><<<(unsigned)ctas, S::kThreads, kBytes, st>>>(a);
     return launched();
 }
 
-template <typename T, int FMT, bool LAYER>
+template <typename T, bool KEPT, bool LAYER>
 int launch_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
     switch (backward_warps(a.cols)) {
-        case 1: return start_backward<T, FMT, LAYER, 1, 1>(a, device, ctas, st);
-        case 2: return start_backward<T, FMT, LAYER, 2, 1>(a, device, ctas, st);
-        case 4: return start_backward<T, FMT, LAYER, 4, 1>(a, device, ctas, st);
-        case 8: return start_backward<T, FMT, LAYER, 8, 1>(a, device, ctas, st);
-        case 16: return start_backward<T, FMT, LAYER, 16, 1>(a, device, ctas, st);
-        default: return start_backward<T, FMT, LAYER, 32, 1>(a, device, ctas, st);
+        case 1: return start_backward<T, KEPT, LAYER, 1, 1>(a, device, ctas, st);
+        case 2: return start_backward<T, KEPT, LAYER, 2, 1>(a, device, ctas, st);
+        case 4: return start_backward<T, KEPT, LAYER, 4, 1>(a, device, ctas, st);
+        case 8: return start_backward<T, KEPT, LAYER, 8, 1>(a, device, ctas, st);
+        case 10: return start_backward<T, KEPT, LAYER, 10, 1>(a, device, ctas, st);
+        case 16: return start_backward<T, KEPT, LAYER, 16, 1>(a, device, ctas, st);
+        default: return start_backward<T, KEPT, LAYER, 32, 1>(a, device, ctas, st);
     }
 }
 
-template <typename T, bool LAYER>
-int dispatch_forward(int fmt, const ForwardArgs& a, cudaStream_t st) {
-    if (fmt == AMPQ_FMT_E4M3) return launch_forward<T, AMPQ_FMT_E4M3, LAYER>(a, st);
-    if (fmt == AMPQ_FMT_E5M2) return launch_forward<T, AMPQ_FMT_E5M2, LAYER>(a, st);
-    return launch_forward<T, AMPQ_FMT_BASE, LAYER>(a, st);
+template <typename T>
+int dispatch_forward(bool kept, bool layer, const ForwardArgs& a, cudaStream_t st) {
+    if (kept) return layer ? launch_forward<T, true, true>(a, st) : launch_forward<T, true, false>(a, st);
+    return layer ? launch_forward<T, false, true>(a, st) : launch_forward<T, false, false>(a, st);
 }
 
-template <typename T, bool LAYER>
-int dispatch_backward(int fmt, const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
-    if (fmt == AMPQ_FMT_E4M3) return launch_backward<T, AMPQ_FMT_E4M3, LAYER>(a, device, ctas, st);
-    if (fmt == AMPQ_FMT_E5M2) return launch_backward<T, AMPQ_FMT_E5M2, LAYER>(a, device, ctas, st);
-    return launch_backward<T, AMPQ_FMT_BASE, LAYER>(a, device, ctas, st);
+template <typename T>
+int dispatch_backward(bool kept, bool layer, const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
+    if (kept) return layer ? launch_backward<T, true, true>(a, device, ctas, st) : launch_backward<T, true, false>(a, device, ctas, st);
+    return layer ? launch_backward<T, false, true>(a, device, ctas, st) : launch_backward<T, false, false>(a, device, ctas, st);
 }
 
 int check_norm(int kind, int dtype, int param_dtype, int fmt, long long cols) {
@@ -700,11 +724,12 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     a.rows = rows; a.ld_x = ld_x; a.ld_y = ld_y; a.ld_codes = ld_codes; a.ld_scales = ld_scales;
     a.cols = (int)cols;
     a.eps = eps;
+    a.e4m3 = fmt == AMPQ_FMT_E4M3;
     a.whole = cols % (dtype == AMPQ_F32 ? 8 : 16) == 0;
     a.param_bf16 = param_dtype == AMPQ_BF16;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    if (dtype == AMPQ_F32) return layer ? dispatch_forward<float, true>(fmt, a, st) : dispatch_forward<float, false>(fmt, a, st);
-    return layer ? dispatch_forward<__nv_bfloat16, true>(fmt, a, st) : dispatch_forward<__nv_bfloat16, false>(fmt, a, st);
+    const bool kept = fmt != AMPQ_FMT_BASE;
+    return dtype == AMPQ_F32 ? dispatch_forward<float>(kept, layer, a, st) : dispatch_forward<__nv_bfloat16>(kept, layer, a, st);
 }
 
 int ampq_norm_backward_workspace(int device, long long rows, long long cols, long long* bytes) {
@@ -753,13 +778,12 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.cols = (int)cols;
         a.param_bf16 = param_dtype == AMPQ_BF16;
         a.sum_b = gbias != nullptr;
+        a.e4m3 = fmt == AMPQ_FMT_E4M3;
         a.aligned_gy = rows_aligned(gy, ld_gy, dtype);
         a.aligned_x = rows_aligned(x, ld_x, dtype);
         a.aligned_scales = aligned_to(scales, 4) && ld_scales % 4 == 0 && ((cols + kGroup - 1) / kGroup) % 4 == 0;
-        if (dtype == AMPQ_F32)
-            rc = layer ? dispatch_backward<float, true>(fmt, a, device, ctas, st) : dispatch_backward<float, false>(fmt, a, device, ctas, st);
-        else
-            rc = layer ? dispatch_backward<__nv_bfloat16, true>(fmt, a, device, ctas, st) : dispatch_backward<__nv_bfloat16, false>(fmt, a, device, ctas, st);
+        const bool kept = fmt != AMPQ_FMT_BASE;
+        rc = dtype == AMPQ_F32 ? dispatch_backward<float>(kept, layer, a, device, ctas, st) : dispatch_backward<__nv_bfloat16>(kept, layer, a, device, ctas, st);
         if (rc) return rc;
     }
     if (!sums) return AMPQ_OK;

@@ -35,14 +35,12 @@ constexpr int kStages = 6;
 constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kStoreWarp = 4;
 constexpr int kPatch = 32 * 33;               // floats: a 32 x 32 patch of the output on its way out
 
-// Storing warps: four cover the 128 TMEM lanes once; with fp32 planes eight share
-// the columns, so that the running sums fit their registers.
-template <int PLANES>
-struct Roles {
-    static constexpr int kStoreWarps = PLANES == 1 ? 4 : 8;
-    static constexpr int kThreads = 32 * (kStoreWarp + kStoreWarps);
-    static constexpr int kSmemBytes = kStages * 2 * kTileBytes + kStoreWarps * kPatch * 4 + 1024;
-};
+// Four storing warps cover the 128 TMEM lanes, eight share the columns too: the
+// running sums of fp32 gradients fit their registers, and rows off the 16-byte
+// boundaries, which go out two bytes a lane, take half the time.
+constexpr int kStoreWarps = 8;
+constexpr int kThreads = 32 * (kStoreWarp + kStoreWarps);
+constexpr int kSmemBytes = kStages * 2 * kTileBytes + kStoreWarps * kPatch * 4 + 1024;
 
 // Polls of an mbarrier before a wait gives up.  A test build lets the waits
 // between the stages give up at once; the wait that drains products in flight
@@ -291,14 +289,13 @@ __device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned
 // the copies and products in flight are waited for, and what was not stored yet
 // becomes NaN.
 template <int CG, int PLANES, typename OUT>
-__global__ void __launch_bounds__(Roles<PLANES>::kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap g_map, const __grid_constant__ CUtensorMap x_map, const ProductArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap g_map, const __grid_constant__ CUtensorMap x_map, const ProductArgs a) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ alignas(8) unsigned long long s_bars[2 * kStages + 5];
     __shared__ unsigned s_tmem;
     __shared__ int s_gave_up;
     constexpr int kSide = CG * kCtaSide;  // of the tile
     constexpr unsigned kTmemCols = 2 * kSide;
-    constexpr int kStoreWarps = Roles<PLANES>::kStoreWarps;
     const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     unsigned rank = 0;
     if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -564,28 +561,83 @@ __device__ __forceinline__ void cut3(float g, unsigned short (&h)[3]) {
     h[2] = (unsigned short)(__float_as_uint(r2) >> 16);
 }
 
-// Copies gY into rows of `pitch` (a multiple of 8) bf16, one plane for bf16, three
-// for fp32: for gradients that TMA cannot read as they lie.  One pair of columns
-// per thread.
-template <typename T>
-__global__ void __launch_bounds__(256) lay_out_kernel(const T* __restrict__ g, long long ld, long long rows, long long cols, unsigned* __restrict__ out,
-                                                      long long pitch) {
-    const long long pair = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (2 * pair >= cols) return;
-    const bool two = 2 * pair + 1 < cols;
-    for (long long n = blockIdx.y; n < rows; n += gridDim.y) {
-        const T* p = g + n * ld + 2 * pair;
-        const long long at = (n * pitch) / 2 + pair;
-        if (sizeof(T) == 2) {
-            const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
-            out[at] = __ldg(q) | (two ? (unsigned)__ldg(q + 1) << 16 : 0u);
-        } else {
-            unsigned short lo[3], hi[3];
-            cut3(load_elem(p), lo);
-            cut3(two ? load_elem(p + 1) : 0.0f, hi);
+// One read of gY: the sums of its columns per sample (`sums`, may be null), and
+// with COPY its bf16 planes in rows of `pitch` elements, for gradients that TMA
+// cannot read as they lie (fp32, or rows off the 16-byte boundaries).  A block
+// takes eight chunks of columns, 32 rows at a time; the eight blocks of a cluster
+// share a sample's rows and add their sums up through each other's shared memory,
+// in order, so no second launch is needed.
+constexpr int kSweepChunks = 8, kSweepWays = 32, kSweepParts = 8;
+
+template <typename T, bool COPY>
+__global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChunks * kSweepWays)
+    sweep_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols, unsigned short* __restrict__ out, long long pitch,
+                 T* __restrict__ sums) {
+    using K = Chunk<T>;
+    constexpr int E = K::kElems, kCols = kSweepChunks * E;
+    __shared__ float part[kSweepWays][kCols + 1];
+    __shared__ float total[kCols];
+    const int cx = threadIdx.x % kSweepChunks, way = threadIdx.x / kSweepChunks;
+    const long long c = (long long)blockIdx.x * kCols + cx * E;
+    const int n_cols = (int)max(0LL, min((long long)E, cols - c));
+    for (long long r = blockIdx.z; r < samples; r += gridDim.z) {
+        float2 sum[E / 2];
 #pragma unroll
-            for (int k = 0; k < 3; ++k) out[at + k * (rows * pitch / 2)] = lo[k] | (unsigned)hi[k] << 16;
+        for (int i = 0; i < E / 2; ++i) sum[i] = make_float2(0.0f, 0.0f);
+        if (n_cols > 0) {
+#pragma unroll 4
+            for (long long n = blockIdx.y * kSweepWays + way; n < rows; n += kSweepParts * kSweepWays) {
+                const long long row = r * rows + n;
+                unsigned w[8];
+                K::load_words(g + row * ld + c, n_cols, w);
+                K k;
+                k.from_words(w);
+                if (COPY && sizeof(T) == 2) {
+                    uint4* to = reinterpret_cast<uint4*>(out + row * pitch + c);
+                    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (n_cols > 8) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+                if (COPY && sizeof(T) == 4) {
+                    unsigned short h[8][3];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) cut3(__uint_as_float(w[i]), h[i]);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+                        *reinterpret_cast<uint4*>(out + ((long long)p * samples * rows + row) * pitch + c) =
+                            make_uint4(h[0][p] | (unsigned)h[1][p] << 16, h[2][p] | (unsigned)h[3][p] << 16, h[4][p] | (unsigned)h[5][p] << 16,
+                                       h[6][p] | (unsigned)h[7][p] << 16);
+                }
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) sum[i] = __fadd2_rn(sum[i], k.v[i]);
+            }
         }
+        if (!sums) continue;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            part[way][cx * E + 2 * i] = sum[i].x;
+            part[way][cx * E + 2 * i + 1] = sum[i].y;
+        }
+        __syncthreads();
+        if (threadIdx.x < kCols) {
+            float t = 0.0f;
+#pragma unroll 8
+            for (int k = 0; k < kSweepWays; ++k) t += part[k][threadIdx.x];
+            total[threadIdx.x] = t;
+        }
+        asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+        const long long col = (long long)blockIdx.x * kCols + threadIdx.x;
+        if (blockIdx.y == 0 && threadIdx.x < kCols && col < cols) {
+            float t = 0.0f;
+#pragma unroll
+            for (unsigned k = 0; k < kSweepParts; ++k) {
+                float v;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(smem_u32(&total[threadIdx.x]), k)) : "memory");
+                t += v;
+            }
+            store_elem(sums + r * cols + col, t);
+        }
+        // the sums of every block have been read before they change or the block ends
+        asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
     }
 }
 
@@ -601,53 +653,6 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* __restric
     }
 }
 
-// Column sums of gY, in parts: block (x, y, r) sums every gridDim.y-th run of
-// kSumRows rows of sample r for 256 columns.  Eight columns a thread; `part` has
-// one row per part, or `out` takes the sums if there is one part.
-constexpr int kSumCols = 256, kSumWays = 8, kSumRows = 64;
-
-template <typename T>
-__global__ void __launch_bounds__(256) column_sums_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols,
-                                                          float* __restrict__ part, T* __restrict__ out, bool vec) {
-    __shared__ float sums[kSumWays][kSumCols];
-    const int cx = threadIdx.x % 32 * 8, way = threadIdx.x / 32;
-    const long long c = (long long)blockIdx.x * kSumCols + cx;
-    const int n_cols = (int)max(0LL, min(8LL, cols - c));
-    for (long long r = blockIdx.z; r < samples; r += gridDim.z) {
-        float s[8] = {};
-        if (n_cols > 0)
-            for (long long run = (long long)blockIdx.y * kSumRows; run < rows; run += (long long)gridDim.y * kSumRows) {
-                const long long last = min(rows, run + kSumRows);
-#pragma unroll 4
-                for (long long n = run + way; n < last; n += kSumWays) {
-                    Raw8<T> raw;
-                    if (vec)
-                        load8<true>(raw, g + (r * rows + n) * ld + c, n_cols);
-                    else
-                        load8<false>(raw, g + (r * rows + n) * ld + c, n_cols);
-                    float v[8];
-                    raw.values(v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i] += v[i];
-                }
-            }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sums[way][cx + i] = s[i];
-        __syncthreads();
-        const long long col = (long long)blockIdx.x * kSumCols + threadIdx.x;
-        if (col < cols) {
-            float t = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kSumWays; ++k) t += sums[k][threadIdx.x];
-            if (gridDim.y > 1)
-                part[(r * gridDim.y + blockIdx.y) * cols + col] = t;
-            else
-                store_elem(out + r * cols + col, t);
-        }
-    }
-}
-
 // ---------------------------------------------------------------------------
 // host side
 
@@ -655,19 +660,17 @@ struct Problem {
     int dtype;
     const void* gy;
     long long ld_gy, samples, rows, cols, outs;
-    bool bias;
 };
 
 // How a product is run, and what its workspace holds: the copied gradient, X^ in
-// bf16, the partial products, the partial column sums, each at a multiple of 256
-// bytes.
+// bf16, the partial products, each at a multiple of 256 bytes.
 struct Plan {
     bool small, copy, pair;
-    int planes, splits, sum_parts;
+    int planes, splits;
     long long pitch, x_pitch;
     int k_tiles, c_tiles, steps, steps_per_split;
     long long tiles;
-    long long at_x, at_part, at_sums, bytes;
+    long long at_x, at_part, bytes;
 };
 
 // Products of at most this many tokens, and of no more 64 x 64 tiles than four per
@@ -700,19 +703,12 @@ Plan make_plan(const Problem& q, int sms) {
     p.steps_per_split = p.steps > 0 ? (int)((p.steps + splits - 1) / splits) : 1;
     p.splits = p.steps > 0 ? (p.steps + p.steps_per_split - 1) / p.steps_per_split : 1;
     p.tiles = tiles * p.splits;
-    // about four blocks of column sums per SM
-    const long long sum_blocks = (q.outs + kSumCols - 1) / kSumCols * (q.samples > 0 ? q.samples : 1), runs = (q.rows + kSumRows - 1) / kSumRows;
-    long long parts = sum_blocks > 0 ? 4LL * sms / sum_blocks : 1;
-    if (parts > runs) parts = runs;
-    p.sum_parts = (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
     long long at = 0;
     if (p.copy) at = round_up(2LL * p.planes * q.samples * q.rows * p.pitch, 256);
     p.at_x = at;
     at += round_up(2LL * q.samples * q.rows * p.x_pitch, 256);
     p.at_part = at;
     if (p.splits > 1) at += round_up(4LL * q.samples * p.splits * q.outs * q.cols, 256);
-    p.at_sums = at;
-    if (q.bias && p.sum_parts > 1) at += round_up(4LL * q.samples * p.sum_parts * q.outs, 256);
     p.bytes = at;
     return p;
 }
@@ -793,7 +789,7 @@ int launch_persistent(ProductKernel kernel, std::atomic<bool>* prepared, int cg,
 template <int CG, int PLANES, typename OUT>
 int launch_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, int device, int sms, cudaStream_t st) {
     static std::atomic<bool> prepared[kMaxDevices];
-    return launch_persistent(product_kernel<CG, PLANES, OUT>, prepared, CG, Roles<PLANES>::kThreads, Roles<PLANES>::kSmemBytes, g_map, x_map, a, device, sms, st);
+    return launch_persistent(product_kernel<CG, PLANES, OUT>, prepared, CG, kThreads, kSmemBytes, g_map, x_map, a, device, sms, st);
 }
 
 template <int PLANES, typename OUT>
@@ -818,14 +814,24 @@ int run_small(const Problem& q, const Operands& o, cudaStream_t st) {
 }
 
 template <typename T>
+int sweep(const Problem& q, const Operands& o, bool copy, long long pitch, cudaStream_t st) {
+    if (!copy && !o.gb) return AMPQ_OK;
+    constexpr int kCols = kSweepChunks * Chunk<T>::kElems;
+    const dim3 grid((unsigned)((q.outs + kCols - 1) / kCols), kSweepParts, (unsigned)(q.samples < 65535 ? q.samples : 65535));
+    const T* gy = static_cast<const T*>(q.gy);
+    if (copy)
+        sweep_kernel<T, true><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, reinterpret_cast<unsigned short*>(o.ws), pitch,
+                                                                          static_cast<T*>(o.gb));
+    else
+        sweep_kernel<T, false><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, nullptr, 0, static_cast<T*>(o.gb));
+    return launched();
+}
+
+template <typename T>
 int run_large(const Problem& q, const Plan& p, const Operands& o, int device, int sms, cudaStream_t st) {
     const long long rows = q.samples * q.rows;
     int rc;
-    if (p.copy) {
-        const unsigned by = (unsigned)(rows < 65535 ? rows : 65535);
-        lay_out_kernel<T><<<dim3((unsigned)((q.outs + 511) / 512), by), 256, 0, st>>>(static_cast<const T*>(q.gy), q.ld_gy, rows, q.outs, reinterpret_cast<unsigned*>(o.ws), p.pitch);
-        if ((rc = launched())) return rc;
-    }
+    if ((rc = sweep<T>(q, o, p.copy, p.pitch, st))) return rc;
     if ((rc = launch_ckpt_unpack(AMPQ_BF16, o.fmt, o.codes, o.ld_codes, o.scales, o.ld_scales, rows, q.cols, o.ws + p.at_x, p.x_pitch, st))) return rc;
     CUtensorMap g_map, x_map;
     if ((rc = operand_map(&g_map, p.copy ? o.ws : q.gy, p.pitch, q.outs, q, p.planes))) return rc;
@@ -852,21 +858,10 @@ int run_large(const Problem& q, const Plan& p, const Operands& o, int device, in
 }
 
 template <typename T>
-int bias_grad(const Problem& q, const Plan& p, const Operands& o, cudaStream_t st) {
-    float* part = reinterpret_cast<float*>(o.ws + p.at_sums);
-    const unsigned bz = (unsigned)(q.samples < 65535 ? q.samples : 65535);
-    column_sums_kernel<T><<<dim3((unsigned)((q.outs + kSumCols - 1) / kSumCols), p.sum_parts, bz), 256, 0, st>>>(
-        static_cast<const T*>(q.gy), q.ld_gy, q.samples, q.rows, q.outs, part, static_cast<T*>(o.gb), rows_aligned(q.gy, q.ld_gy, q.dtype));
-    const int rc = launched();
-    return rc || p.sum_parts == 1 ? rc : launch_join_columns(part, q.samples, p.sum_parts, q.outs, o.gb, nullptr, q.dtype, st);
-}
-
-template <typename T>
 int run(const Problem& q, const Plan& p, const Operands& o, int device, int sms, cudaStream_t st) {
     if (q.rows > 0 && q.cols > 0) {
         if (p.small) return o.fmt == AMPQ_FMT_E4M3 ? run_small<T, AMPQ_FMT_E4M3>(q, o, st) : run_small<T, AMPQ_FMT_E5M2>(q, o, st);
-        const int rc = run_large<T>(q, p, o, device, sms, st);
-        return rc || !o.gb ? rc : bias_grad<T>(q, p, o, st);
+        return run_large<T>(q, p, o, device, sms, st);
     }
     // no product: zeros, or no columns at all
     bool ok = true;
@@ -878,10 +873,7 @@ int run(const Problem& q, const Plan& p, const Operands& o, int device, int sms,
         cudaGetLastError();
         return AMPQ_ERR_CUDA;
     }
-    if (q.rows == 0 || !o.gb) return AMPQ_OK;
-    Plan one = p;
-    one.sum_parts = 1;
-    return bias_grad<T>(q, one, o, st);
+    return q.rows == 0 ? AMPQ_OK : sweep<T>(q, o, false, 0, st);
 }
 
 int check_sizes(int dtype, long long samples, long long rows, long long cols, long long outs) {
@@ -901,7 +893,7 @@ extern "C" {
 #pragma GCC visibility push(default)
 
 int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void* gy, long long ld_gy, long long samples, long long rows, long long cols,
-                                    long long outs, int bias, long long* bytes) {
+                                    long long outs, long long* bytes) {
     if (!bytes) return AMPQ_ERR_INVALID;
     const int rc = check_sizes(dtype, samples, rows, cols, outs);
     if (rc) return rc;
@@ -909,7 +901,7 @@ int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void* gy, long 
     if (cur.status) return cur.status;
     const int sms = sm_count(device);
     if (sms < 2) return AMPQ_ERR_CUDA;
-    *bytes = rows > 0 && cols > 0 ? make_plan(Problem{dtype, gy, ld_gy, samples, rows, cols, outs, bias != 0}, sms).bytes : 0;
+    *bytes = rows > 0 && cols > 0 ? make_plan(Problem{dtype, gy, ld_gy, samples, rows, cols, outs}, sms).bytes : 0;
     return AMPQ_OK;
 }
 
@@ -928,8 +920,8 @@ int ampq_ckpt_weight_grad(int device, void* cuda_stream, int dtype, int fmt, con
     if (samples == 0 || outs == 0) return AMPQ_OK;
     const int sms = sm_count(device);
     if (sms < 2) return AMPQ_ERR_CUDA;
-    const Problem q{dtype, gy, ld_gy, samples, rows, cols, outs, gb != nullptr};
-    Plan p = make_plan(q, sms);
+    const Problem q{dtype, gy, ld_gy, samples, rows, cols, outs};
+    const Plan p = make_plan(q, sms);
     if (rows > 0 && cols > 0 && p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return AMPQ_ERR_INVALID;
     const Operands o{codes, scales, ld_codes, ld_scales, fmt, gw, gb, static_cast<unsigned char*>(workspace)};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

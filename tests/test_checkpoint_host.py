@@ -69,9 +69,9 @@ def test_workspace_queries_refuse(ampq):
     assert L.ampq_norm_backward_workspace(0, 4, 4, None) == ampq.ERR_INVALID
     assert L.ampq_norm_backward_workspace(0, -1, 4, C.byref(n)) == ampq.ERR_INVALID
     assert L.ampq_norm_backward_workspace(0, 4, 16385, C.byref(n)) == ampq.ERR_TOO_LARGE
-    assert L.ampq_ckpt_weight_grad_workspace(0, 0, None, 4, 1, 1, 4, 4, 1, None) == ampq.ERR_INVALID
-    assert L.ampq_ckpt_weight_grad_workspace(0, 7, None, 4, 1, 1, 4, 4, 1, C.byref(n)) == ampq.ERR_INVALID
-    assert L.ampq_ckpt_weight_grad_workspace(0, 0, None, 4, 1 << 20, 1 << 20, 4, 4, 1, C.byref(n)) == ampq.ERR_TOO_LARGE
+    assert L.ampq_ckpt_weight_grad_workspace(0, 0, None, 4, 1, 1, 4, 4, None) == ampq.ERR_INVALID
+    assert L.ampq_ckpt_weight_grad_workspace(0, 7, None, 4, 1, 1, 4, 4, C.byref(n)) == ampq.ERR_INVALID
+    assert L.ampq_ckpt_weight_grad_workspace(0, 0, None, 4, 1 << 20, 1 << 20, 4, 4, C.byref(n)) == ampq.ERR_TOO_LARGE
 
 
 def test_no_device_is_an_error(ampq):

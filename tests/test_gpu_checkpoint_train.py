@@ -67,9 +67,11 @@ def test_linear_parts(ckpt):
     assert [t.dtype for t in kept] == [torch.float32]
     xg, wg, bg = x.clone().requires_grad_(), w.clone().requires_grad_(), b.clone().requires_grad_()
     ckpt.linear(xg, w, b).sum().backward()   # the gradient of a sum is one number expanded
-    assert torch.allclose(xg.grad, w.sum(0).expand(40, 64), rtol=1e-5)
+    # a sum of n terms in fp32, whatever its order, is off by at most n * 2^-24 of the absolute sum
+    assert bool(((xg.grad - w.double().sum(0)).abs() <= 24 * U * w.double().abs().sum(0)).all())
     ckpt.linear(x, wg, b).sum().backward()
-    assert torch.allclose(wg.grad, ckpt.unpack(ckpt.pack(x), torch.float32).sum(0).expand(24, 64), rtol=1e-4, atol=1e-4)
+    kept_x = ckpt.unpack(ckpt.pack(x), torch.float32).double()
+    assert bool(((wg.grad - kept_x.sum(0)).abs() <= (2 * 40 + 8) * U * kept_x.abs().sum(0)).all())
     ckpt.linear(x, w, bg).sum().backward()
     assert torch.equal(bg.grad, torch.full_like(b, 40.0))
 
