@@ -158,6 +158,18 @@ __device__ __forceinline__ void store8(const Raw8<T>& r, T* p, int n) {
         if (i < n) store_elem(p + i, v[i]);
 }
 
+// The ends of rows, out of line: in line their predicated accesses are issued for
+// every chunk.
+template <typename T>
+__device__ __noinline__ void store_some(T* p, int n, const unsigned* w) {
+    for (int i = 0; i < n; ++i) {
+        if (sizeof(T) == 4)
+            reinterpret_cast<unsigned*>(p)[i] = w[i];
+        else
+            reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(w[i / 2] >> (16 * (i & 1)));
+    }
+}
+
 // ---------------------------------------------------------------------------
 // chunks: 32 consecutive bytes of a row, 16 bf16 or 8 fp32, one thread's share
 
@@ -242,14 +254,15 @@ struct Chunk {
     }
     __device__ __forceinline__ void store(T* p, int n) const {
         const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15);
-        if (n < kElems) {
-#pragma unroll
-            for (int i = 0; i < kElems; ++i)
-                if (i < n) store_elem(p + i, at(i));
-            return;
-        }
         unsigned w[8];
         to_words(w);
+        if (n < kElems) {
+            unsigned some[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) some[i] = w[i];
+            store_some(p, n, some);
+            return;
+        }
         if (off == 0) {
             if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
                 asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),

@@ -297,7 +297,7 @@ __device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long 
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = __funnelshift_r(w[i], i < 7 ? w[i + 1] : next, 16);
     }
-    if (n < Chunk<T>::kElems) {
+    if (__any_sync(0xFFFFFFFFu, n < Chunk<T>::kElems)) {  // a row's last warp
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (sizeof(T) == 4) {
