@@ -70,6 +70,47 @@ __device__ __forceinline__ void load_params(const void* p, bool bf16, int c0, in
     }
 }
 
+// Whole rows come by bulk copies, whose bytes an mbarrier counts.
+__device__ __forceinline__ void row_expect(unsigned bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void row_copy(unsigned dst, const void* src, unsigned bytes, unsigned bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// Waits for a row, with a limit; false when it runs out.
+__device__ __forceinline__ bool row_wait(unsigned bar, unsigned parity) {
+    for (unsigned i = 0; i < (1u << 22); ++i) {
+        unsigned ok;
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 2000;\n"
+            "selp.u32 %0, 1, 0, p;\n"
+            "}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+
+__device__ __forceinline__ uint4 take16(unsigned src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
+
+// A chunk that lies in shared memory as it does in its row: the upper four of
+// eight lanes read their second half first, so that the eight meet all 32 banks.
+__device__ __forceinline__ void take_words(unsigned at, unsigned lane, unsigned (&w)[8]) {
+    const unsigned swap = (lane >> 2) & 1;
+    const uint4 p = take16(at + 16 * swap), q = take16(at + 16 * (1 - swap));
+    const uint4 lo = swap ? q : p, hi = swap ? p : q;
+    w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w;
+    w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+}
+
 struct ForwardArgs {
     const void *x, *w, *b;
     void* y;
@@ -81,104 +122,153 @@ struct ForwardArgs {
     bool param_bf16;
     bool whole;  // the last chunk of a row is a whole one
     bool e4m3;   // the checkpoint's format
+    bool bulk;   // rows can be copied whole, and there are several to a group
 };
 
-// One row per group of WPR warps, held in registers between the statistics (mean,
+// CTAs of the forward pass that share an SM, and the shared memory of one: two
+// rows of each row group, the current one and the next.
+template <typename T, int WPR, int WIDE>
+struct ForwardRing {
+    static constexpr int kRow = 512 * WPR * WIDE * (int)sizeof(T);
+    static constexpr int kBytes = 2 * Shape<WPR, WIDE>::kGroups * kRow;
+    static constexpr int kFit = 200 * 1024 / kBytes, kThreadFit = 1024 / Shape<WPR, WIDE>::kThreads;
+    static constexpr int kCtas = kFit < kThreadFit ? kFit : kThreadFit;
+};
+
+// A row to a group of WPR warps, held in registers between the statistics (mean,
 // then the sum of squared differences from it) and the output, so x is read once.
-// Thread t of a group holds the chunks (j * threads + t): loads are contiguous
-// and neighbouring lanes make the groups of the checkpoint.
+// Thread t of a group holds the chunks (j * threads + t): neighbouring lanes make
+// the groups of the checkpoint.  Where there are several rows to a group and their
+// layout allows it, the next row comes by a bulk copy meanwhile.
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
-__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads) norm_forward_kernel(const ForwardArgs a) {
+__global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR, WIDE>::kCtas) norm_forward_kernel(const ForwardArgs a) {
     using S = Shape<WPR, WIDE>;
     using K = Chunk<T>;
+    using Ring = ForwardRing<T, WPR, WIDE>;
     constexpr int V = kChunks<T, WIDE>, E = K::kElems;
-    __shared__ float red[2][S::kWarps];
-    const int warp = threadIdx.x / 32;
+    extern __shared__ __align__(128) unsigned char rows_smem[];
+    __shared__ float red[2][2][S::kWarps];
+    __shared__ alignas(8) unsigned long long s_bars[2 * S::kGroups];
+    const int warp = threadIdx.x / 32, group = warp / WPR;
     const int t = threadIdx.x % (32 * WPR);
-    const long long row = (long long)blockIdx.x * S::kGroups + warp / WPR;
-    const bool live = row < a.rows;
-    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    K k[V];
-    int n[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c0 = (j * 32 * WPR + t) * E;
-        n[j] = live ? min(E, a.cols - c0) : 0;
-        k[j].zero();
-        if (n[j] > 0) k[j].load(x + c0, n[j]);
+    const unsigned lane = threadIdx.x % 32;
+    const long long stride = (long long)gridDim.x * S::kGroups, first = (long long)blockIdx.x * S::kGroups + group;
+    const unsigned slots = (unsigned)__cvta_generic_to_shared(rows_smem) + 2 * group * Ring::kRow;
+    const unsigned bars = (unsigned)__cvta_generic_to_shared(s_bars) + 16 * group;
+    const unsigned row_bytes = (unsigned)a.cols * (unsigned)sizeof(T);
+    auto begin_copy = [&](long long row, int slot) {
+        row_expect(bars + 8 * slot, row_bytes);
+        row_copy(slots + slot * Ring::kRow, static_cast<const T*>(a.x) + row * a.ld_x, row_bytes, bars + 8 * slot);
+    };
+    if (a.bulk) {
+        if (t == 0) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+        if (t == 0) {
+            if (first < a.rows) begin_copy(first, 0);
+            if (first + stride < a.rows) begin_copy(first + stride, 1);
+        }
     }
     const float inv_cols = 1.0f / (float)a.cols;
-    float mean = 0.0f;
-    if (LAYER) {
-        float2 s2 = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) s2 = __fadd2_rn(s2, k[j].v[i]);
-        float s[1] = {s2.x + s2.y};
-        row_sum<WPR, 1>(s, red[0], warp);
-        mean = s[0] * inv_cols;
-    }
-    const float2 minus = make_float2(-mean, -mean);
-    float2 q2 = make_float2(0.0f, 0.0f);
-    if (!LAYER || a.whole) {
+    int taken = 0;  // rows of this group so far
+    for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += stride, ++taken) {
+        const long long row = row0 + group;
+        const bool live = row < a.rows;
+        const int slot = taken & 1;
+        const bool here = !a.bulk || !live || row_wait(bars + 8 * slot, (taken >> 1) & 1);
+        K k[V];
+        int n[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (LAYER && n[j] <= 0) continue;
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                const float2 d = LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i];
-                q2 = __ffma2_rn(d, d, q2);
+            const int c0 = (j * 32 * WPR + t) * E;
+            n[j] = live ? min(E, a.cols - c0) : 0;
+            k[j].zero();
+            if (a.bulk) {
+                unsigned w[8];
+                take_words(slots + slot * Ring::kRow + (j * 32 * WPR + t) * 32, lane, w);
+                if (n[j] > 0) k[j].from_words(w);
+            } else if (n[j] > 0) {
+                k[j].load(static_cast<const T*>(a.x) + row * a.ld_x + c0, n[j]);
             }
         }
-    } else {
+        float mean = 0.0f;
+        if (LAYER) {
+            float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
+            for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                float2 d = __fadd2_rn(k[j].v[i], minus);
-                d = make_float2(2 * i < n[j] ? d.x : 0.0f, 2 * i + 1 < n[j] ? d.y : 0.0f);
-                q2 = __ffma2_rn(d, d, q2);
+                for (int i = 0; i < E / 2; ++i) s2 = __fadd2_rn(s2, k[j].v[i]);
+            float s[1] = {s2.x + s2.y};
+            row_sum<WPR, 1>(s, red[slot][0], warp);
+            mean = s[0] * inv_cols;
+        }
+        const float2 minus = make_float2(-mean, -mean);
+        float2 q2 = make_float2(0.0f, 0.0f);
+        if (!LAYER || a.whole) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (LAYER && n[j] <= 0) continue;
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) {
+                    const float2 d = LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i];
+                    q2 = __ffma2_rn(d, d, q2);
+                }
             }
-    }
-    float q[1] = {q2.x + q2.y};
-    row_sum<WPR, 1>(q, red[1], warp);
-    const float rstd = 1.0f / sqrtf(q[0] * inv_cols + a.eps);
-    if (live && t == 0) {
-        if (LAYER) a.mean[row] = mean;
-        a.rstd[row] = rstd;
-    }
+        } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c0 = (j * 32 * WPR + t) * E;
-        if (KEPT) {
-            const unsigned amax = k[j].group_amax();
-            const unsigned byte = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(amax) : scale_byte<AMPQ_FMT_E5M2>(amax);
-            if (live && (c0 & ~(kGroup - 1)) < a.cols) {  // whole groups: the columns behind the last are stored as 0
-                unsigned c[E / 4];
-                if (a.e4m3)
-                    k[j].template encode<AMPQ_FMT_E4M3>(byte, c);
-                else
-                    k[j].template encode<AMPQ_FMT_E5M2>(byte, c);
-                store_codes(a.codes + row * a.ld_codes + c0, c);
-                if (t % K::kLanes == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) {
+                    float2 d = __fadd2_rn(k[j].v[i], minus);
+                    d = make_float2(2 * i < n[j] ? d.x : 0.0f, 2 * i + 1 < n[j] ? d.y : 0.0f);
+                    q2 = __ffma2_rn(d, d, q2);
+                }
+        }
+        float q[1] = {q2.x + q2.y};
+        row_sum<WPR, 1>(q, red[slot][1], warp);
+        // every thread of the group has read its part of the row: its place takes the row after the next
+        if (WPR == 1) __syncwarp();
+        if (a.bulk && t == 0 && row + 2 * stride < a.rows) begin_copy(row + 2 * stride, slot);
+        const float rstd = here ? 1.0f / sqrtf(q[0] * inv_cols + a.eps) : __uint_as_float(0x7FC00000u);
+        if (live && t == 0) {
+            if (LAYER) a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c0 = (j * 32 * WPR + t) * E;
+            if (KEPT) {
+                const unsigned amax = k[j].group_amax();
+                const unsigned byte = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(amax) : scale_byte<AMPQ_FMT_E5M2>(amax);
+                if (live && (c0 & ~(kGroup - 1)) < a.cols) {  // whole groups: the columns behind the last are stored as 0
+                    unsigned c[E / 4];
+                    if (a.e4m3)
+                        k[j].template encode<AMPQ_FMT_E4M3>(byte, c);
+                    else
+                        k[j].template encode<AMPQ_FMT_E5M2>(byte, c);
+                    store_codes(a.codes + row * a.ld_codes + c0, c);
+                    if (t % K::kLanes == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
+                }
             }
-        }
-        if (n[j] <= 0) continue;
+            if (n[j] <= 0) continue;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i], make_float2(rstd, rstd));
-        K p;
-        if (a.w) {
-            load_params(a.w, a.param_bf16, c0, n[j], p);
+            for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i], make_float2(rstd, rstd));
+            K p;
+            if (a.w) {
+                load_params(a.w, a.param_bf16, c0, n[j], p);
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(k[j].v[i], p.v[i]);
-        }
-        if (LAYER && a.b) {
-            load_params(a.b, a.param_bf16, c0, n[j], p);
+                for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(k[j].v[i], p.v[i]);
+            }
+            if (LAYER && a.b) {
+                load_params(a.b, a.param_bf16, c0, n[j], p);
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fadd2_rn(k[j].v[i], p.v[i]);
+                for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fadd2_rn(k[j].v[i], p.v[i]);
+            }
+            k[j].store(static_cast<T*>(a.y) + row * a.ld_y + c0, n[j]);
         }
-        k[j].store(static_cast<T*>(a.y) + row * a.ld_y + c0, n[j]);
     }
 }
 
@@ -199,12 +289,6 @@ struct BackwardArgs {
 __device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ uint4 take16(unsigned src) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void copy4(unsigned dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -281,12 +365,7 @@ __device__ __forceinline__ void copy_scales(unsigned to, const unsigned char* sc
 // This lane's chunk of a piece, zeros from element n on.  All lanes call it.
 template <typename T>
 __device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long ld, long long row, int at, bool aligned, unsigned lane, int n, unsigned (&w)[8]) {
-    // the upper four of eight lanes read their second half first: the eight meet all 32 banks
-    const unsigned swap = (lane >> 2) & 1, a = from + 32 * lane;
-    const uint4 p = take16(a + 16 * swap), q = take16(a + 16 * (1 - swap));
-    const uint4 lo = swap ? q : p, hi = swap ? p : q;
-    w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w;
-    w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+    take_words(from + 32 * lane, lane, w);
     if (aligned) {
         if (n * (int)sizeof(T) <= 16) w[4] = w[5] = w[6] = w[7] = 0;
         return;
@@ -621,26 +700,42 @@ int backward_ctas(long long rows, int cols, int sms) {
     return (int)(need < most ? need : most);
 }
 
+constexpr int kMaxDevices = 64;
+
+// Lets a kernel use `bytes` of dynamic shared memory, once per device.
+template <class Kernel>
+bool allow_smem(Kernel kernel, int bytes, std::atomic<bool>* prepared, int device) {
+    if (device < kMaxDevices && prepared[device].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
+    return true;
+}
+
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
-int start_forward(const ForwardArgs& a, cudaStream_t st) {
+int start_forward(ForwardArgs a, int device, int sms, cudaStream_t st) {
     using S = Shape<WPR, WIDE>;
-    const long long blocks = (a.rows + S::kGroups - 1) / S::kGroups;
-    norm_forward_kernel<T, KEPT, LAYER, WPR, WIDE><<<(unsigned)blocks, S::kThreads, 0, st>>>(a);
+    using Ring = ForwardRing<T, WPR, WIDE>;
+    static std::atomic<bool> prepared[kMaxDevices];
+    const long long need = (a.rows + S::kGroups - 1) / S::kGroups, most = (long long)sms * Ring::kCtas;
+    a.bulk = a.bulk && need > most;  // fewer rows are all read at once
+    if (a.bulk && !allow_smem(norm_forward_kernel<T, KEPT, LAYER, WPR, WIDE>, Ring::kBytes, prepared, device)) return AMPQ_ERR_CUDA;
+    norm_forward_kernel<T, KEPT, LAYER, WPR, WIDE><<<(unsigned)(a.bulk ? most : need), S::kThreads, a.bulk ? Ring::kBytes : 0, st>>>(a);
     return launched();
 }
 
 template <typename T, bool KEPT, bool LAYER>
-int launch_forward(const ForwardArgs& a, cudaStream_t st) {
-    if (a.cols > 4096) return a.cols <= 8192 ? start_forward<T, KEPT, LAYER, 8, 2>(a, st) : start_forward<T, KEPT, LAYER, 16, 2>(a, st);
+int launch_forward(const ForwardArgs& a, int device, int sms, cudaStream_t st) {
+    if (a.cols > 4096) return a.cols <= 8192 ? start_forward<T, KEPT, LAYER, 8, 2>(a, device, sms, st) : start_forward<T, KEPT, LAYER, 16, 2>(a, device, sms, st);
     switch (warps_per_row(a.cols)) {
-        case 1: return start_forward<T, KEPT, LAYER, 1, 1>(a, st);
-        case 2: return start_forward<T, KEPT, LAYER, 2, 1>(a, st);
-        case 4: return start_forward<T, KEPT, LAYER, 4, 1>(a, st);
-        default: return start_forward<T, KEPT, LAYER, 8, 1>(a, st);
+        case 1: return start_forward<T, KEPT, LAYER, 1, 1>(a, device, sms, st);
+        case 2: return start_forward<T, KEPT, LAYER, 2, 1>(a, device, sms, st);
+        case 4: return start_forward<T, KEPT, LAYER, 4, 1>(a, device, sms, st);
+        default: return start_forward<T, KEPT, LAYER, 8, 1>(a, device, sms, st);
     }
 }
-
-constexpr int kMaxDevices = 64;
 
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 int start_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st) {
@@ -648,13 +743,7 @@ int start_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st)
     using S = Shape<WPR, WIDE>;
     constexpr int kJoin = S::kGroups > 1 ? S::kGroups * 512 * WPR * WIDE * 4 : 0;
     constexpr int kBytes = Ring<T, KEPT, WPR, WIDE>::kBytes > kJoin ? Ring<T, KEPT, WPR, WIDE>::kBytes : kJoin;
-    if (kBytes > 32 * 1024 && (device >= kMaxDevices || !prepared[device].load(std::memory_order_acquire))) {
-        if (cudaFuncSetAttribute(norm_backward_kernel<T, KEPT, LAYER, WPR, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
-            cudaGetLastError();
-            return AMPQ_ERR_CUDA;
-        }
-        if (device < kMaxDevices) prepared[device].store(true, std::memory_order_release);
-    }
+    if (!allow_smem(norm_backward_kernel<T, KEPT, LAYER, WPR, WIDE>, kBytes, prepared, device)) return AMPQ_ERR_CUDA;
     norm_backward_kernel<T, KEPT, LAYER, WPR, WIDE><<<(unsigned)ctas, S::kThreads, kBytes, st>>>(a);
     return launched();
 }
@@ -673,9 +762,9 @@ int launch_backward(const BackwardArgs& a, int device, int ctas, cudaStream_t st
 }
 
 template <typename T>
-int dispatch_forward(bool kept, bool layer, const ForwardArgs& a, cudaStream_t st) {
-    if (kept) return layer ? launch_forward<T, true, true>(a, st) : launch_forward<T, true, false>(a, st);
-    return layer ? launch_forward<T, false, true>(a, st) : launch_forward<T, false, false>(a, st);
+int dispatch_forward(bool kept, bool layer, const ForwardArgs& a, int device, int sms, cudaStream_t st) {
+    if (kept) return layer ? launch_forward<T, true, true>(a, device, sms, st) : launch_forward<T, true, false>(a, device, sms, st);
+    return layer ? launch_forward<T, false, true>(a, device, sms, st) : launch_forward<T, false, false>(a, device, sms, st);
 }
 
 template <typename T>
@@ -717,6 +806,8 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     CkptDevice cur(device);
     if (cur.status) return cur.status;
     if (rows == 0 || cols == 0) return AMPQ_OK;
+    const int sms = sm_count(device);
+    if (sms < 1) return AMPQ_ERR_CUDA;
     ForwardArgs a;
     a.x = x; a.w = weight; a.b = bias; a.y = y;
     a.mean = mean; a.rstd = rstd;
@@ -726,10 +817,11 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     a.eps = eps;
     a.e4m3 = fmt == AMPQ_FMT_E4M3;
     a.whole = cols % (dtype == AMPQ_F32 ? 8 : 16) == 0;
+    a.bulk = rows_aligned(x, ld_x, dtype) && a.whole;
     a.param_bf16 = param_dtype == AMPQ_BF16;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const bool kept = fmt != AMPQ_FMT_BASE;
-    return dtype == AMPQ_F32 ? dispatch_forward<float>(kept, layer, a, st) : dispatch_forward<__nv_bfloat16>(kept, layer, a, st);
+    return dtype == AMPQ_F32 ? dispatch_forward<float>(kept, layer, a, device, sms, st) : dispatch_forward<__nv_bfloat16>(kept, layer, a, device, sms, st);
 }
 
 int ampq_norm_backward_workspace(int device, long long rows, long long cols, long long* bytes) {
