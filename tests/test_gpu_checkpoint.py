@@ -371,3 +371,91 @@ def test_two_streams_at_once(ckpt):
     for k in range(2):
         for gw, gb in got[k]:
             assert torch.equal(gw, alone[k][0]) and torch.equal(gb, alone[k][1])
+
+
+# More rows than the row groups of a grid: every group works through several, with copies of the next ones on their way.
+MANY = [(9700, 40), (9600, 256), (5200, 1000), (3000, 2048), (1900, 3000), (1400, 4096), (1300, 5120), (900, 4099), (1400, 8192), (650, 9000), (640, 16384)]
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("kind", [0, 1], ids=["layer", "rms"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS.get)
+def test_norms_of_many_rows(ckpt, dtype, kind, layout):
+    """The same bounds as for few rows, against 64 bits on the device; every row and column is compared."""
+    for k, (rows, cols) in enumerate(MANY):
+        fmt = (0, 1, 2, 1)[(k + kind) % 4]
+        g = torch.Generator(device="cuda").manual_seed(rows + cols)
+        x = laid((torch.randn(rows, cols, device="cuda", generator=g) + 0.25 * (1 - kind)).to(dtype), layout)
+        gy = laid((torch.randn(rows, cols, device="cuda", generator=g) * 1e-2).to(dtype), layout)
+        w = (1 + 0.2 * torch.randn(cols, device="cuda", generator=g)).to(dtype)
+        b = torch.randn(cols, device="cuda", generator=g).to(dtype) if kind == 0 else None
+        y, mean, rstd, p = ckpt.norm_forward(x, w, b, 1e-5, kind, fmt)
+        v = x.double()
+        m = v.mean(1, keepdim=True) if kind == 0 else torch.zeros(rows, 1, device="cuda", dtype=torch.float64)
+        d = v - m
+        var = (d * d).mean(1, keepdim=True)
+        r = (var + 1e-5).rsqrt()
+        off_m = (DEPTH + 2) * U * v.abs().mean(1, keepdim=True) if kind == 0 else torch.zeros_like(m)
+        if kind == 0:
+            assert bool(((mean[:, None] - m).abs() <= off_m).all()), (rows, cols)
+        rel_r = 0.5 * ((DEPTH + 6) * U + (off_m ** 2 + 2 * U * off_m * d.abs().mean(1, keepdim=True)) / (var + 1e-5)) * 1.01 + 3 * U
+        assert bool(((rstd[:, None] - r).abs() <= rel_r * r).all()), (rows, cols)
+        wd, h = w.double(), HALF_STEP[dtype]
+        want = d * r * wd + (b.double() if b is not None else 0.0)
+        tol = (d.abs() * (rel_r + 4 * U) + off_m) * r * wd.abs() * 1.01 + (h + 2 * U) * want.abs() + 1e-45
+        assert bool(((y.double() - want).abs() <= tol).all()), (rows, cols)
+        if fmt:
+            q = ckpt.pack(x, fmt)
+            assert torch.equal(p.codes, q.codes) and torch.equal(p.scales, q.scales), (rows, cols)
+        # the backward pass from what the forward pass left
+        gx, gw, gb = ckpt.norm_backward(gy, p if fmt else x, mean, rstd, w, kind)
+        v = ckpt.unpack(p, torch.float32).double() if fmt else v
+        gd, r = gy.double(), rstd.double()[:, None]
+        hn = (v - (mean.double()[:, None] if kind == 0 else 0.0)) * r
+        t = gd * wd
+        c2 = (t * hn).mean(1, keepdim=True)
+        c1 = t.mean(1, keepdim=True) if kind == 0 else torch.zeros_like(c2)
+        want = r * (t - c1 - hn * c2)
+        e1 = (DEPTH + 6) * U * t.abs().mean(1, keepdim=True) if kind == 0 else 0.0
+        e2 = (DEPTH + 10) * U * (t * hn).abs().mean(1, keepdim=True)
+        tol = r * (8 * U * (t.abs() + c1.abs() + (hn * c2).abs()) + e1 + hn.abs() * e2) * 1.01 + h * want.abs() + 1e-45
+        assert bool(((gx.double() - want).abs() <= tol).all()), (rows, cols)
+        # the sums: at most all rows one after the other
+        want = (gd * hn).sum(0)
+        assert bool(((gw.double() - want).abs() <= (rows + 8) * U * (gd * hn).abs().sum(0) * 1.01 + h * want.abs() + 1e-45).all()), (rows, cols)
+        if kind == 0:
+            want = gd.sum(0)
+            assert bool(((gb.double() - want).abs() <= (rows + 8) * U * gd.abs().sum(0) * 1.01 + h * want.abs() + 1e-45).all()), (rows, cols)
+
+
+LARGE = [(1, 700, 2600, 2500), (3, 600, 1700, 2300), (2, 4096, 520, 264), (1, 130, 4100, 2100), (5, 300, 1024, 1024)]
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS.get)
+def test_weight_grad_of_many_tiles(ckpt, dtype, layout):
+    """More tiles than the grid, pairs of CTAs, parts of the token axis: against 64 bits on the device."""
+    for k, (samples, rows, cols, outs) in enumerate(LARGE):
+        p, gy = wgrad_case(ckpt, dtype, 1 + k % 2, samples, rows, cols, outs, layout, 9)
+        gw, gb = ckpt.weight_grad(p, gy, samples=samples, bias=True)
+        x = ckpt.unpack(p, torch.float32).double().reshape(samples, rows, cols)
+        g = gy.double().reshape(samples, rows, outs)
+        want, size = torch.matmul(g.transpose(1, 2), x), torch.matmul(g.abs().transpose(1, 2), x.abs())
+        h = HALF_STEP[dtype]
+        assert bool(((gw.double() - want).abs() <= (2 * rows + 8) * U * size * (1 + h) + h * want.abs()).all()), (samples, rows, cols, outs)
+        want = g.sum(1)
+        assert bool(((gb.double() - want).abs() <= (rows + 8) * U * g.abs().sum(1) * (1 + h) + h * want.abs()).all())
+        again, _ = ckpt.weight_grad(p, gy, samples=samples)
+        assert torch.equal(gw, again)
+
+
+def test_weight_grad_fp32_does_not_drift(ckpt):
+    """Sums of one sign over 8192 tokens in fp32: a sum that is cut at every addition would be off by 4e-5 of itself; rounded
+    to nearest after each 64 tokens it stays within the sixteen additions of a run (cut: 2^-23 each) and 128 roundings."""
+    x = torch.rand(8192, 256, device="cuda") + 0.5
+    gy = torch.rand(8192, 512, device="cuda") + 0.5
+    p = ckpt.pack(x)
+    gw, _ = ckpt.weight_grad(p, gy)
+    want = torch.matmul(gy.double().T, ckpt.unpack(p, torch.float32).double())
+    assert float(((gw[0].double() - want) / want).abs().max()) <= 16 * 2 * U + 128 * U
+    assert float(((gw[0].double() - want) / want).mean().abs()) <= 8 * 2 * U
