@@ -283,7 +283,7 @@ struct BackwardArgs {
     bool param_bf16, sum_b;
     bool e4m3;               // the checkpoint's format
     bool aligned_gy, aligned_x;  // rows start on 16-byte boundaries
-    bool aligned_scales;         // rows of scale bytes are whole words
+    bool whole;                  // rows can be copied whole
 };
 
 __device__ __forceinline__ void copy16(unsigned dst, const void* src, int bytes) {  // the first `bytes` of 16, zeros behind them
@@ -393,9 +393,10 @@ __device__ __forceinline__ void take_chunk(unsigned from, const T* m, long long 
 template <typename T, int WIDE>
 constexpr int kSmallPiece = 16 + 32 * kChunks<T, WIDE>;
 
-// Shared memory of a CTA per row on its way: gy, x or its codes, the row's small values.
+// Shared memory of a CTA per row on its way: gy, x or its codes, the row's small
+// values, and the scale bytes of rows that come whole.
 template <typename T, bool KEPT, int WPR, int WIDE>
-constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (KEPT ? 512 * WIDE : kChunks<T, WIDE> * kPiece) + kSmallPiece<T, WIDE>);
+constexpr int kRowBytes = Shape<WPR, WIDE>::kWarps * (kChunks<T, WIDE> * kPiece + (KEPT ? 512 * WIDE : kChunks<T, WIDE> * kPiece) + kSmallPiece<T, WIDE> + (KEPT ? 16 * WIDE : 0));
 
 // Rows on their way, the current one among them: four, or as many as leave room
 // for the CTAs meant to be resident; 0 where not even two fit (fp32 rows of more
@@ -423,6 +424,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     constexpr int kAhead = Ring<T, KEPT, WPR, WIDE>::kRows;
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float red[2][S::kWarps * 2];
+    __shared__ alignas(8) unsigned long long s_bars[4 * S::kGroups];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
     const int group = warp / WPR;
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     const unsigned ring_x = ring_gy + kAhead * kGyRow;
     const unsigned ring_codes = (unsigned)__cvta_generic_to_shared(ring) + kAhead * kGyRow + threadIdx.x * 16;
     constexpr int kSmall = kSmallPiece<T, WIDE>;
-    const unsigned ring_small = (unsigned)__cvta_generic_to_shared(ring) + kAhead * (kRowBytes<T, KEPT, WPR, WIDE> - S::kWarps * kSmall) + warp * kSmall;
+    const unsigned ring_small = (unsigned)__cvta_generic_to_shared(ring) + kAhead * (kRowBytes<T, KEPT, WPR, WIDE> - S::kWarps * (kSmall + (KEPT ? 16 * WIDE : 0))) + warp * kSmall;
     const int groups = (a.cols + kGroup - 1) / kGroup;
     float2 sum_w[V][E / 2], sum_b[V][E / 2];
 #pragma unroll
@@ -441,52 +443,31 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         for (int i = 0; i < E / 2; ++i) sum_w[j][i] = sum_b[j][i] = make_float2(0.0f, 0.0f);
     const float inv_cols = 1.0f / (float)a.cols;
     const long long stride = (long long)gridDim.x * S::kGroups;
-    // Rows on 16-byte boundaries: where this lane copies from next, and how much.
-    const bool straight = a.aligned_gy && (KEPT ? a.aligned_scales : a.aligned_x);
-    constexpr int kPer = 16 / (int)sizeof(T);
-    const long long copy_first = (long long)blockIdx.x * S::kGroups + group;
-    const T* from_gy = static_cast<const T*>(a.gy) + copy_first * a.ld_gy + (t - (int)lane) * E + (int)lane * kPer;
-    const T* from_x = KEPT ? nullptr : static_cast<const T*>(a.x) + copy_first * a.ld_x + (t - (int)lane) * E + (int)lane * kPer;
-    const unsigned char* from_codes = KEPT ? a.codes + copy_first * a.ld_codes + t * E : nullptr;
-    const unsigned char* from_scales = KEPT ? a.scales + copy_first * a.ld_scales + (t - (int)lane) * E / kGroup + 4 * lane : nullptr;
-    const float* from_stats = (lane ? a.rstd : a.mean) + copy_first;
-    auto copy_straight = [&](long long row, int slot) {
+    // Rows on 16-byte boundaries come whole, by bulk copies that one thread of the
+    // group starts (of the kernel's instructions, a fifth were copies by 16 bytes a
+    // lane); they lie as in memory.
+    const bool whole = kAhead > 0 && a.whole;
+    const unsigned base = (unsigned)__cvta_generic_to_shared(ring);
+    const unsigned row_gy = base + group * (WPR * V * 1024), row_x = row_gy + kAhead * kGyRow;
+    const unsigned row_codes = base + kAhead * kGyRow + group * (WPR * 512 * WIDE);
+    const unsigned row_scales = base + kAhead * (kRowBytes<T, KEPT, WPR, WIDE> - S::kWarps * 16 * WIDE) + group * (WPR * 16 * WIDE);
+    const unsigned bars = (unsigned)__cvta_generic_to_shared(s_bars) + 8 * group;
+    auto copy_whole = [&](long long row, int slot) {
         if (row < a.rows) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                constexpr int kStep = 32 * WPR * E;
-                const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = j * kStep + (t - (int)lane) * E + (32 * k + (int)lane) * kPer;
-                    const int bytes = min(16, (a.cols - at) * (int)sizeof(T));
-                    if (bytes > 0) {
-                        copy16(ring_gy + piece + 16 * (32 * k + lane), from_gy + j * kStep + 32 * k * kPer, bytes);
-                        if (!KEPT) copy16(ring_x + piece + 16 * (32 * k + lane), from_x + j * kStep + 32 * k * kPer, bytes);
-                    }
-                }
+            if (t == 0) {
+                const unsigned bar = bars + 8 * S::kGroups * slot, bytes = (unsigned)a.cols * (unsigned)sizeof(T);
+                row_expect(bar, KEPT ? bytes + (unsigned)groups * (kGroup + 1) : 2 * bytes);
+                row_copy(row_gy + slot * kGyRow, static_cast<const T*>(a.gy) + row * a.ld_gy, bytes, bar);
                 if (KEPT) {
-                    const int c0 = (j * 32 * WPR + t) * E;
-                    if (c0 < a.cols) {
-                        if (E == 16)
-                            copy16(ring_codes + (unsigned)((slot * WIDE + j) * kThreads * 16), from_codes + j * kStep, 16);
-                        else
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ring_codes + (unsigned)((slot * WIDE + j / 2) * kThreads * 16) + 8 * (j & 1)), "l"(from_codes + j * kStep) : "memory");
-                    }
-                    if ((int)lane < E / 4 && (j * kStep + (t - (int)lane) * E) / kGroup + 4 * (int)lane < groups)
-                        copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall + 16 + 32 * j) + 4 * lane, from_scales + j * kStep / kGroup);
+                    row_copy(row_codes + slot * (kThreads * 16 * WIDE), a.codes + row * a.ld_codes, groups * kGroup, bar);
+                    row_copy(row_scales + slot * (S::kWarps * 16 * WIDE), a.scales + row * a.ld_scales, groups, bar);
+                } else {
+                    row_copy(row_x + slot * kGyRow, static_cast<const T*>(a.x) + row * a.ld_x, bytes, bar);
                 }
             }
-            if (lane < 2 && (lane || LAYER)) copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall) + 4 * lane, from_stats);
+            if (lane < 2 && (lane || LAYER)) copy4(ring_small + (unsigned)(slot * S::kWarps * kSmall) + 4 * lane, (lane ? a.rstd : a.mean) + row);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        from_gy += stride * a.ld_gy;
-        if (!KEPT) from_x += stride * a.ld_x;
-        if (KEPT) {
-            from_codes += stride * a.ld_codes;
-            from_scales += stride * a.ld_scales;
-        }
-        from_stats += stride;
     };
     auto copy_any = [&](long long row, int slot) {
         if (row < a.rows) {
@@ -512,15 +493,20 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto begin_copy = [&](long long row, int slot) {
-        if (straight)
-            copy_straight(row, slot);
-        else
-            copy_any(row, slot);
-    };
     const long long first = (long long)blockIdx.x * S::kGroups + group;
+    if (whole) {
+        if (t == 0) {
+            for (int s = 0; s < kAhead; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * S::kGroups * s) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
 #pragma unroll
-    for (int s = 0; s < kAhead - 1; ++s) begin_copy(first + s * stride, s);
+        for (int s = 0; s < kAhead; ++s) copy_whole(first + s * stride, s);
+    } else {
+#pragma unroll
+        for (int s = 0; s < kAhead - 1; ++s) copy_any(first + s * stride, s);
+    }
+    unsigned lap = 0;  // parity of the ring's turn
     int slot = 0;
     int phase = 0;
     K weight[V];
@@ -537,9 +523,10 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         const long long row = row0 + group;
         const bool live = row < a.rows;
         __syncwarp();  // the piece that is copied over has been read by all lanes
-        if (kAhead > 0) begin_copy(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
+        if (kAhead > 0 && !whole) copy_any(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead > 0 ? kAhead - 1 : 0) : "memory");
         __syncwarp();
+        const bool here = !whole || !live || row_wait(bars + 8 * S::kGroups * slot, lap);
         float mean = 0.0f, rstd = 0.0f, p[V];
         if (live) {
             if (kAhead > 0) {
@@ -549,9 +536,13 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 if (KEPT) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const unsigned from = straight ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3);
+                        unsigned at;
+                        if (whole)
+                            at = row_scales + (unsigned)(slot * (S::kWarps * 16 * WIDE) + (j * 32 * WPR + t) * E / kGroup);
+                        else
+                            at = small + 16 + 32 * j + (unsigned)(reinterpret_cast<uintptr_t>(a.scales + row * a.ld_scales + (j * 32 * WPR + t - (int)lane) * E / kGroup) & 3) + lane / K::kLanes;
                         unsigned byte;
-                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(small + 16 + 32 * j + from + lane / K::kLanes) : "memory");
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(at) : "memory");
                         p[j] = scale_of(byte);
                     }
                 }
@@ -559,6 +550,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 rstd = __ldg(a.rstd + row);
                 if (LAYER) mean = __ldg(a.mean + row);
             }
+            if (!here) rstd = __uint_as_float(0x7FC00000u);
         }
         K g[V], h[kTwice ? 1 : V];                 // gy * weight; (x - mean) * rstd, or
         unsigned xr[V][KEPT ? E / 4 : 8];          // the codes or words of x to form it again
@@ -589,7 +581,11 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
             const int c0 = (j * 32 * WPR + t) * E;
             const int n = live ? min(E, a.cols - c0) : 0;
             unsigned w8[8];
-            if constexpr (kAhead > 0) {
+            if (whole) {
+                const unsigned at = (unsigned)(slot * kGyRow + (j * 32 * WPR + t) * 32);
+                take_words(row_gy + at, lane, w8);
+                if constexpr (!KEPT) take_words(row_x + at, lane, xr[j]);
+            } else if constexpr (kAhead > 0) {
                 const unsigned piece = (unsigned)(slot * kGyRow + j * kPiece);
                 take_chunk(ring_gy + piece, static_cast<const T*>(a.gy), a.ld_gy, row, c0, a.aligned_gy, lane, n, w8);
                 if constexpr (!KEPT) take_chunk(ring_x + piece, static_cast<const T*>(a.x), a.ld_x, row, c0, a.aligned_x, lane, n, xr[j]);
@@ -599,12 +595,13 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
             }
             if (n <= 0) continue;
             if constexpr (KEPT) {
-                const uint4 q = take16(ring_codes + (unsigned)((slot * WIDE + j * E / 16) * kThreads * 16));
+                const unsigned at = whole ? row_codes + (unsigned)(slot * (kThreads * 16 * WIDE) + (j * 32 * WPR + t) * E)
+                                          : ring_codes + (unsigned)((slot * WIDE + j * E / 16) * kThreads * 16 + j * E % 16);
                 if (E == 16) {
+                    const uint4 q = take16(at);
                     xr[j][0] = q.x; xr[j][1] = q.y; xr[j][2 % (E / 4)] = q.z; xr[j][3 % (E / 4)] = q.w;
                 } else {
-                    xr[j][0] = j & 1 ? q.z : q.x;
-                    xr[j][1] = j & 1 ? q.w : q.y;
+                    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(xr[j][0]), "=r"(xr[j][1]) : "r"(at) : "memory");
                 }
             }
             g[j].from_words(w8);
@@ -632,6 +629,9 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
             both[0] = one[0];
         }
         phase ^= 1;
+        // every thread of the group has read its part of the row: its place takes another one
+        if (WPR == 1) __syncwarp();
+        if (whole) copy_whole(row + kAhead * stride, slot);
         const float m2 = -both[0] * inv_cols, m1 = LAYER ? -both[1] * inv_cols : 0.0f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -651,7 +651,10 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
             }
             g[j].store(static_cast<T*>(a.gx) + row * a.ld_gx + c0, n);
         }
-        if (++slot == kAhead) slot = 0;
+        if (++slot == kAhead) {
+            slot = 0;
+            lap ^= 1;
+        }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.part) return;
@@ -873,7 +876,9 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.e4m3 = fmt == AMPQ_FMT_E4M3;
         a.aligned_gy = rows_aligned(gy, ld_gy, dtype);
         a.aligned_x = rows_aligned(x, ld_x, dtype);
-        a.aligned_scales = aligned_to(scales, 4) && ld_scales % 4 == 0 && ((cols + kGroup - 1) / kGroup) % 4 == 0;
+        const long long groups = cols / kGroup;
+        a.whole = a.aligned_gy && cols % (dtype == AMPQ_F32 ? 8 : 16) == 0 &&
+                  (fmt == AMPQ_FMT_BASE ? a.aligned_x : cols % kGroup == 0 && groups % 16 == 0 && ld_scales % 16 == 0 && aligned_to(scales, 16));
         const bool kept = fmt != AMPQ_FMT_BASE;
         rc = dtype == AMPQ_F32 ? dispatch_backward<float>(kept, layer, a, device, ctas, st) : dispatch_backward<__nv_bfloat16>(kept, layer, a, device, ctas, st);
         if (rc) return rc;
