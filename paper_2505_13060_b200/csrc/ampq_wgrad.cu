@@ -471,9 +471,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 // ---------------------------------------------------------------------------
 // small products
 
-constexpr int kSmallSide = 64, kSmallStep = 16;
+constexpr int kSmallSide = 64, kSmallStep = 32;
 
-// A 64 x 64 tile of one sample's gradient per block, sixteen tokens at a time
+// A 64 x 64 tile of one sample's gradient per block, 32 tokens at a time
 // through shared memory, fp32 products and sums.  The blocks of the first column
 // of tiles also sum the columns of gY.
 template <typename T, int FMT>
@@ -483,24 +483,22 @@ __global__ void __launch_bounds__(256) small_product_kernel(const T* __restrict_
     __shared__ float sg[kSmallStep][kSmallSide + 4], sx[kSmallStep][kSmallSide + 4];
     const long long k0 = (long long)blockIdx.x * kSmallSide, c0 = (long long)blockIdx.y * kSmallSide, r = blockIdx.z;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    // this thread's part of a step: four gradient elements, and (half of the threads) eight codes
-    const int gn = threadIdx.x / 16, gk = threadIdx.x % 16;
-    const int xn = threadIdx.x / 8, xc = threadIdx.x % 8 * 8;
-    float g[4], x[8];
+    // this thread's part of a step: a token's gradient elements gk, gk + 8, ..., and eight of its codes
+    const int n = threadIdx.x / 8, gk = threadIdx.x % 8, xc = threadIdx.x % 8 * 8;
+    float g[8];
+    uint2 x;
+    unsigned byte;
     auto fetch = [&](long long n0) {
-        const T* p = gy + (r * rows + n0 + gn) * ld_gy + k0;
+        const long long row = r * rows + n0 + n;
+        const bool in = n0 + n < rows;
+        const T* p = gy + row * ld_gy + k0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = n0 + gn < rows && k0 + gk + 16 * i < outs ? load_elem(p + gk + 16 * i) : 0.0f;
-        if (threadIdx.x < kSmallStep * 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-            if (n0 + xn < rows && c0 + xc < cols) {
-                const long long row = r * rows + n0 + xn;
-                decode8<FMT>(__ldg(reinterpret_cast<const uint2*>(codes + row * ld_codes + c0 + xc)), x);
-                const float s = scale_of(__ldg(scales + row * ld_scales + (c0 + xc) / kGroup));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= s;
-            }
+        for (int i = 0; i < 8; ++i) g[i] = in && k0 + gk + 8 * i < outs ? load_elem(p + gk + 8 * i) : 0.0f;
+        x = make_uint2(0, 0);
+        byte = 127;
+        if (in && c0 + xc < cols) {
+            x = __ldg(reinterpret_cast<const uint2*>(codes + row * ld_codes + c0 + xc));
+            byte = __ldg(scales + row * ld_scales + (c0 + xc) / kGroup);
         }
     };
     float acc[4][4] = {}, sum[4] = {};
@@ -508,18 +506,20 @@ __global__ void __launch_bounds__(256) small_product_kernel(const T* __restrict_
     fetch(0);
     for (long long n0 = 0; n0 < rows; n0 += kSmallStep) {
         __syncthreads();
+        float v[8];
+        decode8<FMT>(x, v);
+        const float scale = scale_of(byte);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sg[gn][gk + 16 * i] = g[i];
-        if (threadIdx.x < kSmallStep * 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sx[xn][xc + i] = x[i];
+        for (int i = 0; i < 8; ++i) {
+            sg[n][gk + 8 * i] = g[i];
+            sx[n][xc + i] = v[i] * scale;
         }
         __syncthreads();
         if (n0 + kSmallStep < rows) fetch(n0 + kSmallStep);
-#pragma unroll
-        for (int n = 0; n < kSmallStep; ++n) {
-            const float4 u = *reinterpret_cast<const float4*>(&sg[n][ty * 4]), v = *reinterpret_cast<const float4*>(&sx[n][tx * 4]);
-            const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll 16
+        for (int m = 0; m < kSmallStep; ++m) {
+            const float4 u = *reinterpret_cast<const float4*>(&sg[m][ty * 4]), w = *reinterpret_cast<const float4*>(&sx[m][tx * 4]);
+            const float uu[4] = {u.x, u.y, u.z, u.w}, vv[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -572,7 +572,7 @@ constexpr int kSweepChunks = 8, kSweepWays = 32, kSweepParts = 8;
 template <typename T, bool COPY>
 __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChunks * kSweepWays)
     sweep_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols, unsigned short* __restrict__ out, long long pitch,
-                 T* __restrict__ sums) {
+                 T* __restrict__ sums, bool straight) {
     using K = Chunk<T>;
     constexpr int E = K::kElems, kCols = kSweepChunks * E;
     __shared__ float part[kSweepWays][kCols + 1];
@@ -585,11 +585,7 @@ __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChun
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) sum[i] = make_float2(0.0f, 0.0f);
         if (n_cols > 0) {
-#pragma unroll 4
-            for (long long n = blockIdx.y * kSweepWays + way; n < rows; n += kSweepParts * kSweepWays) {
-                const long long row = r * rows + n;
-                unsigned w[8];
-                K::load_words(g + row * ld + c, n_cols, w);
+            auto use = [&](long long row, const unsigned(&w)[8]) {
                 K k;
                 k.from_words(w);
                 if (COPY && sizeof(T) == 2) {
@@ -609,6 +605,52 @@ __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChun
                 }
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) sum[i] = __fadd2_rn(sum[i], k.v[i]);
+            };
+            constexpr long long kStep = kSweepParts * kSweepWays;
+            long long n = blockIdx.y * kSweepWays + way;
+            // four rows at a time without a branch between their loads
+            if (n_cols == E && straight) {
+                for (; n + 3 * kStep < rows; n += 4 * kStep) {
+                    unsigned w[4][8];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint4* p = reinterpret_cast<const uint4*>(g + (r * rows + n + u * kStep) * ld + c);
+                        const uint4 lo = __ldg(p), hi = __ldg(p + 1);
+                        w[u][0] = lo.x; w[u][1] = lo.y; w[u][2] = lo.z; w[u][3] = lo.w;
+                        w[u][4] = hi.x; w[u][5] = hi.y; w[u][6] = hi.z; w[u][7] = hi.w;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) use(r * rows + n + u * kStep, w[u]);
+                }
+            } else if (n_cols == E) {
+                for (; n + 3 * kStep < rows; n += 4 * kStep) {
+                    unsigned v[4][9];
+                    unsigned shift[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        // the words that the chunk's elements lie in; for rows between two words the ninth holds the last one
+                        // (both halves of the outermost words are read on their own: they may be all there is)
+                        const uintptr_t p = reinterpret_cast<uintptr_t>(g + (r * rows + n + u * kStep) * ld + c);
+                        shift[u] = (unsigned)(p & 2) * 8;
+                        const unsigned* q = reinterpret_cast<const unsigned*>(p & ~(uintptr_t)3);
+                        v[u][0] = shift[u] ? (unsigned)__ldg(reinterpret_cast<const unsigned short*>(p)) << 16 : __ldg(q);
+#pragma unroll
+                        for (int i = 1; i < 8; ++i) v[u][i] = __ldg(q + i);
+                        v[u][8] = shift[u] ? (unsigned)__ldg(reinterpret_cast<const unsigned short*>(q + 8)) : 0u;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        unsigned w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = __funnelshift_r(v[u][i], v[u][i + 1], shift[u]);
+                        use(r * rows + n + u * kStep, w);
+                    }
+                }
+            }
+            for (; n < rows; n += kStep) {
+                unsigned w[8];
+                K::load_words(g + (r * rows + n) * ld + c, n_cols, w);
+                use(r * rows + n, w);
             }
         }
         if (!sums) continue;
@@ -690,7 +732,11 @@ Plan make_plan(const Problem& q, int sms) {
     p.x_pitch = round_up(q.cols, 8);
     p.steps = (int)((q.rows + kStepRows - 1) / kStepRows);
     const long long pairs = ((q.outs + 255) / 256) * ((q.cols + 255) / 256) * q.samples;
-    p.pair = pairs * 2 >= sms;
+    // A pair's tile runs at twice the rate per SM (its operands are read from shared
+    // memory half as often): 1 x 2048 x 2048 x 2048, 64 pairs, 26.6 us against 34.5.
+    // With few tiles single CTAs spread better: 1 x 4096 x 1024 x 1024, 16 pairs,
+    // 35.6 us against 32.4.
+    p.pair = pairs * 4 >= sms;
     const int side = p.pair ? 256 : 128;
     p.k_tiles = (int)((q.outs + side - 1) / side);
     p.c_tiles = (int)((q.cols + side - 1) / side);
@@ -819,11 +865,12 @@ int sweep(const Problem& q, const Operands& o, bool copy, long long pitch, cudaS
     constexpr int kCols = kSweepChunks * Chunk<T>::kElems;
     const dim3 grid((unsigned)((q.outs + kCols - 1) / kCols), kSweepParts, (unsigned)(q.samples < 65535 ? q.samples : 65535));
     const T* gy = static_cast<const T*>(q.gy);
+    const bool straight = rows_aligned(q.gy, q.ld_gy, q.dtype);  // rows on 16-byte boundaries
     if (copy)
         sweep_kernel<T, true><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, reinterpret_cast<unsigned short*>(o.ws), pitch,
-                                                                          static_cast<T*>(o.gb));
+                                                                          static_cast<T*>(o.gb), straight);
     else
-        sweep_kernel<T, false><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, nullptr, 0, static_cast<T*>(o.gb));
+        sweep_kernel<T, false><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, nullptr, 0, static_cast<T*>(o.gb), straight);
     return launched();
 }
 
