@@ -453,7 +453,11 @@ int ampq_ckpt_unpack(int device, void *cuda_stream, int dtype, int fmt, const un
  *   gw      [samples, outs, cols] of `dtype`, contiguous
  *   gb      [samples, outs] of `dtype`, contiguous, or NULL
  * rows = 0 gives zeros.  Products are exact, sums are fp32, one rounding to
- * `dtype` at the end.  The workspace query takes the same gy (only its alignment
+ * `dtype` at the end.  The internal waits are bounded: entries not stored when one
+ * runs out are NaN.  The workspace of larger products holds x as bf16, the
+ * gradient once more where it is fp32 or its rows do not start on 16-byte
+ * boundaries, and partial products where there are few outputs and many rows;
+ * small ones need none.  The workspace query takes the same gy (only its alignment
  * matters). */
 int ampq_ckpt_weight_grad_workspace(int device, int dtype, const void *gy, long long ld_gy, long long samples, long long rows,
                                     long long cols, long long outs, long long *bytes);

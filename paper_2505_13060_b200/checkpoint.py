@@ -297,15 +297,17 @@ class _Norm(torch.autograd.Function):
 def linear(x: torch.Tensor, weight: torch.Tensor, bias=None, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
     """``torch.nn.functional.linear`` that keeps x for the backward pass in 8 bits:
     the weight's gradient is that of the decoded x, everything else is exact."""
+    if not torch.is_grad_enabled():
+        return torch.nn.functional.linear(x, weight, bias)
     return _Linear.apply(x, weight, bias, fmt)
 
 
 def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
     """Layer norm over the last dimension; x is kept for the backward pass in 8 bits,
     or in full with ``FMT_BASE``."""
-    return _Norm.apply(x, weight, bias, eps, ampq.NORM_LAYER, fmt)
+    return _Norm.apply(x, weight, bias, eps, ampq.NORM_LAYER, fmt if torch.is_grad_enabled() else ampq.FMT_BASE)
 
 
 def rms_norm(x: torch.Tensor, weight=None, eps: float = 1e-5, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
     """RMS norm over the last dimension; x is kept as in ``layer_norm``."""
-    return _Norm.apply(x, weight, None, eps, ampq.NORM_RMS, fmt)
+    return _Norm.apply(x, weight, None, eps, ampq.NORM_RMS, fmt if torch.is_grad_enabled() else ampq.FMT_BASE)

