@@ -126,14 +126,14 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const unsigned char* _
 constexpr int kJoinCols = 32, kJoinWays = 32;
 
 template <typename T>
-__global__ void __launch_bounds__(kJoinCols * kJoinWays) join_columns_kernel(const float* __restrict__ part, int parts, long long cols, T* __restrict__ out,
+__global__ void __launch_bounds__(kJoinCols * kJoinWays) join_columns_kernel(const float* __restrict__ part, int parts, long long cols, long long pitch, T* __restrict__ out,
                                                                              T* __restrict__ second) {
     __shared__ float sums[kJoinWays][kJoinCols];
     const long long c = (long long)blockIdx.x * kJoinCols + threadIdx.x;
     const long long batch = blockIdx.y;
     float s = 0.0f;
     if (c < cols)
-        for (int p = threadIdx.y; p < parts; p += kJoinWays) s += __ldg(part + (batch * parts + p) * cols + c);
+        for (int p = threadIdx.y; p < parts; p += kJoinWays) s += __ldg(part + (batch * parts + p) * pitch + c);
     sums[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.y == 0 && c < cols) {
@@ -185,20 +185,20 @@ int sm_count(int device) {
 }
 
 template <typename T>
-static void join_columns(const float* part, long long batches, int parts, long long cols, T* out, T* second, cudaStream_t st) {
+static void join_columns(const float* part, long long batches, int parts, long long cols, long long pitch, T* out, T* second, cudaStream_t st) {
     const unsigned bx = (unsigned)((cols + kJoinCols - 1) / kJoinCols);
     for (long long b0 = 0; b0 < batches; b0 += 65535) {  // the largest y extent of a grid
         const unsigned by = (unsigned)(batches - b0 < 65535 ? batches - b0 : 65535);
-        join_columns_kernel<T><<<dim3(bx, by), dim3(kJoinCols, kJoinWays), 0, st>>>(part + b0 * parts * cols, parts, cols, out + b0 * cols, second);
+        join_columns_kernel<T><<<dim3(bx, by), dim3(kJoinCols, kJoinWays), 0, st>>>(part + b0 * parts * pitch, parts, cols, pitch, out + b0 * cols, second);
     }
 }
 
-int launch_join_columns(const float* part, long long batches, int parts, long long cols, void* out, void* second, int dtype, cudaStream_t st) {
+int launch_join_columns(const float* part, long long batches, int parts, long long cols, long long pitch, void* out, void* second, int dtype, cudaStream_t st) {
     if (batches <= 0 || cols <= 0) return AMPQ_OK;
     if (dtype == AMPQ_F32)
-        join_columns(part, batches, parts, cols, static_cast<float*>(out), static_cast<float*>(second), st);
+        join_columns(part, batches, parts, cols, pitch, static_cast<float*>(out), static_cast<float*>(second), st);
     else
-        join_columns(part, batches, parts, cols, static_cast<__nv_bfloat16*>(out), static_cast<__nv_bfloat16*>(second), st);
+        join_columns(part, batches, parts, cols, pitch, static_cast<__nv_bfloat16*>(out), static_cast<__nv_bfloat16*>(second), st);
     return launched();
 }
 

@@ -358,9 +358,9 @@ int sm_count(int device);  // multiprocessors of a device, 0 on error
 int launch_ckpt_unpack(int dtype, int fmt, const unsigned char* codes, long long ld_codes, const unsigned char* scales, long long ld_scales,
                        long long rows, long long cols, void* out, long long ld, cudaStream_t st);
 
-// Sums `parts` fp32 partial rows of `cols` columns in a fixed order and stores
-// them in `dtype`: out[b][c] = sum_p part[b][p][c], `batches` of them.  With
+// Sums `parts` fp32 partial rows of `cols` columns, `pitch` apart, in a fixed order
+// and stores them in `dtype`: out[b][c] = sum_p part[b][p][c], `batches` of them.  With
 // `second` (two batches) batch 1 goes there.
-int launch_join_columns(const float* part, long long batches, int parts, long long cols, void* out, void* second, int dtype, cudaStream_t st);
+int launch_join_columns(const float* part, long long batches, int parts, long long cols, long long pitch, void* out, void* second, int dtype, cudaStream_t st);
 
 }  // namespace ampq

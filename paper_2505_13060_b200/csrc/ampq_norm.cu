@@ -111,6 +111,39 @@ __device__ __forceinline__ void take_words(unsigned at, unsigned lane, unsigned 
     w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
 }
 
+// Stores a warp's piece of a row whose rows do not start on 16-byte boundaries: its
+// chunks go through `scratch` (1040 bytes of shared memory), so that a store writes
+// 32 neighbouring words instead of 32 places 32 bytes apart.  p: the piece's first
+// element, n of them; all lanes call it.
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, int n, const Chunk<T>& k, unsigned scratch, unsigned lane) {
+    unsigned w[8];
+    k.to_words(w);
+    __syncwarp();
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(scratch + 32 * lane), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(scratch + 32 * lane + 16), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    __syncwarp();
+    const bool between = reinterpret_cast<uintptr_t>(p) & 2;  // bf16 rows that start between two words
+    constexpr int kPer = 4 / (int)sizeof(T);
+    unsigned* q = reinterpret_cast<unsigned*>(reinterpret_cast<uintptr_t>(p) + (between ? 2 : 0));
+    const int words = (between ? n - 1 : n) / kPer;           // whole words of the row
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int j = 32 * i + (int)lane;
+        unsigned a, b;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(a) : "r"(scratch + 4 * j) : "memory");
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(b) : "r"(scratch + 4 * j + 4) : "memory");
+        if (j < words) q[j] = between ? __funnelshift_r(a, b, 16) : a;
+    }
+    if (sizeof(T) == 2 && lane < 2) {  // what is left at the ends: half a word each
+        const int at = lane ? n - 1 : 0;
+        const bool alone = lane ? (between ? (n - 1) % 2 == 1 : n % 2 == 1) && (n > 1 || !between) : between;
+        unsigned short h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(scratch + 2 * at) : "memory");
+        if (alone) reinterpret_cast<unsigned short*>(p)[at] = h;
+    }
+}
+
 struct ForwardArgs {
     const void *x, *w, *b;
     void* y;
@@ -150,6 +183,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
     constexpr int V = kChunks<T, WIDE>, E = K::kElems;
     extern __shared__ __align__(128) unsigned char rows_smem[];
     __shared__ float red[2][2][S::kWarps];
+    __shared__ alignas(16) unsigned char s_scratch[S::kWarps][1040];
     __shared__ alignas(8) unsigned long long s_bars[2 * S::kGroups];
     const int warp = threadIdx.x / 32, group = warp / WPR;
     const int t = threadIdx.x % (32 * WPR);
@@ -255,21 +289,29 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
                     if (t % K::kLanes == 0) a.scales[row * a.ld_scales + c0 / kGroup] = (unsigned char)byte;
                 }
             }
-            if (n[j] <= 0) continue;
+            T* y = static_cast<T*>(a.y) + row * a.ld_y;
+            const bool straight = (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+            if (straight && n[j] <= 0) continue;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(LAYER ? __fadd2_rn(k[j].v[i], minus) : k[j].v[i], make_float2(rstd, rstd));
             K p;
             if (a.w) {
-                load_params(a.w, a.param_bf16, c0, n[j], p);
+                load_params(a.w, a.param_bf16, c0, max(n[j], 0), p);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fmul2_rn(k[j].v[i], p.v[i]);
             }
             if (LAYER && a.b) {
-                load_params(a.b, a.param_bf16, c0, n[j], p);
+                load_params(a.b, a.param_bf16, c0, max(n[j], 0), p);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) k[j].v[i] = __fadd2_rn(k[j].v[i], p.v[i]);
             }
-            k[j].store(static_cast<T*>(a.y) + row * a.ld_y + c0, n[j]);
+            if (straight) {
+                k[j].store(y + c0, n[j]);
+            } else {
+                const int at = c0 - (int)lane * E;
+                if (live && at < a.cols)
+                    store_piece(y + at, min(32 * E, a.cols - at), k[j], (unsigned)__cvta_generic_to_shared(s_scratch[warp]), lane);
+            }
         }
     }
 }
@@ -279,7 +321,8 @@ struct BackwardArgs {
     const unsigned char *codes, *scales;
     const float *mean, *rstd;
     void* gx;
-    float* part;  // [2][CTAs][cols]: sums of gy*h, then of gy
+    float* part;  // [2][CTAs][part_pitch]: sums of gy*h, then of gy
+    long long part_pitch;
     long long rows, ld_gy, ld_x, ld_codes, ld_scales, ld_gx;
     int cols;
     bool param_bf16, sum_b;
@@ -642,11 +685,14 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         if (WPR == 1) __syncwarp();
         if (whole) copy_whole(row + kAhead * stride, slot);
         const float m2 = -both[0] * inv_cols, m1 = LAYER ? -both[1] * inv_cols : 0.0f;
+        T* gx = static_cast<T*>(a.gx) + row * a.ld_gx;
+        // the row's pieces of gy have been read: their place is free for gx on its way out
+        const bool pieces = kAhead > 0 && !whole && (reinterpret_cast<uintptr_t>(gx) & 15) != 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int c0 = (j * 32 * WPR + t) * E;
             const int n = live ? min(E, a.cols - c0) : 0;
-            if (n <= 0) continue;
+            if (!pieces && n <= 0) continue;
             K k;
             if constexpr (kTwice)
                 k = normalized(j);
@@ -658,7 +704,12 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 if (LAYER) o = __fadd2_rn(o, make_float2(m1, m1));
                 g[j].v[i] = __fmul2_rn(o, make_float2(rstd, rstd));
             }
-            g[j].store(static_cast<T*>(a.gx) + row * a.ld_gx + c0, n);
+            if (pieces) {
+                const int at = c0 - (int)lane * E;
+                if (live && at < a.cols) store_piece(gx + at, min(32 * E, a.cols - at), g[j], ring_gy + (unsigned)(slot * kGyRow + j * kPiece), lane);
+            } else {
+                g[j].store(gx + c0, n);
+            }
         }
         if (++slot == kAhead) {
             slot = 0;
@@ -669,15 +720,16 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     if (!a.part) return;
     float* join = reinterpret_cast<float*>(ring);
     for (int k = 0; k < (LAYER && a.sum_b ? 2 : 1); ++k) {
-        float* out = a.part + ((long long)k * gridDim.x + blockIdx.x) * a.cols;
+        float* out = a.part + ((long long)k * gridDim.x + blockIdx.x) * a.part_pitch;
         if (S::kGroups == 1) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int c0 = (j * 32 * WPR + t) * E;
+                if (c0 >= a.cols) continue;  // whole chunks fit into the pitch
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const float2 f = k ? sum_b[j][i / 2] : sum_w[j][i / 2];
-                    if (c0 + i < a.cols) out[c0 + i] = i & 1 ? f.y : f.x;
+                for (int i = 0; i < E / 2; i += 2) {
+                    const float2 f = k ? sum_b[j][i] : sum_w[j][i], h = k ? sum_b[j][i + 1] : sum_w[j][i + 1];
+                    *reinterpret_cast<float4*>(out + c0 + 2 * i) = make_float4(f.x, f.y, h.x, h.y);
                 }
             }
         } else {
@@ -702,6 +754,9 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
 int warps_per_row(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 8192 ? 8 : 16; }
 // of the backward pass: 512 columns each, and ten warps up to 5120
 int backward_warps(int cols) { return cols <= 512 ? 1 : cols <= 1024 ? 2 : cols <= 2048 ? 4 : cols <= 4096 ? 8 : cols <= 5120 ? 10 : cols <= 8192 ? 16 : 32; }
+
+// Columns of a partial row: whole chunks.
+long long part_pitch(long long cols) { return (cols + 15) / 16 * 16; }
 
 // CTAs of the backward pass: every row group gets a row before one gets two, and
 // no more CTAs than are resident, so that the sums stay in registers.
@@ -843,7 +898,7 @@ int ampq_norm_backward_workspace(int device, long long rows, long long cols, lon
     if (cur.status) return cur.status;
     const int sms = sm_count(device);
     if (sms < 1) return AMPQ_ERR_CUDA;
-    *bytes = 2LL * backward_ctas(rows, (int)cols, sms) * cols * (long long)sizeof(float);
+    *bytes = 2LL * backward_ctas(rows, (int)cols, sms) * part_pitch(cols) * (long long)sizeof(float);
     return AMPQ_OK;
 }
 
@@ -869,7 +924,7 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
     if (sms < 1) return AMPQ_ERR_CUDA;
     const int ctas = backward_ctas(rows, (int)cols, sms);
     const bool sums = gweight != nullptr;
-    if (sums && ctas > 0 && (!workspace || workspace_bytes < 2LL * ctas * cols * (long long)sizeof(float))) return AMPQ_ERR_INVALID;
+    if (sums && ctas > 0 && (!workspace || workspace_bytes < 2LL * ctas * part_pitch(cols) * (long long)sizeof(float))) return AMPQ_ERR_INVALID;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (rows > 0) {
         BackwardArgs a;
@@ -878,6 +933,7 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         a.mean = mean; a.rstd = rstd;
         a.gx = gx;
         a.part = sums ? static_cast<float*>(workspace) : nullptr;
+        a.part_pitch = part_pitch(cols);
         a.rows = rows; a.ld_gy = ld_gy; a.ld_x = ld_x; a.ld_codes = ld_codes; a.ld_scales = ld_scales; a.ld_gx = ld_gx;
         a.cols = (int)cols;
         a.param_bf16 = param_dtype == AMPQ_BF16;
@@ -893,7 +949,7 @@ int ampq_norm_backward(int device, void* cuda_stream, int kind, int dtype, int p
         if (rc) return rc;
     }
     if (!sums) return AMPQ_OK;
-    return launch_join_columns(static_cast<const float*>(workspace), gbias ? 2 : 1, ctas, cols, gweight, gbias, param_dtype, st);
+    return launch_join_columns(static_cast<const float*>(workspace), gbias ? 2 : 1, ctas, cols, part_pitch(cols), gweight, gbias, param_dtype, st);
 }
 
 #pragma GCC visibility pop
