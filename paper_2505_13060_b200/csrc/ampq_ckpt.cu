@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(kJoinCols * kJoinWays) join_columns_kernel(con
     const long long batch = blockIdx.y;
     float s = 0.0f;
     if (c < cols)
+#pragma unroll 5
         for (int p = threadIdx.y; p < parts; p += kJoinWays) s += __ldg(part + (batch * parts + p) * pitch + c);
     sums[threadIdx.y][threadIdx.x] = s;
     __syncthreads();

@@ -460,12 +460,13 @@ struct Ring {
 // few threads that the sums' registers allow.  The groups of a CTA are joined in
 // shared memory, the CTAs by join_columns_kernel, in a fixed order.
 //
-// Bound by the instructions of sixteen warps (20 to an element) and a row's barrier:
-// RMS norm of 8192 x 8192 from 8 bits 75 us (4.5 TB/s), layer norm from bf16 90 us.
+// Bound by the instructions of sixteen warps and a row's barrier: RMS norm of 8192 x
+// 8192 from 8 bits 76 us (4.4 TB/s), layer norm from bf16 87 us (4.6 TB/s).
 // Holding a row back until the next row's sums are under way (103 us against 102 at
 // that point) and two CTAs of half the warps (145 us) cost more in registers and
 // repeated work than the barrier.  Rows off the 16-byte boundaries are copied and
-// put together by words: 2047 x 4099 bf16 47 us.
+// put together by words, and stored through shared memory: 2047 x 4099 bf16 33 us
+// (47 us with each lane's words stored in place).
 template <typename T, bool KEPT, bool LAYER, int WPR, int WIDE>
 __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::kThreads <= 320 ? 2 : 1) norm_backward_kernel(const BackwardArgs a) {
     using S = Shape<WPR, WIDE>;
