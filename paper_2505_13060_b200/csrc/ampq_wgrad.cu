@@ -573,14 +573,14 @@ __device__ __forceinline__ void cut3(float g, unsigned short (&h)[3]) {
 // One read of gY: the sums of its columns per sample (`sums`, may be null), and
 // with COPY its bf16 planes in rows of `pitch` elements, for gradients that TMA
 // cannot read as they lie (fp32, or rows off the 16-byte boundaries).  A block
-// takes eight chunks of columns, 32 rows at a time; the eight blocks of a cluster
-// share a sample's rows and add their sums up through each other's shared memory,
-// in order, so no second launch is needed.  Sums of 2 x 4096 x 28672 bf16 98 us (4.8
+// takes eight chunks of columns, 32 rows at a time; the blocks of a cluster (one to
+// eight, gridDim.y) share a sample's rows and add their sums up through each
+// other's shared memory, in order, so no second launch is needed.  Sums of 2 x 4096 x 28672 bf16 98 us (4.8
 // TB/s); of 8192 x 4096 20 us, where the blocks' joining shows.
-constexpr int kSweepChunks = 8, kSweepWays = 32, kSweepParts = 8;
+constexpr int kSweepChunks = 8, kSweepWays = 32;
 
 template <typename T, bool COPY>
-__global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChunks * kSweepWays)
+__global__ void __launch_bounds__(kSweepChunks * kSweepWays)
     sweep_kernel(const T* __restrict__ g, long long ld, long long samples, long long rows, long long cols, unsigned short* __restrict__ out, long long pitch,
                  T* __restrict__ sums, bool straight) {
     using K = Chunk<T>;
@@ -616,31 +616,31 @@ __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChun
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) sum[i] = __fadd2_rn(sum[i], k.v[i]);
             };
-            constexpr long long kStep = kSweepParts * kSweepWays;
+            const long long step = (long long)gridDim.y * kSweepWays;
             long long n = blockIdx.y * kSweepWays + way;
             // four rows at a time without a branch between their loads
             if (n_cols == E && straight) {
-                for (; n + 3 * kStep < rows; n += 4 * kStep) {
+                for (; n + 3 * step < rows; n += 4 * step) {
                     unsigned w[4][8];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        const uint4* p = reinterpret_cast<const uint4*>(g + (r * rows + n + u * kStep) * ld + c);
+                        const uint4* p = reinterpret_cast<const uint4*>(g + (r * rows + n + u * step) * ld + c);
                         const uint4 lo = __ldg(p), hi = __ldg(p + 1);
                         w[u][0] = lo.x; w[u][1] = lo.y; w[u][2] = lo.z; w[u][3] = lo.w;
                         w[u][4] = hi.x; w[u][5] = hi.y; w[u][6] = hi.z; w[u][7] = hi.w;
                     }
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) use(r * rows + n + u * kStep, w[u]);
+                    for (int u = 0; u < 4; ++u) use(r * rows + n + u * step, w[u]);
                 }
             } else if (n_cols == E) {
-                for (; n + 3 * kStep < rows; n += 4 * kStep) {
+                for (; n + 3 * step < rows; n += 4 * step) {
                     unsigned v[4][9];
                     unsigned shift[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         // the words that the chunk's elements lie in; for rows between two words the ninth holds the last one
                         // (both halves of the outermost words are read on their own: they may be all there is)
-                        const uintptr_t p = reinterpret_cast<uintptr_t>(g + (r * rows + n + u * kStep) * ld + c);
+                        const uintptr_t p = reinterpret_cast<uintptr_t>(g + (r * rows + n + u * step) * ld + c);
                         shift[u] = (unsigned)(p & 2) * 8;
                         const unsigned* q = reinterpret_cast<const unsigned*>(p & ~(uintptr_t)3);
                         v[u][0] = shift[u] ? (unsigned)__ldg(reinterpret_cast<const unsigned short*>(p)) << 16 : __ldg(q);
@@ -653,11 +653,11 @@ __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChun
                         unsigned w[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) w[i] = __funnelshift_r(v[u][i], v[u][i + 1], shift[u]);
-                        use(r * rows + n + u * kStep, w);
+                        use(r * rows + n + u * step, w);
                     }
                 }
             }
-            for (; n < rows; n += kStep) {
+            for (; n < rows; n += step) {
                 unsigned w[8];
                 K::load_words(g + (r * rows + n) * ld + c, n_cols, w);
                 use(r * rows + n, w);
@@ -680,8 +680,7 @@ __global__ void __cluster_dims__(1, kSweepParts, 1) __launch_bounds__(kSweepChun
         const long long col = (long long)blockIdx.x * kCols + threadIdx.x;
         if (blockIdx.y == 0 && threadIdx.x < kCols && col < cols) {
             float t = 0.0f;
-#pragma unroll
-            for (unsigned k = 0; k < kSweepParts; ++k) {
+            for (unsigned k = 0; k < gridDim.y; ++k) {
                 float v;
                 asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(smem_u32(&total[threadIdx.x]), k)) : "memory");
                 t += v;
@@ -870,25 +869,47 @@ int run_small(const Problem& q, const Operands& o, cudaStream_t st) {
 }
 
 template <typename T>
-int sweep(const Problem& q, const Operands& o, bool copy, long long pitch, cudaStream_t st) {
+int sweep(const Problem& q, const Operands& o, bool copy, long long pitch, int sms, cudaStream_t st) {
     if (!copy && !o.gb) return AMPQ_OK;
     constexpr int kCols = kSweepChunks * Chunk<T>::kElems;
-    const dim3 grid((unsigned)((q.outs + kCols - 1) / kCols), kSweepParts, (unsigned)(q.samples < 65535 ? q.samples : 65535));
     const T* gy = static_cast<const T*>(q.gy);
     const bool straight = rows_aligned(q.gy, q.ld_gy, q.dtype);  // rows on 16-byte boundaries
-    if (copy)
-        sweep_kernel<T, true><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, reinterpret_cast<unsigned short*>(o.ws), pitch,
-                                                                          static_cast<T*>(o.gb), straight);
-    else
-        sweep_kernel<T, false><<<grid, kSweepChunks * kSweepWays, 0, st>>>(gy, q.ld_gy, q.samples, q.rows, q.outs, nullptr, 0, static_cast<T*>(o.gb), straight);
-    return launched();
+    // Parts of the rows: the fewest microseconds by a rough count, three blocks on an
+    // SM at a time, 6 us for a block's joining and 1.5 us for each 128 rows of a part.
+    const long long blocks = (q.outs + kCols - 1) / kCols * q.samples;
+    int parts = 1;
+    double least = 0.0;
+    for (int p = 1; p <= 8; p *= 2) {
+        const double us = (double)((blocks * p + 3LL * sms - 1) / (3LL * sms)) * (6.0 + 1.5 * (double)((q.rows + 128LL * p - 1) / (128LL * p)));
+        if (p == 1 || us < least) {
+            least = us;
+            parts = p;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((q.outs + kCols - 1) / kCols), parts, (unsigned)(q.samples < 65535 ? q.samples : 65535));
+    cfg.blockDim = dim3(kSweepChunks * kSweepWays);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.y = parts;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    unsigned short* out = copy ? reinterpret_cast<unsigned short*>(o.ws) : nullptr;
+    if (cudaLaunchKernelEx(&cfg, copy ? sweep_kernel<T, true> : sweep_kernel<T, false>, gy, q.ld_gy, q.samples, q.rows, q.outs, out, pitch, static_cast<T*>(o.gb),
+                           straight) != cudaSuccess) {
+        cudaGetLastError();
+        return AMPQ_ERR_CUDA;
+    }
+    return AMPQ_OK;
 }
 
 template <typename T>
 int run_large(const Problem& q, const Plan& p, const Operands& o, int device, int sms, cudaStream_t st) {
     const long long rows = q.samples * q.rows;
     int rc;
-    if ((rc = sweep<T>(q, o, p.copy, p.pitch, st))) return rc;
+    if ((rc = sweep<T>(q, o, p.copy, p.pitch, sms, st))) return rc;
     if ((rc = launch_ckpt_unpack(AMPQ_BF16, o.fmt, o.codes, o.ld_codes, o.scales, o.ld_scales, rows, q.cols, o.ws + p.at_x, p.x_pitch, st))) return rc;
     CUtensorMap g_map, x_map;
     if ((rc = operand_map(&g_map, p.copy ? o.ws : q.gy, p.pitch, q.outs, q, p.planes))) return rc;
@@ -930,7 +951,7 @@ int run(const Problem& q, const Plan& p, const Operands& o, int device, int sms,
         cudaGetLastError();
         return AMPQ_ERR_CUDA;
     }
-    return q.rows == 0 ? AMPQ_OK : sweep<T>(q, o, false, 0, st);
+    return q.rows == 0 ? AMPQ_OK : sweep<T>(q, o, false, 0, sms, st);
 }
 
 int check_sizes(int dtype, long long samples, long long rows, long long cols, long long outs) {

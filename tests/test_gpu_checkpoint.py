@@ -548,3 +548,37 @@ def test_tensor_level_refusals(ampq, ckpt):
         with pytest.raises(ampq.AmpqError) as e:
             call()
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("pitch", [0, 16, 3], ids=["same", "wide", "odd"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS.get)
+def test_norm_outputs_in_wider_rows(ampq, ckpt, dtype, pitch):
+    """Outputs of the C calls in rows of their own pitch: the values of contiguous outputs, and nothing behind a row, behind
+    the last row or in front of the first is written."""
+    L, st, code = ampq.lib(), torch.cuda.current_stream().cuda_stream, 0 if dtype == torch.float32 else 1
+    for rows, cols in ((5, 40), (2500, 64), (700, 4096), (40, 4099), (300, 1001), (310, 5121)):
+        x, gy = values(rows, cols, dtype, 60), values(rows, cols, dtype, 61, 1e-2)
+        w, b = torch.rand(cols, device="cuda").to(dtype), torch.rand(cols, device="cuda").to(dtype)
+        y, mean, rstd, _ = ckpt.norm_forward(x, w, b, 1e-5, 0)
+        gx, gw, gb = ckpt.norm_backward(gy, x, mean, rstd, w, 0)
+        ld = cols + pitch
+
+        def room():
+            return torch.full((rows + 2, ld), 9.0, dtype=dtype, device="cuda")
+
+        def inside(t):
+            inner = t[1:rows + 1, :cols]
+            rest = torch.ones(t.shape, dtype=torch.bool, device="cuda")
+            rest[1:rows + 1, :cols] = False
+            assert bool((t[rest] == 9.0).all()), (rows, cols)
+            return inner
+
+        t = room()
+        assert L.ampq_norm_forward(0, st, 0, code, code, 0, x.data_ptr(), cols, rows, cols, w.data_ptr(), b.data_ptr(), 1e-5, t[1].data_ptr(), ld,
+                                   mean.data_ptr(), rstd.data_ptr(), 0, 0, 0, 0) == 0
+        assert torch.equal(inside(t), y)
+        t, ws = room(), torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+        gw2, gb2 = torch.empty_like(gw), torch.empty_like(gb)
+        assert L.ampq_norm_backward(0, st, 0, code, code, 0, gy.data_ptr(), cols, x.data_ptr(), cols, 0, 0, 0, 0, rows, cols, mean.data_ptr(),
+                                    rstd.data_ptr(), w.data_ptr(), t[1].data_ptr(), ld, gw2.data_ptr(), gb2.data_ptr(), ws.data_ptr(), ws.numel()) == 0
+        assert torch.equal(inside(t), gx) and torch.equal(gw, gw2) and torch.equal(gb, gb2)
