@@ -575,8 +575,9 @@ __device__ __forceinline__ void cut3(float g, unsigned short (&h)[3]) {
 // cannot read as they lie (fp32, or rows off the 16-byte boundaries).  A block
 // takes eight chunks of columns, 32 rows at a time; the blocks of a cluster (one to
 // eight, gridDim.y) share a sample's rows and add their sums up through each
-// other's shared memory, in order, so no second launch is needed.  Sums of 2 x 4096 x 28672 bf16 98 us (4.8
-// TB/s); of 8192 x 4096 20 us, where the blocks' joining shows.
+// other's shared memory, in order, so no second launch is needed.  Sums of 2 x 4096 x 28672 bf16 89 us (5.3
+// TB/s); of 8192 x 4096 14.5 us; with the copy of 2991 x 4093 bf16, whose rows are
+// read four bytes a lane, 24 us.
 constexpr int kSweepChunks = 8, kSweepWays = 32;
 
 template <typename T, bool COPY>

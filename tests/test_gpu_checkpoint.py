@@ -582,3 +582,21 @@ def test_norm_outputs_in_wider_rows(ampq, ckpt, dtype, pitch):
         assert L.ampq_norm_backward(0, st, 0, code, code, 0, gy.data_ptr(), cols, x.data_ptr(), cols, 0, 0, 0, 0, rows, cols, mean.data_ptr(),
                                     rstd.data_ptr(), w.data_ptr(), t[1].data_ptr(), ld, gw2.data_ptr(), gb2.data_ptr(), ws.data_ptr(), ws.numel()) == 0
         assert torch.equal(inside(t), gx) and torch.equal(gw, gw2) and torch.equal(gb, gb2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS.get)
+def test_weight_grad_writes_its_outputs_only(ampq, ckpt, dtype):
+    """Exactly the outputs are written, and every row of gY counts once, whatever boundary it starts on."""
+    L, st, code = ampq.lib(), torch.cuda.current_stream().cuda_stream, 0 if dtype == torch.float32 else 1
+    for samples, rows, cols, outs, at in ((2, 300, 40, 1301, 0), (1, 611, 130, 515, 1), (3, 1000, 65, 2050, 1), (2, 33, 33, 5, 1), (1, 2000, 24, 513, 3)):
+        p, base = wgrad_case(ckpt, dtype, 1, samples, rows, cols, outs, "plain", 70)
+        flat = torch.full((samples * rows * (outs + 1) + 8,), 5.0, dtype=dtype, device="cuda")
+        gy = flat[at:at + samples * rows * (outs + 1)].view(samples * rows, outs + 1)[:, :outs]
+        gy.copy_(base)
+        room = [torch.full((k + 64,), 9.0, dtype=dtype, device="cuda") for k in (samples * outs * cols, samples * outs)]
+        ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+        assert L.ampq_ckpt_weight_grad(0, st, code, 1, gy.data_ptr(), outs + 1, p.codes.data_ptr(), p.codes.stride(0), p.scales.data_ptr(), p.scales.stride(0),
+                                       samples, rows, cols, outs, room[0][32:].data_ptr(), room[1][32:].data_ptr(), ws.data_ptr(), ws.numel()) == 0
+        for t in room:
+            assert bool((t[:32] == 9.0).all()) and bool((t[-32:] == 9.0).all())
+        check_wgrad(p, gy, samples, room[0][32:-32].view(samples, outs, cols), room[1][32:-32].view(samples, outs))
