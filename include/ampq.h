@@ -453,7 +453,11 @@ int ampq_ckpt_unpack(int device, void *cuda_stream, int dtype, int fmt, const un
  *   gw      [samples, outs, cols] of `dtype`, contiguous
  *   gb      [samples, outs] of `dtype`, contiguous, or NULL
  * rows = 0 gives zeros.  Products are exact, sums are fp32, one rounding to
- * `dtype` at the end.  The internal waits are bounded: entries not stored when one
+ * `dtype` at the end.  Larger products run on the tensor cores, whose fp32
+ * additions cut instead of rounding to nearest: for fp32 the sum of every 64
+ * tokens, for bf16 of every 4096, is joined to the rest by an addition that
+ * rounds (a bf16 sum of one sign comes out smaller by 2e-5 of itself at most,
+ * where half a step is 2e-3 or more).  The internal waits are bounded: entries not stored when one
  * runs out are NaN.  The workspace of larger products holds x as bf16, the
  * gradient once more where it is fp32 or its rows do not start on 16-byte
  * boundaries, and partial products where there are few outputs and many rows;

@@ -13,9 +13,13 @@
 //
 // fp32 gradients are cut into three bf16 planes, g = g0 + g1 + g2 exactly (24
 // significant bits), and each 64 tokens are multiplied plane by plane, the smallest
-// first.  The tensor core's additions cut instead of rounding: 2.9e-8 per addition,
-// all towards zero, 4e-5 over 8192 tokens.  So the sum of each 64 tokens is taken
-// out of TMEM and added to the rest in registers, rounded to nearest.
+// first.
+//
+// The tensor core's additions cut instead of rounding: 2.9e-8 per addition, all
+// towards zero, 4e-5 over 8192 tokens of one sign and more than half a step of bf16
+// over 2^20.  So the sum of each run of tokens is taken out of TMEM and added to the
+// rest in registers, rounded to nearest: of 64 tokens for fp32, of kRunTokens for
+// bf16, where up to so many tokens are one run.
 //
 // Small products (few tokens, few tiles) are one launch of plain fp32 arithmetic.
 #include "ampq_ckpt.h"
@@ -32,6 +36,12 @@ constexpr int kCtaSide = 128;                 // columns of gY, and of X^, of on
 constexpr int kBoxBytes = kStepRows * 128;    // 64 tokens x 64 bf16
 constexpr int kTileBytes = 2 * kBoxBytes;     // one operand of one stage: 128 x 64 bf16
 constexpr int kStages = 6;
+// Tokens whose sum a bf16 gradient leaves to the tensor core: cut by 2e-5 of a sum of
+// one sign, a hundredth of half a step of the output or less.  A kernel that adds runs
+// up takes longer even where there is one run only (4 x 2048 x 4096 x 4096 268 us
+// against 262, 2 x 4096 x 8192 x 28672 3.20 ms against 3.10; runs of 512 tokens 278 us
+// and 3.44 ms), so it is used where there are several.
+constexpr int kRunTokens = 4096;
 constexpr int kProducerWarp = 0, kMmaWarp = 1, kTmemWarp = 2, kStoreWarp = 4;
 constexpr int kPatch = 32 * 33;               // floats: a 32 x 32 patch of the output on its way out
 
@@ -280,7 +290,7 @@ __device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned
 // 2: one 256 x 256 tile per pair, products issued by the pair's first CTA; each
 // CTA holds 128 columns of both operands and 128 rows of the accumulators.  CG =
 // 1: one 128 x 128 tile per CTA.  Two accumulators, so that one is read while the
-// next is filled: one per tile, or with three planes one per 64 tokens.
+// next is filled: one per tile (RUN = 0) or one per RUN steps of a tile.
 //
 // Barriers, per stage: `loaded` (both operands have landed, in both CTAs of a
 // pair; held by the first), `empty` (the products that read the stage are done).
@@ -296,7 +306,7 @@ __device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned
 // A wait that runs out raises the CTA's flag; its threads then leave their loops,
 // the copies and products in flight are waited for, and what was not stored yet
 // becomes NaN.
-template <int CG, int PLANES, typename OUT>
+template <int CG, int PLANES, int RUN, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap g_map, const __grid_constant__ CUtensorMap x_map, const ProductArgs a) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ alignas(8) unsigned long long s_bars[2 * kStages + 5];
@@ -374,7 +384,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
                 for (int step = p.first_step; step < p.last_step && ok; ++step) {
-                    if (PLANES > 1 || step == p.first_step) {
+                    const int in_run = RUN > 0 ? (step - p.first_step) % RUN : step - p.first_step;
+                    if (in_run == 0) {
                         ok = mbar_wait(drained(acc), acc_parity ^ 1, gave_up);
                         if (!ok) break;
                         fence_tcgen05_after();
@@ -385,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                         if (!ok) break;
                         fence_tcgen05_after();
                         const unsigned long long dg = operand_desc(tiles_g + stage * kTileBytes), dx = operand_desc(tiles_x + stage * kTileBytes);
-                        const bool more = PLANES > 1 ? plane < PLANES - 1 : step > p.first_step;
+                        const bool more = in_run > 0 || plane < PLANES - 1;
 #pragma unroll
                         for (int i = 0; i < kStepRows / 16; ++i)  // 16 tokens: two groups of eight, 2048 bytes
                             tcgen05_mma<CG>(tmem + acc * kSide, dg + i * (2048 >> 4), dx + i * (2048 >> 4), kIdesc, more || i > 0);
@@ -395,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                             parity ^= 1;
                         }
                     }
-                    if (ok && (PLANES > 1 || step + 1 == p.last_step)) {
+                    if (ok && ((RUN > 0 && in_run == RUN - 1) || step + 1 == p.last_step)) {
                         tcgen05_commit<CG>(filled(acc));
                         acc ^= 1;
                         if (acc == 0) acc_parity ^= 1;
@@ -418,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const long long k0 = (long long)p.kt * kSide + rank * kCtaSide + quarter * 32, c0 = (long long)p.ct * kSide + from;
             OUT* row = static_cast<OUT*>(a.out) + (((long long)p.sample * a.splits + p.split) * a.outs + k0 + lane) * a.cols + c0;
             const unsigned lanes = tmem + ((quarter * 32) << 16) + from;
-            if constexpr (PLANES == 1) {
+            if constexpr (RUN == 0) {
                 if (ok) ok = mbar_wait(filled(acc), acc_parity, gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 fence_tcgen05_after();
@@ -444,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 for (int c = 0; c < kCols / 32; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum[c][i] = 0.0f;
-                for (int step = p.first_step; step < p.last_step && ok; ++step) {
+                for (int step = p.first_step; step < p.last_step && ok; step += RUN) {
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait(filled(acc), acc_parity, gave_up));
                     if (!ok) break;
                     fence_tcgen05_after();
@@ -842,15 +853,24 @@ int launch_persistent(ProductKernel kernel, std::atomic<bool>* prepared, int cg,
     return AMPQ_OK;
 }
 
-template <int CG, int PLANES, typename OUT>
+template <int CG, int PLANES, int RUN, typename OUT>
 int launch_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, int device, int sms, cudaStream_t st) {
     static std::atomic<bool> prepared[kMaxDevices];
-    return launch_persistent(product_kernel<CG, PLANES, OUT>, prepared, CG, kThreads, kSmemBytes, g_map, x_map, a, device, sms, st);
+    return launch_persistent(product_kernel<CG, PLANES, RUN, OUT>, prepared, CG, kThreads, kSmemBytes, g_map, x_map, a, device, sms, st);
 }
 
-template <int PLANES, typename OUT>
+template <int PLANES, int RUN, typename OUT>
 int run_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, bool pair, int device, int sms, cudaStream_t st) {
-    return pair ? launch_product<2, PLANES, OUT>(g_map, x_map, a, device, sms, st) : launch_product<1, PLANES, OUT>(g_map, x_map, a, device, sms, st);
+    return pair ? launch_product<2, PLANES, RUN, OUT>(g_map, x_map, a, device, sms, st) : launch_product<1, PLANES, RUN, OUT>(g_map, x_map, a, device, sms, st);
+}
+
+// OUT: the type of gw, or fp32 for partial products.
+template <typename T, typename OUT>
+int choose_product(const CUtensorMap& g_map, const CUtensorMap& x_map, const ProductArgs& a, bool pair, int device, int sms, cudaStream_t st) {
+    constexpr int kRun = kRunTokens / kStepRows;
+    if constexpr (sizeof(T) == 4) return run_product<3, 1, OUT>(g_map, x_map, a, pair, device, sms, st);
+    else if (a.steps_per_split <= kRun) return run_product<1, 0, OUT>(g_map, x_map, a, pair, device, sms, st);
+    else return run_product<1, kRun, OUT>(g_map, x_map, a, pair, device, sms, st);
 }
 
 struct Operands {
@@ -927,8 +947,7 @@ int run_large(const Problem& q, const Plan& p, const Operands& o, int device, in
     a.steps = p.steps;
     a.steps_per_split = p.steps_per_split;
     a.vec = rows_aligned(a.out, q.cols, partial ? AMPQ_F32 : q.dtype);
-    constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
-    rc = partial ? run_product<kPlanes, float>(g_map, x_map, a, p.pair, device, sms, st) : run_product<kPlanes, T>(g_map, x_map, a, p.pair, device, sms, st);
+    rc = partial ? choose_product<T, float>(g_map, x_map, a, p.pair, device, sms, st) : choose_product<T, T>(g_map, x_map, a, p.pair, device, sms, st);
     if (rc || !partial) return rc;
     const long long n = q.outs * q.cols, blocks = (q.samples * n + 255) / 256;
     join_splits_kernel<T><<<(unsigned)(blocks < 8LL * sms ? blocks : 8LL * sms), 256, 0, st>>>(reinterpret_cast<const float*>(o.ws + p.at_part), q.samples, p.splits, n,

@@ -1,0 +1,35 @@
+"""Sums of the weight gradient over very many tokens, against sums in 64 bits."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ckpt(ampq):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2505_13060_b200 import checkpoint
+
+    return checkpoint
+
+
+@pytest.mark.parametrize("outs,cols", [(1280, 2048), (1280, 1024)], ids=["pairs", "single"])
+def test_bf16_sums_of_one_sign(ckpt, outs, cols):
+    """2^20 tokens of one sign in bf16.  The tensor core cuts each addition by up to 2^-23 of the partial sum, always the
+    same way: over all the tokens, which one tile takes here (there are too many tiles to share the token axis), that is
+    more than half a step of bf16 (5e-3).  Taken out every 4096 tokens: at most 4096 cut additions in a run, 256 rounded ones
+    that join the runs (2^-24 each), and half a step, 2^-8, at the end."""
+    rows = 2 ** 20
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    gy = torch.empty(rows, outs, dtype=torch.bfloat16, device="cuda").uniform_(1.0, 2.0, generator=g)
+    gy *= torch.empty(outs, dtype=torch.bfloat16, device="cuda").uniform_(1.0, 2.0, generator=g)
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").uniform_(1.0, 2.0, generator=g)
+    p = ckpt.pack(x)
+    del x
+    gw, _ = ckpt.weight_grad(p, gy)
+    some = ckpt.Packed(p.codes[:, :64], p.scales[:, :2], 64, p.fmt)
+    want = torch.matmul(gy[:, :64].double().T, ckpt.unpack(some, torch.float32).double())
+    off = (gw[0, :64, :64].double() - want).abs() / want
+    assert float(off.max()) <= 2.0 ** -8 + 1.01 * (4096 * 2 * U + 256 * U)
