@@ -92,9 +92,10 @@ __device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatil
     *gave_up = 1;
     return false;
 }
-__device__ __forceinline__ void mbar_drain(unsigned bar, unsigned parity) {
+__device__ __forceinline__ bool mbar_drain(unsigned bar, unsigned parity) {
     for (unsigned i = 0; i < kDrainPolls; ++i)
-        if (mbar_poll(bar, parity, 2000u)) return;
+        if (mbar_poll(bar, parity, 2000u)) return true;
+    return false;
 }
 // Address of the same shared-memory variable in CTA `rank` of the cluster.
 __device__ __forceinline__ unsigned in_cta(unsigned addr, unsigned rank) {
@@ -266,13 +267,18 @@ __device__ __forceinline__ unsigned tmem_alloc(unsigned* where, unsigned warp, u
     return *where;
 }
 
-// The end of every thread of a CTA: no CTA of a pair ends, or gives up its TMEM,
-// while the other still works.
+// All threads of the CTA, or of both CTAs of a pair, meet.
 template <int CG>
-__device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned cols) {
+__device__ __forceinline__ void meet() {
     __syncwarp();
     __syncthreads();
     if (CG == 2) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// The end of every thread of a CTA, after all have met: no CTA of a pair ends, or
+// gives up its TMEM, while the other still works.
+template <int CG>
+__device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned cols) {
     if (warp == kTmemWarp) {
         __syncwarp();
         fence_tcgen05_after();
@@ -283,6 +289,40 @@ __device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
         }
+    }
+}
+
+// Where a producer stands when it ends: the position of its next stage in two turns
+// of the ring, the stages issued (16 bits), and whether a wait of its CTA ran out.
+__device__ __forceinline__ unsigned end_word(unsigned position, unsigned issued, bool gave_up) {
+    return position | (issued & 0xFFFFu) << 8 | (gave_up ? 1u << 31 : 0u);
+}
+
+// Waits, with a limit, for the copies of stages that were loaded and never
+// multiplied.  end[k]: where CTA k's producer stands; one thread of each CTA calls it,
+// after all have met.  The bytes of a pair are counted together, so the CTA that is
+// behind (by kStages at most: stages that were multiplied had come in both) first
+// issues what it lacks, from the operands' first corner; nothing reads it.  The last
+// use of every stage is then waited for: uses before that have been multiplied, and
+// a stage never used passes at once.
+template <int CG>
+__device__ __noinline__ void drain_copies(const unsigned (&end)[2], unsigned rank, unsigned tiles_g, unsigned tiles_x, unsigned loaded, const CUtensorMap* g_map,
+                                          const CUtensorMap* x_map) {
+    const int ahead = CG == 2 ? (short)((end[1] >> 8) - (end[0] >> 8)) : 0;  // of CTA 1
+    const int lacks = min(kStages, rank == 0 ? ahead : -ahead);
+    for (int i = 0; i < lacks; ++i) {
+        const unsigned stage = ((end[rank] & 0xFFu) + i) % kStages, to = stage * kTileBytes, bar = in_cta(loaded + 8 * stage, 0);
+        if (rank == 0) mbar_expect(loaded + 8 * stage, CG * 2 * kTileBytes);
+        for (unsigned half = 0; half < 2; ++half) {
+            tma_load<CG>(tiles_g + to + half * kBoxBytes, g_map, bar, 0, 0, 0, 0);
+            tma_load<CG>(tiles_x + to + half * kBoxBytes, x_map, bar, 0, 0, 0, 0);
+        }
+    }
+    if (rank != 0) return;
+    const unsigned next = end[ahead > 0 ? 1 : 0] & 0xFFu;
+    for (unsigned j = 1; j <= kStages; ++j) {
+        const unsigned at = (next + 2 * kStages - j) % (2 * kStages);
+        if (!mbar_drain(loaded + 8 * (at % kStages), at / kStages)) return;
     }
 }
 
@@ -304,13 +344,16 @@ __device__ __forceinline__ void tmem_free(unsigned tmem, unsigned warp, unsigned
 // the largest size).
 //
 // A wait that runs out raises the CTA's flag; its threads then leave their loops,
-// the copies and products in flight are waited for, and what was not stored yet
-// becomes NaN.
+// what was not stored yet becomes NaN, and the products and copies in flight are
+// waited for, with a limit, before the CTA ends: the products by the warp that issues
+// them, the copies once all threads have met (the producer may have ended by then,
+// with its last stages loaded and never multiplied).
 template <int CG, int PLANES, int RUN, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap g_map, const __grid_constant__ CUtensorMap x_map, const ProductArgs a) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ alignas(8) unsigned long long s_bars[2 * kStages + 5];
-    __shared__ unsigned s_tmem;
+    __shared__ unsigned s_tmem, s_end[2];
+    __shared__ unsigned s_position, s_issued;
     __shared__ int s_gave_up;
     constexpr int kSide = CG * kCtaSide;  // of the tile
     constexpr unsigned kTmemCols = 2 * kSide;
@@ -345,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 
     if (warp == kProducerWarp) {
         if (lane == 0) {
-            unsigned stage = 0, parity = 0;
+            unsigned stage = 0, parity = 0, issued = 0;
             bool ok = true;
             for (long long t = first_tile; t < a.tiles && ok; t += tile_stride) {
                 const TilePos p(a, t);
@@ -362,6 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                         tma_load<CG>(tiles_g + to + kBoxBytes, &g_map, bar, k0 + 64, n0, p.sample, plane);
                         tma_load<CG>(tiles_x + to, &x_map, bar, c0, n0, p.sample, 0);
                         tma_load<CG>(tiles_x + to + kBoxBytes, &x_map, bar, c0 + 64, n0, p.sample, 0);
+                        ++issued;
                         if (++stage == kStages) {
                             stage = 0;
                             parity ^= 1;
@@ -369,11 +413,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     }
                 }
             }
-            // Every stage loaded has been multiplied before the last accumulator is
-            // filled, which the storing warps wait for.  A CTA that gave up does not
-            // know which copies are in flight: it lets a millisecond pass.
-            if (!ok)
-                for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+            s_position = stage + kStages * parity;
+            s_issued = issued;
         }
     } else if (warp == kMmaWarp) {
         if (rank == 0 && lane == 0) {
@@ -483,6 +524,19 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 }
             }
         }
+    }
+    // the CTAs of a pair tell each other how they ended before they meet: the other one's memory is there that long
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const unsigned end = end_word(s_position, s_issued, s_gave_up);
+        s_end[rank] = end;
+        if (CG == 2) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(smem_u32(&s_end[rank]), rank ^ 1)), "r"(end) : "memory");
+    }
+    meet<CG>();
+    if ((s_end[0] | (CG == 2 ? s_end[1] : 0u)) >> 31) {
+        if (threadIdx.x == 0) drain_copies<CG>(s_end, rank, tiles_g, tiles_x, bars, &g_map, &x_map);
+        meet<CG>();
     }
     tmem_free<CG>(tmem, warp, kTmemCols);
 }
