@@ -77,23 +77,49 @@ __device__ __forceinline__ void row_expect(unsigned bar, unsigned bytes) {
 __device__ __forceinline__ void row_copy(unsigned dst, const void* src, unsigned bytes, unsigned bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// Waits for a row, with a limit; false when it runs out.
-__device__ __forceinline__ bool row_wait(unsigned bar, unsigned parity) {
-    for (unsigned i = 0; i < (1u << 22); ++i) {
-        unsigned ok;
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 2000;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (ok) return true;
+template <unsigned HINT_NS>
+__device__ __forceinline__ bool row_poll(unsigned bar, unsigned parity) {
+    unsigned ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "n"(HINT_NS)
+        : "memory");
+    return ok != 0;
+}
+// Polls of a row before a wait gives up.  A test build lets the rows' waits give up at
+// once; the wait that drains copies in flight keeps the full limit.
+constexpr unsigned kDrainPolls = 1u << 22;
+#ifdef AMPQ_TEST_SHORT_WAITS
+constexpr unsigned kRowPolls = 0u, kRowHintNs = 0u;
+#else
+constexpr unsigned kRowPolls = 1u << 22, kRowHintNs = 2000u;
+#endif
+// Waits for a row, with a limit; false when it runs out or the row group has given up
+// (a row that is there is taken all the same).  A thread that missed a row takes none
+// after it: what it would have written becomes NaN, and through the sums that its
+// group shares so do the group's outputs of that row.  The thread that copies goes by
+// its own rows: one that it has seen has left its place; once it missed one it starts
+// no more copies and waits for those in flight.
+__device__ __forceinline__ bool row_wait(unsigned bar, unsigned parity, volatile int* gave_up) {
+    if (row_poll<kRowHintNs>(bar, parity)) return true;
+    for (unsigned i = 0; i < kRowPolls; ++i) {
+        if (*gave_up) return false;
+        if (row_poll<kRowHintNs>(bar, parity)) return true;
     }
+    *gave_up = 1;
     return false;
 }
+__device__ __forceinline__ bool row_drain(unsigned bar, unsigned parity) {
+    for (unsigned i = 0; i < kDrainPolls; ++i)
+        if (row_poll<2000u>(bar, parity)) return true;
+    return false;
+}
+constexpr unsigned kNanBits = 0x7FC00000u;
 
 __device__ __forceinline__ uint4 take16(unsigned src) {
     uint4 v;
@@ -185,7 +211,9 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
     __shared__ float red[2][2][S::kWarps];
     __shared__ alignas(16) unsigned char s_scratch[S::kWarps][1040];
     __shared__ alignas(8) unsigned long long s_bars[2 * S::kGroups];
+    __shared__ int s_gave_up[S::kGroups];
     const int warp = threadIdx.x / 32, group = warp / WPR;
+    volatile int* gave_up = s_gave_up + group;
     const int t = threadIdx.x % (32 * WPR);
     const unsigned lane = threadIdx.x % 32;
     const long long stride = (long long)gridDim.x * S::kGroups, first = (long long)blockIdx.x * S::kGroups + group;
@@ -200,6 +228,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
         if (t == 0) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8) : "memory");
+            *gave_up = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -210,11 +239,15 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
     }
     const float inv_cols = 1.0f / (float)a.cols;
     int taken = 0;  // rows of this group so far
+    bool late = false;  // this thread missed a row
     for (long long row0 = (long long)blockIdx.x * S::kGroups; row0 < a.rows; row0 += stride, ++taken) {
         const long long row = row0 + group;
         const bool live = row < a.rows;
         const int slot = taken & 1;
-        const bool here = !a.bulk || !live || row_wait(bars + 8 * slot, (taken >> 1) & 1);
+        if (a.bulk && live && !late && !row_wait(bars + 8 * slot, (taken >> 1) & 1, gave_up)) {
+            late = true;
+            if (t == 0 && row_drain(bars + 8 * slot, (taken >> 1) & 1) && row + stride < a.rows) row_drain(bars + 8 * (slot ^ 1), ((taken + 1) >> 1) & 1);
+        }
         K k[V];
         int n[V];
 #pragma unroll
@@ -226,6 +259,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
                 unsigned w[8];
                 take_words(slots + slot * Ring::kRow + (j * 32 * WPR + t) * 32, lane, w);
                 if (n[j] > 0) k[j].from_words(w);
+                if (late) k[j].v[0].x = __uint_as_float(kNanBits);  // and so the row's sums and the checkpoint's group
             } else if (n[j] > 0) {
                 k[j].load(static_cast<const T*>(a.x) + row * a.ld_x + c0, n[j]);
             }
@@ -267,8 +301,8 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, ForwardRing<T, WPR
         row_sum<WPR, 1>(q, red[slot][1], warp);
         // every thread of the group has read its part of the row: its place takes the row after the next
         if (WPR == 1) __syncwarp();
-        if (a.bulk && t == 0 && row + 2 * stride < a.rows) begin_copy(row + 2 * stride, slot);
-        const float rstd = here ? 1.0f / sqrtf(q[0] * inv_cols + a.eps) : __uint_as_float(0x7FC00000u);
+        if (a.bulk && t == 0 && !late && row + 2 * stride < a.rows) begin_copy(row + 2 * stride, slot);
+        const float rstd = 1.0f / sqrtf(q[0] * inv_cols + a.eps);
         if (live && t == 0) {
             if (LAYER) a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -478,6 +512,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float red[2][S::kWarps * 2];
     __shared__ alignas(8) unsigned long long s_bars[4 * S::kGroups];
+    __shared__ int s_gave_up[S::kGroups];
     const int warp = threadIdx.x / 32;
     const int t = threadIdx.x % (32 * WPR);
     const int group = warp / WPR;
@@ -505,9 +540,11 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     const unsigned row_codes = base + kAhead * kGyRow + group * (WPR * 512 * WIDE);
     const unsigned row_scales = base + kAhead * (kRowBytes<T, KEPT, WPR, WIDE> - S::kWarps * 16 * WIDE) + group * (WPR * 16 * WIDE);
     const unsigned bars = (unsigned)__cvta_generic_to_shared(s_bars) + 8 * group;
+    volatile int* gave_up = s_gave_up + group;
+    bool late = false;  // this thread missed a row
     auto copy_whole = [&](long long row, int slot) {
         if (row < a.rows) {
-            if (t == 0) {
+            if (t == 0 && !late) {
                 const unsigned bar = bars + 8 * S::kGroups * slot, bytes = (unsigned)a.cols * (unsigned)sizeof(T);
                 row_expect(bar, KEPT ? bytes + (unsigned)groups * (kGroup + 1) : 2 * bytes);
                 row_copy(row_gy + slot * kGyRow, static_cast<const T*>(a.gy) + row * a.ld_gy, bytes, bar);
@@ -550,6 +587,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     if (whole) {
         if (t == 0) {
             for (int s = 0; s < kAhead; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * S::kGroups * s) : "memory");
+            *gave_up = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -579,7 +617,13 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
         if (kAhead > 0 && !whole) copy_any(row + (kAhead - 1) * stride, slot == 0 ? kAhead - 1 : slot - 1);
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead > 0 ? kAhead - 1 : 0) : "memory");
         __syncwarp();
-        const bool here = !whole || !live || row_wait(bars + 8 * S::kGroups * slot, lap);
+        if (whole && live && !late && !row_wait(bars + 8 * S::kGroups * slot, lap, gave_up)) {
+            late = true;
+            for (int s = 0; t == 0 && s < kAhead && row + s * stride < a.rows; ++s) {  // the copies of this row and the next ones
+                const bool wraps = slot + s >= kAhead;
+                if (!row_drain(bars + 8 * S::kGroups * (slot + s - (wraps ? kAhead : 0)), wraps ? lap ^ 1 : lap)) break;
+            }
+        }
         float mean = 0.0f, rstd = 0.0f, p[V];
         if (live) {
             if (kAhead > 0) {
@@ -603,7 +647,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 rstd = __ldg(a.rstd + row);
                 if (LAYER) mean = __ldg(a.mean + row);
             }
-            if (!here) rstd = __uint_as_float(0x7FC00000u);
+            if (late) rstd = __uint_as_float(kNanBits);
         }
         K g[V], h[kTwice ? 1 : V];                 // gy * weight; (x - mean) * rstd, or
         unsigned xr[V][KEPT ? E / 4 : 8];          // the codes or words of x to form it again
@@ -673,7 +717,7 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
                 if (LAYER) c1 = __fadd2_rn(c1, g[j].v[i]);
             }
         }
-        float both[2] = {c2.x + c2.y, c1.x + c1.y};
+        float both[2] = {late ? __uint_as_float(kNanBits) : c2.x + c2.y, c1.x + c1.y};
         if (LAYER) {
             row_sum<WPR, 2>(both, red[phase], warp);
         } else {
@@ -719,6 +763,11 @@ __global__ void __launch_bounds__(Shape<WPR, WIDE>::kThreads, Shape<WPR, WIDE>::
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.part) return;
+    if (LAYER && late)  // sum_w is NaN already
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) sum_b[j][i] = make_float2(__uint_as_float(kNanBits), __uint_as_float(kNanBits));
     float* join = reinterpret_cast<float*>(ring);
     for (int k = 0; k < (LAYER && a.sum_b ? 2 : 1); ++k) {
         float* out = a.part + ((long long)k * gridDim.x + blockIdx.x) * a.part_pitch;

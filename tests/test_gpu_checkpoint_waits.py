@@ -43,6 +43,53 @@ def weight_gradients():
     print("gave up", gave_up)
 
 
+def norms():
+    """Rows that come by bulk copies, many to a group.  A row that a warp of its group missed has NaN outputs, and its
+    checkpoint decodes to NaN or is right; the other rows are those of the same kernel fed by loads (rows off the 16-byte
+    boundaries)."""
+    import torch
+
+    from paper_2505_13060_b200 import checkpoint as ckpt
+
+    def odd(t):
+        full = torch.empty(t.shape[0], t.shape[1] + 3, dtype=t.dtype, device="cuda")
+        full[:, 1:-2] = t
+        return full[:, 1:-2]
+
+    gave_up = 0
+    for dtype in (torch.bfloat16, torch.float32):
+        for rows, cols in ((40000, 512), (20001, 1024), (9000, 4096), (5000, 5120), (3000, 8192), (2000, 16384)):
+            g = torch.Generator(device="cuda").manual_seed(cols)
+            x, gy = (torch.randn(rows, cols, device="cuda", generator=g).to(dtype) for _ in range(2))
+            w = torch.rand(cols, device="cuda", generator=g).to(dtype)
+            for kind in (0, 1):
+                y, mean, rstd, p = ckpt.norm_forward(x, w, None, 1e-5, kind, 1)
+                y2, mean2, rstd2, p2 = ckpt.norm_forward(odd(x), w, None, 1e-5, kind, 1)
+                lost = torch.isnan(rstd)
+                gave_up += int(lost.any())
+                assert torch.equal(torch.isnan(y), lost[:, None].expand_as(y))
+                codes, codes2 = p.codes.view(rows, -1, 32), p2.codes.view(rows, -1, 32)
+                right = (p.scales == p2.scales) & (codes == codes2).all(2)
+                assert bool((right | ((p.scales == 255) & (codes == 0).all(2) & lost[:, None])).all())
+                kept = ~lost
+                for a, b in ((y, y2), (rstd, rstd2)) + (((mean, mean2),) if kind == 0 else ()):
+                    assert torch.equal(a[kept], b[kept]), (dtype, rows, cols, kind)
+                if kind == 0:
+                    assert torch.equal(torch.isnan(mean), lost)
+                for base in (p2, x):
+                    if base is x and dtype == torch.float32 and cols > 8192:
+                        continue   # rows are read as they come
+                    gx, gw, gb = ckpt.norm_backward(gy, base, mean2, rstd2, w, kind)
+                    gx2, gw2, gb2 = ckpt.norm_backward(odd(gy), base, mean2, rstd2, w, kind)
+                    lost = torch.isnan(gx).any(1)
+                    gave_up += int(lost.any())
+                    assert bool(torch.isnan(gx[lost]).all()) and torch.equal(gx[~lost], gx2[~lost])
+                    for a, b in ((gw, gw2), (gb, gb2)) if kind == 0 else ((gw, gw2),):
+                        assert bool((torch.isnan(a) | (a == b)).all())
+    assert gave_up, "no wait ran out"
+    print("gave up", gave_up)
+
+
 @pytest.fixture(scope="module")
 def short_waits(tmp_path_factory):
     from paper_2505_13060_b200 import build
@@ -50,7 +97,7 @@ def short_waits(tmp_path_factory):
     return build.build(out=str(tmp_path_factory.mktemp("short") / "libampq_short.so"), defines=["AMPQ_TEST_SHORT_WAITS"])
 
 
-@pytest.mark.parametrize("what", ["weight_gradients"])
+@pytest.mark.parametrize("what", ["weight_gradients", "norms"])
 def test_waits_that_run_out(short_waits, what):
     r = subprocess.run([sys.executable, os.path.abspath(__file__), what], env=dict(os.environ, AMPQ_LIBRARY=short_waits), capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout + r.stderr
