@@ -184,7 +184,8 @@ class Calibrator:
                         return plain(x)
                     if isinstance(m, torch.nn.LayerNorm):
                         return ckpt.layer_norm(x, m.weight, m.bias, m.eps, fmt)
-                    return ckpt.rms_norm(x, m.weight, torch.finfo(x.dtype).eps if m.eps is None else m.eps, fmt)
+                    # without an eps of its own the module takes that of fp32, in which it computes, whatever x's type
+                    return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt)
 
                 self._replace(m, norm)
 

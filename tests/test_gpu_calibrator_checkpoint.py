@@ -1,0 +1,54 @@
+"""A calibration with 8-bit checkpoints runs the model it is given: the same forward pass but for the norms' last rounding,
+every layer scored or the call refused, and model and context left as they were."""
+import contextlib
+
+import pytest
+import torch
+
+import ckpt_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hooks(ampq):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2505_13060_b200 import hooks
+
+    return hooks
+
+
+@pytest.fixture
+def ctx(ampq):
+    c = ampq.Context(0, torch.cuda.current_stream().cuda_stream)
+    c.set_formats([0, 1])
+    yield c
+    c.destroy()
+
+
+@contextlib.contextmanager
+def one_sample(hooks, ctx, net, fmt=1):
+    cal = hooks.Calibrator(ctx, net, 1, checkpoint=fmt)
+    cal.begin()
+    with cal.sample(0):
+        yield cal
+    cal.result = cal.end()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("affine", [True, False])
+def test_rms_norm_of_default_eps(hooks, ctx, dtype, affine):
+    """torch computes an RMSNorm without eps in fp32 with fp32's eps, whatever the input's type.  Values around 0.01 show
+    which eps was used: bf16's own is as large as their square's root.  Both sides round an fp32 result once, off by half a
+    step each; the fp32 results themselves agree to far less than a hundredth of a bf16 step, and to 2^-20 in fp32."""
+    torch.manual_seed(1)
+    norm = torch.nn.RMSNorm(192, elementwise_affine=affine).cuda().to(dtype)
+    net = torch.nn.Sequential(norm, torch.nn.Linear(192, 8)).cuda().to(dtype)
+    x = (torch.randn(40, 192, device="cuda") * 0.01).to(dtype)
+    want = norm(x).double()
+    with one_sample(hooks, ctx, net):
+        got = norm(x).double()
+        net(x).float().square().sum().backward()
+    step = 2.0 ** -7 * 1.01 if dtype == torch.bfloat16 else 2.0 ** -20
+    assert bool(((got - want).abs() <= step * want.abs()).all())
