@@ -18,7 +18,8 @@ pending.  Everything the method computes happens in the CUDA library; this
 module only moves pointers.
 
 With ``checkpoint=FMT_E4M3`` (or ``FMT_E5M2``) the calibration keeps the inputs of
-the linear layers and of ``torch.nn.LayerNorm`` and ``torch.nn.RMSNorm`` modules in
+the linear layers and of ``torch.nn.LayerNorm`` and ``torch.nn.RMSNorm`` modules
+(those with a forward of their own apart, which run as without checkpoints) in
 8 bits between the forward and the backward pass -- the memory that calibration
 needs beyond the model (Sec. 1) -- and forms the sample's weight gradients and the
 norms' gradients from there (``checkpoint``).  What is scored is what the backward
@@ -158,6 +159,12 @@ class Calibrator:
         self._keep += [x, gx, w, gw]
 
     # -- 8-bit checkpoints ------------------------------------------------------
+    @staticmethod
+    def _plain(module, base) -> bool:
+        """Whether a module computes what its base class does: subclasses with a forward of their own and modules that
+        somebody has wrapped already run as they are."""
+        return isinstance(module, base) and type(module).forward is base.forward and "forward" not in module.__dict__
+
     def _replace(self, module, forward):
         self._replaced.append((module, module.__dict__.get("forward")))
         module.forward = forward
@@ -170,14 +177,14 @@ class Calibrator:
             return self._r is not None and torch.is_grad_enabled() and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16)
 
         for idx, (_, m) in enumerate(self.modules):
-            if isinstance(m, torch.nn.Linear):
+            if self._plain(m, torch.nn.Linear):
 
                 def linear(x, m=m, idx=idx, plain=m.forward):
                     return _ScoredLinear.apply(x, m.weight, m.bias, self, idx) if active(x) else plain(x)
 
                 self._replace(m, linear)
         for m in self.model.modules():
-            if isinstance(m, (torch.nn.LayerNorm, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
+            if (self._plain(m, torch.nn.LayerNorm) or self._plain(m, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
 
                 def norm(x, m=m, plain=m.forward):
                     if not active(x):
@@ -194,8 +201,9 @@ class Calibrator:
         if self.checkpoint != ampq.FMT_BASE:
             self.ctx.set_measured(False)
             self._use_checkpoints()
+        replaced = {m for m, _ in self._replaced}
         for idx, (_, m) in enumerate(self.modules):
-            if self._replaced and isinstance(m, torch.nn.Linear):
+            if m in replaced:
                 continue
             self._handles.append(m.register_forward_hook(self._fwd(idx)))
             self._handles.append(m.register_full_backward_hook(self._bwd(idx)))

@@ -52,3 +52,44 @@ def test_rms_norm_of_default_eps(hooks, ctx, dtype, affine):
         net(x).float().square().sum().backward()
     step = 2.0 ** -7 * 1.01 if dtype == torch.bfloat16 else 2.0 ** -20
     assert bool(((got - want).abs() <= step * want.abs()).all())
+
+
+class Norm2d(torch.nn.LayerNorm):
+    """A norm over the channels of [batch, channels, ...]."""
+
+    def forward(self, x):
+        return super().forward(x.transpose(1, -1)).transpose(1, -1)
+
+
+class Doubled(torch.nn.Linear):
+    """A linear layer with something beside its product."""
+
+    def forward(self, x):
+        return 2.0 * super().forward(x) + x.sum()
+
+
+class Shifted(torch.nn.RMSNorm):
+    def forward(self, x):
+        return super().forward(x + 1.0)
+
+
+@pytest.mark.parametrize("which", ["norm", "linear", "rms", "wrapped"])
+def test_modules_with_a_forward_of_their_own(hooks, ctx, which):
+    """Subclasses that do more than their base, and modules that somebody has wrapped already, run as they are; their
+    linear layers are scored all the same."""
+    torch.manual_seed(2)
+    net = torch.nn.Sequential(Doubled(24, 24) if which == "linear" else torch.nn.Linear(24, 24),
+                              {"norm": Norm2d(6), "rms": Shifted(24)}.get(which, torch.nn.LayerNorm(24)), torch.nn.Linear(24, 8)).cuda()
+    if which == "wrapped":
+        plain = net[0].forward
+        net[0].forward = lambda x: plain(x) * 3.0
+        mine = net[0].forward
+    x = torch.randn(2, 6, 24, device="cuda")
+    want = net(x).detach()
+    with one_sample(hooks, ctx, net) as cal:
+        y = net(x)
+        y.square().sum().backward()
+    # a norm of the library instead of torch's: some roundings of fp32 apart
+    assert bool(((y - want).abs() <= 1e-5 * want.abs().max()).all())
+    assert len(cal.result) == 2 and all(r["s_mean"] > 0 for r in cal.result)
+    assert net[0].__dict__.get("forward") is (mine if which == "wrapped" else None)
