@@ -179,22 +179,21 @@ class Calibrator:
         for idx, (_, m) in enumerate(self.modules):
             if self._plain(m, torch.nn.Linear):
 
-                def linear(x, m=m, idx=idx, plain=m.forward):
-                    return _ScoredLinear.apply(x, m.weight, m.bias, self, idx) if active(x) else plain(x)
+                def linear(input, m=m, idx=idx, plain=m.forward):   # the module's own name for its argument
+                    return _ScoredLinear.apply(input, m.weight, m.bias, self, idx) if active(input) else plain(input)
 
                 self._replace(m, linear)
         for m in self.model.modules():
             if (self._plain(m, torch.nn.LayerNorm) or self._plain(m, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
 
-                def norm(x, m=m, plain=m.forward):
-                    if not active(x):
-                        return plain(x)
-                    if isinstance(m, torch.nn.LayerNorm):
-                        return ckpt.layer_norm(x, m.weight, m.bias, m.eps, fmt)
-                    # without an eps of its own the module takes that of fp32, in which it computes, whatever x's type
-                    return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt)
+                def layer_norm(input, m=m, plain=m.forward):
+                    return ckpt.layer_norm(input, m.weight, m.bias, m.eps, fmt) if active(input) else plain(input)
 
-                self._replace(m, norm)
+                def rms_norm(x, m=m, plain=m.forward):
+                    # without an eps of its own the module takes that of fp32, in which it computes, whatever x's type
+                    return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt) if active(x) else plain(x)
+
+                self._replace(m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm)
 
     def begin(self):
         self._handles = []

@@ -93,3 +93,13 @@ def test_modules_with_a_forward_of_their_own(hooks, ctx, which):
     assert bool(((y - want).abs() <= 1e-5 * want.abs().max()).all())
     assert len(cal.result) == 2 and all(r["s_mean"] > 0 for r in cal.result)
     assert net[0].__dict__.get("forward") is (mine if which == "wrapped" else None)
+
+
+def test_arguments_by_name(hooks, ctx):
+    """Linear and LayerNorm call their argument `input`, RMSNorm `x`: all three are called by name as without checkpoints."""
+    lin, ln, rms = torch.nn.Linear(32, 32).cuda(), torch.nn.LayerNorm(32).cuda(), torch.nn.RMSNorm(32).cuda()
+    net = torch.nn.ModuleList([lin, ln, rms])
+    x = torch.randn(5, 32, device="cuda")
+    with one_sample(hooks, ctx, net) as cal:
+        rms(x=ln(input=lin(input=x))).square().sum().backward()
+    assert cal.result[0]["s_mean"] > 0
