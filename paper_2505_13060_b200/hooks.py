@@ -58,7 +58,7 @@ class _ScoredLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, calibrator, idx):
         y = torch.nn.functional.linear(x, weight, bias)
-        p = ckpt.pack(x.detach(), calibrator.checkpoint)
+        p = ckpt.pack(x.detach(), calibrator.checkpoint)   # refuses what cannot be kept: a layer is not left out silently
         ctx.save_for_backward(weight, p.codes, p.scales)
         ctx.x_shape, ctx.calibrator, ctx.idx, ctx.r = x.shape, calibrator, idx, calibrator._r
         return y
@@ -173,14 +173,17 @@ class Calibrator:
         """Sends the linear layers and norms through the calls that keep their input in 8 bits."""
         fmt = self.checkpoint
 
+        def scored():
+            return self._r is not None and torch.is_grad_enabled()
+
         def active(x):
-            return self._r is not None and torch.is_grad_enabled() and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16)
+            return scored() and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16)
 
         for idx, (_, m) in enumerate(self.modules):
             if self._plain(m, torch.nn.Linear):
 
                 def linear(input, m=m, idx=idx, plain=m.forward):   # the module's own name for its argument
-                    return _ScoredLinear.apply(input, m.weight, m.bias, self, idx) if active(input) else plain(input)
+                    return _ScoredLinear.apply(input, m.weight, m.bias, self, idx) if scored() else plain(input)
 
                 self._replace(m, linear)
         for m in self.model.modules():

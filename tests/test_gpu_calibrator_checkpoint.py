@@ -103,3 +103,13 @@ def test_arguments_by_name(hooks, ctx):
     with one_sample(hooks, ctx, net) as cal:
         rms(x=ln(input=lin(input=x))).square().sum().backward()
     assert cal.result[0]["s_mean"] > 0
+
+
+def test_types_that_cannot_be_kept_are_refused(hooks, ctx):
+    """A layer that cannot be scored raises, as it does without checkpoints; it is not left out of the result silently."""
+    net = torch.nn.Sequential(torch.nn.Linear(32, 8)).cuda().half()
+    cal = hooks.Calibrator(ctx, net, 1, checkpoint=1)
+    cal.begin()
+    with pytest.raises(TypeError), cal.sample(0):
+        net(torch.randn(4, 32, device="cuda").half()).float().square().sum().backward()
+    cal.end()
