@@ -176,8 +176,12 @@ class Calibrator:
         def scored():
             return self._r is not None and torch.is_grad_enabled()
 
-        def active(x):
-            return scored() and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16)
+        types = (torch.float32, torch.bfloat16)
+
+        def known(x, m):   # a norm that the library has; torch runs the others, or says what is wrong with them
+            params = [t for t in (m.weight, getattr(m, "bias", None)) if t is not None]
+            return (scored() and x.is_cuda and x.dtype in types and x.shape[-1:] == m.normalized_shape
+                    and all(t.device == x.device and t.dtype in types and t.dtype == params[0].dtype for t in params))
 
         for idx, (_, m) in enumerate(self.modules):
             if self._plain(m, torch.nn.Linear):
@@ -190,11 +194,11 @@ class Calibrator:
             if (self._plain(m, torch.nn.LayerNorm) or self._plain(m, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
 
                 def layer_norm(input, m=m, plain=m.forward):
-                    return ckpt.layer_norm(input, m.weight, m.bias, m.eps, fmt) if active(input) else plain(input)
+                    return ckpt.layer_norm(input, m.weight, m.bias, m.eps, fmt) if known(input, m) else plain(input)
 
                 def rms_norm(x, m=m, plain=m.forward):
                     # without an eps of its own the module takes that of fp32, in which it computes, whatever x's type
-                    return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt) if active(x) else plain(x)
+                    return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt) if known(x, m) else plain(x)
 
                 self._replace(m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm)
 

@@ -113,3 +113,14 @@ def test_types_that_cannot_be_kept_are_refused(hooks, ctx):
     with pytest.raises(TypeError), cal.sample(0):
         net(torch.randn(4, 32, device="cuda").half()).float().square().sum().backward()
     cal.end()
+
+
+def test_norms_that_the_library_does_not_have_run_plain(hooks, ctx):
+    """fp16 parameters and inputs of another width: what torch does, its own error included."""
+    ln = torch.nn.LayerNorm(32, elementwise_affine=False).cuda()
+    net = torch.nn.ModuleList([ln, torch.nn.LayerNorm(32).cuda().half(), torch.nn.Linear(4, 4).cuda()])
+    x = torch.randn(3, 32, device="cuda")
+    with one_sample(hooks, ctx, net):
+        with pytest.raises(RuntimeError):
+            ln(torch.randn(3, 64, device="cuda"))
+        assert torch.equal(net[1](x.half()), torch.nn.functional.layer_norm(x.half(), (32,), net[1].weight, net[1].bias))
