@@ -72,6 +72,9 @@ class _ScoredLinear(torch.autograd.Function):
         gx = torch.matmul(gy, weight)
         gw, gb = ckpt.weight_grad(p, gy, bias=need_b)
         if cal._r is not None:
+            if ctx.idx in cal._done:
+                raise RuntimeError("layer %s was used twice in sample %d: it has one pair of operands" % (cal.modules[ctx.idx][0], ctx.r))
+            cal._done.add(ctx.idx)
             cal._stream_linear(ctx.idx, ctx.r, ckpt.unpack(p, weight.dtype), gx, weight.detach(), gw[0])
         return gx if need_x else None, gw[0] if need_w else None, gb[0] if need_b else None, None, None
 
@@ -92,6 +95,7 @@ class Calibrator:
                 self.layer_ids.append(ctx.register_layer(ampq.BGEMM, name, R))
         self._r = None
         self._x = {}
+        self._done = set()   # layers with a checkpoint that were streamed in the current sample
         self._keep = []      # tensors the library borrowed during the current sample
         self._pending = []   # (event on the context's stream, tensors) of earlier samples
         self._handles = []
@@ -224,6 +228,7 @@ class Calibrator:
         finally:
             self._r = None
             self._x.clear()
+            self._done.clear()
             self._release_sample()
 
     def end(self):

@@ -124,3 +124,17 @@ def test_norms_that_the_library_does_not_have_run_plain(hooks, ctx):
         with pytest.raises(RuntimeError):
             ln(torch.randn(3, 64, device="cuda"))
         assert torch.equal(net[1](x.half()), torch.nn.functional.layer_norm(x.half(), (32,), net[1].weight, net[1].bias))
+
+
+def test_a_layer_that_runs_twice_is_refused(hooks, ctx):
+    """One sample of a layer has one pair of operands: a layer that is used twice raises, as without checkpoints, instead of
+    keeping the last use only."""
+    lin = torch.nn.Linear(16, 16).cuda()
+    for fmt in (0, 1):
+        cal = hooks.Calibrator(ctx, lin, 1, checkpoint=fmt)
+        cal.begin()
+        with pytest.raises((KeyError, RuntimeError)), cal.sample(0):
+            lin(lin(torch.randn(4, 16, device="cuda"))).square().sum().backward()
+        with cal.sample(0):   # the sample again, used once
+            lin(torch.randn(4, 16, device="cuda")).square().sum().backward()
+        assert cal.end()[0]["s_mean"] > 0
