@@ -258,6 +258,8 @@ class Context:
             raise AmpqError(rc, "ampq_create")
         self.F = 2
         self._R = {}
+        self.measured = True          # what set_measured says
+        self._measured_after = None   # what it said before a pass that has a setting of its own
         self.device, self.stream = device, stream   # the cudaStream_t handle every call of this context runs on
 
     def _check(self, rc: int):
@@ -300,6 +302,21 @@ class Context:
 
     def set_measured(self, on: bool):
         self._check(lib().ampq_set_measured(self._h, 1 if on else 0))
+        self.measured, self._measured_after = bool(on), None
+
+    def _settle(self):
+        """Before a new pass: puts back the setting that the last one had replaced.  (Not at that pass's end: the
+        results would go with it.)"""
+        before = self._measured_after
+        if before is None:
+            return
+        try:
+            self.set_measured(before)
+        except AmpqError as e:
+            if e.status != ERR_STATE:
+                raise
+            self.stream_end()   # that pass was never ended
+            self.set_measured(before)
 
     def set_sharing(self, on: bool):
         self._check(lib().ampq_set_sharing(self._h, 1 if on else 0))
@@ -308,6 +325,7 @@ class Context:
         self._check(lib().ampq_set_scale_mode(self._h, mode))
 
     def measure_amax(self):
+        self._settle()
         self._check(lib().ampq_measure_amax(self._h))
 
     def get_amax(self, layer_id: int) -> np.ndarray:
@@ -316,9 +334,16 @@ class Context:
         return out
 
     def score(self):
+        self._settle()
         self._check(lib().ampq_score(self._h))
 
-    def stream_begin(self):
+    def stream_begin(self, measured=None):
+        """``measured``: a ``set_measured`` for this pass alone."""
+        self._settle()
+        if measured is not None and bool(measured) != self.measured:
+            before = self.measured
+            self.set_measured(measured)
+            self._measured_after = before
         self._check(lib().ampq_stream_begin(self._h))
 
     def stream_sample(self, layer_id: int, operand: int, r: int, dtype: int, values_ptr: int, grads_ptr: int,

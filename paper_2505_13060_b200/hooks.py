@@ -26,8 +26,8 @@ norms' gradients from there (``checkpoint``).  What is scored is what the backwa
 pass has: the decoded inputs, each off by at most half a step of the format
 (2^-4 relative in E4M3), so the model's term S of an operand is off by at most
 13 %, on average by about the format's noise constant.  The measured term of a
-tensor that was already rounded says nothing, so the context is switched to the
-model's term alone (``set_measured(False)``).
+tensor that was already rounded says nothing, so the pass scores the model's term
+alone (``set_measured(False)``; the context's next pass has its own setting again).
 
 ``quantised(...)`` runs the model with chosen layers' inputs and weights replaced
 by their FP8-rounded values (``ampq_fake_quant``), which is how the predicted
@@ -84,7 +84,7 @@ class Calibrator:
         if checkpoint not in (ampq.FMT_BASE, ampq.FMT_E4M3, ampq.FMT_E5M2):
             raise ValueError("checkpoint is FMT_BASE (inputs kept in full), FMT_E4M3 or FMT_E5M2")
         self.ctx, self.model, self.R, self.checkpoint = ctx, model, R, checkpoint
-        self._replaced = []   # (module, its own forward attribute if it had one)
+        self._replaced = []   # (module, the forward that keeps its input in 8 bits), in place while a sample runs
         self.modules, self.layer_ids = [], []
         for name, m in model.named_modules():
             if isinstance(m, torch.nn.Linear):
@@ -169,13 +169,10 @@ class Calibrator:
         somebody has wrapped already run as they are."""
         return isinstance(module, base) and type(module).forward is base.forward and "forward" not in module.__dict__
 
-    def _replace(self, module, forward):
-        self._replaced.append((module, module.__dict__.get("forward")))
-        module.forward = forward
-
-    def _use_checkpoints(self):
-        """Sends the linear layers and norms through the calls that keep their input in 8 bits."""
+    def _find_replaced(self):
+        """The linear layers and norms that go through the calls that keep their input in 8 bits."""
         fmt = self.checkpoint
+        self._replaced = []
 
         def scored():
             return self._r is not None and torch.is_grad_enabled()
@@ -193,7 +190,7 @@ class Calibrator:
                 def linear(input, m=m, idx=idx, plain=m.forward):   # the module's own name for its argument
                     return _ScoredLinear.apply(input, m.weight, m.bias, self, idx) if scored() else plain(input)
 
-                self._replace(m, linear)
+                self._replaced.append((m, linear))
         for m in self.model.modules():
             if (self._plain(m, torch.nn.LayerNorm) or self._plain(m, torch.nn.RMSNorm)) and len(m.normalized_shape) == 1 and m.normalized_shape[0] <= ampq.NORM_MAX_COLS:
 
@@ -204,47 +201,51 @@ class Calibrator:
                     # without an eps of its own the module takes that of fp32, in which it computes, whatever x's type
                     return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt) if known(x, m) else plain(x)
 
-                self._replace(m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm)
+                self._replaced.append((m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm))
+
+    def _remove_hooks(self):
+        for h in self._handles:
+            h.remove()
+        self._handles = []
 
     def begin(self):
-        self._handles = []
+        self._remove_hooks()   # of a pass that was never ended
         if self.checkpoint != ampq.FMT_BASE:
-            self.ctx.set_measured(False)
-            self._use_checkpoints()
+            self._find_replaced()
         replaced = {m for m, _ in self._replaced}
         for idx, (_, m) in enumerate(self.modules):
             if m in replaced:
                 continue
             self._handles.append(m.register_forward_hook(self._fwd(idx)))
             self._handles.append(m.register_full_backward_hook(self._bwd(idx)))
-        self.ctx.stream_begin()
+        self.ctx.stream_begin(measured=None if self.checkpoint == ampq.FMT_BASE else False)
 
     @contextlib.contextmanager
     def sample(self, r: int):
         """Run one sample's forward and backward inside this block."""
+        for m, _ in self._replaced:
+            if "forward" in m.__dict__:
+                raise RuntimeError("a module's forward was replaced after begin()")
         self._r = r
         try:
+            for m, forward in self._replaced:
+                m.forward = forward
             yield
         finally:
+            for m, _ in self._replaced:
+                m.__dict__.pop("forward", None)   # the class's again
             self._r = None
             self._x.clear()
             self._done.clear()
             self._release_sample()
 
     def end(self):
+        self._remove_hooks()
+        self._replaced = []
         self.ctx.stream_end()
         res = [self.ctx.get_layer(lid) for lid in self.layer_ids]   # synchronises: the borrowed tensors are free
         self._keep = []
         self._pending = []
-        for h in self._handles:
-            h.remove()
-        self._handles = []
-        for m, own in self._replaced:
-            if own is None:
-                del m.forward   # the class's again
-            else:
-                m.forward = own
-        self._replaced = []
         return res
 
     # -- running the model in a low-precision configuration --------------------

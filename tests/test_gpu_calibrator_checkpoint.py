@@ -138,3 +138,69 @@ def test_a_layer_that_runs_twice_is_refused(hooks, ctx):
         with cal.sample(0):   # the sample again, used once
             lin(torch.randn(4, 16, device="cuda")).square().sum().backward()
         assert cal.end()[0]["s_mean"] > 0
+
+
+def scored(cal, net, x, r=0):
+    with cal.sample(r):
+        net(x).square().sum().backward()
+
+
+@pytest.mark.parametrize("how", ["ended", "raised", "dropped", "off"])
+def test_the_context_and_the_model_are_left_as_they_were(hooks, ctx, how):
+    """After a calibration with checkpoints the context scores the terms it scored before, also when a sample raised and
+    when the calibration was dropped for another one."""
+    net = torch.nn.Sequential(torch.nn.Linear(24, 24), torch.nn.LayerNorm(24), torch.nn.Linear(24, 8)).cuda()
+    x = torch.randn(10, 24, device="cuda")
+    if how == "off":
+        ctx.set_measured(False)
+    cal = hooks.Calibrator(ctx, net, 1, checkpoint=1)
+    cal.begin()
+    if how in ("raised", "dropped"):
+        with pytest.raises(ZeroDivisionError), cal.sample(0):
+            net(x)
+            1 / 0
+        assert not any("forward" in m.__dict__ for m in net.modules())
+    if how == "raised":
+        cal.begin()
+    if how != "dropped":
+        scored(cal, net, x)
+        assert cal.end()[0]["s_mean"] > 0
+        assert not any("forward" in m.__dict__ for m in net.modules())
+    plain = hooks.Calibrator(ctx, net, 1)
+    plain.begin()
+    scored(plain, net, x)
+    got = plain.end()[-2 if how != "dropped" else -1]
+    assert (got["d_meas"][1] > 0) == (how != "off")
+
+
+def test_results_stay_after_the_end(hooks, ctx):
+    """Group costs and selections work on what was scored, as after any pass; the context's setting comes back with the next
+    one, bound or streamed."""
+    net = torch.nn.Linear(24, 8).cuda()
+    x = torch.randn(10, 24, device="cuda")
+    with one_sample(hooks, ctx, net) as cal:
+        net(x).square().sum().backward()
+    lid = cal.layer_ids[0]
+    assert ctx.get_layer(lid)["s_mean"] == cal.result[0]["s_mean"] > 0
+    g = torch.randn(10, 24, device="cuda")
+    gw = torch.randn(8, 24, device="cuda")
+    ctx.bind_operand(lid, 0, 0, x.data_ptr(), x.numel(), True, g.data_ptr(), x.numel())
+    ctx.bind_operand(lid, 1, 0, net.weight.data_ptr(), gw.numel(), False, gw.data_ptr(), gw.numel())
+    ctx.score()
+    assert ctx.get_layer(lid)["d_meas"][1] > 0
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_begin_again_after_a_sample_that_raised(hooks, ctx, fmt):
+    """The hooks of the pass that was left are gone: each layer is seen once."""
+    net = torch.nn.Sequential(torch.nn.Linear(24, 24), torch.nn.LayerNorm(24), torch.nn.Linear(24, 8)).cuda()
+    x = torch.randn(10, 24, device="cuda")
+    cal = hooks.Calibrator(ctx, net, 1, checkpoint=fmt)
+    cal.begin()
+    with pytest.raises(ZeroDivisionError), cal.sample(0):
+        net(x)
+        1 / 0
+    cal.begin()
+    scored(cal, net, x)
+    assert all(r["s_mean"] > 0 for r in cal.end())
+    assert not any(m._forward_hooks or m._backward_hooks for m in net.modules())
