@@ -104,6 +104,12 @@ class Calibrator:
     def _same_stream(self) -> bool:
         return torch.cuda.current_stream().cuda_stream == self.ctx.stream
 
+    def _borrowed(self, *tensors):
+        """Holds what the library's work on the context's stream reads until the sample is over; on torch's own stream
+        that work comes before any reuse of the memory, and nothing is held."""
+        if not self._same_stream():
+            self._keep += tensors
+
     def _release_sample(self):
         """Called when a sample's block ends: nothing more will be launched on its tensors."""
         if not self._keep:
@@ -138,7 +144,7 @@ class Calibrator:
                     x = x.contiguous()
                     gx = (torch.zeros_like(x) if gx is None else gx.detach().reshape(x.shape)).contiguous()
                     self.ctx.stream_sample(lid, k, self._r, ampq.torch_dtype_code(x), x.data_ptr(), gx.data_ptr(), x.numel())
-                    self._keep += [x, gx]
+                    self._borrowed(x, gx)
                 return
             x = self._x.pop(idx)
             gy = grad_output[0].detach()
@@ -160,7 +166,7 @@ class Calibrator:
         lid = self.layer_ids[idx]
         self.ctx.stream_sample(lid, 0, r, code, x.data_ptr(), gx.data_ptr(), x.numel())
         self.ctx.stream_sample(lid, 1, r, code, w.data_ptr(), gw.data_ptr(), w.numel())
-        self._keep += [x, gx, w, gw]
+        self._borrowed(x, gx, w, gw)
 
     # -- 8-bit checkpoints ------------------------------------------------------
     @staticmethod

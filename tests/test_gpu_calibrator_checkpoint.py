@@ -173,6 +173,30 @@ def test_the_context_and_the_model_are_left_as_they_were(hooks, ctx, how):
     assert (got["d_meas"][1] > 0) == (how != "off")
 
 
+def test_what_a_sample_keeps(hooks, ctx):
+    """On torch's own stream nothing of a layer outlives its backward step: the peak of a sample is its packed inputs (33/64
+    of them in bf16) and what one layer needs, not every layer's decoded input and gradients."""
+    tokens, c, layers = 4096, 2048, 24
+    net = torch.nn.Sequential(*[torch.nn.Linear(c, c, bias=False) for _ in range(layers)]).cuda().bfloat16()
+    x = torch.randn(tokens, c, device="cuda").bfloat16()
+    full = x.numel() * 2
+    peak = {}
+    for fmt in (0, 1):
+        cal = hooks.Calibrator(ctx, net, 2, checkpoint=fmt)
+        cal.begin()
+        scored(cal, net, x, 0)   # the parameters' gradients exist from here on
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        scored(cal, net, x, 1)
+        torch.cuda.synchronize()
+        peak[fmt] = (torch.cuda.max_memory_allocated() - before) / full
+        cal.end()
+    print("peak of a sample in inputs of a layer:", peak)
+    assert peak[1] <= layers * 33 / 64 + 8
+    assert peak[0] <= layers + 8
+
+
 def test_results_stay_after_the_end(hooks, ctx):
     """Group costs and selections work on what was scored, as after any pass; the context's setting comes back with the next
     one, bound or streamed."""
