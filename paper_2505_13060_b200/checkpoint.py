@@ -294,9 +294,19 @@ class _Norm(torch.autograd.Function):
         return gx, gw, gb, None, None, None
 
 
+def autocast(*tensors):
+    """Operands of a product as autocast would give them to torch's own: in its type, where it is on."""
+    if not torch.is_autocast_enabled("cuda"):
+        return tensors
+    dtype = torch.get_autocast_dtype("cuda")
+    return tuple(t.to(dtype) if t is not None and t.is_cuda and t.is_floating_point() and t.dtype != torch.float64 else t for t in tensors)
+
+
 def linear(x: torch.Tensor, weight: torch.Tensor, bias=None, fmt: int = ampq.FMT_E4M3) -> torch.Tensor:
     """``torch.nn.functional.linear`` that keeps x for the backward pass in 8 bits:
-    the weight's gradient is that of the decoded x, everything else is exact."""
+    the weight's gradient is that of the decoded x, everything else is exact.  Under
+    autocast the operands are cast first, as torch does."""
+    x, weight, bias = autocast(x, weight, bias)
     if not torch.is_grad_enabled():
         return torch.nn.functional.linear(x, weight, bias)
     return _Linear.apply(x, weight, bias, fmt)

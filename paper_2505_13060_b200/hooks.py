@@ -187,14 +187,14 @@ class Calibrator:
 
         def known(x, m):   # a norm that the library has; torch runs the others, or says what is wrong with them
             params = [t for t in (m.weight, getattr(m, "bias", None)) if t is not None]
-            return (scored() and x.is_cuda and x.dtype in types and x.shape[-1:] == m.normalized_shape
+            return (scored() and not torch.is_autocast_enabled("cuda") and x.is_cuda and x.dtype in types and x.shape[-1:] == m.normalized_shape
                     and all(t.device == x.device and t.dtype in types and t.dtype == params[0].dtype for t in params))
 
         for idx, (_, m) in enumerate(self.modules):
             if self._plain(m, torch.nn.Linear):
 
                 def linear(input, m=m, idx=idx, plain=m.forward):   # the module's own name for its argument
-                    return _ScoredLinear.apply(input, m.weight, m.bias, self, idx) if scored() else plain(input)
+                    return _ScoredLinear.apply(*ckpt.autocast(input, m.weight, m.bias), self, idx) if scored() else plain(input)
 
                 self._replaced.append((m, linear))
         for m in self.model.modules():

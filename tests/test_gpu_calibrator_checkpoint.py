@@ -197,6 +197,29 @@ def test_what_a_sample_keeps(hooks, ctx):
     assert peak[0] <= layers + 8
 
 
+def test_autocast(hooks, ctx):
+    """Under autocast the layers compute in bf16 from fp32 parameters, and are scored on what their product reads."""
+    torch.manual_seed(3)
+    net = torch.nn.Sequential(torch.nn.Linear(40, 32), torch.nn.LayerNorm(32), torch.nn.Linear(32, 8)).cuda()
+    x = torch.randn(20, 40, device="cuda")
+    with torch.autocast("cuda", torch.bfloat16):
+        want = net(x).detach()
+    with one_sample(hooks, ctx, net) as cal:
+        with torch.autocast("cuda", torch.bfloat16):
+            y = net(x)
+            loss = y.float().square().sum()
+        loss.backward()
+    assert y.dtype == want.dtype and torch.equal(y, want)   # the norm is torch's own under autocast
+    assert net[0].weight.grad.dtype == torch.float32 and bool(net[0].weight.grad.abs().sum() > 0)
+    g = (2.0 * y.detach().double()).bfloat16().double()
+    w = net[2].weight.detach().bfloat16().double()
+    kept = net[1](torch.nn.functional.linear(x.bfloat16(), net[0].weight.bfloat16(), net[0].bias.bfloat16()).float()).detach().bfloat16().double()
+    v = torch.tensor(ref.unpack(*ref.pack(kept.cpu().numpy(), 1), 32, 1), device="cuda")
+    s = ((v * (g @ w)).square().sum() + (w * (g.T @ v)).square().sum()).item()
+    # bf16 operands and gradients, each rounded by at most 2^-8: their products by 2 * 2^-8, the squares by twice that
+    assert abs(cal.result[1]["s_mean"] - s) <= 0.02 * s
+
+
 def test_results_stay_after_the_end(hooks, ctx):
     """Group costs and selections work on what was scored, as after any pass; the context's setting comes back with the next
     one, bound or streamed."""

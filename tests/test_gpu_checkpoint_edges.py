@@ -1,0 +1,42 @@
+"""Edges of the checkpointed functions and norms: autocast, parameters of other types and shapes, rows without columns."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ckpt(ampq):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2505_13060_b200 import checkpoint
+
+    return checkpoint
+
+
+def test_linear_under_autocast(ckpt):
+    """As torch's linear: operands cast to autocast's type, gradients in the parameters' own."""
+    x, w, b = (torch.randn(*s, device="cuda").requires_grad_() for s in ((50, 72), (40, 72), (40,)))
+    gy = torch.randn(50, 40, device="cuda").bfloat16()
+    with torch.autocast("cuda", torch.bfloat16):
+        y = ckpt.linear(x, w, b)
+        want = torch.nn.functional.linear(x, w, b)
+    assert y.dtype == torch.bfloat16 and torch.equal(y, want)
+    y.backward(gy)
+    cast = [t.detach().bfloat16().requires_grad_() for t in (x, w, b)]
+    ckpt.linear(*cast).backward(gy)
+    for t, c in zip((x, w, b), cast):
+        assert t.grad.dtype == torch.float32 and torch.equal(t.grad, c.grad.float())
+
+
+def test_linear_under_autocast_to_fp16_is_refused(ckpt):
+    x, w = torch.randn(50, 72, device="cuda"), torch.randn(40, 72, device="cuda").requires_grad_()
+    with torch.autocast("cuda", torch.float16), pytest.raises(TypeError):
+        ckpt.linear(x, w)
+
+
+def test_linear_of_two_types_is_refused(ckpt):
+    """In the forward pass, by torch's own product."""
+    with pytest.raises(RuntimeError):
+        ckpt.linear(torch.randn(4, 32, device="cuda"), torch.randn(8, 32, device="cuda").bfloat16().requires_grad_())
