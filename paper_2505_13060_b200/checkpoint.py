@@ -210,9 +210,10 @@ def norm_forward(x: torch.Tensor, weight, bias, eps: float, kind: int = ampq.NOR
     return y, mean, rstd, p
 
 
-def norm_backward(gy: torch.Tensor, x, mean, rstd: torch.Tensor, weight, kind: int = ampq.NORM_LAYER, bias: bool = True):
+def norm_backward(gy: torch.Tensor, x, mean, rstd: torch.Tensor, weight, kind: int = ampq.NORM_LAYER, bias: bool = True, bias_dtype=None):
     """Backward pass of ``norm_forward``; x is the input or its checkpoint.  Returns
-    (gx, gw, gb): gw is None without a weight, gb unless a layer norm with a bias."""
+    (gx, gw, gb): gw is None without a weight, gb unless a layer norm with a bias.
+    They are in the weight's type; without a weight gb is in ``bias_dtype``, or gy's."""
     g = _matrix(gy)
     device = _device_of(g)
     rows, cols = g.shape
@@ -230,7 +231,10 @@ def norm_backward(gy: torch.Tensor, x, mean, rstd: torch.Tensor, weight, kind: i
             raise ValueError("mean and rstd are as norm_forward returned them")
     where, code = g.device, _code(g)
     weight = _param(weight, cols)
-    pdtype, pcode = (weight.dtype, _code(weight)) if weight is not None else (g.dtype, code)
+    pdtype = weight.dtype if weight is not None else bias_dtype or g.dtype
+    pcode = _CODE.get(pdtype)
+    if pcode is None:
+        raise TypeError("parameters are float32 or bfloat16, got %s" % pdtype)
     gx = torch.empty(gy.shape, dtype=g.dtype, device=where)
     bias = bias and layer
     gw = torch.empty(cols, dtype=pdtype, device=where) if weight is not None or bias else None
@@ -282,6 +286,7 @@ class _Norm(torch.autograd.Function):
         ctx.kept = p is not None
         ctx.save_for_backward(weight, mean, rstd, *((p.codes, p.scales) if p is not None else (x,)))
         ctx.cols, ctx.kind, ctx.fmt = x.shape[-1], kind, fmt
+        ctx.bias_dtype = bias.dtype if bias is not None else None
         return y
 
     @staticmethod
@@ -290,7 +295,7 @@ class _Norm(torch.autograd.Function):
         weight, mean, rstd, *kept = ctx.saved_tensors
         need_b = ctx.needs_input_grad[2]
         x = Packed(*kept, ctx.cols, ctx.fmt) if ctx.kept else kept[0]
-        gx, gw, gb = norm_backward(gy, x, mean, rstd, weight, ctx.kind, bias=need_b)
+        gx, gw, gb = norm_backward(gy, x, mean, rstd, weight, ctx.kind, bias=need_b, bias_dtype=ctx.bias_dtype)
         return gx, gw, gb, None, None, None
 
 

@@ -40,3 +40,14 @@ def test_linear_of_two_types_is_refused(ckpt):
     """In the forward pass, by torch's own product."""
     with pytest.raises(RuntimeError):
         ckpt.linear(torch.randn(4, 32, device="cuda"), torch.randn(8, 32, device="cuda").bfloat16().requires_grad_())
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_bias_without_weight(ckpt, fmt):
+    """The bias's gradient comes in the bias's type, rounded to that alone: 300 additions in fp32."""
+    x = torch.randn(300, 64, device="cuda").bfloat16()
+    b = torch.randn(64, device="cuda").requires_grad_()
+    gy = torch.randn(300, 64, device="cuda").bfloat16()
+    ckpt.layer_norm(x, None, b, 1e-5, fmt).backward(gy)
+    want = gy.double().sum(0)
+    assert bool(((b.grad.double() - want).abs() <= 300 * U * gy.double().abs().sum(0)).all())
