@@ -287,6 +287,7 @@ class _Norm(torch.autograd.Function):
         ctx.save_for_backward(weight, mean, rstd, *((p.codes, p.scales) if p is not None else (x,)))
         ctx.cols, ctx.kind, ctx.fmt = x.shape[-1], kind, fmt
         ctx.bias_dtype = bias.dtype if bias is not None else None
+        ctx.shapes = [t.shape if t is not None else None for t in (weight, bias)]
         return y
 
     @staticmethod
@@ -296,6 +297,7 @@ class _Norm(torch.autograd.Function):
         need_b = ctx.needs_input_grad[2]
         x = Packed(*kept, ctx.cols, ctx.fmt) if ctx.kept else kept[0]
         gx, gw, gb = norm_backward(gy, x, mean, rstd, weight, ctx.kind, bias=need_b, bias_dtype=ctx.bias_dtype)
+        gw, gb = (g.view(s) if g is not None else None for g, s in zip((gw, gb), ctx.shapes))   # [1, C] parameters too
         return gx, gw, gb, None, None, None
 
 

@@ -51,3 +51,14 @@ def test_bias_without_weight(ckpt, fmt):
     ckpt.layer_norm(x, None, b, 1e-5, fmt).backward(gy)
     want = gy.double().sum(0)
     assert bool(((b.grad.double() - want).abs() <= 300 * U * gy.double().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_parameters_of_more_dimensions(ckpt, fmt):
+    """[1, C] parameters get gradients of their own shape."""
+    x, gy = torch.randn(30, 64, device="cuda"), torch.randn(30, 64, device="cuda")
+    w, b = torch.rand(1, 64, device="cuda").requires_grad_(), torch.rand(1, 64, device="cuda").requires_grad_()
+    ckpt.layer_norm(x, w, b, 1e-5, fmt).backward(gy)
+    v, c = w.detach()[0].clone().requires_grad_(), b.detach()[0].clone().requires_grad_()
+    ckpt.layer_norm(x, v, c, 1e-5, fmt).backward(gy)
+    assert torch.equal(w.grad[0], v.grad) and torch.equal(b.grad[0], c.grad)
