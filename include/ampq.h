@@ -475,7 +475,7 @@ int ampq_ckpt_weight_grad(int device, void *cuda_stream, int dtype, int fmt, con
  *   RMS    y = x * rstd * weight, rstd = 1 / sqrt(mean of x^2 + eps)
  * weight, bias: `param_dtype`, cols elements, each may be NULL (1 and 0; bias is
  * LAYER only).  mean (LAYER only) and rstd: fp32, one per row, kept for the
- * backward pass.  fmt = AMPQ_FMT_E4M3 or AMPQ_FMT_E5M2 also writes the
+ * backward pass; NaN in rows without columns.  fmt = AMPQ_FMT_E4M3 or AMPQ_FMT_E5M2 also writes the
  * checkpoint of x in the same read; AMPQ_FMT_BASE does not (codes and scales are
  * ignored). */
 enum { AMPQ_NORM_LAYER = 0, AMPQ_NORM_RMS = 1 };

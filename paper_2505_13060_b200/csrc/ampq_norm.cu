@@ -922,7 +922,16 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
         return AMPQ_ERR_ALIGN;
     CkptDevice cur(device);
     if (cur.status) return cur.status;
-    if (rows == 0 || cols == 0) return AMPQ_OK;
+    if (rows == 0) return AMPQ_OK;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if (cols == 0) {  // the mean of nothing: NaN, all bits set
+        for (float* p : {layer ? mean : nullptr, rstd})
+            if (p && cudaMemsetAsync(p, 0xFF, (size_t)rows * sizeof(float), st) != cudaSuccess) {
+                cudaGetLastError();
+                return AMPQ_ERR_CUDA;
+            }
+        return AMPQ_OK;
+    }
     const int sms = sm_count(device);
     if (sms < 1) return AMPQ_ERR_CUDA;
     ForwardArgs a;
@@ -936,7 +945,6 @@ int ampq_norm_forward(int device, void* cuda_stream, int kind, int dtype, int pa
     a.whole = cols % (dtype == AMPQ_F32 ? 8 : 16) == 0;
     a.bulk = rows_aligned(x, ld_x, dtype) && a.whole;
     a.param_bf16 = param_dtype == AMPQ_BF16;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const bool kept = fmt != AMPQ_FMT_BASE;
     return dtype == AMPQ_F32 ? dispatch_forward<float>(kept, layer, a, device, sms, st) : dispatch_forward<__nv_bfloat16>(kept, layer, a, device, sms, st);
 }

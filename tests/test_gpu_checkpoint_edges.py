@@ -62,3 +62,18 @@ def test_parameters_of_more_dimensions(ckpt, fmt):
     v, c = w.detach()[0].clone().requires_grad_(), b.detach()[0].clone().requires_grad_()
     ckpt.layer_norm(x, v, c, 1e-5, fmt).backward(gy)
     assert torch.equal(w.grad[0], v.grad) and torch.equal(b.grad[0], c.grad)
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_rows_without_columns_have_no_statistics(ampq, ckpt, kind, fmt):
+    """The mean of nothing is NaN, and so is what follows from it; nothing is left unwritten."""
+    mean, rstd = torch.full((7,), 3.0, device="cuda"), torch.full((7,), 3.0, device="cuda")
+    rc = ampq.lib().ampq_norm_forward(0, torch.cuda.current_stream().cuda_stream, kind, 0, 0, fmt, 0, 0, 5, 0, 0, 0, 1e-5, 0, 0,
+                                      mean.data_ptr() if kind == 0 else 0, rstd.data_ptr(), 0, 0, 0, 0)
+    assert rc == 0
+    assert bool(torch.isnan(rstd[:5]).all()) and bool((rstd[5:] == 3.0).all())
+    if kind == 0:
+        assert bool(torch.isnan(mean[:5]).all()) and bool((mean[5:] == 3.0).all())
+    y, mean, rstd, p = ckpt.norm_forward(torch.empty(2, 3, 0, device="cuda"), None, None, 1e-5, kind, fmt)
+    assert y.shape == (2, 3, 0) and bool(torch.isnan(rstd).all()) and (mean is None or bool(torch.isnan(mean).all()))
