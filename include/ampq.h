@@ -430,7 +430,8 @@ int ampq_score_segment_noalloc(int device, void *cuda_stream, int dtype, int fmt
  * aligned, at least as large as the query says for the same arguments, and free
  * again when the work on the stream has finished: calls that may overlap on the
  * GPU need one each.  Sizes: rows (all samples together) up to 2^31 - 1, columns
- * up to 2^30 - 1, AMPQ_ERR_TOO_LARGE beyond. */
+ * up to 2^30 - 1, AMPQ_ERR_TOO_LARGE beyond, and where a call's outputs or
+ * workspace would take more than 2^52 bytes. */
 #define AMPQ_CKPT_GROUP 32
 
 /* Writes the checkpoint of `values` in format `fmt` (AMPQ_FMT_E4M3 or

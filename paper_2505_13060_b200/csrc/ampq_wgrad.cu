@@ -1033,6 +1033,10 @@ int check_sizes(int dtype, long long samples, long long rows, long long cols, lo
     if (cols > kMaxCols || outs > kMaxCols || samples > kMaxRows || rows > kMaxRows || (samples > 0 && rows > kMaxRows / samples)) return AMPQ_ERR_TOO_LARGE;
     // tiles of one sample are counted in 32 bits
     if (((outs + 127) / 128) * ((cols + 127) / 128) > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
+    // gradients and workspaces are counted in 64 bits (the partial products of few tiles are at most one per SM)
+    const double tokens = (double)samples * (double)rows, most = 4503599627370496.0;  // 2^52 bytes
+    if (12.0 * tokens * (double)outs > most || 2.0 * tokens * (double)cols > most || 4.0 * (double)samples * (double)outs * (double)cols > most)
+        return AMPQ_ERR_TOO_LARGE;
     return AMPQ_OK;
 }
 
