@@ -33,3 +33,22 @@ def test_bf16_sums_of_one_sign(ckpt, outs, cols):
     want = torch.matmul(gy[:, :64].double().T, ckpt.unpack(some, torch.float32).double())
     off = (gw[0, :64, :64].double() - want).abs() / want
     assert float(off.max()) <= 2.0 ** -8 + 1.01 * (4096 * 2 * U + 256 * U)
+
+
+@pytest.mark.parametrize("rows", [200, 300], ids=["small", "large"])
+@pytest.mark.parametrize("exponent", [-100, -112, -120, -126, -140])
+def test_fp32_gradients_near_the_smallest(ckpt, rows, exponent):
+    """fp32 gradients are read to 24 significant bits down to 2^-110 and below that, where the products run on the tensor
+    cores, to 2^-133 (bf16's last bit): what is cut off a gradient times |x|, on top of the bound of the sum itself and of an
+    fp32 result, whose own last bit is 2^-149."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    gy = (torch.randn(rows, 520, device="cuda", generator=g).double() * 2.0 ** exponent).float()
+    p = ckpt.pack(torch.randn(rows, 512, device="cuda", generator=g))
+    x = ckpt.unpack(p, torch.float32).double()
+    gw, gb = ckpt.weight_grad(p, gy, bias=True)
+    want, size = gy.double().T @ x, gy.double().abs().T @ x.abs()
+    tol = (2 * rows + 8) * U * size + U * want.abs() + 2.0 ** -150 * rows
+    if rows > 256 and exponent < -100:
+        tol += 2.0 ** -133 * x.abs().sum(0)
+    assert bool(((gw[0].double() - want).abs() <= tol).all())
+    assert bool(((gb[0].double() - gy.double().sum(0)).abs() <= rows * U * gy.double().abs().sum(0)).all())
