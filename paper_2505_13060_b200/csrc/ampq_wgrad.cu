@@ -790,16 +790,24 @@ struct Plan {
     long long at_x, at_part, bytes;
 };
 
-// Products of at most this many tokens, and of no more 64 x 64 tiles than four per
-// SM, are small.
-constexpr long long kSmallRows = 256;
+// Products of at most kSmallRows tokens, and of at most kSmallWork tokens x 64 x 64
+// tiles per SM, are small.  The small kernel's time goes with the tokens and the waves
+// of tiles; the other form takes three to five launches, and a workspace, whatever the
+// size.  Microseconds of a call from Python (in a graph), small against other:
+//   fp32, 256 tokens: 128 tiles 16.7 (15.5) against 24.8 (16.6), 256 tiles 24.6 (22.9)
+//     against 24.5 (16.6), 576 tiles 43 (42) against 25 (18.5)
+//   bf16, 256 tokens: 128 tiles 20.5 (18.4) against 20.6 (11.7), 576 tiles 45 (42)
+//     against 21 (12.7)
+//   64 tokens: 576 tiles, fp32 15.5 (12.8) against 23.7 (14.8), bf16 14.4 (12.8)
+//     against 20.7 (11.4); 1024 tiles 22.6 (21) against 24.7 (18.4), 23.4 (13.2)
+constexpr long long kSmallRows = 256, kSmallWork = 320;
 
 long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 
 Plan make_plan(const Problem& q, int sms) {
     Plan p = {};
     const long long small_tiles = ((q.outs + kSmallSide - 1) / kSmallSide) * ((q.cols + kSmallSide - 1) / kSmallSide);
-    p.small = q.rows <= kSmallRows && small_tiles <= 65535 && q.samples <= 65535 && small_tiles * q.samples <= 4LL * sms;
+    p.small = q.rows <= kSmallRows && small_tiles <= 65535 && q.samples <= 65535 && small_tiles * q.samples * q.rows <= kSmallWork * sms;
     if (p.small) return p;
     p.copy = q.dtype == AMPQ_F32 || !rows_aligned(q.gy, q.ld_gy, q.dtype);
     p.planes = q.dtype == AMPQ_F32 ? 3 : 1;
