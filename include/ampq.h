@@ -453,8 +453,9 @@ int ampq_ckpt_unpack(int device, void *cuda_stream, int dtype, int fmt, const un
  *   codes, scales   checkpoint of [samples * rows, cols]
  *   gw      [samples, outs, cols] of `dtype`, contiguous
  *   gb      [samples, outs] of `dtype`, contiguous, or NULL
- * rows = 0 gives zeros.  Products are exact, sums are fp32, one rounding to
- * `dtype` at the end.  Larger products run on the tensor cores, whose fp32
+ * rows = 0 gives zeros.  Products are exact (in larger ones bits of an fp32
+ * gradient below 2^-133 are not seen), sums are fp32, one rounding to `dtype` at
+ * the end.  Larger products run on the tensor cores, whose fp32
  * additions cut instead of rounding to nearest: for fp32 the sum of every 64
  * tokens, for bf16 of every 4096, is joined to the rest by an addition that
  * rounds (a bf16 sum of one sign comes out smaller by 2e-5 of itself at most,

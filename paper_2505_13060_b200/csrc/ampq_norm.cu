@@ -494,8 +494,10 @@ struct Ring {
 // few threads that the sums' registers allow.  The groups of a CTA are joined in
 // shared memory, the CTAs by join_columns_kernel, in a fixed order.
 //
-// Bound by the instructions of sixteen warps and a row's barrier: RMS norm of 8192 x
-// 8192 from 8 bits 76 us (4.4 TB/s), layer norm from bf16 87 us (4.6 TB/s).
+// Bound by the row's latency: sixteen warps go through one row in step with a barrier,
+// and no other row fills the gap (issue slots and DRAM both half busy, a quarter of
+// the warps).  RMS norm of 8192 x 8192 from 8 bits 76 us (4.4 TB/s), layer norm from
+// bf16 87 us (4.6 TB/s).
 // Holding a row back until the next row's sums are under way (103 us against 102 at
 // that point) and two CTAs of half the warps (145 us) cost more in registers and
 // repeated work than the barrier.  Rows off the 16-byte boundaries are copied and

@@ -11,9 +11,9 @@
 // it, took the power and the issue slots that the tensor cores need (8192^3: 1200
 // TFLOP/s against 1510 with the pass included).
 //
-// fp32 gradients are cut into three bf16 planes, g = g0 + g1 + g2 exactly (24
-// significant bits), and each 64 tokens are multiplied plane by plane, the smallest
-// first.
+// fp32 gradients are cut into three bf16 planes, g = g0 + g1 + g2 (24 significant
+// bits, exact from 2^-110 up; below that what is smaller than 2^-133, bf16's last bit,
+// is lost), and each 64 tokens are multiplied plane by plane, the smallest first.
 //
 // The tensor core's additions cut instead of rounding: 2.9e-8 per addition, all
 // towards zero, 4e-5 over 8192 tokens of one sign and more than half a step of bf16
@@ -337,7 +337,7 @@ __device__ __noinline__ void drain_copies(const unsigned (&end)[2], unsigned ran
 // Per accumulator: `filled`, `drained`.
 //
 // Bound by the tensor cores and, over more than a few ms, by the board's power:
-// 8192^3 in bf16 690 us (1590 TFLOP/s), 2 x 4096 x 8192 x 28672 2.57 ms (1500; a
+// 8192^3 in bf16 (one run) 690 us (1590 TFLOP/s), 2 x 4096 x 8192 x 28672 2.57 ms (1500; a
 // library's matrix product reaches 1613 in a burst and 1344 sustained), 4 x 2048 x 4096 x 4096 191 us (1440: 1024 tiles on 74 pairs).  fp32,
 // three planes: 2048^3 52 us (330 of fp32 arithmetic).  Six stages or seven, bands
 // of 4, 8 or 16 tiles: within 2 % of each other, but for bands of 4 (8 % slower at
@@ -617,8 +617,8 @@ __global__ void __launch_bounds__(256) small_product_kernel(const T* __restrict_
 // ---------------------------------------------------------------------------
 // what a large product needs beforehand
 
-// fp32 -> three bf16 planes that add up to it exactly: the upper 8 significant
-// bits, the next 8, the last 8.  A value that is not finite keeps its kind in the
+// fp32 -> three bf16 planes: the upper 8 significant bits, the next 8, the last 8.
+// They add up to it but for bits below 2^-133.  A value that is not finite keeps its kind in the
 // first plane and leaves the others 0.
 __device__ __forceinline__ void cut3(float g, unsigned short (&h)[3]) {
     const unsigned u = __float_as_uint(g);

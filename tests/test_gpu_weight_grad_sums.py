@@ -52,3 +52,17 @@ def test_fp32_gradients_near_the_smallest(ckpt, rows, exponent):
         tol += 2.0 ** -133 * x.abs().sum(0)
     assert bool(((gw[0].double() - want).abs() <= tol).all())
     assert bool(((gb[0].double() - gy.double().sum(0)).abs() <= rows * U * gy.double().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("samples,rows,cols,outs", [(2, 128, 256, 256), (3, 997, 1031, 2053), (1, 9000, 300, 520), (1, 6000, 4096, 2560), (2, 4096, 2048, 4096)])
+def test_results_repeat_themselves(ckpt, dtype, samples, rows, cols, outs):
+    """The same bits every time, with other work in between: sums are added in an order fixed by the sizes."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    p = ckpt.pack(torch.randn(samples * rows, cols, device="cuda", generator=g).to(dtype))
+    gy = torch.randn(samples * rows, outs, device="cuda", generator=g).to(dtype)
+    first = ckpt.weight_grad(p, gy, samples=samples, bias=True)
+    for _ in range(8):
+        ckpt.weight_grad(p, gy + 1, samples=samples, bias=True)
+        again = ckpt.weight_grad(p, gy, samples=samples, bias=True)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
