@@ -251,3 +251,22 @@ def test_begin_again_after_a_sample_that_raised(hooks, ctx, fmt):
     scored(cal, net, x)
     assert all(r["s_mean"] > 0 for r in cal.end())
     assert not any(m._forward_hooks or m._backward_hooks for m in net.modules())
+
+
+def test_a_context_on_a_stream_of_its_own(hooks, ampq):
+    """The same sensitivities as on torch's stream, over more samples than are held at a time."""
+    torch.manual_seed(4)
+    net = torch.nn.Sequential(torch.nn.Linear(64, 256), torch.nn.LayerNorm(256), torch.nn.Linear(256, 64), torch.nn.RMSNorm(64), torch.nn.Linear(64, 8)).cuda().bfloat16()
+    x = torch.randn(6, 500, 64, device="cuda").bfloat16()
+    got = []
+    side = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), side):
+        c = ampq.Context(0, stream.cuda_stream)
+        c.set_formats([0, 1])
+        cal = hooks.Calibrator(c, net, 6, checkpoint=1)
+        cal.begin()
+        for r in range(6):
+            scored(cal, net, x[r], r)
+        got.append([list(res["s_per_sample"]) for res in cal.end()])
+        c.destroy()
+    assert got[0] == got[1] and all(s > 0 for layer in got[0] for s in layer)
