@@ -96,7 +96,7 @@ def test_modules_with_a_forward_of_their_own(hooks, ctx, which):
 
 
 def test_arguments_by_name(hooks, ctx):
-    """Linear and LayerNorm call their argument `input`, RMSNorm `x`: all three are called by name as without checkpoints."""
+    """Linear and LayerNorm call their argument `input`, RMSNorm `x`: all three can be called by name."""
     lin, ln, rms = torch.nn.Linear(32, 32).cuda(), torch.nn.LayerNorm(32).cuda(), torch.nn.RMSNorm(32).cuda()
     net = torch.nn.ModuleList([lin, ln, rms])
     x = torch.randn(5, 32, device="cuda")

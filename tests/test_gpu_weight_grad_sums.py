@@ -66,3 +66,21 @@ def test_results_repeat_themselves(ckpt, dtype, samples, rows, cols, outs):
         ckpt.weight_grad(p, gy + 1, samples=samples, bias=True)
         again = ckpt.weight_grad(p, gy, samples=samples, bias=True)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("outs,cols", [(2050, 1290), (1290, 1030)], ids=["pairs", "single"])
+@pytest.mark.parametrize("rows", [4096, 4097, 8193])
+def test_around_the_length_of_a_run(ckpt, dtype, outs, cols, rows):
+    """One run of tokens, a second one of a single token, a third: every output, odd widths.  A sum of n terms is off by at
+    most 2 n * 2^-24 of its absolute sum (cut additions), and half a step at the end."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    p = ckpt.pack(torch.randn(rows, cols, device="cuda", generator=g).to(dtype))
+    gy = torch.randn(rows, outs, device="cuda", generator=g).to(dtype)
+    x = ckpt.unpack(p, torch.float32).double()
+    gw, gb = ckpt.weight_grad(p, gy, bias=True)
+    want, size = gy.double().T @ x, gy.double().abs().T @ x.abs()
+    half = U if dtype == torch.float32 else 2.0 ** -8
+    assert bool(((gw[0].double() - want).abs() <= 2 * rows * U * size + 1.01 * half * want.abs()).all())
+    want, size = gy.double().sum(0), gy.double().abs().sum(0)
+    assert bool(((gb[0].double() - want).abs() <= rows * U * size + 1.01 * half * want.abs()).all())
