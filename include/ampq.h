@@ -499,6 +499,96 @@ int ampq_norm_backward(int device, void *cuda_stream, int kind, int dtype, int p
                        long long ld_scales, long long rows, long long cols, const float *mean, const float *rstd, const void *weight,
                        void *gx, long long ld_gx, void *gweight, void *gbias, void *workspace, long long workspace_bytes);
 
+/* ---------------------------------------------------------------------------
+ * The other operators of a decoder's pass: the embedding in front, the norms of
+ * queries and keys with the position rotation between the linear layers and the
+ * product Q K^T, and a loss behind the head that needs no labels.  The rules above
+ * (device and stream, alignment, rows, workspaces, capture) hold for them too.
+ * Indices (tokens, positions, columns) are of `index_type`; none that is out of
+ * range is used as an address. */
+enum { AMPQ_I32 = 0, AMPQ_I64 = 1 };
+
+/* Embedding lookup: y[i] = scale * weight[tokens[i]], i < n, weight [vocab, cols].
+ * The product is rounded once.  A token outside [0, vocab) has a row of NaN. */
+int ampq_embed_forward(int device, void *cuda_stream, int dtype, int index_type, const void *tokens, long long n, const void *weight, long long ld_w,
+                       long long vocab, long long cols, float scale, void *y, long long ld_y);
+
+/* Its gradient: gw[v] = scale * sum of gy[i] over the i with tokens[i] = v.  All of
+ * gw [vocab, cols] (contiguous) is written: rows of no token and row `padding` are 0
+ * (padding < 0: no such row).  Tokens outside [0, vocab) count for no row.  The
+ * tokens are sorted, the rows of one token added in fp32 in an order that the tokens
+ * and sizes fix, and the sum is rounded once.  vocab up to 2^31 - 1. */
+int ampq_embed_backward_workspace(int device, int dtype, long long n, long long vocab, long long cols, long long *bytes);
+int ampq_embed_backward(int device, void *cuda_stream, int dtype, int index_type, const void *tokens, long long n, const void *gy, long long ld_gy,
+                        long long vocab, long long cols, float scale, long long padding, void *gw, void *workspace, long long workspace_bytes);
+
+/* Queries or keys of ampq_head_norm_*: tensors [batch, tokens, heads, cols] of
+ * `dtype` whose columns are neighbours; the other strides are in elements, not
+ * negative, and those of `out` make no two elements one. */
+typedef struct ampq_heads {
+    long long heads;
+    const void *x;       /* input (not looked at by a backward pass from a checkpoint) */
+    long long x_batch, x_token, x_head;
+    const void *gy;      /* gradient of the output (backward) */
+    long long gy_batch, gy_token, gy_head;
+    void *out;           /* output, or gradient of the input (backward) */
+    long long out_batch, out_token, out_head;
+    const void *weight;  /* `param_dtype`, cols elements; NULL for ones */
+    void *gweight;       /* its gradient (backward), or NULL */
+    float *rstd;         /* [batch, tokens, heads]: written forward, read backward */
+    unsigned char *codes;  /* checkpoint of x as a matrix of batch * tokens * heads rows: written forward, read backward */
+    long long ld_codes;
+    unsigned char *scales;
+    long long ld_scales;
+} ampq_heads;
+
+/* RMS norm of each head of each token and the rotation by the angle of the token's
+ * position.  With n = x * rstd * weight, rstd = 1 / sqrt(mean of x^2 + eps):
+ *   y_i = n_i cos_p - n_j sin_p,  y_j = n_j cos_p + n_i sin_p   for the pairs p < rot / 2 of the first rot columns,
+ *   (i, j) = (p, p + rot / 2), or (2 p, 2 p + 1) when `interleaved`;  y = n behind them.
+ * cols: even, up to AMPQ_HEAD_MAX_COLS (AMPQ_ERR_TOO_LARGE beyond); rot: even, 0 to
+ * cols.  cos, sin: [angles, rot / 2], contiguous, 16-byte aligned; row
+ * positions[b * position_batch + t] is that of token t of batch b, or row t where
+ * positions is NULL.  A position without a row gives NaN in the turned columns (and
+ * in the whole gradient of its heads).  k may be NULL.  fmt = AMPQ_FMT_E4M3 or AMPQ_FMT_E5M2 also
+ * writes the checkpoint of x, one row for each head (groups do not cross heads). */
+#define AMPQ_HEAD_MAX_COLS 256
+int ampq_head_norm_forward(int device, void *cuda_stream, int dtype, int param_dtype, int index_type, int fmt, int interleaved, long long batch,
+                           long long tokens, long long cols, long long rot, const float *cos, const float *sin, long long angles, const void *positions,
+                           long long position_batch, float eps, const ampq_heads *q, const ampq_heads *k);
+
+/* Its backward pass.  With t the gradient turned back, h = x * rstd and u = t * weight:
+ *   gx = rstd * (u - h * mean_c(u * h)),  gweight = sum over batch, tokens and heads of t * h.
+ * x itself (fmt = AMPQ_FMT_BASE) or its checkpoint.  The workspace is needed when a
+ * gweight is. */
+int ampq_head_norm_backward_workspace(int device, long long batch, long long tokens, long long cols, long long *bytes);
+int ampq_head_norm_backward(int device, void *cuda_stream, int dtype, int param_dtype, int index_type, int fmt, int interleaved, long long batch,
+                            long long tokens, long long cols, long long rot, const float *cos, const float *sin, long long angles, const void *positions,
+                            long long position_batch, const ampq_heads *q, const ampq_heads *k, void *workspace, long long workspace_bytes);
+
+/* Distillation from the `top` largest logits of a teacher.  Row n of logits
+ * [rows, cols] has a list of columns indices[n][k] and the teacher's logits
+ * teacher[n][k] (`teacher_dtype`), k < top <= AMPQ_DISTILL_MAX_TOP
+ * (AMPQ_ERR_TOO_LARGE beyond); an entry with a negative index is no entry.  With
+ * p = softmax over the row's entries of teacher / T and q = softmax over all columns
+ * of logits / T:
+ *   loss[n] = T^2 * sum_k p_k (log p_k - log q[indices[n][k]])   (0 where p_k is 0),
+ *   stats[n] = {max_j logits[n][j], sum_j exp((logits[n][j] - max) / T)}.
+ * A row without entries is not read: loss 0, stats 0.  A column may be listed more
+ * than once; an index of cols or more makes the loss NaN.  Logits of -Inf have q = 0;
+ * rows with +Inf, NaN or nothing but -Inf have loss NaN.  T in [2^-20, 2^20]. */
+#define AMPQ_DISTILL_MAX_TOP 1024
+int ampq_distill_forward(int device, void *cuda_stream, int dtype, int teacher_dtype, int index_type, const void *logits, long long ld, long long rows,
+                         long long cols, const void *indices, long long ld_indices, const void *teacher, long long ld_teacher, long long top,
+                         float temperature, float *loss, float *stats);
+
+/* Its gradient: gs[n][j] = gl[n * gl_stride] * T * (q_j - sum of p_k over the k with
+ * indices[n][k] = j), 0 in rows without entries; stats as the forward pass left them
+ * (gl_stride 0: one number for all rows). */
+int ampq_distill_backward(int device, void *cuda_stream, int dtype, int teacher_dtype, int index_type, const float *gl, long long gl_stride,
+                          const void *logits, long long ld, long long rows, long long cols, const void *indices, long long ld_indices, const void *teacher,
+                          long long ld_teacher, long long top, const float *stats, float temperature, void *gs, long long ld_gs);
+
 #ifdef __cplusplus
 }
 #endif

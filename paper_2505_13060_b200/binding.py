@@ -25,6 +25,8 @@ MEM_DEVICE, MEM_HOST = 0, 1
 SCALE_AMAX, SCALE_POW2 = 0, 1
 NORM_LAYER, NORM_RMS = 0, 1
 CKPT_GROUP, NORM_MAX_COLS = 32, 16384
+I32, I64 = 0, 1
+HEAD_MAX_COLS, DISTILL_MAX_TOP = 256, 1024
 
 OK = 0
 ERR_INVALID, ERR_ALIGN, ERR_STATE, ERR_CUDA = -1, -2, -3, -4
@@ -43,8 +45,19 @@ EXPORTS = [
     "ampq_set_sharing", "ampq_get_pass_bytes", "ampq_merge_sample_tables", "ampq_get_layer_table", "ampq_last_tile_shift",
     "ampq_ckpt_pack", "ampq_ckpt_unpack", "ampq_ckpt_weight_grad_workspace", "ampq_ckpt_weight_grad",
     "ampq_norm_forward", "ampq_norm_backward_workspace", "ampq_norm_backward",
+    "ampq_embed_forward", "ampq_embed_backward_workspace", "ampq_embed_backward",
+    "ampq_head_norm_forward", "ampq_head_norm_backward_workspace", "ampq_head_norm_backward",
+    "ampq_distill_forward", "ampq_distill_backward",
 ]
 NOALLOC_MAX_NUMEL = 2147483648
+
+class Heads(C.Structure):
+    """``ampq_heads``: queries or keys of ``ampq_head_norm_*``."""
+
+    _fields_ = [(name, C.c_void_p if name in ("x", "gy", "out", "weight", "gweight", "rstd", "codes", "scales") else C.c_longlong) for name in (
+        "heads", "x", "x_batch", "x_token", "x_head", "gy", "gy_batch", "gy_token", "gy_head", "out", "out_batch", "out_token", "out_head",
+        "weight", "gweight", "rstd", "codes", "ld_codes", "scales", "ld_scales")]
+
 
 _lib = None
 
@@ -117,6 +130,15 @@ def lib():
     L.ampq_norm_forward.argtypes = [i, vp, i, i, i, i, vp, ll, ll, ll, vp, vp, C.c_float, vp, ll, vp, vp, vp, ll, vp, ll]
     L.ampq_norm_backward_workspace.argtypes = [i, ll, ll, C.POINTER(ll)]
     L.ampq_norm_backward.argtypes = [i, vp, i, i, i, i, vp, ll, vp, ll, vp, ll, vp, ll, ll, ll, vp, vp, vp, vp, ll, vp, vp, vp, ll]
+    f = C.c_float
+    L.ampq_embed_forward.argtypes = [i, vp, i, i, vp, ll, vp, ll, ll, ll, f, vp, ll]
+    L.ampq_embed_backward_workspace.argtypes = [i, i, ll, ll, ll, C.POINTER(ll)]
+    L.ampq_embed_backward.argtypes = [i, vp, i, i, vp, ll, vp, ll, ll, ll, f, ll, vp, vp, ll]
+    L.ampq_head_norm_forward.argtypes = [i, vp, i, i, i, i, i, ll, ll, ll, ll, vp, vp, ll, vp, ll, f, vp, vp]
+    L.ampq_head_norm_backward_workspace.argtypes = [i, ll, ll, ll, C.POINTER(ll)]
+    L.ampq_head_norm_backward.argtypes = [i, vp, i, i, i, i, i, ll, ll, ll, ll, vp, vp, ll, vp, ll, vp, vp, vp, ll]
+    L.ampq_distill_forward.argtypes = [i, vp, i, i, i, vp, ll, ll, ll, vp, ll, vp, ll, ll, f, vp, vp]
+    L.ampq_distill_backward.argtypes = [i, vp, i, i, i, vp, ll, vp, ll, ll, ll, vp, ll, vp, ll, ll, vp, f, vp, ll]
     for name in EXPORTS:
         if name not in ("ampq_strerror", "ampq_last_error"):
             getattr(L, name).restype = i

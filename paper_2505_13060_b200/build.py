@@ -13,8 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libampq.so")
 SOURCES = ["ampq_kernels.cu", "ampq_lib.cu", "ampq_noalloc.cu", "ampq_select.cpp", "ampq_graph.cpp",
-           "ampq_ckpt.cu", "ampq_norm.cu", "ampq_wgrad.cu"]
-HEADERS = ["ampq_device.h", "ampq_kernels.h", "ampq_select.h", "ampq_ckpt.h", os.path.join("..", "..", "include", "ampq.h")]
+           "ampq_ckpt.cu", "ampq_norm.cu", "ampq_wgrad.cu", "ampq_heads.cu", "ampq_embed.cu", "ampq_distill.cu"]
+HEADERS = ["ampq_device.h", "ampq_kernels.h", "ampq_select.h", "ampq_ckpt.h", "ampq_decoder.h", os.path.join("..", "..", "include", "ampq.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
