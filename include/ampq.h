@@ -574,7 +574,8 @@ int ampq_head_norm_backward(int device, void *cuda_stream, int dtype, int param_
  * of logits / T:
  *   loss[n] = T^2 * sum_k p_k (log p_k - log q[indices[n][k]])   (0 where p_k is 0),
  *   stats[n] = {max_j logits[n][j], sum_j exp((logits[n][j] - max) / T)}.
- * A row without entries is not read: loss 0, stats 0.  A column may be listed more
+ * A row without entries has loss 0 and stats 0,
+ * whatever its logits are.  A column may be listed more
  * than once; an index of cols or more makes the loss NaN.  Logits of -Inf have q = 0;
  * rows with +Inf, NaN or nothing but -Inf have loss NaN.  T in [2^-20, 2^20]. */
 #define AMPQ_DISTILL_MAX_TOP 1024

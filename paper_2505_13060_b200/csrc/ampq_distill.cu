@@ -16,7 +16,9 @@ namespace ampq {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kPer = AMPQ_DISTILL_MAX_TOP / kThreads;  // entries of a row's list to a thread
+// vectors that a thread has in flight, and CTAs that share an SM
+constexpr int kForwardAhead = 1, kForwardCtas = 8;
+constexpr int kBackwardAhead = 1, kBackwardCtas = 6;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
 struct DistillArgs {
@@ -92,38 +94,34 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return a;
 }
 
-// The list of a row: entry tid + kThreads * i of every thread.
-struct Entries {
-    unsigned index[kPer];
-    float t[kPer];
-    bool there[kPer];
+// The list of a row in shared memory: column (kNone: no entry, `cols`: no column), the
+// teacher's logit and the row's own.  Out of the registers that the streams need.
+constexpr unsigned kNone = 0xFFFFFFFFu;
+struct List {
+    unsigned index[AMPQ_DISTILL_MAX_TOP];
+    float t[AMPQ_DISTILL_MAX_TOP], s[AMPQ_DISTILL_MAX_TOP];
+    // Thread by thread, each its own entries; whether one of them is there.
     __device__ __forceinline__ bool load(const DistillArgs& a, long long row) {
         bool any = false;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int k = threadIdx.x + kThreads * i;
-            there[i] = false;
-            index[i] = 0;
-            t[i] = -INFINITY;
-            if (k < a.top) {
-                const long long j = load_index(a.indices, row * a.ld_indices + k, a.wide);
-                there[i] = j >= 0;
-                if (there[i]) {
-                    const bool known = j < (long long)a.cols;  // a column that is not there: the row's loss is NaN
-                    index[i] = known ? (unsigned)j : a.cols;
-                    t[i] = known ? load_param(a.teacher, row * a.ld_teacher + k, a.teacher_bf16) : NAN;
-                }
-            }
-            any |= there[i];
+        for (int k = threadIdx.x; k < a.top; k += kThreads) {
+            const long long j = load_index(a.indices, row * a.ld_indices + k, a.wide);
+            const bool known = j < (long long)a.cols;  // a column that is not there: the row's loss is NaN
+            index[k] = j < 0 ? kNone : known ? (unsigned)j : a.cols;
+            t[k] = j < 0 ? -INFINITY : known ? load_param(a.teacher, row * a.ld_teacher + k, a.teacher_bf16) : NAN;
+            any |= j >= 0;
         }
         return any;
     }
-    // Largest t of the row; all threads call it.
-    __device__ __forceinline__ float largest(float* red) const {
+    // The row's logits at the thread's entries (of those that `mine` says).
+    template <typename T, typename F>
+    __device__ __forceinline__ void gather(const DistillArgs& a, const T* x, F mine) {
+        for (int k = threadIdx.x; k < a.top; k += kThreads)
+            if (index[k] < a.cols && mine(index[k])) s[k] = load_elem(x + index[k]);
+    }
+    // Largest t of the row; all threads call it, and each has its own entries.
+    __device__ __forceinline__ float largest(const DistillArgs& a, float* red) const {
         float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (there[i]) m = max_nan(m, t[i]);
+        for (int k = threadIdx.x; k < a.top; k += kThreads) m = max_nan(m, t[k]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
         if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = m;
@@ -134,6 +132,18 @@ struct Entries {
         return m;
     }
 };
+
+// 32 bytes on a 32-byte boundary, read once.
+__device__ __forceinline__ void load_vector(const void* p, unsigned (&w)[8]) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+}
+__device__ __forceinline__ void store_vector(void* p, const unsigned (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
 
 // Sums over the CTA, in a fixed order; all threads call it.
 template <int N>
@@ -163,17 +173,29 @@ __device__ __forceinline__ unsigned cluster_rank() {
 // A row to a CTA, or to a cluster of `parts` CTAs where there are few rows; the parts'
 // maxima and sums meet in the first CTA's shared memory.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_forward_kernel(const DistillArgs a) {
+__global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
-    constexpr int kAhead = 4;
+    __shared__ List list;
     __shared__ Running s_warps[kWarps];
     __shared__ Running s_parts[kMaxParts];
     __shared__ float s_top[kWarps];
     __shared__ float s_sums[kWarps][2];
     const unsigned part = a.parts > 1 ? cluster_rank() : 0u;
-    const long long row = blockIdx.x / (unsigned)a.parts;
+    const long long row = a.parts > 1 ? blockIdx.x / (unsigned)a.parts : blockIdx.x;
     if (a.parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    Entries list;
+    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+    const Row<T> r(x, a.cols);
+    const T* body = x + r.head;
+    const unsigned end = r.first(part + 1, a.parts);
+    unsigned v = r.first(part, a.parts) + threadIdx.x;
+    // the first vectors are on their way while the list is looked at
+    unsigned w[kForwardAhead][8];
+    auto fetch = [&](unsigned from) {
+#pragma unroll
+        for (int u = 0; u < kForwardAhead; ++u)
+            if (from + u * kThreads < end) load_vector(body + (size_t)(from + u * kThreads) * K::kElems, w[u]);
+    };
+    fetch(v);
     const bool used = __syncthreads_or(list.load(a, row));
     if (!used) {  // the same in every part
         if (part == 0 && threadIdx.x == 0) {
@@ -183,26 +205,17 @@ __global__ void __launch_bounds__(kThreads) distill_forward_kernel(const Distill
         if (a.parts > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         return;
     }
-    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
-    float s[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) s[i] = part == 0 && list.there[i] && list.index[i] < a.cols ? load_elem(x + list.index[i]) : 0.0f;
-
-    const Row<T> r(x, a.cols);
+    if (part == 0) list.gather(a, x, [](unsigned) { return true; });
     Running run;
     if (part == 0 && threadIdx.x < r.head + r.tail) run.add(load_elem(x + r.edge(threadIdx.x)), a.k);
-    const T* body = x + r.head;
-    const unsigned end = r.first(part + 1, a.parts);
-    for (unsigned v = r.first(part, a.parts) + threadIdx.x; v < end; v += kAhead * kThreads) {
-        unsigned w[kAhead][8];
+    for (; v < end; v += kForwardAhead * kThreads) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (v + u * kThreads < end) K::load_words(body + (size_t)(v + u * kThreads) * K::kElems, K::kElems, w[u]);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kForwardAhead; ++u)
             if (v + u * kThreads < end) {
                 K k;
                 k.from_words(w[u]);
+                const unsigned next = v + (kForwardAhead + u) * kThreads;
+                if (next < end) load_vector(body + (size_t)next * K::kElems, w[u]);
                 run.add(k.v, a.k);
             }
     }
@@ -225,19 +238,19 @@ __global__ void __launch_bounds__(kThreads) distill_forward_kernel(const Distill
             asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(at));
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(run.m), "f"(run.sum) : "memory");
         }
-        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         if (part != 0) return;
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         run = s_parts[0];
         for (int p = 1; p < a.parts; ++p) run.merge(s_parts[p], a.k);
     }
-    const float tmax = list.largest(s_top);
+    const float tmax = list.largest(a, s_top);
     float sums[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (list.there[i]) {
-            const float e = expf((list.t[i] - tmax) * a.inv_T);
+    for (int k = threadIdx.x; k < a.top; k += kThreads)
+        if (list.index[k] != kNone) {
+            const float e = expf((list.t[k] - tmax) * a.inv_T);
             sums[0] += e;
-            if (e > 0.0f) sums[1] += e * (((list.t[i] - tmax) - (s[i] - run.m)) * a.inv_T);  // p log(p / q) is 0 where p is
+            if (e > 0.0f) sums[1] += e * (((list.t[k] - tmax) - (list.s[k] - run.m)) * a.inv_T);  // p log(p / q) is 0 where p is
         }
     block_sum(sums, s_sums);
     if (threadIdx.x == 0) {
@@ -251,11 +264,9 @@ __global__ void __launch_bounds__(kThreads) distill_forward_kernel(const Distill
 // of a row by the formula's first term, and then once more the columns of the list
 // that lie in it, by the whole formula: a barrier is between the two.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_backward_kernel(const DistillArgs a) {
+__global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
-    constexpr int kAhead = 4;
-    __shared__ unsigned s_index[AMPQ_DISTILL_MAX_TOP];
-    __shared__ float s_p[AMPQ_DISTILL_MAX_TOP];
+    __shared__ List list;
     __shared__ float s_top[kWarps];
     __shared__ float s_sums[kWarps][1];
     const unsigned part = blockIdx.x % (unsigned)a.parts;
@@ -264,77 +275,77 @@ __global__ void __launch_bounds__(kThreads) distill_backward_kernel(const Distil
     T* out = static_cast<T*>(a.gs) + row * a.ld_gs;
     const Row<T> r(x, a.cols);
     const unsigned begin = r.first(part, a.parts), end = r.first(part + 1, a.parts);
-    Entries list;
+    const T* body = x + r.head;
+    T* to = out + r.head;
+    const bool alike = (reinterpret_cast<uintptr_t>(to) & 31) == 0;  // the gradient's row lies to the boundaries as the logits' does
+    unsigned v = begin + threadIdx.x;
+    unsigned w[kBackwardAhead][8];
+#pragma unroll
+    for (int u = 0; u < kBackwardAhead; ++u)
+        if (v + u * kThreads < end) load_vector(body + (size_t)(v + u * kThreads) * K::kElems, w[u]);
     const bool used = __syncthreads_or(list.load(a, row));
+    auto write = [&](unsigned at, const K& k) {
+        if (alike) {
+            unsigned o[8];
+            k.to_words(o);
+            store_vector(to + (size_t)at * K::kElems, o);
+        } else {
+            k.store(to + (size_t)at * K::kElems, K::kElems);
+        }
+    };
     if (!used) {
         K zero;
         zero.zero();
         if (part == 0 && threadIdx.x < r.head + r.tail) store_elem(out + r.edge(threadIdx.x), 0.0f);
-        for (unsigned v = begin + threadIdx.x; v < end; v += kThreads) zero.store(out + r.head + (size_t)v * K::kElems, K::kElems);
+        for (; v < end; v += kThreads) write(v, zero);
         return;
     }
-    float s[kPer];
-    bool mine[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const unsigned at = list.index[i] - r.head, v = at / K::kElems;  // columns before the vectors wrap round
-        const bool in_vectors = list.index[i] >= r.head && v < r.vectors;
-        mine[i] = list.there[i] && list.index[i] < a.cols && (in_vectors ? v >= begin && v < end : part == 0);
-        s[i] = mine[i] ? load_elem(x + list.index[i]) : 0.0f;
-    }
+    auto mine = [&](unsigned j) {  // a column of this part
+        const unsigned at = (j - r.head) / K::kElems;
+        return j >= r.head && at < r.vectors ? at >= begin && at < end : part == 0;
+    };
+    list.gather(a, x, mine);
     const float m = a.stats[2 * row], inv = 1.0f / a.stats[2 * row + 1];
     const float c = a.gl[row * a.gl_stride] * a.T, ci = c * inv;
     if (part == 0 && threadIdx.x < r.head + r.tail) {
         const unsigned j = r.edge(threadIdx.x);
         store_elem(out + j, exp2_fast((load_elem(x + j) - m) * a.k) * ci);
     }
-    for (unsigned v = begin + threadIdx.x; v < end; v += kAhead * kThreads) {
-        unsigned w[kAhead][8];
+    for (; v < end; v += kBackwardAhead * kThreads) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (v + u * kThreads < end) K::load_words(x + r.head + (size_t)(v + u * kThreads) * K::kElems, K::kElems, w[u]);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kBackwardAhead; ++u)
             if (v + u * kThreads < end) {
                 K k;
                 k.from_words(w[u]);
+                const unsigned next = v + (kBackwardAhead + u) * kThreads;
+                if (next < end) load_vector(body + (size_t)next * K::kElems, w[u]);
 #pragma unroll
                 for (int i = 0; i < K::kElems / 2; ++i) {
                     const float2 d = __fmul2_rn(__fadd2_rn(k.v[i], make_float2(-m, -m)), make_float2(a.k, a.k));
                     k.v[i] = __fmul2_rn(make_float2(exp2_fast(d.x), exp2_fast(d.y)), make_float2(ci, ci));
                 }
-                k.store(out + r.head + (size_t)(v + u * kThreads) * K::kElems, K::kElems);
+                write(v + u * kThreads, k);
             }
     }
-    const float tmax = list.largest(s_top);
-    float sums[1] = {0.0f}, e[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        e[i] = list.there[i] ? expf((list.t[i] - tmax) * a.inv_T) : 0.0f;
-        sums[0] += e[i];
+    const float tmax = list.largest(a, s_top);
+    float sums[1] = {0.0f};
+    for (int k = threadIdx.x; k < a.top; k += kThreads) {
+        list.t[k] = list.index[k] != kNone ? expf((list.t[k] - tmax) * a.inv_T) : 0.0f;
+        sums[0] += list.t[k];
     }
     block_sum(sums, s_sums);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int k = threadIdx.x + kThreads * i;
-        if (k < a.top) {
-            s_index[k] = list.there[i] ? list.index[i] : 0xFFFFFFFFu;
-            s_p[k] = e[i] / sums[0];
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        if (!mine[i]) continue;
-        const int k = threadIdx.x + kThreads * i;
-        float p = 0.0f;
+    const float inv_sum = 1.0f / sums[0];
+    for (int k = threadIdx.x; k < a.top; k += kThreads) {
+        const unsigned j = list.index[k];
+        if (j >= a.cols || !mine(j)) continue;
+        float e = 0.0f;
         bool again = false;  // an earlier entry of the same column stores it
-        for (int j = 0; j < a.top; ++j)
-            if (s_index[j] == list.index[i]) {
-                p += s_p[j];
-                again |= j < k;
+        for (int i = 0; i < a.top; ++i)
+            if (list.index[i] == j) {
+                e += list.t[i];
+                again |= i < k;
             }
-        if (!again) store_elem(out + list.index[i], (exp2_fast((s[i] - m) * a.k) * inv - p) * c);
+        if (!again) store_elem(out + j, (exp2_fast((list.s[k] - m) * a.k) * inv - e * inv_sum) * c);
     }
 }
 
