@@ -21,6 +21,11 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
+// CTAs that share an SM
+template <int V>
+constexpr int kForwardCtas = V >= 4 ? 3 : 2;
+constexpr int kBackwardCtas = 2;
+constexpr int kMaxRun = 4;  // steps of a run
 
 struct Side {  // queries or keys
     const void *x, *gy, *w;
@@ -36,176 +41,196 @@ struct HeadArgs {
     const float *cos, *sin;
     const void* positions;
     float* part;
-    long long rows, tokens, angles, position_batch;  // rows: batch * tokens
-    int cols, half, lanes, vectors, runs, pitch;      // half: rot / 2; vectors: pairs of vectors of a head
+    long long position_batch;
+    unsigned rows, tokens;  // rows: batch * tokens
+    long long angles;
+    int cols, half, lanes, vectors, pitch;  // half: rot / 2; vectors: pairs of vectors of a head
+    int run, runs[2];                       // steps of a run of heads, runs of a token's queries and keys
     float eps, inv_cols;
     bool param_bf16, wide, e4m3, sums;
     bool lane_groups;  // a checkpoint's groups are whole vectors of neighbouring lanes
 };
 
-// V neighbouring elements, aligned to their size.
-template <typename T, int V>
-__device__ __forceinline__ void load_vec(const T* p, float (&v)[V]) {
-    constexpr int B = V * (int)sizeof(T);
-    if constexpr (B == 16) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
-        const unsigned w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                v[i] = __uint_as_float(w[i]);
-            } else {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        }
-    } else if constexpr (B == 8) {
-        const float2 q = __ldg(reinterpret_cast<const float2*>(p));
-        v[0] = q.x;
-        v[1] = q.y;
-    } else if constexpr (V == 2) {
-        const unsigned q = __ldg(reinterpret_cast<const unsigned*>(p));
-        v[0] = __uint_as_float(q << 16);
-        v[1] = __uint_as_float(q & 0xFFFF0000u);
-    } else {
-        v[0] = load_elem(p);
-    }
-}
+// V neighbouring elements of T as they lie in memory, aligned to their size, and as
+// pairs in fp32 (with V = 1 half a pair).
+template <int V>
+constexpr int kPairs = (V + 1) / 2;
 
 template <typename T, int V>
-__device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
+struct Raw {
+    static constexpr int B = V * (int)sizeof(T), W = (B + 3) / 4;
+    unsigned w[W];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (B == 16) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (B == 8) {
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+            w[0] = q.x; w[1] = q.y;
+        } else if constexpr (B == 4) {
+            w[0] = __ldg(reinterpret_cast<const unsigned*>(p));
+        } else {
+            w[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void unpack(float2 (&v)[kPairs<V>]) const {
+#pragma unroll
+        for (int i = 0; i < kPairs<V>; ++i) {
+            if constexpr (sizeof(T) == 4)
+                v[i] = make_float2(__uint_as_float(w[2 * i]), V == 1 ? 0.0f : __uint_as_float(w[(2 * i + 1) % W]));
+            else
+                v[i] = make_float2(__uint_as_float(w[i] << 16), V == 1 ? 0.0f : __uint_as_float(w[i] & 0xFFFF0000u));
+        }
+    }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T* p, const float2 (&v)[kPairs<V>]) {
     constexpr int B = V * (int)sizeof(T);
-    if constexpr (B == 16 && sizeof(T) == 4)
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    if constexpr (V == 1)
+        store_elem(p, v[0].x);
+    else if constexpr (sizeof(T) == 4 && B == 16)
+        *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    else if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float2*>(p) = v[0];
     else if constexpr (B == 16)
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
     else if constexpr (B == 8)
-        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
-    else if constexpr (V == 2)
-        *reinterpret_cast<unsigned*>(p) = pack_bf16(v[0], v[1]);
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y));
     else
-        store_elem(p, v[0]);
+        *reinterpret_cast<unsigned*>(p) = pack_bf16(v[0].x, v[0].y);
 }
 
 // V codes of FP8, element 0 in the lowest byte.
 template <int V>
-__device__ __forceinline__ void load_code_vec(const unsigned char* p, bool e4m3, float scale, float (&v)[V]) {
-    uint2 c = make_uint2(0, 0);
-    if constexpr (V == 8) c = __ldg(reinterpret_cast<const uint2*>(p));
-    if constexpr (V == 4) c.x = __ldg(reinterpret_cast<const unsigned*>(p));
-    if constexpr (V == 2) c.x = __ldg(reinterpret_cast<const unsigned short*>(p));
-    if constexpr (V == 1) c.x = __ldg(p);
-    float f[8];
-    if (e4m3)
-        decode8<AMPQ_FMT_E4M3>(c, f);
-    else
-        decode8<AMPQ_FMT_E5M2>(c, f);
+struct RawCodes {
+    uint2 c;
+    __device__ __forceinline__ void load(const unsigned char* p) {
+        c = make_uint2(0, 0);
+        if constexpr (V == 8) c = __ldg(reinterpret_cast<const uint2*>(p));
+        if constexpr (V == 4) c.x = __ldg(reinterpret_cast<const unsigned*>(p));
+        if constexpr (V == 2) c.x = __ldg(reinterpret_cast<const unsigned short*>(p));
+        if constexpr (V == 1) c.x = __ldg(p);
+    }
+    __device__ __forceinline__ void unpack(bool e4m3, float scale, float2 (&v)[kPairs<V>]) const {
+        float f[8];
+        if (e4m3)
+            decode8<AMPQ_FMT_E4M3>(c, f);
+        else
+            decode8<AMPQ_FMT_E5M2>(c, f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = f[i] * scale;
-}
+        for (int i = 0; i < kPairs<V>; ++i) v[i] = __fmul2_rn(make_float2(f[2 * i], V == 1 ? 0.0f : f[2 * i + 1]), make_float2(scale, scale));
+    }
+};
 
 template <int V>
-__device__ __forceinline__ void store_code_vec(unsigned char* p, bool e4m3, unsigned byte, const float (&v)[V]) {
+__device__ __forceinline__ void store_code_vec(unsigned char* p, bool e4m3, unsigned byte, const float2 (&v)[kPairs<V>]) {
     const float inv = inv_scale_of(byte);
-    unsigned short c[V / 2 + 1];
+    unsigned c[kPairs<V>];
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-        const float lo = v[i] * inv, hi = i + 1 < V ? v[(i + 1) % V] * inv : 0.0f;
+    for (int i = 0; i < kPairs<V>; ++i) {
+        const float2 f = __fmul2_rn(v[i], make_float2(inv, inv));
+        unsigned short h;
         if (e4m3)
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c[i / 2]) : "f"(hi), "f"(lo));
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(f.y), "f"(f.x));
         else
-            asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(c[i / 2]) : "f"(hi), "f"(lo));
-        if (byte == kNanScale) c[i / 2] = 0;
+            asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(h) : "f"(f.y), "f"(f.x));
+        c[i] = byte == kNanScale ? 0u : h;
     }
-    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | (unsigned)c[1] << 16, c[2] | (unsigned)c[3] << 16);
-    if constexpr (V == 4) *reinterpret_cast<unsigned*>(p) = c[0] | (unsigned)c[1] << 16;
-    if constexpr (V == 2) *reinterpret_cast<unsigned short*>(p) = c[0];
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    if constexpr (V == 4) *reinterpret_cast<unsigned*>(p) = c[0] | c[1] << 16;
+    if constexpr (V == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)c[0];
     if constexpr (V == 1) *p = (unsigned char)c[0];
 }
 
-// Columns of a thread's j-th pair of vectors, and the angle that its first pair has
-// (-1: not turned).
+// Columns of a thread's j-th two vectors, and the first of their V angles (-1: not turned).
 struct Columns {
-    int a, b, angle;
+    int col[2], angle;
 };
 template <int V, bool NEXT>
 __device__ __forceinline__ Columns columns_of(const HeadArgs& p, int j) {
     const int turned = p.half / V;  // pairs of vectors that are turned
-    if (NEXT) return Columns{2 * V * j, 2 * V * j + V, j < turned ? V * j : -1};
-    if (j < turned) return Columns{V * j, p.half + V * j, V * j};
+    if (NEXT) return Columns{{2 * V * j, 2 * V * j + V}, j < turned ? V * j : -1};
+    if (j < turned) return Columns{{V * j, p.half + V * j}, V * j};
     const int rest = (p.cols - 2 * p.half) / 2, at = 2 * p.half + V * (j - turned);
-    return Columns{at, at + rest, -1};
+    return Columns{{at, at + rest}, -1};
 }
 
-// The elements as pairs: x[i] and y[i] are turned into one another.
+// The elements that those of vector m are turned with, where the pairs are neighbours
+// (each float2 is one) and where they are halves of the head.
 template <int V, bool NEXT>
-__device__ __forceinline__ void to_pairs(float (&x)[V], float (&y)[V]) {
-    if (!NEXT || V == 1) return;
-    float e[2 * V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        e[i] = x[i];
-        e[V + i] = y[i];
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        x[i] = e[2 * i];
-        y[i] = e[2 * i + 1];
-    }
-}
-template <int V, bool NEXT>
-__device__ __forceinline__ void from_pairs(float (&x)[V], float (&y)[V]) {
-    if (!NEXT || V == 1) return;
-    float e[2 * V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        e[2 * i] = x[i];
-        e[2 * i + 1] = y[i];
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        x[i] = e[i];
-        y[i] = e[V + i];
-    }
+__device__ __forceinline__ float2 partner(const float2 (&v)[2][kPairs<V>], int m, int i) {
+    if (NEXT && V > 1) return make_float2(v[m][i].y, v[m][i].x);
+    return v[1 - m][i];
 }
 
-// Angles of a token for a thread's pairs.  A position outside the table has NaN.
-template <int V>
-__device__ __forceinline__ void load_angles(const HeadArgs& p, long long position, int angle, float (&c)[V], float (&s)[V]) {
-    const bool known = position >= 0 && position < p.angles;
-    const long long at = position * p.half + angle;
+// Cosines and sines of a token for a thread's V angles, as factors of its elements:
+// turned value = own * c + partner * s.  `back` turns the other way.  A position
+// outside the table has NaN.
+template <int V, bool NEXT>
+__device__ __forceinline__ void load_angles(const HeadArgs& p, long long position, int angle, bool back, float2 (&c)[2][kPairs<V>], float2 (&s)[2][kPairs<V>]) {
+    float cv[V], sv[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        c[i] = angle < 0 ? 1.0f : NAN;
-        s[i] = angle < 0 ? 0.0f : NAN;
-    }
-    if (angle < 0 || !known) return;
-    if constexpr (V >= 4) {
-        if ((p.half & 3) == 0) {  // rows of the table on 16-byte boundaries (its base is)
+    for (int i = 0; i < V; ++i) cv[i] = sv[i] = NAN;
+    if (position >= 0 && position < p.angles) {
+        const float *cp = p.cos + position * p.half + angle, *sp = p.sin + position * p.half + angle;
+        if (V >= 4 && (p.half & 3) == 0) {  // rows of the table on 16-byte boundaries (its base is)
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
-                const float4 f = __ldg(reinterpret_cast<const float4*>(p.cos + at + i)), g = __ldg(reinterpret_cast<const float4*>(p.sin + at + i));
-                c[i] = f.x; c[i + 1] = f.y; c[(i + 2) % V] = f.z; c[(i + 3) % V] = f.w;
-                s[i] = g.x; s[i + 1] = g.y; s[(i + 2) % V] = g.z; s[(i + 3) % V] = g.w;
+                const float4 f = __ldg(reinterpret_cast<const float4*>(cp + i)), g = __ldg(reinterpret_cast<const float4*>(sp + i));
+                cv[i] = f.x; cv[(i + 1) % V] = f.y; cv[(i + 2) % V] = f.z; cv[(i + 3) % V] = f.w;
+                sv[i] = g.x; sv[(i + 1) % V] = g.y; sv[(i + 2) % V] = g.z; sv[(i + 3) % V] = g.w;
             }
-            return;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                cv[i] = __ldg(cp + i);
+                sv[i] = __ldg(sp + i);
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        c[i] = __ldg(p.cos + at + i);
-        s[i] = __ldg(p.sin + at + i);
-    }
-}
-
-template <int V>
-__device__ __forceinline__ void load_weights(const HeadArgs& p, const void* w, int col, float (&v)[V]) {
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = w ? load_param(w, col + i, p.param_bf16) : 1.0f;
+        for (int i = 0; i < kPairs<V>; ++i) {
+            if (NEXT && V > 1) {
+                const float x = cv[(m * V / 2 + i) % V], y = sv[(m * V / 2 + i) % V];
+                c[m][i] = make_float2(x, x);
+                s[m][i] = back ? make_float2(y, -y) : make_float2(-y, y);
+            } else {
+                const float2 y = make_float2(sv[2 * i], sv[(2 * i + 1) % V]);
+                c[m][i] = make_float2(cv[2 * i], cv[(2 * i + 1) % V]);
+                s[m][i] = (m == 0) != back ? make_float2(-y.x, -y.y) : y;
+            }
+        }
 }
 
-__device__ __forceinline__ long long position_of(const HeadArgs& p, long long batch, long long token) {
-    return p.positions ? load_index(p.positions, batch * p.position_batch + token, p.wide) : token;
+// The weights of both sides in shared memory, in fp32.
+__device__ __forceinline__ void stage_weights(const HeadArgs& a, float (*w)[kHeadCols]) {
+    for (int k = threadIdx.x; k < 2 * a.cols; k += kThreads) {
+        const int side = k >= a.cols, c = k - side * a.cols;
+        w[side][c] = a.side[side].w ? load_param(a.side[side].w, c, a.param_bf16) : 1.0f;
+    }
+    __syncthreads();
+}
+template <int V>
+__device__ __forceinline__ void take_weights(const float* w, float2 (&v)[kPairs<V>]) {
+    if constexpr (V == 1) {
+        v[0] = make_float2(w[0], 0.0f);
+    } else if constexpr (V == 2) {
+        v[0] = make_float2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(w + i);  // columns of a vector begin at a multiple of V
+            v[i / 2] = make_float2(f.x, f.y);
+            v[i / 2 + 1] = make_float2(f.z, f.w);
+        }
+    }
 }
 
 // Sum over the `lanes` neighbouring lanes of a head.
@@ -214,268 +239,353 @@ __device__ __forceinline__ float head_sum(float s, int lanes) {
     return s;
 }
 
+// A warp's share: one run of heads (of the queries or of the keys) of every
+// `stride`-th token, so that what goes with the columns is set up once.
+struct Share {
+    int side, step0, steps;
+    unsigned row, stride;
+    bool some;
+    __device__ __forceinline__ Share(const HeadArgs& a, unsigned warp_of_grid, int per) {
+        const unsigned runs = (unsigned)(a.runs[0] + a.runs[1]), warps = gridDim.x * kWarps;
+        unsigned run = warp_of_grid % runs;
+        row = warp_of_grid / runs;
+        stride = warps / runs;
+        some = row < stride && row < a.rows;  // the last few warps may have none
+        side = run >= (unsigned)a.runs[0];
+        if (side) run -= (unsigned)a.runs[0];
+        step0 = (int)run * a.run;
+        steps = min(a.run, (a.side[side].heads + per - 1) / per - step0);
+    }
+};
+
+__device__ __forceinline__ long long position_of(const HeadArgs& a, unsigned row) {
+    if (!a.positions) return row % a.tokens;
+    const unsigned batch = row / a.tokens;
+    return load_index(a.positions, (long long)batch * a.position_batch + (row - batch * a.tokens), a.wide);
+}
+
 // ---------------------------------------------------------------------------
 
-// A warp takes a run of heads of one token (a.runs runs cover queries and keys), so
-// that its angles are read once.
 template <typename T, int V, int NV, bool NEXT, bool KEPT>
-__global__ void __launch_bounds__(kThreads) head_norm_forward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_kernel(const HeadArgs a) {
+    constexpr int P = kPairs<V>;
+    __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ unsigned s_amax[kWarps][64];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const long long task = (long long)blockIdx.x * kWarps + warp;
-    if (task >= a.rows * a.runs) return;
-    const long long row = task / a.runs;
-    const int run = (int)(task - row * a.runs);
-    const long long batch = row / a.tokens, token = row - batch * a.tokens;
     const int per = 32 / a.lanes, sub = lane % a.lanes, slot = lane / a.lanes;  // heads of a warp; this lane's place in its head
-    const int steps0 = (a.side[0].heads + per - 1) / per, steps1 = (a.side[1].heads + per - 1) / per, steps = steps0 + steps1;
-    const int from = (int)((long long)steps * run / a.runs), to = (int)((long long)steps * (run + 1) / a.runs);
-    const long long position = a.half > 0 ? position_of(a, batch, token) : 0;
-
+    stage_weights(a, s_w);
+    const Share mine(a, blockIdx.x * kWarps + warp, per);
+    if (!mine.some) return;
+    const Side& q = a.side[mine.side];
     Columns col[NV];
-    float c[NV][V], s[NV][V], wx[NV][V], wy[NV][V];
+    bool ok[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         col[i] = columns_of<V, NEXT>(a, sub + a.lanes * i);
-        if (sub + a.lanes * i < a.vectors) load_angles<V>(a, position, col[i].angle, c[i], s[i]);
+        ok[i] = sub + a.lanes * i < a.vectors;
     }
-    int side = -1;
-    for (int step = from; step < to; ++step) {
-        if (side < 0 || (side == 0 && step >= steps0)) {
-            side = step >= steps0;
+    Raw<T, V> raw[NV][2];
+    auto fetch = [&](unsigned row, int step) {
+        const unsigned batch = row / a.tokens;
+        const int head = (mine.step0 + step) * per + slot;
+        const T* in = static_cast<const T*>(q.x) + batch * q.x_batch + (row - batch * a.tokens) * q.x_token + head * q.x_head;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                raw[i][m].zero();
+                if (head < q.heads && ok[i]) raw[i][m].load(in + col[i].col[m]);
+            }
+    };
+    fetch(mine.row, 0);
+    long long position = a.half > 0 ? position_of(a, mine.row) : 0;
+    for (unsigned row = mine.row; row < a.rows; row += mine.stride) {
+        const unsigned next = row + mine.stride < a.rows ? row + mine.stride : row;  // rows < 2^31
+        const long long here = position;
+        if (a.half > 0) position = position_of(a, next);
+        // y = rstd * (own * f + partner * g): the weights times the cosines and sines of this token
+        float2 f[NV][2][P], g[NV][2][P];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float2 w[2][P];
+            if (!ok[i]) continue;
+            take_weights<V>(s_w[mine.side] + col[i].col[0], w[0]);
+            take_weights<V>(s_w[mine.side] + col[i].col[1], w[1]);
+            if (col[i].angle >= 0) load_angles<V, NEXT>(a, here, col[i].angle, false, f[i], g[i]);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    if (col[i].angle >= 0) {
+                        f[i][m][k] = __fmul2_rn(f[i][m][k], w[m][k]);
+                        g[i][m][k] = __fmul2_rn(g[i][m][k], partner<V, NEXT>(w, m, k));
+                    } else {
+                        f[i][m][k] = w[m][k];
+                    }
+                }
+        }
+        const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
+        for (int step = 0; step < mine.steps; ++step) {
+            const int head = (mine.step0 + step) * per + slot;
+            const bool live = head < q.heads;
+            float2 x[NV][2][P];
+            float2 sq = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (sub + a.lanes * i < a.vectors) {
-                    load_weights<V>(a, a.side[side].w, col[i].a, wx[i]);
-                    load_weights<V>(a, a.side[side].w, col[i].b, wy[i]);
-                    to_pairs<V, NEXT>(wx[i], wy[i]);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    raw[i][m].unpack(x[i][m]);
+#pragma unroll
+                    for (int k = 0; k < P; ++k) sq = __ffma2_rn(x[i][m][k], x[i][m][k], sq);
                 }
-        }
-        const Side& q = a.side[side];
-        const int head = (step - (side ? steps0 : 0)) * per + slot;
-        const bool live = head < q.heads;
-        const T* in = static_cast<const T*>(q.x) + batch * q.x_batch + token * q.x_token + head * q.x_head;
-        float x[NV][V], y[NV][V];
-        float sum = 0.0f;
+            // the next step's elements, or the next token's
+            if (step + 1 < mine.steps)
+                fetch(row, step + 1);
+            else if (next != row)
+                fetch(next, 0);
+            const float rstd = 1.0f / sqrtf(head_sum(sq.x + sq.y, a.lanes) * a.inv_cols + a.eps);
+            const long long at = (long long)row * q.heads + head;  // row of the statistics and of the checkpoint
+            if (live && sub == 0) q.rstd[at] = rstd;
+            if (KEPT) {
+                // bits of the largest |x| of each group of 32 columns, a NaN on top
+                unsigned top[NV][2];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+                for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int k = 0; k < V; ++k) x[i][k] = y[i][k] = 0.0f;
-            if (live && sub + a.lanes * i < a.vectors) {
-                load_vec<T, V>(in + col[i].a, x[i]);
-                load_vec<T, V>(in + col[i].b, y[i]);
+                    for (int m = 0; m < 2; ++m) {
+                        float t = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < P; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x[i][m][k].x), "f"(x[i][m][k].y));
+                        top[i][m] = __float_as_uint(t) & 0x7FFFFFFFu;
+                    }
+                if (a.lane_groups) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        if (NEXT) top[i][0] = max(top[i][0], top[i][1]);
+#pragma unroll
+                        for (int o = (NEXT ? kGroup / 2 : kGroup) / V / 2; o > 0; o >>= 1) {
+                            top[i][0] = max(top[i][0], __shfl_xor_sync(0xFFFFFFFFu, top[i][0], o));
+                            if (!NEXT) top[i][1] = max(top[i][1], __shfl_xor_sync(0xFFFFFFFFu, top[i][1], o));
+                        }
+                        if (NEXT) top[i][1] = top[i][0];
+                    }
+                } else {
+                    unsigned* amax = s_amax[warp] + slot * ((a.cols + kGroup - 1) / kGroup);
+                    __syncwarp();
+                    s_amax[warp][lane] = s_amax[warp][lane + 32] = 0;
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            if (live && ok[i]) atomicMax(amax + col[i].col[m] / kGroup, top[i][m]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            if (live && ok[i]) top[i][m] = amax[col[i].col[m] / kGroup];
+                }
+                if (live) {
+                    unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            if (!ok[i]) continue;
+                            const int c0 = col[i].col[m];
+                            const unsigned byte = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(top[i][m]) : scale_byte<AMPQ_FMT_E5M2>(top[i][m]);
+                            store_code_vec<V>(codes + c0, a.e4m3, byte, x[i][m]);
+                            if (c0 % kGroup == 0) scales[c0 / kGroup] = (unsigned char)byte;  // by whoever holds a group's first column
+                        }
+                    for (int k = a.cols + sub; k < (a.cols + kGroup - 1) / kGroup * kGroup; k += a.lanes) codes[k] = 0;
+                }
             }
-#pragma unroll
-            for (int k = 0; k < V; ++k) sum += x[i][k] * x[i][k] + y[i][k] * y[i][k];
-        }
-        const float rstd = 1.0f / sqrtf(head_sum(sum, a.lanes) * a.inv_cols + a.eps);
-        const long long at = row * q.heads + head;  // row of the statistics and of the checkpoint
-        if (live && sub == 0) q.rstd[at] = rstd;
-        if (KEPT) {
-            // largest |x| of each group of 32 columns: an integer maximum of the bits, a NaN on top
-            unsigned mx[NV], my[NV];
+            if (!live) continue;
+            T* out = static_cast<T*>(q.out) + batch * q.out_batch + token * q.out_token + head * q.out_head;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                mx[i] = my[i] = 0;
+                if (!ok[i]) continue;
+                float2 y[2][P];
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    mx[i] = max(mx[i], __float_as_uint(x[i][k]) & 0x7FFFFFFFu);
-                    my[i] = max(my[i], __float_as_uint(y[i][k]) & 0x7FFFFFFFu);
-                }
-            }
-            if (a.lane_groups) {
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (NEXT) mx[i] = my[i] = max(mx[i], my[i]);
-                    for (int o = (NEXT ? kGroup / 2 : kGroup) / V / 2; o > 0; o >>= 1) {
-                        mx[i] = max(mx[i], __shfl_xor_sync(0xFFFFFFFFu, mx[i], o));
-                        my[i] = max(my[i], __shfl_xor_sync(0xFFFFFFFFu, my[i], o));
+                    for (int k = 0; k < P; ++k) {
+                        y[m][k] = __fmul2_rn(x[i][m][k], f[i][m][k]);
+                        if (col[i].angle >= 0) y[m][k] = __ffma2_rn(partner<V, NEXT>(x[i], m, k), g[i][m][k], y[m][k]);
+                        y[m][k] = __fmul2_rn(y[m][k], make_float2(rstd, rstd));
                     }
-                }
-            } else {
-                const int groups = (a.cols + kGroup - 1) / kGroup;
-                unsigned* amax = s_amax[warp] + slot * groups;
-                __syncwarp();
-                s_amax[warp][lane] = s_amax[warp][lane + 32] = 0;
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (live && sub + a.lanes * i < a.vectors) {
-                        atomicMax(amax + col[i].a / kGroup, mx[i]);
-                        atomicMax(amax + col[i].b / kGroup, my[i]);
-                    }
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (live && sub + a.lanes * i < a.vectors) {
-                        mx[i] = amax[col[i].a / kGroup];
-                        my[i] = amax[col[i].b / kGroup];
-                    }
+                store_vec<T, V>(out + col[i].col[0], y[0]);
+                store_vec<T, V>(out + col[i].col[1], y[1]);
             }
-            if (live) {
-                unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (sub + a.lanes * i >= a.vectors) continue;
-                    const unsigned bx = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(mx[i]) : scale_byte<AMPQ_FMT_E5M2>(mx[i]);
-                    const unsigned by = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(my[i]) : scale_byte<AMPQ_FMT_E5M2>(my[i]);
-                    store_code_vec<V>(codes + col[i].a, a.e4m3, bx, x[i]);
-                    store_code_vec<V>(codes + col[i].b, a.e4m3, by, y[i]);
-                    // a group's byte by whoever holds its first column
-                    if (col[i].a % kGroup == 0) scales[col[i].a / kGroup] = (unsigned char)bx;
-                    if (col[i].b % kGroup == 0) scales[col[i].b / kGroup] = (unsigned char)by;
-                }
-                for (int k = a.cols + sub; k < (a.cols + kGroup - 1) / kGroup * kGroup; k += a.lanes) codes[k] = 0;
-            }
-        }
-        if (!live) continue;
-        T* out = static_cast<T*>(q.out) + batch * q.out_batch + token * q.out_token + head * q.out_head;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (sub + a.lanes * i >= a.vectors) continue;
-            to_pairs<V, NEXT>(x[i], y[i]);
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float nx = x[i][k] * rstd * wx[i][k], ny = y[i][k] * rstd * wy[i][k];
-                const bool turn = col[i].angle >= 0;  // 0 * Inf is not 0
-                x[i][k] = turn ? nx * c[i][k] - ny * s[i][k] : nx;
-                y[i][k] = turn ? ny * c[i][k] + nx * s[i][k] : ny;
-            }
-            from_pairs<V, NEXT>(x[i], y[i]);
-            store_vec<T, V>(out + col[i].a, x[i]);
-            store_vec<T, V>(out + col[i].b, y[i]);
         }
     }
 }
 
-// A CTA goes through tokens, the queries of all of them and then the keys, so that a
-// thread's sums for the weight's gradient stay in registers; its warps share a token's
-// heads.  part[side][CTA][column] are joined afterwards.
+// A warp's sums for the weight's gradient stay in registers over its tokens;
+// part[side][CTA][column] are joined afterwards.
 template <typename T, int V, int NV, bool NEXT, bool KEPT>
-__global__ void __launch_bounds__(kThreads) head_norm_backward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_kernel(const HeadArgs a) {
+    constexpr int P = kPairs<V>;
+    __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ float s_sums[kWarps][kHeadCols];
+    __shared__ int s_side[kWarps];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int per = 32 / a.lanes, sub = lane % a.lanes, slot = lane / a.lanes;
+    stage_weights(a, s_w);
+    const Share mine(a, blockIdx.x * kWarps + warp, per);
+    const Side& q = a.side[mine.side];
     Columns col[NV];
+    bool ok[NV];
+    float2 gw[NV][2][P], w[NV][2][P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) col[i] = columns_of<V, NEXT>(a, sub + a.lanes * i);
-    for (int side = 0; side < 2; ++side) {
-        const Side& q = a.side[side];
-        if (q.heads == 0) continue;
-        float wx[NV][V], wy[NV][V], gwx[NV][V], gwy[NV][V];
+    for (int i = 0; i < NV; ++i) {
+        col[i] = columns_of<V, NEXT>(a, sub + a.lanes * i);
+        ok[i] = sub + a.lanes * i < a.vectors;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int m = 0; m < 2; ++m) {
+            if (ok[i]) take_weights<V>(s_w[mine.side] + col[i].col[m], w[i][m]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) gwx[i][k] = gwy[i][k] = 0.0f;
-            if (sub + a.lanes * i < a.vectors) {
-                load_weights<V>(a, q.w, col[i].a, wx[i]);
-                load_weights<V>(a, q.w, col[i].b, wy[i]);
-                to_pairs<V, NEXT>(wx[i], wy[i]);
-            }
+            for (int k = 0; k < P; ++k) gw[i][m][k] = make_float2(0.0f, 0.0f);
         }
-        // a run of a token's heads to a warp, as in the forward pass
-        const int steps = (q.heads + per - 1) / per;
-        const int runs = min(a.runs, steps);
-        for (long long task = (long long)blockIdx.x * kWarps + warp; task < a.rows * runs; task += (long long)gridDim.x * kWarps) {
-            const long long row = task / runs;
-            const int run = (int)(task - row * runs);
-            const long long batch = row / a.tokens, token = row - batch * a.tokens;
-            const int from = (int)((long long)steps * run / runs), to = (int)((long long)steps * (run + 1) / runs);
-            const long long position = a.half > 0 ? position_of(a, batch, token) : 0;
-            float c[NV][V], s[NV][V];
+    }
+    if (mine.some) {
+        Raw<T, V> raw_g[NV][2], raw_x[NV][2];
+        RawCodes<V> raw_c[NV][2];
+        unsigned raw_s[NV][2];
+        float raw_r;
+        auto fetch = [&](unsigned row, int step) {
+            const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
+            const int head = (mine.step0 + step) * per + slot;
+            const bool live = head < q.heads;
+            const long long at = (long long)row * q.heads + head;
+            const T* g = static_cast<const T*>(q.gy) + batch * q.gy_batch + token * q.gy_token + head * q.gy_head;
+            const T* x = static_cast<const T*>(q.x) + batch * q.x_batch + token * q.x_token + head * q.x_head;
+            const unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
+            raw_r = live ? __ldg(q.rstd + at) : 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (sub + a.lanes * i < a.vectors) load_angles<V>(a, position, col[i].angle, c[i], s[i]);
-            for (int step = from; step < to; ++step) {
-                const int head = step * per + slot;
-                const bool live = head < q.heads;
-                const long long at = row * q.heads + head;
-                const float rstd = live ? __ldg(q.rstd + at) : 0.0f;
-                const T* g = static_cast<const T*>(q.gy) + batch * q.gy_batch + token * q.gy_token + head * q.gy_head;
-                float hx[NV][V], hy[NV][V], ux[NV][V], uy[NV][V];
-                float sum = 0.0f;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!live || sub + a.lanes * i >= a.vectors) continue;
-                    load_vec<T, V>(g + col[i].a, ux[i]);
-                    load_vec<T, V>(g + col[i].b, uy[i]);
+                for (int m = 0; m < 2; ++m) {
+                    const int c0 = col[i].col[m];
+                    raw_g[i][m].zero();
+                    raw_x[i][m].zero();
+                    raw_c[i][m].c = make_uint2(0, 0);
+                    raw_s[i][m] = 0;
+                    if (!live || !ok[i]) continue;
+                    raw_g[i][m].load(g + c0);
                     if (KEPT) {
-                        const unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
-                        load_code_vec<V>(codes + col[i].a, a.e4m3, scale_of(__ldg(scales + col[i].a / kGroup)), hx[i]);
-                        load_code_vec<V>(codes + col[i].b, a.e4m3, scale_of(__ldg(scales + col[i].b / kGroup)), hy[i]);
+                        raw_c[i][m].load(codes + c0);
+                        raw_s[i][m] = __ldg(scales + c0 / kGroup);
                     } else {
-                        const T* x = static_cast<const T*>(q.x) + batch * q.x_batch + token * q.x_token + head * q.x_head;
-                        load_vec<T, V>(x + col[i].a, hx[i]);
-                        load_vec<T, V>(x + col[i].b, hy[i]);
-                    }
-                    to_pairs<V, NEXT>(ux[i], uy[i]);
-                    to_pairs<V, NEXT>(hx[i], hy[i]);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const bool turn = col[i].angle >= 0;
-                        const float tx = turn ? ux[i][k] * c[i][k] + uy[i][k] * s[i][k] : ux[i][k];
-                        const float ty = turn ? uy[i][k] * c[i][k] - ux[i][k] * s[i][k] : uy[i][k];
-                        hx[i][k] *= rstd;
-                        hy[i][k] *= rstd;
-                        gwx[i][k] += tx * hx[i][k];
-                        gwy[i][k] += ty * hy[i][k];
-                        ux[i][k] = tx * wx[i][k];
-                        uy[i][k] = ty * wy[i][k];
-                        sum += ux[i][k] * hx[i][k] + uy[i][k] * hy[i][k];
+                        raw_x[i][m].load(x + c0);
                     }
                 }
-                const float mean = head_sum(sum, a.lanes) * a.inv_cols;
+        };
+        fetch(mine.row, 0);
+        long long position = a.half > 0 ? position_of(a, mine.row) : 0;
+        for (unsigned row = mine.row; row < a.rows; row += mine.stride) {
+            const unsigned next = row + mine.stride < a.rows ? row + mine.stride : row;
+            const long long here = position;
+            if (a.half > 0) position = position_of(a, next);
+            float2 c[NV][2][P], s[NV][2][P];
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (ok[i] && col[i].angle >= 0) load_angles<V, NEXT>(a, here, col[i].angle, true, c[i], s[i]);
+            const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
+            for (int step = 0; step < mine.steps; ++step) {
+                const int head = (mine.step0 + step) * per + slot;
+                const bool live = head < q.heads;
+                const float rstd = raw_r;
+                float2 g[NV][2][P], h[NV][2][P];
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        raw_g[i][m].unpack(g[i][m]);
+                        if (KEPT)
+                            raw_c[i][m].unpack(a.e4m3, scale_of(raw_s[i][m]), h[i][m]);
+                        else
+                            raw_x[i][m].unpack(h[i][m]);
+                    }
+                if (step + 1 < mine.steps)
+                    fetch(row, step + 1);
+                else if (next != row)
+                    fetch(next, 0);
+                float2 dot = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!live || !ok[i]) continue;
+                    float2 t[2][P];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int k = 0; k < P; ++k) {
+                            t[m][k] = g[i][m][k];
+                            if (col[i].angle >= 0) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
+                            h[i][m][k] = __fmul2_rn(h[i][m][k], make_float2(rstd, rstd));
+                            gw[i][m][k] = __ffma2_rn(t[m][k], h[i][m][k], gw[i][m][k]);
+                            t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
+                            dot = __ffma2_rn(t[m][k], h[i][m][k], dot);
+                        }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int k = 0; k < P; ++k) g[i][m][k] = t[m][k];
+                }
+                const float mean = -head_sum(dot.x + dot.y, a.lanes) * a.inv_cols;
                 if (!live) continue;
                 T* out = static_cast<T*>(q.out) + batch * q.out_batch + token * q.out_token + head * q.out_head;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    if (sub + a.lanes * i >= a.vectors) continue;
+                    if (!ok[i]) continue;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        ux[i][k] = rstd * (ux[i][k] - hx[i][k] * mean);
-                        uy[i][k] = rstd * (uy[i][k] - hy[i][k] * mean);
+                    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                        for (int k = 0; k < P; ++k)
+                            g[i][m][k] = __fmul2_rn(__ffma2_rn(h[i][m][k], make_float2(mean, mean), g[i][m][k]), make_float2(rstd, rstd));
+                        store_vec<T, V>(out + col[i].col[m], g[i][m]);
                     }
-                    from_pairs<V, NEXT>(ux[i], uy[i]);
-                    store_vec<T, V>(out + col[i].a, ux[i]);
-                    store_vec<T, V>(out + col[i].b, uy[i]);
                 }
             }
         }
-        if (!a.sums) continue;
-        __syncthreads();
+    }
+    if (!a.sums) return;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int k = 0; k < V; ++k)  // the warp's heads
-                for (int o = 16; o >= a.lanes; o >>= 1) {
-                    gwx[i][k] += __shfl_xor_sync(0xFFFFFFFFu, gwx[i][k], o);
-                    gwy[i][k] += __shfl_xor_sync(0xFFFFFFFFu, gwy[i][k], o);
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                float2 v = gw[i][m][k];
+                for (int o = 16; o >= a.lanes; o >>= 1) {  // the warp's heads
+                    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+                    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
                 }
-            from_pairs<V, NEXT>(gwx[i], gwy[i]);
-            if (slot == 0 && sub + a.lanes * i < a.vectors)
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    s_sums[warp][col[i].a + k] = gwx[i][k];
-                    s_sums[warp][col[i].b + k] = gwy[i][k];
+                if (slot == 0 && ok[i]) {
+                    s_sums[warp][col[i].col[m] + 2 * k] = v.x;
+                    if (V > 1) s_sums[warp][col[i].col[m] + 2 * k + 1] = v.y;
                 }
-        }
-        __syncthreads();
-        if ((int)threadIdx.x < a.cols) {
-            float s = 0.0f;
+            }
+    if (lane == 0) s_side[warp] = mine.side;
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * a.cols; k += kThreads) {
+        const int side = k >= a.cols, c = k - side * a.cols;
+        float v = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) s += s_sums[w][threadIdx.x];
-            a.part[((long long)side * gridDim.x + blockIdx.x) * a.pitch + threadIdx.x] = s;
-        }
+        for (int i = 0; i < kWarps; ++i)
+            if (s_side[i] == side) v += s_sums[i][c];
+        a.part[((long long)side * gridDim.x + blockIdx.x) * a.pitch + c] = v;
     }
 }
 
 // ---------------------------------------------------------------------------
 // host side
 
-// CTAs of the backward pass: enough for every run of heads, no more than are resident.
+// CTAs of the backward pass: no more than are resident, four to a token at most.
 int backward_ctas(long long rows, int sms) {
-    const long long most = 2LL * sms;
-    return (int)(rows < most ? rows : most);
+    const long long most = (long long)kBackwardCtas * sms;
+    return (int)(4 * rows < most ? 4 * rows : most);
 }
 
 int part_pitch(long long cols) { return (int)((cols + 15) / 16 * 16); }
@@ -559,17 +669,24 @@ int start(HeadArgs a, bool backward, int sms, int ctas, cudaStream_t st) {
     while (a.lanes < 32 && a.lanes < a.vectors) a.lanes *= 2;
     a.lane_groups = NEXT ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0;
     const int per = 32 / a.lanes;
-    const int steps = (a.side[0].heads + per - 1) / per + (a.side[1].heads + per - 1) / per;
-    // runs of up to eight steps, shorter ones while there are SMs without a CTA
-    a.runs = (steps + 7) / 8;
-    while (a.runs < steps && a.rows * a.runs < 2LL * sms * kWarps) a.runs = a.runs * 2 < steps ? a.runs * 2 : steps;
+    const int steps[2] = {(a.side[0].heads + per - 1) / per, (a.side[1].heads + per - 1) / per};
+    auto runs = [&] {
+        for (int s = 0; s < 2; ++s) a.runs[s] = (steps[s] + a.run - 1) / a.run;
+        return (long long)a.runs[0] + a.runs[1];
+    };
+    // Runs are of one length where that is a divisor of both sides' steps, and short
+    // while there are warps without one.
+    long long most = backward ? (long long)ctas * kWarps : (long long)kForwardCtas<V> * sms * kWarps;
+    for (a.run = kMaxRun; a.run > 1 && (steps[0] % a.run || steps[1] % a.run || a.rows * runs() < most); --a.run) {}
     if (backward) {
+        while (runs() > most) a.run *= 2;  // every run has its warp
         head_norm_backward_kernel<T, V, NV, NEXT, KEPT><<<(unsigned)ctas, kThreads, 0, st>>>(a);
         return launched();
     }
-    const long long blocks = (a.rows * a.runs + kWarps - 1) / kWarps;
-    if (blocks > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    head_norm_forward_kernel<T, V, NV, NEXT, KEPT><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    const long long total = runs();
+    if (most < total) most = total;
+    const long long need = a.rows * total < most ? a.rows * total : most;
+    head_norm_forward_kernel<T, V, NV, NEXT, KEPT><<<(unsigned)((need + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
     return launched();
 }
 
@@ -594,7 +711,7 @@ HeadArgs head_args(int param_dtype, int index_type, int fmt, long long batch, lo
     a.side[1] = side_of(k, backward, fmt != AMPQ_FMT_BASE);
     a.cos = cos; a.sin = sin;
     a.positions = positions;
-    a.rows = batch * tokens; a.tokens = tokens; a.angles = angles; a.position_batch = position_batch;
+    a.rows = (unsigned)(batch * tokens); a.tokens = (unsigned)tokens; a.angles = angles; a.position_batch = position_batch;
     a.cols = (int)cols; a.half = (int)rot / 2;
     a.inv_cols = cols > 0 ? 1.0f / (float)cols : 0.0f;
     a.pitch = part_pitch(cols);
@@ -627,7 +744,7 @@ int ampq_head_norm_forward(int device, void* cuda_stream, int dtype, int param_d
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (cols == 0) {  // the mean of nothing: NaN, all bits set
         for (const Side& s : a.side)
-            if (s.heads > 0 && s.rstd && cudaMemsetAsync(s.rstd, 0xFF, (size_t)(a.rows * s.heads) * sizeof(float), st) != cudaSuccess) {
+            if (s.heads > 0 && s.rstd && cudaMemsetAsync(s.rstd, 0xFF, (size_t)((long long)a.rows * s.heads) * sizeof(float), st) != cudaSuccess) {
                 cudaGetLastError();
                 return AMPQ_ERR_CUDA;
             }
@@ -673,13 +790,11 @@ int ampq_head_norm_backward(int device, void* cuda_stream, int dtype, int param_
                                : dispatch<__nv_bfloat16>(a, interleaved != 0, kept, true, dtype, sms, ctas, st);
         if (rc) return rc;
     }
-    for (int s = 0; s < 2; ++s) {
-        const ampq_heads* h = s ? k : q;
-        if (!h || !h->gweight) continue;
-        rc = launch_join_columns(a.part + (long long)s * ctas * a.pitch, 1, h->heads > 0 ? ctas : 0, cols, a.pitch, h->gweight, nullptr, param_dtype, st);
-        if (rc) return rc;
-    }
-    return AMPQ_OK;
+    if (!a.sums) return AMPQ_OK;
+    const int parts = a.rows > 0 && a.side[0].heads + a.side[1].heads > 0 ? ctas : 0;
+    if (q->gweight && k && k->gweight) return launch_join_columns(a.part, 2, parts, cols, a.pitch, q->gweight, k->gweight, param_dtype, st);
+    return q->gweight ? launch_join_columns(a.part, 1, parts, cols, a.pitch, q->gweight, nullptr, param_dtype, st)
+                      : launch_join_columns(a.part + (long long)parts * a.pitch, 1, parts, cols, a.pitch, k->gweight, nullptr, param_dtype, st);
 }
 
 #pragma GCC visibility pop

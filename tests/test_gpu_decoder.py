@@ -296,7 +296,11 @@ def test_queries_alone_and_other_dimensions(dec):
     assert torch.equal(three[0], yq[1]) and torch.equal(three[3], rk[1])
     g = dec.head_norm_backward(c.gq, c.gk, c.q, c.k, rq, rk, c.wq, c.wk, *c.angles())
     a = dec.head_norm_backward(c.gq, None, c.q, None, rq, None, c.wq, None, *c.angles())
-    assert torch.equal(a[0], g[0]) and torch.equal(a[2], g[2]) and a[1] is a[3] is None
+    assert torch.equal(a[0], g[0]) and a[1] is a[3] is None
+    # The weight's gradient is a sum of 72 products whose order goes by the sizes, the keys' heads among them: each of the two is
+    # off by at most (72 + 6) U of the absolute sum, as in check_heads, so they differ by twice that.
+    size = ref.head_norm_grad(f64(c.gq), f64(c.q), f64(rq), f64(c.wq), c.c, c.s, 32, False)[4]
+    within(a[2], f64(g[2]), 2 * 78 * U * size)
 
 
 def test_heads_nothing(dec):
