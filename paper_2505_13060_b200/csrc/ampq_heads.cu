@@ -23,7 +23,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
 // CTAs that share an SM
 template <int V>
-constexpr int kForwardCtas = V >= 4 ? 3 : 2;
+constexpr int kForwardCtas = 2;
 constexpr int kBackwardCtas = 2;
 constexpr int kMaxRun = 4;  // steps of a run
 
@@ -45,11 +45,21 @@ struct HeadArgs {
     unsigned rows, tokens;  // rows: batch * tokens
     long long angles;
     int cols, half, lanes, vectors, pitch;  // half: rot / 2; vectors: pairs of vectors of a head
-    int run, runs[2];                       // steps of a run of heads, runs of a token's queries and keys
+    int run[2], runs[2];                    // queries and keys: steps of a run of heads, runs of a token,
+    int ctas[2];                            // and CTAs
     float eps, inv_cols;
     bool param_bf16, wide, e4m3, sums;
     bool lane_groups;  // a checkpoint's groups are whole vectors of neighbouring lanes
 };
+
+// A kernel's format: none, one of the two, or the one that the arguments say.
+constexpr int kEither = 3;
+
+template <int FMT>
+__device__ __forceinline__ unsigned group_byte(bool e4m3, unsigned amax) {
+    if (FMT == AMPQ_FMT_E4M3 || (FMT == kEither && e4m3)) return scale_byte<AMPQ_FMT_E4M3>(amax);
+    return scale_byte<AMPQ_FMT_E5M2>(amax);
+}
 
 // V neighbouring elements of T as they lie in memory, aligned to their size, and as
 // pairs in fp32 (with V = 1 half a pair).
@@ -73,6 +83,12 @@ struct Raw {
             w[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
         }
     }
+    __device__ __forceinline__ void take(const void* smem) {
+        if constexpr (B == 16) {
+            const uint4 q = *static_cast<const uint4*>(smem);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        }
+    }
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int i = 0; i < W; ++i) w[i] = 0;
@@ -87,6 +103,25 @@ struct Raw {
         }
     }
 };
+
+// Vectors of 16 bytes come by asynchronous copies into shared memory, each thread's to
+// its own places, while the step before is worked on; smaller ones into registers.
+template <typename T, int V>
+constexpr bool kAsync = V * sizeof(T) == 16;
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* smem, const void* p) {
+    const unsigned at = (unsigned)__cvta_generic_to_shared(smem);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(p) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(p), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void commit_async() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_async() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
 
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T* p, const float2 (&v)[kPairs<V>]) {
@@ -116,9 +151,10 @@ struct RawCodes {
         if constexpr (V == 2) c.x = __ldg(reinterpret_cast<const unsigned short*>(p));
         if constexpr (V == 1) c.x = __ldg(p);
     }
+    template <int FMT>
     __device__ __forceinline__ void unpack(bool e4m3, float scale, float2 (&v)[kPairs<V>]) const {
         float f[8];
-        if (e4m3)
+        if (FMT == AMPQ_FMT_E4M3 || (FMT == kEither && e4m3))
             decode8<AMPQ_FMT_E4M3>(c, f);
         else
             decode8<AMPQ_FMT_E5M2>(c, f);
@@ -127,7 +163,7 @@ struct RawCodes {
     }
 };
 
-template <int V>
+template <int V, int FMT>
 __device__ __forceinline__ void store_code_vec(unsigned char* p, bool e4m3, unsigned byte, const float2 (&v)[kPairs<V>]) {
     const float inv = inv_scale_of(byte);
     unsigned c[kPairs<V>];
@@ -135,16 +171,17 @@ __device__ __forceinline__ void store_code_vec(unsigned char* p, bool e4m3, unsi
     for (int i = 0; i < kPairs<V>; ++i) {
         const float2 f = __fmul2_rn(v[i], make_float2(inv, inv));
         unsigned short h;
-        if (e4m3)
+        if (FMT == AMPQ_FMT_E4M3 || (FMT == kEither && e4m3))
             asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(f.y), "f"(f.x));
         else
             asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(h) : "f"(f.y), "f"(f.x));
-        c[i] = byte == kNanScale ? 0u : h;
+        c[i] = h;
     }
-    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-    if constexpr (V == 4) *reinterpret_cast<unsigned*>(p) = c[0] | c[1] << 16;
-    if constexpr (V == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)c[0];
-    if constexpr (V == 1) *p = (unsigned char)c[0];
+    const unsigned keep = byte == kNanScale ? 0u : 0xFFFFFFFFu;
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2((c[0] | c[1] << 16) & keep, (c[2] | c[3] << 16) & keep);
+    if constexpr (V == 4) *reinterpret_cast<unsigned*>(p) = (c[0] | c[1] << 16) & keep;
+    if constexpr (V == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)(c[0] & keep);
+    if constexpr (V == 1) *p = (unsigned char)(c[0] & keep);
 }
 
 // Columns of a thread's j-th two vectors, and the first of their V angles (-1: not turned).
@@ -152,11 +189,11 @@ struct Columns {
     int col[2], angle;
 };
 template <int V, bool NEXT>
-__device__ __forceinline__ Columns columns_of(const HeadArgs& p, int j) {
-    const int turned = p.half / V;  // pairs of vectors that are turned
+__device__ __forceinline__ Columns columns_of(int cols, int half, int j) {
+    const int turned = half / V;  // pairs of vectors that are turned
     if (NEXT) return Columns{{2 * V * j, 2 * V * j + V}, j < turned ? V * j : -1};
-    if (j < turned) return Columns{{V * j, p.half + V * j}, V * j};
-    const int rest = (p.cols - 2 * p.half) / 2, at = 2 * p.half + V * (j - turned);
+    if (j < turned) return Columns{{V * j, half + V * j}, V * j};
+    const int rest = (cols - 2 * half) / 2, at = 2 * half + V * (j - turned);
     return Columns{{at, at + rest}, -1};
 }
 
@@ -172,13 +209,13 @@ __device__ __forceinline__ float2 partner(const float2 (&v)[2][kPairs<V>], int m
 // turned value = own * c + partner * s.  `back` turns the other way.  A position
 // outside the table has NaN.
 template <int V, bool NEXT>
-__device__ __forceinline__ void load_angles(const HeadArgs& p, long long position, int angle, bool back, float2 (&c)[2][kPairs<V>], float2 (&s)[2][kPairs<V>]) {
+__device__ __forceinline__ void load_angles(const HeadArgs& p, int half, long long position, int angle, bool back, float2 (&c)[2][kPairs<V>], float2 (&s)[2][kPairs<V>]) {
     float cv[V], sv[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) cv[i] = sv[i] = NAN;
     if (position >= 0 && position < p.angles) {
-        const float *cp = p.cos + position * p.half + angle, *sp = p.sin + position * p.half + angle;
-        if (V >= 4 && (p.half & 3) == 0) {  // rows of the table on 16-byte boundaries (its base is)
+        const float *cp = p.cos + position * half + angle, *sp = p.sin + position * half + angle;
+        if (V >= 4 && (half & 3) == 0) {  // rows of the table on 16-byte boundaries (its base is)
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
                 const float4 f = __ldg(reinterpret_cast<const float4*>(cp + i)), g = __ldg(reinterpret_cast<const float4*>(sp + i));
@@ -235,99 +272,181 @@ __device__ __forceinline__ void take_weights(const float* w, float2 (&v)[kPairs<
 
 // Sum over the `lanes` neighbouring lanes of a head.
 __device__ __forceinline__ float head_sum(float s, int lanes) {
-    for (int o = lanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float t = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        s = o < lanes ? s + t : s;
+    }
     return s;
 }
 
+// 1 / sqrt(v), the hardware's approximation improved by one of Newton's steps, to
+// within an ulp; 0 of infinity and infinity of 0.
+__device__ __forceinline__ float inverse_root(float v) {
+    float r;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    const float e = fmaf(-v * r, r, 1.0f);  // NaN where r is not a number that can be improved
+    const float better = fmaf(0.5f * r, e, r);
+    return better == better ? better : r;
+}
+
 // A warp's share: one run of heads (of the queries or of the keys) of every
-// `stride`-th token, so that what goes with the columns is set up once.
+// `stride`-th token, so that what goes with the columns is set up once.  The grid's
+// first CTAs have queries, the others keys, by how many steps there are of each.  It
+// walks over its rows, whose batch and token are kept up to date.
 struct Share {
-    int side, step0, steps;
-    unsigned row, stride;
+    int side, head0, steps;  // head0: the first head of this lane
+    unsigned row, stride, batch, token;
     bool some;
-    __device__ __forceinline__ Share(const HeadArgs& a, unsigned warp_of_grid, int per) {
-        const unsigned runs = (unsigned)(a.runs[0] + a.runs[1]), warps = gridDim.x * kWarps;
-        unsigned run = warp_of_grid % runs;
-        row = warp_of_grid / runs;
-        stride = warps / runs;
+    __device__ __forceinline__ Share(const HeadArgs& a, unsigned warp, int per, int slot) {
+        side = (int)blockIdx.x >= a.ctas[0];
+        warp += (blockIdx.x - (side ? a.ctas[0] : 0)) * kWarps;
+        const unsigned runs = (unsigned)a.runs[side];
+        stride = (unsigned)a.ctas[side] * kWarps / runs;
+        row = warp / runs;
         some = row < stride && row < a.rows;  // the last few warps may have none
-        side = run >= (unsigned)a.runs[0];
-        if (side) run -= (unsigned)a.runs[0];
-        step0 = (int)run * a.run;
-        steps = min(a.run, (a.side[side].heads + per - 1) / per - step0);
+        const int step0 = (int)(warp % runs) * a.run[side];
+        head0 = step0 * per + slot;
+        steps = min(a.run[side], (a.side[side].heads + per - 1) / per - step0);
+        batch = row / a.tokens;
+        token = row - batch * a.tokens;
+    }
+    __device__ __forceinline__ bool last(const HeadArgs& a) const { return row + stride >= a.rows; }  // rows < 2^31
+    __device__ __forceinline__ void advance(const HeadArgs& a) {
+        row += stride;
+        token += stride;
+        if (token >= a.tokens) {
+            const unsigned more = token / a.tokens;
+            batch += more;
+            token -= more * a.tokens;
+        }
+    }
+    __device__ __forceinline__ long long position(const HeadArgs& a) const {
+        return a.positions ? load_index(a.positions, (long long)batch * a.position_batch + token, a.wide) : (long long)token;
+    }
+    template <typename T>
+    __device__ __forceinline__ T* at(T* p, long long by_batch, long long by_token, long long by_head) const {
+        return p + ((long long)batch * by_batch + (long long)token * by_token + (long long)head0 * by_head);
     }
 };
 
-__device__ __forceinline__ long long position_of(const HeadArgs& a, unsigned row) {
-    if (!a.positions) return row % a.tokens;
-    const unsigned batch = row / a.tokens;
-    return load_index(a.positions, (long long)batch * a.position_batch + (row - batch * a.tokens), a.wide);
-}
-
 // ---------------------------------------------------------------------------
 
-template <typename T, int V, int NV, bool NEXT, bool KEPT>
+// COLS: heads of so many columns, all of them turned, or 0 for any.  What depends on
+// the columns alone is then known to the compiler (a third of the instructions).
+template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_kernel(const HeadArgs a) {
     constexpr int P = kPairs<V>;
+    constexpr bool ASYNC = kAsync<T, V>;
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ unsigned s_amax[kWarps][64];
+    __shared__ uint4 s_in[2][2][ASYNC ? kThreads : 1];  // [turn][vector][thread]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int per = 32 / a.lanes, sub = lane % a.lanes, slot = lane / a.lanes;  // heads of a warp; this lane's place in its head
+    const int cols = COLS ? COLS : a.cols, half = COLS ? COLS / 2 : a.half;
+    const float inv_cols = COLS ? 1.0f / (float)COLS : a.inv_cols;
+    const int lanes = COLS ? COLS / 2 / V : a.lanes;
+    const int per = 32 / lanes, sub = lane % lanes, slot = lane / lanes;  // heads of a warp; this lane's place in its head
     stage_weights(a, s_w);
-    const Share mine(a, blockIdx.x * kWarps + warp, per);
+    Share mine(a, warp, per, slot);  // the row that is fetched from
     if (!mine.some) return;
     const Side& q = a.side[mine.side];
+    const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
-    bool ok[NV];
+    bool ok[NV], turned[NV];
+    Raw<T, V> raw[NV][2];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        col[i] = columns_of<V, NEXT>(a, sub + a.lanes * i);
-        ok[i] = sub + a.lanes * i < a.vectors;
+        col[i] = columns_of<V, NEXT>(cols, half, sub + lanes * i);
+        ok[i] = COLS > 0 || sub + lanes * i < a.vectors;
+        turned[i] = COLS > 0 || col[i].angle >= 0;
+        raw[i][0].zero();  // lanes without a vector keep zeros; those of no head have anything
+        raw[i][1].zero();
     }
-    Raw<T, V> raw[NV][2];
-    auto fetch = [&](unsigned row, int step) {
-        const unsigned batch = row / a.tokens;
-        const int head = (mine.step0 + step) * per + slot;
-        const T* in = static_cast<const T*>(q.x) + batch * q.x_batch + (row - batch * a.tokens) * q.x_token + head * q.x_head;
+    uint4* places = &s_in[0][0][ASYNC ? threadIdx.x : 0];
+    constexpr int kTurn = 2 * kThreads;
+    if constexpr (ASYNC)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int k = 0; k < 4; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
+    int turn = 0;
+    const long long x_step = per * q.x_head, out_step = per * q.out_head;
+    const T* in = nullptr;
+    auto fetch = [&](int head) {
+        if (head < heads) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                raw[i][m].zero();
-                if (head < q.heads && ok[i]) raw[i][m].load(in + col[i].col[m]);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (ok[i]) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        if constexpr (ASYNC)
+                            copy_async<16>(places + turn + m * kThreads, in + col[i].col[m]);
+                        else
+                            raw[i][m].load(in + col[i].col[m]);
+                    }
+                }
+        }
+        in += x_step;
     };
-    fetch(mine.row, 0);
-    long long position = a.half > 0 ? position_of(a, mine.row) : 0;
-    for (unsigned row = mine.row; row < a.rows; row += mine.stride) {
-        const unsigned next = row + mine.stride < a.rows ? row + mine.stride : row;  // rows < 2^31
+    in = mine.at(static_cast<const T*>(q.x), q.x_batch, q.x_token, q.x_head);
+    fetch(mine.head0);
+    if (ASYNC) commit_async();
+    long long position = half > 0 ? mine.position(a) : 0;
+    for (bool more = true; more;) {
         const long long here = position;
-        if (a.half > 0) position = position_of(a, next);
+        T* out = mine.at(static_cast<T*>(q.out), q.out_batch, q.out_token, q.out_head);
+        const long long at = (long long)mine.row * heads + mine.head0;  // row of the statistics and of the checkpoint
+        float* stat = q.rstd + at;
+        unsigned char *codes = nullptr, *scales = nullptr;
+        if (FMT) {
+            codes = q.codes + at * q.ld_codes;
+            scales = q.scales + at * q.ld_scales;
+        }
+        more = !mine.last(a);
+        if (more) mine.advance(a);
+        if (half > 0) position = mine.position(a);
         // y = rstd * (own * f + partner * g): the weights times the cosines and sines of this token
         float2 f[NV][2][P], g[NV][2][P];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float2 w[2][P];
             if (!ok[i]) continue;
+            float2 w[2][P];
             take_weights<V>(s_w[mine.side] + col[i].col[0], w[0]);
             take_weights<V>(s_w[mine.side] + col[i].col[1], w[1]);
-            if (col[i].angle >= 0) load_angles<V, NEXT>(a, here, col[i].angle, false, f[i], g[i]);
+            if (turned[i]) {
+                load_angles<V, NEXT>(a, half, here, col[i].angle, false, f[i], g[i]);
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    if (col[i].angle >= 0) {
+                    for (int k = 0; k < P; ++k) {
                         f[i][m][k] = __fmul2_rn(f[i][m][k], w[m][k]);
                         g[i][m][k] = __fmul2_rn(g[i][m][k], partner<V, NEXT>(w, m, k));
-                    } else {
-                        f[i][m][k] = w[m][k];
                     }
-                }
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int k = 0; k < P; ++k) f[i][m][k] = w[m][k];
+            }
         }
-        const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
-        for (int step = 0; step < mine.steps; ++step) {
-            const int head = (mine.step0 + step) * per + slot;
-            const bool live = head < q.heads;
+        for (int step = 0, head = mine.head0; step < steps; ++step, head += per) {
+            const bool live = head < heads;
+            // the next step's elements, or the next token's: into the other place, or behind this step's in the registers
+            auto ahead = [&] {
+                if (step + 1 < steps) {
+                    fetch(head + per);
+                } else if (more) {
+                    in = mine.at(static_cast<const T*>(q.x), q.x_batch, q.x_token, q.x_head);
+                    fetch(mine.head0);
+                }
+            };
+            if constexpr (ASYNC) {
+                const uint4* now = places + turn;
+                turn ^= kTurn;
+                ahead();
+                commit_async();
+                wait_async<1>();
+#pragma unroll
+                for (int m = 0; m < 2; ++m) raw[0][m].take(now + m * kThreads);
+            }
             float2 x[NV][2][P];
             float2 sq = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -338,15 +457,11 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
 #pragma unroll
                     for (int k = 0; k < P; ++k) sq = __ffma2_rn(x[i][m][k], x[i][m][k], sq);
                 }
-            // the next step's elements, or the next token's
-            if (step + 1 < mine.steps)
-                fetch(row, step + 1);
-            else if (next != row)
-                fetch(next, 0);
-            const float rstd = 1.0f / sqrtf(head_sum(sq.x + sq.y, a.lanes) * a.inv_cols + a.eps);
-            const long long at = (long long)row * q.heads + head;  // row of the statistics and of the checkpoint
-            if (live && sub == 0) q.rstd[at] = rstd;
-            if (KEPT) {
+            if constexpr (!ASYNC) ahead();
+            const float rstd = inverse_root(head_sum(sq.x + sq.y, lanes) * inv_cols + a.eps);
+            if (live && sub == 0) *stat = rstd;
+            stat += per;
+            if (FMT) {
                 // bits of the largest |x| of each group of 32 columns, a NaN on top
                 unsigned top[NV][2];
 #pragma unroll
@@ -358,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
                         for (int k = 0; k < P; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x[i][m][k].x), "f"(x[i][m][k].y));
                         top[i][m] = __float_as_uint(t) & 0x7FFFFFFFu;
                     }
-                if (a.lane_groups) {
+                if (COLS || a.lane_groups) {
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         if (NEXT) top[i][0] = max(top[i][0], top[i][1]);
@@ -370,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
                         if (NEXT) top[i][1] = top[i][0];
                     }
                 } else {
-                    unsigned* amax = s_amax[warp] + slot * ((a.cols + kGroup - 1) / kGroup);
+                    unsigned* amax = s_amax[warp] + slot * ((cols + kGroup - 1) / kGroup);
                     __syncwarp();
                     s_amax[warp][lane] = s_amax[warp][lane + 32] = 0;
                     __syncwarp();
@@ -387,61 +502,71 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
                             if (live && ok[i]) top[i][m] = amax[col[i].col[m] / kGroup];
                 }
                 if (live) {
-                    unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
+                    for (int i = 0; i < NV; ++i) {
+                        if (!ok[i]) continue;
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
-                            if (!ok[i]) continue;
                             const int c0 = col[i].col[m];
-                            const unsigned byte = a.e4m3 ? scale_byte<AMPQ_FMT_E4M3>(top[i][m]) : scale_byte<AMPQ_FMT_E5M2>(top[i][m]);
-                            store_code_vec<V>(codes + c0, a.e4m3, byte, x[i][m]);
+                            const unsigned byte = group_byte<FMT>(a.e4m3, top[i][m]);
+                            store_code_vec<V, FMT>(codes + c0, a.e4m3, byte, x[i][m]);
                             if (c0 % kGroup == 0) scales[c0 / kGroup] = (unsigned char)byte;  // by whoever holds a group's first column
                         }
-                    for (int k = a.cols + sub; k < (a.cols + kGroup - 1) / kGroup * kGroup; k += a.lanes) codes[k] = 0;
+                    }
+                    if (cols % kGroup)
+                        for (int k = cols + sub; k < (cols + kGroup - 1) / kGroup * kGroup; k += lanes) codes[k] = 0;
+                }
+                codes += per * q.ld_codes;
+                scales += per * q.ld_scales;
+            }
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!ok[i]) continue;
+                    float2 y[2][P];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int k = 0; k < P; ++k) {
+                            y[m][k] = __fmul2_rn(x[i][m][k], f[i][m][k]);
+                            if (turned[i]) y[m][k] = __ffma2_rn(partner<V, NEXT>(x[i], m, k), g[i][m][k], y[m][k]);
+                            y[m][k] = __fmul2_rn(y[m][k], make_float2(rstd, rstd));
+                        }
+                    store_vec<T, V>(out + col[i].col[0], y[0]);
+                    store_vec<T, V>(out + col[i].col[1], y[1]);
                 }
             }
-            if (!live) continue;
-            T* out = static_cast<T*>(q.out) + batch * q.out_batch + token * q.out_token + head * q.out_head;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (!ok[i]) continue;
-                float2 y[2][P];
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int k = 0; k < P; ++k) {
-                        y[m][k] = __fmul2_rn(x[i][m][k], f[i][m][k]);
-                        if (col[i].angle >= 0) y[m][k] = __ffma2_rn(partner<V, NEXT>(x[i], m, k), g[i][m][k], y[m][k]);
-                        y[m][k] = __fmul2_rn(y[m][k], make_float2(rstd, rstd));
-                    }
-                store_vec<T, V>(out + col[i].col[0], y[0]);
-                store_vec<T, V>(out + col[i].col[1], y[1]);
-            }
+            out += out_step;
         }
     }
 }
 
 // A warp's sums for the weight's gradient stay in registers over its tokens;
-// part[side][CTA][column] are joined afterwards.
-template <typename T, int V, int NV, bool NEXT, bool KEPT>
+// part[CTA][column] of a side's CTAs are joined afterwards.
+template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_kernel(const HeadArgs a) {
     constexpr int P = kPairs<V>;
+    constexpr bool ASYNC = kAsync<T, V>;
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ float s_sums[kWarps][kHeadCols];
-    __shared__ int s_side[kWarps];
+    __shared__ uint4 s_in[2][4][ASYNC ? kThreads : 1];  // [turn][gradient, input or codes][thread]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int per = 32 / a.lanes, sub = lane % a.lanes, slot = lane / a.lanes;
+    const int cols = COLS ? COLS : a.cols, half = COLS ? COLS / 2 : a.half;
+    const float inv_cols = COLS ? 1.0f / (float)COLS : a.inv_cols;
+    const int lanes = COLS ? COLS / 2 / V : a.lanes;
+    const int per = 32 / lanes, sub = lane % lanes, slot = lane / lanes;
     stage_weights(a, s_w);
-    const Share mine(a, blockIdx.x * kWarps + warp, per);
+    Share mine(a, warp, per, slot);  // the row that is fetched from
     const Side& q = a.side[mine.side];
+    const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
-    bool ok[NV];
+    bool ok[NV], turned[NV];
     float2 gw[NV][2][P], w[NV][2][P];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        col[i] = columns_of<V, NEXT>(a, sub + a.lanes * i);
-        ok[i] = sub + a.lanes * i < a.vectors;
+        col[i] = columns_of<V, NEXT>(cols, half, sub + lanes * i);
+        ok[i] = COLS > 0 || sub + lanes * i < a.vectors;
+        turned[i] = COLS > 0 || col[i].angle >= 0;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             if (ok[i]) take_weights<V>(s_w[mine.side] + col[i].col[m], w[i][m]);
@@ -453,100 +578,167 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
         Raw<T, V> raw_g[NV][2], raw_x[NV][2];
         RawCodes<V> raw_c[NV][2];
         unsigned raw_s[NV][2];
-        float raw_r;
-        auto fetch = [&](unsigned row, int step) {
-            const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
-            const int head = (mine.step0 + step) * per + slot;
-            const bool live = head < q.heads;
-            const long long at = (long long)row * q.heads + head;
-            const T* g = static_cast<const T*>(q.gy) + batch * q.gy_batch + token * q.gy_token + head * q.gy_head;
-            const T* x = static_cast<const T*>(q.x) + batch * q.x_batch + token * q.x_token + head * q.x_head;
-            const unsigned char *codes = q.codes + at * q.ld_codes, *scales = q.scales + at * q.ld_scales;
-            raw_r = live ? __ldg(q.rstd + at) : 0.0f;
+        float raw_r = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const int c0 = col[i].col[m];
-                    raw_g[i][m].zero();
-                    raw_x[i][m].zero();
-                    raw_c[i][m].c = make_uint2(0, 0);
-                    raw_s[i][m] = 0;
-                    if (!live || !ok[i]) continue;
-                    raw_g[i][m].load(g + c0);
-                    if (KEPT) {
-                        raw_c[i][m].load(codes + c0);
-                        raw_s[i][m] = __ldg(scales + c0 / kGroup);
-                    } else {
-                        raw_x[i][m].load(x + c0);
+            for (int m = 0; m < 2; ++m) {
+                raw_g[i][m].zero();
+                raw_x[i][m].zero();
+                raw_c[i][m].c = make_uint2(0, 0);
+                raw_s[i][m] = 0;
+            }
+        uint4* places = &s_in[0][0][ASYNC ? threadIdx.x : 0];
+        constexpr int kTurn = 4 * kThreads;
+        if constexpr (ASYNC)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
+        int turn = 0;
+        const long long g_step = per * q.gy_head, x_step = per * q.x_head, out_step = per * q.out_head;
+        const T *gp = nullptr, *xp = nullptr;
+        const unsigned char *cp = nullptr, *sp = nullptr;
+        const float* rp = nullptr;
+        auto begin = [&] {  // of the row
+            const long long at = (long long)mine.row * heads + mine.head0;
+            gp = mine.at(static_cast<const T*>(q.gy), q.gy_batch, q.gy_token, q.gy_head);
+            rp = q.rstd + at;
+            if (FMT) {
+                cp = q.codes + at * q.ld_codes;
+                sp = q.scales + at * q.ld_scales;
+            } else {
+                xp = mine.at(static_cast<const T*>(q.x), q.x_batch, q.x_token, q.x_head);
+            }
+        };
+        auto fetch = [&](int head) {
+            if (head < heads) {
+                raw_r = __ldg(rp);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!ok[i]) continue;
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const int c0 = col[i].col[m];
+                        if constexpr (ASYNC) {
+                            copy_async<16>(places + turn + m * kThreads, gp + c0);
+                            if (FMT)
+                                copy_async<V>(places + turn + (2 + m) * kThreads, cp + c0);
+                            else
+                                copy_async<16>(places + turn + (2 + m) * kThreads, xp + c0);
+                        } else {
+                            raw_g[i][m].load(gp + c0);
+                            if (FMT)
+                                raw_c[i][m].load(cp + c0);
+                            else
+                                raw_x[i][m].load(xp + c0);
+                        }
+                        if (FMT) raw_s[i][m] = __ldg(sp + c0 / kGroup);
                     }
                 }
+            }
+            gp += g_step;
+            rp += per;
+            if (FMT) {
+                cp += per * q.ld_codes;
+                sp += per * q.ld_scales;
+            } else {
+                xp += x_step;
+            }
         };
-        fetch(mine.row, 0);
-        long long position = a.half > 0 ? position_of(a, mine.row) : 0;
-        for (unsigned row = mine.row; row < a.rows; row += mine.stride) {
-            const unsigned next = row + mine.stride < a.rows ? row + mine.stride : row;
+        begin();
+        fetch(mine.head0);
+        if (ASYNC) commit_async();
+        long long position = half > 0 ? mine.position(a) : 0;
+        for (bool more = true; more;) {
             const long long here = position;
-            if (a.half > 0) position = position_of(a, next);
+            T* out = mine.at(static_cast<T*>(q.out), q.out_batch, q.out_token, q.out_head);
+            more = !mine.last(a);
+            if (more) mine.advance(a);
+            if (half > 0) position = mine.position(a);
             float2 c[NV][2][P], s[NV][2][P];
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (ok[i] && col[i].angle >= 0) load_angles<V, NEXT>(a, here, col[i].angle, true, c[i], s[i]);
-            const unsigned batch = row / a.tokens, token = row - batch * a.tokens;
-            for (int step = 0; step < mine.steps; ++step) {
-                const int head = (mine.step0 + step) * per + slot;
-                const bool live = head < q.heads;
+                if (ok[i] && turned[i]) load_angles<V, NEXT>(a, half, here, col[i].angle, true, c[i], s[i]);
+            for (int step = 0, head = mine.head0; step < steps; ++step, head += per) {
+                const bool live = head < heads;
                 const float rstd = raw_r;
+                float scale[NV][2];
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) scale[i][m] = scale_of(raw_s[i][m]);
+                auto ahead = [&] {
+                    if (step + 1 < steps) {
+                        fetch(head + per);
+                    } else if (more) {
+                        begin();
+                        fetch(mine.head0);
+                    }
+                };
+                if constexpr (ASYNC) {
+                    const uint4* now = places + turn;
+                    turn ^= kTurn;
+                    ahead();
+                    commit_async();
+                    wait_async<1>();
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        raw_g[0][m].take(now + m * kThreads);
+                        if (FMT)
+                            raw_c[0][m].c = *reinterpret_cast<const uint2*>(now + (2 + m) * kThreads);  // fp32: the first word
+                        else
+                            raw_x[0][m].take(now + (2 + m) * kThreads);
+                    }
+                }
                 float2 g[NV][2][P], h[NV][2][P];
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         raw_g[i][m].unpack(g[i][m]);
-                        if (KEPT)
-                            raw_c[i][m].unpack(a.e4m3, scale_of(raw_s[i][m]), h[i][m]);
+                        if constexpr (FMT != 0)
+                            raw_c[i][m].template unpack<FMT>(a.e4m3, scale[i][m], h[i][m]);
                         else
                             raw_x[i][m].unpack(h[i][m]);
                     }
-                if (step + 1 < mine.steps)
-                    fetch(row, step + 1);
-                else if (next != row)
-                    fetch(next, 0);
+                if constexpr (!ASYNC) ahead();
                 float2 dot = make_float2(0.0f, 0.0f);
+                if (live) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!live || !ok[i]) continue;
-                    float2 t[2][P];
+                    for (int i = 0; i < NV; ++i) {
+                        if (!ok[i]) continue;
+                        float2 t[2][P];
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int k = 0; k < P; ++k) {
-                            t[m][k] = g[i][m][k];
-                            if (col[i].angle >= 0) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
-                            h[i][m][k] = __fmul2_rn(h[i][m][k], make_float2(rstd, rstd));
-                            gw[i][m][k] = __ffma2_rn(t[m][k], h[i][m][k], gw[i][m][k]);
-                            t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
-                            dot = __ffma2_rn(t[m][k], h[i][m][k], dot);
-                        }
+                            for (int k = 0; k < P; ++k) {
+                                t[m][k] = g[i][m][k];
+                                if (turned[i]) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
+                                h[i][m][k] = __fmul2_rn(h[i][m][k], make_float2(rstd, rstd));
+                                gw[i][m][k] = __ffma2_rn(t[m][k], h[i][m][k], gw[i][m][k]);
+                                t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
+                                dot = __ffma2_rn(t[m][k], h[i][m][k], dot);
+                            }
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int k = 0; k < P; ++k) g[i][m][k] = t[m][k];
-                }
-                const float mean = -head_sum(dot.x + dot.y, a.lanes) * a.inv_cols;
-                if (!live) continue;
-                T* out = static_cast<T*>(q.out) + batch * q.out_batch + token * q.out_token + head * q.out_head;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!ok[i]) continue;
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-#pragma unroll
-                        for (int k = 0; k < P; ++k)
-                            g[i][m][k] = __fmul2_rn(__ffma2_rn(h[i][m][k], make_float2(mean, mean), g[i][m][k]), make_float2(rstd, rstd));
-                        store_vec<T, V>(out + col[i].col[m], g[i][m]);
+                            for (int k = 0; k < P; ++k) g[i][m][k] = t[m][k];
                     }
                 }
+                const float mean = -head_sum(dot.x + dot.y, lanes) * inv_cols;
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        if (!ok[i]) continue;
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                            for (int k = 0; k < P; ++k)
+                                g[i][m][k] = __fmul2_rn(__ffma2_rn(h[i][m][k], make_float2(mean, mean), g[i][m][k]), make_float2(rstd, rstd));
+                            store_vec<T, V>(out + col[i].col[m], g[i][m]);
+                        }
+                    }
+                }
+                out += out_step;
             }
         }
     }
@@ -558,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
 #pragma unroll
             for (int k = 0; k < P; ++k) {
                 float2 v = gw[i][m][k];
-                for (int o = 16; o >= a.lanes; o >>= 1) {  // the warp's heads
+                for (int o = 16; o >= lanes; o >>= 1) {  // the warp's heads
                     v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
                     v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
                 }
@@ -567,15 +759,12 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
                     if (V > 1) s_sums[warp][col[i].col[m] + 2 * k + 1] = v.y;
                 }
             }
-    if (lane == 0) s_side[warp] = mine.side;
     __syncthreads();
-    for (int k = threadIdx.x; k < 2 * a.cols; k += kThreads) {
-        const int side = k >= a.cols, c = k - side * a.cols;
+    for (int c = threadIdx.x; c < cols; c += kThreads) {
         float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i)
-            if (s_side[i] == side) v += s_sums[i][c];
-        a.part[((long long)side * gridDim.x + blockIdx.x) * a.pitch + c] = v;
+        for (int i = 0; i < kWarps; ++i) v += s_sums[i][c];
+        a.part[(long long)blockIdx.x * a.pitch + c] = v;
     }
 }
 
@@ -585,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
 // CTAs of the backward pass: no more than are resident, four to a token at most.
 int backward_ctas(long long rows, int sms) {
     const long long most = (long long)kBackwardCtas * sms;
-    return (int)(4 * rows < most ? 4 * rows : most);
+    return rows == 0 ? 0 : (int)(4 * rows < most ? 4 * rows : most);
 }
 
 int part_pitch(long long cols) { return (int)((cols + 15) / 16 * 16); }
@@ -662,46 +851,85 @@ Side side_of(const ampq_heads* h, bool backward, bool kept) {
     return s;
 }
 
-template <typename T, int V, int NV, bool NEXT, bool KEPT>
-int start(HeadArgs a, bool backward, int sms, int ctas, cudaStream_t st) {
+// Sets up the lanes of a head, the runs, and the CTAs of each side; returns the grid's size.
+long long lay_out(HeadArgs& a, int V, bool next, bool backward, int ctas_per_sm, int sms, int ctas) {
     a.vectors = a.cols / 2 / V;
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < a.vectors) a.lanes *= 2;
-    a.lane_groups = NEXT ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0;
+    a.lane_groups = next ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0;
     const int per = 32 / a.lanes;
     const int steps[2] = {(a.side[0].heads + per - 1) / per, (a.side[1].heads + per - 1) / per};
-    auto runs = [&] {
-        for (int s = 0; s < 2; ++s) a.runs[s] = (steps[s] + a.run - 1) / a.run;
-        return (long long)a.runs[0] + a.runs[1];
+    const long long most = (backward ? (long long)ctas : (long long)ctas_per_sm * sms) * kWarps;
+    // Long runs share a token's angles among more heads; shorter ones while there are
+    // warps without one.
+    auto set = [&](int longest) {
+        long long total = 0;
+        for (int s = 0; s < 2; ++s) {
+            const int n = (steps[s] + longest - 1) / longest;
+            a.run[s] = n ? (steps[s] + n - 1) / n : 1;
+            a.runs[s] = (steps[s] + a.run[s] - 1) / a.run[s];
+            total += (a.runs[s] + kWarps - 1) / kWarps * kWarps;  // a side has whole CTAs
+        }
+        return total;
     };
-    // Runs are of one length where that is a divisor of both sides' steps, and short
-    // while there are warps without one.
-    long long most = backward ? (long long)ctas * kWarps : (long long)kForwardCtas<V> * sms * kWarps;
-    for (a.run = kMaxRun; a.run > 1 && (steps[0] % a.run || steps[1] % a.run || a.rows * runs() < most); --a.run) {}
-    if (backward) {
-        while (runs() > most) a.run *= 2;  // every run has its warp
-        head_norm_backward_kernel<T, V, NV, NEXT, KEPT><<<(unsigned)ctas, kThreads, 0, st>>>(a);
-        return launched();
+    int longest = kMaxRun;
+    long long total = set(longest);
+    while (longest > 1 && (long long)a.rows * (a.runs[0] + a.runs[1]) < most) total = set(longest /= 2);
+    while (backward && total > most) total = set(longest *= 2);  // every run has its warp
+    long long grid = ctas;
+    if (!backward) {
+        const long long need = ((long long)a.rows * a.runs[0] + kWarps - 1) / kWarps + ((long long)a.rows * a.runs[1] + kWarps - 1) / kWarps;
+        grid = need < most / kWarps ? need : most / kWarps;
+        if (grid < total / kWarps) grid = total / kWarps;
     }
-    const long long total = runs();
-    if (most < total) most = total;
-    const long long need = a.rows * total < most ? a.rows * total : most;
-    head_norm_forward_kernel<T, V, NV, NEXT, KEPT><<<(unsigned)((need + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
+    // the CTAs go to the sides by their steps, one warp to a run at least
+    const long long least[2] = {(a.runs[0] + kWarps - 1) / kWarps, (a.runs[1] + kWarps - 1) / kWarps};
+    long long first = (grid * steps[0] + (steps[0] + steps[1]) / 2) / (steps[0] + steps[1]);
+    first = first < least[0] ? least[0] : first > grid - least[1] ? grid - least[1] : first;
+    a.ctas[0] = (int)first;
+    a.ctas[1] = (int)(grid - first);
+    return grid;
+}
+
+template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
+int start(HeadArgs& a, bool backward, int sms, int ctas, cudaStream_t st) {
+    const long long grid = lay_out(a, V, NEXT, backward, kForwardCtas<V>, sms, ctas);
+    if (grid > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
+    if (backward)
+        head_norm_backward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kThreads, 0, st>>>(a);
+    else
+        head_norm_forward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kThreads, 0, st>>>(a);
     return launched();
 }
 
-template <typename T, bool NEXT, bool KEPT>
-int pick(const HeadArgs& a, bool backward, int dtype, int sms, int ctas, cudaStream_t st) {
-    constexpr int kWide = 16 / (int)sizeof(T);
-    if (vectors_fit(a, dtype, kWide)) return start<T, kWide, 1, NEXT, KEPT>(a, backward, sms, ctas, st);
-    if (vectors_fit(a, dtype, 2)) return start<T, 2, kHeadCols / 128, NEXT, KEPT>(a, backward, sms, ctas, st);
-    return start<T, 1, kHeadCols / 64, NEXT, KEPT>(a, backward, sms, ctas, st);
+// The head sizes of most models.
+template <typename T, int V, bool NEXT, int COLS>
+int known(HeadArgs& a, int fmt, bool backward, int sms, int ctas, cudaStream_t st) {
+    if (fmt == AMPQ_FMT_E4M3) return start<T, V, 1, NEXT, AMPQ_FMT_E4M3, COLS>(a, backward, sms, ctas, st);
+    if (fmt == AMPQ_FMT_E5M2) return start<T, V, 1, NEXT, AMPQ_FMT_E5M2, COLS>(a, backward, sms, ctas, st);
+    return start<T, V, 1, NEXT, AMPQ_FMT_BASE, COLS>(a, backward, sms, ctas, st);
 }
 
-template <typename T>
-int dispatch(const HeadArgs& a, bool next, bool kept, bool backward, int dtype, int sms, int ctas, cudaStream_t st) {
-    if (next) return kept ? pick<T, true, true>(a, backward, dtype, sms, ctas, st) : pick<T, true, false>(a, backward, dtype, sms, ctas, st);
-    return kept ? pick<T, false, true>(a, backward, dtype, sms, ctas, st) : pick<T, false, false>(a, backward, dtype, sms, ctas, st);
+template <typename T, bool NEXT>
+int pick(HeadArgs& a, int fmt, bool backward, int dtype, int sms, int ctas, cudaStream_t st) {
+    constexpr int kWide = 16 / (int)sizeof(T);
+    const bool kept = fmt != AMPQ_FMT_BASE;
+    if (vectors_fit(a, dtype, kWide)) {
+        if (2 * a.half == a.cols && a.cols == 64) return known<T, kWide, NEXT, 64>(a, fmt, backward, sms, ctas, st);
+        if (2 * a.half == a.cols && a.cols == 128) return known<T, kWide, NEXT, 128>(a, fmt, backward, sms, ctas, st);
+        if (2 * a.half == a.cols && a.cols == 256) return known<T, kWide, NEXT, 256>(a, fmt, backward, sms, ctas, st);
+        return kept ? start<T, kWide, 1, NEXT, kEither, 0>(a, backward, sms, ctas, st) : start<T, kWide, 1, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
+    }
+    if (vectors_fit(a, dtype, 2))
+        return kept ? start<T, 2, kHeadCols / 128, NEXT, kEither, 0>(a, backward, sms, ctas, st)
+                    : start<T, 2, kHeadCols / 128, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
+    return kept ? start<T, 1, kHeadCols / 64, NEXT, kEither, 0>(a, backward, sms, ctas, st)
+                : start<T, 1, kHeadCols / 64, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
+}
+
+int dispatch(HeadArgs& a, bool next, int fmt, bool backward, int dtype, int sms, int ctas, cudaStream_t st) {
+    if (dtype == AMPQ_F32) return next ? pick<float, true>(a, fmt, backward, dtype, sms, ctas, st) : pick<float, false>(a, fmt, backward, dtype, sms, ctas, st);
+    return next ? pick<__nv_bfloat16, true>(a, fmt, backward, dtype, sms, ctas, st) : pick<__nv_bfloat16, false>(a, fmt, backward, dtype, sms, ctas, st);
 }
 
 HeadArgs head_args(int param_dtype, int index_type, int fmt, long long batch, long long tokens, long long cols, long long rot, const float* cos, const float* sin,
@@ -751,9 +979,7 @@ int ampq_head_norm_forward(int device, void* cuda_stream, int dtype, int param_d
         return AMPQ_OK;
     }
     a.eps = eps;
-    const bool kept = fmt != AMPQ_FMT_BASE;
-    return dtype == AMPQ_F32 ? dispatch<float>(a, interleaved != 0, kept, false, dtype, sms, 0, st)
-                             : dispatch<__nv_bfloat16>(a, interleaved != 0, kept, false, dtype, sms, 0, st);
+    return dispatch(a, interleaved != 0, fmt, false, dtype, sms, 0, st);
 }
 
 int ampq_head_norm_backward_workspace(int device, long long batch, long long tokens, long long cols, long long* bytes) {
@@ -763,7 +989,7 @@ int ampq_head_norm_backward_workspace(int device, long long batch, long long tok
     if (cur.status) return cur.status;
     const int sms = sm_count(device);
     if (sms < 1) return AMPQ_ERR_CUDA;
-    *bytes = 2LL * backward_ctas(batch * tokens, sms) * part_pitch(cols) * (long long)sizeof(float);
+    *bytes = (long long)backward_ctas(batch * tokens, sms) * part_pitch(cols) * (long long)sizeof(float);
     return AMPQ_OK;
 }
 
@@ -781,20 +1007,19 @@ int ampq_head_norm_backward(int device, void* cuda_stream, int dtype, int param_
     HeadArgs a = head_args(param_dtype, index_type, fmt, batch, tokens, cols, rot, cos, sin, angles, positions, position_batch, q, k, true);
     const int ctas = backward_ctas(a.rows, sms);
     a.sums = q->gweight || (k && k->gweight);
-    if (a.sums && ctas > 0 && (!workspace || workspace_bytes < 2LL * ctas * a.pitch * (long long)sizeof(float))) return AMPQ_ERR_INVALID;
+    if (a.sums && ctas > 0 && (!workspace || workspace_bytes < (long long)ctas * a.pitch * (long long)sizeof(float))) return AMPQ_ERR_INVALID;
     a.part = static_cast<float*>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const bool kept = fmt != AMPQ_FMT_BASE;
-    if (a.rows > 0 && a.side[0].heads + a.side[1].heads > 0) {
-        rc = dtype == AMPQ_F32 ? dispatch<float>(a, interleaved != 0, kept, true, dtype, sms, ctas, st)
-                               : dispatch<__nv_bfloat16>(a, interleaved != 0, kept, true, dtype, sms, ctas, st);
+    const bool some = a.rows > 0 && a.side[0].heads + a.side[1].heads > 0;
+    if (some) {
+        rc = dispatch(a, interleaved != 0, fmt, true, dtype, sms, ctas, st);
         if (rc) return rc;
     }
-    if (!a.sums) return AMPQ_OK;
-    const int parts = a.rows > 0 && a.side[0].heads + a.side[1].heads > 0 ? ctas : 0;
-    if (q->gweight && k && k->gweight) return launch_join_columns(a.part, 2, parts, cols, a.pitch, q->gweight, k->gweight, param_dtype, st);
-    return q->gweight ? launch_join_columns(a.part, 1, parts, cols, a.pitch, q->gweight, nullptr, param_dtype, st)
-                      : launch_join_columns(a.part + (long long)parts * a.pitch, 1, parts, cols, a.pitch, k->gweight, nullptr, param_dtype, st);
+    // the queries' CTAs come first, then the keys'
+    if (q->gweight) rc = launch_join_columns(a.part, 1, some && a.side[0].heads ? a.ctas[0] : 0, cols, a.pitch, q->gweight, nullptr, param_dtype, st);
+    if (!rc && k && k->gweight)
+        rc = launch_join_columns(a.part + (long long)a.ctas[0] * a.pitch, 1, some && a.side[1].heads ? a.ctas[1] : 0, cols, a.pitch, k->gweight, nullptr, param_dtype, st);
+    return rc;
 }
 
 #pragma GCC visibility pop
