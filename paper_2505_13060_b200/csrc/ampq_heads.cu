@@ -19,11 +19,13 @@
 namespace ampq {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
-// CTAs that share an SM
-template <int V>
-constexpr int kForwardCtas = 2;
+// Threads of a CTA and CTAs that share an SM: as many warps as the registers leave
+// (forward above all the rotation's factors of an element and of its partner, which are
+// not the same ones where the pairs are neighbours).
+constexpr int kForwardThreads = 128, kBackwardThreads = 256;
+template <int V, bool NEXT>
+constexpr int kForwardCtas = V >= 8 && NEXT ? 4 : 5;
 constexpr int kBackwardCtas = 2;
 constexpr int kMaxRun = 4;  // steps of a run
 
@@ -248,7 +250,7 @@ __device__ __forceinline__ void load_angles(const HeadArgs& p, int half, long lo
 
 // The weights of both sides in shared memory, in fp32.
 __device__ __forceinline__ void stage_weights(const HeadArgs& a, float (*w)[kHeadCols]) {
-    for (int k = threadIdx.x; k < 2 * a.cols; k += kThreads) {
+    for (int k = threadIdx.x; k < 2 * a.cols; k += (int)blockDim.x) {
         const int side = k >= a.cols, c = k - side * a.cols;
         w[side][c] = a.side[side].w ? load_param(a.side[side].w, c, a.param_bf16) : 1.0f;
     }
@@ -298,11 +300,11 @@ struct Share {
     int side, head0, steps;  // head0: the first head of this lane
     unsigned row, stride, batch, token;
     bool some;
-    __device__ __forceinline__ Share(const HeadArgs& a, unsigned warp, int per, int slot) {
+    __device__ __forceinline__ Share(const HeadArgs& a, unsigned warp, unsigned warps, int per, int slot) {
         side = (int)blockIdx.x >= a.ctas[0];
-        warp += (blockIdx.x - (side ? a.ctas[0] : 0)) * kWarps;
+        warp += (blockIdx.x - (side ? a.ctas[0] : 0)) * warps;
         const unsigned runs = (unsigned)a.runs[side];
-        stride = (unsigned)a.ctas[side] * kWarps / runs;
+        stride = (unsigned)a.ctas[side] * warps / runs;
         row = warp / runs;
         some = row < stride && row < a.rows;  // the last few warps may have none
         const int step0 = (int)(warp % runs) * a.run[side];
@@ -335,7 +337,8 @@ struct Share {
 // COLS: heads of so many columns, all of them turned, or 0 for any.  What depends on
 // the columns alone is then known to the compiler (a third of the instructions).
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
-__global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_norm_forward_kernel(const HeadArgs a) {
+    constexpr int kThreads = kForwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
     __shared__ alignas(16) float s_w[2][kHeadCols];
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
     const int lanes = COLS ? COLS / 2 / V : a.lanes;
     const int per = 32 / lanes, sub = lane % lanes, slot = lane / lanes;  // heads of a warp; this lane's place in its head
     stage_weights(a, s_w);
-    Share mine(a, warp, per, slot);  // the row that is fetched from
+    Share mine(a, warp, kWarps, per, slot);  // the row that is fetched from
     if (!mine.some) return;
     const Side& q = a.side[mine.side];
     const int heads = q.heads, steps = mine.steps;
@@ -544,7 +547,8 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas<V>) head_norm_forward_k
 // A warp's sums for the weight's gradient stay in registers over its tokens;
 // part[CTA][column] of a side's CTAs are joined afterwards.
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
-__global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_backward_kernel(const HeadArgs a) {
+    constexpr int kThreads = kBackwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
     __shared__ alignas(16) float s_w[2][kHeadCols];
@@ -556,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
     const int lanes = COLS ? COLS / 2 / V : a.lanes;
     const int per = 32 / lanes, sub = lane % lanes, slot = lane / lanes;
     stage_weights(a, s_w);
-    Share mine(a, warp, per, slot);  // the row that is fetched from
+    Share mine(a, warp, kWarps, per, slot);  // the row that is fetched from
     const Side& q = a.side[mine.side];
     const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
@@ -768,6 +772,35 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) head_norm_backward_ke
     }
 }
 
+// Adds up the CTAs' partial rows of a side, queries (blockIdx.y 0) and keys, in a fixed
+// order: 32 columns to a block, 32 parts at a time.
+struct JoinArgs {
+    const float* part[2];
+    void* out[2];
+    int parts[2], cols, pitch;
+    bool bf16;
+};
+__global__ void __launch_bounds__(1024) head_join_kernel(const JoinArgs a) {
+    __shared__ float sums[32][32];
+    const int side = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
+    if (!a.out[side]) return;
+    float s = 0.0f;
+    if (c < a.cols)
+#pragma unroll 5
+        for (int p = threadIdx.y; p < a.parts[side]; p += 32) s += __ldg(a.part[side] + (long long)p * a.pitch + c);
+    sums[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < a.cols) {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) t += sums[k][threadIdx.x];
+        if (a.bf16)
+            store_elem(static_cast<__nv_bfloat16*>(a.out[side]) + c, t);
+        else
+            store_elem(static_cast<float*>(a.out[side]) + c, t);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // host side
 
@@ -852,14 +885,14 @@ Side side_of(const ampq_heads* h, bool backward, bool kept) {
 }
 
 // Sets up the lanes of a head, the runs, and the CTAs of each side; returns the grid's size.
-long long lay_out(HeadArgs& a, int V, bool next, bool backward, int ctas_per_sm, int sms, int ctas) {
+long long lay_out(HeadArgs& a, int V, bool next, bool backward, int warps, long long ctas) {
     a.vectors = a.cols / 2 / V;
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < a.vectors) a.lanes *= 2;
     a.lane_groups = next ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0;
     const int per = 32 / a.lanes;
     const int steps[2] = {(a.side[0].heads + per - 1) / per, (a.side[1].heads + per - 1) / per};
-    const long long most = (backward ? (long long)ctas : (long long)ctas_per_sm * sms) * kWarps;
+    const long long most = ctas * warps;
     // Long runs share a token's angles among more heads; shorter ones while there are
     // warps without one.
     auto set = [&](int longest) {
@@ -868,7 +901,7 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int ctas_per_sm,
             const int n = (steps[s] + longest - 1) / longest;
             a.run[s] = n ? (steps[s] + n - 1) / n : 1;
             a.runs[s] = (steps[s] + a.run[s] - 1) / a.run[s];
-            total += (a.runs[s] + kWarps - 1) / kWarps * kWarps;  // a side has whole CTAs
+            total += (a.runs[s] + warps - 1) / warps * warps;  // a side has whole CTAs
         }
         return total;
     };
@@ -878,12 +911,12 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int ctas_per_sm,
     while (backward && total > most) total = set(longest *= 2);  // every run has its warp
     long long grid = ctas;
     if (!backward) {
-        const long long need = ((long long)a.rows * a.runs[0] + kWarps - 1) / kWarps + ((long long)a.rows * a.runs[1] + kWarps - 1) / kWarps;
-        grid = need < most / kWarps ? need : most / kWarps;
-        if (grid < total / kWarps) grid = total / kWarps;
+        const long long need = ((long long)a.rows * a.runs[0] + warps - 1) / warps + ((long long)a.rows * a.runs[1] + warps - 1) / warps;
+        grid = need < most / warps ? need : most / warps;
+        if (grid < total / warps) grid = total / warps;
     }
     // the CTAs go to the sides by their steps, one warp to a run at least
-    const long long least[2] = {(a.runs[0] + kWarps - 1) / kWarps, (a.runs[1] + kWarps - 1) / kWarps};
+    const long long least[2] = {(a.runs[0] + warps - 1) / warps, (a.runs[1] + warps - 1) / warps};
     long long first = (grid * steps[0] + (steps[0] + steps[1]) / 2) / (steps[0] + steps[1]);
     first = first < least[0] ? least[0] : first > grid - least[1] ? grid - least[1] : first;
     a.ctas[0] = (int)first;
@@ -893,12 +926,13 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int ctas_per_sm,
 
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 int start(HeadArgs& a, bool backward, int sms, int ctas, cudaStream_t st) {
-    const long long grid = lay_out(a, V, NEXT, backward, kForwardCtas<V>, sms, ctas);
+    const long long most = backward ? (long long)ctas : (long long)kForwardCtas<V, NEXT> * sms;
+    const long long grid = lay_out(a, V, NEXT, backward, (backward ? kBackwardThreads : kForwardThreads) / 32, most);
     if (grid > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
     if (backward)
-        head_norm_backward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        head_norm_backward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kBackwardThreads, 0, st>>>(a);
     else
-        head_norm_forward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kThreads, 0, st>>>(a);
+        head_norm_forward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kForwardThreads, 0, st>>>(a);
     return launched();
 }
 
@@ -1015,11 +1049,18 @@ int ampq_head_norm_backward(int device, void* cuda_stream, int dtype, int param_
         rc = dispatch(a, interleaved != 0, fmt, true, dtype, sms, ctas, st);
         if (rc) return rc;
     }
-    // the queries' CTAs come first, then the keys'
-    if (q->gweight) rc = launch_join_columns(a.part, 1, some && a.side[0].heads ? a.ctas[0] : 0, cols, a.pitch, q->gweight, nullptr, param_dtype, st);
-    if (!rc && k && k->gweight)
-        rc = launch_join_columns(a.part + (long long)a.ctas[0] * a.pitch, 1, some && a.side[1].heads ? a.ctas[1] : 0, cols, a.pitch, k->gweight, nullptr, param_dtype, st);
-    return rc;
+    if (!a.sums) return AMPQ_OK;
+    JoinArgs j{};
+    for (int side = 0; side < 2; ++side) {  // the queries' CTAs come first, then the keys'
+        const ampq_heads* h = side ? k : q;
+        j.part[side] = a.part + (side ? (long long)a.ctas[0] * a.pitch : 0);
+        j.parts[side] = some && a.side[side].heads ? a.ctas[side] : 0;
+        j.out[side] = h ? h->gweight : nullptr;
+    }
+    j.cols = a.cols; j.pitch = a.pitch;
+    j.bf16 = a.param_bf16;
+    head_join_kernel<<<dim3((unsigned)(a.cols + 31) / 32, 2), dim3(32, 32), 0, st>>>(j);
+    return launched();
 }
 
 #pragma GCC visibility pop

@@ -17,11 +17,12 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import struct
 
 import torch
 
 from . import binding as ampq
-from .checkpoint import Packed, _check, _code, _device_of, _matrix, _new_packed, _pitch, _ptr, _same_device, _stream_of
+from .checkpoint import Packed, _check, _code, _device_of, _matrix, _new_packed, _packed_args, _pitch, _ptr, _same_device, _stream_of
 
 _INDEX = {torch.int32: ampq.I32, torch.int64: ampq.I64}
 
@@ -95,42 +96,47 @@ def rotary_table(length: int, rot: int, base: float = 10000.0, device="cuda"):
 
 def _by_token(x: torch.Tensor):
     """x [..., tokens, heads, columns] as [batch, tokens, heads, columns], in place where the layout allows it."""
-    if x.dim() < 3:
-        raise ValueError("queries and keys are [..., tokens, heads, columns], got %s" % (tuple(x.shape),))
     if x.dim() != 4:
+        if x.dim() < 3:
+            raise ValueError("queries and keys are [..., tokens, heads, columns], got %s" % (tuple(x.shape),))
         batch = 1
         for d in x.shape[:-3]:
             batch *= d
         x = x.reshape(batch, *x.shape[-3:])
-    if x.shape[3] > 1 and x.stride(3) != 1:
+    if x.stride(3) != 1 and x.shape[3] > 1:
         x = x.contiguous()
     return x
 
 
 def _rotation(cos, sin, positions, batch: int, tokens: int, device: int, leading):
-    """(cos, sin, columns turned, table rows, positions, their index type, elements between batches)."""
+    """(pointer of cos, of sin, columns turned, table rows, pointer of the positions, their index type, elements between
+    batches), and the tensors that these are of."""
     if cos is None and sin is None:
-        return None, None, 0, 0, None, ampq.I64, 0
+        return (0, 0, 0, 0, 0, ampq.I64, 0), ()
     if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
         raise ValueError("cos and sin are tables [positions, pairs] of one shape")
     if cos.dtype != torch.float32 or sin.dtype != torch.float32:
         raise TypeError("cos and sin are float32, got %s and %s" % (cos.dtype, sin.dtype))
     _same_device(device, cos, sin, positions)
-    cos, sin = (t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format) for t in (cos, sin))
-    index, stride = ampq.I64, 0
-    if positions is not None:
-        index = _index_code(positions)
-        if positions.dim() == 1 and positions.shape[0] == tokens:
-            pass
-        elif tuple(positions.shape) == (*leading, tokens):
-            positions = positions.reshape(batch, tokens)
-            stride = positions.stride(0) if batch > 1 else 0
-        else:
-            raise ValueError("positions are [%d] or %s, got %s" % (tokens, (*leading, tokens), tuple(positions.shape)))
-        if (tokens > 1 and positions.stride(-1) != 1) or stride < 0:
-            positions = positions.contiguous()
-            stride = tokens if positions.dim() == 2 else 0
-    return cos, sin, 2 * cos.shape[1], cos.shape[0], positions, index, stride
+    if not cos.is_contiguous() or cos.data_ptr() % 16:
+        cos = cos.clone(memory_format=torch.contiguous_format)
+    if not sin.is_contiguous() or sin.data_ptr() % 16:
+        sin = sin.clone(memory_format=torch.contiguous_format)
+    angles, pairs = cos.shape
+    if positions is None:
+        return (cos.data_ptr(), sin.data_ptr(), 2 * pairs, angles, 0, ampq.I64, 0), (cos, sin)
+    index, shape = _index_code(positions), positions.shape
+    if len(shape) == 1 and shape[0] == tokens:
+        stride = 0
+    elif shape == (*leading, tokens):
+        positions = positions if len(shape) == 2 else positions.reshape(batch, tokens)
+        stride = positions.stride(0) if batch > 1 else 0
+    else:
+        raise ValueError("positions are [%d] or %s, got %s" % (tokens, (*leading, tokens), tuple(shape)))
+    if tokens > 1 and positions.stride(-1) != 1:
+        positions = positions.contiguous()
+        stride = tokens if positions.dim() == 2 else 0
+    return (cos.data_ptr(), sin.data_ptr(), 2 * pairs, angles, positions.data_ptr(), index, stride), (cos, sin, positions)
 
 
 def _head_weight(w, cols: int, like):
@@ -144,19 +150,21 @@ def _head_weight(w, cols: int, like):
 
 
 def _strides(t):
-    b, n, h, c = t.shape
-    return (t.stride(0) if b > 1 else 0, t.stride(1) if n > 1 else 0, t.stride(2) if h > 1 else 0) if t.numel() else (0, 0, 0)
+    """Pointer of t [batch, tokens, heads, columns] and its strides; those of single elements have no meaning."""
+    if t is None:
+        return 0, 0, 0, 0
+    (b, n, h, _), (sb, sn, sh, _) = t.shape, t.stride()
+    return t.data_ptr(), sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0
+
+
+_HEADS = struct.Struct("20q")   # ampq_heads
 
 
 def _side(out, rstd, w, x=None, gy=None, gw=None, kept=None):
-    heads, none = out.shape[2], (0, 0, 0)
-    return ampq.Heads(heads, _ptr(x), *(_strides(x) if x is not None else none), _ptr(gy), *(_strides(gy) if gy is not None else none), out.data_ptr(),
-                      *_strides(out), _ptr(w), _ptr(gw), rstd.data_ptr(),
-                      *((kept.codes.data_ptr(), _pitch(kept.codes), kept.scales.data_ptr(), _pitch(kept.scales)) if kept is not None else (0, 0, 0, 0)))
-
-
-def _ref(side):
-    return C.byref(side) if side is not None else None
+    """The bytes of an ``ampq_heads``."""
+    ptr, *strides = _strides(out)
+    return _HEADS.pack(out.shape[2], *_strides(x), *_strides(gy), ptr, *strides, _ptr(w), _ptr(gw), rstd.data_ptr(),
+                       *(_packed_args(kept) if kept is not None else (0, 0, 0, 0)))
 
 
 def head_norm_forward(q: torch.Tensor, k, wq=None, wk=None, cos=None, sin=None, positions=None, eps: float = 1e-5, interleaved: bool = False,
@@ -168,11 +176,11 @@ def head_norm_forward(q: torch.Tensor, k, wq=None, wk=None, cos=None, sin=None, 
 
     Returns (yq, yk, rq, rk, pq, pk): the outputs, the reciprocals [..., tokens, heads] of the root mean squares, and the
     checkpoints of q and k (a row for each head) or None for ``FMT_BASE``."""
-    x = [_by_token(q), _by_token(k) if k is not None else None]
-    device = _device_of(x[0])
-    _same_device(device, x[1], wq, wk)
-    batch, tokens, _, cols = x[0].shape
-    code = _code(x[0])
+    x = _by_token(q)
+    device = _device_of(x)
+    batch, tokens, heads, cols = x.shape
+    code, where = _code(x), x.device
+    _same_device(device, k, wq, wk)
     if k is not None:
         if q.shape[:-2] != k.shape[:-2] or k.shape[-1] != cols:
             raise ValueError("queries %s and keys %s differ in more than their heads" % (tuple(q.shape), tuple(k.shape)))
@@ -180,23 +188,27 @@ def head_norm_forward(q: torch.Tensor, k, wq=None, wk=None, cos=None, sin=None, 
             raise TypeError("queries and keys are of one type, got %s and %s" % (q.dtype, k.dtype))
     wq = _head_weight(wq, cols, None)
     wk = _head_weight(wk, cols, wq) if k is not None else None
-    cos, sin, rot, angles, positions, index, stride = _rotation(cos, sin, positions, batch, tokens, device, q.shape[:-3])
+    turn, held = _rotation(cos, sin, positions, batch, tokens, device, q.shape[:-3])
     pcode = _code(wq) if wq is not None else _code(wk) if wk is not None else code
-    y, r, p, sides = [None, None], [None, None], [None, None], [None, None]
-    for i, (t, w) in enumerate(zip(x, (wq, wk))):
-        if t is None:
-            continue
-        y[i] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        r[i] = torch.empty(t.shape[:3], dtype=torch.float32, device=t.device)
-        if fmt != ampq.FMT_BASE:
-            p[i] = _new_packed(t.shape[0] * t.shape[1] * t.shape[2], cols, fmt, t.device)
-        sides[i] = _side(y[i], r[i], w, x=t, kept=p[i])
-    _check(ampq.lib().ampq_head_norm_forward(device, _stream_of(device), code, pcode, index, fmt, 1 if interleaved else 0, batch, tokens, cols, rot, _ptr(cos),
-                                             _ptr(sin), angles, _ptr(positions), stride, eps, _ref(sides[0]), _ref(sides[1])), "ampq_head_norm_forward")
-    yq, rq = y[0].view(q.shape), r[0].view(q.shape[:-1])
-    if k is None:
-        return yq, None, rq, None, p[0], None
-    return yq, y[1].view(k.shape), rq, r[1].view(k.shape[:-1]), p[0], p[1]
+
+    def side(x, w):
+        y = torch.empty(x.shape, dtype=x.dtype, device=where)
+        r = torch.empty(x.shape[:3], dtype=torch.float32, device=where)
+        p = _new_packed(r.numel(), cols, fmt, where) if fmt != ampq.FMT_BASE else None
+        return y, r, p, _side(y, r, w, x=x, kept=p)
+
+    yq, rq, pq, first = side(x, wq)
+    yk = rk = pk = second = None
+    if k is not None:
+        k4 = _by_token(k)
+        yk, rk, pk, second = side(k4, wk)
+    _check(ampq.lib().ampq_head_norm_forward(device, _stream_of(device), code, pcode, turn[5], fmt, 1 if interleaved else 0, batch, tokens, cols, turn[2], turn[0],
+                                             turn[1], turn[3], turn[4], turn[6], eps, first, second), "ampq_head_norm_forward")
+    if q.dim() != 4:
+        yq, rq = yq.view(q.shape), rq.view(q.shape[:-1])
+        if k is not None:
+            yk, rk = yk.view(k.shape), rk.view(k.shape[:-1])
+    return yq, yk, rq, rk, pq, pk
 
 
 @functools.lru_cache(maxsize=4096)
@@ -223,9 +235,10 @@ def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq
     wq = _head_weight(wq, cols, None)
     wk = _head_weight(wk, cols, wq) if gk is not None else None
     _same_device(device, g[1], rq, rk, wq, wk, *((q.codes, k.codes if k is not None else None) if kept else (q, k)))
-    cos, sin, rot, angles, positions, index, stride = _rotation(cos, sin, positions, batch, tokens, device, gq.shape[:-3])
+    turn, held = _rotation(cos, sin, positions, batch, tokens, device, gq.shape[:-3])
     pcode = _code(wq) if wq is not None else _code(wk) if wk is not None else code
     gx, gw, sides = [None, None], [None, None], [None, None]
+    inputs = []
     for i, (t, x, r, w) in enumerate(zip(g, (q, k), (rq, rk), (wq, wk))):
         if t is None:
             continue
@@ -235,6 +248,7 @@ def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq
                 raise ValueError("a checkpoint of %d rows of %d columns for %d of %d" % (x.rows, x.cols, rows, cols))
         else:
             x = _by_token(x)
+            inputs.append(x)   # a copy lives until the call
             if x.shape != t.shape or x.dtype != t.dtype:
                 raise ValueError("input %s %s and gradient %s %s" % (tuple(x.shape), x.dtype, tuple(t.shape), t.dtype))
         if r.dtype != torch.float32 or r.numel() != rows or not r.is_contiguous():
@@ -244,10 +258,13 @@ def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq
         sides[i] = _side(gx[i], r, w, x=None if kept else x, gy=t, gw=gw[i], kept=x if kept else None)
     need = _head_norm_backward_bytes(device, batch, tokens, cols) if gw[0] is not None or gw[1] is not None else 0
     ws = torch.empty(need, dtype=torch.uint8, device=g[0].device) if need else None
-    _check(ampq.lib().ampq_head_norm_backward(device, _stream_of(device), code, pcode, index, q.fmt if kept else ampq.FMT_BASE, 1 if interleaved else 0, batch,
-                                              tokens, cols, rot, _ptr(cos), _ptr(sin), angles, _ptr(positions), stride, _ref(sides[0]), _ref(sides[1]),
-                                              _ptr(ws), need), "ampq_head_norm_backward")
-    return gx[0].view(gq.shape), gx[1].view(gk.shape) if gk is not None else None, gw[0], gw[1]
+    _check(ampq.lib().ampq_head_norm_backward(device, _stream_of(device), code, pcode, turn[5], q.fmt if kept else ampq.FMT_BASE, 1 if interleaved else 0, batch,
+                                              tokens, cols, turn[2], turn[0], turn[1], turn[3], turn[4], turn[6], *sides, _ptr(ws), need),
+           "ampq_head_norm_backward")
+    if gq.dim() != 4:
+        gx[0] = gx[0].view(gq.shape)
+        gx[1] = gx[1].view(gk.shape) if gk is not None else None
+    return gx[0], gx[1], gw[0], gw[1]
 
 
 # -- distillation -------------------------------------------------------------------------------------------------------

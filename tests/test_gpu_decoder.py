@@ -347,7 +347,7 @@ def test_heads_write_their_outputs_only(ampq, dec):
         sides.append(s)
     st = torch.cuda.current_stream().cuda_stream
     rc = ampq.lib().ampq_head_norm_forward(0, st, ampq.BF16, ampq.BF16, ampq.I64, 0, 0, 2, 5, 64, 64, c.cos.data_ptr(), c.sin.data_ptr(), 200,
-                                           c.positions.data_ptr(), 5, 1e-5, dec._ref(sides[0]), dec._ref(sides[1]))
+                                           c.positions.data_ptr(), 5, 1e-5, *sides)
     assert rc == 0
     assert torch.equal(full[:, :, :3, :64], want[0]) and torch.equal(full[:, :, 4:6, :64], want[1])
     full[:, :, :3, :64] = full[:, :, 4:6, :64] = 5.0
