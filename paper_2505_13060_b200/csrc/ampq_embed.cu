@@ -26,9 +26,120 @@ struct RowSplit {
     }
 };
 
+// A warp's block of a row: 32 chunks.  A lane has one of them where rows start on
+// 16-byte boundaries.  Elsewhere (STRIDED) a chunk is not one access; there a lane has
+// every 32nd element (fp32) or pair (bf16), so that a warp's accesses are neighbours.
+template <typename T, bool STRIDED>
+struct Block {
+    static constexpr int E = Chunk<T>::kElems, kPer = 4 / (int)sizeof(T);  // elements of a word
+    // Column of a lane's word i.
+    __device__ static __forceinline__ int column(int c_block, int i) { return c_block + kPer * ((int)(threadIdx.x % 32) + 32 * i); }
+    __device__ static __forceinline__ void load_words(const T* row, int c_block, int cols, unsigned (&w)[8]) {
+        if constexpr (!STRIDED) {
+            const int c0 = c_block + (int)(threadIdx.x % 32) * E;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 0;
+            if (c0 < cols) Chunk<T>::load_words(row + c0, min(E, cols - c0), w);
+        } else {
+            const bool words = (reinterpret_cast<uintptr_t>(row) & 3) == 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = column(c_block, i);
+                if constexpr (sizeof(T) == 4) {
+                    w[i] = c < cols ? __ldg(reinterpret_cast<const unsigned*>(row) + c) : 0u;
+                } else if (words && c + 1 < cols) {
+                    w[i] = __ldg(reinterpret_cast<const unsigned*>(row + c));
+                } else {
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(row) + c;
+                    const unsigned lo = c < cols ? __ldg(h) : 0u, hi = c + 1 < cols ? __ldg(h + 1) : 0u;
+                    w[i] = lo | hi << 16;
+                }
+            }
+        }
+    }
+    __device__ static __forceinline__ void store(T* row, int c_block, int cols, const Chunk<T>& k) {
+        if constexpr (!STRIDED) {
+            const int c0 = c_block + (int)(threadIdx.x % 32) * E;
+            if (c0 < cols) k.store(row + c0, min(E, cols - c0));
+        } else {
+            unsigned w[8];
+            k.to_words(w);
+            const bool words = (reinterpret_cast<uintptr_t>(row) & 3) == 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = column(c_block, i);
+                if constexpr (sizeof(T) == 4) {
+                    if (c < cols) reinterpret_cast<unsigned*>(row)[c] = w[i];
+                } else if (words && c + 1 < cols) {
+                    *reinterpret_cast<unsigned*>(row + c) = w[i];
+                } else {
+                    unsigned short* h = reinterpret_cast<unsigned short*>(row) + c;
+                    if (c < cols) h[0] = (unsigned short)w[i];
+                    if (c + 1 < cols) h[1] = (unsigned short)(w[i] >> 16);
+                }
+            }
+        }
+    }
+    // The block in fp32, in a row that starts on a 16-byte boundary and has whole chunks.
+    __device__ static __forceinline__ void store_part(float* row, int c_block, int cols, const Chunk<T>& k) {
+        if constexpr (!STRIDED) {
+            const int c0 = c_block + (int)(threadIdx.x % 32) * E;
+            if (c0 >= cols) return;
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i)
+                reinterpret_cast<float4*>(row + c0)[i] = make_float4(k.v[2 * i].x, k.v[2 * i].y, k.v[2 * i + 1].x, k.v[2 * i + 1].y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = column(c_block, i);
+                if (c >= cols) continue;
+                if constexpr (kPer == 2)
+                    *reinterpret_cast<float2*>(row + c) = k.v[i % (E / 2)];
+                else
+                    row[c] = i % 2 ? k.v[i / 2].y : k.v[i / 2].x;
+            }
+        }
+    }
+    __device__ static __forceinline__ void add_part(const float* row, int c_block, int cols, Chunk<T>& k) {
+        if constexpr (!STRIDED) {
+            const int c0 = c_block + (int)(threadIdx.x % 32) * E;
+            if (c0 >= cols) return;
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i) {
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(row + c0) + i);
+                k.v[2 * i] = __fadd2_rn(k.v[2 * i], make_float2(f.x, f.y));
+                k.v[2 * i + 1] = __fadd2_rn(k.v[2 * i + 1], make_float2(f.z, f.w));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = column(c_block, i);
+                if (c >= cols) continue;
+                if constexpr (kPer == 2)
+                    k.v[i % (E / 2)] = __fadd2_rn(k.v[i % (E / 2)], __ldcg(reinterpret_cast<const float2*>(row + c)));
+                else
+                    (i % 2 ? k.v[i / 2].y : k.v[i / 2].x) += __ldcg(row + c);
+            }
+        }
+    }
+};
+
+// Zeros to a row, by `threads` threads: whole 32-byte vectors on their boundaries, and
+// the elements before and behind them.
+template <typename T>
+__device__ __forceinline__ void zero_row(T* row, int cols, int t, int threads) {
+    constexpr int E = 32 / (int)sizeof(T);
+    const int over = (int)(reinterpret_cast<uintptr_t>(row) & 31) / (int)sizeof(T), head = min(over ? E - over : 0, cols);
+    const int vectors = (cols - head) / E, tail = cols - head - vectors * E;
+    for (int i = t; i < vectors; i += threads)
+        asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(row + head + (long long)i * E), "r"(0u) : "memory");
+    if (t < head) store_elem(row + t, 0.0f);
+    if (t < tail) store_elem(row + head + vectors * E + t, 0.0f);
+}
+
 // y[n] = scale * weight[token[n]]; bound by the reads and writes of rows.  A block
 // takes a slab of one row, or whole rows.
-template <typename T>
+template <typename T, bool STRIDED>
 __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const void* __restrict__ tokens, bool wide, unsigned n, const T* __restrict__ weight,
                                                                  long long ld_w, long long vocab, int cols, float scale, T* __restrict__ y, long long ld_y,
                                                                  int row_threads, unsigned slabs) {
@@ -36,19 +147,20 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const void* __r
     const unsigned group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
     const unsigned row = group * (unsigned)(kThreads / row_threads) + threadIdx.x / (unsigned)row_threads;
     if (row >= n) return;
-    const int c0 = ((int)slab * row_threads + (int)(threadIdx.x % (unsigned)row_threads)) * K::kElems;
-    if (c0 >= cols) return;
-    const int m = min(K::kElems, cols - c0);
+    const int c_block = ((int)slab * row_threads + (int)(threadIdx.x % (unsigned)row_threads) / 32 * 32) * K::kElems;
+    if (c_block >= cols) return;
     const long long token = load_index(tokens, row, wide);
     K k;
     if (token >= 0 && token < vocab) {
-        k.load(weight + token * ld_w + c0, m);
+        unsigned w[8];
+        Block<T, STRIDED>::load_words(weight + token * ld_w, c_block, cols, w);
+        k.from_words(w);
         k.scale(scale);
     } else {
 #pragma unroll
         for (int i = 0; i < K::kElems / 2; ++i) k.v[i] = make_float2(NAN, NAN);
     }
-    k.store(y + row * ld_y + c0, m);
+    Block<T, STRIDED>::store(y + row * ld_y, c_block, cols, k);
 }
 
 // ---------------------------------------------------------------------------
@@ -84,6 +196,7 @@ __global__ void __launch_bounds__(32 * kRankWarps) sort_few_kernel(const Keys ke
     __shared__ unsigned s_rank[kRankWarps][32];
     unsigned* all = reinterpret_cast<unsigned*>(s_all);
     const unsigned padded = (n + 4 * kRankWarps - 1) / (4 * kRankWarps) * (4 * kRankWarps);
+#pragma unroll 8
     for (unsigned i = threadIdx.x; i < padded; i += 32 * kRankWarps) all[i] = i < n ? key_of(i) << kRankBits | i : 0xFFFFFFFFu;
     for (unsigned i = blockIdx.x * 32 * kRankWarps + threadIdx.x; i < counters; i += gridDim.x * 32 * kRankWarps) arrived[i] = 0;
     __syncthreads();
@@ -225,53 +338,59 @@ struct GradArgs {
     void* gw;
     long long vocab, ld_gy, pitch;
     unsigned n, pieces, slabs, blocks;  // blocks: of 32 chunks, in a row
-    int cols, piece, row_threads, fill_rows;
-    unsigned sum_blocks;
+    int cols, piece, row_threads;
+    unsigned sum_blocks, mix;
     float scale;
 };
 
-template <typename T>
-__device__ __forceinline__ void store_scaled(const GradArgs& a, unsigned token, int c0, Chunk<T> k) {
+template <typename T, bool STRIDED>
+__device__ __forceinline__ void store_scaled(const GradArgs& a, unsigned token, int c_block, Chunk<T> k) {
     k.scale(a.scale);
-    if (c0 < a.cols) k.store(static_cast<T*>(a.gw) + (long long)token * a.cols + c0, min(Chunk<T>::kElems, a.cols - c0));
+    Block<T, STRIDED>::store(static_cast<T*>(a.gw) + (long long)token * a.cols, c_block, a.cols, k);
 }
 
-// The first (or, `last`, the last) entry with this key, of which entry `at` is one: the
-// warp looks at 32 places at a time.
-__device__ __forceinline__ unsigned run_end(const GradArgs& a, unsigned token, unsigned at, bool last) {
-    const unsigned lane = threadIdx.x % 32;
-    unsigned inside = at, outside = last ? a.n : 0xFFFFFFFFu;  // (one before the first entry)
-    while ((last ? outside - inside : inside - outside) > 1) {
-        const unsigned gap = last ? outside - inside : inside - outside, step = (gap + 32) / 33;
-        const unsigned probe = last ? inside + step * (lane + 1) : inside - step * (lane + 1);
-        const bool valid = step * (lane + 1) < gap;
-        const unsigned same = __ballot_sync(0xFFFFFFFFu, valid && __ldg(a.keys + probe) == token);
-        const unsigned many = __popc(same);  // equal keys are neighbours: a run of lanes from the first on
-        const unsigned in = step * many, out = step * (many + 1);
-        if (last) {
-            outside = out < gap ? inside + out : outside;
-            inside += in;
-        } else {
-            outside = out < gap ? inside - out : outside;
-            inside -= in;
+// The first and the last entry of the run that entry `at` is in: the warp looks at the
+// 32 neighbours on either side, and at 32 places spread over what is left where those
+// are all of the run.
+__device__ __forceinline__ void run_ends(const GradArgs& a, unsigned token, unsigned at, unsigned& first, unsigned& last) {
+    const unsigned off = threadIdx.x % 32 + 1;
+    const bool down = off <= at && __ldg(a.keys + (at - min(off, at))) == token;
+    const bool up = off < a.n - at && __ldg(a.keys + min(at + off, a.n - 1)) == token;
+    const unsigned many_down = __popc(__ballot_sync(0xFFFFFFFFu, down)), many_up = __popc(__ballot_sync(0xFFFFFFFFu, up));
+    first = at - many_down;  // equal keys are neighbours: lanes from the first on
+    last = at + many_up;
+    if (many_down == 32) {
+        unsigned gap = first + 1;  // entries from here down to the nearest one known not to be of the run (or none)
+        while (gap > 1) {
+            const unsigned step = (gap + 32) / 33;
+            const unsigned many = __popc(__ballot_sync(0xFFFFFFFFu, step * off < gap && __ldg(a.keys + (first - min(step * off, first))) == token));
+            first -= step * many;
+            gap = min(gap - step * many, step);
         }
     }
-    return inside;
+    if (many_up == 32) {
+        unsigned gap = a.n - last;
+        while (gap > 1) {
+            const unsigned step = (gap + 32) / 33;
+            const unsigned many = __popc(__ballot_sync(0xFFFFFFFFu, step * off < gap && __ldg(a.keys + min(last + step * off, a.n - 1)) == token));
+            last += step * many;
+            gap = min(gap - step * many, step);
+        }
+    }
 }
 
 // A partial sum of a run that was cut: the piece's first partial row for a run that
 // began before it, its second for one that begins in it.  The last of the run's pieces
 // to come (a warp of 32 chunks to a piece) adds them up in order.
-template <typename T>
-__device__ void leave_part(const GradArgs& a, unsigned token, unsigned piece, bool before, int c0, unsigned block, Chunk<T> k) {
-    constexpr int kVectors = Chunk<T>::kElems / 4;
-    if (c0 < a.cols) {  // whole chunks fit into the pitch
-        float4* p = reinterpret_cast<float4*>(a.part + (2LL * piece + (before ? 0 : 1)) * a.pitch + c0);
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) p[i] = make_float4(k.v[2 * i].x, k.v[2 * i].y, k.v[2 * i + 1].x, k.v[2 * i + 1].y);
-    }
+template <typename T, bool STRIDED>
+__device__ void leave_part(const GradArgs& a, unsigned token, unsigned piece, bool before, int c_block, unsigned block, Chunk<T> k) {
+    using B = Block<T, STRIDED>;
+    B::store_part(a.part + (2LL * piece + (before ? 0 : 1)) * a.pitch, c_block, a.cols, k);
     const unsigned anchor = before ? piece * (unsigned)a.piece : min((piece + 1) * (unsigned)a.piece, a.n) - 1;
-    const unsigned first = run_end(a, token, anchor, false) / (unsigned)a.piece, last = run_end(a, token, anchor, true) / (unsigned)a.piece;
+    unsigned first, last;
+    run_ends(a, token, anchor, first, last);
+    first /= (unsigned)a.piece;
+    last /= (unsigned)a.piece;
     __threadfence();
     __syncwarp();
     unsigned come = 0;
@@ -279,82 +398,71 @@ __device__ void leave_part(const GradArgs& a, unsigned token, unsigned piece, bo
     come = __shfl_sync(0xFFFFFFFFu, come, 0);
     if (come != last - first) return;
     __threadfence();
-    if (c0 >= a.cols) return;
     k.zero();
-    constexpr int kAhead = 4;
-    for (unsigned p = first; p <= last; p += kAhead) {
-        float4 f[kAhead][kVectors];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const float4* from = reinterpret_cast<const float4*>(a.part + (2LL * (p + u) + (p + u == first ? 1 : 0)) * a.pitch + c0);
-#pragma unroll
-            for (int i = 0; i < kVectors; ++i) f[u][i] = p + u <= last ? __ldcg(from + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (p + u <= last)
-#pragma unroll
-                for (int i = 0; i < kVectors; ++i) {
-                    k.v[2 * i] = __fadd2_rn(k.v[2 * i], make_float2(f[u][i].x, f[u][i].y));
-                    k.v[2 * i + 1] = __fadd2_rn(k.v[2 * i + 1], make_float2(f[u][i].z, f[u][i].w));
-                }
-    }
-    store_scaled<T>(a, token, c0, k);
+    B::add_part(a.part + (2LL * first + 1) * a.pitch, c_block, a.cols, k);
+#pragma unroll 4
+    for (unsigned p = first + 1; p <= last; ++p) B::add_part(a.part + 2LL * p * a.pitch, c_block, a.cols, k);
+    store_scaled<T, STRIDED>(a, token, c_block, k);
 }
 
-// The first blocks sum: `piece` sorted tokens and a slab of columns to a group of
-// row_threads threads; a run inside a piece is stored at once.  The other blocks write
-// zeros to the rows of no token, those v for which keys[some[v]] is not v (`some` was
-// written for the tokens that there are and holds anything elsewhere).
-template <typename T>
-__global__ void __launch_bounds__(kThreads) embed_backward_kernel(const GradArgs a) {
+// Some blocks sum: `piece` sorted tokens and a slab of columns to a group of
+// row_threads threads; a run inside a piece is stored at once.  The others write zeros
+// to the rows of no token, those v for which keys[some[v]] is not v (`some` was written
+// for the tokens that there are and holds anything elsewhere).  The sums wait for their
+// loads, the zeros for the memory: one block in `mix` sums while there are any to do.
+template <typename T, bool STRIDED>
+__global__ void __launch_bounds__(kThreads, 2) embed_backward_kernel(const GradArgs a) {
     using K = Chunk<T>;
     const int group = threadIdx.x / a.row_threads, t = threadIdx.x % a.row_threads, groups = kThreads / a.row_threads;
-    if (blockIdx.x >= a.sum_blocks) {
-        const long long v0 = (long long)(blockIdx.x - a.sum_blocks) * a.fill_rows;
-        K zero;
-        zero.zero();
-        for (long long v = v0 + group; v < v0 + a.fill_rows && v < a.vocab; v += groups) {
-            const unsigned e = a.n > 0 ? __ldg(a.some + v) : 0u;
-            if (e < a.n && __ldg(a.keys + e) == (unsigned)v) continue;
-            T* row = static_cast<T*>(a.gw) + v * a.cols;
-            for (int c0 = t * K::kElems; c0 < a.cols; c0 += a.row_threads * K::kElems) zero.store(row + c0, min(K::kElems, a.cols - c0));
+    const unsigned lane = threadIdx.x % 32;
+    const unsigned turn = blockIdx.x / a.mix, place = blockIdx.x - turn * a.mix;
+    if (place != 0 || turn >= a.sum_blocks) {
+        const unsigned fill = blockIdx.x - (turn >= a.sum_blocks ? a.sum_blocks : turn + 1);
+        const long long v0 = ((long long)fill * groups + group) * 32;
+        bool unused = v0 + lane < a.vocab;
+        if (unused && a.n > 0) {
+            const unsigned e = __ldg(a.some + v0 + lane);
+            unused = e >= a.n || __ldg(a.keys + e) != (unsigned)(v0 + lane);
         }
+        for (unsigned rows = __ballot_sync(0xFFFFFFFFu, unused); rows; rows &= rows - 1)
+            zero_row(static_cast<T*>(a.gw) + (v0 + __ffs(rows) - 1) * a.cols, a.cols, t, a.row_threads);
         return;
     }
-    const unsigned item = blockIdx.x / a.slabs, slab = blockIdx.x - item * a.slabs;
+    const unsigned item = turn / a.slabs, slab = turn - item * a.slabs;
     const unsigned piece = item * (unsigned)groups + (unsigned)group;
     if (piece >= a.pieces) return;
-    const int chunk = (int)slab * a.row_threads + t, c0 = chunk * K::kElems;
-    const unsigned block = (unsigned)chunk / 32;
+    const unsigned block = (slab * (unsigned)a.row_threads + (unsigned)t) / 32;
     if (block >= a.blocks) return;  // a warp behind the last column
-    const int m = min(K::kElems, a.cols - c0);
-    const unsigned begin = piece * (unsigned)a.piece, end = min(begin + (unsigned)a.piece, a.n);
+    const int c_block = (int)block * 32 * K::kElems;
+    const unsigned begin = piece * (unsigned)a.piece, here = min((unsigned)a.piece, a.n - begin);  // at most 32
     const unsigned none = (unsigned)a.vocab;
-    unsigned token = __ldg(a.keys + begin);
-    bool before = begin > 0 && __ldg(a.keys + begin - 1) == token;
+    // a lane's entry of the piece, and the keys on its borders
+    const unsigned my_key = lane < here ? __ldg(a.keys + begin + lane) : none, my_place = lane < here ? __ldg(a.places + begin + lane) : 0u;
+    const unsigned key_before = begin > 0 ? __ldg(a.keys + begin - 1) : none, key_after = begin + here < a.n ? __ldg(a.keys + begin + here) : none;
+    const unsigned count = __popc(__ballot_sync(0xFFFFFFFFu, my_key != none));  // those of no row are the last ones
+    if (count == 0) return;
+    unsigned token = __shfl_sync(0xFFFFFFFFu, my_key, 0);
+    bool before = key_before == token;
     K sum;
     sum.zero();
     constexpr int kAhead = 4;
-    for (unsigned e = begin; e < end && token != none; e += kAhead) {
-        unsigned key[kAhead];
+    for (unsigned e = 0; e < count; e += kAhead) {
         unsigned w[kAhead][8];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            key[u] = e + u < end ? __ldg(a.keys + e + u) : none;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[u][i] = 0;
-            if (key[u] != none && m > 0) K::load_words(static_cast<const T*>(a.gy) + (long long)__ldg(a.places + e + u) * a.ld_gy + c0, m, w[u]);
+            const unsigned from = __shfl_sync(0xFFFFFFFFu, my_place, (e + u) % 32);
+            if (e + u < count) Block<T, STRIDED>::load_words(static_cast<const T*>(a.gy) + (long long)from * a.ld_gy, c_block, a.cols, w[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (e + u >= end || token == none) break;
-            if (key[u] != token) {
+            if (e + u >= count) break;
+            const unsigned key = __shfl_sync(0xFFFFFFFFu, my_key, e + u);
+            if (key != token) {
                 if (before)
-                    leave_part<T>(a, token, piece, true, c0, block, sum);
+                    leave_part<T, STRIDED>(a, token, piece, true, c_block, block, sum);
                 else
-                    store_scaled<T>(a, token, c0, sum);
-                token = key[u];
+                    store_scaled<T, STRIDED>(a, token, c_block, sum);
+                token = key;
                 before = false;
                 sum.zero();
             }
@@ -364,12 +472,10 @@ __global__ void __launch_bounds__(kThreads) embed_backward_kernel(const GradArgs
             for (int i = 0; i < K::kElems / 2; ++i) sum.v[i] = __fadd2_rn(sum.v[i], k.v[i]);
         }
     }
-    if (token == none) return;
-    const bool after = end < a.n && __ldg(a.keys + end) == token;
-    if (before || after)
-        leave_part<T>(a, token, piece, before, c0, block, sum);
+    if (before || (count == here && key_after == token))
+        leave_part<T, STRIDED>(a, token, piece, before, c_block, block, sum);
     else
-        store_scaled<T>(a, token, c0, sum);
+        store_scaled<T, STRIDED>(a, token, c_block, sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -387,9 +493,9 @@ struct Plan {
     Plan(int dtype, long long n, long long vocab, long long cols, int sms) {
         const int elems = dtype == AMPQ_F32 ? 8 : 16;
         const RowSplit split(cols, elems);
-        // longer pieces while there is enough to do for every SM
-        piece = 8;
-        while (piece < 64 && n * (long long)split.slabs / piece > 16LL * sms) piece *= 2;
+        // longer pieces while there is enough to do for every SM; a lane has an entry
+        piece = 16;
+        while (piece < 32 && n * (long long)split.slabs / piece > 16LL * sms) piece *= 2;
         pieces = (unsigned)((n + piece - 1) / piece);
         tiles = (unsigned)((n + kTile - 1) / kTile);
         passes = 1;
@@ -431,8 +537,10 @@ int launch_embed(const void* tokens, bool wide, long long n, const void* weight,
     const RowSplit split(cols, Chunk<T>::kElems);
     const long long rows = kThreads / split.threads, blocks = (n + rows - 1) / rows * split.slabs;
     if (blocks > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    embed_forward_kernel<T><<<(unsigned)blocks, kThreads, 0, st>>>(tokens, wide, (unsigned)n, static_cast<const T*>(weight), ld_w, vocab, (int)cols, scale,
-                                                                   static_cast<T*>(y), ld_y, split.threads, split.slabs);
+    constexpr int kType = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
+    auto kernel = rows_aligned(weight, ld_w, kType) && rows_aligned(y, ld_y, kType) ? embed_forward_kernel<T, false> : embed_forward_kernel<T, true>;
+    kernel<<<(unsigned)blocks, kThreads, 0, st>>>(tokens, wide, (unsigned)n, static_cast<const T*>(weight), ld_w, vocab, (int)cols, scale, static_cast<T*>(y),
+                                                  ld_y, split.threads, split.slabs);
     return launched();
 }
 
@@ -443,11 +551,13 @@ int launch_sums(GradArgs a, cudaStream_t st) {
     a.slabs = split.slabs;
     const long long groups = kThreads / split.threads;
     const long long sums = (a.pieces + groups - 1) / groups * split.slabs;
-    a.fill_rows = (int)groups * 4;
-    const long long fills = (a.vocab + a.fill_rows - 1) / a.fill_rows;
+    const long long fills = (a.vocab + 32 * groups - 1) / (32 * groups);
     if (sums + fills > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
     a.sum_blocks = (unsigned)sums;
-    embed_backward_kernel<T><<<(unsigned)(sums + fills), kThreads, 0, st>>>(a);
+    a.mix = sums > 0 ? (unsigned)(fills / sums + 1) : 1u;
+    constexpr int kType = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
+    auto kernel = rows_aligned(a.gy, a.ld_gy, kType) && rows_aligned(a.gw, a.cols, kType) ? embed_backward_kernel<T, false> : embed_backward_kernel<T, true>;
+    kernel<<<(unsigned)(sums + fills), kThreads, 0, st>>>(a);
     return launched();
 }
 
