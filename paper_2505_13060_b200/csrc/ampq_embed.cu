@@ -31,7 +31,8 @@ struct RowSplit {
 // every 32nd element (fp32) or pair (bf16), so that a warp's accesses are neighbours.
 template <typename T, bool STRIDED>
 struct Block {
-    static constexpr int E = Chunk<T>::kElems, kPer = 4 / (int)sizeof(T);  // elements of a word
+    static constexpr int E = Chunk<T>::kElems;
+    static constexpr int kPer = 4 / (int)sizeof(T);  // elements of a word
     // Column of a lane's word i.
     __device__ static __forceinline__ int column(int c_block, int i) { return c_block + kPer * ((int)(threadIdx.x % 32) + 32 * i); }
     __device__ static __forceinline__ void load_words(const T* row, int c_block, int cols, unsigned (&w)[8]) {
@@ -139,7 +140,7 @@ __device__ __forceinline__ void zero_row(T* row, int cols, int t, int threads) {
 
 // y[n] = scale * weight[token[n]]; bound by the reads and writes of rows.  A block
 // takes a slab of one row, or whole rows.
-template <typename T, bool STRIDED>
+template <typename T, bool STRIDED, int U>
 __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const void* __restrict__ tokens, bool wide, unsigned n, const T* __restrict__ weight,
                                                                  long long ld_w, long long vocab, int cols, float scale, T* __restrict__ y, long long ld_y,
                                                                  int row_threads, unsigned slabs) {
@@ -147,20 +148,26 @@ __global__ void __launch_bounds__(kThreads) embed_forward_kernel(const void* __r
     const unsigned group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
     const unsigned row = group * (unsigned)(kThreads / row_threads) + threadIdx.x / (unsigned)row_threads;
     if (row >= n) return;
-    const int c_block = ((int)slab * row_threads + (int)(threadIdx.x % (unsigned)row_threads) / 32 * 32) * K::kElems;
-    if (c_block >= cols) return;
+    const int c_first = ((int)slab * U * row_threads + (int)(threadIdx.x % (unsigned)row_threads) / 32 * 32) * K::kElems, c_step = row_threads * K::kElems;
     const long long token = load_index(tokens, row, wide);
-    K k;
-    if (token >= 0 && token < vocab) {
-        unsigned w[8];
-        Block<T, STRIDED>::load_words(weight + token * ld_w, c_block, cols, w);
-        k.from_words(w);
-        k.scale(scale);
-    } else {
+    const bool known = token >= 0 && token < vocab;
+    unsigned w[U][8];
 #pragma unroll
-        for (int i = 0; i < K::kElems / 2; ++i) k.v[i] = make_float2(NAN, NAN);
+    for (int u = 0; u < U; ++u) {
+        if (known && c_first + u * c_step < cols) {
+            Block<T, STRIDED>::load_words(weight + token * ld_w, c_first + u * c_step, cols, w[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[u][i] = 0xFFFFFFFFu;  // NaN in either type
+        }
     }
-    Block<T, STRIDED>::store(y + row * ld_y, c_block, cols, k);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        K k;
+        k.from_words(w[u]);
+        k.scale(scale);
+        if (c_first + u * c_step < cols) Block<T, STRIDED>::store(y + row * ld_y, c_first + u * c_step, cols, k);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -190,14 +197,27 @@ struct Keys {
 constexpr int kRankBits = 13, kRankTokens = 1 << kRankBits, kRankWarps = 8;
 constexpr long long kRankVocab = 1LL << (32 - kRankBits);  // keys below it, `vocab` itself among them
 
+__device__ __forceinline__ void count_below(unsigned k, unsigned mine, unsigned& rank) {
+    asm("{\n.reg .pred p;\nsetp.lt.u32 p, %1, %2;\n@p add.u32 %0, %0, 1;\n}" : "+r"(rank) : "r"(k), "r"(mine));
+}
+
 __global__ void __launch_bounds__(32 * kRankWarps) sort_few_kernel(const Keys key_of, unsigned n, unsigned* __restrict__ keys, unsigned* __restrict__ places,
                                                                    unsigned* __restrict__ some, unsigned* __restrict__ arrived, unsigned counters) {
     extern __shared__ uint4 s_all[];
     __shared__ unsigned s_rank[kRankWarps][32];
     unsigned* all = reinterpret_cast<unsigned*>(s_all);
     const unsigned padded = (n + 4 * kRankWarps - 1) / (4 * kRankWarps) * (4 * kRankWarps);
-#pragma unroll 8
-    for (unsigned i = threadIdx.x; i < padded; i += 32 * kRankWarps) all[i] = i < n ? key_of(i) << kRankBits | i : 0xFFFFFFFFu;
+    for (unsigned i0 = threadIdx.x; i0 < padded; i0 += 8 * 32 * kRankWarps) {
+        unsigned k[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {  // eight loads in flight
+            const unsigned i = i0 + u * 32 * kRankWarps;
+            k[u] = i < n ? key_of(i) << kRankBits | i : 0xFFFFFFFFu;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i0 + u * 32 * kRankWarps < padded) all[i0 + u * 32 * kRankWarps] = k[u];
+    }
     for (unsigned i = blockIdx.x * 32 * kRankWarps + threadIdx.x; i < counters; i += gridDim.x * 32 * kRankWarps) arrived[i] = 0;
     __syncthreads();
     const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32, i = blockIdx.x * 32 + lane;
@@ -207,7 +227,10 @@ __global__ void __launch_bounds__(32 * kRankWarps) sort_few_kernel(const Keys ke
 #pragma unroll 4
     for (unsigned j = 0; j < quads; ++j) {
         const uint4 k = s_all[warp * quads + j];
-        rank += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+        count_below(k.x, mine, rank);
+        count_below(k.y, mine, rank);
+        count_below(k.z, mine, rank);
+        count_below(k.w, mine, rank);
     }
     s_rank[warp][lane] = rank;
     __syncthreads();
@@ -531,14 +554,21 @@ int check_embed(int dtype, int index_type, const void* tokens, long long n, long
     return AMPQ_OK;
 }
 
+// From so many slabs of rows on a thread takes two chunks.
+constexpr long long kManyBlocks = 4096;
+
 template <typename T>
 int launch_embed(const void* tokens, bool wide, long long n, const void* weight, long long ld_w, long long vocab, long long cols, float scale, void* y,
                  long long ld_y, cudaStream_t st) {
-    const RowSplit split(cols, Chunk<T>::kElems);
+    RowSplit split(cols, Chunk<T>::kElems);
+    constexpr int kType = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
+    const bool aligned = rows_aligned(weight, ld_w, kType) && rows_aligned(y, ld_y, kType);
+    const bool two = split.slabs > 1 && n * split.slabs >= kManyBlocks;
+    if (two) split.slabs = (split.slabs + 1) / 2;
+    auto kernel = aligned ? (two ? embed_forward_kernel<T, false, 2> : embed_forward_kernel<T, false, 1>)
+                          : (two ? embed_forward_kernel<T, true, 2> : embed_forward_kernel<T, true, 1>);
     const long long rows = kThreads / split.threads, blocks = (n + rows - 1) / rows * split.slabs;
     if (blocks > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    constexpr int kType = sizeof(T) == 4 ? AMPQ_F32 : AMPQ_BF16;
-    auto kernel = rows_aligned(weight, ld_w, kType) && rows_aligned(y, ld_y, kType) ? embed_forward_kernel<T, false> : embed_forward_kernel<T, true>;
     kernel<<<(unsigned)blocks, kThreads, 0, st>>>(tokens, wide, (unsigned)n, static_cast<const T*>(weight), ld_w, vocab, (int)cols, scale, static_cast<T*>(y),
                                                   ld_y, split.threads, split.slabs);
     return launched();
