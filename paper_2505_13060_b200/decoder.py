@@ -218,9 +218,10 @@ def _head_norm_backward_bytes(device: int, batch: int, tokens: int, cols: int) -
     return need.value
 
 
-def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq=None, wk=None, cos=None, sin=None, positions=None, interleaved: bool = False):
+def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq=None, wk=None, cos=None, sin=None, positions=None, interleaved: bool = False,
+                       weight_grads: bool = True):
     """Backward pass of ``head_norm_forward``; q and k are the inputs or their checkpoints, gq and gk the gradients of the
-    outputs.  Returns (gxq, gxk, gwq, gwk), the last two in their weight's type, None without one."""
+    outputs.  Returns (gxq, gxk, gwq, gwk), the last two in their weight's type, None without one (or without ``weight_grads``)."""
     g = [_by_token(gq), _by_token(gk) if gk is not None else None]
     device = _device_of(g[0])
     batch, tokens, _, cols = g[0].shape
@@ -254,7 +255,7 @@ def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq
         if r.dtype != torch.float32 or r.numel() != rows or not r.is_contiguous():
             raise ValueError("rq and rk are as head_norm_forward returned them")
         gx[i] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        gw[i] = torch.empty(w.shape, dtype=w.dtype, device=t.device) if w is not None else None
+        gw[i] = torch.empty(w.shape, dtype=w.dtype, device=t.device) if w is not None and weight_grads else None
         sides[i] = _side(gx[i], r, w, x=None if kept else x, gy=t, gw=gw[i], kept=x if kept else None)
     need = _head_norm_backward_bytes(device, batch, tokens, cols) if gw[0] is not None or gw[1] is not None else 0
     ws = torch.empty(need, dtype=torch.uint8, device=g[0].device) if need else None
@@ -351,7 +352,7 @@ class _HeadNorm(torch.autograd.Function):
     def backward(ctx, gq, gk):
         wq, wk, cos, sin, positions, rq, rk, *kept = ctx.saved_tensors
         x = [Packed(a, b, ctx.cols, ctx.fmt) if b is not None else a for a, b in (kept[:2], kept[2:])]
-        gxq, gxk, gwq, gwk = head_norm_backward(gq, gk, x[0], x[1], rq, rk, wq, wk, cos, sin, positions, ctx.interleaved)
+        gxq, gxk, gwq, gwk = head_norm_backward(gq, gk, x[0], x[1], rq, rk, wq, wk, cos, sin, positions, ctx.interleaved, any(ctx.needs_input_grad[2:4]))
         return gxq, gxk, gwq, gwk, None, None, None, None, None, None
 
 
@@ -372,6 +373,8 @@ class _DistillLoss(torch.autograd.Function):
 def embedding(tokens: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, padding_idx=None) -> torch.Tensor:
     """``embed``, differentiable in the table: the gradient's rows are added in an order that the tokens fix.  The row
     ``padding_idx`` gets no gradient."""
+    if padding_idx is not None and not 0 <= padding_idx < weight.shape[0]:
+        raise ValueError("padding_idx %d is no row of a table of %d" % (padding_idx, weight.shape[0]))
     return _Embedding.apply(tokens, weight, scale, padding_idx)
 
 
@@ -379,7 +382,8 @@ def head_norm(q: torch.Tensor, k=None, wq=None, wk=None, cos=None, sin=None, pos
               fmt: int = ampq.FMT_E4M3):
     """The outputs (yq, yk) of ``head_norm_forward``, differentiable; q and k are kept for the backward pass in 8 bits, or
     in full with ``FMT_BASE``."""
-    return _HeadNorm.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, fmt if torch.is_grad_enabled() else ampq.FMT_BASE)
+    keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk))
+    return _HeadNorm.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, fmt if keep else ampq.FMT_BASE)
 
 
 def distill_loss(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0) -> torch.Tensor:
@@ -387,3 +391,34 @@ def distill_loss(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.Ten
     if teacher.requires_grad:
         raise ValueError("the teacher's logits are a constant here: detach them")
     return _DistillLoss.apply(logits, indices, teacher, temperature)
+
+
+# -- modules --------------------------------------------------------------------------------------------------------------
+
+
+class ScaledEmbedding(torch.nn.Embedding):
+    """``torch.nn.Embedding`` whose rows are multiplied by ``scale`` and whose gradient is the same bits every time."""
+
+    def __init__(self, num_embeddings: int, embedding_dim: int, scale: float = 1.0, padding_idx=None, **kwargs):
+        super().__init__(num_embeddings, embedding_dim, padding_idx=padding_idx, **kwargs)
+        if self.max_norm is not None or self.scale_grad_by_freq or self.sparse:
+            raise ValueError("max_norm, scale_grad_by_freq and sparse are not for this module")
+        self.scale = scale
+
+    def forward(self, input):
+        return embedding(input, self.weight, self.scale, self.padding_idx)
+
+
+class HeadNorm(torch.nn.Module):
+    """Norms of queries and keys for each head with the position rotation, between the layers that make them and their
+    product.  Its inputs are kept in full for the backward pass, in 8 bits in a calibration with checkpoints
+    (``hooks.Calibrator``)."""
+
+    def __init__(self, cols: int, eps: float = 1e-5, interleaved: bool = False, device=None, dtype=None):
+        super().__init__()
+        self.weight_q = torch.nn.Parameter(torch.ones(cols, device=device, dtype=dtype))
+        self.weight_k = torch.nn.Parameter(torch.ones(cols, device=device, dtype=dtype))
+        self.eps, self.interleaved = eps, interleaved
+
+    def forward(self, q, k, cos=None, sin=None, positions=None, fmt: int = ampq.FMT_BASE):
+        return head_norm(q, k, self.weight_q, self.weight_k, cos, sin, positions, self.eps, self.interleaved, fmt)

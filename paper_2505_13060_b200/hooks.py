@@ -41,9 +41,12 @@ S of inputs and of weights off by 0.1 % on average, 0.2 % at worst in E4M3, 0.4 
 tensor that was already rounded says nothing, so the pass scores the model's term
 alone (``set_measured(False)``; the context's next pass has its own setting again).
 
+``decoder.HeadNorm`` modules of a model keep their inputs the same way.
+
 ``quantised(...)`` runs the model with chosen layers' inputs and weights replaced
 by their FP8-rounded values (``ampq_fake_quant``), which is how the predicted
-loss MSE is checked against a measured one (Sec. 3.2).
+loss MSE is checked against a measured one (Sec. 3.2); ``divergence(...)`` compares
+its outputs with those of the model as it is, which needs no labels.
 """
 from __future__ import annotations
 
@@ -53,6 +56,7 @@ import torch
 
 from . import binding as ampq
 from . import checkpoint as ckpt
+from . import decoder
 
 
 class BatchedMatmul(torch.nn.Module):
@@ -220,6 +224,12 @@ class Calibrator:
                     return ckpt.rms_norm(x, m.weight, torch.finfo(torch.float32).eps if m.eps is None else m.eps, fmt) if known(x, m) else plain(x)
 
                 self._replaced.append((m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm))
+            elif self._plain(m, decoder.HeadNorm):
+
+                def head_norm(q, k, cos=None, sin=None, positions=None, fmt=fmt, plain=m.forward):
+                    return plain(q, k, cos, sin, positions, fmt if scored() else ampq.FMT_BASE)
+
+                self._replaced.append((m, head_norm))
 
     def _remove_hooks(self):
         for h in self._handles:
@@ -315,3 +325,16 @@ class Calibrator:
             if not self._same_stream():
                 torch.cuda.ExternalStream(self.ctx.stream).synchronize()
             self._keep = []
+
+    def divergence(self, forward, fmt_of_layer, top: int = 64, temperature: float = 1.0, amax_x=None):
+        """How far a low-precision configuration's outputs are from the model's own: ``forward()`` runs the model and
+        returns logits [..., classes]; it is called once as it is and once in the configuration (``quantised``).  Returns
+        the divergence of the second's logits from the first's ``top`` largest (``decoder.distill_forward``), one fp32
+        number for each row."""
+        with torch.no_grad():
+            logits = forward()
+            teacher, indices = logits.topk(min(top, logits.shape[-1]), dim=-1)
+            del logits
+            with self.quantised(fmt_of_layer, amax_x):
+                logits = forward()
+            return decoder.distill_forward(logits, indices, teacher, temperature)[0]
