@@ -523,3 +523,14 @@ def test_distill_repeats_itself(dec):
     first = dec.distill_forward(s, index, teacher)
     for _ in range(5):
         assert all(torch.equal(a, b) for a, b in zip(first, dec.distill_forward(s, index, teacher)))
+
+
+@pytest.mark.parametrize("n", [129, 144, 300, 8192, 8193, 40000])
+def test_embed_grad_of_one_run(dec, n):
+    """Runs of 9 pieces and more, which are added up in groups: one token for all but a few, over several blocks of columns."""
+    tokens = torch.full((n,), 5)
+    tokens[::97] = 2
+    check_embed_grad(dec, tokens.cuda(), randn((n, 24), torch.float32, n), 7, 1.0)
+    if n < 10000:
+        check_embed_grad(dec, tokens.cuda(), randn((n, 1100), torch.bfloat16, n), 7, 1.0)
+        check_embed_grad(dec, tokens.cuda(), randn((n, 523), torch.float32, n), 7, 1.0)
