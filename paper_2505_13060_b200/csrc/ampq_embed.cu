@@ -191,10 +191,9 @@ struct Keys {
 
 // Few tokens: a token's place is the number of those before it in the order, which is
 // counted by comparing it with all.  Keys get the place they have now in their low
-// bits, so that no two are alike.  A CTA takes 32 tokens, one to a lane, and each of
-// its warps a part of the others; 8192 tokens are 6 us, three passes of the other sort
-// 45 us, and at 16384 the two meet.
-constexpr int kRankBits = 13, kRankTokens = 1 << kRankBits, kRankWarps = 8;
+// bits, so that no two are alike.  A CTA takes 64 tokens, two to a lane, and each of
+// its warps a part of the others.
+constexpr int kRankBits = 13, kRankTokens = 1 << kRankBits, kRankWarps = 32, kRankShare = 64;
 constexpr long long kRankVocab = 1LL << (32 - kRankBits);  // keys below it, `vocab` itself among them
 
 __device__ __forceinline__ void count_below(unsigned k, unsigned mine, unsigned& rank) {
@@ -204,7 +203,7 @@ __device__ __forceinline__ void count_below(unsigned k, unsigned mine, unsigned&
 __global__ void __launch_bounds__(32 * kRankWarps) sort_few_kernel(const Keys key_of, unsigned n, unsigned* __restrict__ keys, unsigned* __restrict__ places,
                                                                    unsigned* __restrict__ some, unsigned* __restrict__ arrived, unsigned counters) {
     extern __shared__ uint4 s_all[];
-    __shared__ unsigned s_rank[kRankWarps][32];
+    __shared__ unsigned s_rank[kRankWarps][kRankShare];
     unsigned* all = reinterpret_cast<unsigned*>(s_all);
     const unsigned padded = (n + 4 * kRankWarps - 1) / (4 * kRankWarps) * (4 * kRankWarps);
     for (unsigned i0 = threadIdx.x; i0 < padded; i0 += 8 * 32 * kRankWarps) {
@@ -220,25 +219,31 @@ __global__ void __launch_bounds__(32 * kRankWarps) sort_few_kernel(const Keys ke
     }
     for (unsigned i = blockIdx.x * 32 * kRankWarps + threadIdx.x; i < counters; i += gridDim.x * 32 * kRankWarps) arrived[i] = 0;
     __syncthreads();
-    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32, i = blockIdx.x * 32 + lane;
-    const unsigned mine = i < n ? all[i] : 0;
-    unsigned rank = 0;
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32, base = blockIdx.x * kRankShare;
+    const unsigned mine0 = base + lane < n ? all[base + lane] : 0u, mine1 = base + 32 + lane < n ? all[base + 32 + lane] : 0u;
+    unsigned rank0 = 0, rank1 = 0;
     const unsigned quads = padded / (4 * kRankWarps);
 #pragma unroll 4
     for (unsigned j = 0; j < quads; ++j) {
         const uint4 k = s_all[warp * quads + j];
-        count_below(k.x, mine, rank);
-        count_below(k.y, mine, rank);
-        count_below(k.z, mine, rank);
-        count_below(k.w, mine, rank);
+        count_below(k.x, mine0, rank0);
+        count_below(k.y, mine0, rank0);
+        count_below(k.z, mine0, rank0);
+        count_below(k.w, mine0, rank0);
+        count_below(k.x, mine1, rank1);
+        count_below(k.y, mine1, rank1);
+        count_below(k.z, mine1, rank1);
+        count_below(k.w, mine1, rank1);
     }
-    s_rank[warp][lane] = rank;
+    s_rank[warp][lane] = rank0;
+    s_rank[warp][32 + lane] = rank1;
     __syncthreads();
-    if (warp == 0 && i < n) {
-        rank = 0;
+    const unsigned i = base + threadIdx.x;
+    if (threadIdx.x < kRankShare && i < n) {
+        unsigned rank = 0;
 #pragma unroll
-        for (int w = 0; w < kRankWarps; ++w) rank += s_rank[w][lane];
-        const unsigned key = mine >> kRankBits;
+        for (int w = 0; w < kRankWarps; ++w) rank += s_rank[w][threadIdx.x];
+        const unsigned key = all[i] >> kRankBits;
         keys[rank] = key;
         places[rank] = i;
         if (key != (unsigned)key_of.vocab) some[key] = rank;
@@ -677,7 +682,7 @@ int ampq_embed_backward(int device, void* cuda_stream, int dtype, int index_type
     if (n > 0) {
         const Keys key_of{tokens, vocab, padding, index_type == AMPQ_I64};
         if (plan.few) {
-            sort_few_kernel<<<(unsigned)((n + 31) / 32), 32 * kRankWarps, (size_t)((n + 4 * kRankWarps - 1) / (4 * kRankWarps) * (16 * kRankWarps)), st>>>(
+            sort_few_kernel<<<(unsigned)((n + kRankShare - 1) / kRankShare), 32 * kRankWarps, (size_t)((n + 4 * kRankWarps - 1) / (4 * kRankWarps) * (16 * kRankWarps)), st>>>(
                 key_of, (unsigned)n, words(plan.keys[0]), words(plan.places[0]), some, arrived, counters);
         } else {
             token_keys_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, st>>>(key_of, (unsigned)n, words(plan.keys[0]), arrived, counters);
