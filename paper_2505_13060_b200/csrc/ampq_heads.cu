@@ -25,9 +25,10 @@ constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
 // not the same ones where the pairs are neighbours).
 constexpr int kForwardThreads = 128, kBackwardThreads = 256;
 template <int V, bool NEXT>
-constexpr int kForwardCtas = V >= 8 && NEXT ? 4 : 5;
+constexpr int kForwardCtas = 4;
 constexpr int kBackwardCtas = 2;
 constexpr int kMaxRun = 4;  // steps of a run
+constexpr int kTogether = 2;
 
 struct Side {  // queries or keys
     const void *x, *gy, *w;
@@ -341,9 +342,10 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_n
     constexpr int kThreads = kForwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
+    constexpr int U = ASYNC ? kTogether : 1;  // steps that a warp works on together
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ unsigned s_amax[kWarps][64];
-    __shared__ uint4 s_in[2][2][ASYNC ? kThreads : 1];  // [turn][vector][thread]
+    __shared__ uint4 s_in[2][2 * U][ASYNC ? kThreads : 1];  // [turn][step, vector][thread]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int cols = COLS ? COLS : a.cols, half = COLS ? COLS / 2 : a.half;
     const float inv_cols = COLS ? 1.0f / (float)COLS : a.inv_cols;
@@ -366,28 +368,32 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_n
         raw[i][1].zero();
     }
     uint4* places = &s_in[0][0][ASYNC ? threadIdx.x : 0];
-    constexpr int kTurn = 2 * kThreads;
+    constexpr int kTurn = 2 * U * kThreads;
     if constexpr (ASYNC)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 4 * U; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
     int turn = 0;
     const long long x_step = per * q.x_head, out_step = per * q.out_head;
+    const int end = min(heads, mine.head0 + steps * per);  // behind this lane's heads
     const T* in = nullptr;
     auto fetch = [&](int head) {
-        if (head < heads) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (ok[i]) {
+        for (int u = 0; u < U; ++u) {
+            if (head + u * per < end) {
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        if constexpr (ASYNC)
-                            copy_async<16>(places + turn + m * kThreads, in + col[i].col[m]);
-                        else
-                            raw[i][m].load(in + col[i].col[m]);
+                for (int i = 0; i < NV; ++i)
+                    if (ok[i]) {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            if constexpr (ASYNC)
+                                copy_async<16>(places + turn + (2 * u + m) * kThreads, in + col[i].col[m]);
+                            else
+                                raw[i][m].load(in + col[i].col[m]);
+                        }
                     }
-                }
+            }
+            in += x_step;
         }
-        in += x_step;
     };
     in = mine.at(static_cast<const T*>(q.x), q.x_batch, q.x_token, q.x_head);
     fetch(mine.head0);
@@ -430,116 +436,145 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_n
                     for (int k = 0; k < P; ++k) f[i][m][k] = w[m][k];
             }
         }
-        for (int step = 0, head = mine.head0; step < steps; ++step, head += per) {
-            const bool live = head < heads;
-            // the next step's elements, or the next token's: into the other place, or behind this step's in the registers
+        for (int step = 0, head = mine.head0; step < steps; step += U, head += U * per) {
+            // the next steps' elements, or the next token's: into the other place, or behind these in the registers
             auto ahead = [&] {
-                if (step + 1 < steps) {
-                    fetch(head + per);
+                if (step + U < steps) {
+                    fetch(head + U * per);
                 } else if (more) {
                     in = mine.at(static_cast<const T*>(q.x), q.x_batch, q.x_token, q.x_head);
                     fetch(mine.head0);
                 }
             };
+            const uint4* now = places + turn;
             if constexpr (ASYNC) {
-                const uint4* now = places + turn;
                 turn ^= kTurn;
                 ahead();
                 commit_async();
                 wait_async<1>();
-#pragma unroll
-                for (int m = 0; m < 2; ++m) raw[0][m].take(now + m * kThreads);
             }
-            float2 x[NV][2][P];
-            float2 sq = make_float2(0.0f, 0.0f);
+            float2 x[U][NV][2][P];
+            float rstd[U];
+            bool live[U];
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    raw[i][m].unpack(x[i][m]);
-#pragma unroll
-                    for (int k = 0; k < P; ++k) sq = __ffma2_rn(x[i][m][k], x[i][m][k], sq);
-                }
-            if constexpr (!ASYNC) ahead();
-            const float rstd = inverse_root(head_sum(sq.x + sq.y, lanes) * inv_cols + a.eps);
-            if (live && sub == 0) *stat = rstd;
-            stat += per;
-            if (FMT) {
-                // bits of the largest |x| of each group of 32 columns, a NaN on top
-                unsigned top[NV][2];
+            for (int u = 0; u < U; ++u) {
+                live[u] = head + u * per < end;
+                float2 sq = make_float2(0.0f, 0.0f);
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
-                        float t = 0.0f;
+                        if (ASYNC) raw[i][m].take(now + (2 * u + m) * kThreads);
+                        raw[i][m].unpack(x[u][i][m]);
 #pragma unroll
-                        for (int k = 0; k < P; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x[i][m][k].x), "f"(x[i][m][k].y));
-                        top[i][m] = __float_as_uint(t) & 0x7FFFFFFFu;
+                        for (int k = 0; k < P; ++k) sq = __ffma2_rn(x[u][i][m][k], x[u][i][m][k], sq);
                     }
+                rstd[u] = sq.x + sq.y;
+            }
+            if constexpr (!ASYNC) ahead();
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (COLS && o >= lanes) continue;
+                    const float t = __shfl_xor_sync(0xFFFFFFFFu, rstd[u], o);
+                    rstd[u] = o < lanes ? rstd[u] + t : rstd[u];
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                rstd[u] = inverse_root(rstd[u] * inv_cols + a.eps);
+                if (live[u] && sub == 0) stat[u * per] = rstd[u];
+            }
+            stat += U * per;
+            if (FMT) {
+                // bits of the largest |x| of each group of 32 columns, a NaN on top
+                unsigned top[U][NV][2];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            float t = 0.0f;
+#pragma unroll
+                            for (int k = 0; k < P; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x[u][i][m][k].x), "f"(x[u][i][m][k].y));
+                            top[u][i][m] = __float_as_uint(t) & 0x7FFFFFFFu;
+                        }
                 if (COLS || a.lane_groups) {
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        if (NEXT) top[i][0] = max(top[i][0], top[i][1]);
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int o = (NEXT ? kGroup / 2 : kGroup) / V / 2; o > 0; o >>= 1) {
-                            top[i][0] = max(top[i][0], __shfl_xor_sync(0xFFFFFFFFu, top[i][0], o));
-                            if (!NEXT) top[i][1] = max(top[i][1], __shfl_xor_sync(0xFFFFFFFFu, top[i][1], o));
+                        for (int i = 0; i < NV; ++i) {
+                            if (NEXT) top[u][i][0] = max(top[u][i][0], top[u][i][1]);
+#pragma unroll
+                            for (int o = (NEXT ? kGroup / 2 : kGroup) / V / 2; o > 0; o >>= 1) {
+                                top[u][i][0] = max(top[u][i][0], __shfl_xor_sync(0xFFFFFFFFu, top[u][i][0], o));
+                                if (!NEXT) top[u][i][1] = max(top[u][i][1], __shfl_xor_sync(0xFFFFFFFFu, top[u][i][1], o));
+                            }
+                            if (NEXT) top[u][i][1] = top[u][i][0];
                         }
-                        if (NEXT) top[i][1] = top[i][0];
-                    }
                 } else {
-                    unsigned* amax = s_amax[warp] + slot * ((cols + kGroup - 1) / kGroup);
-                    __syncwarp();
-                    s_amax[warp][lane] = s_amax[warp][lane + 32] = 0;
-                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
+                    for (int u = 0; u < U; ++u) {
+                        unsigned* amax = s_amax[warp] + slot * ((cols + kGroup - 1) / kGroup);
+                        __syncwarp();
+                        s_amax[warp][lane] = s_amax[warp][lane + 32] = 0;
+                        __syncwarp();
 #pragma unroll
-                        for (int m = 0; m < 2; ++m)
-                            if (live && ok[i]) atomicMax(amax + col[i].col[m] / kGroup, top[i][m]);
-                    __syncwarp();
+                        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
+                            for (int m = 0; m < 2; ++m)
+                                if (live[u] && ok[i]) atomicMax(amax + col[i].col[m] / kGroup, top[u][i][m]);
+                        __syncwarp();
 #pragma unroll
-                        for (int m = 0; m < 2; ++m)
-                            if (live && ok[i]) top[i][m] = amax[col[i].col[m] / kGroup];
+                        for (int i = 0; i < NV; ++i)
+#pragma unroll
+                            for (int m = 0; m < 2; ++m)
+                                if (live[u] && ok[i]) top[u][i][m] = amax[col[i].col[m] / kGroup];
+                    }
                 }
-                if (live) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (live[u]) {
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            if (!ok[i]) continue;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const int c0 = col[i].col[m];
+                                const unsigned byte = group_byte<FMT>(a.e4m3, top[u][i][m]);
+                                store_code_vec<V, FMT>(codes + c0, a.e4m3, byte, x[u][i][m]);
+                                if (c0 % kGroup == 0) scales[c0 / kGroup] = (unsigned char)byte;  // by whoever holds a group's first column
+                            }
+                        }
+                        if (cols % kGroup)
+                            for (int k = cols + sub; k < (cols + kGroup - 1) / kGroup * kGroup; k += lanes) codes[k] = 0;
+                    }
+                    codes += per * q.ld_codes;
+                    scales += per * q.ld_scales;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (live[u]) {
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         if (!ok[i]) continue;
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
-                            const int c0 = col[i].col[m];
-                            const unsigned byte = group_byte<FMT>(a.e4m3, top[i][m]);
-                            store_code_vec<V, FMT>(codes + c0, a.e4m3, byte, x[i][m]);
-                            if (c0 % kGroup == 0) scales[c0 / kGroup] = (unsigned char)byte;  // by whoever holds a group's first column
+                            float2 y[P];
+#pragma unroll
+                            for (int k = 0; k < P; ++k) {
+                                y[k] = __fmul2_rn(x[u][i][m][k], f[i][m][k]);
+                                if (turned[i]) y[k] = __ffma2_rn(partner<V, NEXT>(x[u][i], m, k), g[i][m][k], y[k]);
+                                y[k] = __fmul2_rn(y[k], make_float2(rstd[u], rstd[u]));
+                            }
+                            store_vec<T, V>(out + col[i].col[m], y);
                         }
                     }
-                    if (cols % kGroup)
-                        for (int k = cols + sub; k < (cols + kGroup - 1) / kGroup * kGroup; k += lanes) codes[k] = 0;
                 }
-                codes += per * q.ld_codes;
-                scales += per * q.ld_scales;
+                out += out_step;
             }
-            if (live) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!ok[i]) continue;
-                    float2 y[2][P];
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int k = 0; k < P; ++k) {
-                            y[m][k] = __fmul2_rn(x[i][m][k], f[i][m][k]);
-                            if (turned[i]) y[m][k] = __ffma2_rn(partner<V, NEXT>(x[i], m, k), g[i][m][k], y[m][k]);
-                            y[m][k] = __fmul2_rn(y[m][k], make_float2(rstd, rstd));
-                        }
-                    store_vec<T, V>(out + col[i].col[0], y[0]);
-                    store_vec<T, V>(out + col[i].col[1], y[1]);
-                }
-            }
-            out += out_step;
         }
     }
 }
