@@ -20,15 +20,17 @@ namespace ampq {
 namespace {
 
 constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
-// Threads of a CTA and CTAs that share an SM: as many warps as the registers leave
-// (forward above all the rotation's factors of an element and of its partner, which are
-// not the same ones where the pairs are neighbours).
-constexpr int kForwardThreads = 128, kBackwardThreads = 256;
-template <int V, bool NEXT>
-constexpr int kForwardCtas = 4;
-constexpr int kBackwardCtas = 2;
+// Threads of a CTA, CTAs that share an SM, and the steps that a warp works on together.
+// The shuffles, the root and the loads of a step are a chain of latencies: two steps
+// side by side fill it better than more warps would, and a spilled register costs more
+// than either brings.  Measured on 2 x 4096 tokens of 64 + 8 heads of 128 columns (one
+// step at a time with more warps, two): forward bf16 with a checkpoint 79 us, 75 us;
+// without 62 us, 58 us; fp32 118 us, 111 us; backward fp32 126 us, 118 us, but bf16
+// from 8 bits, whose sums and factors leave no room, 87 us, 95 us.
+constexpr int kForwardThreads = 128, kBackwardThreads = 128, kForwardCtas = 4, kBackwardCtas = 4, kForwardTogether = 2;
+template <typename T>
+constexpr int kBackwardTogether = sizeof(T) == 4 ? 2 : 1;
 constexpr int kMaxRun = 4;  // steps of a run
-constexpr int kTogether = 2;
 
 struct Side {  // queries or keys
     const void *x, *gy, *w;
@@ -273,14 +275,18 @@ __device__ __forceinline__ void take_weights(const float* w, float2 (&v)[kPairs<
     }
 }
 
-// Sum over the `lanes` neighbouring lanes of a head.
-__device__ __forceinline__ float head_sum(float s, int lanes) {
+// Sums over the `lanes` neighbouring lanes of a head, of U heads side by side.
+template <int U, int COLS>
+__device__ __forceinline__ void head_sums(float (&s)[U], int lanes) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        const float t = __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        s = o < lanes ? s + t : s;
+        if (COLS && o >= lanes) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float t = __shfl_xor_sync(0xFFFFFFFFu, s[u], o);
+            s[u] = o < lanes ? s[u] + t : s[u];
+        }
     }
-    return s;
 }
 
 // 1 / sqrt(v), the hardware's approximation improved by one of Newton's steps, to
@@ -338,11 +344,11 @@ struct Share {
 // COLS: heads of so many columns, all of them turned, or 0 for any.  What depends on
 // the columns alone is then known to the compiler (a third of the instructions).
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
-__global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_norm_forward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forward_kernel(const HeadArgs a) {
     constexpr int kThreads = kForwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
-    constexpr int U = ASYNC ? kTogether : 1;  // steps that a warp works on together
+    constexpr int U = ASYNC ? kForwardTogether : 1;  // steps that a warp works on together
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ unsigned s_amax[kWarps][64];
     __shared__ uint4 s_in[2][2 * U][ASYNC ? kThreads : 1];  // [turn][step, vector][thread]
@@ -472,14 +478,7 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas<V, NEXT>) head_n
                 rstd[u] = sq.x + sq.y;
             }
             if constexpr (!ASYNC) ahead();
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (COLS && o >= lanes) continue;
-                    const float t = __shfl_xor_sync(0xFFFFFFFFu, rstd[u], o);
-                    rstd[u] = o < lanes ? rstd[u] + t : rstd[u];
-                }
+            head_sums<U, COLS>(rstd, lanes);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 rstd[u] = inverse_root(rstd[u] * inv_cols + a.eps);
@@ -586,9 +585,10 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
     constexpr int kThreads = kBackwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
+    constexpr int U = ASYNC ? kBackwardTogether<T> : 1;  // steps that a warp works on together
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ float s_sums[kWarps][kHeadCols];
-    __shared__ uint4 s_in[2][4][ASYNC ? kThreads : 1];  // [turn][gradient, input or codes][thread]
+    __shared__ uint4 s_in[2][4 * U][ASYNC ? kThreads : 1];  // [turn][step, gradient, input or codes][thread]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int cols = COLS ? COLS : a.cols, half = COLS ? COLS / 2 : a.half;
     const float inv_cols = COLS ? 1.0f / (float)COLS : a.inv_cols;
@@ -616,8 +616,8 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
     if (mine.some) {
         Raw<T, V> raw_g[NV][2], raw_x[NV][2];
         RawCodes<V> raw_c[NV][2];
-        unsigned raw_s[NV][2];
-        float raw_r = 0.0f;
+        unsigned raw_s[U][NV][2];
+        float raw_r[U];
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -625,15 +625,19 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
                 raw_g[i][m].zero();
                 raw_x[i][m].zero();
                 raw_c[i][m].c = make_uint2(0, 0);
-                raw_s[i][m] = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw_s[u][i][m] = 0;
             }
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw_r[u] = 0.0f;
         uint4* places = &s_in[0][0][ASYNC ? threadIdx.x : 0];
-        constexpr int kTurn = 4 * kThreads;
+        constexpr int kTurn = 4 * U * kThreads;
         if constexpr (ASYNC)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < 8 * U; ++k) places[k * kThreads] = make_uint4(0, 0, 0, 0);
         int turn = 0;
         const long long g_step = per * q.gy_head, x_step = per * q.x_head, out_step = per * q.out_head;
+        const int end = min(heads, mine.head0 + steps * per);  // behind this lane's heads
         const T *gp = nullptr, *xp = nullptr;
         const unsigned char *cp = nullptr, *sp = nullptr;
         const float* rp = nullptr;
@@ -649,38 +653,41 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
             }
         };
         auto fetch = [&](int head) {
-            if (head < heads) {
-                raw_r = __ldg(rp);
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!ok[i]) continue;
+            for (int u = 0; u < U; ++u) {
+                if (head + u * per < end) {
+                    raw_r[u] = __ldg(rp);
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const int c0 = col[i].col[m];
-                        if constexpr (ASYNC) {
-                            copy_async<16>(places + turn + m * kThreads, gp + c0);
-                            if (FMT)
-                                copy_async<V>(places + turn + (2 + m) * kThreads, cp + c0);
-                            else
-                                copy_async<16>(places + turn + (2 + m) * kThreads, xp + c0);
-                        } else {
-                            raw_g[i][m].load(gp + c0);
-                            if (FMT)
-                                raw_c[i][m].load(cp + c0);
-                            else
-                                raw_x[i][m].load(xp + c0);
+                    for (int i = 0; i < NV; ++i) {
+                        if (!ok[i]) continue;
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const int c0 = col[i].col[m];
+                            if constexpr (ASYNC) {
+                                copy_async<16>(places + turn + (4 * u + m) * kThreads, gp + c0);
+                                if (FMT)
+                                    copy_async<V>(places + turn + (4 * u + 2 + m) * kThreads, cp + c0);
+                                else
+                                    copy_async<16>(places + turn + (4 * u + 2 + m) * kThreads, xp + c0);
+                            } else {
+                                raw_g[i][m].load(gp + c0);
+                                if (FMT)
+                                    raw_c[i][m].load(cp + c0);
+                                else
+                                    raw_x[i][m].load(xp + c0);
+                            }
+                            if (FMT) raw_s[u][i][m] = __ldg(sp + c0 / kGroup);
                         }
-                        if (FMT) raw_s[i][m] = __ldg(sp + c0 / kGroup);
                     }
                 }
-            }
-            gp += g_step;
-            rp += per;
-            if (FMT) {
-                cp += per * q.ld_codes;
-                sp += per * q.ld_scales;
-            } else {
-                xp += x_step;
+                gp += g_step;
+                rp += per;
+                if (FMT) {
+                    cp += per * q.ld_codes;
+                    sp += per * q.ld_scales;
+                } else {
+                    xp += x_step;
+                }
             }
         };
         begin();
@@ -697,87 +704,99 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (ok[i] && turned[i]) load_angles<V, NEXT>(a, half, here, col[i].angle, true, c[i], s[i]);
-            for (int step = 0, head = mine.head0; step < steps; ++step, head += per) {
-                const bool live = head < heads;
-                const float rstd = raw_r;
-                float scale[NV][2];
+            for (int step = 0, head = mine.head0; step < steps; step += U, head += U * per) {
+                bool live[U];
+                float rstd[U], dot[U];
+                float2 g[U][NV][2][P], h[U][NV][2][P];  // in the end u and x * rstd
+                float scale[U][NV][2];
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+                for (int u = 0; u < U; ++u) {
+                    live[u] = head + u * per < end;
+                    rstd[u] = raw_r[u];
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) scale[i][m] = scale_of(raw_s[i][m]);
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) scale[u][i][m] = FMT ? scale_of(raw_s[u][i][m]) * rstd[u] : rstd[u];  // a power of two: exact
+                }
                 auto ahead = [&] {
-                    if (step + 1 < steps) {
-                        fetch(head + per);
+                    if (step + U < steps) {
+                        fetch(head + U * per);
                     } else if (more) {
                         begin();
                         fetch(mine.head0);
                     }
                 };
+                const uint4* now = places + turn;
                 if constexpr (ASYNC) {
-                    const uint4* now = places + turn;
                     turn ^= kTurn;
                     ahead();
                     commit_async();
                     wait_async<1>();
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        raw_g[0][m].take(now + m * kThreads);
-                        if (FMT)
-                            raw_c[0][m].c = *reinterpret_cast<const uint2*>(now + (2 + m) * kThreads);  // fp32: the first word
-                        else
-                            raw_x[0][m].take(now + (2 + m) * kThreads);
-                    }
                 }
-                float2 g[NV][2][P], h[NV][2][P];
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        raw_g[i][m].unpack(g[i][m]);
-                        if constexpr (FMT != 0)
-                            raw_c[i][m].template unpack<FMT>(a.e4m3, scale[i][m], h[i][m]);
-                        else
-                            raw_x[i][m].unpack(h[i][m]);
-                    }
-                if constexpr (!ASYNC) ahead();
-                float2 dot = make_float2(0.0f, 0.0f);
-                if (live) {
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        if (!ok[i]) continue;
-                        float2 t[2][P];
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
-#pragma unroll
-                            for (int k = 0; k < P; ++k) {
-                                t[m][k] = g[i][m][k];
-                                if (turned[i]) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
-                                h[i][m][k] = __fmul2_rn(h[i][m][k], make_float2(rstd, rstd));
-                                gw[i][m][k] = __ffma2_rn(t[m][k], h[i][m][k], gw[i][m][k]);
-                                t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
-                                dot = __ffma2_rn(t[m][k], h[i][m][k], dot);
-                            }
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
-#pragma unroll
-                            for (int k = 0; k < P; ++k) g[i][m][k] = t[m][k];
-                    }
-                }
-                const float mean = -head_sum(dot.x + dot.y, lanes) * inv_cols;
-                if (live) {
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        if (!ok[i]) continue;
+                    for (int i = 0; i < NV; ++i)
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
+                            if (ASYNC) raw_g[i][m].take(now + (4 * u + m) * kThreads);
+                            raw_g[i][m].unpack(g[u][i][m]);
+                            if constexpr (FMT != 0) {
+                                if (ASYNC) raw_c[i][m].c = *reinterpret_cast<const uint2*>(now + (4 * u + 2 + m) * kThreads);  // fp32: the first word
+                                raw_c[i][m].template unpack<FMT>(a.e4m3, scale[u][i][m], h[u][i][m]);
+                            } else {
+                                if (ASYNC) raw_x[i][m].take(now + (4 * u + 2 + m) * kThreads);
+                                raw_x[i][m].unpack(h[u][i][m]);
 #pragma unroll
-                            for (int k = 0; k < P; ++k)
-                                g[i][m][k] = __fmul2_rn(__ffma2_rn(h[i][m][k], make_float2(mean, mean), g[i][m][k]), make_float2(rstd, rstd));
-                            store_vec<T, V>(out + col[i].col[m], g[i][m]);
+                                for (int k = 0; k < P; ++k) h[u][i][m][k] = __fmul2_rn(h[u][i][m][k], make_float2(rstd[u], rstd[u]));
+                            }
+                        }
+                if constexpr (!ASYNC) ahead();
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float2 sum = make_float2(0.0f, 0.0f);
+                    if (live[u]) {
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            if (!ok[i]) continue;
+                            float2 t[2][P];
+#pragma unroll
+                            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                                for (int k = 0; k < P; ++k) {
+                                    t[m][k] = g[u][i][m][k];
+                                    if (turned[i]) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[u][i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
+                                    gw[i][m][k] = __ffma2_rn(t[m][k], h[u][i][m][k], gw[i][m][k]);
+                                    t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
+                                    sum = __ffma2_rn(t[m][k], h[u][i][m][k], sum);
+                                }
+#pragma unroll
+                            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                                for (int k = 0; k < P; ++k) g[u][i][m][k] = t[m][k];
                         }
                     }
+                    dot[u] = sum.x + sum.y;
                 }
-                out += out_step;
+                head_sums<U, COLS>(dot, lanes);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (live[u]) {
+                        const float mean = -dot[u] * inv_cols;
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            if (!ok[i]) continue;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                                for (int k = 0; k < P; ++k)
+                                    g[u][i][m][k] = __fmul2_rn(__ffma2_rn(h[u][i][m][k], make_float2(mean, mean), g[u][i][m][k]), make_float2(rstd[u], rstd[u]));
+                                store_vec<T, V>(out + col[i].col[m], g[u][i][m]);
+                            }
+                        }
+                    }
+                    out += out_step;
+                }
             }
         }
     }
@@ -961,7 +980,7 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int warps, long 
 
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 int start(HeadArgs& a, bool backward, int sms, int ctas, cudaStream_t st) {
-    const long long most = backward ? (long long)ctas : (long long)kForwardCtas<V, NEXT> * sms;
+    const long long most = backward ? (long long)ctas : (long long)kForwardCtas * sms;
     const long long grid = lay_out(a, V, NEXT, backward, (backward ? kBackwardThreads : kForwardThreads) / 32, most);
     if (grid > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
     if (backward)
