@@ -24,10 +24,12 @@ constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
 // The shuffles, the root and the loads of a step are a chain of latencies: two steps
 // side by side fill it better than more warps would, and a spilled register costs more
 // than either brings.  Measured on 2 x 4096 tokens of 64 + 8 heads of 128 columns (one
-// step at a time with more warps, two): forward bf16 with a checkpoint 79 us, 75 us;
-// without 62 us, 58 us; fp32 118 us, 111 us; backward fp32 126 us, 118 us, but bf16
-// from 8 bits, whose sums and factors leave no room, 87 us, 95 us.
-constexpr int kForwardThreads = 128, kBackwardThreads = 128, kForwardCtas = 4, kBackwardCtas = 4, kForwardTogether = 2;
+// step at a time with more warps, then two together): forward bf16 with a checkpoint
+// 79 and 75 us, without 62 and 58 us, fp32 118 and 111 us; backward fp32 126 and 118
+// us, but bf16 from 8 bits, whose sums and factors leave no room, 87 and 95 us.
+constexpr int kForwardThreads = 128, kBackwardThreads = 128, kMostCtas = 4, kForwardTogether = 2;
+template <int V>
+constexpr int kCtas = V >= 4 ? kMostCtas : 3;  // small vectors come through registers
 template <typename T>
 constexpr int kBackwardTogether = sizeof(T) == 4 ? 2 : 1;
 constexpr int kMaxRun = 4;  // steps of a run
@@ -341,10 +343,13 @@ struct Share {
 
 // ---------------------------------------------------------------------------
 
+// Bound by HBM and, with a checkpoint, by the warps' latencies: 2 x 4096 tokens of
+// 64 + 8 heads of 128 columns, bf16, take 54 us (5.7 TB/s) and 69 us with the
+// checkpoint (5.6 TB/s), fp32 112 us (6.2 TB/s).
 // COLS: heads of so many columns, all of them turned, or 0 for any.  What depends on
 // the columns alone is then known to the compiler (a third of the instructions).
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
-__global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_kernel(const HeadArgs a) {
     constexpr int kThreads = kForwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
@@ -364,14 +369,18 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forwa
     const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
     bool ok[NV], turned[NV];
-    Raw<T, V> raw[NV][2];
+    constexpr int R = ASYNC ? 1 : U;
+    Raw<T, V> raw[R][NV][2];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         col[i] = columns_of<V, NEXT>(cols, half, sub + lanes * i);
         ok[i] = COLS > 0 || sub + lanes * i < a.vectors;
         turned[i] = COLS > 0 || col[i].angle >= 0;
-        raw[i][0].zero();  // lanes without a vector keep zeros; those of no head have anything
-        raw[i][1].zero();
+#pragma unroll
+        for (int u = 0; u < R; ++u) {  // lanes without a vector keep zeros; those of no head have anything
+            raw[u][i][0].zero();
+            raw[u][i][1].zero();
+        }
     }
     uint4* places = &s_in[0][0][ASYNC ? threadIdx.x : 0];
     constexpr int kTurn = 2 * U * kThreads;
@@ -394,7 +403,7 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forwa
                             if constexpr (ASYNC)
                                 copy_async<16>(places + turn + (2 * u + m) * kThreads, in + col[i].col[m]);
                             else
-                                raw[i][m].load(in + col[i].col[m]);
+                                raw[u % R][i][m].load(in + col[i].col[m]);
                         }
                     }
             }
@@ -470,8 +479,8 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forwa
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
-                        if (ASYNC) raw[i][m].take(now + (2 * u + m) * kThreads);
-                        raw[i][m].unpack(x[u][i][m]);
+                        if (ASYNC) raw[0][i][m].take(now + (2 * u + m) * kThreads);
+                        raw[u % R][i][m].unpack(x[u][i][m]);
 #pragma unroll
                         for (int k = 0; k < P; ++k) sq = __ffma2_rn(x[u][i][m][k], x[u][i][m][k], sq);
                     }
@@ -579,13 +588,16 @@ __global__ void __launch_bounds__(kForwardThreads, kForwardCtas) head_norm_forwa
 }
 
 // A warp's sums for the weight's gradient stay in registers over its tokens;
-// part[CTA][column] of a side's CTAs are joined afterwards.
+// part[CTA][column] of a side's CTAs are joined afterwards.  The same size: bf16 81 us
+// from 8 bits (4.7 TB/s), 83 us from the input (5.6 TB/s), fp32 118 us from 8 bits;
+// 16 warps an SM and instructions bound the first (77 us of it, 4 the joining).
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
-__global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_backward_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward_kernel(const HeadArgs a) {
     constexpr int kThreads = kBackwardThreads, kWarps = kThreads / 32;
     constexpr int P = kPairs<V>;
     constexpr bool ASYNC = kAsync<T, V>;
     constexpr int U = ASYNC ? kBackwardTogether<T> : 1;  // steps that a warp works on together
+    constexpr int R = ASYNC ? 1 : U;
     __shared__ alignas(16) float s_w[2][kHeadCols];
     __shared__ float s_sums[kWarps][kHeadCols];
     __shared__ uint4 s_in[2][4 * U][ASYNC ? kThreads : 1];  // [turn][step, gradient, input or codes][thread]
@@ -614,17 +626,20 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
         }
     }
     if (mine.some) {
-        Raw<T, V> raw_g[NV][2], raw_x[NV][2];
-        RawCodes<V> raw_c[NV][2];
+        Raw<T, V> raw_g[R][NV][2], raw_x[R][NV][2];
+        RawCodes<V> raw_c[R][NV][2];
         unsigned raw_s[U][NV][2];
         float raw_r[U];
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                raw_g[i][m].zero();
-                raw_x[i][m].zero();
-                raw_c[i][m].c = make_uint2(0, 0);
+#pragma unroll
+                for (int u = 0; u < R; ++u) {
+                    raw_g[u][i][m].zero();
+                    raw_x[u][i][m].zero();
+                    raw_c[u][i][m].c = make_uint2(0, 0);
+                }
 #pragma unroll
                 for (int u = 0; u < U; ++u) raw_s[u][i][m] = 0;
             }
@@ -670,11 +685,11 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
                                 else
                                     copy_async<16>(places + turn + (4 * u + 2 + m) * kThreads, xp + c0);
                             } else {
-                                raw_g[i][m].load(gp + c0);
+                                raw_g[u % R][i][m].load(gp + c0);
                                 if (FMT)
-                                    raw_c[i][m].load(cp + c0);
+                                    raw_c[u % R][i][m].load(cp + c0);
                                 else
-                                    raw_x[i][m].load(xp + c0);
+                                    raw_x[u % R][i][m].load(xp + c0);
                             }
                             if (FMT) raw_s[u][i][m] = __ldg(sp + c0 / kGroup);
                         }
@@ -739,14 +754,14 @@ __global__ void __launch_bounds__(kBackwardThreads, kBackwardCtas) head_norm_bac
                     for (int i = 0; i < NV; ++i)
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
-                            if (ASYNC) raw_g[i][m].take(now + (4 * u + m) * kThreads);
-                            raw_g[i][m].unpack(g[u][i][m]);
+                            if (ASYNC) raw_g[0][i][m].take(now + (4 * u + m) * kThreads);
+                            raw_g[u % R][i][m].unpack(g[u][i][m]);
                             if constexpr (FMT != 0) {
-                                if (ASYNC) raw_c[i][m].c = *reinterpret_cast<const uint2*>(now + (4 * u + 2 + m) * kThreads);  // fp32: the first word
-                                raw_c[i][m].template unpack<FMT>(a.e4m3, scale[u][i][m], h[u][i][m]);
+                                if (ASYNC) raw_c[0][i][m].c = *reinterpret_cast<const uint2*>(now + (4 * u + 2 + m) * kThreads);  // fp32: the first word
+                                raw_c[u % R][i][m].template unpack<FMT>(a.e4m3, scale[u][i][m], h[u][i][m]);
                             } else {
-                                if (ASYNC) raw_x[i][m].take(now + (4 * u + 2 + m) * kThreads);
-                                raw_x[i][m].unpack(h[u][i][m]);
+                                if (ASYNC) raw_x[0][i][m].take(now + (4 * u + 2 + m) * kThreads);
+                                raw_x[u % R][i][m].unpack(h[u][i][m]);
 #pragma unroll
                                 for (int k = 0; k < P; ++k) h[u][i][m][k] = __fmul2_rn(h[u][i][m][k], make_float2(rstd[u], rstd[u]));
                             }
@@ -860,7 +875,7 @@ __global__ void __launch_bounds__(1024) head_join_kernel(const JoinArgs a) {
 
 // CTAs of the backward pass: no more than are resident, four to a token at most.
 int backward_ctas(long long rows, int sms) {
-    const long long most = (long long)kBackwardCtas * sms;
+    const long long most = (long long)kMostCtas * sms;
     return rows == 0 ? 0 : (int)(4 * rows < most ? 4 * rows : most);
 }
 
@@ -939,11 +954,12 @@ Side side_of(const ampq_heads* h, bool backward, bool kept) {
 }
 
 // Sets up the lanes of a head, the runs, and the CTAs of each side; returns the grid's size.
-long long lay_out(HeadArgs& a, int V, bool next, bool backward, int warps, long long ctas) {
+constexpr int kTokenWork = 2;
+long long lay_out(HeadArgs& a, int V, int NV, bool next, bool backward, int warps, int together, long long ctas) {
     a.vectors = a.cols / 2 / V;
     a.lanes = 1;
-    while (a.lanes < 32 && a.lanes < a.vectors) a.lanes *= 2;
-    a.lane_groups = next ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0;
+    while (a.lanes * NV < a.vectors) a.lanes *= 2;
+    a.lane_groups = (next ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0) && (next ? kGroup / 2 : kGroup) / V <= a.lanes;
     const int per = 32 / a.lanes;
     const int steps[2] = {(a.side[0].heads + per - 1) / per, (a.side[1].heads + per - 1) / per};
     const long long most = ctas * warps;
@@ -969,9 +985,13 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int warps, long 
         grid = need < most / warps ? need : most / warps;
         if (grid < total / warps) grid = total / warps;
     }
-    // the CTAs go to the sides by their steps, one warp to a run at least
+    // The CTAs go to the sides by their work, one warp to a run at least.  What a run does
+    // once for a token is about two steps' work, and steps are done `together`.  (Shared out
+    // by steps alone the keys' CTAs of 64 + 8 heads came last: 77 us instead of 69.)
     const long long least[2] = {(a.runs[0] + warps - 1) / warps, (a.runs[1] + warps - 1) / warps};
-    long long first = (grid * steps[0] + (steps[0] + steps[1]) / 2) / (steps[0] + steps[1]);
+    long long work[2];
+    for (int s = 0; s < 2; ++s) work[s] = (long long)a.runs[s] * (kTokenWork + (a.run[s] + together - 1) / together * together);
+    long long first = (grid * work[0] + (work[0] + work[1]) / 2) / (work[0] + work[1]);
     first = first < least[0] ? least[0] : first > grid - least[1] ? grid - least[1] : first;
     a.ctas[0] = (int)first;
     a.ctas[1] = (int)(grid - first);
@@ -980,8 +1000,9 @@ long long lay_out(HeadArgs& a, int V, bool next, bool backward, int warps, long 
 
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 int start(HeadArgs& a, bool backward, int sms, int ctas, cudaStream_t st) {
-    const long long most = backward ? (long long)ctas : (long long)kForwardCtas * sms;
-    const long long grid = lay_out(a, V, NEXT, backward, (backward ? kBackwardThreads : kForwardThreads) / 32, most);
+    long long most = (long long)kCtas<V> * sms;
+    if (backward && most > ctas) most = ctas;
+    const long long grid = lay_out(a, V, NV, NEXT, backward, (backward ? kBackwardThreads : kForwardThreads) / 32, kAsync<T, V> ? (backward ? kBackwardTogether<T> : kForwardTogether) : 1, most);
     if (grid > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
     if (backward)
         head_norm_backward_kernel<T, V, NV, NEXT, FMT, COLS><<<(unsigned)grid, kBackwardThreads, 0, st>>>(a);
@@ -1009,8 +1030,8 @@ int pick(HeadArgs& a, int fmt, bool backward, int dtype, int sms, int ctas, cuda
         return kept ? start<T, kWide, 1, NEXT, kEither, 0>(a, backward, sms, ctas, st) : start<T, kWide, 1, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
     }
     if (vectors_fit(a, dtype, 2))
-        return kept ? start<T, 2, kHeadCols / 128, NEXT, kEither, 0>(a, backward, sms, ctas, st)
-                    : start<T, 2, kHeadCols / 128, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
+        return kept ? start<T, 2, kHeadCols / 64, NEXT, kEither, 0>(a, backward, sms, ctas, st)
+                    : start<T, 2, kHeadCols / 64, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
     return kept ? start<T, 1, kHeadCols / 64, NEXT, kEither, 0>(a, backward, sms, ctas, st)
                 : start<T, 1, kHeadCols / 64, NEXT, AMPQ_FMT_BASE, 0>(a, backward, sms, ctas, st);
 }
