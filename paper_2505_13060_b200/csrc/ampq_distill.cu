@@ -19,6 +19,9 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 // vectors that a thread has in flight, and CTAs that share an SM
 constexpr int kForwardAhead = 1, kForwardCtas = 8;
 constexpr int kBackwardAhead = 1, kBackwardCtas = 6;
+constexpr int kPartVectors = 8 * kThreads;           // of the gradient's part of a row
+constexpr unsigned kPartColumns = 16 * kPartVectors;  // at most
+constexpr int kFewEntries = 128;  // 100: 333 us compared, 358 us with bits; 256: 530 and 369 us (4096 rows of 128000)
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
 struct DistillArgs {
@@ -262,13 +265,20 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
 
 // gs_j = gl T (q_j - sum of the p of the entries of column j).  A CTA writes its part
 // of a row by the formula's first term, and then once more the columns of the list
-// that lie in it, by the whole formula: a barrier is between the two.
-template <typename T>
+// that lie in it, by the whole formula: a barrier is between the two.  A column that
+// is listed more than once is stored by its first entry, with the sum of all.  Few
+// entries are compared with each other.  Of MANY each leaves a bit for its column, and
+// who finds it there sets one that says so: compared with each other a thousand took
+// 15 times the rest of the kernel, but the bits cost a short list 5 % of it.
+template <typename T, bool MANY>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
     __shared__ List list;
     __shared__ float s_top[kWarps];
     __shared__ float s_sums[kWarps][1];
+    __shared__ unsigned s_listed[MANY ? kPartColumns / 32 + 1 : 1], s_again[MANY ? kPartColumns / 32 + 1 : 1];
+    if (MANY)  // seen by all behind the list's barrier
+        for (int i = threadIdx.x; i < (int)kPartColumns / 32 + 1; i += kThreads) s_listed[i] = s_again[i] = 0;
     const unsigned part = blockIdx.x % (unsigned)a.parts;
     const long long row = blockIdx.x / (unsigned)a.parts;
     const T* x = static_cast<const T*>(a.logits) + row * a.ld;
@@ -335,17 +345,34 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kern
     }
     block_sum(sums, s_sums);
     const float inv_sum = 1.0f / sums[0];
+    auto place = [&](unsigned j) {  // a column's bit: those of the part's vectors, then the row's first and last ones
+        const unsigned at = j - r.head, vectors = r.vectors * K::kElems;
+        return j >= r.head && at < vectors ? at - begin * K::kElems : kPartColumns + (j < r.head ? j : 16 + at - vectors);
+    };
+    if (MANY) {
+        for (int k = threadIdx.x; k < a.top; k += kThreads) {
+            const unsigned j = list.index[k];
+            if (j >= a.cols || !mine(j)) continue;
+            const unsigned p = place(j);
+            if (atomicOr(s_listed + p / 32, 1u << p % 32) >> p % 32 & 1) atomicOr(s_again + p / 32, 1u << p % 32);
+        }
+        __syncthreads();
+    }
     for (int k = threadIdx.x; k < a.top; k += kThreads) {
         const unsigned j = list.index[k];
         if (j >= a.cols || !mine(j)) continue;
         float e = 0.0f;
-        bool again = false;  // an earlier entry of the same column stores it
-        for (int i = 0; i < a.top; ++i)
-            if (list.index[i] == j) {
-                e += list.t[i];
-                again |= i < k;
-            }
-        if (!again) store_elem(out + j, (exp2_fast((list.s[k] - m) * a.k) * inv - e * inv_sum) * c);
+        bool later = false;
+        if (MANY && !(s_again[place(j) / 32] >> place(j) % 32 & 1)) {
+            e = list.t[k];
+        } else {
+            for (int i = 0; i < a.top; ++i)
+                if (list.index[i] == j) {
+                    e += list.t[i];
+                    later |= i < k;
+                }
+        }
+        if (!later) store_elem(out + j, (exp2_fast((list.s[k] - m) * a.k) * inv - e * inv_sum) * c);
     }
 }
 
@@ -405,10 +432,11 @@ template <typename T>
 int launch_backward(DistillArgs a, cudaStream_t st) {
     // a part of a row: eight vectors a thread
     const long long vectors = (long long)a.cols / Row<T>::E;
-    const long long parts = (vectors + 8 * kThreads - 1) / (8 * kThreads);
+    const long long parts = (vectors + kPartVectors - 1) / kPartVectors;
     a.parts = parts < 1 ? 1 : (int)parts;
     if (a.rows * a.parts > 0x7FFFFFFFLL) return AMPQ_ERR_TOO_LARGE;
-    distill_backward_kernel<T><<<(unsigned)(a.rows * a.parts), kThreads, 0, st>>>(a);
+    auto kernel = a.top > kFewEntries ? distill_backward_kernel<T, true> : distill_backward_kernel<T, false>;
+    kernel<<<(unsigned)(a.rows * a.parts), kThreads, 0, st>>>(a);
     return launched();
 }
 

@@ -842,27 +842,35 @@ __global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward
 }
 
 // Adds up the CTAs' partial rows of a side, queries (blockIdx.y 0) and keys, in a fixed
-// order: 32 columns to a block, 32 parts at a time.
+// order: eight columns to a block, 128 parts at a time.
 struct JoinArgs {
     const float* part[2];
     void* out[2];
     int parts[2], cols, pitch;
     bool bf16;
 };
-__global__ void __launch_bounds__(1024) head_join_kernel(const JoinArgs a) {
-    __shared__ float sums[32][32];
-    const int side = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
+constexpr int kJoinCols = 8, kJoinWays = 128, kJoinSums = 16;
+__global__ void __launch_bounds__(kJoinCols* kJoinWays) head_join_kernel(const JoinArgs a) {
+    __shared__ float sums[kJoinWays][kJoinCols + 1], few[kJoinSums][kJoinCols + 1];
+    const int side = blockIdx.y, x = threadIdx.x, y = threadIdx.y, c = blockIdx.x * kJoinCols + x;
     if (!a.out[side]) return;
     float s = 0.0f;
     if (c < a.cols)
 #pragma unroll 5
-        for (int p = threadIdx.y; p < a.parts[side]; p += 32) s += __ldg(a.part[side] + (long long)p * a.pitch + c);
-    sums[threadIdx.y][threadIdx.x] = s;
+        for (int p = y; p < a.parts[side]; p += kJoinWays) s += __ldg(a.part[side] + (long long)p * a.pitch + c);
+    sums[y][x] = s;
     __syncthreads();
-    if (threadIdx.y == 0 && c < a.cols) {
+    if (y < kJoinSums) {
         float t = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) t += sums[k][threadIdx.x];
+        for (int k = 0; k < kJoinWays / kJoinSums; ++k) t += sums[y * (kJoinWays / kJoinSums) + k][x];
+        few[y][x] = t;
+    }
+    __syncthreads();
+    if (y == 0 && c < a.cols) {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kJoinSums; ++k) t += few[k][x];
         if (a.bf16)
             store_elem(static_cast<__nv_bfloat16*>(a.out[side]) + c, t);
         else
@@ -1134,7 +1142,7 @@ int ampq_head_norm_backward(int device, void* cuda_stream, int dtype, int param_
     }
     j.cols = a.cols; j.pitch = a.pitch;
     j.bf16 = a.param_bf16;
-    head_join_kernel<<<dim3((unsigned)(a.cols + 31) / 32, 2), dim3(32, 32), 0, st>>>(j);
+    head_join_kernel<<<dim3((unsigned)((a.cols + kJoinCols - 1) / kJoinCols), 2), dim3(kJoinCols, kJoinWays), 0, st>>>(j);
     return launched();
 }
 

@@ -11,7 +11,9 @@ The calls of ``include/ampq.h`` (``ampq_embed_*``, ``ampq_head_norm_*``,
 ``ampq_distill_*``): operands are float32 or bfloat16, indices int32 or int64,
 outputs and workspaces come from torch's caching allocator, and everything runs on
 torch's current stream of the tensors' device.  No index is checked on the host (that
-would wait for the device); the kernels use none that is out of range.
+would wait for the device); the kernels use none that is out of range.  Everything can
+be captured into a graph; a captured backward pass has leaves of its own, as any of
+torch's.
 """
 from __future__ import annotations
 

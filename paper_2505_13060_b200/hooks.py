@@ -226,8 +226,8 @@ class Calibrator:
                 self._replaced.append((m, layer_norm if isinstance(m, torch.nn.LayerNorm) else rms_norm))
             elif self._plain(m, decoder.HeadNorm):
 
-                def head_norm(q, k, cos=None, sin=None, positions=None, fmt=fmt, plain=m.forward):
-                    return plain(q, k, cos, sin, positions, fmt if scored() else ampq.FMT_BASE)
+                def head_norm(q, k, cos=None, sin=None, positions=None, fmt=ampq.FMT_BASE, plain=m.forward):
+                    return plain(q, k, cos, sin, positions, self.checkpoint if scored() and fmt == ampq.FMT_BASE else fmt)
 
                 self._replaced.append((m, head_norm))
 

@@ -534,3 +534,16 @@ def test_embed_grad_of_one_run(dec, n):
     if n < 10000:
         check_embed_grad(dec, tokens.cuda(), randn((n, 1100), torch.bfloat16, n), 7, 1.0)
         check_embed_grad(dec, tokens.cuda(), randn((n, 523), torch.float32, n), 7, 1.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=IDS.get)
+def test_distill_of_repeated_columns(dec, dtype):
+    """Long lists with columns listed many times over, the row's first and last columns among them, in rows of one part and
+    of several."""
+    for rows, cols, top, seed in [(6, 45, 900, 1), (5, 50021, 1024, 2), (4, 70007, 129, 3), (3, 40, 128, 4)]:
+        s = randn((rows, cols), dtype, seed, 2.0)
+        index = lists(rows, cols, top, seed)
+        index[:, ::7] = 0
+        index[:, 3::7] = cols - 1
+        index[0, 1::7] = cols // 2
+        check_distill(dec, s, index, randn((rows, top), torch.float32, seed + 10), 1.0)

@@ -454,3 +454,32 @@ def test_divergence_of_a_configuration(ampq, dec):
         with cal.sample(0):
             net(tokens[:1]).square().mean().backward()
         assert len(cal.end()) == 13
+
+
+def test_head_norm_module_in_a_calibration(ampq, dec):
+    """Outside of samples, and without gradients inside of one, the module keeps what it is told to; a format that the call
+    names is not replaced; the forward pass is the same one."""
+    with a_decoder(ampq, dec) as (hooks, net, ctx, tokens, index, teacher):
+        m = net.blocks[0].head_norm
+        cos, sin = (t.cuda() for t in net.turn)
+        q, k = randn((1, 24, 4, 32), 1).requires_grad_(), randn((1, 24, 2, 32), 2)
+        want = m(q, k, cos, sin)
+        cal = hooks.Calibrator(ctx, net, 1, checkpoint=1)
+        cal.begin()
+
+        def codes(**fmt):
+            kept = []
+            with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
+                y = m(q, k=k, cos=cos, sin=sin, positions=None, **fmt)
+            assert all(torch.equal(a, b) for a, b in zip(y, want))
+            return [t for t in kept if t.dtype == torch.uint8]
+
+        assert not codes()
+        with cal.sample(0):
+            by_default, e5m2 = codes(), codes(fmt=2)
+            with torch.no_grad():
+                assert not codes()
+            net(tokens[:1]).square().mean().backward()
+        assert len(by_default) == 4 and not torch.equal(by_default[0], e5m2[0])
+        assert not codes() and len(codes(fmt=2)) == 4
+        cal.end()
