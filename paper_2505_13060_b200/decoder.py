@@ -36,6 +36,19 @@ def _index_code(t: torch.Tensor) -> int:
     return code
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of t's shape and type.  (Like a tensor or with strides torch makes one in half the time.)"""
+    return torch.empty_like(t) if t.is_contiguous() else _new(t.shape, t.dtype, t.device)
+
+
+def _new(shape, dtype, where) -> torch.Tensor:
+    strides, n = [], 1
+    for d in reversed(shape):
+        strides.append(n)
+        n *= d or 1
+    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=where)
+
+
 # -- embedding --------------------------------------------------------------------------------------------------------
 
 
@@ -49,7 +62,7 @@ def embed(tokens: torch.Tensor, weight: torch.Tensor, scale: float = 1.0) -> tor
     index, code = _index_code(tokens), _code(w)
     t = tokens if tokens.is_contiguous() else tokens.contiguous()
     vocab, cols = w.shape
-    y = torch.empty(*tokens.shape, cols, dtype=w.dtype, device=w.device)
+    y = _new((*tokens.shape, cols), w.dtype, w.device)
     _check(ampq.lib().ampq_embed_forward(device, _stream_of(device), code, index, t.data_ptr(), t.numel(), w.data_ptr(), _pitch(w), vocab, cols, scale,
                                          y.data_ptr(), cols), "ampq_embed_forward")
     return y
@@ -76,9 +89,9 @@ def embed_backward(tokens: torch.Tensor, gy: torch.Tensor, vocab: int, scale: fl
     index, code = _index_code(tokens), _code(g)
     t = tokens if tokens.is_contiguous() else tokens.contiguous()
     n, cols = g.shape
-    gw = torch.empty(vocab, cols, dtype=g.dtype, device=g.device)
+    gw = _new((vocab, cols), g.dtype, g.device)
     need = _embed_backward_bytes(device, code, n, vocab, cols)
-    ws = torch.empty(need, dtype=torch.uint8, device=g.device)
+    ws = _new((need,), torch.uint8, g.device)
     _check(ampq.lib().ampq_embed_backward(device, _stream_of(device), code, index, t.data_ptr(), n, g.data_ptr(), _pitch(g), vocab, cols, scale, padding,
                                           gw.data_ptr(), ws.data_ptr(), need), "ampq_embed_backward")
     return gw
@@ -194,8 +207,8 @@ def head_norm_forward(q: torch.Tensor, k, wq=None, wk=None, cos=None, sin=None, 
     pcode = _code(wq) if wq is not None else _code(wk) if wk is not None else code
 
     def side(x, w):
-        y = torch.empty(x.shape, dtype=x.dtype, device=where)
-        r = torch.empty(x.shape[:3], dtype=torch.float32, device=where)
+        y = _like(x)
+        r = _new(x.shape[:3], torch.float32, where)
         p = _new_packed(r.numel(), cols, fmt, where) if fmt != ampq.FMT_BASE else None
         return y, r, p, _side(y, r, w, x=x, kept=p)
 
@@ -256,11 +269,11 @@ def head_norm_backward(gq: torch.Tensor, gk, q, k, rq: torch.Tensor, rk=None, wq
                 raise ValueError("input %s %s and gradient %s %s" % (tuple(x.shape), x.dtype, tuple(t.shape), t.dtype))
         if r.dtype != torch.float32 or r.numel() != rows or not r.is_contiguous():
             raise ValueError("rq and rk are as head_norm_forward returned them")
-        gx[i] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        gw[i] = torch.empty(w.shape, dtype=w.dtype, device=t.device) if w is not None and weight_grads else None
+        gx[i] = _like(t)
+        gw[i] = _like(w) if w is not None and weight_grads else None
         sides[i] = _side(gx[i], r, w, x=None if kept else x, gy=t, gw=gw[i], kept=x if kept else None)
     need = _head_norm_backward_bytes(device, batch, tokens, cols) if gw[0] is not None or gw[1] is not None else 0
-    ws = torch.empty(need, dtype=torch.uint8, device=g[0].device) if need else None
+    ws = _new((need,), torch.uint8, g[0].device) if need else None
     _check(ampq.lib().ampq_head_norm_backward(device, _stream_of(device), code, pcode, turn[5], q.fmt if kept else ampq.FMT_BASE, 1 if interleaved else 0, batch,
                                               tokens, cols, turn[2], turn[0], turn[1], turn[3], turn[4], turn[6], *sides, _ptr(ws), need),
            "ampq_head_norm_backward")
@@ -294,8 +307,8 @@ def distill_forward(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.
     entry) with the teacher's logits ``teacher`` [..., k], whose probabilities are those of softmax(teacher / T) over the
     row's entries.  Returns (loss [...] in fp32, times T^2; stats [..., 2] for the backward pass)."""
     s, i, t, device, codes = _lists(logits, indices, teacher)
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=s.device)
-    stats = torch.empty(*logits.shape[:-1], 2, dtype=torch.float32, device=s.device)
+    leading = logits.shape[:-1]
+    loss, stats = _new(leading, torch.float32, s.device), _new((*leading, 2), torch.float32, s.device)
     _check(ampq.lib().ampq_distill_forward(device, _stream_of(device), *codes, *_list_args(s, i, t), temperature, loss.data_ptr(), stats.data_ptr()),
            "ampq_distill_forward")
     return loss, stats
@@ -316,7 +329,7 @@ def distill_backward(gl: torch.Tensor, logits: torch.Tensor, indices: torch.Tens
         gl = gl if gl.is_contiguous() else gl.contiguous()
         stride = 1
     stats = stats if stats.is_contiguous() else stats.contiguous()
-    gs = torch.empty(logits.shape, dtype=s.dtype, device=s.device)
+    gs = _like(logits)
     _check(ampq.lib().ampq_distill_backward(device, _stream_of(device), *codes, gl.data_ptr(), stride, *_list_args(s, i, t), stats.data_ptr(), temperature,
                                             gs.data_ptr(), s.shape[1]), "ampq_distill_backward")
     return gs
