@@ -6,12 +6,12 @@
 // backward, with t the gradient turned back, h = x r and u = t w:
 //   gx = r (u - h mean_c(u h)), gw = sum over tokens and heads of t h
 //
-// Layout.  A thread holds the two vectors of V columns that are turned into one
-// another, so a rotation needs no exchange between threads: columns j V and
-// rot / 2 + j V, or 2 V neighbouring columns where the pairs are neighbours.  The
-// columns that are not turned are halved in the same way (cos 1, sin 0).  A head
-// takes the smallest power of two of lanes that holds it, a warp several heads at
-// once; the sum over a head's columns is a few shuffles.
+// Layout.  A thread holds two vectors of V columns that need no other's for the
+// rotation: columns j V and rot / 2 + j V, which are turned into one another, and
+// behind them the two halves of the columns that are not turned; where pairs are
+// neighbours, j V and cols / 2 + j V.  Either way neighbouring lanes have neighbouring
+// vectors.  A head takes the smallest power of two of lanes that holds it, a warp
+// several heads at once; the sum over a head's columns is a few shuffles.
 #include "ampq_decoder.h"
 
 #include <cmath>
@@ -191,17 +191,23 @@ __device__ __forceinline__ void store_code_vec(unsigned char* p, bool e4m3, unsi
     if constexpr (V == 1) *p = (unsigned char)(c[0] & keep);
 }
 
-// Columns of a thread's j-th two vectors, and the first of their V angles (-1: not turned).
+// Columns of a thread's j-th two vectors, and the first angle of each (-1: not turned):
+// V of them, the same ones for both, or V / 2 for each where pairs are neighbours.
 struct Columns {
-    int col[2], angle;
+    int col[2], angle[2];
 };
 template <int V, bool NEXT>
 __device__ __forceinline__ Columns columns_of(int cols, int half, int j) {
+    if (NEXT && V > 1) {
+        const int a = V * j, b = cols / 2 + V * j;
+        return Columns{{a, b}, {a < 2 * half ? a / 2 : -1, b < 2 * half ? b / 2 : -1}};
+    }
     const int turned = half / V;  // pairs of vectors that are turned
-    if (NEXT) return Columns{{2 * V * j, 2 * V * j + V}, j < turned ? V * j : -1};
-    if (j < turned) return Columns{{V * j, half + V * j}, V * j};
+    const int angle = j < turned ? V * j : -1;
+    if (NEXT) return Columns{{2 * j, 2 * j + 1}, {angle, angle}};
+    if (j < turned) return Columns{{V * j, half + V * j}, {angle, angle}};
     const int rest = (cols - 2 * half) / 2, at = 2 * half + V * (j - turned);
-    return Columns{{at, at + rest}, -1};
+    return Columns{{at, at + rest}, {-1, -1}};
 }
 
 // The elements that those of vector m are turned with, where the pairs are neighbours
@@ -212,45 +218,67 @@ __device__ __forceinline__ float2 partner(const float2 (&v)[2][kPairs<V>], int m
     return v[1 - m][i];
 }
 
-// Cosines and sines of a token for a thread's V angles, as factors of its elements:
-// turned value = own * c + partner * s.  `back` turns the other way.  A position
-// outside the table has NaN.
+// sum + partner * factor.  Neighbours are multiplied one by one: as a pair they would
+// have to change places first.
 template <int V, bool NEXT>
-__device__ __forceinline__ void load_angles(const HeadArgs& p, int half, long long position, int angle, bool back, float2 (&c)[2][kPairs<V>], float2 (&s)[2][kPairs<V>]) {
-    float cv[V], sv[V];
+__device__ __forceinline__ float2 turn_with(const float2 (&v)[2][kPairs<V>], int m, int i, float2 factor, float2 sum) {
+    if (NEXT && V > 1) return make_float2(fmaf(v[m][i].y, factor.x, sum.x), fmaf(v[m][i].x, factor.y, sum.y));
+    return __ffma2_rn(v[1 - m][i], factor, sum);
+}
+
+// N values of a table, the first one at a multiple of N of a row whose length is one too.
+template <int N>
+__device__ __forceinline__ void load_row(const float* p, bool known, float (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) cv[i] = sv[i] = NAN;
-    if (position >= 0 && position < p.angles) {
-        const float *cp = p.cos + position * half + angle, *sp = p.sin + position * half + angle;
-        if (V >= 4 && (half & 3) == 0) {  // rows of the table on 16-byte boundaries (its base is)
+    for (int i = 0; i < N; ++i) v[i] = NAN;
+    if (!known) return;
+    if constexpr (N % 4 == 0) {
 #pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                const float4 f = __ldg(reinterpret_cast<const float4*>(cp + i)), g = __ldg(reinterpret_cast<const float4*>(sp + i));
-                cv[i] = f.x; cv[(i + 1) % V] = f.y; cv[(i + 2) % V] = f.z; cv[(i + 3) % V] = f.w;
-                sv[i] = g.x; sv[(i + 1) % V] = g.y; sv[(i + 2) % V] = g.z; sv[(i + 3) % V] = g.w;
-            }
-        } else {
+        for (int i = 0; i < N; i += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(p + i));
+            v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+        }
+    } else if constexpr (N == 2) {
+        const float2 f = __ldg(reinterpret_cast<const float2*>(p));
+        v[0] = f.x; v[1] = f.y;
+    } else {
+        v[0] = __ldg(p);
+    }
+}
+
+// Cosines and sines of a token for a thread's columns, as factors of its elements:
+// turned value = own * c + partner * s, where the columns are turned.  `back` turns the
+// other way.  A position outside the table has NaN.
+template <int V, bool NEXT>
+__device__ __forceinline__ void load_angles(const HeadArgs& p, int half, long long position, const int (&angle)[2], bool back, float2 (&c)[2][kPairs<V>],
+                                            float2 (&s)[2][kPairs<V>]) {
+    const bool known = position >= 0 && position < p.angles;
+    if constexpr (NEXT && V > 1) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                cv[i] = __ldg(cp + i);
-                sv[i] = __ldg(sp + i);
+        for (int m = 0; m < 2; ++m) {
+            if (angle[m] < 0) continue;
+            float cv[V / 2], sv[V / 2];
+            load_row<V / 2>(p.cos + position * half + angle[m], known, cv);
+            load_row<V / 2>(p.sin + position * half + angle[m], known, sv);
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                c[m][i] = make_float2(cv[i], cv[i]);
+                s[m][i] = back ? make_float2(sv[i], -sv[i]) : make_float2(-sv[i], sv[i]);
             }
         }
-    }
+    } else if (angle[0] >= 0) {
+        float cv[V], sv[V];
+        load_row<V>(p.cos + position * half + angle[0], known, cv);
+        load_row<V>(p.sin + position * half + angle[0], known, sv);
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int i = 0; i < kPairs<V>; ++i) {
-            if (NEXT && V > 1) {
-                const float x = cv[(m * V / 2 + i) % V], y = sv[(m * V / 2 + i) % V];
-                c[m][i] = make_float2(x, x);
-                s[m][i] = back ? make_float2(y, -y) : make_float2(-y, y);
-            } else {
+            for (int i = 0; i < kPairs<V>; ++i) {
                 const float2 y = make_float2(sv[2 * i], sv[(2 * i + 1) % V]);
                 c[m][i] = make_float2(cv[2 * i], cv[(2 * i + 1) % V]);
                 s[m][i] = (m == 0) != back ? make_float2(-y.x, -y.y) : y;
             }
-        }
+    }
 }
 
 // The weights of both sides in shared memory, in fp32.
@@ -303,7 +331,7 @@ __device__ __forceinline__ float inverse_root(float v) {
 
 // A warp's share: one run of heads (of the queries or of the keys) of every
 // `stride`-th token, so that what goes with the columns is set up once.  The grid's
-// first CTAs have queries, the others keys, by how many steps there are of each.  It
+// first CTAs have queries, the others keys, by how much work there is of each.  It
 // walks over its rows, whose batch and token are kept up to date.
 struct Share {
     int side, head0, steps;  // head0: the first head of this lane
@@ -368,14 +396,15 @@ __global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_k
     const Side& q = a.side[mine.side];
     const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
-    bool ok[NV], turned[NV];
+    bool ok[NV], turned[NV][2];
     constexpr int R = ASYNC ? 1 : U;
     Raw<T, V> raw[R][NV][2];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         col[i] = columns_of<V, NEXT>(cols, half, sub + lanes * i);
         ok[i] = COLS > 0 || sub + lanes * i < a.vectors;
-        turned[i] = COLS > 0 || col[i].angle >= 0;
+        turned[i][0] = COLS > 0 || col[i].angle[0] >= 0;
+        turned[i][1] = COLS > 0 || col[i].angle[1] >= 0;
 #pragma unroll
         for (int u = 0; u < R; ++u) {  // lanes without a vector keep zeros; those of no head have anything
             raw[u][i][0].zero();
@@ -435,21 +464,14 @@ __global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_k
             float2 w[2][P];
             take_weights<V>(s_w[mine.side] + col[i].col[0], w[0]);
             take_weights<V>(s_w[mine.side] + col[i].col[1], w[1]);
-            if (turned[i]) {
-                load_angles<V, NEXT>(a, half, here, col[i].angle, false, f[i], g[i]);
+            load_angles<V, NEXT>(a, half, here, col[i].angle, false, f[i], g[i]);
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int k = 0; k < P; ++k) {
-                        f[i][m][k] = __fmul2_rn(f[i][m][k], w[m][k]);
-                        g[i][m][k] = __fmul2_rn(g[i][m][k], partner<V, NEXT>(w, m, k));
-                    }
-            } else {
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int k = 0; k < P; ++k) f[i][m][k] = w[m][k];
-            }
+                for (int k = 0; k < P; ++k) {
+                    f[i][m][k] = turned[i][m] ? __fmul2_rn(f[i][m][k], w[m][k]) : w[m][k];
+                    g[i][m][k] = __fmul2_rn(g[i][m][k], partner<V, NEXT>(w, m, k));
+                }
         }
         for (int step = 0, head = mine.head0; step < steps; step += U, head += U * per) {
             // the next steps' elements, or the next token's: into the other place, or behind these in the registers
@@ -513,13 +535,11 @@ __global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_k
                     for (int u = 0; u < U; ++u)
 #pragma unroll
                         for (int i = 0; i < NV; ++i) {
-                            if (NEXT) top[u][i][0] = max(top[u][i][0], top[u][i][1]);
 #pragma unroll
-                            for (int o = (NEXT ? kGroup / 2 : kGroup) / V / 2; o > 0; o >>= 1) {
+                            for (int o = kGroup / V / 2; o > 0; o >>= 1) {
                                 top[u][i][0] = max(top[u][i][0], __shfl_xor_sync(0xFFFFFFFFu, top[u][i][0], o));
-                                if (!NEXT) top[u][i][1] = max(top[u][i][1], __shfl_xor_sync(0xFFFFFFFFu, top[u][i][1], o));
+                                top[u][i][1] = max(top[u][i][1], __shfl_xor_sync(0xFFFFFFFFu, top[u][i][1], o));
                             }
-                            if (NEXT) top[u][i][1] = top[u][i][0];
                         }
                 } else {
 #pragma unroll
@@ -574,7 +594,7 @@ __global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_k
 #pragma unroll
                             for (int k = 0; k < P; ++k) {
                                 y[k] = __fmul2_rn(x[u][i][m][k], f[i][m][k]);
-                                if (turned[i]) y[k] = __ffma2_rn(partner<V, NEXT>(x[u][i], m, k), g[i][m][k], y[k]);
+                                if (turned[i][m]) y[k] = turn_with<V, NEXT>(x[u][i], m, k, g[i][m][k], y[k]);
                                 y[k] = __fmul2_rn(y[k], make_float2(rstd[u], rstd[u]));
                             }
                             store_vec<T, V>(out + col[i].col[m], y);
@@ -611,13 +631,14 @@ __global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward
     const Side& q = a.side[mine.side];
     const int heads = q.heads, steps = mine.steps;
     Columns col[NV];
-    bool ok[NV], turned[NV];
+    bool ok[NV], turned[NV][2];
     float2 gw[NV][2][P], w[NV][2][P];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         col[i] = columns_of<V, NEXT>(cols, half, sub + lanes * i);
         ok[i] = COLS > 0 || sub + lanes * i < a.vectors;
-        turned[i] = COLS > 0 || col[i].angle >= 0;
+        turned[i][0] = COLS > 0 || col[i].angle[0] >= 0;
+        turned[i][1] = COLS > 0 || col[i].angle[1] >= 0;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             if (ok[i]) take_weights<V>(s_w[mine.side] + col[i].col[m], w[i][m]);
@@ -718,7 +739,7 @@ __global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward
             float2 c[NV][2][P], s[NV][2][P];
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (ok[i] && turned[i]) load_angles<V, NEXT>(a, half, here, col[i].angle, true, c[i], s[i]);
+                if (ok[i]) load_angles<V, NEXT>(a, half, here, col[i].angle, true, c[i], s[i]);
             for (int step = 0, head = mine.head0; step < steps; step += U, head += U * per) {
                 bool live[U];
                 float rstd[U], dot[U];
@@ -780,7 +801,7 @@ __global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward
 #pragma unroll
                                 for (int k = 0; k < P; ++k) {
                                     t[m][k] = g[u][i][m][k];
-                                    if (turned[i]) t[m][k] = __ffma2_rn(partner<V, NEXT>(g[u][i], m, k), s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
+                                    if (turned[i][m]) t[m][k] = turn_with<V, NEXT>(g[u][i], m, k, s[i][m][k], __fmul2_rn(t[m][k], c[i][m][k]));
                                     gw[i][m][k] = __ffma2_rn(t[m][k], h[u][i][m][k], gw[i][m][k]);
                                     t[m][k] = __fmul2_rn(t[m][k], w[i][m][k]);
                                     sum = __ffma2_rn(t[m][k], h[u][i][m][k], sum);
@@ -967,7 +988,7 @@ long long lay_out(HeadArgs& a, int V, int NV, bool next, bool backward, int warp
     a.vectors = a.cols / 2 / V;
     a.lanes = 1;
     while (a.lanes * NV < a.vectors) a.lanes *= 2;
-    a.lane_groups = (next ? a.cols % kGroup == 0 : a.half % kGroup == 0 && (a.cols / 2 - a.half) % kGroup == 0) && (next ? kGroup / 2 : kGroup) / V <= a.lanes;
+    a.lane_groups = V > 1 && kGroup / V <= a.lanes && a.cols / 2 % kGroup == 0 && (next || a.half % kGroup == 0);
     const int per = 32 / a.lanes;
     const int steps[2] = {(a.side[0].heads + per - 1) / per, (a.side[1].heads + per - 1) / per};
     const long long most = ctas * warps;
