@@ -175,9 +175,10 @@ __device__ __forceinline__ unsigned cluster_rank() {
 
 // A row to a CTA, or to a cluster of `parts` CTAs where there are few rows; the parts'
 // maxima and sums meet in the first CTA's shared memory.  Bound by HBM, with the
-// exponentials' pipe close behind (4096 x 128000 bf16 170 us, 5.9 TB/s; its exponentials
-// alone 120 us): the more warps the better, so one vector in flight a thread and eight
-// CTAs an SM (three vectors and four CTAs 184 us).
+// exponentials' pipe close behind (4096 x 128000 bf16 170 to 182 us by board, 5.5 to 5.9
+// TB/s; its exponentials alone 120 us): the more warps the better, so one vector in
+// flight a thread and eight CTAs an SM (three vectors and four CTAs 184 us, where these
+// took 170).
 template <typename T>
 __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
 }
 
 // gs_j = gl T (q_j - sum of the p of the entries of column j); bound by HBM (4096 x
-// 128000 bf16 322 us, 6.4 TB/s).  A CTA writes its part
+// 128000 bf16 322 to 331 us by board, 6.2 to 6.4 TB/s).  A CTA writes its part
 // of a row by the formula's first term, and then once more the columns of the list
 // that lie in it, by the whole formula: a barrier is between the two.  A column that
 // is listed more than once is stored by its first entry, with the sum of all.  Few

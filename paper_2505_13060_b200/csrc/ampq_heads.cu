@@ -24,9 +24,10 @@ constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
 // The shuffles, the root and the loads of a step are a chain of latencies: two steps
 // side by side fill it better than more warps would, and a spilled register costs more
 // than either brings.  Measured on 2 x 4096 tokens of 64 + 8 heads of 128 columns (one
-// step at a time with more warps, then two together): forward bf16 with a checkpoint
-// 79 and 75 us, without 62 and 58 us, fp32 118 and 111 us; backward fp32 126 and 118
-// us, but bf16 from 8 bits, whose sums and factors leave no room, 87 and 95 us.
+// step at a time, the same with six CTAs an SM, two together): forward bf16 with a
+// checkpoint 74, 80 and 68 us, without 59, 58 and 53 us, fp32 125, 129 and 111 us.
+// Backward (one step, two): fp32 124 and 115 us, but bf16, whose sums and factors
+// leave no room, from 8 bits 78 and 119 us, from the input 80 and 110 us.
 constexpr int kForwardThreads = 128, kBackwardThreads = 128, kMostCtas = 4, kForwardTogether = 2;
 template <int V>
 constexpr int kCtas = V >= 4 ? kMostCtas : 3;  // small vectors come through registers
@@ -372,8 +373,8 @@ struct Share {
 // ---------------------------------------------------------------------------
 
 // Bound by HBM and, with a checkpoint, by the warps' latencies: 2 x 4096 tokens of
-// 64 + 8 heads of 128 columns, bf16, take 54 us (5.7 TB/s) and 69 us with the
-// checkpoint (5.6 TB/s), fp32 112 us (6.2 TB/s).
+// 64 + 8 heads of 128 columns, bf16, take 53 us (5.8 TB/s) and 68 us with the
+// checkpoint (5.7 TB/s), fp32 111 us (6.2 TB/s).
 // COLS: heads of so many columns, all of them turned, or 0 for any.  What depends on
 // the columns alone is then known to the compiler (a third of the instructions).
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
@@ -608,9 +609,9 @@ __global__ void __launch_bounds__(kForwardThreads, kCtas<V>) head_norm_forward_k
 }
 
 // A warp's sums for the weight's gradient stay in registers over its tokens;
-// part[CTA][column] of a side's CTAs are joined afterwards.  The same size: bf16 81 us
-// from 8 bits (4.7 TB/s), 83 us from the input (5.6 TB/s), fp32 118 us from 8 bits;
-// 16 warps an SM and instructions bound the first (77 us of it, 4 the joining).
+// part[CTA][column] of a side's CTAs are joined afterwards.  The same size: bf16 79 us
+// from 8 bits (4.9 TB/s), 80 us from the input (5.7 TB/s), fp32 115 us from 8 bits;
+// 16 warps an SM and instructions bound the first.
 template <typename T, int V, int NV, bool NEXT, int FMT, int COLS>
 __global__ void __launch_bounds__(kBackwardThreads, kCtas<V>) head_norm_backward_kernel(const HeadArgs a) {
     constexpr int kThreads = kBackwardThreads, kWarps = kThreads / 32;
@@ -1016,7 +1017,7 @@ long long lay_out(HeadArgs& a, int V, int NV, bool next, bool backward, int warp
     }
     // The CTAs go to the sides by their work, one warp to a run at least.  What a run does
     // once for a token is about two steps' work, and steps are done `together`.  (Shared out
-    // by steps alone the keys' CTAs of 64 + 8 heads came last: 77 us instead of 69.)
+    // by steps alone the keys' CTAs of 64 + 8 heads came last: 76 us instead of 68.)
     const long long least[2] = {(a.runs[0] + warps - 1) / warps, (a.runs[1] + warps - 1) / warps};
     long long work[2];
     for (int s = 0; s < 2; ++s) work[s] = (long long)a.runs[s] * (kTokenWork + (a.run[s] + together - 1) / together * together);
