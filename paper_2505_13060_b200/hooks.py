@@ -277,6 +277,18 @@ class Calibrator:
         return res
 
     # -- running the model in a low-precision configuration --------------------
+    def _rounded(self, x, fmt: int, amax: float = -1.0):
+        """x rounded to format ``fmt``, in the order of torch's current stream: the context's waits for what made x, and
+        torch's for the result, so neither tensor has to be held."""
+        x = x.detach().contiguous()
+        out = torch.empty_like(x)
+        if not self._same_stream():
+            torch.cuda.ExternalStream(self.ctx.stream).wait_stream(torch.cuda.current_stream())
+        self.ctx.fake_quant(ampq.torch_dtype_code(x), fmt, x.data_ptr(), x.numel(), amax, out.data_ptr())
+        if not self._same_stream():
+            torch.cuda.current_stream().wait_stream(torch.cuda.ExternalStream(self.ctx.stream))
+        return out
+
     @contextlib.contextmanager
     def quantised(self, fmt_of_layer, amax_x=None):
         """Inside this block layer i (index into ``modules``) runs with its input and
@@ -291,27 +303,16 @@ class Calibrator:
             if isinstance(m, BatchedMatmul):   # both inputs rounded, each with its own measured amax
 
                 def pre2(module, inputs, fmt=fmt):
-                    outs = []
-                    for x in inputs:
-                        x = x.contiguous()
-                        out = torch.empty_like(x)
-                        self.ctx.fake_quant(ampq.torch_dtype_code(x), fmt, x.data_ptr(), x.numel(), -1.0, out.data_ptr())
-                        self._keep.append(x)
-                        outs.append(out)
-                    return tuple(outs)
+                    return tuple(self._rounded(x, fmt) for x in inputs)
 
                 handles.append(m.register_forward_pre_hook(pre2))
                 continue
             w = m.weight.data
             saved.append((m, w.clone()))
-            self.ctx.fake_quant(ampq.torch_dtype_code(w), fmt, w.data_ptr(), w.numel(), -1.0, w.data_ptr())
+            w.copy_(self._rounded(w, fmt))
 
             def pre(module, inputs, fmt=fmt, a=(-1.0 if amax_x is None else float(amax_x[idx]))):
-                x = inputs[0].contiguous()
-                out = torch.empty_like(x)
-                self.ctx.fake_quant(ampq.torch_dtype_code(x), fmt, x.data_ptr(), x.numel(), a, out.data_ptr())
-                self._keep.append(x)
-                return (out,) + tuple(inputs[1:])
+                return (self._rounded(inputs[0], fmt, a),) + tuple(inputs[1:])
 
             handles.append(m.register_forward_pre_hook(pre))
         try:
@@ -322,9 +323,6 @@ class Calibrator:
                 h.remove()
             for m, w in saved:
                 m.weight.data.copy_(w)
-            if not self._same_stream():
-                torch.cuda.ExternalStream(self.ctx.stream).synchronize()
-            self._keep = []
 
     def divergence(self, forward, fmt_of_layer, top: int = 64, temperature: float = 1.0, amax_x=None):
         """How far a low-precision configuration's outputs are from the model's own: ``forward()`` runs the model and
