@@ -95,6 +95,18 @@ class _ScoredLinear(torch.autograd.Function):
         return gx if need_x else None, gw[0] if need_w else None, gb[0] if need_b else None, None, None
 
 
+class _RoundedWeight(torch.autograd.Function):
+    """A weight as a low-precision format holds it; its gradient is the weight's."""
+
+    @staticmethod
+    def forward(ctx, weight, calibrator, fmt):
+        return calibrator._rounded(weight, fmt)
+
+    @staticmethod
+    def backward(ctx, g):
+        return g, None, None
+
+
 class Calibrator:
     def __init__(self, ctx: "ampq.Context", model: torch.nn.Module, R: int, checkpoint: int = ampq.FMT_BASE):
         if checkpoint not in (ampq.FMT_BASE, ampq.FMT_E4M3, ampq.FMT_E5M2):
@@ -294,35 +306,41 @@ class Calibrator:
         """Inside this block layer i (index into ``modules``) runs with its input and
         weight rounded to format ``fmt_of_layer[i]`` (0 leaves it alone).
         ``amax_x[i]`` is the static amax of the layer's input (measured per call if
-        absent); the weight's amax is always measured."""
+        absent); the weight's amax is always measured.  A layer's rounded weight is
+        its own: what else reads the same weight (a tied embedding, another layer)
+        has it as it was."""
+        fmts = [fmt_of_layer[i] for i in range(len(self.modules))]
         saved, handles = [], []
-        for idx, (_, m) in enumerate(self.modules):
-            fmt = fmt_of_layer[idx]
-            if not fmt:
-                continue
-            if isinstance(m, BatchedMatmul):   # both inputs rounded, each with its own measured amax
-
-                def pre2(module, inputs, fmt=fmt):
-                    return tuple(self._rounded(x, fmt) for x in inputs)
-
-                handles.append(m.register_forward_pre_hook(pre2))
-                continue
-            w = m.weight.data
-            saved.append((m, w.clone()))
-            w.copy_(self._rounded(w, fmt))
-
-            def pre(module, inputs, fmt=fmt, a=(-1.0 if amax_x is None else float(amax_x[idx]))):
-                return (self._rounded(inputs[0], fmt, a),) + tuple(inputs[1:])
-
-            handles.append(m.register_forward_pre_hook(pre))
         try:
+            for idx, ((name, m), fmt) in enumerate(zip(self.modules, fmts)):
+                if not fmt:
+                    continue
+                if isinstance(m, BatchedMatmul):   # both inputs rounded, each with its own measured amax
+
+                    def pre2(module, inputs, fmt=fmt):
+                        return tuple(self._rounded(x, fmt) for x in inputs)
+
+                    handles.append(m.register_forward_pre_hook(pre2))
+                    continue
+                a = -1.0 if amax_x is None else float(amax_x[idx])
+                place = next((d for d in (m._parameters, m._buffers) if isinstance(d.get("weight"), torch.Tensor)), None)
+                if place is None:   # a norm of it, or a mask: what is put in its place would be computed anew
+                    raise ValueError("layer %s computes its weight at each call: it cannot be replaced by a rounded one" % name)
+                weight = place["weight"]
+                saved.append((place, weight))
+                place["weight"] = _RoundedWeight.apply(weight, self, fmt)
+
+                def pre(module, inputs, fmt=fmt, a=a):
+                    return (self._rounded(inputs[0], fmt, a),) + tuple(inputs[1:])
+
+                handles.append(m.register_forward_pre_hook(pre))
             yield
         finally:
-            torch.cuda.current_stream().synchronize()
             for h in handles:
                 h.remove()
-            for m, w in saved:
-                m.weight.data.copy_(w)
+            for place, weight in saved:
+                place["weight"] = weight
+            torch.cuda.current_stream().synchronize()
 
     def divergence(self, forward, fmt_of_layer, top: int = 64, temperature: float = 1.0, amax_x=None):
         """How far a low-precision configuration's outputs are from the model's own: ``forward()`` runs the model and

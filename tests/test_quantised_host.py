@@ -5,6 +5,7 @@ import ctypes as C
 import numpy as np
 import pytest
 import torch
+import torch.nn.utils.prune
 
 
 class Stream:
@@ -75,3 +76,72 @@ def test_rounding_is_ordered_between_two_streams(setup):
             assert log == once
             cal.model(x)
             assert log == 4 * once
+
+
+def test_shared_weights_are_rounded_for_their_layer_alone(setup):
+    """An embedding that is tied to the head is looked up as it was, layers that share a weight have it in their own formats,
+    and afterwards everything is as before."""
+    make, _ = setup
+    lookup, head, other, alone = torch.nn.Embedding(5, 4), torch.nn.Linear(4, 5, bias=False), torch.nn.Linear(4, 5, bias=False), torch.nn.Linear(4, 4)
+    head.weight = other.weight = lookup.weight
+    before = lookup.weight.detach().clone()
+    net = torch.nn.ModuleList([lookup, head, other, alone])
+    cal = make(net)
+    with cal.quantised([1, 3, 0]):
+        assert torch.equal(lookup(torch.arange(5)), before)
+        assert torch.equal(head(torch.eye(4)), rounded(before, 1).t()) and torch.equal(other(torch.eye(4)), rounded(before, 3).t())
+        assert not torch.equal(rounded(before, 1), rounded(before, 3))
+    assert head.weight is other.weight is lookup.weight and isinstance(head.weight, torch.nn.Parameter) and torch.equal(lookup.weight, before)
+    assert len(list(net.parameters())) == 3
+
+
+def test_an_exception_leaves_the_model_as_it_was(setup):
+    make, _ = setup
+    net = torch.nn.Sequential(*(torch.nn.Linear(4, 4) for _ in range(3)))
+    before, x = [p.detach().clone() for p in net.parameters()], torch.randn(2, 4)
+    cal = make(net)
+
+    def same():
+        return all(torch.equal(a, b) for a, b in zip(before, net.parameters())) and not any(m._forward_pre_hooks for m in net)
+
+    for formats, amax in (([1, 2], None), ([1, 2, -1], None), ([1, 2, 3], [1.0]), ([1, 2, 3], [1.0, 2.0, None])):
+        with pytest.raises((ValueError, IndexError, TypeError)):
+            with cal.quantised(formats, amax):
+                pass
+        assert same()
+    with cal.quantised([1, 0, 3], [1.0, None, -1.0]), torch.no_grad():   # what is not rounded has no amax
+        net(x)
+    assert same()
+    net[2].double()
+    with pytest.raises((ValueError, KeyError, TypeError)):   # a weight of a type that is not rounded
+        with cal.quantised([1, 2, 3]):
+            pass
+    net[2].float()
+    assert same()
+    with pytest.raises(KeyError):
+        with cal.quantised([1, 2, 3]):
+            net(x)
+            raise KeyError
+    assert same()
+
+
+def test_weights_that_are_no_parameters(setup):
+    """A buffer, a view of a wider tensor, a gradient through a rounded weight, and a weight that the module computes."""
+    make, _ = setup
+    wide = torch.randn(4, 9)
+    copy = wide.clone()
+    a, b = torch.nn.Linear(6, 4, bias=False), torch.nn.Linear(4, 3, bias=False)
+    del a.weight
+    a.register_buffer("weight", wide[:, :6])
+    cal = make(torch.nn.Sequential(a, b))
+    x = torch.round(torch.randn(2, 6))
+    with cal.quantised([1, 2]):
+        h = a(x)
+        assert torch.equal(h, x @ rounded(copy[:, :6], 1).t())
+        b(h).sum().backward()
+    assert torch.equal(wide, copy) and a.weight.data_ptr() == wide.data_ptr()
+    assert torch.allclose(b.weight.grad, rounded(h, 2).sum(0).expand(3, 4))
+    for c in (torch.nn.utils.parametrizations.weight_norm(torch.nn.Linear(4, 4)), torch.nn.utils.prune.l1_unstructured(torch.nn.Linear(4, 4), "weight", 0.5)):
+        with pytest.raises(ValueError, match="computes its weight"):
+            with make(torch.nn.Sequential(c)).quantised([1]):
+                pass
