@@ -302,6 +302,19 @@ def _list_args(s, i, t):
     return s.data_ptr(), _pitch(s), rows, cols, i.data_ptr(), _pitch(i), t.data_ptr(), _pitch(t), i.shape[1]
 
 
+def list_length(logits: torch.Tensor, top: int) -> int:
+    """Length of a list of the ``top`` largest of logits [..., classes]; raises where ``distill_forward`` would refuse the
+    logits or the list."""
+    if logits.dim() < 1:
+        raise ValueError("logits are [..., classes], got %s" % (tuple(logits.shape),))
+    _device_of(logits)
+    _code(logits)
+    top = min(top, logits.shape[-1])
+    if top > ampq.DISTILL_MAX_TOP:
+        raise ValueError("lists hold up to %d columns, got %d" % (ampq.DISTILL_MAX_TOP, top))
+    return top
+
+
 def distill_forward(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0):
     """Divergence of softmax(logits / T) [..., vocabulary] from a teacher's: the columns ``indices`` [..., k] (negative: no
     entry) with the teacher's logits ``teacher`` [..., k], whose probabilities are those of softmax(teacher / T) over the

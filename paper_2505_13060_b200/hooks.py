@@ -347,9 +347,14 @@ class Calibrator:
         returns logits [..., classes]; it is called once as it is and once in the configuration (``quantised``).  Returns
         the divergence of the second's logits from the first's ``top`` largest (``decoder.distill_forward``), one fp32
         number for each row."""
+        if top < 0 or not 2.0 ** -20 <= temperature <= 2.0 ** 20:
+            raise ValueError("a list of %d at temperature %g" % (top, temperature))
+        for i in range(len(self.modules)):
+            fmt_of_layer[i]   # raises here, not between the passes
         with torch.no_grad():
             logits = forward()
-            teacher, indices = logits.topk(min(top, logits.shape[-1]), dim=-1)
+            top = decoder.list_length(logits, top)
+            teacher, indices = logits.topk(top, dim=-1)
             del logits
             with self.quantised(fmt_of_layer, amax_x):
                 logits = forward()

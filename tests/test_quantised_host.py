@@ -145,3 +145,33 @@ def test_weights_that_are_no_parameters(setup):
         with pytest.raises(ValueError, match="computes its weight"):
             with make(torch.nn.Sequential(c)).quantised([1]):
                 pass
+
+
+def test_divergence_refuses_before_the_second_pass(setup, monkeypatch):
+    """What it cannot do with its arguments is said before the model runs, what it cannot do with the logits before it
+    runs again; the model stays as it was."""
+    from paper_2505_13060_b200 import decoder
+
+    make, _ = setup
+    net = torch.nn.Linear(4, 5)
+    cal, calls, logits = make(net), [], [torch.zeros(2, 3000)]
+
+    def forward():
+        calls.append(1)
+        return logits[0]
+
+    for formats, more in (([], {}), ([1], dict(top=-1)), ([1], dict(temperature=0.0)), ([1], dict(temperature=2.0 ** 21)), ([1], dict(temperature=float("nan")))):
+        with pytest.raises((ValueError, IndexError)):
+            cal.divergence(forward, formats, **more)
+    assert not calls
+    with pytest.raises(ValueError, match="CUDA"):
+        cal.divergence(forward, [1])
+    monkeypatch.setattr(decoder, "_device_of", lambda t: 0)
+    for bad, top, error in ((logits[0].half(), 64, TypeError), (logits[0], 1025, ValueError), (logits[0].sum(), 64, ValueError)):
+        logits[0] = bad
+        calls.clear()
+        with pytest.raises(error):
+            cal.divergence(forward, [1], top=top)
+        assert len(calls) == 1
+    assert not net._forward_pre_hooks
+    assert decoder.list_length(torch.zeros(2, 301), 5000) == 301   # of all there are
