@@ -52,8 +52,8 @@ struct Row {
     __device__ __forceinline__ unsigned first(unsigned part, unsigned parts) const { return (unsigned)((unsigned long long)vectors * part / parts); }
 };
 
-// Sum of exp2((s - m) * k) with the largest s so far as m.
-struct Running {
+// Sum of exp2((s - m) * k) with the largest s so far as m.  Stored as one word of 8 bytes.
+struct alignas(8) Running {
     float m = -INFINITY, sum = 0.0f;
     __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }  // -inf - -inf is not 0
     __device__ __forceinline__ void raise(float to, float k) {
@@ -241,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
     if (a.parts > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // the first CTA has begun
         if (threadIdx.x == 0) {
+            static_assert(alignof(Running) == 8 && sizeof(Running) == 8, "the store below");
             unsigned at = (unsigned)__cvta_generic_to_shared(&s_parts[part]), there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(at));
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(run.m), "f"(run.sum) : "memory");
