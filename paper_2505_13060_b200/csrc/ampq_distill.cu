@@ -24,6 +24,16 @@ constexpr unsigned kPartColumns = 16 * kPartVectors;  // at most
 constexpr int kFewEntries = 128;  // 100: 333 us compared, 358 us with bits; 256: 530 and 369 us (4096 rows of 128000)
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
+// log2(e) / T in two parts.  Rounded to fp32 alone it is off by up to 2^-24 of itself,
+// which moves every exponent of a row the same way: 4096 x 128000, T = 1, 7e-8 of the
+// sums; with the rest what is left is the rounding of each exponent.  `hi` is
+// rounded down and `lo` above 0, so that -Inf times both stays -Inf.
+struct Factor {
+    float hi, lo, slack;  // slack: 16 T log 2
+    __device__ __forceinline__ float times(float d) const { return fmaf(d, hi, d * lo); }
+    __device__ __forceinline__ float2 times(float2 d) const { return __ffma2_rn(d, make_float2(hi, hi), __fmul2_rn(d, make_float2(lo, lo))); }
+};
+
 struct DistillArgs {
     const void *logits, *indices, *teacher;
     const float* gl;
@@ -32,7 +42,8 @@ struct DistillArgs {
     long long rows, ld, ld_indices, ld_teacher, ld_gs, gl_stride;
     unsigned cols;
     int top, parts;
-    float T, inv_T, k;  // k = log2(e) / T
+    float T, inv_T;
+    Factor k;
     bool wide, teacher_bf16;
 };
 
@@ -52,43 +63,65 @@ struct Row {
     __device__ __forceinline__ unsigned first(unsigned part, unsigned parts) const { return (unsigned)((unsigned long long)vectors * part / parts); }
 };
 
-// Sum of exp2((s - m) * k) with the largest s so far as m.  Stored as one word of 8 bytes.
+// Sum of exp((s - m) / T) over some of a row, and the largest s of them as m (-Inf for
+// none, or NaN alone).  Stored as one word of 8 bytes.
 struct alignas(8) Running {
-    float m = -INFINITY, sum = 0.0f;
-    __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }  // -inf - -inf is not 0
-    __device__ __forceinline__ void raise(float to, float k) {
-        if (to > m) {
-            sum *= exp2_fast((m - to) * k);
-            m = to;
+    float m, sum;
+    // The sum under a larger maximum.  expf has errors of either sign; exp2_fast is 5e-8 low
+    // on average, and in a row's sum the errors of all the times that it is put under a
+    // larger maximum add up: with exp2_fast for each of these, sums of 4096 x 128000 were 1.7e-7 low.
+    __device__ __forceinline__ float under(float to, const Factor& k) const { return m == to ? sum : sum * expf(k.times(m - to) * 0.6931472f); }
+    // Of `n` of them, in a fixed order.
+    __device__ __forceinline__ static Running join(const Running* r, int n, const Factor& k) {
+        Running all{r[0].m, 0.0f};
+        for (int i = 1; i < n; ++i) all.m = fmaxf(all.m, r[i].m);
+        for (int i = 0; i < n; ++i) all.sum += r[i].under(all.m, k);
+        return all;
+    }
+    __device__ __forceinline__ void join_warp(const Factor& k) {
+        float to = m;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, o));
+        sum = under(to, k);
+        m = to;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    }
+};
+
+// A thread's sum of exp((s - base) / T).  The base is a logit that need not be the
+// largest: it is raised to one that is 16 T log 2 above it, so that terms stay below 2^16
+// and few sums are ever put under another.
+struct Terms {
+    float base = 0.0f, limit = -INFINITY, top = -INFINITY, sum = 0.0f;
+    __device__ __forceinline__ void raise(float to, const Factor& k) {
+        top = fmaxf(top, to);
+        if (to > limit) {
+            sum = limit == -INFINITY ? sum * 0.0f : Running{base, sum}.under(to, k);  // nothing, or NaN
+            base = to;
+            limit = to + k.slack;
         }
     }
-    __device__ __forceinline__ void add(float s, float k) {
+    __device__ __forceinline__ void add(float s, const Factor& k) {
         raise(s, k);
-        sum += exp2_fast((s - base()) * k);
+        sum += exp2_fast(k.times(s - base));
     }
     template <int N>
-    __device__ __forceinline__ void add(const float2 (&v)[N], float k) {
-        float top = v[0].x;
+    __device__ __forceinline__ void add(const float2 (&v)[N], const Factor& k) {
+        float most = v[0].x;
 #pragma unroll
-        for (int i = 0; i < N; ++i) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[i].x), "f"(v[i].y));
-        raise(top, k);
-        const float b = base();
+        for (int i = 0; i < N; ++i) asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(v[i].x), "f"(v[i].y));
+        raise(most, k);
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float2 d = __fmul2_rn(__fadd2_rn(v[i], make_float2(-b, -b)), make_float2(k, k));
+            const float2 d = k.times(__fadd2_rn(v[i], make_float2(-base, -base)));
             s = __fadd2_rn(s, make_float2(exp2_fast(d.x), exp2_fast(d.y)));
         }
         sum += s.x + s.y;
     }
-    __device__ __forceinline__ void merge(const Running& o, float k) {
-        const float to = fmaxf(m, o.m);
-        if (to == -INFINITY) {  // nothing yet, or NaN alone
-            sum += o.sum;
-            return;
-        }
-        sum = sum * exp2_fast((m == to ? 0.0f : m - to) * k) + o.sum * exp2_fast((o.m == to ? 0.0f : o.m - to) * k);
-        m = to;
+    __device__ __forceinline__ Running under_top(const Factor& k) const {
+        return Running{top, limit == -INFINITY ? sum : Running{base, sum}.under(top, k)};
     }
 };
 
@@ -213,8 +246,8 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
         return;
     }
     if (part == 0) list.gather(a, x, [](unsigned) { return true; });
-    Running run;
-    if (part == 0 && threadIdx.x < r.head + r.tail) run.add(load_elem(x + r.edge(threadIdx.x)), a.k);
+    Terms terms;
+    if (part == 0 && threadIdx.x < r.head + r.tail) terms.add(load_elem(x + r.edge(threadIdx.x)), a.k);
     for (; v < end; v += kForwardAhead * kThreads) {
 #pragma unroll
         for (int u = 0; u < kForwardAhead; ++u)
@@ -223,21 +256,14 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
                 k.from_words(w[u]);
                 const unsigned next = v + (kForwardAhead + u) * kThreads;
                 if (next < end) load_vector(body + (size_t)next * K::kElems, w[u]);
-                run.add(k.v, a.k);
+                terms.add(k.v, a.k);
             }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Running other;
-        other.m = __shfl_xor_sync(0xFFFFFFFFu, run.m, o);
-        other.sum = __shfl_xor_sync(0xFFFFFFFFu, run.sum, o);
-        run.merge(other, a.k);
-    }
+    Running run = terms.under_top(a.k);
+    run.join_warp(a.k);
     if (threadIdx.x % 32 == 0) s_warps[threadIdx.x / 32] = run;
     __syncthreads();
-    run = s_warps[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) run.merge(s_warps[w], a.k);
+    run = Running::join(s_warps, kWarps, a.k);
     if (a.parts > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // the first CTA has begun
         if (threadIdx.x == 0) {
@@ -249,8 +275,7 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         if (part != 0) return;
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        run = s_parts[0];
-        for (int p = 1; p < a.parts; ++p) run.merge(s_parts[p], a.k);
+        run = Running::join(s_parts, a.parts, a.k);
     }
     const float tmax = list.largest(a, s_top);
     float sums[2] = {0.0f, 0.0f};
@@ -325,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kern
     const float c = a.gl[row * a.gl_stride] * a.T, ci = c * inv;
     if (part == 0 && threadIdx.x < r.head + r.tail) {
         const unsigned j = r.edge(threadIdx.x);
-        store_elem(out + j, exp2_fast((load_elem(x + j) - m) * a.k) * ci);
+        store_elem(out + j, exp2_fast(a.k.times(load_elem(x + j) - m)) * ci);
     }
     for (; v < end; v += kBackwardAhead * kThreads) {
 #pragma unroll
@@ -337,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kern
                 if (next < end) load_vector(body + (size_t)next * K::kElems, w[u]);
 #pragma unroll
                 for (int i = 0; i < K::kElems / 2; ++i) {
-                    const float2 d = __fmul2_rn(__fadd2_rn(k.v[i], make_float2(-m, -m)), make_float2(a.k, a.k));
+                    const float2 d = a.k.times(__fadd2_rn(k.v[i], make_float2(-m, -m)));
                     k.v[i] = __fmul2_rn(make_float2(exp2_fast(d.x), exp2_fast(d.y)), make_float2(ci, ci));
                 }
                 write(v + u * kThreads, k);
@@ -378,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kern
                     later |= i < k;
                 }
         }
-        if (!later) store_elem(out + j, (exp2_fast((list.s[k] - m) * a.k) * inv - e * inv_sum) * c);
+        if (!later) store_elem(out + j, (exp2_fast(a.k.times(list.s[k] - m)) * inv - e * inv_sum) * c);
     }
 }
 
@@ -405,7 +430,11 @@ DistillArgs distill_args(int teacher_dtype, int index_type, const void* logits, 
     a.parts = 1;
     a.T = temperature;
     a.inv_T = 1.0f / temperature;
-    a.k = (float)(1.4426950408889634 / (double)temperature);
+    const double k = 1.4426950408889634 / (double)temperature;
+    a.k.hi = (float)k;
+    if ((double)a.k.hi >= k) a.k.hi = std::nextafterf(a.k.hi, 0.0f);
+    a.k.lo = (float)(k - (double)a.k.hi);
+    a.k.slack = (float)(16.0 * 0.6931471805599453 * (double)temperature);
     a.wide = index_type == AMPQ_I64;
     a.teacher_bf16 = teacher_dtype == AMPQ_BF16;
     return a;
