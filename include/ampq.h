@@ -577,7 +577,10 @@ int ampq_head_norm_backward(int device, void *cuda_stream, int dtype, int param_
  * A row without entries has loss 0 and stats 0,
  * whatever its logits are.  A column may be listed more
  * than once; an index of cols or more makes the loss NaN.  Logits of -Inf have q = 0;
- * rows with +Inf, NaN or nothing but -Inf have loss NaN.  T in [2^-20, 2^20]. */
+ * rows with +Inf, NaN or nothing but -Inf have loss NaN.  T in [2^-20, 2^20].
+ * Sums are fp32 up to T = 8: the loss is then off by a few T^2 * 2^-24, times 1 + the
+ * largest difference to the maximum that counts, over T.  Above, where it is a small difference of
+ * large terms, sums are 64 bits and only the result is rounded. */
 #define AMPQ_DISTILL_MAX_TOP 1024
 int ampq_distill_forward(int device, void *cuda_stream, int dtype, int teacher_dtype, int index_type, const void *logits, long long ld, long long rows,
                          long long cols, const void *indices, long long ld_indices, const void *teacher, long long ld_teacher, long long top,

@@ -4,24 +4,28 @@
 // With q = softmax(s / T) over a row of logits and p = softmax(t / T) over the
 // row's entries,
 //   loss = T^2 sum_k p_k (log p_k - log q_k)
-//        = T^2 (sum_k p_k ((t_k - tmax) - (s_k - m)) / T + log total - log sum_k e_k),
+//        = T^2 (sum_k p_k ((t_k - tmax) - (s_k - m)) / T + log(total / sum_k e_k)),
 // m = max s, total = sum_j exp((s_j - m) / T), e_k = exp((t_k - tmax) / T), p_k = e_k / sum e.
-// The forward pass reads the logits once, every thread with its own running maximum
-// and sum; the backward pass reads them once more and writes the gradient once.
+// The forward pass reads the logits once, every thread with its own running sum; the backward pass reads them once more and writes the gradient once.
 #include "ampq_decoder.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace ampq {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 // vectors that a thread has in flight, and CTAs that share an SM
-constexpr int kForwardAhead = 1, kForwardCtas = 8;
+constexpr int kForwardAhead = 1, kForwardCtas = 8, kHighCtas = 4;
 constexpr int kBackwardAhead = 1, kBackwardCtas = 6;
 constexpr int kPartVectors = 8 * kThreads;           // of the gradient's part of a row
 constexpr unsigned kPartColumns = 16 * kPartVectors;  // at most
 constexpr int kFewEntries = 128;  // 100: 333 us compared, 358 us with bits; 256: 530 and 369 us (4096 rows of 128000)
+// Above it the forward pass computes in 64 bits.  Rows of 1000, all listed, loss 0.12: in
+// fp32 off by up to 4e-7 at T = 1, 1.4e-5 at 8, in 64 bits by its last rounding at any T;
+// but 4096 x 128000 bf16 take 1177 us instead of 170.
+constexpr float kHighT = 8.0f;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
 // log2(e) / T in two parts.  Rounded to fp32 alone it is off by up to 2^-24 of itself,
@@ -125,6 +129,76 @@ struct Terms {
     }
 };
 
+// The same at high temperatures, in 64 bits.  There all exponentials are near 1 and the
+// loss is what is left of T^2 log(total): the sums are those of exp - 1, of `n` terms.
+struct HighFactor {
+    double inv_T;
+    float slack;
+    __device__ __forceinline__ double times(float s, float m) const { return ((double)s - (double)m) * inv_T; }
+};
+struct alignas(8) HighRunning {
+    double sum;
+    float m;
+    int n;
+    __device__ __forceinline__ double under(float to, const HighFactor& k) const {
+        if (m == to) return sum;
+        const double g = expm1(k.times(m, to));
+        return sum + (sum + (double)n) * g;
+    }
+    __device__ __forceinline__ static HighRunning join(const HighRunning* r, int n, const HighFactor& k) {
+        HighRunning all{0.0, r[0].m, 0};
+        for (int i = 1; i < n; ++i) all.m = fmaxf(all.m, r[i].m);
+        for (int i = 0; i < n; ++i) {
+            all.sum += r[i].under(all.m, k);
+            all.n += r[i].n;
+        }
+        return all;
+    }
+    __device__ __forceinline__ void join_warp(const HighFactor& k) {
+        float to = m;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, o));
+        sum = under(to, k);
+        m = to;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+        }
+    }
+};
+struct HighTerms {
+    double sum = 0.0;
+    float base = 0.0f, limit = -INFINITY, top = -INFINITY;
+    int n = 0;
+    __device__ __forceinline__ void raise(float to, const HighFactor& k) {
+        top = fmaxf(top, to);
+        if (to > limit) {
+            if (limit != -INFINITY) sum = HighRunning{sum, base, n}.under(to, k);  // all before were -Inf (or NaN): -1 under any
+            base = to;
+            limit = to + k.slack;
+        }
+    }
+    __device__ __forceinline__ void add(float s, const HighFactor& k) {
+        raise(s, k);
+        sum += expm1(k.times(s, base));
+        ++n;
+    }
+    template <int N>
+    __device__ __forceinline__ void add(const float2 (&v)[N], const HighFactor& k) {
+        float most = v[0].x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(v[i].x), "f"(v[i].y));
+        raise(most, k);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += expm1(k.times(v[i].x, base)) + expm1(k.times(v[i].y, base));
+        n += 2 * N;
+    }
+    __device__ __forceinline__ HighRunning under_top(const HighFactor& k) const {
+        return HighRunning{limit == -INFINITY ? sum : HighRunning{sum, base, n}.under(top, k), top, n};
+    }
+};
+
 __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
     return a;
@@ -182,8 +256,8 @@ __device__ __forceinline__ void store_vector(void* p, const unsigned (&w)[8]) {
 }
 
 // Sums over the CTA, in a fixed order; all threads call it.
-template <int N>
-__device__ __forceinline__ void block_sum(float (&s)[N], float (*red)[N]) {
+template <typename F, int N>
+__device__ __forceinline__ void block_sum(F (&s)[N], F (*red)[N]) {
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -194,7 +268,7 @@ __device__ __forceinline__ void block_sum(float (&s)[N], float (*red)[N]) {
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        s[n] = 0.0f;
+        s[n] = 0;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) s[n] += red[w][n];
     }
@@ -212,14 +286,21 @@ __device__ __forceinline__ unsigned cluster_rank() {
 // TB/s; its exponentials alone 120 us): the more warps the better, so one vector in
 // flight a thread and eight CTAs an SM (three vectors and four CTAs 184 us, where these
 // took 170).
-template <typename T>
-__global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel(const DistillArgs a) {
+template <typename T, bool HIGH>
+__global__ void __launch_bounds__(kThreads, HIGH ? kHighCtas : kForwardCtas) distill_forward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
+    using Sum = std::conditional_t<HIGH, HighRunning, Running>;
+    using F = std::conditional_t<HIGH, double, float>;
     __shared__ List list;
-    __shared__ Running s_warps[kWarps];
-    __shared__ Running s_parts[kMaxParts];
+    __shared__ Sum s_warps[kWarps];
+    __shared__ Sum s_parts[kMaxParts];
     __shared__ float s_top[kWarps];
-    __shared__ float s_sums[kWarps][2];
+    __shared__ F s_sums[kWarps][HIGH ? 3 : 2];
+    std::conditional_t<HIGH, HighFactor, Factor> factor;
+    if constexpr (HIGH)
+        factor = HighFactor{1.0 / (double)a.T, a.k.slack};
+    else
+        factor = a.k;
     const unsigned part = a.parts > 1 ? cluster_rank() : 0u;
     const long long row = a.parts > 1 ? blockIdx.x / (unsigned)a.parts : blockIdx.x;
     if (a.parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
@@ -246,8 +327,8 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
         return;
     }
     if (part == 0) list.gather(a, x, [](unsigned) { return true; });
-    Terms terms;
-    if (part == 0 && threadIdx.x < r.head + r.tail) terms.add(load_elem(x + r.edge(threadIdx.x)), a.k);
+    std::conditional_t<HIGH, HighTerms, Terms> terms;
+    if (part == 0 && threadIdx.x < r.head + r.tail) terms.add(load_elem(x + r.edge(threadIdx.x)), factor);
     for (; v < end; v += kForwardAhead * kThreads) {
 #pragma unroll
         for (int u = 0; u < kForwardAhead; ++u)
@@ -256,40 +337,63 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) distill_forward_kernel
                 k.from_words(w[u]);
                 const unsigned next = v + (kForwardAhead + u) * kThreads;
                 if (next < end) load_vector(body + (size_t)next * K::kElems, w[u]);
-                terms.add(k.v, a.k);
+                terms.add(k.v, factor);
             }
     }
-    Running run = terms.under_top(a.k);
-    run.join_warp(a.k);
+    Sum run = terms.under_top(factor);
+    run.join_warp(factor);
     if (threadIdx.x % 32 == 0) s_warps[threadIdx.x / 32] = run;
     __syncthreads();
-    run = Running::join(s_warps, kWarps, a.k);
+    run = Sum::join(s_warps, kWarps, factor);
     if (a.parts > 1) {
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // the first CTA has begun
         if (threadIdx.x == 0) {
-            static_assert(alignof(Running) == 8 && sizeof(Running) == 8, "the store below");
+            static_assert(alignof(Sum) == 8 && sizeof(Sum) % 8 == 0, "the stores below");
             unsigned at = (unsigned)__cvta_generic_to_shared(&s_parts[part]), there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(at));
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(run.m), "f"(run.sum) : "memory");
+            unsigned long long words[sizeof(Sum) / 8];
+            memcpy(words, &run, sizeof(Sum));
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(Sum) / 8; ++i)
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there + 8 * i), "l"(words[i]) : "memory");
         }
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         if (part != 0) return;
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        run = Running::join(s_parts, a.parts, a.k);
+        run = Sum::join(s_parts, a.parts, factor);
     }
     const float tmax = list.largest(a, s_top);
-    float sums[2] = {0.0f, 0.0f};
-    for (int k = threadIdx.x; k < a.top; k += kThreads)
-        if (list.index[k] != kNone) {
-            const float e = expf((list.t[k] - tmax) * a.inv_T);
-            sums[0] += e;
-            if (e > 0.0f) sums[1] += e * (((list.t[k] - tmax) - (list.s[k] - run.m)) * a.inv_T);  // p log(p / q) is 0 where p is
+    if constexpr (HIGH) {
+        // with A and B the sums of exponentials of the list and of the row: sum p log(p / q) = sum p (a - b) + log(B / A)
+        double sums[3] = {0.0, 0.0, 0.0};  // of exp(a) - 1, of exp(a) (a - b), entries
+        for (int k = threadIdx.x; k < a.top; k += kThreads)
+            if (list.index[k] != kNone) {
+                const double d = factor.times(list.t[k], tmax), e = exp(d);
+                sums[0] += expm1(d);
+                if (e > 0.0) sums[1] += e * (d - factor.times(list.s[k], run.m));
+                sums[2] += 1.0;
+            }
+        block_sum(sums, s_sums);
+        if (threadIdx.x == 0) {
+            const double listed = sums[2] + sums[0], more = ((double)a.cols - sums[2]) + (run.sum - sums[0]);
+            a.loss[row] = (float)((double)a.T * (double)a.T * (sums[1] / listed + log1p(more / listed)));
+            a.stats[2 * row] = run.m;
+            a.stats[2 * row + 1] = (float)((double)a.cols + run.sum);
         }
-    block_sum(sums, s_sums);
-    if (threadIdx.x == 0) {
-        a.loss[row] = a.T * a.T * (sums[1] / sums[0] + (logf(run.sum) - logf(sums[0])));
-        a.stats[2 * row] = run.m;
-        a.stats[2 * row + 1] = run.sum;
+    } else {
+        float sums[2] = {0.0f, 0.0f};
+        for (int k = threadIdx.x; k < a.top; k += kThreads)
+            if (list.index[k] != kNone) {
+                const float e = expf((list.t[k] - tmax) * a.inv_T);
+                sums[0] += e;
+                if (e > 0.0f) sums[1] += e * (((list.t[k] - tmax) - (list.s[k] - run.m)) * a.inv_T);  // p log(p / q) is 0 where p is
+            }
+        block_sum(sums, s_sums);
+        if (threadIdx.x == 0) {
+            a.loss[row] = a.T * a.T * (sums[1] / sums[0] + logf(run.sum / sums[0]));  // the logarithms' difference would lose more of it
+            a.stats[2 * row] = run.m;
+            a.stats[2 * row + 1] = run.sum;
+        }
     }
 }
 
@@ -440,7 +544,7 @@ DistillArgs distill_args(int teacher_dtype, int index_type, const void* logits, 
     return a;
 }
 
-template <typename T>
+template <typename T, bool HIGH>
 int launch_forward(DistillArgs a, int sms, cudaStream_t st) {
     // few rows are shared out while that gives every SM up to four CTAs, a part having two vectors a thread at least
     const long long vectors = (long long)a.cols / Row<T>::E;
@@ -456,7 +560,7 @@ int launch_forward(DistillArgs a, int sms, cudaStream_t st) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.parts > 1 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, distill_forward_kernel<T>, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, distill_forward_kernel<T, HIGH>, a) != cudaSuccess) {
         cudaGetLastError();
         return AMPQ_ERR_CUDA;
     }
@@ -498,7 +602,8 @@ int ampq_distill_forward(int device, void* cuda_stream, int dtype, int teacher_d
     DistillArgs a = distill_args(teacher_dtype, index_type, logits, ld, rows, cols, indices, ld_indices, teacher, ld_teacher, top, temperature);
     a.loss = loss; a.stats = stats;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    return dtype == AMPQ_F32 ? launch_forward<float>(a, sms, st) : launch_forward<__nv_bfloat16>(a, sms, st);
+    if (temperature > kHighT) return dtype == AMPQ_F32 ? launch_forward<float, true>(a, sms, st) : launch_forward<__nv_bfloat16, true>(a, sms, st);
+    return dtype == AMPQ_F32 ? launch_forward<float, false>(a, sms, st) : launch_forward<__nv_bfloat16, false>(a, sms, st);
 }
 
 int ampq_distill_backward(int device, void* cuda_stream, int dtype, int teacher_dtype, int index_type, const float* gl, long long gl_stride,
