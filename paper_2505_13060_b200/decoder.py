@@ -143,11 +143,13 @@ def _rotation(cos, sin, positions, batch: int, tokens: int, device: int, leading
     index, shape = _index_code(positions), positions.shape
     if len(shape) == 1 and shape[0] == tokens:
         stride = 0
-    elif shape == (*leading, tokens):
-        positions = positions if len(shape) == 2 else positions.reshape(batch, tokens)
+    elif shape[-1:] == (tokens,) and len(shape) <= len(leading) + 1 and all(a in (1, b) for a, b in zip(reversed(shape[:-1]), reversed(leading))):
+        if shape != (*leading, tokens):
+            positions = positions.expand(*leading, tokens)
+        positions = positions if len(leading) == 1 else positions.reshape(batch, tokens)
         stride = positions.stride(0) if batch > 1 else 0
     else:
-        raise ValueError("positions are [%d] or %s, got %s" % (tokens, (*leading, tokens), tuple(shape)))
+        raise ValueError("positions are [%d] or as many as %s, got %s" % (tokens, (*leading, tokens), tuple(shape)))
     if tokens > 1 and positions.stride(-1) != 1:
         positions = positions.contiguous()
         stride = tokens if positions.dim() == 2 else 0
@@ -187,7 +189,8 @@ def head_norm_forward(q: torch.Tensor, k, wq=None, wk=None, cos=None, sin=None, 
     """RMS norm of each head of q [..., tokens, heads, columns] and of k [..., tokens, key heads, columns] (or None), with the
     weights wq and wk [columns] that their heads share (None for ones), and the rotation of the first ``2 * cos.shape[1]``
     columns by the angles of the tokens' positions: row ``positions[..., t]`` of the tables cos and sin
-    (``rotary_table``), row t without positions, no rotation without tables.  Pairs are (i, i + half) or, ``interleaved``, (2 i, 2 i + 1).
+    (``rotary_table``), row t without positions, no rotation without tables.  Positions are [tokens] or [..., tokens],
+    where dimensions of 1 hold for all of a batch.  Pairs are (i, i + half) or, ``interleaved``, (2 i, 2 i + 1).
 
     Returns (yq, yk, rq, rk, pq, pk): the outputs, the reciprocals [..., tokens, heads] of the root mean squares, and the
     checkpoints of q and k (a row for each head) or None for ``FMT_BASE``."""

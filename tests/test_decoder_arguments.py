@@ -1,0 +1,42 @@
+"""Arguments of the decoder's operators that are looked at before anything runs: nothing here needs a GPU."""
+import pytest
+import torch
+
+
+@pytest.fixture
+def dec(ampq, monkeypatch):
+    from paper_2505_13060_b200 import decoder
+
+    monkeypatch.setattr(decoder, "_same_device", lambda *a: None)
+    return decoder
+
+
+def rows_of(dec, positions, leading, tokens):
+    """The positions [batch, tokens] that the kernel would read."""
+    batch = 1
+    for d in leading:
+        batch *= d
+    cos, sin = dec.rotary_table(50, 8, device="cpu")
+    turn, held = dec._rotation(cos, sin, positions, batch, tokens, 0, torch.Size(leading))
+    p, stride = held[2], turn[6]
+    assert turn[4] == p.data_ptr()
+    return torch.as_strided(p, (batch, tokens), (stride, 1), p.storage_offset())
+
+
+@pytest.mark.parametrize("shape,leading", [((7,), (3,)), ((3, 7), (3,)), ((1, 7), (3,)), ((1, 7), (1,)), ((7,), ()), ((2, 3, 7), (2, 3)), ((1, 3, 7), (2, 3)),
+                                           ((2, 1, 7), (2, 3)), ((1, 1, 7), (2, 3)), ((3, 7), (2, 3)), ((1, 7), (2, 3)), ((1, 7), (0,)), ((2, 3, 1), (2, 3)), ((1, 1), (4,))])
+def test_positions_of_a_batch(dec, shape, leading):
+    """Positions that hold for several of a batch, as models hand them on: [1, tokens] for a batch of any size."""
+    tokens = shape[-1]
+    p = torch.randint(0, 50, shape, generator=torch.Generator().manual_seed(0))
+    want = p.expand(*leading, tokens).reshape(-1, tokens)
+    assert torch.equal(rows_of(dec, p, leading, tokens), want)
+    wide = torch.zeros(*shape[:-1], 2 * tokens, dtype=torch.int64)
+    wide[..., ::2] = p
+    assert torch.equal(rows_of(dec, wide[..., ::2], leading, tokens), want)
+
+
+@pytest.mark.parametrize("shape,leading", [((2, 7), (3,)), ((1, 1, 7), (3,)), ((3, 1), (3,)), ((6,), (3,)), ((), (3,)), ((3, 2, 7), (2, 3)), ((2, 7), (2, 3)), ((1, 7), ())])
+def test_positions_that_are_not_those_of_the_tokens(dec, shape, leading):
+    with pytest.raises(ValueError, match="positions"):
+        rows_of(dec, torch.zeros(shape, dtype=torch.int64), leading, 7)
