@@ -413,13 +413,15 @@ def head_norm(q: torch.Tensor, k=None, wq=None, wk=None, cos=None, sin=None, pos
               fmt: int = ampq.FMT_E4M3):
     """The outputs (yq, yk) of ``head_norm_forward``, differentiable; q and k are kept for the backward pass in 8 bits, or
     in full with ``FMT_BASE``."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (cos, sin)):
+        raise ValueError("the angles are a constant here: detach them")
     keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk))
     return _HeadNorm.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, fmt if keep else ampq.FMT_BASE)
 
 
 def distill_loss(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0) -> torch.Tensor:
     """The losses [...] of ``distill_forward``, differentiable in the logits.  The teacher is a constant."""
-    if teacher.requires_grad:
+    if torch.is_grad_enabled() and teacher.requires_grad:
         raise ValueError("the teacher's logits are a constant here: detach them")
     return _DistillLoss.apply(logits, indices, teacher, temperature)
 

@@ -40,3 +40,15 @@ def test_positions_of_a_batch(dec, shape, leading):
 def test_positions_that_are_not_those_of_the_tokens(dec, shape, leading):
     with pytest.raises(ValueError, match="positions"):
         rows_of(dec, torch.zeros(shape, dtype=torch.int64), leading, 7)
+
+
+def test_constants_that_want_a_gradient(dec):
+    """Refused where their gradient would be dropped without a word, and only there."""
+    x, cos, sin = torch.zeros(3, 2, 8), *dec.rotary_table(3, 8, device="cpu")
+    lists = torch.zeros(9, 2, dtype=torch.int64), torch.zeros(9, 2, requires_grad=True)
+    for call in (lambda: dec.head_norm(x, None, None, None, cos.requires_grad_(), sin.detach()), lambda: dec.head_norm(x, None, None, None, cos.detach(), sin.requires_grad_()),
+                 lambda: dec.distill_loss(torch.zeros(9, 40), *lists)):
+        with pytest.raises(ValueError, match="constant"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):   # what is wrong then is only that there is no GPU
+            call()
