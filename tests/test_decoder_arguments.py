@@ -52,3 +52,21 @@ def test_constants_that_want_a_gradient(dec):
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):   # what is wrong then is only that there is no GPU
             call()
+
+
+def test_one_layout_of_the_heads(dec, ampq):
+    """What a call packs is the structure field by field."""
+    import ctypes as C
+
+    from paper_2505_13060_b200.checkpoint import Packed
+
+    out, x, gy = torch.zeros(2, 3, 4, 8), torch.zeros(2, 3, 6, 8)[:, :, :4], torch.zeros(2, 4, 3, 8).transpose(1, 2)
+    rstd, w, gw = torch.zeros(2, 3, 4), torch.zeros(8), torch.zeros(8)
+    p = object.__new__(Packed)
+    p.codes, p.scales = torch.zeros(24, 32, dtype=torch.uint8), torch.zeros(24, 1, dtype=torch.uint8)
+    want = ampq.Heads(heads=4, x=x.data_ptr(), x_batch=144, x_token=48, x_head=8, gy=gy.data_ptr(), gy_batch=96, gy_token=8, gy_head=24, out=out.data_ptr(), out_batch=96,
+                      out_token=32, out_head=8, weight=w.data_ptr(), gweight=gw.data_ptr(), rstd=rstd.data_ptr(), codes=p.codes.data_ptr(), ld_codes=32,
+                      scales=p.scales.data_ptr(), ld_scales=1)
+    assert dec._side(out, rstd, w, x=x, gy=gy, gw=gw, kept=p) == bytes(want)
+    none = ampq.Heads(heads=4, out=out.data_ptr(), out_batch=96, out_token=32, out_head=8, rstd=rstd.data_ptr())
+    assert dec._side(out, rstd, None) == bytes(none) and C.sizeof(none) == 8 * len(none._fields_)
