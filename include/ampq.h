@@ -588,7 +588,11 @@ int ampq_distill_forward(int device, void *cuda_stream, int dtype, int teacher_d
 
 /* Its gradient: gs[n][j] = gl[n * gl_stride] * T * (q_j - sum of p_k over the k with
  * indices[n][k] = j), 0 in rows without entries; stats as the forward pass left them
- * (gl_stride 0: one number for all rows). */
+ * (gl_stride 0: one number for all rows).  q and p are fp32, each off by a few 2^-24 of
+ * itself: at high T, where they nearly cancel, that is a few T * 2^-24 of the difference that is left.
+ * q below 2^-126 is 0.  Where p has no number (an index of cols or more, a teacher's logit of NaN
+ * or +Inf) the row's listed columns are NaN; its other columns have q_j alone, as
+ * the formula says. */
 int ampq_distill_backward(int device, void *cuda_stream, int dtype, int teacher_dtype, int index_type, const float *gl, long long gl_stride,
                           const void *logits, long long ld, long long rows, long long cols, const void *indices, long long ld_indices, const void *teacher,
                           long long ld_teacher, long long top, const float *stats, float temperature, void *gs, long long ld_gs);

@@ -6,7 +6,8 @@
 //   loss = T^2 sum_k p_k (log p_k - log q_k)
 //        = T^2 (sum_k p_k ((t_k - tmax) - (s_k - m)) / T + log(total / sum_k e_k)),
 // m = max s, total = sum_j exp((s_j - m) / T), e_k = exp((t_k - tmax) / T), p_k = e_k / sum e.
-// The forward pass reads the logits once, every thread with its own running sum; the backward pass reads them once more and writes the gradient once.
+// The forward pass reads the logits once, every thread with its own running sum; the
+// backward pass reads them once more and writes the gradient once.
 #include "ampq_decoder.h"
 
 #include <cmath>
@@ -283,9 +284,10 @@ __device__ __forceinline__ unsigned cluster_rank() {
 // A row to a CTA, or to a cluster of `parts` CTAs where there are few rows; the parts'
 // maxima and sums meet in the first CTA's shared memory.  Bound by HBM, with the
 // exponentials' pipe close behind (4096 x 128000 bf16 170 to 182 us by board, 5.5 to 5.9
-// TB/s; its exponentials alone 120 us): the more warps the better, so one vector in
-// flight a thread and eight CTAs an SM (three vectors and four CTAs 184 us, where these
-// took 170).
+// TB/s; its exponentials alone 120 us; 2048 x 128000 fp32 153 us, 6.5 TB/s): the more warps
+// the better, so one vector in flight a thread and eight CTAs an SM (three vectors and
+// four CTAs 184 us, where these took 170; with six CTAs fp32 took 175).  The bf16 kernel
+// spills 20 bytes behind its stream.  HIGH computes in 64 bits, bound by these (1177 us).
 template <typename T, bool HIGH>
 __global__ void __launch_bounds__(kThreads, HIGH ? kHighCtas : kForwardCtas) distill_forward_kernel(const DistillArgs a) {
     using K = Chunk<T>;
@@ -405,6 +407,8 @@ __global__ void __launch_bounds__(kThreads, HIGH ? kHighCtas : kForwardCtas) dis
 // entries are compared with each other.  Of MANY each leaves a bit for its column, and
 // who finds it there sets one that says so: compared with each other a thousand took
 // 15 times the rest of the kernel, but the bits cost a short list 5 % of it.
+// (With the bits the kernels spill up to 48 bytes at six CTAs an SM.  Lists of 64, 256 and
+// 1000 at six and five: 323, 370 and 491 us; 340, 353 and 485 us.)
 template <typename T, bool MANY>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas) distill_backward_kernel(const DistillArgs a) {
     using K = Chunk<T>;

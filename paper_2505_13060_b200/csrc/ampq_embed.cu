@@ -425,7 +425,8 @@ __device__ __forceinline__ bool last_to_come(unsigned* counter, unsigned all) {
 // began before it, its second for one that begins in it.  The last of the run's pieces
 // to come (a warp of 32 chunks to a piece) adds them up in order.  Long runs are added
 // up in groups of about the root of their pieces first, by the last of each group, and
-// then the groups' sums by the last of these: 512 pieces took 90 us in one row.
+// then the groups' sums by the last of these: 512 pieces took 90 us in one row.  One run in rows
+// of 4096 bf16, the whole gradient at once and in groups: 8 pieces 12.6 and 13.3 us, 16 pieces 17.3 and 15.0 us.
 constexpr unsigned kOneGroup = 8;
 
 template <typename T, bool STRIDED>
@@ -585,7 +586,9 @@ int check_embed(int dtype, int index_type, const void* tokens, long long n, long
     return AMPQ_OK;
 }
 
-// From so many slabs of rows on a thread takes two chunks.
+// From so many slabs of rows on a thread takes two chunks.  Rows of 8192 bf16, one chunk and
+// two: 512 tokens (1024 slabs) 3.4 and 3.6 us, 1024 tokens 5.2 and 4.8, 2048 tokens 9.4 and 8.7, 4096 tokens 19.5
+// and 16.8, 8192 tokens 37.3 and 36.3.
 constexpr long long kManyBlocks = 4096;
 
 template <typename T>

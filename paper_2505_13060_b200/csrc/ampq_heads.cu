@@ -22,18 +22,23 @@ namespace {
 constexpr int kHeadCols = AMPQ_HEAD_MAX_COLS;
 // Threads of a CTA, CTAs that share an SM, and the steps that a warp works on together.
 // The shuffles, the root and the loads of a step are a chain of latencies: two steps
-// side by side fill it better than more warps would, and a spilled register costs more
-// than either brings.  Measured on 2 x 4096 tokens of 64 + 8 heads of 128 columns (one
+// side by side fill it better than more warps would.  Measured on 2 x 4096 tokens of 64 + 8 heads of 128 columns (one
 // step at a time, the same with six CTAs an SM, two together): forward bf16 with a
 // checkpoint 74, 80 and 68 us, without 59, 58 and 53 us, fp32 125, 129 and 111 us.
 // Backward (one step, two): fp32 124 and 115 us, but bf16, whose sums and factors
-// leave no room, from 8 bits 78 and 119 us, from the input 80 and 110 us.
+// leave no room, from 8 bits 78 and 119 us, from the input 80 and 110 us.  Three CTAs an
+// SM instead of four: forward bf16 74 and 59 us, fp32 126 us, backward 85 us and fp32
+// 127 us.  At four the bf16 backward kernels of neighbouring pairs that read a checkpoint
+// spill 32 to 56 bytes and are no slower for it (84 us, at three 85).  Most backward
+// kernels with vectors of two elements spill at three (up to 80 bytes); not tried with two.
 constexpr int kForwardThreads = 128, kBackwardThreads = 128, kMostCtas = 4, kForwardTogether = 2;
 template <int V>
 constexpr int kCtas = V >= 4 ? kMostCtas : 3;  // small vectors come through registers
 template <typename T>
 constexpr int kBackwardTogether = sizeof(T) == 4 ? 2 : 1;
-constexpr int kMaxRun = 4;  // steps of a run
+// Steps of a run.  The same size, runs of 1, 2, 4 and 8: forward bf16 with a checkpoint 121,
+// 80, 69 and 70 us, fp32 197, 134, 112 and 132, backward from 8 bits 106, 87, 79 and 78, fp32 180, 127, 116 and 129.
+constexpr int kMaxRun = 4;
 
 struct Side {  // queries or keys
     const void *x, *gy, *w;
@@ -1016,8 +1021,8 @@ long long lay_out(HeadArgs& a, int V, int NV, bool next, bool backward, int warp
         if (grid < total / warps) grid = total / warps;
     }
     // The CTAs go to the sides by their work, one warp to a run at least.  What a run does
-    // once for a token is about two steps' work, and steps are done `together`.  (Shared out
-    // by steps alone the keys' CTAs of 64 + 8 heads came last: 76 us instead of 68.)
+    // once for a token is about two steps' work, and steps are done `together`.  (64 + 8 heads,
+    // forward and backward: counted as none, the keys' CTAs came last, 76 and 84 us; as one, two or four steps 68 and 79.)
     const long long least[2] = {(a.runs[0] + warps - 1) / warps, (a.runs[1] + warps - 1) / warps};
     long long work[2];
     for (int s = 0; s < 2; ++s) work[s] = (long long)a.runs[s] * (kTokenWork + (a.run[s] + together - 1) / together * together);

@@ -331,7 +331,8 @@ def distill_forward(logits: torch.Tensor, indices: torch.Tensor, teacher: torch.
 
 
 def distill_backward(gl: torch.Tensor, logits: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, stats: torch.Tensor, temperature: float = 1.0):
-    """Gradient of the logits from that of the losses, gl [...] (a number expanded to the rows is read in place)."""
+    """Gradient of the logits from that of the losses, gl [...] (a number expanded to the rows is read in place).  Where a
+    list names a column that is none, its other columns are NaN, and what is not listed has the first term alone."""
     s, i, t, device, codes = _lists(logits, indices, teacher)
     if gl.shape != logits.shape[:-1] or stats.shape != (*logits.shape[:-1], 2):
         raise ValueError("a gradient and statistics for each row: logits %s, gl %s, stats %s" % (tuple(logits.shape), tuple(gl.shape), tuple(stats.shape)))
@@ -411,7 +412,8 @@ def embedding(tokens: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, pa
 def head_norm(q: torch.Tensor, k=None, wq=None, wk=None, cos=None, sin=None, positions=None, eps: float = 1e-5, interleaved: bool = False,
               fmt: int = ampq.FMT_E4M3):
     """The outputs (yq, yk) of ``head_norm_forward``, differentiable; q and k are kept for the backward pass in 8 bits, or
-    in full with ``FMT_BASE``."""
+    in full with ``FMT_BASE``.  The default is that of ``checkpoint.linear`` and the norms there: the gradients are those of
+    the decoded inputs.  (The module ``HeadNorm`` keeps them in full by default.)  cos and sin are constants."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (cos, sin)):
         raise ValueError("the angles are a constant here: detach them")
     keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk))
@@ -443,8 +445,8 @@ class ScaledEmbedding(torch.nn.Embedding):
 
 class HeadNorm(torch.nn.Module):
     """Norms of queries and keys for each head with the position rotation, between the layers that make them and their
-    product.  Its inputs are kept in full for the backward pass, in 8 bits in a calibration with checkpoints
-    (``hooks.Calibrator``)."""
+    product.  Its inputs are kept in full for the backward pass unless ``fmt`` names a format, unlike ``head_norm``'s, which
+    are kept in E4M3 by default; in a calibration with checkpoints (``hooks.Calibrator``) they are in its format."""
 
     def __init__(self, cols: int, eps: float = 1e-5, interleaved: bool = False, device=None, dtype=None):
         super().__init__()
