@@ -293,6 +293,8 @@ class Calibrator:
         """x rounded to format ``fmt``, in the order of torch's current stream: the context's waits for what made x, and
         torch's for the result, so neither tensor has to be held."""
         x = x.detach().contiguous()
+        if self._device_of(x) != self.ctx.device:   # its address means nothing to the context
+            raise ValueError("a tensor on %s for a context on cuda:%d" % (x.device, self.ctx.device))
         out = torch.empty_like(x)
         if not self._same_stream():
             torch.cuda.ExternalStream(self.ctx.stream).wait_stream(torch.cuda.current_stream())
@@ -300,6 +302,10 @@ class Calibrator:
         if not self._same_stream():
             torch.cuda.current_stream().wait_stream(torch.cuda.ExternalStream(self.ctx.stream))
         return out
+
+    @staticmethod
+    def _device_of(x) -> int:
+        return x.device.index if x.is_cuda else -1
 
     @contextlib.contextmanager
     def quantised(self, fmt_of_layer, amax_x=None):

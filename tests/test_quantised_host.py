@@ -23,7 +23,7 @@ class Context:
     """Rounds fp32 values to multiples of 2^-fmt; -1 is a format that it does not list."""
 
     def __init__(self, log, stream):
-        self.log, self.stream, self.layers = log, stream, 0
+        self.log, self.stream, self.layers, self.device = log, stream, 0, 0
 
     def register_layer(self, kind, name, R):
         self.layers += 1
@@ -49,6 +49,7 @@ def setup(monkeypatch):
 
     log = []
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream(log, "torch", 7))
+    monkeypatch.setattr(hooks.Calibrator, "_device_of", staticmethod(lambda x: x.device.index or 0), raising=False)
     monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, *a: Stream(log, "context", handle))
     return lambda model, stream=7: hooks.Calibrator(Context(log, stream), model, 1), log
 
@@ -175,3 +176,20 @@ def test_divergence_refuses_before_the_second_pass(setup, monkeypatch):
         assert len(calls) == 1
     assert not net._forward_pre_hooks
     assert decoder.list_length(torch.zeros(2, 301), 5000) == 301   # of all there are
+
+
+def test_tensors_that_are_not_on_the_contexts_device(setup, monkeypatch):
+    """Their addresses never reach the context: a model on the host, or on another GPU."""
+    from paper_2505_13060_b200 import hooks
+
+    make, log = setup
+    net = torch.nn.Linear(4, 4)
+    before = net.weight.detach().clone()
+    for where in (-1, 1):
+        monkeypatch.setattr(hooks.Calibrator, "_device_of", staticmethod(lambda x: where))
+        with pytest.raises(ValueError, match="context on cuda:0"):
+            with make(net).quantised([1]):
+                pass
+    assert not log.count("round") and torch.equal(net.weight, before)
+    monkeypatch.undo()
+    assert hooks.Calibrator._device_of(net.weight) == -1
