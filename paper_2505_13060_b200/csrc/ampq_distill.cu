@@ -283,7 +283,7 @@ __device__ __forceinline__ unsigned cluster_rank() {
 
 // A row to a CTA, or to a cluster of `parts` CTAs where there are few rows; the parts'
 // maxima and sums meet in the first CTA's shared memory.  Bound by HBM, with the
-// exponentials' pipe close behind (4096 x 128000 bf16 170 to 182 us by board, 5.5 to 5.9
+// exponentials' pipe close behind (4096 x 128000 bf16 167 to 184 us by board, 5.4 to 6.0
 // TB/s; its exponentials alone 120 us; 2048 x 128000 fp32 153 us, 6.5 TB/s): the more warps
 // the better, so one vector in flight a thread and eight CTAs an SM (three vectors and
 // four CTAs 184 us, where these took 170; with six CTAs fp32 took 175).  The bf16 kernel
